@@ -219,6 +219,9 @@ def _routing_tables(c):
 def _router(st, c):
     """The package's routing context: the handle that a serving program keeps."""
     from paper_2602_21140_b200 import binding as B
+    if c["op"] == "experts":
+        cfg = B.make_config(c["E"], c["k"], c["H"], c["T"], 1, c["P"], 2)
+        return B.MoeRouter(cfg, [p if p < c["E"] else -1 for p in range(c["P"])], None, [1.0] * c["P"])
     cfg = B.make_config(c["E"], c["k"], c["H"], c["T"], c["R"], c["S"], 2, int(c["sigmoid"]), c["n_group"], c["topk_group"])
     r = B.MoeRouter(cfg, st["s2e"], st["bias"].cpu().numpy() if c["sigmoid"] else None, st["slot_scale"].cpu().numpy())
     if c["failed"] >= 0:
@@ -246,6 +249,8 @@ def prepare(case, seed):
         # row 2i of the first projection is the gate of feature i, row 2i + 1 its up-projection
         st["gate_up"] = _mx_weights(c["P"], 2 * c["I"], H, seed, 4)
         st["down"] = _mx_weights(c["P"], H, c["I"], seed, 5)
+        if own:
+            st["router"] = _router(st, c)
         return st
     st["logits"] = logits
     st["s2e"], st["live"], st["n_live"] = _routing_tables(c)
@@ -334,9 +339,9 @@ def _own(st):
     op = st["case"]["op"]
     if op == "quantize":
         return B.mx_dequantize(B.mx_quantize(st["x"]))
-    if op == "experts":
-        return B.mx_expert_ffn(B.MxRows(*st["rows"]), st["counts"], st["offsets"], B.MxRows(*st["gate_up"]), B.MxRows(*st["down"]))
     r = st["router"]
+    if op == "experts":
+        return r.mx_expert_ffn(B.MxRows(*st["rows"]), st["counts"], st["offsets"], B.MxRows(*st["gate_up"]), B.MxRows(*st["down"]))
     if op == "dispatch":
         out, rows = r.mx_dispatch(st["logits"], st["x"], st["out"])
         return {"topk_weights": out.topk_weights, "rows": B.mx_dequantize(rows), **{f: getattr(out, f) for f in INDICES}}
