@@ -296,6 +296,112 @@ moe_status moe_ep_plan_host(const int32_t *counts_all, int32_t world, int32_t ra
                             int32_t *src_base, int32_t *recv_slot_offsets);
 
 /*
+ * ---- 4-bit rows: quantisation, dispatch and the experts' products ------------------
+ * (No counterpart in the paper.)  Holding the experts in 4 bits quarters the memory and the
+ * traffic of their weights, so that the ranks that survive a failure have room for more replicas.
+ *
+ * Format (microscaled 4-bit floating point): a row of `cols` elements, cols % 32 == 0, is
+ *   codes  [cols/2] u8: two elements per byte, the even one in the low half.  A code is a sign, two
+ *          exponent bits and one mantissa bit: +-{0, 0.5, 1, 1.5, 2, 3, 4, 6}.
+ *   scales [moe_mx_scale_pitch(cols)] u8: one per 32 elements, s stands for 2^(s - 127), 255 for NaN.
+ *          The pitch is cols/32 rounded up to 16; the padding is never interpreted.
+ * A block's scale is clamp(floor(log2 max|x|) - 2 + 127, 0, 254), 0 for a block of zeros and 255 for a
+ * block with a NaN or an infinity (the whole block then stands for NaN); elements are rounded to the
+ * nearest code, ties to even, and magnitudes beyond 6 to 6.  Codes and scales are separate,
+ * contiguous row-major arrays, 16-byte aligned.
+ */
+enum { MOE_DTYPE_BF16 = 0, MOE_DTYPE_F16 = 1, MOE_DTYPE_F32 = 2 };
+
+/* Bytes of a row of scales; 0 if cols is not a positive multiple of 32. */
+int32_t moe_mx_scale_pitch(int32_t cols);
+
+/*
+ * moe_mx_quantize — rows to 4 bits.  No context: any rows on the current device, activations or
+ * weights ([experts, features, cols] flattened to rows).
+ *   x device [rows, cols] of `dtype`, `row_stride` elements from row to row (>= cols, rows 16-byte
+ *     aligned); codes, scales device out, as above (the padding of the scales is written as 0)
+ * rows = 0 succeeds and launches nothing.  CAPACITY beyond 2^40 elements.  Allocates nothing, does not wait.
+ */
+moe_status moe_mx_quantize(const void *x, int32_t dtype, int64_t rows, int32_t cols, int64_t row_stride,
+                           uint8_t *codes, uint8_t *scales, void *cuda_stream);
+
+/*
+ * moe_mx_dequantize — the values that 4-bit rows stand for: y device out [rows, cols] of `dtype`.
+ * Exact in f32 and bf16 unless a value leaves the type's range (scales 253 and 254), rounded once in f16.
+ */
+moe_status moe_mx_dequantize(const uint8_t *codes, const uint8_t *scales, int64_t rows, int32_t cols, void *y,
+                             int32_t dtype, int64_t row_stride, void *cuda_stream);
+
+/*
+ * moe_mx_dispatch — moe_dispatch with a send buffer of 4-bit rows: the same routing and permutation;
+ * each token's row is quantised once and its codes and scales are written to its k rows.
+ *   out->send_buf is not used and may be NULL
+ *   send_codes device out [T*k, H/2], send_scales device out [T*k, moe_mx_scale_pitch(H)]
+ * INVALID_ARG if H % 32 != 0, otherwise as moe_dispatch.  moe_combine and the gradients may follow it.
+ */
+moe_status moe_mx_dispatch(moe_ctx *ctx, const float *logits, const void *x, int32_t T,
+                           const moe_dispatch_out *out, uint8_t *send_codes, uint8_t *send_scales,
+                           void *cuda_stream);
+
+/*
+ * moe_mx_expert_product — every slot's matrix on the rows of its segment (Sec. 2.1, the experts):
+ *   y[r, f] = bf16( sum_c a[r, c] * w[p, f, c] )   for slot_offsets[p] <= r < slot_offsets[p] + slot_counts[p]
+ * fp32 accumulation, one rounding.  Rows outside every segment are left as they are.
+ *   a_codes, a_scales device: `rows` 4-bit rows of n_in elements (a dispatch's send buffer)
+ *   slot_counts, slot_offsets device [P] (of a dispatch; a longer slot_offsets is fine).  Segments are
+ *     cut at `rows`; segments must not overlap.
+ *   w_codes, w_scales device [P, n_out] 4-bit rows of n_in elements, P slots of this context
+ *   y device out [rows, n_out] bf16, 16-byte aligned
+ * n_in % 32 == 0, n_out % 8 == 0, rows <= 2^30.  rows = 0 launches nothing.  Allocates nothing, does not wait;
+ * a bounded wait that gives up sets the context's device status.
+ */
+moe_status moe_mx_expert_product(moe_ctx *ctx, const uint8_t *a_codes, const uint8_t *a_scales, int64_t rows,
+                                 const int32_t *slot_counts, const int32_t *slot_offsets,
+                                 const uint8_t *w_codes, const uint8_t *w_scales, int32_t n_out, int32_t n_in,
+                                 void *y, void *cuda_stream);
+
+/*
+ * moe_mx_expert_gated — first half of a gated feed-forward expert, 4 bits in and out:
+ *   h[r, i] = silu(a[r, :] . w[p, 2i, :]) * (a[r, :] . w[p, 2i + 1, :]),  silu(g) = g / (1 + exp(-g))
+ * in fp32, then quantised.  Row 2i of a slot's matrix is the gate of feature i, row 2i + 1 its
+ * up-projection.
+ *   w_codes, w_scales device [P, 2 * n_hidden] 4-bit rows of n_in elements
+ *   h_codes, h_scales device out: `rows` 4-bit rows of n_hidden elements (the padding of the scales is not written)
+ * n_hidden % 32 == 0; otherwise as moe_mx_expert_product, which takes h to the expert's output.
+ */
+moe_status moe_mx_expert_gated(moe_ctx *ctx, const uint8_t *a_codes, const uint8_t *a_scales, int64_t rows,
+                               const int32_t *slot_counts, const int32_t *slot_offsets,
+                               const uint8_t *w_codes, const uint8_t *w_scales, int32_t n_hidden, int32_t n_in,
+                               uint8_t *h_codes, uint8_t *h_scales, void *cuda_stream);
+
+/*
+ * ---- Gradients of the routed step ---------------------------------------------------
+ * (No counterpart in the paper.)  For tuning the router and the experts that are left after a
+ * failure.  Both use the topk_*, dst_row buffers of the latest moe_dispatch or moe_mx_dispatch on this
+ * context, like moe_combine, and the same T; INVALID_ARG otherwise, and after moe_ep_route.  The
+ * selection itself, the replica pick and the 4-bit rounding have no gradient (the last is passed through).
+ *
+ * moe_combine_backward — from dy device [T,H] bf16 and the expert_buf [T*k,H] bf16 of the forward:
+ *   d_expert_buf[dst_row[t*k+j], :] = bf16( (w[t,j] * slot_scale[slot]) * dy[t,:] )       [T*k,H] bf16 out
+ *   d_weights[t,j] = slot_scale[slot] * sum_c expert_buf[dst_row[t*k+j], c] * dy[t,c]     [T,k] f32 out
+ * fp32 sums in a fixed order.  expert_buf, dy and d_expert_buf 16-byte aligned; d_expert_buf may not be expert_buf.
+ */
+moe_status moe_combine_backward(moe_ctx *ctx, const void *expert_buf, const void *dy, int32_t T,
+                                void *d_expert_buf, float *d_weights, void *cuda_stream);
+
+/*
+ * moe_dispatch_backward — from d_send_buf device [T*k,H] bf16 and d_weights device [T,k] f32:
+ *   dx[t,:] = bf16( sum_j d_send_buf[dst_row[t*k+j], :] )                                  [T,H] bf16 out
+ *   d_logits[t, id_j] = w_j * (d_weights_j - sum_i w_i * d_weights_i / route_scale)        [T,E] f32 out
+ *                       (times 1 - sigmoid(logit) for sigmoid scores), 0 for every other expert
+ * logits: those of the forward, read for sigmoid scores only.  d_weights and d_logits may both be
+ * NULL; they must be for MOE_ROUTE_DENSE_TP, whose weights are constants.  d_send_buf, dx and
+ * d_logits 16-byte aligned.
+ */
+moe_status moe_dispatch_backward(moe_ctx *ctx, const float *logits, const void *d_send_buf, const float *d_weights,
+                                 int32_t T, void *dx, float *d_logits, void *cuda_stream);
+
+/*
  * moe_step_host — one dispatch + combine fed from HOST memory, for callers
  * that hold activations on the CPU: copies logits and x to the given device
  * staging buffers, runs moe_dispatch and moe_combine (expert_buf = the send

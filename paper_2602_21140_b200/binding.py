@@ -34,6 +34,7 @@ MOE_ERR_DEVICE_TIMEOUT = 5
 MOE_SCORE_SOFTMAX = 0
 MOE_SCORE_SIGMOID = 1
 MOE_ROUTE_DENSE_TP = 2
+MOE_DTYPE_BF16, MOE_DTYPE_F16, MOE_DTYPE_F32 = range(3)
 # options of moe_set_tuning (include/moe_route.h, moe_tuning_option)
 (MOE_TUNE_PDL, MOE_TUNE_SCATTER_IMPL, MOE_TUNE_SCATTER_BULK_STAGES, MOE_TUNE_SCATTER_BULK_CTAS_PER_SM,
  MOE_TUNE_SCATTER_BLOCKS_PER_SM, MOE_TUNE_SCATTER_UNROLL, MOE_TUNE_COMBINE_IMPL, MOE_TUNE_COMBINE_CHUNK,
@@ -48,6 +49,8 @@ EXPORTED_SYMBOLS = (
     "moe_set_failed_experts", "moe_compact_ranks", "moe_set_rank_order",
     "moe_ep_attach", "moe_ep_route", "moe_ep_scatter", "moe_ep_combine", "moe_ep_plan_host",
     "moe_set_tuning", "moe_debug_skip_ticket",
+    "moe_mx_scale_pitch", "moe_mx_quantize", "moe_mx_dequantize", "moe_mx_dispatch", "moe_mx_expert_product",
+    "moe_mx_expert_gated", "moe_combine_backward", "moe_dispatch_backward",
 )
 
 
@@ -91,7 +94,7 @@ def _lib():
                 f"{_LIB_PATH} is missing: build it with "
                 "`python -m paper_2602_21140_b200.build` (needs nvcc); there is no fallback path")
         lib = ctypes.CDLL(_LIB_PATH)
-        vp, i32 = ctypes.c_void_p, ctypes.c_int32
+        vp, i32, i64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64
         lib.moe_route_init.restype = ctypes.c_int
         lib.moe_route_init.argtypes = [ctypes.POINTER(moe_config), vp, vp, vp, vp, ctypes.POINTER(vp)]
         lib.moe_set_failed_ranks.restype = ctypes.c_int
@@ -139,6 +142,22 @@ def _lib():
         lib.moe_set_tuning.argtypes = [vp, i32, i32]
         lib.moe_debug_skip_ticket.restype = ctypes.c_int
         lib.moe_debug_skip_ticket.argtypes = [vp]
+        lib.moe_mx_scale_pitch.restype = i32
+        lib.moe_mx_scale_pitch.argtypes = [i32]
+        lib.moe_mx_quantize.restype = ctypes.c_int
+        lib.moe_mx_quantize.argtypes = [vp, i32, i64, i32, i64, vp, vp, vp]
+        lib.moe_mx_dequantize.restype = ctypes.c_int
+        lib.moe_mx_dequantize.argtypes = [vp, vp, i64, i32, vp, i32, i64, vp]
+        lib.moe_mx_dispatch.restype = ctypes.c_int
+        lib.moe_mx_dispatch.argtypes = [vp, vp, vp, i32, ctypes.POINTER(moe_dispatch_out), vp, vp, vp]
+        lib.moe_mx_expert_product.restype = ctypes.c_int
+        lib.moe_mx_expert_product.argtypes = [vp, vp, vp, i64, vp, vp, vp, vp, i32, i32, vp, vp]
+        lib.moe_mx_expert_gated.restype = ctypes.c_int
+        lib.moe_mx_expert_gated.argtypes = [vp, vp, vp, i64, vp, vp, vp, vp, i32, i32, vp, vp, vp]
+        lib.moe_combine_backward.restype = ctypes.c_int
+        lib.moe_combine_backward.argtypes = [vp, vp, vp, i32, vp, vp, vp]
+        lib.moe_dispatch_backward.restype = ctypes.c_int
+        lib.moe_dispatch_backward.argtypes = [vp, vp, vp, vp, i32, vp, vp, vp]
         lib.moe_status_string.restype = ctypes.c_char_p
         lib.moe_status_string.argtypes = [ctypes.c_int]
         _lib_handle = lib
@@ -325,6 +344,50 @@ def moe_ep_plan_host(counts_all, rank: int):
     return st, src_base, recv_off
 
 
+def moe_mx_scale_pitch(cols: int) -> int:
+    return int(_lib().moe_mx_scale_pitch(cols))
+
+
+def moe_mx_quantize(x_ptr: int, dtype: int, rows: int, cols: int, row_stride: int, codes_ptr: int, scales_ptr: int,
+                    cuda_stream: int = 0) -> int:
+    return _lib().moe_mx_quantize(x_ptr, dtype, rows, cols, row_stride, codes_ptr, scales_ptr, cuda_stream)
+
+
+def moe_mx_dequantize(codes_ptr: int, scales_ptr: int, rows: int, cols: int, y_ptr: int, dtype: int, row_stride: int,
+                      cuda_stream: int = 0) -> int:
+    return _lib().moe_mx_dequantize(codes_ptr, scales_ptr, rows, cols, y_ptr, dtype, row_stride, cuda_stream)
+
+
+def moe_mx_dispatch(ctx, logits_ptr: int, x_ptr: int, T: int, out: moe_dispatch_out, send_codes_ptr: int,
+                    send_scales_ptr: int, cuda_stream: int = 0) -> int:
+    return _lib().moe_mx_dispatch(ctx, logits_ptr, x_ptr, T, ctypes.byref(out), send_codes_ptr, send_scales_ptr, cuda_stream)
+
+
+def moe_mx_expert_product(ctx, a_codes_ptr: int, a_scales_ptr: int, rows: int, slot_counts_ptr: int, slot_offsets_ptr: int,
+                          w_codes_ptr: int, w_scales_ptr: int, n_out: int, n_in: int, y_ptr: int, cuda_stream: int = 0) -> int:
+    return _lib().moe_mx_expert_product(ctx, a_codes_ptr, a_scales_ptr, rows, slot_counts_ptr, slot_offsets_ptr, w_codes_ptr,
+                                        w_scales_ptr, n_out, n_in, y_ptr, cuda_stream)
+
+
+def moe_mx_expert_gated(ctx, a_codes_ptr: int, a_scales_ptr: int, rows: int, slot_counts_ptr: int, slot_offsets_ptr: int,
+                        w_codes_ptr: int, w_scales_ptr: int, n_hidden: int, n_in: int, h_codes_ptr: int, h_scales_ptr: int,
+                        cuda_stream: int = 0) -> int:
+    return _lib().moe_mx_expert_gated(ctx, a_codes_ptr, a_scales_ptr, rows, slot_counts_ptr, slot_offsets_ptr, w_codes_ptr,
+                                      w_scales_ptr, n_hidden, n_in, h_codes_ptr, h_scales_ptr, cuda_stream)
+
+
+def moe_combine_backward(ctx, expert_buf_ptr: int, dy_ptr: int, T: int, d_expert_buf_ptr: int, d_weights_ptr: int,
+                         cuda_stream: int = 0) -> int:
+    return _lib().moe_combine_backward(ctx, expert_buf_ptr, dy_ptr, T, d_expert_buf_ptr, d_weights_ptr, cuda_stream)
+
+
+def moe_dispatch_backward(ctx, logits_ptr: int, d_send_buf_ptr: int, d_weights_ptr: int, T: int, dx_ptr: int,
+                          d_logits_ptr: int, cuda_stream: int = 0) -> int:
+    """d_weights_ptr and d_logits_ptr may both be 0; logits_ptr may be 0 unless the scores are sigmoids."""
+    return _lib().moe_dispatch_backward(ctx, logits_ptr or None, d_send_buf_ptr, d_weights_ptr or None, T, dx_ptr,
+                                        d_logits_ptr or None, cuda_stream)
+
+
 def moe_route_destroy(ctx) -> int:
     return _lib().moe_route_destroy(ctx)
 
@@ -345,10 +408,95 @@ class DispatchBuffers:
     rank_offsets: torch.Tensor
     dst_row: torch.Tensor
     src_index: torch.Tensor
-    send_buf: torch.Tensor
+    send_buf: torch.Tensor | None      # None: the buffers of a dispatch with 4-bit rows
 
     def as_struct(self) -> moe_dispatch_out:
-        return moe_dispatch_out(*(getattr(self, f).data_ptr() for f, _ in moe_dispatch_out._fields_))
+        return moe_dispatch_out(self.topk_ids.data_ptr(), self.topk_weights.data_ptr(), self.topk_slot.data_ptr(),
+                                self.slot_counts.data_ptr(), self.slot_offsets.data_ptr(), self.rank_counts.data_ptr(),
+                                self.rank_offsets.data_ptr(), self.dst_row.data_ptr(), self.src_index.data_ptr(),
+                                None if self.send_buf is None else self.send_buf.data_ptr())
+
+
+@dataclass
+class MxRows:
+    """4-bit rows (format: include/moe_route.h): any leading dimensions, contiguous."""
+    codes: torch.Tensor      # uint8 [..., cols / 2]
+    scales: torch.Tensor     # uint8 [..., moe_mx_scale_pitch(cols)]
+
+    @property
+    def cols(self) -> int:
+        return 2 * self.codes.shape[-1]
+
+
+_DTYPE_CODE = {torch.bfloat16: MOE_DTYPE_BF16, torch.float16: MOE_DTYPE_F16, torch.float32: MOE_DTYPE_F32}
+
+
+def _require(ok: bool, where: str) -> None:
+    if not ok:
+        raise MoeError(MOE_ERR_INVALID_ARG, where)
+
+
+def _mx_pitch(cols: int) -> int:
+    return (cols // 32 + 15) // 16 * 16
+
+
+def _is_mx(m: MxRows, device, lead=None) -> bool:
+    c, s = m.codes, m.scales
+    return (c.dtype == torch.uint8 and s.dtype == torch.uint8 and c.is_contiguous() and s.is_contiguous()
+            and c.device == device and s.device == device and c.dim() == s.dim() and c.dim() > 0 and c.shape[-1] % 16 == 0
+            and c.shape[:-1] == s.shape[:-1] and s.shape[-1] == _mx_pitch(m.cols) and (lead is None or tuple(c.shape[:-1]) == lead))
+
+
+def _on_device(index: int, call, *args) -> int:
+    """call(*args) with that device current (a kernel launch needs its stream's device)."""
+    if torch.cuda.current_device() == index:
+        return call(*args)
+    with torch.cuda.device(index):
+        return call(*args)
+
+
+def mx_empty(*shape, device="cuda") -> MxRows:
+    """Uninitialised 4-bit rows of the given logical shape (last dimension: elements of a row)."""
+    lead, cols = shape[:-1], shape[-1]
+    _require(cols > 0 and cols % 32 == 0, "mx_empty")
+    return MxRows(torch.empty((*lead, cols // 2), dtype=torch.uint8, device=device),
+                  torch.empty((*lead, _mx_pitch(cols)), dtype=torch.uint8, device=device))
+
+
+def mx_quantize(x: torch.Tensor, out: MxRows | None = None) -> MxRows:
+    """Rows of ``x`` ([..., cols], bf16 / fp16 / fp32) in 4 bits, on the current stream of its device.
+    A 2-D ``x`` may have any row stride that keeps its rows 16-byte aligned; others are contiguous."""
+    _require(x.is_cuda and x.dtype in _DTYPE_CODE and x.dim() >= 1 and x.shape[-1] > 0 and x.shape[-1] % 32 == 0, "mx_quantize")
+    _require(x.is_contiguous() or (x.dim() == 2 and x.stride(1) == 1), "mx_quantize")
+    cols = x.shape[-1]
+    if out is None:
+        out = mx_empty(*x.shape, device=x.device)
+    else:
+        _require(_is_mx(out, x.device, tuple(x.shape[:-1])) and out.cols == cols, "mx_quantize")
+    rows = x.numel() // cols
+    stride = x.stride(0) if x.dim() == 2 and not x.is_contiguous() else cols
+    st = _on_device(x.device.index, moe_mx_quantize, x.data_ptr(), _DTYPE_CODE[x.dtype], rows, cols, stride,
+                    out.codes.data_ptr(), out.scales.data_ptr(), torch.cuda.current_stream(x.device).cuda_stream)
+    if st != MOE_OK:
+        raise MoeError(st, "moe_mx_quantize")
+    return out
+
+
+def mx_dequantize(m: MxRows, dtype: torch.dtype = torch.bfloat16, out: torch.Tensor | None = None) -> torch.Tensor:
+    """The values that 4-bit rows stand for."""
+    device = m.codes.device
+    _require(m.codes.is_cuda and dtype in _DTYPE_CODE and _is_mx(m, device) and m.cols > 0, "mx_dequantize")
+    shape = (*m.codes.shape[:-1], m.cols)
+    if out is None:
+        out = torch.empty(shape, dtype=dtype, device=device)
+    _require(tuple(out.shape) == shape and out.dtype == dtype and out.device == device
+             and (out.is_contiguous() or (out.dim() == 2 and out.stride(1) == 1)), "mx_dequantize")
+    stride = out.stride(0) if out.dim() == 2 and not out.is_contiguous() else m.cols
+    st = _on_device(device.index, moe_mx_dequantize, m.codes.data_ptr(), m.scales.data_ptr(), out.numel() // m.cols, m.cols,
+                    out.data_ptr(), _DTYPE_CODE[dtype], stride, torch.cuda.current_stream(device).cuda_stream)
+    if st != MOE_OK:
+        raise MoeError(st, "moe_mx_dequantize")
+    return out
 
 
 def make_config(num_experts, top_k, hidden, max_tokens, num_ranks, slots_per_rank, max_replicas=2,
@@ -380,7 +528,7 @@ class MoeRouter:
     def num_slots(self) -> int:
         return self.cfg.num_ranks * self.cfg.slots_per_rank
 
-    def alloc_outputs(self, T: int) -> DispatchBuffers:
+    def alloc_outputs(self, T: int, send_buf: bool = True) -> DispatchBuffers:
         c, dev = self.cfg, self.device
         n = T * c.top_k
         i32 = dict(dtype=torch.int32, device=dev)
@@ -394,7 +542,7 @@ class MoeRouter:
             rank_offsets=torch.empty(c.num_ranks + 1, **i32),
             dst_row=torch.empty(n, **i32),
             src_index=torch.empty(n, **i32),
-            send_buf=torch.empty((n, c.hidden), dtype=torch.bfloat16, device=dev))
+            send_buf=torch.empty((n, c.hidden), dtype=torch.bfloat16, device=dev) if send_buf else None)
 
     # -- recovery -----------------------------------------------------------
     def set_failed_ranks(self, ranks) -> None:
@@ -438,6 +586,129 @@ class MoeRouter:
         if st != MOE_OK:
             raise MoeError(st, "moe_combine")
         return y
+
+    # -- 4-bit rows: dispatch and the experts' products ----------------------
+    def _here(self, t: torch.Tensor, dtype, shape) -> bool:
+        return t.dtype == dtype and tuple(t.shape) == shape and t.is_contiguous() and t.device == self._index_device()
+
+    def _index_device(self) -> torch.device:
+        if self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
+        return self.device
+
+    def mx_dispatch(self, logits: torch.Tensor, x: torch.Tensor, out: DispatchBuffers | None = None,
+                    rows: MxRows | None = None):
+        """As dispatch, with a send buffer of 4-bit rows.  Returns (buffers, rows)."""
+        c, dev = self.cfg, self._index_device()
+        T = x.shape[0]
+        n = T * c.top_k
+        _require(self._here(logits, torch.float32, (T, c.num_experts)) and self._here(x, torch.bfloat16, (T, c.hidden)), "mx_dispatch")
+        if out is None:
+            out = self.alloc_outputs(T, send_buf=False)
+        if rows is None:
+            rows = mx_empty(n, c.hidden, device=dev)
+        else:
+            _require(_is_mx(rows, dev, (n,)) and rows.cols == c.hidden, "mx_dispatch")
+        st = moe_mx_dispatch(self._ctx, logits.data_ptr(), x.data_ptr(), T, out.as_struct(), rows.codes.data_ptr(),
+                             rows.scales.data_ptr(), self._stream())
+        if st != MOE_OK:
+            raise MoeError(st, "moe_mx_dispatch")
+        return out, rows
+
+    def _segments_ok(self, rows: MxRows, slot_counts, slot_offsets, weight: MxRows) -> bool:
+        dev, P = self._index_device(), self.num_slots
+        return (_is_mx(rows, dev) and rows.codes.dim() == 2 and _is_mx(weight, dev) and weight.codes.dim() == 3
+                and weight.codes.shape[0] == P and weight.cols == rows.cols and self._here(slot_counts, torch.int32, (P,))
+                and slot_offsets.dim() == 1 and slot_offsets.shape[0] >= P
+                and self._here(slot_offsets, torch.int32, tuple(slot_offsets.shape)))
+
+    def mx_expert_product(self, rows: MxRows, slot_counts: torch.Tensor, slot_offsets: torch.Tensor, weight: MxRows,
+                          y: torch.Tensor | None = None) -> torch.Tensor:
+        """y[r] = weight[slot of r] @ rows[r]: weight [P, n_out, cols] and rows [n, cols] in 4 bits, y [n, n_out] bf16."""
+        _require(self._segments_ok(rows, slot_counts, slot_offsets, weight), "mx_expert_product")
+        n, n_out = rows.codes.shape[0], weight.codes.shape[1]
+        if y is None:
+            y = torch.empty((n, n_out), dtype=torch.bfloat16, device=self.device)
+        _require(self._here(y, torch.bfloat16, (n, n_out)), "mx_expert_product")
+        st = moe_mx_expert_product(self._ctx, rows.codes.data_ptr(), rows.scales.data_ptr(), n, slot_counts.data_ptr(),
+                                   slot_offsets.data_ptr(), weight.codes.data_ptr(), weight.scales.data_ptr(), n_out, rows.cols,
+                                   y.data_ptr(), self._stream())
+        if st != MOE_OK:
+            raise MoeError(st, "moe_mx_expert_product")
+        return y
+
+    def mx_expert_gated(self, rows: MxRows, slot_counts: torch.Tensor, slot_offsets: torch.Tensor, gate_up: MxRows,
+                        out: MxRows | None = None) -> MxRows:
+        """silu(gate) * up in 4 bits.  gate_up [P, 2 * n_hidden, cols]: row 2i is the gate of feature i, row 2i + 1 its up-projection."""
+        _require(self._segments_ok(rows, slot_counts, slot_offsets, gate_up) and gate_up.codes.shape[1] % 64 == 0
+                 and gate_up.codes.shape[1] > 0, "mx_expert_gated")
+        n, n_hidden = rows.codes.shape[0], gate_up.codes.shape[1] // 2
+        if out is None:
+            out = mx_empty(n, n_hidden, device=self.device)
+        else:
+            _require(_is_mx(out, self.device, (n,)) and out.cols == n_hidden, "mx_expert_gated")
+        st = moe_mx_expert_gated(self._ctx, rows.codes.data_ptr(), rows.scales.data_ptr(), n, slot_counts.data_ptr(),
+                                 slot_offsets.data_ptr(), gate_up.codes.data_ptr(), gate_up.scales.data_ptr(), n_hidden, rows.cols,
+                                 out.codes.data_ptr(), out.scales.data_ptr(), self._stream())
+        if st != MOE_OK:
+            raise MoeError(st, "moe_mx_expert_gated")
+        return out
+
+    def mx_expert_ffn(self, rows: MxRows, slot_counts: torch.Tensor, slot_offsets: torch.Tensor, gate_up: MxRows, down: MxRows,
+                      y: torch.Tensor | None = None, hidden: MxRows | None = None) -> torch.Tensor:
+        """The gated feed-forward expert of every slot on its rows: mx_expert_gated, then mx_expert_product."""
+        hidden = self.mx_expert_gated(rows, slot_counts, slot_offsets, gate_up, hidden)
+        return self.mx_expert_product(hidden, slot_counts, slot_offsets, down, y)
+
+    def mx_step(self, logits: torch.Tensor, x: torch.Tensor, gate_up: MxRows, down: MxRows, out: DispatchBuffers | None = None,
+                y: torch.Tensor | None = None) -> torch.Tensor:
+        """One whole layer: 4-bit dispatch, the experts, and the combine (times slot_scale, as always)."""
+        out, rows = self.mx_dispatch(logits, x, out)
+        buf = self.mx_expert_ffn(rows, out.slot_counts, out.slot_offsets, gate_up, down)
+        _require(buf.shape[1] == self.cfg.hidden, "mx_step")
+        return self.combine(buf, x.shape[0], y)
+
+    # -- gradients of the routed step ----------------------------------------
+    def combine_backward(self, expert_buf: torch.Tensor, dy: torch.Tensor, d_expert_buf: torch.Tensor | None = None,
+                         d_weights: torch.Tensor | None = None):
+        """Gradients of the latest combine by its rows and its gate weights: (d_expert_buf, d_weights)."""
+        c, T = self.cfg, dy.shape[0]
+        n = T * c.top_k
+        if d_expert_buf is None:
+            d_expert_buf = torch.empty((n, c.hidden), dtype=torch.bfloat16, device=self.device)
+        if d_weights is None:
+            d_weights = torch.empty((T, c.top_k), dtype=torch.float32, device=self.device)
+        _require(self._here(expert_buf, torch.bfloat16, (n, c.hidden)) and self._here(dy, torch.bfloat16, (T, c.hidden))
+                 and self._here(d_expert_buf, torch.bfloat16, (n, c.hidden))
+                 and self._here(d_weights, torch.float32, (T, c.top_k)), "combine_backward")
+        st = moe_combine_backward(self._ctx, expert_buf.data_ptr(), dy.data_ptr(), T, d_expert_buf.data_ptr(),
+                                  d_weights.data_ptr(), self._stream())
+        if st != MOE_OK:
+            raise MoeError(st, "moe_combine_backward")
+        return d_expert_buf, d_weights
+
+    def dispatch_backward(self, logits: torch.Tensor | None, d_send_buf: torch.Tensor, d_weights: torch.Tensor | None = None,
+                          dx: torch.Tensor | None = None, d_logits: torch.Tensor | None = None):
+        """Gradients of the latest dispatch: (dx, d_logits).  d_logits is None without d_weights."""
+        c = self.cfg
+        n = d_send_buf.shape[0]
+        T = n // c.top_k
+        if dx is None:
+            dx = torch.empty((T, c.hidden), dtype=torch.bfloat16, device=self.device)
+        ok = self._here(d_send_buf, torch.bfloat16, (T * c.top_k, c.hidden)) and self._here(dx, torch.bfloat16, (T, c.hidden))
+        if d_weights is not None:
+            if d_logits is None:
+                d_logits = torch.empty((T, c.num_experts), dtype=torch.float32, device=self.device)
+            ok = (ok and self._here(d_weights, torch.float32, (T, c.top_k))
+                  and self._here(d_logits, torch.float32, (T, c.num_experts)))
+        ok = ok and (logits is None or self._here(logits, torch.float32, (T, c.num_experts)))
+        _require(ok, "dispatch_backward")
+        st = moe_dispatch_backward(self._ctx, 0 if logits is None else logits.data_ptr(), d_send_buf.data_ptr(),
+                                   0 if d_weights is None else d_weights.data_ptr(), T, dx.data_ptr(),
+                                   0 if d_logits is None else d_logits.data_ptr(), self._stream())
+        if st != MOE_OK:
+            raise MoeError(st, "moe_dispatch_backward")
+        return dx, d_logits
 
     # -- expert parallelism over several GPUs -------------------------------
     def ep_attach(self, world: int, rank: int, recv_buf_ptrs, recv_rows: int) -> None:

@@ -8,8 +8,9 @@ import sys
 _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(CSRC, "libmoe_route.so")
-SOURCES = ["moe_route.cu", "permute_static.cu"]
+SOURCES = ["moe_route.cu", "permute_static.cu", "mx_rows.cu", "mx_product.cu"]
 HEADERS = ["device_utils.cuh", "route_kernels.cuh", "scatter_kernels.cuh", "combine_kernels.cuh", "ep_kernels.cuh",
+           "backward_kernels.cuh", "mx_format.cuh", "mx_scatter.cuh", "mx_product.h",
            os.path.join("..", "..", "include", "moe_route.h")]
 
 
@@ -26,7 +27,7 @@ def build_library(force: bool = False, verbose: bool = False) -> str:
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
     tmp = LIB + f".tmp{os.getpid()}"
     cmd = [nvcc, "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-           "-Xcompiler", "-fPIC", "-shared", "-o", tmp]
+           "-Xcompiler", "-fPIC", "--threads", "0", "-shared", "-o", tmp]
     if verbose:
         cmd += ["-Xptxas", "-v"]
     cmd += [os.path.join(CSRC, s) for s in SOURCES]

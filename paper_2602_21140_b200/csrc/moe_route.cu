@@ -12,8 +12,11 @@
 #include <new>
 #include <vector>
 
+#include "backward_kernels.cuh"
 #include "combine_kernels.cuh"
 #include "ep_kernels.cuh"
+#include "mx_product.h"
+#include "mx_scatter.cuh"
 #include "route_kernels.cuh"
 #include "scatter_kernels.cuh"
 
@@ -252,7 +255,8 @@ struct moe_ctx {
     int combine_stages, combine_u, combine_ctas_per_sm, combine_warps;
     size_t combine_smem;
     size_t route_smem;
-    // what the latest dispatch wrote, for combine
+    // what the latest dispatch wrote, for combine and the gradients
+    const int32_t *last_ids;
     const float *last_weights;
     const int32_t *last_slot;
     const int32_t *last_dst_row;
@@ -403,6 +407,17 @@ moe_status enqueue_combine_bulk(moe_ctx *ctx, const CombineParams &cp, cudaStrea
         default: launch_kernel(k_combine_bulk<4, 0>, g, b, sm, st, pdl, cp, stg, ctl); break;
     }
     return cudaGetLastError() == cudaSuccess ? MOE_OK : MOE_ERR_CUDA;
+}
+
+// The combine kernel of the context's choice.
+moe_status enqueue_combine(moe_ctx *ctx, const CombineParams &cp, cudaStream_t st)
+{
+    if (ctx->combine_impl == 1) return enqueue_combine_bulk(ctx, cp, st);
+    const int chunks = (cp.hv + kCombineChunk - 1) / kCombineChunk;
+    const long long items = (long long)cp.T * chunks;
+    const long long want = (items + kCombineThreads / 32 - 1) / (kCombineThreads / 32);
+    const int grid = (int)std::min<long long>(want, (long long)ctx->sm_count * ctx->combine_blocks_per_sm);
+    return launch_combine(cp, grid, st) == cudaSuccess ? MOE_OK : MOE_ERR_CUDA;
 }
 
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
@@ -639,7 +654,7 @@ moe_status moe_route_init(const moe_config *cfg, const int32_t *slot_to_expert, 
     ctx->expert_failed = no_lost;
     ctx->rank_order = ident;
     ctx->n_listed = d.R;
-    ctx->last_weights = nullptr; ctx->last_slot = nullptr; ctx->last_dst_row = nullptr;
+    ctx->last_ids = nullptr; ctx->last_weights = nullptr; ctx->last_slot = nullptr; ctx->last_dst_row = nullptr;
     ctx->last_T = -1;
     ctx->timing_event = nullptr;
     ctx->ep_world = 0; ctx->ep_rank = 0; ctx->ep_spg = 0; ctx->ep_recv_rows = 0;
@@ -812,7 +827,7 @@ moe_status moe_dispatch(moe_ctx *ctx, const float *logits, const void *x, int32_
     if (!ctx || !out || T < 0) return MOE_ERR_INVALID_ARG;
     if (T > ctx->cfg.max_tokens) return MOE_ERR_CAPACITY;
     if (T == 0) {                     // nothing to route: no launch, pointers not inspected
-        ctx->last_weights = out->topk_weights; ctx->last_slot = out->topk_slot;
+        ctx->last_ids = out->topk_ids; ctx->last_weights = out->topk_weights; ctx->last_slot = out->topk_slot;
         ctx->last_dst_row = out->dst_row; ctx->last_T = 0;
         return MOE_OK;
     }
@@ -824,7 +839,7 @@ moe_status moe_dispatch(moe_ctx *ctx, const float *logits, const void *x, int32_
     if (!aligned16(x) || !aligned16(out->send_buf) || !aligned16(logits)) return MOE_ERR_INVALID_ARG;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     const Derived &d = ctx->d;
-    ctx->last_weights = out->topk_weights; ctx->last_slot = out->topk_slot;
+    ctx->last_ids = out->topk_ids; ctx->last_weights = out->topk_weights; ctx->last_slot = out->topk_slot;
     ctx->last_dst_row = out->dst_row; ctx->last_T = T;
 
     if (enqueue_route(ctx, logits, T, out, st) != cudaSuccess) return MOE_ERR_CUDA;
@@ -887,13 +902,7 @@ moe_status moe_combine(moe_ctx *ctx, const void *expert_buf, int32_t T, void *y,
     cp.slot_scale = ctx->d_slot_scale;
     cp.peer_bufs = nullptr; cp.slots_per_gpu = 0;
     cp.P = d.P; cp.row_limit = (long long)T * d.k; cp.zero_row = ctx->d_zero_row; cp.spin_limit = ctx->spin_limit;
-    if (ctx->combine_impl == 1) return enqueue_combine_bulk(ctx, cp, st);
-    const int chunks = (cp.hv + kCombineChunk - 1) / kCombineChunk;
-    const long long items = (long long)T * chunks;
-    const long long want = (items + kCombineThreads / 32 - 1) / (kCombineThreads / 32);
-    const int grid = (int)std::min<long long>(want, (long long)ctx->sm_count * ctx->combine_blocks_per_sm);
-    if (launch_combine(cp, grid, st) != cudaSuccess) return MOE_ERR_CUDA;
-    return MOE_OK;
+    return enqueue_combine(ctx, cp, st);
 }
 
 // ---------------------------------------------------------------------------
@@ -974,7 +983,7 @@ moe_status moe_ep_route(moe_ctx *ctx, const float *logits, int32_t T, const moe_
     if (T > 0 && ((!logits && ctx->cfg.score_func != MOE_ROUTE_DENSE_TP) || !aligned16(logits)))
         return MOE_ERR_INVALID_ARG;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    ctx->last_weights = out->topk_weights; ctx->last_slot = out->topk_slot;
+    ctx->last_ids = out->topk_ids; ctx->last_weights = out->topk_weights; ctx->last_slot = out->topk_slot;
     ctx->last_dst_row = out->dst_row; ctx->last_T = T; ctx->ep_routed = true;
     if (T == 0) {                      // this GPU sends nothing, but its counts still take part in the exchange
         if (cudaMemsetAsync(out->slot_counts, 0, (size_t)ctx->d.P * 4, st) != cudaSuccess) return MOE_ERR_CUDA;
@@ -1034,6 +1043,189 @@ moe_status moe_ep_combine(moe_ctx *ctx, int32_t T, void *y, void *cuda_stream)
     cp.peer_bufs = const_cast<const uint4 *const *>(ctx->d_peer_bufs); cp.slots_per_gpu = ctx->ep_spg;
     cp.P = d.P; cp.row_limit = ctx->ep_recv_rows; cp.zero_row = ctx->d_zero_row; cp.spin_limit = ctx->spin_limit;
     return enqueue_combine_bulk(ctx, cp, st);
+}
+
+// ---------------------------------------------------------------------------
+// 4-bit rows and the gradients of the routed step
+// ---------------------------------------------------------------------------
+
+namespace {
+
+// The context's device for the duration of a call, whatever device the caller has current.
+struct DeviceScope {
+    int before = -1;
+    bool ok = true;
+    explicit DeviceScope(int device)
+    {
+        ok = cudaGetDevice(&before) == cudaSuccess;
+        if (ok && before != device) ok = cudaSetDevice(device) == cudaSuccess;
+        else before = -1;
+    }
+    ~DeviceScope() { if (before >= 0) cudaSetDevice(before); }
+};
+
+// Rows read and written by an expert product: common checks.
+moe_status check_product(const moe_ctx *ctx, const uint8_t *a_codes, const uint8_t *a_scales, int64_t rows,
+                         const int32_t *slot_counts, const int32_t *slot_offsets, const uint8_t *w_codes,
+                         const uint8_t *w_scales, int32_t n_out, int32_t n_in)
+{
+    if (!ctx || rows < 0 || n_out < 1 || n_in < kMxBlock || n_in % kMxBlock != 0) return MOE_ERR_INVALID_ARG;
+    // 32-bit tile numbers and tensor-map strides (2^40 bytes)
+    const long long feats = ((long long)n_out + 127) / 128;
+    if (rows > (1ll << 30) || feats * (ctx->d.P + rows / 32) > (1ll << 30)) return MOE_ERR_CAPACITY;
+    if ((long long)n_out * (n_in / 2) >= (1ll << 40)) return MOE_ERR_CAPACITY;
+    if (rows == 0) return MOE_OK;
+    if (!a_codes || !a_scales || !slot_counts || !slot_offsets || !w_codes || !w_scales) return MOE_ERR_INVALID_ARG;
+    if (!aligned16(a_codes) || !aligned16(a_scales) || !aligned16(w_codes) || !aligned16(w_scales)) return MOE_ERR_INVALID_ARG;
+    return MOE_OK;
+}
+
+MxProductArgs product_args(const moe_ctx *ctx, const uint8_t *a_codes, const uint8_t *a_scales, int64_t rows,
+                           const int32_t *slot_counts, const int32_t *slot_offsets, const uint8_t *w_codes,
+                           const uint8_t *w_scales, int32_t n_out, int32_t n_in)
+{
+    MxProductArgs a = {};
+    a.a_codes = a_codes; a.a_scales = a_scales; a.rows = rows;
+    a.slot_counts = slot_counts; a.slot_offsets = slot_offsets; a.P = ctx->d.P;
+    a.w_codes = w_codes; a.w_scales = w_scales; a.N = n_out; a.K = n_in;
+    a.ctl = ctx->d_ctl; a.spin_limit = ctx->spin_limit; a.sm_count = ctx->sm_count; a.pdl = ctx->pdl;
+    return a;
+}
+
+}  // namespace
+
+moe_status moe_mx_dispatch(moe_ctx *ctx, const float *logits, const void *x, int32_t T, const moe_dispatch_out *out,
+                           uint8_t *send_codes, uint8_t *send_scales, void *cuda_stream)
+{
+    if (!ctx || !out || T < 0) return MOE_ERR_INVALID_ARG;
+    if (ctx->d.H % kMxBlock != 0) return MOE_ERR_INVALID_ARG;
+    if (T > ctx->cfg.max_tokens) return MOE_ERR_CAPACITY;
+    if (T > 0) {
+        if (!out->topk_ids || !out->topk_weights || !out->topk_slot || !out->slot_counts || !out->slot_offsets ||
+            !out->rank_counts || !out->rank_offsets || !out->dst_row || !out->src_index || !send_codes || !send_scales)
+            return MOE_ERR_INVALID_ARG;
+        if (!x || (!logits && ctx->cfg.score_func != MOE_ROUTE_DENSE_TP)) return MOE_ERR_INVALID_ARG;
+        if (!aligned16(x) || !aligned16(logits) || !aligned16(send_codes) || !aligned16(send_scales)) return MOE_ERR_INVALID_ARG;
+    }
+    ctx->last_ids = out->topk_ids; ctx->last_weights = out->topk_weights; ctx->last_slot = out->topk_slot;
+    ctx->last_dst_row = out->dst_row; ctx->last_T = T;
+    ctx->ep_routed = false;
+    if (T == 0) return MOE_OK;
+    DeviceScope scope(ctx->device);
+    if (!scope.ok) return MOE_ERR_CUDA;
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    const Derived &d = ctx->d;
+    if (enqueue_route(ctx, logits, T, out, st) != cudaSuccess) return MOE_ERR_CUDA;
+    if (ctx->timing_event && cudaEventRecord(ctx->timing_event, st) != cudaSuccess) return MOE_ERR_CUDA;
+    MxScatterParams mp;
+    ScatterParams &sp = mp.s;
+    sp.x = static_cast<const uint4 *>(x); sp.send = nullptr;
+    sp.T = T; sp.k = d.k; sp.hv = d.H / 8; sp.P = d.P; sp.spin_limit = ctx->spin_limit;
+    sp.topk_slot = out->topk_slot; sp.slot_offsets = out->slot_offsets; sp.pos_in_slot = ctx->d_pos;
+    sp.dst_row = out->dst_row; sp.src_index = out->src_index; sp.ctl = ctx->d_ctl;
+    mp.codes = send_codes; mp.scales = send_scales; mp.pitch = mx_scale_pitch(d.H);
+    // A warp takes a whole row when there are rows enough for every SM's warps, and single 1024-column
+    // pieces otherwise.
+    const int pieces = (sp.hv + 127) / 128;
+    mp.pieces = T >= ctx->sm_count * 16 ? pieces : 1;
+    const long long items = (long long)T * ((pieces + mp.pieces - 1) / mp.pieces);
+    const long long want = (items + kScatterThreads / 32 - 1) / (kScatterThreads / 32);
+    const int grid = (int)std::min<long long>(want, (long long)ctx->sm_count * 8);
+    if (launch_kernel(k_mx_scatter, dim3(grid), dim3(kScatterThreads), 0, st, ctx->pdl, mp) != cudaSuccess) return MOE_ERR_CUDA;
+    return MOE_OK;
+}
+
+moe_status moe_mx_expert_product(moe_ctx *ctx, const uint8_t *a_codes, const uint8_t *a_scales, int64_t rows,
+                                 const int32_t *slot_counts, const int32_t *slot_offsets, const uint8_t *w_codes,
+                                 const uint8_t *w_scales, int32_t n_out, int32_t n_in, void *y, void *cuda_stream)
+{
+    const moe_status ms = check_product(ctx, a_codes, a_scales, rows, slot_counts, slot_offsets, w_codes, w_scales, n_out, n_in);
+    if (ms != MOE_OK) return ms;
+    if (n_out % 8 != 0) return MOE_ERR_INVALID_ARG;
+    if (rows == 0) return MOE_OK;
+    if (!y || !aligned16(y)) return MOE_ERR_INVALID_ARG;
+    DeviceScope scope(ctx->device);
+    if (!scope.ok) return MOE_ERR_CUDA;
+    MxProductArgs a = product_args(ctx, a_codes, a_scales, rows, slot_counts, slot_offsets, w_codes, w_scales, n_out, n_in);
+    a.gated = false; a.y = y;
+    return mx_product_launch(a, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? MOE_OK : MOE_ERR_CUDA;
+}
+
+moe_status moe_mx_expert_gated(moe_ctx *ctx, const uint8_t *a_codes, const uint8_t *a_scales, int64_t rows,
+                               const int32_t *slot_counts, const int32_t *slot_offsets, const uint8_t *w_codes,
+                               const uint8_t *w_scales, int32_t n_hidden, int32_t n_in, uint8_t *h_codes, uint8_t *h_scales,
+                               void *cuda_stream)
+{
+    if (n_hidden < kMxBlock || n_hidden % kMxBlock != 0 || n_hidden > (1 << 29)) return MOE_ERR_INVALID_ARG;
+    const moe_status ms = check_product(ctx, a_codes, a_scales, rows, slot_counts, slot_offsets, w_codes, w_scales, 2 * n_hidden, n_in);
+    if (ms != MOE_OK || rows == 0) return ms;
+    if (!h_codes || !h_scales || !aligned16(h_codes) || !aligned16(h_scales)) return MOE_ERR_INVALID_ARG;
+    DeviceScope scope(ctx->device);
+    if (!scope.ok) return MOE_ERR_CUDA;
+    MxProductArgs a = product_args(ctx, a_codes, a_scales, rows, slot_counts, slot_offsets, w_codes, w_scales, 2 * n_hidden, n_in);
+    a.gated = true; a.h_codes = h_codes; a.h_scales = h_scales;
+    return mx_product_launch(a, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? MOE_OK : MOE_ERR_CUDA;
+}
+
+moe_status moe_combine_backward(moe_ctx *ctx, const void *expert_buf, const void *dy, int32_t T, void *d_expert_buf,
+                                float *d_weights, void *cuda_stream)
+{
+    if (!ctx || T < 0) return MOE_ERR_INVALID_ARG;
+    if (ctx->last_T < 0 || T != ctx->last_T || ctx->ep_routed) return MOE_ERR_INVALID_ARG;
+    if (T == 0) return MOE_OK;
+    if (!expert_buf || !dy || !d_expert_buf || !d_weights) return MOE_ERR_INVALID_ARG;
+    if (!aligned16(expert_buf) || !aligned16(dy) || !aligned16(d_expert_buf)) return MOE_ERR_INVALID_ARG;
+    if (expert_buf == d_expert_buf) return MOE_ERR_INVALID_ARG;   // rows are read ahead of the ones written
+    DeviceScope scope(ctx->device);
+    if (!scope.ok) return MOE_ERR_CUDA;
+    const Derived &d = ctx->d;
+    CombineBackwardParams p;
+    p.buf = static_cast<const uint4 *>(expert_buf); p.dy = static_cast<const uint4 *>(dy);
+    p.d_buf = static_cast<uint4 *>(d_expert_buf); p.d_weights = d_weights;
+    p.T = T; p.k = d.k; p.hv = d.H / 8; p.P = d.P;
+    p.dst_row = ctx->last_dst_row; p.topk_weights = ctx->last_weights; p.topk_slot = ctx->last_slot;
+    p.slot_scale = ctx->d_slot_scale;
+    const int threads = std::min(kCombineBwdThreads, std::max(32, (p.hv + 31) / 32 * 32));
+    const int grid = std::min(T, ctx->sm_count * 8 * (kCombineBwdThreads / threads));
+    if (launch_kernel(k_combine_backward, dim3(grid), dim3(threads), 0, static_cast<cudaStream_t>(cuda_stream), ctx->pdl, p) !=
+        cudaSuccess)
+        return MOE_ERR_CUDA;
+    return MOE_OK;
+}
+
+moe_status moe_dispatch_backward(moe_ctx *ctx, const float *logits, const void *d_send_buf, const float *d_weights, int32_t T,
+                                 void *dx, float *d_logits, void *cuda_stream)
+{
+    if (!ctx || T < 0) return MOE_ERR_INVALID_ARG;
+    if (ctx->last_T < 0 || T != ctx->last_T || ctx->ep_routed) return MOE_ERR_INVALID_ARG;
+    // d_weights and d_logits come together; constant weights (dense-FFN mode) have no gradient
+    if ((d_weights == nullptr) != (d_logits == nullptr)) return MOE_ERR_INVALID_ARG;
+    if (d_logits && ctx->cfg.score_func == MOE_ROUTE_DENSE_TP) return MOE_ERR_INVALID_ARG;
+    if (T == 0) return MOE_OK;
+    if (!d_send_buf || !dx || !aligned16(d_send_buf) || !aligned16(dx)) return MOE_ERR_INVALID_ARG;
+    if (d_logits && (!aligned16(d_logits) || (ctx->cfg.score_func == MOE_SCORE_SIGMOID && !logits))) return MOE_ERR_INVALID_ARG;
+    DeviceScope scope(ctx->device);
+    if (!scope.ok) return MOE_ERR_CUDA;
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    const Derived &d = ctx->d;
+    if (d_logits) {
+        RouteBackwardParams rp;
+        rp.logits = logits; rp.topk_ids = ctx->last_ids; rp.topk_weights = ctx->last_weights; rp.d_weights = d_weights;
+        rp.d_logits = d_logits; rp.T = T; rp.E = d.E; rp.k = d.k;
+        rp.sigmoid = ctx->cfg.score_func == MOE_SCORE_SIGMOID;
+        rp.inv_scale = 1.0f / ctx->cfg.route_scale;
+        const int warps = kRouteBwdThreads / 32;
+        const int grid = std::min((T + warps - 1) / warps, ctx->sm_count * 8);
+        if (launch_kernel(k_route_backward, dim3(grid), dim3(kRouteBwdThreads), 0, st, ctx->pdl, rp) != cudaSuccess) return MOE_ERR_CUDA;
+    }
+    CombineParams cp;
+    cp.buf = static_cast<const uint4 *>(d_send_buf); cp.y = static_cast<uint4 *>(dx);
+    cp.T = T; cp.k = d.k; cp.hv = d.H / 8;
+    cp.dst_row = ctx->last_dst_row; cp.topk_weights = nullptr; cp.topk_slot = ctx->last_slot;
+    cp.slot_scale = ctx->d_slot_scale;
+    cp.peer_bufs = nullptr; cp.slots_per_gpu = 0;
+    cp.P = d.P; cp.row_limit = (long long)T * d.k; cp.zero_row = ctx->d_zero_row; cp.spin_limit = ctx->spin_limit;
+    return enqueue_combine(ctx, cp, st);
 }
 
 moe_status moe_step_host_async(moe_ctx *ctx, const float *logits_host, const void *x_host, int32_t T,

@@ -1,0 +1,646 @@
+// The experts' products on 4-bit rows: for every physical slot p and every row r of its segment
+//     out[r, f] = sum_k a[r, k] * w[p, f, k]          (fp32 accumulation on the tensor cores)
+// with both operands microscaled (mx_format.cuh), on tcgen05.mma kind::mxf4 with block scales: the
+// scales are applied inside the tensor core, nothing is unpacked.
+//
+// Weights are the M operand (128 features of one slot per tile) and rows the N operand, so a segment
+// of any length costs N = its length rounded up to 16, from one token to hundreds, and a tile's
+// accumulator is [128 lanes = features] x [columns = rows] in TMEM.  K goes in stages of 256 (128
+// bytes of a code row: one 128-byte swizzle span, four MMAs of K = 64).
+//
+// One persistent CTA per SM, eight warps:
+//   warps 0-3   epilogue: TMEM -> registers -> shared memory (transposed) -> HBM
+//   warp 4      TMA loads of the code tiles (weights 128 x 128 B, rows n x 128 B, 128-byte swizzle)
+//   warp 5      scales shared -> TMEM (tcgen05.cp) and the MMAs, from one thread
+//   warps 6-7   scales: 16-byte row pieces HBM -> registers -> the 32 x 16-byte blocks tcgen05.cp wants
+// The accumulator is double buffered, so the epilogue of a tile runs under the products of the next.
+//
+// Tiles are dealt slot by slot, feature tile by feature tile, row tile innermost: CTAs that work at the
+// same time share a weight tile (through L2) as often as possible.
+#include "mx_product.h"
+
+#include <cuda.h>
+
+#include <algorithm>
+#include <mutex>
+
+#include "mx_format.cuh"
+
+namespace {
+
+using namespace moe;
+
+constexpr int kThreads = 256;
+constexpr int kFeat = 128;                 // features per tile (M)
+constexpr int kStageK = 256;               // elements of K per stage
+constexpr int kRowBytes = kStageK / 2;     // bytes of a code row per stage
+constexpr int kATile = kFeat * kRowBytes;  // 16 KB
+constexpr int kMaxP = 4096;
+
+// ------------------------------------------------------------------ tcgen05 in PTX
+
+__device__ __forceinline__ void tmem_alloc(uint32_t *slot, uint32_t cols)
+{
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(slot)), "r"(cols) : "memory");
+}
+
+__device__ __forceinline__ void tmem_dealloc(uint32_t base, uint32_t cols)
+{
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(base), "r"(cols));
+}
+
+__device__ __forceinline__ void mma_commit(uint64_t *bar)
+{
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_addr(bar)) : "memory");
+}
+
+__device__ __forceinline__ void mma_mxf4(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sfa, uint32_t sfb, bool accumulate)
+{
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"((uint32_t)accumulate)
+        : "memory");
+}
+
+// 32 rows of 16 bytes from shared memory to four TMEM columns, repeated in the four lane quarters
+__device__ __forceinline__ void cp_scales(uint32_t tmem, uint64_t desc)
+{
+    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
+}
+
+__device__ __forceinline__ void tmem_ld32(uint32_t addr, uint32_t (&r)[32])
+{
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
+          "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
+          "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(addr));
+}
+
+__device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+__device__ __forceinline__ void mbar_arrive(uint64_t *bar)
+{
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_addr(bar)) : "memory");
+}
+
+__device__ __forceinline__ void tma_2d(void *dst, const CUtensorMap *map, int x, int y, uint64_t *bar)
+{
+    asm volatile("cp.async.bulk.tensor.2d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(
+                     smem_addr(dst)),
+                 "l"(map), "r"(x), "r"(y), "r"(smem_addr(bar))
+                 : "memory");
+}
+
+__device__ __forceinline__ void tma_3d(void *dst, const CUtensorMap *map, int x, int y, int z, uint64_t *bar)
+{
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(
+            smem_addr(dst)),
+        "l"(map), "r"(x), "r"(y), "r"(z), "r"(smem_addr(bar))
+        : "memory");
+}
+
+// Shared-memory matrix descriptor: start and strides in 16-byte units, version 1 (sm_100).
+// Code tiles: K-major, 128-byte swizzle, 8-row groups 1024 bytes apart.
+// Scale blocks: no swizzle, 8-row groups (8 x 16 bytes) 128 bytes apart.
+__device__ __forceinline__ uint64_t desc_codes(uint32_t addr)
+{
+    return (uint64_t)((addr >> 4) & 0x3fffu) | (1ull << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61);
+}
+__device__ __forceinline__ uint64_t desc_scales(uint32_t addr)
+{
+    return (uint64_t)((addr >> 4) & 0x3fffu) | (1ull << 16) | (8ull << 32) | (1ull << 46);
+}
+
+// Instruction descriptor of kind::mxf4: A and B e2m1 (1), both K-major, scales ue8m0 (bit 23),
+// N / 8 at bit 17, M / 16 at bit 24.  sf = which half of a 32-bit scale word (0 or 2) belongs to this K = 64.
+__device__ __forceinline__ uint32_t idesc_mxf4(int n, uint32_t sf)
+{
+    return (sf << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | (1u << 23) | ((uint32_t)(kFeat >> 4) << 24) | (sf << 29);
+}
+
+// ------------------------------------------------------------------------ tiles
+
+struct KernelParams {
+    const uint8_t *a_scales, *w_scales;
+    const int32_t *slot_counts, *slot_offsets;
+    long long rows;
+    int P, N, K;
+    __nv_bfloat16 *y;
+    uint8_t *h_codes, *h_scales;
+    Control *ctl;
+    unsigned spin_limit;
+};
+
+struct Tile {
+    int slot, feat;        // slot, first feature
+    int row;               // first row
+    int rows;              // rows of the tile (1 .. NT)
+    __device__ int n() const { return (rows + 15) & ~15; }
+};
+
+// Rows of slot p that can be worked on: counts and offsets come from device memory, so a segment
+// that leaves the row buffer is cut (or dropped) instead of followed.
+__device__ __forceinline__ int segment(const KernelParams &p, int s, int &first)
+{
+    first = __ldg(p.slot_offsets + s);
+    const long long c = __ldg(p.slot_counts + s);
+    if (first < 0 || c <= 0 || first >= p.rows) return 0;
+    return (int)min(c, p.rows - first);
+}
+
+// A segment of c rows is cut into the fewest tiles of at most NT rows, of equal size.
+template <int NT>
+__device__ __forceinline__ int row_tiles(int c) { return (c + NT - 1) / NT; }
+
+template <int NT>
+__device__ __forceinline__ Tile tile_at(const KernelParams &p, const int *ends, int index)
+{
+    int lo = 0, hi = p.P - 1;                        // first slot whose inclusive end is beyond the index
+    while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (ends[mid] > index) hi = mid; else lo = mid + 1;
+    }
+    const int local = index - (lo ? ends[lo - 1] : 0);
+    Tile t;
+    int first;
+    const int c = segment(p, lo, first);
+    const int nt = row_tiles<NT>(c);
+    const int f = local / nt, r = local - f * nt;
+    const int size = ((c + nt - 1) / nt + 15) & ~15;
+    t.slot = lo; t.feat = f * kFeat;
+    t.row = first + r * size;
+    t.rows = min(size, c - r * size);                // may be <= 0 for the last tile of an uneven cut
+    return t;
+}
+
+template <int NT, int STAGES>
+struct Layout {
+    static constexpr int kBTile = NT * kRowBytes;
+    static constexpr int kRB = (NT + 127) / 128;              // 128-row scale blocks of the row operand
+    static constexpr int kSfA = 2 * 512, kSfB = 2 * kRB * 512;
+    static constexpr int kStage = kATile + kBTile;            // multiples of 1024: swizzle alignment
+    static constexpr int kSf = kSfA + kSfB;
+    static constexpr int kStageOff = 0;
+    static constexpr int kSfOff = STAGES * kStage;
+    static constexpr int kEpiOff = kSfOff + STAGES * kSf;
+    static constexpr int kEpiBytes = 2 * (32 * 48 + 8) * 4;   // gated: two planes; plain: 4 x 2 KB
+    static constexpr int kBarOff = kEpiOff + kEpiBytes;
+    static constexpr int kBars = 3 * STAGES + 5;
+    static constexpr int kEndsOff = kBarOff + ((kBars * 8 + 32 + 15) & ~15);
+    static size_t bytes(int P) { return 1024 + kEndsOff + (size_t)P * 4; }
+};
+
+// Bounded wait.  `quit` is shared by the CTA: the first role that gives up sets it, the others follow.
+__device__ __forceinline__ bool wait_for(uint64_t *bar, unsigned parity, volatile int *quit, unsigned limit)
+{
+    unsigned spins = 0;
+    while (!mbar_try_wait(bar, parity)) {
+        if (++spins > limit || ((spins & 63u) == 0 && *quit)) { *quit = 1; return false; }
+    }
+    return true;
+}
+
+// ---------------------------------------------------------------------- epilogue
+
+// Verdict of the four epilogue warps: true if it is true for all of them.
+__device__ __forceinline__ bool epilogue_all(bool ok)
+{
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.and.pred q, 1, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                 : "=r"(r) : "r"((uint32_t)ok) : "memory");
+    return r != 0;
+}
+
+__device__ __forceinline__ void epilogue_sync() { asm volatile("barrier.cta.sync 1, 128;" ::: "memory"); }
+
+// 32 features (lanes) x 32 rows (v) of the accumulator as bf16 rows: transposed through 2 KB of shared
+// memory of this warp, [32 rows][32 features], then 16-byte stores, four lanes to a row's 64 bytes.
+// The fp32 sum is rounded once.
+__device__ __forceinline__ void store_plain(const KernelParams &p, const Tile &t, int c0, const uint32_t (&v)[32],
+                                            unsigned char *buf, int warp, int lane)
+{
+    __nv_bfloat16 *w = reinterpret_cast<__nv_bfloat16 *>(buf) + lane;
+#pragma unroll
+    for (int j = 0; j < 32; ++j) w[j * 32] = __float2bfloat16_rn(__uint_as_float(v[j]));
+    __syncwarp();
+    const int f = t.feat + warp * 32 + (lane & 3) * 8;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const int r = q * 8 + (lane >> 2);
+        const uint4 o = *reinterpret_cast<const uint4 *>(buf + r * 64 + (lane & 3) * 16);
+        if (c0 + r < t.rows && f < p.N) *reinterpret_cast<uint4 *>(p.y + (size_t)(t.row + c0 + r) * p.N + f) = o;
+    }
+    __syncwarp();
+}
+
+// SwiGLU and quantisation of 128 weight rows (64 pairs of a gate and its up-projection, in even and odd
+// lanes) x 32 rows.  Neighbouring lanes trade one value so that an even lane holds both halves of its
+// pair for the even row of two and an odd lane for the odd one; the 64 results of a row then go through
+// shared memory, two planes (blocks of 32 features) of [32 rows][48], where each half block is taken by
+// one thread, the block's largest magnitude by one shuffle.  Everything before the one rounding to 4 bits is fp32.
+constexpr int kPlanePitch = 48, kPlane = 32 * kPlanePitch + 8;
+
+__device__ __forceinline__ void store_gated(const KernelParams &p, const Tile &t, int c0, const uint32_t (&v)[32], float *buf,
+                                            int warp, int lane)
+{
+    const bool odd = lane & 1;
+    float *w = buf + (warp >> 1) * kPlane + (warp & 1) * 16 + (lane >> 1) + (odd ? kPlanePitch : 0);
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+        const uint32_t other = __shfl_xor_sync(0xffffffffu, odd ? v[2 * j] : v[2 * j + 1], 1);
+        const float gate = __uint_as_float(odd ? other : v[2 * j]), up = __uint_as_float(odd ? v[2 * j + 1] : other);
+        w[2 * j * kPlanePitch] = __fdiv_rn(gate, 1.0f + __expf(-gate)) * up;
+    }
+    epilogue_sync();
+    const int tid = warp * 32 + lane, r = tid >> 2, blk = (tid >> 1) & 1, half = tid & 1;
+    const float4 *src = reinterpret_cast<const float4 *>(buf + blk * kPlane + r * kPlanePitch + half * 16);
+    float x[2][8];
+    uint32_t a = 0;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const float4 f = src[q];
+        const float e[4] = {f.x, f.y, f.z, f.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[q >> 1][(q & 1) * 4 + i] = e[i];
+            a = max(a, __float_as_uint(e[i]) & 0x7fffffffu);
+        }
+    }
+    a = max(a, __shfl_xor_sync(0xffffffffu, a, 1));
+    const uint32_t s = mx_scale_byte(a);
+    const float inv = mx_inverse_scale(s);
+    uint32_t c[2];
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[q][i] *= inv;
+        c[q] = s == 255u ? 0u : mx_pack8(x[q]);
+    }
+    const int cols = p.N / 2, h = t.feat / 2 + blk * 32;       // first feature of the block
+    if (c0 + r < t.rows && h < cols) {
+        const size_t row = (size_t)(t.row + c0 + r);
+        *reinterpret_cast<uint2 *>(p.h_codes + row * (cols / 2) + h / 2 + half * 8) = make_uint2(c[0], c[1]);
+        if (half == 0) p.h_scales[row * mx_scale_pitch(cols) + h / kMxBlock] = (uint8_t)s;
+    }
+    epilogue_sync();
+}
+
+template <int NT, int STAGES, bool GATED>
+__global__ void __launch_bounds__(kThreads, 1)
+k_mx_product(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_a, const KernelParams p)
+{
+    using L = Layout<NT, STAGES>;
+    constexpr int kBox = NT >= 32 ? 32 : 16;                   // rows per TMA load of the row operand
+    extern __shared__ unsigned char raw[];
+    unsigned char *base = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
+    unsigned char *stage = base + L::kStageOff, *sf = base + L::kSfOff, *epi = base + L::kEpiOff;
+    uint64_t *bars = reinterpret_cast<uint64_t *>(base + L::kBarOff);
+    uint64_t *full_tma = bars, *full_sf = bars + STAGES, *empty = bars + 2 * STAGES;
+    uint64_t *acc_full = bars + 3 * STAGES, *acc_empty = acc_full + 2, *drained = acc_full + 4;
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(bars + L::kBars);
+    volatile int *quit = reinterpret_cast<volatile int *>(tmem_slot + 1);
+    int *warp_sums = reinterpret_cast<int *>(epi);             // free before the first epilogue
+    int *ends = reinterpret_cast<int *>(base + L::kEndsOff);
+
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    if (tid == 0) {
+        for (int s = 0; s < STAGES; ++s) { mbar_init(&full_tma[s], 1); mbar_init(&full_sf[s], 2); mbar_init(&empty[s], 1); }
+        for (int b = 0; b < 2; ++b) { mbar_init(&acc_full[b], 1); mbar_init(&acc_empty[b], 4); }
+        mbar_init(drained, 1);
+        *quit = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&map_w));
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&map_a));
+    }
+    if (warp == 5) tmem_alloc(tmem_slot, 512);
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+
+    // inclusive prefix over the slots of their tile counts
+    const int feats = (p.N + kFeat - 1) / kFeat;
+    {
+        const int chunk = (p.P + kThreads - 1) / kThreads;
+        const int s0 = tid * chunk, s1 = min(p.P, s0 + chunk);
+        int sum = 0;
+        for (int s = s0; s < s1; ++s) {
+            int first;
+            sum += feats * row_tiles<NT>(segment(p, s, first));
+            ends[s] = sum;
+        }
+        int incl = sum;
+        for (int off = 1; off < 32; off <<= 1) {
+            const int o = __shfl_up_sync(0xffffffffu, incl, off);
+            if (lane >= off) incl += o;
+        }
+        if (lane == 31) warp_sums[warp] = incl;
+        __syncthreads();
+        int before = incl - sum;
+        for (int w = 0; w < warp; ++w) before += warp_sums[w];
+        for (int s = s0; s < s1; ++s) ends[s] += before;
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+    const int tiles = ends[p.P - 1];
+    const int steps = (p.K + kStageK - 1) / kStageK;
+    constexpr uint32_t kSfCol = 2 * NT;                        // scale columns follow the two accumulators
+    constexpr uint32_t kSfaCols = 8, kSfbCols = 8 * L::kRB;    // per stage parity
+    static_assert(2 * NT + 2 * (kSfaCols + kSfbCols) <= 512, "TMEM columns");
+
+    if (warp == 4) {
+        if (lane == 0) {
+            int issued = 0, s = 0;
+            unsigned parity = 1;                               // a fresh barrier passes the wait for parity 1
+            bool ok = true;
+            for (int i = blockIdx.x; i < tiles && ok; i += gridDim.x) {
+                const Tile t = tile_at<NT>(p, ends, i);
+                if (t.rows <= 0) continue;
+                const int loads = (t.n() + kBox - 1) / kBox;
+                for (int k = 0; k < steps; ++k) {
+                    if (!wait_for(&empty[s], parity, quit, p.spin_limit)) { ok = false; break; }
+                    unsigned char *a = stage + s * L::kStage, *b = a + kATile;
+                    mbar_expect_tx(&full_tma[s], kATile + loads * kBox * kRowBytes);
+                    tma_3d(a, &map_w, k * kRowBytes, t.feat, t.slot, &full_tma[s]);
+                    for (int l = 0; l < loads; ++l)
+                        tma_2d(b + l * kBox * kRowBytes, &map_a, k * kRowBytes, t.row + l * kBox, &full_tma[s]);
+                    ++issued;
+                    if (++s == STAGES) { s = 0; parity ^= 1u; }
+                }
+            }
+            if (!ok) {
+                // loads in flight still land in this CTA's shared memory: a bounded wait for each
+                for (int m = max(0, issued - STAGES); m < issued; ++m) {
+                    unsigned spins = 0;
+                    while (!mbar_try_wait(&full_tma[m % STAGES], (unsigned)(m / STAGES) & 1u) && ++spins < p.spin_limit) {}
+                }
+            }
+        }
+    } else if (warp == 5) {
+        if (lane == 0) {
+            int s = 0, buf = 0;
+            unsigned parity = 0, acc_parity = 1;
+            bool ok = true;
+            uint32_t step_no = 0;
+            for (int i = blockIdx.x; i < tiles && ok; i += gridDim.x) {
+                const Tile t = tile_at<NT>(p, ends, i);
+                if (t.rows <= 0) continue;
+                if (!wait_for(&acc_empty[buf], acc_parity, quit, p.spin_limit)) { ok = false; break; }
+                tc_fence_after();
+                const uint32_t d = tmem + buf * NT;
+                const int n = t.n();
+                for (int k = 0; k < steps; ++k, ++step_no) {
+                    if (!wait_for(&full_tma[s], parity, quit, p.spin_limit) || !wait_for(&full_sf[s], parity, quit, p.spin_limit)) {
+                        ok = false;
+                        break;
+                    }
+                    tc_fence_after();
+                    const uint32_t a = smem_addr(stage + s * L::kStage), b = a + kATile;
+                    const uint32_t sfs = smem_addr(sf + s * L::kSf);
+                    const uint32_t sfa = tmem + kSfCol + (step_no & 1) * (kSfaCols + kSfbCols), sfb = sfa + kSfaCols;
+#pragma unroll
+                    for (int g = 0; g < 2; ++g) {
+                        cp_scales(sfa + 4 * g, desc_scales(sfs + g * 512));
+#pragma unroll
+                        for (int rb = 0; rb < L::kRB; ++rb)
+                            if (rb * 128 < n) cp_scales(sfb + 4 * (g * L::kRB + rb), desc_scales(sfs + L::kSfA + (g * L::kRB + rb) * 512));
+                    }
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        mma_mxf4(d, desc_codes(a + q * 32), desc_codes(b + q * 32), idesc_mxf4(n, (q & 1) * 2), sfa + 4 * (q >> 1),
+                                 sfb + 4 * L::kRB * (q >> 1), k > 0 || q > 0);
+                    mma_commit(&empty[s]);
+                    if (++s == STAGES) { s = 0; parity ^= 1u; }
+                }
+                if (ok) mma_commit(&acc_full[buf]);
+                buf ^= 1;
+                if (buf == 0) acc_parity ^= 1u;
+            }
+            // everything issued has left the tensor core before TMEM is given back
+            mma_commit(drained);
+            unsigned spins = 0;
+            while (!mbar_try_wait(drained, 0) && ++spins < p.spin_limit) {}
+        }
+    } else if (warp >= 6) {
+        // scale rows: lane owns rows q, q + 64, ... of [128 weight rows | NT data rows], 16 bytes (K = 512) at a time
+        constexpr int kMine = (kFeat + NT + 63) / 64;
+        const int q0 = (warp - 6) * 32 + lane;
+        const int pitch = mx_scale_pitch(p.K), used = p.K / kMxBlock;
+        const int pieces = (steps + 1) / 2;
+        const uint32_t one = 0x7f7f7f7fu;                      // scale 1: for rows that do not exist
+        const uint8_t *src[kMine];
+        uint4 cur[kMine], nxt[kMine];
+        auto point = [&](const Tile &t) {
+#pragma unroll
+            for (int m = 0; m < kMine; ++m) {
+                const int q = q0 + 64 * m;
+                src[m] = nullptr;
+                if (q < kFeat) {
+                    if (t.feat + q < p.N) src[m] = p.w_scales + ((size_t)t.slot * p.N + t.feat + q) * pitch;
+                } else if (q - kFeat < t.rows) {
+                    src[m] = p.a_scales + (size_t)(t.row + q - kFeat) * pitch;
+                }
+            }
+        };
+        auto fetch = [&](int piece, uint4 (&v)[kMine]) {
+#pragma unroll
+            for (int m = 0; m < kMine; ++m) {
+                v[m] = make_uint4(one, one, one, one);
+                if (src[m]) v[m] = __ldg(reinterpret_cast<const uint4 *>(src[m]) + piece);
+            }
+            const int left = used - piece * 16;                // scales of this piece; the padding counts as 1
+            if (left < 16) {
+#pragma unroll
+                for (int m = 0; m < kMine; ++m) {
+                    uint32_t w[4] = {v[m].x, v[m].y, v[m].z, v[m].w};
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) {
+                        const int keep = min(4, max(0, left - 4 * x));
+                        const uint32_t mask = keep == 4 ? 0xffffffffu : (1u << (8 * keep)) - 1u;
+                        w[x] = (w[x] & mask) | (one & ~mask);
+                    }
+                    v[m] = make_uint4(w[0], w[1], w[2], w[3]);
+                }
+            }
+        };
+        int s = 0;
+        unsigned parity = 1;
+        bool ok = true;
+        int i = blockIdx.x;
+        Tile t{};
+        auto next_tile = [&]() {                               // the next tile that has rows, from i on
+            for (; i < tiles; i += gridDim.x) {
+                t = tile_at<NT>(p, ends, i);
+                if (t.rows > 0) { point(t); return true; }
+            }
+            return false;
+        };
+        bool have = next_tile();
+        if (have) fetch(0, cur);
+        while (have && ok) {
+            for (int piece = 0; piece < pieces && ok; ++piece) {
+                if (piece + 1 < pieces) {
+                    fetch(piece + 1, nxt);
+                } else {
+                    i += gridDim.x;
+                    have = next_tile();
+                    if (have) fetch(0, nxt);
+                }
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    if (piece * 2 + half >= steps) break;
+                    ok = __all_sync(0xffffffffu, wait_for(&empty[s], parity, quit, p.spin_limit));
+                    if (!ok) break;
+                    unsigned char *dst = sf + s * L::kSf;
+#pragma unroll
+                    for (int m = 0; m < kMine; ++m) {
+                        const int q = q0 + 64 * m;
+                        if (q >= kFeat + NT) continue;
+                        const uint32_t w0 = half ? cur[m].z : cur[m].x, w1 = half ? cur[m].w : cur[m].y;
+                        const bool is_a = q < kFeat;
+                        const int r = is_a ? q : q - kFeat;
+                        unsigned char *at = dst + (is_a ? 0 : L::kSfA + (r >> 7) * 512) + (r & 31) * 16 + ((r >> 5) & 3) * 4;
+                        *reinterpret_cast<uint32_t *>(at) = w0;
+                        *reinterpret_cast<uint32_t *>(at + (is_a ? 512 : L::kRB * 512)) = w1;
+                    }
+                    fence_async_shared();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&full_sf[s]);
+                    if (++s == STAGES) { s = 0; parity ^= 1u; }
+                }
+#pragma unroll
+                for (int m = 0; m < kMine; ++m) cur[m] = nxt[m];
+            }
+        }
+    } else {
+        // epilogue: lane = feature 32 * warp + lane of the tile, columns = rows
+        int buf = 0;
+        unsigned acc_parity = 0;
+        for (int i = blockIdx.x; i < tiles; i += gridDim.x) {
+            const Tile t = tile_at<NT>(p, ends, i);
+            if (t.rows <= 0) continue;
+            bool ok = wait_for(&acc_full[buf], acc_parity, quit, p.spin_limit);
+            ok = GATED ? epilogue_all(ok) : __all_sync(0xffffffffu, ok);   // the gated epilogue's warps meet at barriers
+            if (!ok) break;
+            tc_fence_after();
+            const uint32_t acc = tmem + buf * NT + ((uint32_t)(warp * 32) << 16);
+            for (int c0 = 0; c0 < t.rows; c0 += 32) {
+                uint32_t v[32];
+                tmem_ld32(acc + c0, v);
+                tmem_wait_ld();
+                if (c0 + 32 >= t.rows) {                        // the accumulator has been read: hand it back
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&acc_empty[buf]);
+                }
+                if (GATED) store_gated(p, t, c0, v, reinterpret_cast<float *>(epi), warp, lane);
+                else store_plain(p, t, c0, v, epi + warp * 2048, warp, lane);
+            }
+            buf ^= 1;
+            if (buf == 0) acc_parity ^= 1u;
+        }
+    }
+
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    if (tid == 0 && *quit) report_status(p.ctl, kDevTimeout);
+    if (warp == 5) {
+        tc_fence_after();
+        tmem_dealloc(tmem, 512);
+    }
+}
+
+// ------------------------------------------------------------------------- host
+
+typedef CUresult (*EncodeTiled)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
+                                const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeTiled encode_fn()
+{
+    static std::once_flag once;
+    static EncodeTiled fn = nullptr;
+    std::call_once(once, [] {
+        void *f = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &q) == cudaSuccess &&
+            q == cudaDriverEntryPointSuccess)
+            fn = reinterpret_cast<EncodeTiled>(f);
+    });
+    return fn;
+}
+
+bool encode(CUtensorMap *map, const uint8_t *ptr, int rank, const cuuint64_t *dims, const cuuint64_t *strides, int box_rows)
+{
+    const cuuint32_t box[3] = {(cuuint32_t)kRowBytes, (cuuint32_t)box_rows, 1u}, one[3] = {1u, 1u, 1u};
+    return encode_fn()(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, rank, const_cast<uint8_t *>(ptr), dims, strides, box, one,
+                       CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                       CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int NT, int STAGES, bool GATED>
+cudaError_t launch(const MxProductArgs &a, cudaStream_t st)
+{
+    using L = Layout<NT, STAGES>;
+    static_assert(L::kEndsOff + 1024 + kMaxP * 4 <= 227 * 1024, "shared memory");
+    static_assert(NT >= 32 && NT % 32 == 0, "row boxes and epilogue chunks are 32 rows");
+    const auto kernel = k_mx_product<NT, STAGES, GATED>;
+    static std::once_flag once;
+    static cudaError_t attr = cudaSuccess;
+    std::call_once(once, [&] {
+        attr = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)L::bytes(kMaxP));
+    });
+    if (attr != cudaSuccess) return attr;
+    if (!encode_fn()) return cudaErrorNotSupported;
+    CUtensorMap map_w, map_a;
+    const cuuint64_t row = (cuuint64_t)a.K / 2;
+    const cuuint64_t wd[3] = {row, (cuuint64_t)a.N, (cuuint64_t)a.P}, ws[2] = {row, row * (cuuint64_t)a.N};
+    const cuuint64_t ad[2] = {row, (cuuint64_t)a.rows}, as[1] = {row};
+    if (!encode(&map_w, a.w_codes, 3, wd, ws, kFeat) || !encode(&map_a, a.a_codes, 2, ad, as, 32)) return cudaErrorInvalidValue;
+    KernelParams p;
+    p.a_scales = a.a_scales; p.w_scales = a.w_scales; p.slot_counts = a.slot_counts; p.slot_offsets = a.slot_offsets;
+    p.rows = a.rows; p.P = a.P; p.N = a.N; p.K = a.K; p.y = static_cast<__nv_bfloat16 *>(a.y);
+    p.h_codes = a.h_codes; p.h_scales = a.h_scales; p.ctl = a.ctl; p.spin_limit = a.spin_limit;
+    // no more CTAs than there can be tiles (the counts are on the device)
+    const long long feats = (a.N + kFeat - 1) / kFeat;
+    const long long most = feats * (std::min<long long>(a.P, a.rows) + a.rows / NT);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)std::min<long long>(a.sm_count, most));
+    cfg.blockDim = dim3(kThreads); cfg.dynamicSmemBytes = L::bytes(a.P); cfg.stream = st;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at; cfg.numAttrs = a.pdl ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, kernel, map_w, map_a, p);
+}
+
+template <bool GATED>
+cudaError_t launch_for(const MxProductArgs &a, cudaStream_t st)
+{
+    // Rows per tile: with few rows a slot the weights dominate, and a narrow tile leaves shared memory
+    // for more stages of them; with many rows a wide tile reads the weights fewer times.
+    if (a.rows <= 64ll * a.P) return launch<64, 7, GATED>(a, st);
+    return launch<224, 4, GATED>(a, st);
+}
+
+}  // namespace
+
+namespace moe {
+
+cudaError_t mx_product_launch(const MxProductArgs &a, cudaStream_t st)
+{
+    return a.gated ? launch_for<true>(a, st) : launch_for<false>(a, st);
+}
+
+}  // namespace moe

@@ -1,0 +1,30 @@
+// Launch interface of the experts' products (mx_product.cu), used by the host side in moe_route.cu.
+#pragma once
+
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "device_utils.cuh"
+
+namespace moe {
+
+struct MxProductArgs {
+    const uint8_t *a_codes, *a_scales;   // [rows, K/2], [rows, pitch(K)]
+    long long rows;
+    const int32_t *slot_counts;          // [P] device
+    const int32_t *slot_offsets;         // [P] device
+    int P;
+    const uint8_t *w_codes, *w_scales;   // [P, N, K/2], [P, N, pitch(K)]
+    int N, K;
+    bool gated;                          // SwiGLU over row pairs, 4-bit output of N/2 columns
+    void *y;                             // plain: [rows, N] bf16
+    uint8_t *h_codes, *h_scales;         // gated: [rows, N/4], [rows, pitch(N/2)]
+    Control *ctl;
+    unsigned spin_limit;
+    int sm_count;
+    bool pdl;
+};
+
+cudaError_t mx_product_launch(const MxProductArgs &a, cudaStream_t st);
+
+}  // namespace moe

@@ -1,0 +1,238 @@
+// moe_mx_quantize / moe_mx_dequantize: rows to the microscaled 4-bit format and back.
+//
+// Both are one pass over the data and bound by HBM: n elements of `size` bytes are read (written)
+// once and n * 17/32 bytes written (read).  A thread owns eight consecutive elements (one 16-byte
+// access of a 16-bit type) and four neighbouring lanes own a block, so the block's largest
+// magnitude takes two shuffles and a warp writes 128 contiguous bytes of codes.  Units of eight
+// elements are numbered through all rows, so short rows fill the warps as well as long ones.
+#include "../../include/moe_route.h"
+
+#include "mx_format.cuh"
+
+namespace {
+
+using namespace moe;
+
+constexpr int kRowThreads = 256;
+
+template <int DT> struct Elem;
+template <> struct Elem<MOE_DTYPE_BF16> { static constexpr int kVec = 1; };
+template <> struct Elem<MOE_DTYPE_F16> { static constexpr int kVec = 1; };
+template <> struct Elem<MOE_DTYPE_F32> { static constexpr int kVec = 2; };
+
+template <int DT>
+__device__ __forceinline__ void to_f32(const uint4 (&u)[Elem<DT>::kVec], float (&v)[8])
+{
+    if constexpr (DT == MOE_DTYPE_BF16) {
+        bf16x8_to_f32(u[0], v);
+    } else if constexpr (DT == MOE_DTYPE_F16) {
+        const __half2 *h = reinterpret_cast<const __half2 *>(&u[0]);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const float2 f = __half22float2(h[q]);
+            v[2 * q] = f.x; v[2 * q + 1] = f.y;
+        }
+    } else {
+        const float *f = reinterpret_cast<const float *>(&u[0]);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) v[q] = f[q];
+    }
+}
+
+template <int DT>
+__device__ __forceinline__ void from_f32(const float (&v)[8], uint4 (&u)[Elem<DT>::kVec])
+{
+    if constexpr (DT == MOE_DTYPE_BF16) {
+        __nv_bfloat162 *h = reinterpret_cast<__nv_bfloat162 *>(&u[0]);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) h[q] = __floats2bfloat162_rn(v[2 * q], v[2 * q + 1]);
+    } else if constexpr (DT == MOE_DTYPE_F16) {
+        __half2 *h = reinterpret_cast<__half2 *>(&u[0]);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) h[q] = __floats2half2_rn(v[2 * q], v[2 * q + 1]);
+    } else {
+        float *f = reinterpret_cast<float *>(&u[0]);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) f[q] = v[q];
+    }
+}
+
+struct RowParams {
+    char *x;             // rows of `stride` bytes
+    long long stride;
+    uint8_t *codes;      // [rows, cols/2]
+    uint8_t *scales;     // [rows, pitch]
+    long long units;     // rows * cols/8
+    int upr;             // units per row
+    int pitch;
+};
+
+// The CTA's first unit as (row, unit in the row), by one 64-bit division; a thread's own units
+// then take a 32-bit one each.
+struct UnitBase { long long row; unsigned col; };
+
+__device__ __forceinline__ UnitBase unit_base(const RowParams &p, long long first)
+{
+    UnitBase b;
+    b.row = first / p.upr;
+    b.col = (unsigned)(first - b.row * p.upr);
+    return b;
+}
+
+template <int DT, int UN>
+__global__ void __launch_bounds__(kRowThreads) k_mx_quantize(RowParams p)
+{
+    const long long first = (long long)blockIdx.x * (kRowThreads * UN);
+    const UnitBase b = unit_base(p, first);
+    uint4 in[UN][Elem<DT>::kVec];
+    long long row[UN]; unsigned col[UN];
+#pragma unroll
+    for (int i = 0; i < UN; ++i) {
+        const unsigned off = b.col + i * kRowThreads + threadIdx.x;
+        const unsigned dr = off / (unsigned)p.upr;
+        row[i] = b.row + dr; col[i] = off - dr * p.upr;
+        if (first + i * kRowThreads + threadIdx.x < p.units) {
+            const uint4 *src = reinterpret_cast<const uint4 *>(p.x + row[i] * p.stride) + (size_t)col[i] * Elem<DT>::kVec;
+#pragma unroll
+            for (int q = 0; q < Elem<DT>::kVec; ++q) in[i][q] = __ldg(src + q);
+        } else {
+#pragma unroll
+            for (int q = 0; q < Elem<DT>::kVec; ++q) in[i][q] = make_uint4(0u, 0u, 0u, 0u);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < UN; ++i) {
+        float v[8];
+        uint32_t s;
+        to_f32<DT>(in[i], v);
+        const uint32_t c = mx_quantize8(v, s);
+        const long long u = first + i * kRowThreads + threadIdx.x;
+        if (u < p.units) {
+            reinterpret_cast<uint32_t *>(p.codes)[u] = c;
+            if ((col[i] & 3u) == 0u) {
+                uint8_t *dst = p.scales + row[i] * p.pitch;
+                dst[col[i] >> 2] = (uint8_t)s;
+                if ((int)col[i] + 4 == p.upr)                 // the row's last block also clears the padding
+                    for (int q = p.upr / 4; q < p.pitch; ++q) dst[q] = 0;
+            }
+        }
+    }
+}
+
+template <int DT, int UN>
+__global__ void __launch_bounds__(kRowThreads) k_mx_dequantize(RowParams p)
+{
+    const long long first = (long long)blockIdx.x * (kRowThreads * UN);
+    const UnitBase b = unit_base(p, first);
+    uint32_t c[UN], s[UN];
+    long long row[UN]; unsigned col[UN];
+#pragma unroll
+    for (int i = 0; i < UN; ++i) {
+        const unsigned off = b.col + i * kRowThreads + threadIdx.x;
+        const unsigned dr = off / (unsigned)p.upr;
+        row[i] = b.row + dr; col[i] = off - dr * p.upr;
+        const long long u = first + i * kRowThreads + threadIdx.x;
+        if (u < p.units) {
+            c[i] = __ldg(reinterpret_cast<const uint32_t *>(p.codes) + u);
+            s[i] = __ldg(p.scales + row[i] * p.pitch + (col[i] >> 2));
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < UN; ++i) {
+        if (first + i * kRowThreads + threadIdx.x >= p.units) continue;
+        float v[8];
+        mx_unpack8(c[i], v);
+        const float scale = mx_scale_value(s[i]);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) v[q] *= scale;            // exact unless the type's range is left
+        uint4 o[Elem<DT>::kVec];
+        from_f32<DT>(v, o);
+        uint4 *dst = reinterpret_cast<uint4 *>(p.x + row[i] * p.stride) + (size_t)col[i] * Elem<DT>::kVec;
+#pragma unroll
+        for (int q = 0; q < Elem<DT>::kVec; ++q) dst[q] = o[q];
+    }
+}
+
+bool aligned(const void *p, unsigned a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+
+// Checks shared by both directions; fills everything but the launch shape.
+moe_status fill(RowParams *p, const void *x, int32_t dtype, long long rows, int32_t cols, long long row_stride,
+                const uint8_t *codes, const uint8_t *scales)
+{
+    if (rows < 0 || cols < kMxBlock || cols % kMxBlock != 0) return MOE_ERR_INVALID_ARG;
+    if (dtype != MOE_DTYPE_BF16 && dtype != MOE_DTYPE_F16 && dtype != MOE_DTYPE_F32) return MOE_ERR_INVALID_ARG;
+    const int size = dtype == MOE_DTYPE_F32 ? 4 : 2;
+    if (rows > 1 && row_stride < cols) return MOE_ERR_INVALID_ARG;
+    if (rows > (1ll << 40) / cols) return MOE_ERR_CAPACITY;          // 2^40 elements
+    if (row_stride > (1ll << 40)) return MOE_ERR_INVALID_ARG;
+    p->units = rows * (cols / 8);
+    if (rows == 0) return MOE_OK;
+    if (!x || !codes || !scales || !aligned(x, 16) || !aligned(codes, 16) || !aligned(scales, 16)) return MOE_ERR_INVALID_ARG;
+    if (rows > 1 && (row_stride * size) % 16 != 0) return MOE_ERR_INVALID_ARG;
+    p->x = static_cast<char *>(const_cast<void *>(x));
+    p->stride = row_stride * size;
+    p->codes = const_cast<uint8_t *>(codes);
+    p->scales = const_cast<uint8_t *>(scales);
+    p->upr = cols / 8;
+    p->pitch = mx_scale_pitch(cols);
+    return MOE_OK;
+}
+
+// Four units per thread keep enough bytes in flight to fill HBM; a call too small to give every SM a
+// CTA of four-unit threads is spread over four times as many CTAs instead (one unit per thread).
+constexpr long long kFewUnits = 148ll * 4 * kRowThreads;
+
+template <int DT>
+void launch_quantize(const RowParams &p, cudaStream_t st)
+{
+    if (p.units <= kFewUnits)
+        k_mx_quantize<DT, 1><<<(unsigned)((p.units + kRowThreads - 1) / kRowThreads), kRowThreads, 0, st>>>(p);
+    else
+        k_mx_quantize<DT, 4><<<(unsigned)((p.units + 4 * kRowThreads - 1) / (4 * kRowThreads)), kRowThreads, 0, st>>>(p);
+}
+
+template <int DT>
+void launch_dequantize(const RowParams &p, cudaStream_t st)
+{
+    if (p.units <= kFewUnits)
+        k_mx_dequantize<DT, 1><<<(unsigned)((p.units + kRowThreads - 1) / kRowThreads), kRowThreads, 0, st>>>(p);
+    else
+        k_mx_dequantize<DT, 4><<<(unsigned)((p.units + 4 * kRowThreads - 1) / (4 * kRowThreads)), kRowThreads, 0, st>>>(p);
+}
+
+}  // namespace
+
+extern "C" {
+
+int32_t moe_mx_scale_pitch(int32_t cols)
+{
+    return cols < kMxBlock || cols % kMxBlock != 0 ? 0 : mx_scale_pitch(cols);
+}
+
+moe_status moe_mx_quantize(const void *x, int32_t dtype, int64_t rows, int32_t cols, int64_t row_stride, uint8_t *codes,
+                           uint8_t *scales, void *cuda_stream)
+{
+    RowParams p;
+    const moe_status ms = fill(&p, x, dtype, rows, cols, row_stride, codes, scales);
+    if (ms != MOE_OK || p.units == 0) return ms;
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    if (dtype == MOE_DTYPE_BF16) launch_quantize<MOE_DTYPE_BF16>(p, st);
+    else if (dtype == MOE_DTYPE_F16) launch_quantize<MOE_DTYPE_F16>(p, st);
+    else launch_quantize<MOE_DTYPE_F32>(p, st);
+    return cudaGetLastError() == cudaSuccess ? MOE_OK : MOE_ERR_CUDA;
+}
+
+moe_status moe_mx_dequantize(const uint8_t *codes, const uint8_t *scales, int64_t rows, int32_t cols, void *y, int32_t dtype,
+                             int64_t row_stride, void *cuda_stream)
+{
+    RowParams p;
+    const moe_status ms = fill(&p, y, dtype, rows, cols, row_stride, codes, scales);
+    if (ms != MOE_OK || p.units == 0) return ms;
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    if (dtype == MOE_DTYPE_BF16) launch_dequantize<MOE_DTYPE_BF16>(p, st);
+    else if (dtype == MOE_DTYPE_F16) launch_dequantize<MOE_DTYPE_F16>(p, st);
+    else launch_dequantize<MOE_DTYPE_F32>(p, st);
+    return cudaGetLastError() == cudaSuccess ? MOE_OK : MOE_ERR_CUDA;
+}
+
+}  // extern "C"
