@@ -8,11 +8,12 @@
 // accumulator is [128 lanes = features] x [columns = rows] in TMEM.  K goes in stages of 256 (128
 // bytes of a code row: one 128-byte swizzle span, four MMAs of K = 64).
 //
-// One persistent CTA per SM, eight warps:
-//   warps 0-3   epilogue: TMEM -> registers -> shared memory (transposed) -> HBM
-//   warp 4      TMA loads of the code tiles (weights 128 x 128 B, rows n x 128 B, 128-byte swizzle)
-//   warp 5      scales shared -> TMEM (tcgen05.cp) and the MMAs, from one thread
-//   warps 6-7   scales: 16-byte row pieces HBM -> registers -> the 32 x 16-byte blocks tcgen05.cp wants
+// One persistent CTA per SM:
+//   warps 0-7   epilogue, two groups of four (a warp reads one quarter of the TMEM lanes): TMEM -> registers ->
+//               shared memory (transposed) -> HBM, 32 rows at a time, the groups taking turns
+//   warp 8      TMA loads of the code tiles (weights 128 x 128 B, rows n x 128 B, 128-byte swizzle)
+//   warp 9      scales shared -> TMEM (tcgen05.cp) and the MMAs, from one thread
+//   warps 10-   scales, a warp per 128 rows: HBM -> registers -> the 32 x 16-byte blocks tcgen05.cp wants
 // The accumulator is double buffered, so the epilogue of a tile runs under the products of the next.
 //
 // Tiles are dealt slot by slot, feature tile by feature tile, row tile innermost: CTAs that work at the
@@ -30,12 +31,12 @@ namespace {
 
 using namespace moe;
 
-constexpr int kThreads = 256;
 constexpr int kFeat = 128;                 // features per tile (M)
 constexpr int kStageK = 256;               // elements of K per stage
 constexpr int kRowBytes = kStageK / 2;     // bytes of a code row per stage
 constexpr int kATile = kFeat * kRowBytes;  // 16 KB
 constexpr int kMaxP = 4096;
+constexpr int kEpiWarps = 8, kTmaWarp = kEpiWarps, kMmaWarp = kEpiWarps + 1, kScaleWarp = kEpiWarps + 2;
 
 // ------------------------------------------------------------------ tcgen05 in PTX
 
@@ -82,10 +83,33 @@ __device__ __forceinline__ void tmem_ld32(uint32_t addr, uint32_t (&r)[32])
         : "r"(addr));
 }
 
+// 32 lanes x 32 columns as two halves of 16 lanes in the fragment layout: v[16 h + 4 i + 2 j + e] is lane
+// 16 h + 8 j + (thread / 4), column 8 i + 2 (thread % 4) + e
+__device__ __forceinline__ void tmem_ld_fragments(uint32_t addr, uint32_t (&r)[32])
+{
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+        asm volatile(
+            "tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+            : "=r"(r[16 * h + 0]), "=r"(r[16 * h + 1]), "=r"(r[16 * h + 2]), "=r"(r[16 * h + 3]), "=r"(r[16 * h + 4]),
+              "=r"(r[16 * h + 5]), "=r"(r[16 * h + 6]), "=r"(r[16 * h + 7]), "=r"(r[16 * h + 8]), "=r"(r[16 * h + 9]),
+              "=r"(r[16 * h + 10]), "=r"(r[16 * h + 11]), "=r"(r[16 * h + 12]), "=r"(r[16 * h + 13]), "=r"(r[16 * h + 14]),
+              "=r"(r[16 * h + 15])
+            : "r"(addr + ((uint32_t)(16 * h) << 16)));
+}
+
 __device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+__device__ __forceinline__ bool mbar_test_wait(uint64_t *bar, unsigned parity)
+{
+    unsigned ok;
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                 : "=r"(ok) : "r"(smem_addr(bar)), "r"(parity) : "memory");
+    return ok != 0;
+}
 
 __device__ __forceinline__ void mbar_arrive(uint64_t *bar)
 {
@@ -122,10 +146,18 @@ __device__ __forceinline__ uint64_t desc_scales(uint32_t addr)
 }
 
 // Instruction descriptor of kind::mxf4: A and B e2m1 (1), both K-major, scales ue8m0 (bit 23),
-// N / 8 at bit 17, M / 16 at bit 24.  sf = which half of a 32-bit scale word (0 or 2) belongs to this K = 64.
-__device__ __forceinline__ uint32_t idesc_mxf4(int n, uint32_t sf)
+// N / 8 at bit 17, M / 16 at bit 24; sf_half: which half of a 32-bit scale word (0 or 2) belongs to this K = 64.
+__device__ __forceinline__ uint32_t idesc_mxf4(int n)
 {
-    return (sf << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | (1u << 23) | ((uint32_t)(kFeat >> 4) << 24) | (sf << 29);
+    return (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | (1u << 23) | ((uint32_t)(kFeat >> 4) << 24);
+}
+__device__ __forceinline__ constexpr uint32_t sf_half(uint32_t id) { return (id << 4) | (id << 29); }
+
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+    return r != 0;
 }
 
 // ------------------------------------------------------------------------ tiles
@@ -183,19 +215,26 @@ __device__ __forceinline__ Tile tile_at(const KernelParams &p, const int *ends, 
     return t;
 }
 
+// Shared memory of the epilogue: a group's two planes of the gated form, shared out to its four warps; the
+// plain form needs 2 KB per warp.
+constexpr int kPlane = 32 * 32 + 8;
+constexpr int kEpiWarpBytes = (2 * kPlane * 4 / 4 + 127) / 128 * 128;
+static_assert(kEpiWarpBytes >= 2048, "plain epilogue");
+
 template <int NT, int STAGES>
 struct Layout {
     static constexpr int kBTile = NT * kRowBytes;
     static constexpr int kRB = (NT + 127) / 128;              // 128-row scale blocks of the row operand
+    static constexpr int kThreads = 32 * (kEpiWarps + 3 + kRB);
     static constexpr int kSfA = 2 * 512, kSfB = 2 * kRB * 512;
     static constexpr int kStage = kATile + kBTile;            // multiples of 1024: swizzle alignment
     static constexpr int kSf = kSfA + kSfB;
     static constexpr int kStageOff = 0;
     static constexpr int kSfOff = STAGES * kStage;
     static constexpr int kEpiOff = kSfOff + STAGES * kSf;
-    static constexpr int kEpiBytes = 2 * (32 * 48 + 8) * 4;   // gated: two planes; plain: 4 x 2 KB
+    static constexpr int kEpiBytes = kEpiWarps * kEpiWarpBytes;
     static constexpr int kBarOff = kEpiOff + kEpiBytes;
-    static constexpr int kBars = 3 * STAGES + 5;
+    static constexpr int kBars = 2 * STAGES + 5;
     static constexpr int kEndsOff = kBarOff + ((kBars * 8 + 32 + 15) & ~15);
     static size_t bytes(int P) { return 1024 + kEndsOff + (size_t)P * 4; }
 };
@@ -212,32 +251,48 @@ __device__ __forceinline__ bool wait_for(uint64_t *bar, unsigned parity, volatil
 
 // ---------------------------------------------------------------------- epilogue
 
-// Verdict of the four epilogue warps: true if it is true for all of them.
-__device__ __forceinline__ bool epilogue_all(bool ok)
+// Verdict of the four warps of an epilogue group: true if it is true for all of them.
+__device__ __forceinline__ bool group_all(int group, bool ok)
 {
     uint32_t r;
-    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.and.pred q, 1, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
-                 : "=r"(r) : "r"((uint32_t)ok) : "memory");
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.and.pred q, %2, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                 : "=r"(r) : "r"((uint32_t)ok), "r"(group + 1) : "memory");
     return r != 0;
 }
 
-__device__ __forceinline__ void epilogue_sync() { asm volatile("barrier.cta.sync 1, 128;" ::: "memory"); }
+__device__ __forceinline__ void group_sync(int group) { asm volatile("barrier.cta.sync %0, 128;" ::"r"(group + 1) : "memory"); }
 
-// 32 features (lanes) x 32 rows (v) of the accumulator as bf16 rows: transposed through 2 KB of shared
-// memory of this warp, [32 rows][32 features], then 16-byte stores, four lanes to a row's 64 bytes.
-// The fp32 sum is rounded once.
+// 32 features x 32 rows of the accumulator as bf16 rows, through 2 KB of shared memory of this warp,
+// [32 rows][32 features].  The accumulator is read in the fragment layout (lane / 4 = feature, two
+// neighbouring rows per register pair), so that a pair is one bf16x2 and stmatrix writes it transposed: 16
+// conversions and 4 stores where one value at a time takes 32 of each.  The 16-byte pieces of a row are
+// swizzled over the banks; they leave as 16-byte stores, four lanes to a row's 64 bytes.  The fp32 sum is
+// rounded once.
 __device__ __forceinline__ void store_plain(const KernelParams &p, const Tile &t, int c0, const uint32_t (&v)[32],
-                                            unsigned char *buf, int warp, int lane)
+                                            unsigned char *buf, int quarter, int lane)
 {
-    __nv_bfloat16 *w = reinterpret_cast<__nv_bfloat16 *>(buf) + lane;
+    const uint32_t base = smem_addr(buf);
 #pragma unroll
-    for (int j = 0; j < 32; ++j) w[j * 32] = __float2bfloat16_rn(__uint_as_float(v[j]));
+    for (int i = 0; i < 4; ++i) {
+        uint32_t m[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {                          // features 8q .. 8q + 7
+            const int at = (q >> 1) * 16 + 4 * i + (q & 1) * 2;
+            const __nv_bfloat162 h = __floats2bfloat162_rn(__uint_as_float(v[at]), __uint_as_float(v[at + 1]));
+            m[q] = *reinterpret_cast<const uint32_t *>(&h);
+        }
+        const int r = 8 * i + (lane & 7);                      // lane names row r, piece lane / 8
+        const uint32_t at = base + r * 64 + ((((uint32_t)lane >> 3) ^ ((r >> 1) & 3)) << 4);
+        asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(m[0]), "r"(m[1]),
+                     "r"(m[2]), "r"(m[3])
+                     : "memory");
+    }
     __syncwarp();
-    const int f = t.feat + warp * 32 + (lane & 3) * 8;
+    const int f = t.feat + quarter * 32 + (lane & 3) * 8;
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
         const int r = q * 8 + (lane >> 2);
-        const uint4 o = *reinterpret_cast<const uint4 *>(buf + r * 64 + (lane & 3) * 16);
+        const uint4 o = *reinterpret_cast<const uint4 *>(buf + r * 64 + (((lane & 3) ^ ((r >> 1) & 3)) << 4));
         if (c0 + r < t.rows && f < p.N) *reinterpret_cast<uint4 *>(p.y + (size_t)(t.row + c0 + r) * p.N + f) = o;
     }
     __syncwarp();
@@ -246,24 +301,31 @@ __device__ __forceinline__ void store_plain(const KernelParams &p, const Tile &t
 // SwiGLU and quantisation of 128 weight rows (64 pairs of a gate and its up-projection, in even and odd
 // lanes) x 32 rows.  Neighbouring lanes trade one value so that an even lane holds both halves of its
 // pair for the even row of two and an odd lane for the odd one; the 64 results of a row then go through
-// shared memory, two planes (blocks of 32 features) of [32 rows][48], where each half block is taken by
-// one thread, the block's largest magnitude by one shuffle.  Everything before the one rounding to 4 bits is fp32.
-constexpr int kPlanePitch = 48, kPlane = 32 * kPlanePitch + 8;
+// shared memory, two planes (blocks of 32 features) of [32 rows][32] with the halves of odd rows swapped
+// (no two lanes of a store meet in a bank), where each half block is taken by one thread and the block's
+// largest magnitude by one shuffle.  Everything before the one rounding to 4 bits is fp32; exp and the
+// reciprocal are the hardware's approximations (2 and 1 units in the last place), far below a 4-bit step.
+__device__ __forceinline__ float silu(float g)
+{
+    float r;
+    asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(1.0f + __expf(-g)));
+    return g * r;
+}
 
 __device__ __forceinline__ void store_gated(const KernelParams &p, const Tile &t, int c0, const uint32_t (&v)[32], float *buf,
-                                            int warp, int lane)
+                                            int group, int quarter, int lane)
 {
     const bool odd = lane & 1;
-    float *w = buf + (warp >> 1) * kPlane + (warp & 1) * 16 + (lane >> 1) + (odd ? kPlanePitch : 0);
+    float *w = buf + (quarter >> 1) * kPlane + ((((quarter & 1) ^ (odd ? 1 : 0)) << 4) | (lane >> 1)) + (odd ? 32 : 0);
 #pragma unroll
     for (int j = 0; j < 16; ++j) {
         const uint32_t other = __shfl_xor_sync(0xffffffffu, odd ? v[2 * j] : v[2 * j + 1], 1);
         const float gate = __uint_as_float(odd ? other : v[2 * j]), up = __uint_as_float(odd ? v[2 * j + 1] : other);
-        w[2 * j * kPlanePitch] = __fdiv_rn(gate, 1.0f + __expf(-gate)) * up;
+        w[64 * j] = silu(gate) * up;
     }
-    epilogue_sync();
-    const int tid = warp * 32 + lane, r = tid >> 2, blk = (tid >> 1) & 1, half = tid & 1;
-    const float4 *src = reinterpret_cast<const float4 *>(buf + blk * kPlane + r * kPlanePitch + half * 16);
+    group_sync(group);
+    const int tid = quarter * 32 + lane, r = tid >> 2, blk = (tid >> 1) & 1, half = tid & 1;
+    const float4 *src = reinterpret_cast<const float4 *>(buf + blk * kPlane + r * 32 + ((half ^ (r & 1)) << 4));
     float x[2][8];
     uint32_t a = 0;
 #pragma unroll
@@ -276,6 +338,7 @@ __device__ __forceinline__ void store_gated(const KernelParams &p, const Tile &t
             a = max(a, __float_as_uint(e[i]) & 0x7fffffffu);
         }
     }
+    group_sync(group);                                         // the planes are free for the next 32 rows
     a = max(a, __shfl_xor_sync(0xffffffffu, a, 1));
     const uint32_t s = mx_scale_byte(a);
     const float inv = mx_inverse_scale(s);
@@ -292,11 +355,10 @@ __device__ __forceinline__ void store_gated(const KernelParams &p, const Tile &t
         *reinterpret_cast<uint2 *>(p.h_codes + row * (cols / 2) + h / 2 + half * 8) = make_uint2(c[0], c[1]);
         if (half == 0) p.h_scales[row * mx_scale_pitch(cols) + h / kMxBlock] = (uint8_t)s;
     }
-    epilogue_sync();
 }
 
 template <int NT, int STAGES, bool GATED>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(Layout<NT, STAGES>::kThreads, 1)
 k_mx_product(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_a, const KernelParams p)
 {
     using L = Layout<NT, STAGES>;
@@ -305,8 +367,8 @@ k_mx_product(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
     unsigned char *base = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
     unsigned char *stage = base + L::kStageOff, *sf = base + L::kSfOff, *epi = base + L::kEpiOff;
     uint64_t *bars = reinterpret_cast<uint64_t *>(base + L::kBarOff);
-    uint64_t *full_tma = bars, *full_sf = bars + STAGES, *empty = bars + 2 * STAGES;
-    uint64_t *acc_full = bars + 3 * STAGES, *acc_empty = acc_full + 2, *drained = acc_full + 4;
+    uint64_t *full = bars, *empty = bars + STAGES;
+    uint64_t *acc_full = bars + 2 * STAGES, *acc_empty = acc_full + 2, *drained = acc_full + 4;
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(bars + L::kBars);
     volatile int *quit = reinterpret_cast<volatile int *>(tmem_slot + 1);
     int *warp_sums = reinterpret_cast<int *>(epi);             // free before the first epilogue
@@ -314,22 +376,22 @@ k_mx_product(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     if (tid == 0) {
-        for (int s = 0; s < STAGES; ++s) { mbar_init(&full_tma[s], 1); mbar_init(&full_sf[s], 2); mbar_init(&empty[s], 1); }
-        for (int b = 0; b < 2; ++b) { mbar_init(&acc_full[b], 1); mbar_init(&acc_empty[b], 4); }
+        for (int s = 0; s < STAGES; ++s) { mbar_init(&full[s], 2 + L::kRB); mbar_init(&empty[s], 1); }
+        for (int b = 0; b < 2; ++b) { mbar_init(&acc_full[b], 1); mbar_init(&acc_empty[b], kEpiWarps); }
         mbar_init(drained, 1);
         *quit = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(&map_w));
         asm volatile("prefetch.tensormap [%0];" ::"l"(&map_a));
     }
-    if (warp == 5) tmem_alloc(tmem_slot, 512);
+    if (warp == kMmaWarp) tmem_alloc(tmem_slot, 512);
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
 
     // inclusive prefix over the slots of their tile counts
     const int feats = (p.N + kFeat - 1) / kFeat;
     {
-        const int chunk = (p.P + kThreads - 1) / kThreads;
+        const int chunk = (p.P + L::kThreads - 1) / L::kThreads;
         const int s0 = tid * chunk, s1 = min(p.P, s0 + chunk);
         int sum = 0;
         for (int s = s0; s < s1; ++s) {
@@ -358,194 +420,202 @@ k_mx_product(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
     constexpr uint32_t kSfaCols = 8, kSfbCols = 8 * L::kRB;    // per stage parity
     static_assert(2 * NT + 2 * (kSfaCols + kSfbCols) <= 512, "TMEM columns");
 
-    if (warp == 4) {
-        if (lane == 0) {
-            int issued = 0, s = 0;
-            unsigned parity = 1;                               // a fresh barrier passes the wait for parity 1
-            bool ok = true;
-            for (int i = blockIdx.x; i < tiles && ok; i += gridDim.x) {
-                const Tile t = tile_at<NT>(p, ends, i);
-                if (t.rows <= 0) continue;
-                const int loads = (t.n() + kBox - 1) / kBox;
-                for (int k = 0; k < steps; ++k) {
-                    if (!wait_for(&empty[s], parity, quit, p.spin_limit)) { ok = false; break; }
-                    unsigned char *a = stage + s * L::kStage, *b = a + kATile;
-                    mbar_expect_tx(&full_tma[s], kATile + loads * kBox * kRowBytes);
-                    tma_3d(a, &map_w, k * kRowBytes, t.feat, t.slot, &full_tma[s]);
+    // The two issuing warps run their loops with all lanes, so that everything the asynchronous instructions
+    // take is uniform over the warp, and issue from one elected lane.  (Behind a plain `lane == 0` the
+    // compiler cannot know that one lane is left and serialises every such instruction over the warp: 80
+    // cycles each, 700-1300 per stage, which bound the whole kernel.)
+    if (warp == kTmaWarp) {
+        int issued = 0, s = 0;
+        unsigned parity = 1;                                   // a fresh barrier passes the wait for parity 1
+        bool ok = true;
+        for (int i = blockIdx.x; i < tiles && ok; i += gridDim.x) {
+            const Tile t = tile_at<NT>(p, ends, i);
+            if (t.rows <= 0) continue;
+            const int loads = (t.n() + kBox - 1) / kBox;
+            for (int k = 0; k < steps; ++k) {
+                ok = __all_sync(0xffffffffu, wait_for(&empty[s], parity, quit, p.spin_limit));
+                if (!ok) break;
+                unsigned char *a = stage + s * L::kStage, *b = a + kATile;
+                if (elect_one()) {
+                    mbar_expect_tx(&full[s], kATile + loads * kBox * kRowBytes);
+                    tma_3d(a, &map_w, k * kRowBytes, t.feat, t.slot, &full[s]);
                     for (int l = 0; l < loads; ++l)
-                        tma_2d(b + l * kBox * kRowBytes, &map_a, k * kRowBytes, t.row + l * kBox, &full_tma[s]);
-                    ++issued;
-                    if (++s == STAGES) { s = 0; parity ^= 1u; }
+                        tma_2d(b + l * kBox * kRowBytes, &map_a, k * kRowBytes, t.row + l * kBox, &full[s]);
                 }
-            }
-            if (!ok) {
-                // loads in flight still land in this CTA's shared memory: a bounded wait for each
-                for (int m = max(0, issued - STAGES); m < issued; ++m) {
-                    unsigned spins = 0;
-                    while (!mbar_try_wait(&full_tma[m % STAGES], (unsigned)(m / STAGES) & 1u) && ++spins < p.spin_limit) {}
-                }
+                __syncwarp();
+                ++issued;
+                if (++s == STAGES) { s = 0; parity ^= 1u; }
             }
         }
-    } else if (warp == 5) {
-        if (lane == 0) {
-            int s = 0, buf = 0;
-            unsigned parity = 0, acc_parity = 1;
-            bool ok = true;
-            uint32_t step_no = 0;
-            for (int i = blockIdx.x; i < tiles && ok; i += gridDim.x) {
-                const Tile t = tile_at<NT>(p, ends, i);
-                if (t.rows <= 0) continue;
-                if (!wait_for(&acc_empty[buf], acc_parity, quit, p.spin_limit)) { ok = false; break; }
+        if (!ok) {
+            // loads in flight still land in this CTA's shared memory: a bounded wait for each (their barriers also
+            // count the scales, so they may not complete, but the wait outlasts any copy)
+            for (int m = max(0, issued - STAGES); m < issued; ++m) {
+                unsigned spins = 0;
+                while (!mbar_try_wait(&full[m % STAGES], (unsigned)(m / STAGES) & 1u) && ++spins < p.spin_limit) {}
+            }
+        }
+    } else if (warp == kMmaWarp) {
+        int s = 0, buf = 0;
+        unsigned parity = 0, acc_parity = 1, step_no = 0;
+        bool ok = true;
+        const uint64_t stage_desc = desc_codes(smem_addr(stage)), sf_desc = desc_scales(smem_addr(sf));
+        for (int i = blockIdx.x; i < tiles && ok; i += gridDim.x) {
+            const Tile t = tile_at<NT>(p, ends, i);
+            if (t.rows <= 0) continue;
+            ok = __all_sync(0xffffffffu, wait_for(&acc_empty[buf], acc_parity, quit, p.spin_limit));
+            if (!ok) break;
+            tc_fence_after();
+            const uint32_t d = tmem + buf * NT;
+            const int n = t.n();
+            const uint32_t idesc = idesc_mxf4(n);
+            bool ready = mbar_test_wait(&full[s], parity);
+            for (int k = 0; k < steps; ++k, ++step_no) {
+                ok = __all_sync(0xffffffffu, ready || wait_for(&full[s], parity, quit, p.spin_limit));
+                if (!ok) break;
                 tc_fence_after();
-                const uint32_t d = tmem + buf * NT;
-                const int n = t.n();
-                for (int k = 0; k < steps; ++k, ++step_no) {
-                    if (!wait_for(&full_tma[s], parity, quit, p.spin_limit) || !wait_for(&full_sf[s], parity, quit, p.spin_limit)) {
-                        ok = false;
-                        break;
-                    }
-                    tc_fence_after();
-                    const uint32_t a = smem_addr(stage + s * L::kStage), b = a + kATile;
-                    const uint32_t sfs = smem_addr(sf + s * L::kSf);
-                    const uint32_t sfa = tmem + kSfCol + (step_no & 1) * (kSfaCols + kSfbCols), sfb = sfa + kSfaCols;
+                // ask for the next stage's barrier now: the answer arrives while this stage is issued
+                const int s_next = s + 1 == STAGES ? 0 : s + 1;
+                ready = mbar_test_wait(&full[s_next], s_next ? parity : parity ^ 1u);
+                // descriptors count in 16-byte units
+                const uint64_t a = stage_desc + (uint32_t)(s * (L::kStage >> 4)), b = a + (kATile >> 4);
+                const uint64_t sfs = sf_desc + (uint32_t)(s * (L::kSf >> 4));
+                const uint32_t sfa = tmem + kSfCol + (step_no & 1) * (kSfaCols + kSfbCols), sfb = sfa + kSfaCols;
+                if (elect_one()) {
 #pragma unroll
                     for (int g = 0; g < 2; ++g) {
-                        cp_scales(sfa + 4 * g, desc_scales(sfs + g * 512));
-#pragma unroll
-                        for (int rb = 0; rb < L::kRB; ++rb)
-                            if (rb * 128 < n) cp_scales(sfb + 4 * (g * L::kRB + rb), desc_scales(sfs + L::kSfA + (g * L::kRB + rb) * 512));
+                        cp_scales(sfa + 4 * g, sfs + g * 32);
+                        cp_scales(sfb + 4 * g * L::kRB, sfs + (L::kSfA >> 4) + g * L::kRB * 32);
+                        if (L::kRB == 2 && n > 128) cp_scales(sfb + 4 * (g * L::kRB + 1), sfs + (L::kSfA >> 4) + (g * L::kRB + 1) * 32);
                     }
 #pragma unroll
                     for (int q = 0; q < 4; ++q)
-                        mma_mxf4(d, desc_codes(a + q * 32), desc_codes(b + q * 32), idesc_mxf4(n, (q & 1) * 2), sfa + 4 * (q >> 1),
-                                 sfb + 4 * L::kRB * (q >> 1), k > 0 || q > 0);
+                        mma_mxf4(d, a + 2 * q, b + 2 * q, idesc | sf_half((q & 1) * 2), sfa + 4 * (q >> 1), sfb + 4 * L::kRB * (q >> 1),
+                                 k > 0 || q > 0);
                     mma_commit(&empty[s]);
-                    if (++s == STAGES) { s = 0; parity ^= 1u; }
+                    if (k == steps - 1) mma_commit(&acc_full[buf]);
                 }
-                if (ok) mma_commit(&acc_full[buf]);
-                buf ^= 1;
-                if (buf == 0) acc_parity ^= 1u;
+                __syncwarp();
+                s = s_next;
+                if (s == 0) parity ^= 1u;
             }
-            // everything issued has left the tensor core before TMEM is given back
-            mma_commit(drained);
-            unsigned spins = 0;
-            while (!mbar_try_wait(drained, 0) && ++spins < p.spin_limit) {}
+            buf ^= 1;
+            if (buf == 0) acc_parity ^= 1u;
         }
-    } else if (warp >= 6) {
-        // scale rows: lane owns rows q, q + 64, ... of [128 weight rows | NT data rows], 16 bytes (K = 512) at a time
-        constexpr int kMine = (kFeat + NT + 63) / 64;
-        const int q0 = (warp - 6) * 32 + lane;
-        const int pitch = mx_scale_pitch(p.K), used = p.K / kMxBlock;
+        // everything issued has left the tensor core before TMEM is given back
+        if (elect_one()) mma_commit(drained);
+        __syncwarp();
+        unsigned spins = 0;
+        while (!mbar_try_wait(drained, 0) && ++spins < p.spin_limit) {}
+    } else if (warp >= kScaleWarp) {
+        // A warp per 128-row block of scales: the weight rows, then the data rows.  Lane l owns rows l, l + 32,
+        // l + 64 and l + 96 and reads 16 bytes of each at a time (K = 512, two stages), kPieces of them ahead.
+        // tcgen05.cp wants, for each K = 128, [32 lanes][4 rows][4 scales]: word w of the lane's four rows is
+        // one 16-byte store, so nothing is transposed and no two lanes meet in a bank.
+        constexpr int kPieces = 4;
+        const int blk = warp - kScaleWarp;                            // 0: weights; 1 + rb: data rows [128 rb, 128 rb + 128)
+        const int pitch = mx_scale_pitch(p.K);
         const int pieces = (steps + 1) / 2;
+        const int left = p.K / kMxBlock - (pieces - 1) * 16;   // scales of the last piece; the padding counts as 1
         const uint32_t one = 0x7f7f7f7fu;                      // scale 1: for rows that do not exist
-        const uint8_t *src[kMine];
-        uint4 cur[kMine], nxt[kMine];
-        auto point = [&](const Tile &t) {
+        uint4 ring[kPieces][4];
+        bool valid[kPieces];
+        const uint8_t *src[4];
+        int i = blockIdx.x, piece = 0;
+        auto fetch = [&](uint4 (&v)[4]) {                      // the next piece, over all tiles; false when there is none
+            if (piece == 0) {
+                Tile t{};
+                for (; i < tiles; i += gridDim.x) {
+                    t = tile_at<NT>(p, ends, i);
+                    if (t.rows > 0) break;
+                }
+                if (i >= tiles) return false;
 #pragma unroll
-            for (int m = 0; m < kMine; ++m) {
-                const int q = q0 + 64 * m;
-                src[m] = nullptr;
-                if (q < kFeat) {
-                    if (t.feat + q < p.N) src[m] = p.w_scales + ((size_t)t.slot * p.N + t.feat + q) * pitch;
-                } else if (q - kFeat < t.rows) {
-                    src[m] = p.a_scales + (size_t)(t.row + q - kFeat) * pitch;
+                for (int g = 0; g < 4; ++g) {
+                    const int r = lane + 32 * g + (blk > 0 ? (blk - 1) * 128 : 0);
+                    if (blk == 0) src[g] = t.feat + r < p.N ? p.w_scales + ((size_t)t.slot * p.N + t.feat + r) * pitch : nullptr;
+                    else src[g] = r < t.rows ? p.a_scales + (size_t)(t.row + r) * pitch : nullptr;
                 }
             }
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+                v[g] = src[g] ? __ldg(reinterpret_cast<const uint4 *>(src[g]) + piece) : make_uint4(one, one, one, one);
+            if (++piece == pieces) { piece = 0; i += gridDim.x; }
+            return true;
         };
-        auto fetch = [&](int piece, uint4 (&v)[kMine]) {
-#pragma unroll
-            for (int m = 0; m < kMine; ++m) {
-                v[m] = make_uint4(one, one, one, one);
-                if (src[m]) v[m] = __ldg(reinterpret_cast<const uint4 *>(src[m]) + piece);
-            }
-            const int left = used - piece * 16;                // scales of this piece; the padding counts as 1
-            if (left < 16) {
-#pragma unroll
-                for (int m = 0; m < kMine; ++m) {
-                    uint32_t w[4] = {v[m].x, v[m].y, v[m].z, v[m].w};
-#pragma unroll
-                    for (int x = 0; x < 4; ++x) {
-                        const int keep = min(4, max(0, left - 4 * x));
-                        const uint32_t mask = keep == 4 ? 0xffffffffu : (1u << (8 * keep)) - 1u;
-                        w[x] = (w[x] & mask) | (one & ~mask);
-                    }
-                    v[m] = make_uint4(w[0], w[1], w[2], w[3]);
-                }
-            }
-        };
-        int s = 0;
+        int s = 0, at = 0;
         unsigned parity = 1;
         bool ok = true;
-        int i = blockIdx.x;
-        Tile t{};
-        auto next_tile = [&]() {                               // the next tile that has rows, from i on
-            for (; i < tiles; i += gridDim.x) {
-                t = tile_at<NT>(p, ends, i);
-                if (t.rows > 0) { point(t); return true; }
-            }
-            return false;
-        };
-        bool have = next_tile();
-        if (have) fetch(0, cur);
-        while (have && ok) {
-            for (int piece = 0; piece < pieces && ok; ++piece) {
-                if (piece + 1 < pieces) {
-                    fetch(piece + 1, nxt);
-                } else {
-                    i += gridDim.x;
-                    have = next_tile();
-                    if (have) fetch(0, nxt);
+#pragma unroll
+        for (int d = 0; d < kPieces; ++d) valid[d] = fetch(ring[d]);
+        while (ok && valid[0]) {
+#pragma unroll
+            for (int d = 0; d < kPieces; ++d) {
+                if (!ok || !valid[d]) { ok = false; break; }
+                uint4 (&v)[4] = ring[d];
+                if (at == pieces - 1 && left < 16) {
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) {
+                        uint32_t w[4] = {v[g].x, v[g].y, v[g].z, v[g].w};
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) {
+                            const int keep = min(4, max(0, left - 4 * x));
+                            const uint32_t mask = keep == 4 ? 0xffffffffu : (1u << (8 * keep)) - 1u;
+                            w[x] = (w[x] & mask) | (one & ~mask);
+                        }
+                        v[g] = make_uint4(w[0], w[1], w[2], w[3]);
+                    }
                 }
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {
-                    if (piece * 2 + half >= steps) break;
+                    if (at * 2 + half >= steps) break;
                     ok = __all_sync(0xffffffffu, wait_for(&empty[s], parity, quit, p.spin_limit));
                     if (!ok) break;
-                    unsigned char *dst = sf + s * L::kSf;
-#pragma unroll
-                    for (int m = 0; m < kMine; ++m) {
-                        const int q = q0 + 64 * m;
-                        if (q >= kFeat + NT) continue;
-                        const uint32_t w0 = half ? cur[m].z : cur[m].x, w1 = half ? cur[m].w : cur[m].y;
-                        const bool is_a = q < kFeat;
-                        const int r = is_a ? q : q - kFeat;
-                        unsigned char *at = dst + (is_a ? 0 : L::kSfA + (r >> 7) * 512) + (r & 31) * 16 + ((r >> 5) & 3) * 4;
-                        *reinterpret_cast<uint32_t *>(at) = w0;
-                        *reinterpret_cast<uint32_t *>(at + (is_a ? 512 : L::kRB * 512)) = w1;
+                    unsigned char *dst = sf + s * L::kSf + (blk == 0 ? 0 : L::kSfA + (blk - 1) * 512) + lane * 16;
+                    const int next = blk == 0 ? 512 : L::kRB * 512;
+                    if (half == 0) {
+                        *reinterpret_cast<uint4 *>(dst) = make_uint4(v[0].x, v[1].x, v[2].x, v[3].x);
+                        *reinterpret_cast<uint4 *>(dst + next) = make_uint4(v[0].y, v[1].y, v[2].y, v[3].y);
+                    } else {
+                        *reinterpret_cast<uint4 *>(dst) = make_uint4(v[0].z, v[1].z, v[2].z, v[3].z);
+                        *reinterpret_cast<uint4 *>(dst + next) = make_uint4(v[0].w, v[1].w, v[2].w, v[3].w);
                     }
                     fence_async_shared();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(&full_sf[s]);
+                    if (lane == 0) mbar_arrive(&full[s]);
                     if (++s == STAGES) { s = 0; parity ^= 1u; }
                 }
-#pragma unroll
-                for (int m = 0; m < kMine; ++m) cur[m] = nxt[m];
+                if (++at == pieces) at = 0;
+                valid[d] = fetch(v);
             }
         }
     } else {
-        // epilogue: lane = feature 32 * warp + lane of the tile, columns = rows
+        // epilogue: TMEM lane = feature of the tile, column = row
+        const int group = warp >> 2, quarter = warp & 3;
         int buf = 0;
         unsigned acc_parity = 0;
         for (int i = blockIdx.x; i < tiles; i += gridDim.x) {
             const Tile t = tile_at<NT>(p, ends, i);
             if (t.rows <= 0) continue;
             bool ok = wait_for(&acc_full[buf], acc_parity, quit, p.spin_limit);
-            ok = GATED ? epilogue_all(ok) : __all_sync(0xffffffffu, ok);   // the gated epilogue's warps meet at barriers
+            ok = GATED ? group_all(group, ok) : __all_sync(0xffffffffu, ok);   // the gated epilogue's warps meet at barriers
             if (!ok) break;
             tc_fence_after();
-            const uint32_t acc = tmem + buf * NT + ((uint32_t)(warp * 32) << 16);
-            for (int c0 = 0; c0 < t.rows; c0 += 32) {
+            const uint32_t acc = tmem + buf * NT + ((uint32_t)(quarter * 32) << 16);
+            for (int c0 = group * 32; c0 < t.rows; c0 += 64) {
                 uint32_t v[32];
-                tmem_ld32(acc + c0, v);
+                if (GATED) tmem_ld32(acc + c0, v);
+                else tmem_ld_fragments(acc + c0, v);
                 tmem_wait_ld();
-                if (c0 + 32 >= t.rows) {                        // the accumulator has been read: hand it back
+                if (c0 + 64 >= t.rows) {                        // this warp's last look at the accumulator
                     tc_fence_before();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&acc_empty[buf]);
                 }
-                if (GATED) store_gated(p, t, c0, v, reinterpret_cast<float *>(epi), warp, lane);
-                else store_plain(p, t, c0, v, epi + warp * 2048, warp, lane);
+                if (GATED) store_gated(p, t, c0, v, reinterpret_cast<float *>(epi + group * 4 * kEpiWarpBytes), group, quarter, lane);
+                else store_plain(p, t, c0, v, epi + warp * kEpiWarpBytes, quarter, lane);
             }
+            if (group * 32 >= t.rows && lane == 0) mbar_arrive(&acc_empty[buf]);
             buf ^= 1;
             if (buf == 0) acc_parity ^= 1u;
         }
@@ -555,7 +625,7 @@ k_mx_product(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
     tc_fence_before();
     __syncthreads();
     if (tid == 0 && *quit) report_status(p.ctl, kDevTimeout);
-    if (warp == 5) {
+    if (warp == kMmaWarp) {
         tc_fence_after();
         tmem_dealloc(tmem, 512);
     }
@@ -617,7 +687,7 @@ cudaError_t launch(const MxProductArgs &a, cudaStream_t st)
     const long long most = feats * (std::min<long long>(a.P, a.rows) + a.rows / NT);
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)std::min<long long>(a.sm_count, most));
-    cfg.blockDim = dim3(kThreads); cfg.dynamicSmemBytes = L::bytes(a.P); cfg.stream = st;
+    cfg.blockDim = dim3(L::kThreads); cfg.dynamicSmemBytes = L::bytes(a.P); cfg.stream = st;
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;
