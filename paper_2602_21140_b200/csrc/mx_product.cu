@@ -221,6 +221,40 @@ constexpr int kPlane = 32 * 32 + 8;
 constexpr int kEpiWarpBytes = (2 * kPlane * 4 / 4 + 127) / 128 * 128;
 static_assert(kEpiWarpBytes >= 2048, "plain epilogue");
 
+// The tiles of a CTA, blockIdx.x, + gridDim.x, ..., as a warp sees them.  Finding a tile is a chain of
+// dependent reads, so the lanes find the next 32 of them side by side and hand them out one by one.
+template <int NT>
+struct TileStream {
+    const KernelParams &p;
+    const int *ends;
+    const int tiles;
+    int base, at;
+    Tile mine;
+    __device__ TileStream(const KernelParams &p_, const int *ends_, int tiles_)
+        : p(p_), ends(ends_), tiles(tiles_), base(blockIdx.x), at(32), mine{}
+    {
+    }
+    __device__ bool next(Tile &t)                    // false when there are no more
+    {
+        while (true) {
+            if (at == 32) {
+                if (base >= tiles) return false;
+                const int i = base + (int)(threadIdx.x & 31) * (int)gridDim.x;
+                mine.rows = 0; mine.slot = -1;
+                if (i < tiles) mine = tile_at<NT>(p, ends, i);
+                base += 32 * (int)gridDim.x;
+                at = 0;
+                __syncwarp();
+            }
+            t.slot = __shfl_sync(0xffffffffu, mine.slot, at); t.feat = __shfl_sync(0xffffffffu, mine.feat, at);
+            t.row = __shfl_sync(0xffffffffu, mine.row, at); t.rows = __shfl_sync(0xffffffffu, mine.rows, at);
+            ++at;
+            if (t.slot < 0) return false;
+            if (t.rows > 0) return true;
+        }
+    }
+};
+
 template <int NT, int STAGES>
 struct Layout {
     static constexpr int kBTile = NT * kRowBytes;
@@ -428,9 +462,8 @@ k_mx_product(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
         int issued = 0, s = 0;
         unsigned parity = 1;                                   // a fresh barrier passes the wait for parity 1
         bool ok = true;
-        for (int i = blockIdx.x; i < tiles && ok; i += gridDim.x) {
-            const Tile t = tile_at<NT>(p, ends, i);
-            if (t.rows <= 0) continue;
+        Tile t;
+        for (TileStream<NT> stream(p, ends, tiles); ok && stream.next(t);) {
             const int loads = (t.n() + kBox - 1) / kBox;
             for (int k = 0; k < steps; ++k) {
                 ok = __all_sync(0xffffffffu, wait_for(&empty[s], parity, quit, p.spin_limit));
@@ -460,9 +493,8 @@ k_mx_product(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
         unsigned parity = 0, acc_parity = 1, step_no = 0;
         bool ok = true;
         const uint64_t stage_desc = desc_codes(smem_addr(stage)), sf_desc = desc_scales(smem_addr(sf));
-        for (int i = blockIdx.x; i < tiles && ok; i += gridDim.x) {
-            const Tile t = tile_at<NT>(p, ends, i);
-            if (t.rows <= 0) continue;
+        Tile t;
+        for (TileStream<NT> stream(p, ends, tiles); ok && stream.next(t);) {
             ok = __all_sync(0xffffffffu, wait_for(&acc_empty[buf], acc_parity, quit, p.spin_limit));
             if (!ok) break;
             tc_fence_after();
@@ -521,15 +553,12 @@ k_mx_product(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
         uint4 ring[kPieces][4];
         bool valid[kPieces];
         const uint8_t *src[4];
-        int i = blockIdx.x, piece = 0;
+        TileStream<NT> stream(p, ends, tiles);
+        int piece = 0;
         auto fetch = [&](uint4 (&v)[4]) {                      // the next piece, over all tiles; false when there is none
             if (piece == 0) {
-                Tile t{};
-                for (; i < tiles; i += gridDim.x) {
-                    t = tile_at<NT>(p, ends, i);
-                    if (t.rows > 0) break;
-                }
-                if (i >= tiles) return false;
+                Tile t;
+                if (!stream.next(t)) return false;
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {
                     const int r = lane + 32 * g + (blk > 0 ? (blk - 1) * 128 : 0);
@@ -540,7 +569,7 @@ k_mx_product(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
 #pragma unroll
             for (int g = 0; g < 4; ++g)
                 v[g] = src[g] ? __ldg(reinterpret_cast<const uint4 *>(src[g]) + piece) : make_uint4(one, one, one, one);
-            if (++piece == pieces) { piece = 0; i += gridDim.x; }
+            if (++piece == pieces) piece = 0;
             return true;
         };
         int s = 0, at = 0;
@@ -594,9 +623,8 @@ k_mx_product(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
         const int group = warp >> 2, quarter = warp & 3;
         int buf = 0;
         unsigned acc_parity = 0;
-        for (int i = blockIdx.x; i < tiles; i += gridDim.x) {
-            const Tile t = tile_at<NT>(p, ends, i);
-            if (t.rows <= 0) continue;
+        Tile t;
+        for (TileStream<NT> stream(p, ends, tiles); stream.next(t);) {
             bool ok = wait_for(&acc_full[buf], acc_parity, quit, p.spin_limit);
             ok = GATED ? group_all(group, ok) : __all_sync(0xffffffffu, ok);   // the gated epilogue's warps meet at barriers
             if (!ok) break;
