@@ -31,7 +31,7 @@ namespace {
 
 using namespace moe;
 
-constexpr int kFeat = 128;                 // features per tile (M)
+constexpr int kFeat = 128;                 // features per CTA and tile
 constexpr int kStageK = 256;               // elements of K per stage
 constexpr int kRowBytes = kStageK / 2;     // bytes of a code row per stage
 constexpr int kATile = kFeat * kRowBytes;  // 16 KB
@@ -40,35 +40,64 @@ constexpr int kEpiWarps = 8, kTmaWarp = kEpiWarps, kMmaWarp = kEpiWarps + 1, kSc
 
 // ------------------------------------------------------------------ tcgen05 in PTX
 
+// CG = CTAs that work on one MMA (1, or 2: a cluster of two SMs, each with half of the features in its
+// TMEM and half of the row operand in its shared memory; the first CTA issues for both).
+
+template <int CG>
 __device__ __forceinline__ void tmem_alloc(uint32_t *slot, uint32_t cols)
 {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(slot)), "r"(cols) : "memory");
+    if (CG == 1) asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(slot)), "r"(cols) : "memory");
+    else asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(slot)), "r"(cols) : "memory");
 }
 
+template <int CG>
 __device__ __forceinline__ void tmem_dealloc(uint32_t base, uint32_t cols)
 {
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(base), "r"(cols));
+    if (CG == 1) {
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(base), "r"(cols));
+    } else {
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(base), "r"(cols));
+    }
 }
 
+// Arrive on `bar` (with CG = 2: on that barrier of both CTAs) when everything issued so far is done.
+template <int CG>
 __device__ __forceinline__ void mma_commit(uint64_t *bar)
 {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_addr(bar)) : "memory");
+    if (CG == 1)
+        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_addr(bar)) : "memory");
+    else
+        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(smem_addr(bar)),
+                     "h"((uint16_t)3)
+                     : "memory");
 }
 
+template <int CG>
 __device__ __forceinline__ void mma_mxf4(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sfa, uint32_t sfb, bool accumulate)
 {
-    asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d),
-        "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"((uint32_t)accumulate)
-        : "memory");
+    if (CG == 1)
+        asm volatile(
+            "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
+            "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d),
+            "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"((uint32_t)accumulate)
+            : "memory");
+    else
+        asm volatile(
+            "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
+            "tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d),
+            "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"((uint32_t)accumulate)
+            : "memory");
 }
 
-// 32 rows of 16 bytes from shared memory to four TMEM columns, repeated in the four lane quarters
+// 32 rows of 16 bytes from shared memory to four TMEM columns, repeated in the four lane quarters (with
+// CG = 2 in both CTAs, each from its own shared memory)
+template <int CG>
 __device__ __forceinline__ void cp_scales(uint32_t tmem, uint64_t desc)
 {
-    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
+    if (CG == 1) asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
+    else asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
 }
 
 __device__ __forceinline__ void tmem_ld32(uint32_t addr, uint32_t (&r)[32])
@@ -116,21 +145,71 @@ __device__ __forceinline__ void mbar_arrive(uint64_t *bar)
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_addr(bar)) : "memory");
 }
 
-__device__ __forceinline__ void tma_2d(void *dst, const CUtensorMap *map, int x, int y, uint64_t *bar)
+__device__ __forceinline__ uint32_t cluster_rank()
 {
-    asm volatile("cp.async.bulk.tensor.2d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(
-                     smem_addr(dst)),
-                 "l"(map), "r"(x), "r"(y), "r"(smem_addr(bar))
-                 : "memory");
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
 }
 
-__device__ __forceinline__ void tma_3d(void *dst, const CUtensorMap *map, int x, int y, int z, uint64_t *bar)
+// The address of a barrier in the first CTA of the pair (its own for CG = 1).
+template <int CG>
+__device__ __forceinline__ uint32_t lead_addr(uint64_t *bar)
 {
-    asm volatile(
-        "cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(
-            smem_addr(dst)),
-        "l"(map), "r"(x), "r"(y), "r"(z), "r"(smem_addr(bar))
-        : "memory");
+    if (CG == 1) return smem_addr(bar);
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(smem_addr(bar)));
+    return r;
+}
+
+// Arrival at the first CTA's barrier.  What it announces lies in this CTA's shared memory or TMEM and has
+// been ordered before it (proxy fence, tcgen05 fence), so it needs no release over the cluster: that
+// one waits for the thread's loads and stores in global memory, which took 1500 cycles a stage here.
+template <int CG>
+__device__ __forceinline__ void mbar_arrive_lead(uint64_t *bar)
+{
+    if (CG == 1) mbar_arrive(bar);
+    else asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(lead_addr<2>(bar)) : "memory");
+}
+
+__device__ __forceinline__ void cluster_sync()
+{
+    asm volatile("barrier.cluster.arrive.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+}
+
+// Tile loads into this CTA's shared memory; `bar` is a lead_addr.
+template <int CG>
+__device__ __forceinline__ void tma_2d(void *dst, const CUtensorMap *map, int x, int y, uint32_t bar)
+{
+    if (CG == 1)
+        asm volatile("cp.async.bulk.tensor.2d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(
+                         smem_addr(dst)),
+                     "l"(map), "r"(x), "r"(y), "r"(bar)
+                     : "memory");
+    else
+        asm volatile(
+            "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3}], [%4];" ::"r"(
+                smem_addr(dst)),
+            "l"(map), "r"(x), "r"(y), "r"(bar)
+            : "memory");
+}
+
+template <int CG>
+__device__ __forceinline__ void tma_3d(void *dst, const CUtensorMap *map, int x, int y, int z, uint32_t bar)
+{
+    if (CG == 1)
+        asm volatile(
+            "cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(
+                smem_addr(dst)),
+            "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
+            : "memory");
+    else
+        asm volatile(
+            "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(
+                smem_addr(dst)),
+            "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
+            : "memory");
 }
 
 // Shared-memory matrix descriptor: start and strides in 16-byte units, version 1 (sm_100).
@@ -147,9 +226,10 @@ __device__ __forceinline__ uint64_t desc_scales(uint32_t addr)
 
 // Instruction descriptor of kind::mxf4: A and B e2m1 (1), both K-major, scales ue8m0 (bit 23),
 // N / 8 at bit 17, M / 16 at bit 24; sf_half: which half of a 32-bit scale word (0 or 2) belongs to this K = 64.
+template <int CG>
 __device__ __forceinline__ uint32_t idesc_mxf4(int n)
 {
-    return (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | (1u << 23) | ((uint32_t)(kFeat >> 4) << 24);
+    return (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | (1u << 23) | ((uint32_t)(CG * kFeat >> 4) << 24);
 }
 __device__ __forceinline__ constexpr uint32_t sf_half(uint32_t id) { return (id << 4) | (id << 29); }
 
@@ -194,7 +274,7 @@ __device__ __forceinline__ int segment(const KernelParams &p, int s, int &first)
 template <int NT>
 __device__ __forceinline__ int row_tiles(int c) { return (c + NT - 1) / NT; }
 
-template <int NT>
+template <int NT, int CG>
 __device__ __forceinline__ Tile tile_at(const KernelParams &p, const int *ends, int index)
 {
     int lo = 0, hi = p.P - 1;                        // first slot whose inclusive end is beyond the index
@@ -209,7 +289,7 @@ __device__ __forceinline__ Tile tile_at(const KernelParams &p, const int *ends, 
     const int nt = row_tiles<NT>(c);
     const int f = local / nt, r = local - f * nt;
     const int size = ((c + nt - 1) / nt + 15) & ~15;
-    t.slot = lo; t.feat = f * kFeat;
+    t.slot = lo; t.feat = f * (CG * kFeat);
     t.row = first + r * size;
     t.rows = min(size, c - r * size);                // may be <= 0 for the last tile of an uneven cut
     return t;
@@ -221,9 +301,9 @@ constexpr int kPlane = 32 * 32 + 8;
 constexpr int kEpiWarpBytes = (2 * kPlane * 4 / 4 + 127) / 128 * 128;
 static_assert(kEpiWarpBytes >= 2048, "plain epilogue");
 
-// The tiles of a CTA, blockIdx.x, + gridDim.x, ..., as a warp sees them.  Finding a tile is a chain of
+// The tiles of a CTA (or pair of CTAs) of a grid of `step`, first, first + step, ..., as a warp sees them.  Finding a tile is a chain of
 // dependent reads, so the lanes find the next 32 of them side by side and hand them out one by one.
-template <int NT>
+template <int NT, int CG>
 struct TileStream {
     const KernelParams &p;
     const int *ends;
@@ -231,7 +311,7 @@ struct TileStream {
     int base, at;
     Tile mine;
     __device__ TileStream(const KernelParams &p_, const int *ends_, int tiles_)
-        : p(p_), ends(ends_), tiles(tiles_), base(blockIdx.x), at(32), mine{}
+        : p(p_), ends(ends_), tiles(tiles_), base(blockIdx.x / CG), at(32), mine{}
     {
     }
     __device__ bool next(Tile &t)                    // false when there are no more
@@ -239,10 +319,10 @@ struct TileStream {
         while (true) {
             if (at == 32) {
                 if (base >= tiles) return false;
-                const int i = base + (int)(threadIdx.x & 31) * (int)gridDim.x;
+                const int step = (int)gridDim.x / CG, i = base + (int)(threadIdx.x & 31) * step;
                 mine.rows = 0; mine.slot = -1;
-                if (i < tiles) mine = tile_at<NT>(p, ends, i);
-                base += 32 * (int)gridDim.x;
+                if (i < tiles) mine = tile_at<NT, CG>(p, ends, i);
+                base += 32 * step;
                 at = 0;
                 __syncwarp();
             }
@@ -255,9 +335,9 @@ struct TileStream {
     }
 };
 
-template <int NT, int STAGES>
+template <int NT, int STAGES, int CG>
 struct Layout {
-    static constexpr int kBTile = NT * kRowBytes;
+    static constexpr int kBTile = (NT / CG + 31) / 32 * 32 * kRowBytes;   // this CTA's rows, in boxes of 32
     static constexpr int kRB = (NT + 127) / 128;              // 128-row scale blocks of the row operand
     static constexpr int kThreads = 32 * (kEpiWarps + 3 + kRB);
     static constexpr int kSfA = 2 * 512, kSfB = 2 * kRB * 512;
@@ -391,11 +471,11 @@ __device__ __forceinline__ void store_gated(const KernelParams &p, const Tile &t
     }
 }
 
-template <int NT, int STAGES, bool GATED>
-__global__ void __launch_bounds__(Layout<NT, STAGES>::kThreads, 1)
+template <int NT, int STAGES, int CG, bool GATED>
+__global__ void __launch_bounds__(Layout<NT, STAGES, CG>::kThreads, 1)
 k_mx_product(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_a, const KernelParams p)
 {
-    using L = Layout<NT, STAGES>;
+    using L = Layout<NT, STAGES, CG>;
     constexpr int kBox = NT >= 32 ? 32 : 16;                   // rows per TMA load of the row operand
     extern __shared__ unsigned char raw[];
     unsigned char *base = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
@@ -409,21 +489,25 @@ k_mx_product(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
     int *ends = reinterpret_cast<int *>(base + L::kEndsOff);
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int rank = CG == 2 ? (int)cluster_rank() : 0;
     if (tid == 0) {
-        for (int s = 0; s < STAGES; ++s) { mbar_init(&full[s], 2 + L::kRB); mbar_init(&empty[s], 1); }
-        for (int b = 0; b < 2; ++b) { mbar_init(&acc_full[b], 1); mbar_init(&acc_empty[b], kEpiWarps); }
+        for (int s = 0; s < STAGES; ++s) {
+            mbar_init(&full[s], 1 + CG * (1 + L::kRB));        // the bytes of the loads, and every scale warp of the pair
+            mbar_init(&empty[s], 1);
+        }
+        for (int b = 0; b < 2; ++b) { mbar_init(&acc_full[b], 1); mbar_init(&acc_empty[b], CG * kEpiWarps); }
         mbar_init(drained, 1);
         *quit = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(&map_w));
         asm volatile("prefetch.tensormap [%0];" ::"l"(&map_a));
     }
-    if (warp == kMmaWarp) tmem_alloc(tmem_slot, 512);
+    if (warp == kMmaWarp) tmem_alloc<CG>(tmem_slot, 512);
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
 
     // inclusive prefix over the slots of their tile counts
-    const int feats = (p.N + kFeat - 1) / kFeat;
+    const int feats = (p.N + CG * kFeat - 1) / (CG * kFeat);
     {
         const int chunk = (p.P + L::kThreads - 1) / L::kThreads;
         const int s0 = tid * chunk, s1 = min(p.P, s0 + chunk);
@@ -444,8 +528,10 @@ k_mx_product(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
         for (int w = 0; w < warp; ++w) before += warp_sums[w];
         for (int s = s0; s < s1; ++s) ends[s] += before;
     }
+    __syncwarp();
     tc_fence_before();
-    __syncthreads();
+    if (CG == 2) cluster_sync();                               // the peer's barriers are set up before anything arrives on them
+    else __syncthreads();
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
     const int tiles = ends[p.P - 1];
@@ -463,17 +549,20 @@ k_mx_product(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
         unsigned parity = 1;                                   // a fresh barrier passes the wait for parity 1
         bool ok = true;
         Tile t;
-        for (TileStream<NT> stream(p, ends, tiles); ok && stream.next(t);) {
-            const int loads = (t.n() + kBox - 1) / kBox;
+        for (TileStream<NT, CG> stream(p, ends, tiles); ok && stream.next(t);) {
+            const int half = t.n() / CG;                       // rows of the tile in this CTA
+            const int loads = (half + kBox - 1) / kBox;
             for (int k = 0; k < steps; ++k) {
                 ok = __all_sync(0xffffffffu, wait_for(&empty[s], parity, quit, p.spin_limit));
                 if (!ok) break;
                 unsigned char *a = stage + s * L::kStage, *b = a + kATile;
                 if (elect_one()) {
-                    mbar_expect_tx(&full[s], kATile + loads * kBox * kRowBytes);
-                    tma_3d(a, &map_w, k * kRowBytes, t.feat, t.slot, &full[s]);
+                    // the first CTA's barrier counts the bytes of both
+                    if (rank == 0) mbar_expect_tx(&full[s], CG * (kATile + loads * kBox * kRowBytes));
+                    const uint32_t bar = lead_addr<CG>(&full[s]);
+                    tma_3d<CG>(a, &map_w, k * kRowBytes, t.feat + rank * kFeat, t.slot, bar);
                     for (int l = 0; l < loads; ++l)
-                        tma_2d(b + l * kBox * kRowBytes, &map_a, k * kRowBytes, t.row + l * kBox, &full[s]);
+                        tma_2d<CG>(b + l * kBox * kRowBytes, &map_a, k * kRowBytes, t.row + rank * half + l * kBox, bar);
                 }
                 __syncwarp();
                 ++issued;
@@ -488,19 +577,19 @@ k_mx_product(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
                 while (!mbar_try_wait(&full[m % STAGES], (unsigned)(m / STAGES) & 1u) && ++spins < p.spin_limit) {}
             }
         }
-    } else if (warp == kMmaWarp) {
+    } else if (warp == kMmaWarp && rank == 0) {
         int s = 0, buf = 0;
         unsigned parity = 0, acc_parity = 1, step_no = 0;
         bool ok = true;
         const uint64_t stage_desc = desc_codes(smem_addr(stage)), sf_desc = desc_scales(smem_addr(sf));
         Tile t;
-        for (TileStream<NT> stream(p, ends, tiles); ok && stream.next(t);) {
+        for (TileStream<NT, CG> stream(p, ends, tiles); ok && stream.next(t);) {
             ok = __all_sync(0xffffffffu, wait_for(&acc_empty[buf], acc_parity, quit, p.spin_limit));
             if (!ok) break;
             tc_fence_after();
             const uint32_t d = tmem + buf * NT;
             const int n = t.n();
-            const uint32_t idesc = idesc_mxf4(n);
+            const uint32_t idesc = idesc_mxf4<CG>(n);
             bool ready = mbar_test_wait(&full[s], parity);
             for (int k = 0; k < steps; ++k, ++step_no) {
                 ok = __all_sync(0xffffffffu, ready || wait_for(&full[s], parity, quit, p.spin_limit));
@@ -516,16 +605,16 @@ k_mx_product(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
                 if (elect_one()) {
 #pragma unroll
                     for (int g = 0; g < 2; ++g) {
-                        cp_scales(sfa + 4 * g, sfs + g * 32);
-                        cp_scales(sfb + 4 * g * L::kRB, sfs + (L::kSfA >> 4) + g * L::kRB * 32);
-                        if (L::kRB == 2 && n > 128) cp_scales(sfb + 4 * (g * L::kRB + 1), sfs + (L::kSfA >> 4) + (g * L::kRB + 1) * 32);
+                        cp_scales<CG>(sfa + 4 * g, sfs + g * 32);
+                        cp_scales<CG>(sfb + 4 * g * L::kRB, sfs + (L::kSfA >> 4) + g * L::kRB * 32);
+                        if (L::kRB == 2 && n > 128) cp_scales<CG>(sfb + 4 * (g * L::kRB + 1), sfs + (L::kSfA >> 4) + (g * L::kRB + 1) * 32);
                     }
 #pragma unroll
                     for (int q = 0; q < 4; ++q)
-                        mma_mxf4(d, a + 2 * q, b + 2 * q, idesc | sf_half((q & 1) * 2), sfa + 4 * (q >> 1), sfb + 4 * L::kRB * (q >> 1),
+                        mma_mxf4<CG>(d, a + 2 * q, b + 2 * q, idesc | sf_half((q & 1) * 2), sfa + 4 * (q >> 1), sfb + 4 * L::kRB * (q >> 1),
                                  k > 0 || q > 0);
-                    mma_commit(&empty[s]);
-                    if (k == steps - 1) mma_commit(&acc_full[buf]);
+                    mma_commit<CG>(&empty[s]);
+                    if (k == steps - 1) mma_commit<CG>(&acc_full[buf]);
                 }
                 __syncwarp();
                 s = s_next;
@@ -535,10 +624,14 @@ k_mx_product(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
             if (buf == 0) acc_parity ^= 1u;
         }
         // everything issued has left the tensor core before TMEM is given back
-        if (elect_one()) mma_commit(drained);
+        if (elect_one()) mma_commit<CG>(drained);
         __syncwarp();
         unsigned spins = 0;
         while (!mbar_try_wait(drained, 0) && ++spins < p.spin_limit) {}
+    } else if (warp == kMmaWarp) {
+        // the second CTA of a pair: stay until the last arrival from the first has come in
+        unsigned spins = 0;
+        while (!mbar_try_wait(drained, 0) && ++spins < p.spin_limit) __nanosleep(256);
     } else if (warp >= kScaleWarp) {
         // A warp per 128-row block of scales: the weight rows, then the data rows.  Lane l owns rows l, l + 32,
         // l + 64 and l + 96 and reads 16 bytes of each at a time (K = 512, two stages), kPieces of them ahead.
@@ -553,12 +646,13 @@ k_mx_product(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
         uint4 ring[kPieces][4];
         bool valid[kPieces];
         const uint8_t *src[4];
-        TileStream<NT> stream(p, ends, tiles);
+        TileStream<NT, CG> stream(p, ends, tiles);
         int piece = 0;
         auto fetch = [&](uint4 (&v)[4]) {                      // the next piece, over all tiles; false when there is none
             if (piece == 0) {
                 Tile t;
                 if (!stream.next(t)) return false;
+                t.feat += rank * kFeat;
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {
                     const int r = lane + 32 * g + (blk > 0 ? (blk - 1) * 128 : 0);
@@ -611,25 +705,26 @@ k_mx_product(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
                     }
                     fence_async_shared();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(&full[s]);
+                    if (lane == 0) mbar_arrive_lead<CG>(&full[s]);
                     if (++s == STAGES) { s = 0; parity ^= 1u; }
                 }
                 if (++at == pieces) at = 0;
                 valid[d] = fetch(v);
             }
         }
-    } else {
+    } else if (warp < kEpiWarps) {
         // epilogue: TMEM lane = feature of the tile, column = row
         const int group = warp >> 2, quarter = warp & 3;
         int buf = 0;
         unsigned acc_parity = 0;
         Tile t;
-        for (TileStream<NT> stream(p, ends, tiles); stream.next(t);) {
+        for (TileStream<NT, CG> stream(p, ends, tiles); stream.next(t);) {
             bool ok = wait_for(&acc_full[buf], acc_parity, quit, p.spin_limit);
             ok = GATED ? group_all(group, ok) : __all_sync(0xffffffffu, ok);   // the gated epilogue's warps meet at barriers
             if (!ok) break;
             tc_fence_after();
             const uint32_t acc = tmem + buf * NT + ((uint32_t)(quarter * 32) << 16);
+            t.feat += rank * kFeat;
             for (int c0 = group * 32; c0 < t.rows; c0 += 64) {
                 uint32_t v[32];
                 if (GATED) tmem_ld32(acc + c0, v);
@@ -638,12 +733,12 @@ k_mx_product(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
                 if (c0 + 64 >= t.rows) {                        // this warp's last look at the accumulator
                     tc_fence_before();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(&acc_empty[buf]);
+                    if (lane == 0) mbar_arrive_lead<CG>(&acc_empty[buf]);
                 }
                 if (GATED) store_gated(p, t, c0, v, reinterpret_cast<float *>(epi + group * 4 * kEpiWarpBytes), group, quarter, lane);
                 else store_plain(p, t, c0, v, epi + warp * kEpiWarpBytes, quarter, lane);
             }
-            if (group * 32 >= t.rows && lane == 0) mbar_arrive(&acc_empty[buf]);
+            if (group * 32 >= t.rows && lane == 0) mbar_arrive_lead<CG>(&acc_empty[buf]);
             buf ^= 1;
             if (buf == 0) acc_parity ^= 1u;
         }
@@ -651,11 +746,12 @@ k_mx_product(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
 
     __syncwarp();
     tc_fence_before();
-    __syncthreads();
+    if (CG == 2) cluster_sync();                               // the pair leaves together: neither arrives on a CTA that is gone
+    else __syncthreads();
     if (tid == 0 && *quit) report_status(p.ctl, kDevTimeout);
     if (warp == kMmaWarp) {
         tc_fence_after();
-        tmem_dealloc(tmem, 512);
+        tmem_dealloc<CG>(tmem, 512);
     }
 }
 
@@ -687,13 +783,13 @@ bool encode(CUtensorMap *map, const uint8_t *ptr, int rank, const cuuint64_t *di
                        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int NT, int STAGES, bool GATED>
+template <int NT, int STAGES, int CG, bool GATED>
 cudaError_t launch(const MxProductArgs &a, cudaStream_t st)
 {
-    using L = Layout<NT, STAGES>;
+    using L = Layout<NT, STAGES, CG>;
     static_assert(L::kEndsOff + 1024 + kMaxP * 4 <= 227 * 1024, "shared memory");
     static_assert(NT >= 32 && NT % 32 == 0, "row boxes and epilogue chunks are 32 rows");
-    const auto kernel = k_mx_product<NT, STAGES, GATED>;
+    const auto kernel = k_mx_product<NT, STAGES, CG, GATED>;
     static std::once_flag once;
     static cudaError_t attr = cudaSuccess;
     std::call_once(once, [&] {
@@ -711,25 +807,28 @@ cudaError_t launch(const MxProductArgs &a, cudaStream_t st)
     p.rows = a.rows; p.P = a.P; p.N = a.N; p.K = a.K; p.y = static_cast<__nv_bfloat16 *>(a.y);
     p.h_codes = a.h_codes; p.h_scales = a.h_scales; p.ctl = a.ctl; p.spin_limit = a.spin_limit;
     // no more CTAs than there can be tiles (the counts are on the device)
-    const long long feats = (a.N + kFeat - 1) / kFeat;
+    const long long feats = (a.N + CG * kFeat - 1) / (CG * kFeat);
     const long long most = feats * (std::min<long long>(a.P, a.rows) + a.rows / NT);
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)std::min<long long>(a.sm_count, most));
+    cfg.gridDim = dim3((unsigned)(CG * std::min<long long>(a.sm_count / CG, most)));
     cfg.blockDim = dim3(L::kThreads); cfg.dynamicSmemBytes = L::bytes(a.P); cfg.stream = st;
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = at; cfg.numAttrs = a.pdl ? 1 : 0;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = CG; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
+    at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at; cfg.numAttrs = a.pdl ? 2 : 1;
     return cudaLaunchKernelEx(&cfg, kernel, map_w, map_a, p);
 }
 
 template <bool GATED>
 cudaError_t launch_for(const MxProductArgs &a, cudaStream_t st)
 {
-    // Rows per tile: with few rows a slot the weights dominate, and a narrow tile leaves shared memory
-    // for more stages of them; with many rows a wide tile reads the weights fewer times.
-    if (a.rows <= 64ll * a.P) return launch<64, 7, GATED>(a, st);
-    return launch<224, 4, GATED>(a, st);
+    // With few rows a slot the weights dominate, and a narrow tile of one CTA leaves shared memory for more
+    // stages of them.  With many rows the products do, and shared memory bounds them: a stage of 256 is written
+    // once and read once by the tensor core.  A pair of CTAs halves what each holds of the row operand.
+    if (a.rows <= 64ll * a.P) return launch<64, 7, 1, GATED>(a, st);
+    return launch<224, 5, 2, GATED>(a, st);
 }
 
 }  // namespace
