@@ -689,23 +689,30 @@ k_mx_product(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
                         v[g] = make_uint4(w[0], w[1], w[2], w[3]);
                     }
                 }
-#pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    if (at * 2 + half >= steps) break;
-                    ok = __all_sync(0xffffffffu, wait_for(&empty[s], parity, quit, p.spin_limit));
-                    if (!ok) break;
-                    unsigned char *dst = sf + s * L::kSf + (blk == 0 ? 0 : L::kSfA + (blk - 1) * 512) + lane * 16;
-                    const int next = blk == 0 ? 512 : L::kRB * 512;
-                    if (half == 0) {
-                        *reinterpret_cast<uint4 *>(dst) = make_uint4(v[0].x, v[1].x, v[2].x, v[3].x);
-                        *reinterpret_cast<uint4 *>(dst + next) = make_uint4(v[0].y, v[1].y, v[2].y, v[3].y);
-                    } else {
-                        *reinterpret_cast<uint4 *>(dst) = make_uint4(v[0].z, v[1].z, v[2].z, v[3].z);
-                        *reinterpret_cast<uint4 *>(dst + next) = make_uint4(v[0].w, v[1].w, v[2].w, v[3].w);
-                    }
-                    fence_async_shared();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive_lead<CG>(&full[s]);
+                // both stages of the piece behind one proxy fence
+                const bool two = at * 2 + 1 < steps;
+                const int s1 = s + 1 == STAGES ? 0 : s + 1;
+                const unsigned parity1 = s1 ? parity : parity ^ 1u;
+                ok = wait_for(&empty[s], parity, quit, p.spin_limit);
+                ok = __all_sync(0xffffffffu, ok && (!two || wait_for(&empty[s1], parity1, quit, p.spin_limit)));
+                if (!ok) break;
+                const int off = (blk == 0 ? 0 : L::kSfA + (blk - 1) * 512) + lane * 16;
+                const int next = blk == 0 ? 512 : L::kRB * 512;
+                unsigned char *dst = sf + s * L::kSf + off, *dst1 = sf + s1 * L::kSf + off;
+                *reinterpret_cast<uint4 *>(dst) = make_uint4(v[0].x, v[1].x, v[2].x, v[3].x);
+                *reinterpret_cast<uint4 *>(dst + next) = make_uint4(v[0].y, v[1].y, v[2].y, v[3].y);
+                if (two) {
+                    *reinterpret_cast<uint4 *>(dst1) = make_uint4(v[0].z, v[1].z, v[2].z, v[3].z);
+                    *reinterpret_cast<uint4 *>(dst1 + next) = make_uint4(v[0].w, v[1].w, v[2].w, v[3].w);
+                }
+                fence_async_shared();
+                __syncwarp();
+                if (lane == 0) {
+                    mbar_arrive_lead<CG>(&full[s]);
+                    if (two) mbar_arrive_lead<CG>(&full[s1]);
+                }
+                s = s1; parity = parity1;
+                if (two) {
                     if (++s == STAGES) { s = 0; parity ^= 1u; }
                 }
                 if (++at == pieces) at = 0;
