@@ -339,7 +339,7 @@ template <int NT, int STAGES, int CG>
 struct Layout {
     static constexpr int kBTile = (NT / CG + 31) / 32 * 32 * kRowBytes;   // this CTA's rows, in boxes of 32
     static constexpr int kRB = (NT + 127) / 128;              // 128-row scale blocks of the row operand
-    static constexpr int kThreads = 32 * (kEpiWarps + 3 + kRB);
+    static constexpr int kThreads = 32 * (kEpiWarps + 2 + 2 * (1 + kRB));
     static constexpr int kSfA = 2 * 512, kSfB = 2 * kRB * 512;
     static constexpr int kStage = kATile + kBTile;            // multiples of 1024: swizzle alignment
     static constexpr int kSf = kSfA + kSfB;
@@ -633,12 +633,14 @@ k_mx_product(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
         unsigned spins = 0;
         while (!mbar_try_wait(drained, 0) && ++spins < p.spin_limit) __nanosleep(256);
     } else if (warp >= kScaleWarp) {
-        // A warp per 128-row block of scales: the weight rows, then the data rows.  Lane l owns rows l, l + 32,
-        // l + 64 and l + 96 and reads 16 bytes of each at a time (K = 512, two stages), kPieces of them ahead.
+        // Two warps per 128-row block of scales (the weight rows, then the data rows), which take the pieces of
+        // 16 bytes a row (K = 512, two stages) in turn, each reading kPieces of its own ahead.  Lane l owns rows
+        // l, l + 32, l + 64 and l + 96.
         // tcgen05.cp wants, for each K = 128, [32 lanes][4 rows][4 scales]: word w of the lane's four rows is
         // one 16-byte store, so nothing is transposed and no two lanes meet in a bank.
-        constexpr int kPieces = 4;
-        const int blk = warp - kScaleWarp;                            // 0: weights; 1 + rb: data rows [128 rb, 128 rb + 128)
+        constexpr int kPieces = 3;
+        const int blk = (warp - kScaleWarp) % (1 + L::kRB);    // 0: weights; 1 + rb: data rows [128 rb, 128 rb + 128)
+        const int turn = (warp - kScaleWarp) / (1 + L::kRB);   // this warp's pieces: even or odd ones
         const int pitch = mx_scale_pitch(p.K);
         const int pieces = (steps + 1) / 2;
         const int left = p.K / kMxBlock - (pieces - 1) * 16;   // scales of the last piece; the padding counts as 1
@@ -648,27 +650,39 @@ k_mx_product(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
         const uint8_t *src[4];
         TileStream<NT, CG> stream(p, ends, tiles);
         int piece = 0;
-        auto fetch = [&](uint4 (&v)[4]) {                      // the next piece, over all tiles; false when there is none
-            if (piece == 0) {
-                Tile t;
-                if (!stream.next(t)) return false;
-                t.feat += rank * kFeat;
+        int whose = 0;                                         // turn of the next piece
+        auto fetch = [&](uint4 (&v)[4]) {                      // this warp's next piece, over all tiles; false when there is none
+            int mine;
+            do {
+                if (piece == 0) {
+                    Tile t;
+                    if (!stream.next(t)) return false;
+                    t.feat += rank * kFeat;
 #pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    const int r = lane + 32 * g + (blk > 0 ? (blk - 1) * 128 : 0);
-                    if (blk == 0) src[g] = t.feat + r < p.N ? p.w_scales + ((size_t)t.slot * p.N + t.feat + r) * pitch : nullptr;
-                    else src[g] = r < t.rows ? p.a_scales + (size_t)(t.row + r) * pitch : nullptr;
+                    for (int g = 0; g < 4; ++g) {
+                        const int r = lane + 32 * g + (blk > 0 ? (blk - 1) * 128 : 0);
+                        if (blk == 0) src[g] = t.feat + r < p.N ? p.w_scales + ((size_t)t.slot * p.N + t.feat + r) * pitch : nullptr;
+                        else src[g] = r < t.rows ? p.a_scales + (size_t)(t.row + r) * pitch : nullptr;
+                    }
                 }
-            }
+                mine = whose == turn ? piece : -1;
+                whose ^= 1;
+                if (++piece == pieces) piece = 0;
+            } while (mine < 0);
 #pragma unroll
             for (int g = 0; g < 4; ++g)
-                v[g] = src[g] ? __ldg(reinterpret_cast<const uint4 *>(src[g]) + piece) : make_uint4(one, one, one, one);
-            if (++piece == pieces) piece = 0;
+                v[g] = src[g] ? __ldg(reinterpret_cast<const uint4 *>(src[g]) + mine) : make_uint4(one, one, one, one);
             return true;
         };
-        int s = 0, at = 0;
+        int s = 0, at = 0;                                     // next stage of the ring, piece of the tile
         unsigned parity = 1;
         bool ok = true;
+        auto skip = [&]() {                                    // past the other warp's piece
+            s += at * 2 + 1 < steps ? 2 : 1;
+            if (s >= STAGES) { s -= STAGES; parity ^= 1u; }
+            if (++at == pieces) at = 0;
+        };
+        if (turn == 1) skip();
 #pragma unroll
         for (int d = 0; d < kPieces; ++d) valid[d] = fetch(ring[d]);
         while (ok && valid[0]) {
@@ -716,6 +730,7 @@ k_mx_product(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
                     if (++s == STAGES) { s = 0; parity ^= 1u; }
                 }
                 if (++at == pieces) at = 0;
+                skip();
                 valid[d] = fetch(v);
             }
         }
