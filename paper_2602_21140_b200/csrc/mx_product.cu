@@ -335,6 +335,20 @@ struct TileStream {
     }
 };
 
+// The next tile with its fields and the verdict in uniform registers (a warp reduction writes those): what
+// tcgen05 and TMA instructions take comes from uniform registers, and a value or a loop that the compiler
+// cannot prove uniform costs a move per operand and instruction.
+template <int NT, int CG>
+__device__ __forceinline__ bool next_uniform(TileStream<NT, CG> &stream, Tile &t)
+{
+    Tile m;
+    const bool more = stream.next(m);
+    if (!__any_sync(0xffffffffu, more)) return false;
+    t.slot = (int)__reduce_max_sync(0xffffffffu, (unsigned)m.slot); t.feat = (int)__reduce_max_sync(0xffffffffu, (unsigned)m.feat);
+    t.row = (int)__reduce_max_sync(0xffffffffu, (unsigned)m.row); t.rows = (int)__reduce_max_sync(0xffffffffu, (unsigned)m.rows);
+    return true;
+}
+
 template <int NT, int STAGES, int CG>
 struct Layout {
     static constexpr int kBTile = (NT / CG + 31) / 32 * 32 * kRowBytes;   // this CTA's rows, in boxes of 32
@@ -473,10 +487,11 @@ __device__ __forceinline__ void store_gated(const KernelParams &p, const Tile &t
 
 template <int NT, int STAGES, int CG, bool GATED>
 __global__ void __launch_bounds__(Layout<NT, STAGES, CG>::kThreads, 1)
-k_mx_product(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_a, const KernelParams p)
+k_mx_product(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_big,
+             const KernelParams p)
 {
     using L = Layout<NT, STAGES, CG>;
-    constexpr int kBox = NT >= 32 ? 32 : 16;                   // rows per TMA load of the row operand
+    constexpr int kBox = 32, kBig = NT / CG;                   // rows per TMA load of the row operand
     extern __shared__ unsigned char raw[];
     unsigned char *base = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
     unsigned char *stage = base + L::kStageOff, *sf = base + L::kSfOff, *epi = base + L::kEpiOff;
@@ -501,6 +516,7 @@ k_mx_product(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(&map_w));
         asm volatile("prefetch.tensormap [%0];" ::"l"(&map_a));
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&map_big));
     }
     if (warp == kMmaWarp) tmem_alloc<CG>(tmem_slot, 512);
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -533,8 +549,12 @@ k_mx_product(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
     if (CG == 2) cluster_sync();                               // the peer's barriers are set up before anything arrives on them
     else __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = *tmem_slot;
-    const int tiles = ends[p.P - 1];
+    // All 512 columns belong to this CTA, so they start at 0: a constant in every TMEM address.  (Anything else
+    // would be reported and no tile touched.)
+    constexpr uint32_t tmem = 0;
+    const bool whole = *tmem_slot == 0;
+    if (tid == 0 && !whole) *quit = 1;
+    const int tiles = whole ? ends[p.P - 1] : 0;
     const int steps = (p.K + kStageK - 1) / kStageK;
     constexpr uint32_t kSfCol = 2 * NT;                        // scale columns follow the two accumulators
     constexpr uint32_t kSfaCols = 8, kSfbCols = 8 * L::kRB;    // per stage parity
@@ -546,22 +566,27 @@ k_mx_product(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
     // cycles each, 700-1300 per stage, which bound the whole kernel.)
     if (warp == kTmaWarp) {
         int issued = 0, s = 0;
+        const uint32_t lead = lead_addr<CG>(full);
         unsigned parity = 1;                                   // a fresh barrier passes the wait for parity 1
         bool ok = true;
         Tile t;
-        for (TileStream<NT, CG> stream(p, ends, tiles); ok && stream.next(t);) {
+        for (TileStream<NT, CG> stream(p, ends, tiles); ok && next_uniform(stream, t);) {
             const int half = t.n() / CG;                       // rows of the tile in this CTA
-            const int loads = (half + kBox - 1) / kBox;
+            // each TMA instruction costs its warp some 80 cycles: many rows come in one box, few in boxes of 32
+            const bool big = half > 2 * kBox;
+            const int loads = big ? 1 : (half + kBox - 1) / kBox;
+            const uint32_t bytes = CG * (kATile + (big ? kBig : loads * kBox) * kRowBytes);
             for (int k = 0; k < steps; ++k) {
                 ok = __all_sync(0xffffffffu, wait_for(&empty[s], parity, quit, p.spin_limit));
                 if (!ok) break;
                 unsigned char *a = stage + s * L::kStage, *b = a + kATile;
                 if (elect_one()) {
                     // the first CTA's barrier counts the bytes of both
-                    if (rank == 0) mbar_expect_tx(&full[s], CG * (kATile + loads * kBox * kRowBytes));
-                    const uint32_t bar = lead_addr<CG>(&full[s]);
+                    if (rank == 0) mbar_expect_tx(&full[s], bytes);
+                    const uint32_t bar = lead + s * 8;
                     tma_3d<CG>(a, &map_w, k * kRowBytes, t.feat + rank * kFeat, t.slot, bar);
-                    for (int l = 0; l < loads; ++l)
+                    if (big) tma_2d<CG>(b, &map_big, k * kRowBytes, t.row + rank * half, bar);
+                    else for (int l = 0; l < loads; ++l)
                         tma_2d<CG>(b + l * kBox * kRowBytes, &map_a, k * kRowBytes, t.row + rank * half + l * kBox, bar);
                 }
                 __syncwarp();
@@ -583,21 +608,23 @@ k_mx_product(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
         bool ok = true;
         const uint64_t stage_desc = desc_codes(smem_addr(stage)), sf_desc = desc_scales(smem_addr(sf));
         Tile t;
-        for (TileStream<NT, CG> stream(p, ends, tiles); ok && stream.next(t);) {
+        for (TileStream<NT, CG> stream(p, ends, tiles); ok && next_uniform(stream, t);) {
             ok = __all_sync(0xffffffffu, wait_for(&acc_empty[buf], acc_parity, quit, p.spin_limit));
             if (!ok) break;
             tc_fence_after();
             const uint32_t d = tmem + buf * NT;
             const int n = t.n();
             const uint32_t idesc = idesc_mxf4<CG>(n);
-            bool ready = mbar_test_wait(&full[s], parity);
+            bool ready = __all_sync(0xffffffffu, mbar_test_wait(&full[s], parity));
             for (int k = 0; k < steps; ++k, ++step_no) {
-                ok = __all_sync(0xffffffffu, ready || wait_for(&full[s], parity, quit, p.spin_limit));
-                if (!ok) break;
+                if (!ready) {
+                    ok = __all_sync(0xffffffffu, wait_for(&full[s], parity, quit, p.spin_limit));
+                    if (!ok) break;
+                }
                 tc_fence_after();
                 // ask for the next stage's barrier now: the answer arrives while this stage is issued
                 const int s_next = s + 1 == STAGES ? 0 : s + 1;
-                ready = mbar_test_wait(&full[s_next], s_next ? parity : parity ^ 1u);
+                const bool next_full = mbar_test_wait(&full[s_next], s_next ? parity : parity ^ 1u);
                 // descriptors count in 16-byte units
                 const uint64_t a = stage_desc + (uint32_t)(s * (L::kStage >> 4)), b = a + (kATile >> 4);
                 const uint64_t sfs = sf_desc + (uint32_t)(s * (L::kSf >> 4));
@@ -616,7 +643,7 @@ k_mx_product(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
                     mma_commit<CG>(&empty[s]);
                     if (k == steps - 1) mma_commit<CG>(&acc_full[buf]);
                 }
-                __syncwarp();
+                ready = __all_sync(0xffffffffu, next_full);
                 s = s_next;
                 if (s == 0) parity ^= 1u;
             }
@@ -819,11 +846,13 @@ cudaError_t launch(const MxProductArgs &a, cudaStream_t st)
     });
     if (attr != cudaSuccess) return attr;
     if (!encode_fn()) return cudaErrorNotSupported;
-    CUtensorMap map_w, map_a;
+    CUtensorMap map_w, map_a, map_big;
     const cuuint64_t row = (cuuint64_t)a.K / 2;
     const cuuint64_t wd[3] = {row, (cuuint64_t)a.N, (cuuint64_t)a.P}, ws[2] = {row, row * (cuuint64_t)a.N};
     const cuuint64_t ad[2] = {row, (cuuint64_t)a.rows}, as[1] = {row};
-    if (!encode(&map_w, a.w_codes, 3, wd, ws, kFeat) || !encode(&map_a, a.a_codes, 2, ad, as, 32)) return cudaErrorInvalidValue;
+    if (!encode(&map_w, a.w_codes, 3, wd, ws, kFeat) || !encode(&map_a, a.a_codes, 2, ad, as, 32) ||
+        !encode(&map_big, a.a_codes, 2, ad, as, NT / CG))
+        return cudaErrorInvalidValue;
     KernelParams p;
     p.a_scales = a.a_scales; p.w_scales = a.w_scales; p.slot_counts = a.slot_counts; p.slot_offsets = a.slot_offsets;
     p.rows = a.rows; p.P = a.P; p.N = a.N; p.K = a.K; p.y = static_cast<__nv_bfloat16 *>(a.y);
@@ -840,7 +869,7 @@ cudaError_t launch(const MxProductArgs &a, cudaStream_t st)
     at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at; cfg.numAttrs = a.pdl ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, kernel, map_w, map_a, p);
+    return cudaLaunchKernelEx(&cfg, kernel, map_w, map_a, map_big, p);
 }
 
 template <bool GATED>
