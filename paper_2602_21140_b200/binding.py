@@ -440,16 +440,28 @@ def _mx_pitch(cols: int) -> int:
     return (cols // 32 + 15) // 16 * 16
 
 
-def _is_mx(m: MxRows, device, lead=None) -> bool:
+def _is_mx(m: MxRows, index: int, lead=None) -> bool:
+    """4-bit rows on CUDA device `index`, of leading shape `lead` where one is given."""
     c, s = m.codes, m.scales
-    return (c.dtype == torch.uint8 and s.dtype == torch.uint8 and c.is_contiguous() and s.is_contiguous()
-            and c.device == device and s.device == device and c.dim() == s.dim() and c.dim() > 0 and c.shape[-1] % 16 == 0
-            and c.shape[:-1] == s.shape[:-1] and s.shape[-1] == _mx_pitch(m.cols) and (lead is None or tuple(c.shape[:-1]) == lead))
+    cs, ss = c.shape, s.shape
+    return (c.dtype is torch.uint8 and s.dtype is torch.uint8 and c.is_contiguous() and s.is_contiguous() and c.is_cuda and s.is_cuda
+            and c.get_device() == index and s.get_device() == index and len(cs) > 0 and cs[-1] % 16 == 0 and cs[:-1] == ss[:-1]
+            and ss[-1] == _mx_pitch(2 * cs[-1]) and (lead is None or cs[:-1] == lead))
+
+
+def _is_dense(t: torch.Tensor, dtype: torch.dtype, shape, index: int) -> bool:
+    return t.dtype is dtype and t.shape == shape and t.is_contiguous() and t.is_cuda and t.get_device() == index
+
+
+# The current stream of a device as the integer that the C entry points take.  (torch.cuda.current_stream builds
+# an object first: 3 of the 15 microseconds that a small call takes on the host.)
+def _raw_stream(index: int) -> int:
+    return torch._C._cuda_getCurrentRawStream(index)
 
 
 def _on_device(index: int, call, *args) -> int:
     """call(*args) with that device current (a kernel launch needs its stream's device)."""
-    if torch.cuda.current_device() == index:
+    if torch._C._cuda_getDevice() == index:
         return call(*args)
     with torch.cuda.device(index):
         return call(*args)
@@ -467,16 +479,17 @@ def mx_quantize(x: torch.Tensor, out: MxRows | None = None) -> MxRows:
     """Rows of ``x`` ([..., cols], bf16 / fp16 / fp32) in 4 bits, on the current stream of its device.
     A 2-D ``x`` may have any row stride that keeps its rows 16-byte aligned; others are contiguous."""
     _require(x.is_cuda and x.dtype in _DTYPE_CODE and x.dim() >= 1 and x.shape[-1] > 0 and x.shape[-1] % 32 == 0, "mx_quantize")
-    _require(x.is_contiguous() or (x.dim() == 2 and x.stride(1) == 1), "mx_quantize")
-    cols = x.shape[-1]
+    flat = x.is_contiguous()
+    _require(flat or (x.dim() == 2 and x.stride(1) == 1), "mx_quantize")
+    cols, index = x.shape[-1], x.get_device()
     if out is None:
         out = mx_empty(*x.shape, device=x.device)
     else:
-        _require(_is_mx(out, x.device, tuple(x.shape[:-1])) and out.cols == cols, "mx_quantize")
+        _require(_is_mx(out, x.get_device(), x.shape[:-1]) and out.cols == cols, "mx_quantize")
     rows = x.numel() // cols
-    stride = x.stride(0) if x.dim() == 2 and not x.is_contiguous() else cols
-    st = _on_device(x.device.index, moe_mx_quantize, x.data_ptr(), _DTYPE_CODE[x.dtype], rows, cols, stride,
-                    out.codes.data_ptr(), out.scales.data_ptr(), torch.cuda.current_stream(x.device).cuda_stream)
+    stride = cols if flat else x.stride(0)
+    st = _on_device(index, moe_mx_quantize, x.data_ptr(), _DTYPE_CODE[x.dtype], rows, cols, stride,
+                    out.codes.data_ptr(), out.scales.data_ptr(), _raw_stream(index))
     if st != MOE_OK:
         raise MoeError(st, "moe_mx_quantize")
     return out
@@ -484,16 +497,19 @@ def mx_quantize(x: torch.Tensor, out: MxRows | None = None) -> MxRows:
 
 def mx_dequantize(m: MxRows, dtype: torch.dtype = torch.bfloat16, out: torch.Tensor | None = None) -> torch.Tensor:
     """The values that 4-bit rows stand for."""
-    device = m.codes.device
-    _require(m.codes.is_cuda and dtype in _DTYPE_CODE and _is_mx(m, device) and m.cols > 0, "mx_dequantize")
-    shape = (*m.codes.shape[:-1], m.cols)
+    index = m.codes.get_device()
+    _require(dtype in _DTYPE_CODE and _is_mx(m, index) and m.codes.shape[-1] > 0, "mx_dequantize")
+    shape, cols = (*m.codes.shape[:-1], m.cols), m.cols
+    stride = cols
     if out is None:
-        out = torch.empty(shape, dtype=dtype, device=device)
-    _require(tuple(out.shape) == shape and out.dtype == dtype and out.device == device
-             and (out.is_contiguous() or (out.dim() == 2 and out.stride(1) == 1)), "mx_dequantize")
-    stride = out.stride(0) if out.dim() == 2 and not out.is_contiguous() else m.cols
-    st = _on_device(device.index, moe_mx_dequantize, m.codes.data_ptr(), m.scales.data_ptr(), out.numel() // m.cols, m.cols,
-                    out.data_ptr(), _DTYPE_CODE[dtype], stride, torch.cuda.current_stream(device).cuda_stream)
+        out = torch.empty(shape, dtype=dtype, device=m.codes.device)
+    else:
+        flat = out.is_contiguous()
+        _require(out.shape == shape and out.dtype is dtype and out.is_cuda and out.get_device() == index
+                 and (flat or (out.dim() == 2 and out.stride(1) == 1)), "mx_dequantize")
+        stride = cols if flat else out.stride(0)
+    st = _on_device(index, moe_mx_dequantize, m.codes.data_ptr(), m.scales.data_ptr(), out.numel() // cols, cols, out.data_ptr(),
+                    _DTYPE_CODE[dtype], stride, _raw_stream(index))
     if st != MOE_OK:
         raise MoeError(st, "moe_mx_dequantize")
     return out
@@ -588,51 +604,49 @@ class MoeRouter:
         return y
 
     # -- 4-bit rows: dispatch and the experts' products ----------------------
-    def _here(self, t: torch.Tensor, dtype, shape) -> bool:
-        return t.dtype == dtype and tuple(t.shape) == shape and t.is_contiguous() and t.device == self._index_device()
-
-    def _index_device(self) -> torch.device:
+    def _index(self) -> int:
         if self.device.index is None:
             self.device = torch.device("cuda", torch.cuda.current_device())
-        return self.device
+        return self.device.index
 
     def mx_dispatch(self, logits: torch.Tensor, x: torch.Tensor, out: DispatchBuffers | None = None,
                     rows: MxRows | None = None):
         """As dispatch, with a send buffer of 4-bit rows.  Returns (buffers, rows)."""
-        c, dev = self.cfg, self._index_device()
-        T = x.shape[0]
-        n = T * c.top_k
-        _require(self._here(logits, torch.float32, (T, c.num_experts)) and self._here(x, torch.bfloat16, (T, c.hidden)), "mx_dispatch")
+        c, dev = self.cfg, self._index()
+        T, H = x.shape[0], c.hidden
+        _require(_is_dense(logits, torch.float32, (T, c.num_experts), dev) and _is_dense(x, torch.bfloat16, (T, H), dev), "mx_dispatch")
         if out is None:
             out = self.alloc_outputs(T, send_buf=False)
         if rows is None:
-            rows = mx_empty(n, c.hidden, device=dev)
+            rows = mx_empty(T * c.top_k, H, device=self.device)
         else:
-            _require(_is_mx(rows, dev, (n,)) and rows.cols == c.hidden, "mx_dispatch")
+            _require(_is_mx(rows, dev, (T * c.top_k,)) and rows.cols == H, "mx_dispatch")
         st = moe_mx_dispatch(self._ctx, logits.data_ptr(), x.data_ptr(), T, out.as_struct(), rows.codes.data_ptr(),
-                             rows.scales.data_ptr(), self._stream())
+                             rows.scales.data_ptr(), _raw_stream(dev))
         if st != MOE_OK:
             raise MoeError(st, "moe_mx_dispatch")
         return out, rows
 
-    def _segments_ok(self, rows: MxRows, slot_counts, slot_offsets, weight: MxRows) -> bool:
-        dev, P = self._index_device(), self.num_slots
-        return (_is_mx(rows, dev) and rows.codes.dim() == 2 and _is_mx(weight, dev) and weight.codes.dim() == 3
-                and weight.codes.shape[0] == P and weight.cols == rows.cols and self._here(slot_counts, torch.int32, (P,))
+    def _segments_ok(self, rows: MxRows, slot_counts, slot_offsets, weight: MxRows, dev: int) -> bool:
+        P, w = self.num_slots, weight.codes.shape
+        return (_is_mx(rows, dev) and len(rows.codes.shape) == 2 and _is_mx(weight, dev) and len(w) == 3 and w[0] == P
+                and w[2] == rows.codes.shape[1] and _is_dense(slot_counts, torch.int32, (P,), dev)
                 and slot_offsets.dim() == 1 and slot_offsets.shape[0] >= P
-                and self._here(slot_offsets, torch.int32, tuple(slot_offsets.shape)))
+                and _is_dense(slot_offsets, torch.int32, slot_offsets.shape, dev))
 
     def mx_expert_product(self, rows: MxRows, slot_counts: torch.Tensor, slot_offsets: torch.Tensor, weight: MxRows,
                           y: torch.Tensor | None = None) -> torch.Tensor:
         """y[r] = weight[slot of r] @ rows[r]: weight [P, n_out, cols] and rows [n, cols] in 4 bits, y [n, n_out] bf16."""
-        _require(self._segments_ok(rows, slot_counts, slot_offsets, weight), "mx_expert_product")
+        dev = self._index()
+        _require(self._segments_ok(rows, slot_counts, slot_offsets, weight, dev), "mx_expert_product")
         n, n_out = rows.codes.shape[0], weight.codes.shape[1]
         if y is None:
             y = torch.empty((n, n_out), dtype=torch.bfloat16, device=self.device)
-        _require(self._here(y, torch.bfloat16, (n, n_out)), "mx_expert_product")
+        else:
+            _require(_is_dense(y, torch.bfloat16, (n, n_out), dev), "mx_expert_product")
         st = moe_mx_expert_product(self._ctx, rows.codes.data_ptr(), rows.scales.data_ptr(), n, slot_counts.data_ptr(),
                                    slot_offsets.data_ptr(), weight.codes.data_ptr(), weight.scales.data_ptr(), n_out, rows.cols,
-                                   y.data_ptr(), self._stream())
+                                   y.data_ptr(), _raw_stream(dev))
         if st != MOE_OK:
             raise MoeError(st, "moe_mx_expert_product")
         return y
@@ -640,16 +654,17 @@ class MoeRouter:
     def mx_expert_gated(self, rows: MxRows, slot_counts: torch.Tensor, slot_offsets: torch.Tensor, gate_up: MxRows,
                         out: MxRows | None = None) -> MxRows:
         """silu(gate) * up in 4 bits.  gate_up [P, 2 * n_hidden, cols]: row 2i is the gate of feature i, row 2i + 1 its up-projection."""
-        _require(self._segments_ok(rows, slot_counts, slot_offsets, gate_up) and gate_up.codes.shape[1] % 64 == 0
+        dev = self._index()
+        _require(self._segments_ok(rows, slot_counts, slot_offsets, gate_up, dev) and gate_up.codes.shape[1] % 64 == 0
                  and gate_up.codes.shape[1] > 0, "mx_expert_gated")
         n, n_hidden = rows.codes.shape[0], gate_up.codes.shape[1] // 2
         if out is None:
             out = mx_empty(n, n_hidden, device=self.device)
         else:
-            _require(_is_mx(out, self.device, (n,)) and out.cols == n_hidden, "mx_expert_gated")
+            _require(_is_mx(out, dev, (n,)) and out.cols == n_hidden, "mx_expert_gated")
         st = moe_mx_expert_gated(self._ctx, rows.codes.data_ptr(), rows.scales.data_ptr(), n, slot_counts.data_ptr(),
                                  slot_offsets.data_ptr(), gate_up.codes.data_ptr(), gate_up.scales.data_ptr(), n_hidden, rows.cols,
-                                 out.codes.data_ptr(), out.scales.data_ptr(), self._stream())
+                                 out.codes.data_ptr(), out.scales.data_ptr(), _raw_stream(dev))
         if st != MOE_OK:
             raise MoeError(st, "moe_mx_expert_gated")
         return out
@@ -672,17 +687,20 @@ class MoeRouter:
     def combine_backward(self, expert_buf: torch.Tensor, dy: torch.Tensor, d_expert_buf: torch.Tensor | None = None,
                          d_weights: torch.Tensor | None = None):
         """Gradients of the latest combine by its rows and its gate weights: (d_expert_buf, d_weights)."""
-        c, T = self.cfg, dy.shape[0]
-        n = T * c.top_k
+        c, T, dev = self.cfg, dy.shape[0], self._index()
+        H, k = c.hidden, c.top_k
+        ok = _is_dense(expert_buf, torch.bfloat16, (T * k, H), dev) and _is_dense(dy, torch.bfloat16, (T, H), dev)
         if d_expert_buf is None:
-            d_expert_buf = torch.empty((n, c.hidden), dtype=torch.bfloat16, device=self.device)
+            d_expert_buf = torch.empty((T * k, H), dtype=torch.bfloat16, device=self.device)
+        else:
+            ok = ok and _is_dense(d_expert_buf, torch.bfloat16, (T * k, H), dev)
         if d_weights is None:
-            d_weights = torch.empty((T, c.top_k), dtype=torch.float32, device=self.device)
-        _require(self._here(expert_buf, torch.bfloat16, (n, c.hidden)) and self._here(dy, torch.bfloat16, (T, c.hidden))
-                 and self._here(d_expert_buf, torch.bfloat16, (n, c.hidden))
-                 and self._here(d_weights, torch.float32, (T, c.top_k)), "combine_backward")
+            d_weights = torch.empty((T, k), dtype=torch.float32, device=self.device)
+        else:
+            ok = ok and _is_dense(d_weights, torch.float32, (T, k), dev)
+        _require(ok, "combine_backward")
         st = moe_combine_backward(self._ctx, expert_buf.data_ptr(), dy.data_ptr(), T, d_expert_buf.data_ptr(),
-                                  d_weights.data_ptr(), self._stream())
+                                  d_weights.data_ptr(), _raw_stream(dev))
         if st != MOE_OK:
             raise MoeError(st, "moe_combine_backward")
         return d_expert_buf, d_weights
@@ -690,22 +708,25 @@ class MoeRouter:
     def dispatch_backward(self, logits: torch.Tensor | None, d_send_buf: torch.Tensor, d_weights: torch.Tensor | None = None,
                           dx: torch.Tensor | None = None, d_logits: torch.Tensor | None = None):
         """Gradients of the latest dispatch: (dx, d_logits).  d_logits is None without d_weights."""
-        c = self.cfg
-        n = d_send_buf.shape[0]
-        T = n // c.top_k
+        c, dev = self.cfg, self._index()
+        T = d_send_buf.shape[0] // c.top_k
+        H, k, E = c.hidden, c.top_k, c.num_experts
+        ok = _is_dense(d_send_buf, torch.bfloat16, (T * k, H), dev)
         if dx is None:
-            dx = torch.empty((T, c.hidden), dtype=torch.bfloat16, device=self.device)
-        ok = self._here(d_send_buf, torch.bfloat16, (T * c.top_k, c.hidden)) and self._here(dx, torch.bfloat16, (T, c.hidden))
+            dx = torch.empty((T, H), dtype=torch.bfloat16, device=self.device)
+        else:
+            ok = ok and _is_dense(dx, torch.bfloat16, (T, H), dev)
         if d_weights is not None:
+            ok = ok and _is_dense(d_weights, torch.float32, (T, k), dev)
             if d_logits is None:
-                d_logits = torch.empty((T, c.num_experts), dtype=torch.float32, device=self.device)
-            ok = (ok and self._here(d_weights, torch.float32, (T, c.top_k))
-                  and self._here(d_logits, torch.float32, (T, c.num_experts)))
-        ok = ok and (logits is None or self._here(logits, torch.float32, (T, c.num_experts)))
+                d_logits = torch.empty((T, E), dtype=torch.float32, device=self.device)
+        if d_logits is not None:
+            ok = ok and _is_dense(d_logits, torch.float32, (T, E), dev)
+        ok = ok and (logits is None or _is_dense(logits, torch.float32, (T, E), dev))
         _require(ok, "dispatch_backward")
         st = moe_dispatch_backward(self._ctx, 0 if logits is None else logits.data_ptr(), d_send_buf.data_ptr(),
                                    0 if d_weights is None else d_weights.data_ptr(), T, dx.data_ptr(),
-                                   0 if d_logits is None else d_logits.data_ptr(), self._stream())
+                                   0 if d_logits is None else d_logits.data_ptr(), _raw_stream(dev))
         if st != MOE_OK:
             raise MoeError(st, "moe_dispatch_backward")
         return dx, d_logits

@@ -24,88 +24,188 @@ struct CombineBackwardParams {
     const float *topk_weights;   // [T,k]
     const int32_t *topk_slot;    // [T,k]
     const float *slot_scale;     // [P]
+    const uint4 *zero_row;       // [H/8] zeros: stands in for a row that was not placed
+    Control *ctl;
+    unsigned spin_limit;
+    int slots;                   // ring slots
+    int slot_units;              // 16-byte units per slot
 };
 
-constexpr int kCombineBwdThreads = 256;
-constexpr int kCombineBwdUnits = 4;      // 16-byte units of dy a thread keeps in registers
+constexpr int kCombineBwdWarps = 8;                        // warps that compute; one more copies
+constexpr int kCombineBwdUnits = 4;                        // 16-byte units of a slot per thread
+constexpr int kCombineBwdSlotUnits = kCombineBwdWarps * 32 * kCombineBwdUnits;   // 16 KB
+constexpr int kCombineBwdMaxSlots = 15;
 constexpr int kMaxTopKDevice = 16;
 
-// One CTA per token: its threads hold the token's dy row (up to 8192 columns at a time) in registers
-// while the k expert rows stream past, each read once for the dot product with the d_buf row going
-// out in its place.  Bound by HBM: (1 + 2k) rows of traffic per token.  The next row's loads are
-// issued before the present row is worked on.  Dot products are reduced in a fixed order.
-__global__ void __launch_bounds__(kCombineBwdThreads) k_combine_backward(CombineBackwardParams p)
+struct CombineBwdTable {                                   // one token's assignments
+    int row[kMaxTopKDevice];
+    float coef[kMaxTopKDevice], scale[kMaxTopKDevice];
+};
+
+inline size_t combine_backward_smem(int slots, int slot_units) { return (size_t)slots * slot_units * 16 + 128; }
+
+// A CTA per token, persistent: one warp asks the TMA engine for the token's dy row and its k expert rows (16 KB
+// of each at a time) through a ring of shared-memory slots that runs ahead over tokens, eight warps keep the dy
+// row in registers, take each expert row from its slot for the dot product and write the d_buf row in its place.
+// Bound by HBM: (1 + 2k) rows of traffic per token.  The ring keeps some 200 KB per SM in flight and has the next
+// token's rows coming while the present one ends; with rows loaded into registers instead the start of every
+// token was idle and 32 KB per SM the most that fitted (8192 tokens of 7168, k = 8: 359 us).
+// Dot products are summed per thread, over the warp and over the warps, always in the same order.
+// K = top_k known at compile time, 0 = any.
+template <int K>
+__global__ void __launch_bounds__((kCombineBwdWarps + 1) * 32, 2) k_combine_backward(CombineBackwardParams p)
 {
-    constexpr int U = kCombineBwdUnits;
-    __shared__ float s_coef[kMaxTopKDevice], s_scale[kMaxTopKDevice];
-    __shared__ int s_row[kMaxTopKDevice];
-    __shared__ float s_dot[kCombineBwdThreads / 32][kMaxTopKDevice];
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, nw = blockDim.x >> 5;
-    const int k = p.k;
+    constexpr int U = kCombineBwdUnits, KK = K > 0 ? K : kMaxTopKDevice;
+    extern __shared__ __align__(128) unsigned char ring[];
+    __shared__ __align__(8) uint64_t full[kCombineBwdMaxSlots], empty[kCombineBwdMaxSlots];
+    __shared__ CombineBwdTable table[kCombineBwdMaxSlots + 1];
+    __shared__ float s_dot[2][kCombineBwdWarps][kMaxTopKDevice];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int k = K > 0 ? K : p.k, S = p.slots;
+    if (tid == 0) {
+        for (int s = 0; s < S; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], kCombineBwdWarps); }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    __syncthreads();
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    for (int t = blockIdx.x; t < p.T; t += gridDim.x) {
-        __syncthreads();                                      // the previous token's tables are free
-        if (tid < k) {
-            const size_t i = (size_t)t * k + tid;
-            const int slot = __ldg(p.topk_slot + i), r = __ldg(p.dst_row + i);
-            const bool placed = (unsigned)slot < (unsigned)p.P && r >= 0 && r < (long long)p.T * k;
-            const float scale = placed ? __ldg(p.slot_scale + slot) : 0.0f;
-            s_row[tid] = placed ? r : -1;
-            s_scale[tid] = scale;
-            s_coef[tid] = placed ? __fmul_rn(__ldg(p.topk_weights + i), scale) : 0.0f;
-        }
-        for (int q = tid; q < nw * kMaxTopKDevice; q += blockDim.x) (&s_dot[0][0])[q] = 0.0f;
-        __syncthreads();
-        const uint4 *dy = p.dy + (size_t)t * p.hv;
-        for (int base = 0; base < p.hv; base += blockDim.x * U) {
-            uint4 g[U], v[U], nv[U];
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int c = base + u * blockDim.x + tid;
-                g[u] = c < p.hv ? ld_stream_v4(dy + c) : make_uint4(0u, 0u, 0u, 0u);
-                const int r0 = s_row[0];
-                v[u] = (c < p.hv && r0 >= 0) ? ld_stream_v4(p.buf + (size_t)r0 * p.hv + c) : make_uint4(0u, 0u, 0u, 0u);
-            }
-            for (int j = 0; j < k; ++j) {
-                const int r = s_row[j], rn = j + 1 < k ? s_row[j + 1] : -1;
-#pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    const int c = base + u * blockDim.x + tid;
-                    nv[u] = (c < p.hv && rn >= 0) ? ld_stream_v4(p.buf + (size_t)rn * p.hv + c) : make_uint4(0u, 0u, 0u, 0u);
+    const int chunks = (p.hv + p.slot_units - 1) / p.slot_units;
+    const size_t slot_bytes = (size_t)p.slot_units * 16;
+    int s = 0;
+    bool ok = true;
+
+    if (warp == kCombineBwdWarps) {
+        unsigned parity = 1;
+        int issued = 0, entry = 0;
+        // lanes j < k hold the assignments of the token to come
+        int row = -1, row_n = -1; float coef = 0.0f, scale = 0.0f, coef_n = 0.0f, scale_n = 0.0f;
+        auto fetch = [&](int t, int &r, float &c, float &sc) {
+            r = -1; c = 0.0f; sc = 0.0f;
+            if (lane < k && t < p.T) {
+                const size_t i = (size_t)t * k + lane;
+                const int slot = __ldg(p.topk_slot + i), d = __ldg(p.dst_row + i);
+                if ((unsigned)slot < (unsigned)p.P && d >= 0 && d < (long long)p.T * k) {
+                    r = d;
+                    sc = __ldg(p.slot_scale + slot);
+                    c = __fmul_rn(__ldg(p.topk_weights + i), sc);
                 }
-                float dot = 0.0f;
-                const float coef = s_coef[j];
+            }
+        };
+        fetch(blockIdx.x, row, coef, scale);
+        for (int t = blockIdx.x; t < p.T && ok; t += gridDim.x) {
+            fetch(t + gridDim.x, row_n, coef_n, scale_n);
+            // Table entries are reused after kCombineBwdMaxSlots + 1 tokens; a token takes at least two slots, so
+            // the ring never holds that many.
+            if (lane < k) { table[entry].row[lane] = row; table[entry].coef[lane] = coef; table[entry].scale[lane] = scale; }
+            __syncwarp();
+            for (int c = 0; c < chunks && ok; ++c) {
+                const int u0 = c * p.slot_units;
+                const unsigned bytes = (unsigned)min(p.slot_units, p.hv - u0) * 16u;
+                for (int j = -1; j < k; ++j) {                  // dy, then the k rows
+                    const int r = __shfl_sync(0xffffffffu, row, j < 0 ? 0 : j);
+                    unsigned spins = 0;
+                    while (!mbar_try_wait(&empty[s], parity))
+                        if (++spins > p.spin_limit) { ok = false; break; }
+                    ok = __all_sync(0xffffffffu, ok);
+                    if (!ok) break;
+                    if (lane == 0) {
+                        const uint4 *src = j < 0 ? p.dy + (size_t)t * p.hv : r >= 0 ? p.buf + (size_t)r * p.hv : p.zero_row;
+                        mbar_expect_tx(&full[s], bytes);        // also publishes the table entry
+                        bulk_load(ring + s * slot_bytes, src + u0, bytes, &full[s]);
+                    }
+                    __syncwarp();
+                    ++issued;
+                    if (++s == S) { s = 0; parity ^= 1u; }
+                }
+            }
+            row = row_n; coef = coef_n; scale = scale_n;
+            if (++entry == kCombineBwdMaxSlots + 1) entry = 0;
+        }
+        if (!ok) {
+            if (lane == 0) report_status(p.ctl, kDevTimeout);
+            // copies in flight still land in this CTA's shared memory: a bounded wait for each
+            for (int m = max(0, issued - S); m < issued; ++m) {
+                unsigned spins = 0;
+                while (!mbar_try_wait(&full[m % S], (unsigned)(m / S) & 1u) && ++spins < p.spin_limit) {}
+            }
+        }
+        return;
+    }
+
+    unsigned parity = 0;
+    int entry = 0, side = 0;
+    auto take = [&](uint4 (&v)[U], int units) {                 // this thread's units of the next slot, which is then handed back
+        unsigned spins = 0;
+        while (ok && !mbar_try_wait(&full[s], parity))
+            if (++spins > p.spin_limit) ok = false;
+        const uint4 *src = reinterpret_cast<const uint4 *>(ring + s * slot_bytes);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int c = u * kCombineBwdWarps * 32 + tid;
+            v[u] = ok && c < units ? src[c] : make_uint4(0u, 0u, 0u, 0u);
+        }
+        __syncwarp();
+        if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_addr(&empty[s])) : "memory");
+        if (++s == S) { s = 0; parity ^= 1u; }
+    };
+    for (int t = blockIdx.x; t < p.T; t += gridDim.x) {
+        float dot[KK];
+#pragma unroll
+        for (int j = 0; j < KK; ++j) dot[j] = 0.0f;
+        for (int c = 0; c < chunks; ++c) {
+            const int u0 = c * p.slot_units, units = min(p.slot_units, p.hv - u0);
+            uint4 g[U];
+            take(g, units);
+#pragma unroll
+            for (int j = 0; j < KK; ++j) {
+                if (K == 0 && j >= k) break;
+                uint4 v[U];
+                take(v, units);
+                const int r = table[entry].row[j];
+                const float coef = table[entry].coef[j];
+                uint4 *dst = p.d_buf + (size_t)max(r, 0) * p.hv + u0;
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
-                    const int c = base + u * blockDim.x + tid;
-                    if (c >= p.hv || r < 0) continue;
+                    const int at = u * kCombineBwdWarps * 32 + tid;
+                    if (at >= units) break;
                     const __nv_bfloat162 *a = reinterpret_cast<const __nv_bfloat162 *>(&v[u]);
                     const __nv_bfloat162 *b = reinterpret_cast<const __nv_bfloat162 *>(&g[u]);
                     float o[8];
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
                         const float2 fa = __bfloat1622float2(a[q]), fb = __bfloat1622float2(b[q]);
-                        dot = __fmaf_rn(fa.x, fb.x, dot);
-                        dot = __fmaf_rn(fa.y, fb.y, dot);
+                        dot[j] = __fmaf_rn(fa.x, fb.x, dot[j]);
+                        dot[j] = __fmaf_rn(fa.y, fb.y, dot[j]);
                         o[2 * q] = coef * fb.x; o[2 * q + 1] = coef * fb.y;
                     }
-                    st_stream_v4(p.d_buf + (size_t)r * p.hv + c, pack_bf16x8(o));
+                    if (ok && r >= 0) st_stream_v4(dst + at, pack_bf16x8(o));
                 }
-#pragma unroll
-                for (int off = 16; off > 0; off >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, off);
-                if (lane == 0) s_dot[warp][j] += dot;
-#pragma unroll
-                for (int u = 0; u < U; ++u) v[u] = nv[u];
             }
         }
-        __syncthreads();
-        if (tid < k) {
-            float dot = 0.0f;
-            for (int w = 0; w < nw; ++w) dot += s_dot[w][tid];
-            p.d_weights[(size_t)t * k + tid] = s_row[tid] >= 0 ? s_scale[tid] * dot : 0.0f;
+#pragma unroll
+        for (int j = 0; j < KK; ++j) {
+            if (K == 0 && j >= k) break;
+#pragma unroll
+            for (int off = 16; off > 0; off >>= 1) dot[j] += __shfl_xor_sync(0xffffffffu, dot[j], off);
+            if (lane == 0) s_dot[side][warp][j] = dot[j];
         }
+        // one barrier a token: the other half of s_dot is used in between.  It also carries the verdict, so that
+        // the warps leave together.
+        uint32_t good;
+        asm volatile("{\n\t.reg .pred a, b;\n\tsetp.ne.u32 a, %1, 0;\n\tbarrier.cta.red.and.pred b, 1, %2, a;\n\tselp.u32 %0, 1, 0, b;\n\t}"
+                     : "=r"(good) : "r"((uint32_t)ok), "n"(kCombineBwdWarps * 32) : "memory");
+        ok = good != 0;
+        if (!ok) break;
+        if (tid < k) {
+            float sum = 0.0f;
+#pragma unroll
+            for (int w = 0; w < kCombineBwdWarps; ++w) sum += s_dot[side][w][tid];
+            p.d_weights[(size_t)t * k + tid] = table[entry].scale[tid] * sum;
+        }
+        side ^= 1;
+        if (++entry == kCombineBwdMaxSlots + 1) entry = 0;
     }
+    if (!ok && tid == 0) report_status(p.ctl, kDevTimeout);
 }
 
 struct RouteBackwardParams {

@@ -493,7 +493,10 @@ bool set_kernel_attributes_once()
           && cudaFuncSetAttribute(k_combine_bulk<4, 2>, at, sm) == cudaSuccess
           && cudaFuncSetAttribute(k_combine_bulk<1, 0>, at, sm) == cudaSuccess
           && cudaFuncSetAttribute(k_combine_bulk<2, 0>, at, sm) == cudaSuccess
-          && cudaFuncSetAttribute(k_combine_bulk<4, 0>, at, sm) == cudaSuccess;
+          && cudaFuncSetAttribute(k_combine_bulk<4, 0>, at, sm) == cudaSuccess
+          && cudaFuncSetAttribute(k_combine_backward<8>, at, 112 * 1024) == cudaSuccess
+          && cudaFuncSetAttribute(k_combine_backward<2>, at, 112 * 1024) == cudaSuccess
+          && cudaFuncSetAttribute(k_combine_backward<0>, at, 112 * 1024) == cudaSuccess;
     });
     return ok;
 }
@@ -1185,12 +1188,19 @@ moe_status moe_combine_backward(moe_ctx *ctx, const void *expert_buf, const void
     p.T = T; p.k = d.k; p.hv = d.H / 8; p.P = d.P;
     p.dst_row = ctx->last_dst_row; p.topk_weights = ctx->last_weights; p.topk_slot = ctx->last_slot;
     p.slot_scale = ctx->d_slot_scale;
-    const int threads = std::min(kCombineBwdThreads, std::max(32, (p.hv + 31) / 32 * 32));
-    const int grid = std::min(T, ctx->sm_count * 8 * (kCombineBwdThreads / threads));
-    if (launch_kernel(k_combine_backward, dim3(grid), dim3(threads), 0, static_cast<cudaStream_t>(cuda_stream), ctx->pdl, p) !=
-        cudaSuccess)
-        return MOE_ERR_CUDA;
-    return MOE_OK;
+    p.zero_row = ctx->d_zero_row; p.ctl = ctx->d_ctl; p.spin_limit = ctx->spin_limit;
+    // two CTAs per SM, each with a ring of half the shared memory
+    p.slot_units = std::min(p.hv, kCombineBwdSlotUnits);
+    const size_t half = (227 * 1024 - 2 * 6 * 1024) / 2;
+    p.slots = std::min<int>(kCombineBwdMaxSlots, (int)((half - 128) / ((size_t)p.slot_units * 16)));
+    const int grid = std::min(T, ctx->sm_count * 2);
+    const dim3 g(grid), b((kCombineBwdWarps + 1) * 32);
+    const size_t sm = combine_backward_smem(p.slots, p.slot_units);
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    const cudaError_t e = d.k == 8   ? launch_kernel(k_combine_backward<8>, g, b, sm, st, ctx->pdl, p)
+                          : d.k == 2 ? launch_kernel(k_combine_backward<2>, g, b, sm, st, ctx->pdl, p)
+                                     : launch_kernel(k_combine_backward<0>, g, b, sm, st, ctx->pdl, p);
+    return e == cudaSuccess ? MOE_OK : MOE_ERR_CUDA;
 }
 
 moe_status moe_dispatch_backward(moe_ctx *ctx, const float *logits, const void *d_send_buf, const float *d_weights, int32_t T,
