@@ -37,19 +37,48 @@ constexpr int kCombineBwdSlotUnits = kCombineBwdWarps * 32 * kCombineBwdUnits;  
 constexpr int kCombineBwdMaxSlots = 15;
 constexpr int kMaxTopKDevice = 16;
 
+// Dynamic tokens without a counter in memory: the grid has a CTA per token, and a resident CTA takes over the
+// next one that has not been launched yet (cluster launch control).  The answer arrives in shared memory behind
+// an mbarrier, so it is asked for a token ahead.
+__device__ __forceinline__ void clc_request(void *answer, uint64_t *bar)
+{
+    mbar_expect_tx(bar, 16);
+    asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(smem_addr(answer)),
+                 "r"(smem_addr(bar))
+                 : "memory");
+}
+
+// blockIdx.x of the CTA that was taken over, -1 if none was left (then nothing may be asked again)
+__device__ __forceinline__ int clc_answer(const void *answer)
+{
+    int ok, x;
+    asm volatile(
+        "{\n\t.reg .b128 r;\n\t.reg .pred p;\n\t"
+        "ld.shared.b128 r, [%2];\n\t"
+        "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, r;\n\t"
+        "selp.s32 %0, 1, 0, p;\n\tmov.s32 %1, 0;\n\t"
+        "@p clusterlaunchcontrol.query_cancel.get_first_ctaid::x.b32.b128 %1, r;\n\t}"
+        : "=r"(ok), "=r"(x)
+        : "r"(smem_addr(answer))
+        : "memory");
+    return ok ? x : -1;
+}
+
 struct CombineBwdTable {                                   // one token's assignments
+    int token;                                             // -1: no more
     int row[kMaxTopKDevice];
     float coef[kMaxTopKDevice], scale[kMaxTopKDevice];
 };
 
 inline size_t combine_backward_smem(int slots, int slot_units) { return (size_t)slots * slot_units * 16 + 128; }
 
-// A CTA per token, persistent: one warp asks the TMA engine for the token's dy row and its k expert rows (16 KB
+// A CTA per token, and as many tokens per CTA as it gets done: one warp asks the TMA engine for the token's dy row and its k expert rows (16 KB
 // of each at a time) through a ring of shared-memory slots that runs ahead over tokens, eight warps keep the dy
 // row in registers, take each expert row from its slot for the dot product and write the d_buf row in its place.
 // Bound by HBM: (1 + 2k) rows of traffic per token.  The ring keeps some 200 KB per SM in flight and has the next
 // token's rows coming while the present one ends; with rows loaded into registers instead the start of every
-// token was idle and 32 KB per SM the most that fitted (8192 tokens of 7168, k = 8: 359 us).
+// token was idle and 32 KB per SM the most that fitted.  Tokens are taken as CTAs get free, because SMs do not get
+// equal shares of HBM: dealt out in advance, the SMs were busy for 83 % of the kernel.
 // Dot products are summed per thread, over the warp and over the warps, always in the same order.
 // K = top_k known at compile time, 0 = any.
 template <int K>
@@ -59,11 +88,14 @@ __global__ void __launch_bounds__((kCombineBwdWarps + 1) * 32, 2) k_combine_back
     extern __shared__ __align__(128) unsigned char ring[];
     __shared__ __align__(8) uint64_t full[kCombineBwdMaxSlots], empty[kCombineBwdMaxSlots];
     __shared__ CombineBwdTable table[kCombineBwdMaxSlots + 1];
+    __shared__ __align__(16) unsigned char clc[16];
+    __shared__ __align__(8) uint64_t clc_bar;
     __shared__ float s_dot[2][kCombineBwdWarps][kMaxTopKDevice];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int k = K > 0 ? K : p.k, S = p.slots;
     if (tid == 0) {
         for (int s = 0; s < S; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], kCombineBwdWarps); }
+        mbar_init(&clc_bar, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     __syncthreads();
@@ -77,11 +109,11 @@ __global__ void __launch_bounds__((kCombineBwdWarps + 1) * 32, 2) k_combine_back
     if (warp == kCombineBwdWarps) {
         unsigned parity = 1;
         int issued = 0, entry = 0;
-        // lanes j < k hold the assignments of the token to come
-        int row = -1, row_n = -1; float coef = 0.0f, scale = 0.0f, coef_n = 0.0f, scale_n = 0.0f;
+        unsigned clc_parity = 0;
+        int row; float coef, scale;                             // lane j < k: assignment j of the token
         auto fetch = [&](int t, int &r, float &c, float &sc) {
             r = -1; c = 0.0f; sc = 0.0f;
-            if (lane < k && t < p.T) {
+            if (lane < k) {
                 const size_t i = (size_t)t * k + lane;
                 const int slot = __ldg(p.topk_slot + i), d = __ldg(p.dst_row + i);
                 if ((unsigned)slot < (unsigned)p.P && d >= 0 && d < (long long)p.T * k) {
@@ -91,13 +123,25 @@ __global__ void __launch_bounds__((kCombineBwdWarps + 1) * 32, 2) k_combine_back
                 }
             }
         };
-        fetch(blockIdx.x, row, coef, scale);
-        for (int t = blockIdx.x; t < p.T && ok; t += gridDim.x) {
-            fetch(t + gridDim.x, row_n, coef_n, scale_n);
+        int t = blockIdx.x;
+        if (lane == 0) clc_request(clc, &clc_bar);
+        while (true) {
             // Table entries are reused after kCombineBwdMaxSlots + 1 tokens; a token takes at least two slots, so
             // the ring never holds that many.
-            if (lane < k) { table[entry].row[lane] = row; table[entry].coef[lane] = coef; table[entry].scale[lane] = scale; }
+            if (t >= 0) {
+                fetch(t, row, coef, scale);
+                if (lane < k) { table[entry].row[lane] = row; table[entry].coef[lane] = coef; table[entry].scale[lane] = scale; }
+            }
+            if (lane == 0) table[entry].token = t;
             __syncwarp();
+            if (t < 0) {                                        // tell the others that there is nothing more
+                unsigned spins = 0;
+                while (!mbar_try_wait(&empty[s], parity))
+                    if (++spins > p.spin_limit) { ok = false; break; }
+                if (lane == 0 && ok) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_addr(&full[s])) : "memory");
+                ok = __all_sync(0xffffffffu, ok);
+                break;
+            }
             for (int c = 0; c < chunks && ok; ++c) {
                 const int u0 = c * p.slot_units;
                 const unsigned bytes = (unsigned)min(p.slot_units, p.hv - u0) * 16u;
@@ -118,12 +162,23 @@ __global__ void __launch_bounds__((kCombineBwdWarps + 1) * 32, 2) k_combine_back
                     if (++s == S) { s = 0; parity ^= 1u; }
                 }
             }
-            row = row_n; coef = coef_n; scale = scale_n;
+            if (!ok) break;
             if (++entry == kCombineBwdMaxSlots + 1) entry = 0;
+            unsigned spins = 0;
+            while (!mbar_try_wait(&clc_bar, clc_parity))
+                if (++spins > p.spin_limit) { ok = false; break; }
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+            clc_parity ^= 1u;
+            t = clc_answer(clc);
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();                                       // every lane has read the answer
+            if (t >= 0 && lane == 0) clc_request(clc, &clc_bar);
         }
         if (!ok) {
             if (lane == 0) report_status(p.ctl, kDevTimeout);
-            // copies in flight still land in this CTA's shared memory: a bounded wait for each
+            // the answer and the copies in flight still land in this CTA's shared memory: a bounded wait for each
+            for (unsigned spins = 0; !mbar_try_wait(&clc_bar, clc_parity) && ++spins < p.spin_limit;) {}
             for (int m = max(0, issued - S); m < issued; ++m) {
                 unsigned spins = 0;
                 while (!mbar_try_wait(&full[m % S], (unsigned)(m / S) & 1u) && ++spins < p.spin_limit) {}
@@ -134,10 +189,13 @@ __global__ void __launch_bounds__((kCombineBwdWarps + 1) * 32, 2) k_combine_back
 
     unsigned parity = 0;
     int entry = 0, side = 0;
-    auto take = [&](uint4 (&v)[U], int units) {                 // this thread's units of the next slot, which is then handed back
+    auto wait_full = [&]() {
         unsigned spins = 0;
         while (ok && !mbar_try_wait(&full[s], parity))
             if (++spins > p.spin_limit) ok = false;
+    };
+    auto take = [&](uint4 (&v)[U], int units) {                 // this thread's units of the next slot, which is then handed back
+        wait_full();
         const uint4 *src = reinterpret_cast<const uint4 *>(ring + s * slot_bytes);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -148,7 +206,17 @@ __global__ void __launch_bounds__((kCombineBwdWarps + 1) * 32, 2) k_combine_back
         if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_addr(&empty[s])) : "memory");
         if (++s == S) { s = 0; parity ^= 1u; }
     };
-    for (int t = blockIdx.x; t < p.T; t += gridDim.x) {
+    // one barrier a token (the other half of s_dot is used in between), which also makes the warps leave together
+    auto verdict = [&]() {
+        uint32_t good;
+        asm volatile("{\n\t.reg .pred a, b;\n\tsetp.ne.u32 a, %1, 0;\n\tbarrier.cta.red.and.pred b, 1, %2, a;\n\tselp.u32 %0, 1, 0, b;\n\t}"
+                     : "=r"(good) : "r"((uint32_t)ok), "n"(kCombineBwdWarps * 32) : "memory");
+        ok = good != 0;
+    };
+    while (true) {
+        wait_full();                                            // the token's first slot: its table entry is there as well
+        const int t = ok ? table[entry].token : 0;
+        if (t < 0) { verdict(); break; }                        // (a warp that gave up is at its barrier too)
         float dot[KK];
 #pragma unroll
         for (int j = 0; j < KK; ++j) dot[j] = 0.0f;
@@ -189,12 +257,7 @@ __global__ void __launch_bounds__((kCombineBwdWarps + 1) * 32, 2) k_combine_back
             for (int off = 16; off > 0; off >>= 1) dot[j] += __shfl_xor_sync(0xffffffffu, dot[j], off);
             if (lane == 0) s_dot[side][warp][j] = dot[j];
         }
-        // one barrier a token: the other half of s_dot is used in between.  It also carries the verdict, so that
-        // the warps leave together.
-        uint32_t good;
-        asm volatile("{\n\t.reg .pred a, b;\n\tsetp.ne.u32 a, %1, 0;\n\tbarrier.cta.red.and.pred b, 1, %2, a;\n\tselp.u32 %0, 1, 0, b;\n\t}"
-                     : "=r"(good) : "r"((uint32_t)ok), "n"(kCombineBwdWarps * 32) : "memory");
-        ok = good != 0;
+        verdict();
         if (!ok) break;
         if (tid < k) {
             float sum = 0.0f;

@@ -1193,8 +1193,7 @@ moe_status moe_combine_backward(moe_ctx *ctx, const void *expert_buf, const void
     p.slot_units = std::min(p.hv, kCombineBwdSlotUnits);
     const size_t half = (227 * 1024 - 2 * 6 * 1024) / 2;
     p.slots = std::min<int>(kCombineBwdMaxSlots, (int)((half - 128) / ((size_t)p.slot_units * 16)));
-    const int grid = std::min(T, ctx->sm_count * 2);
-    const dim3 g(grid), b((kCombineBwdWarps + 1) * 32);
+    const dim3 g(T), b((kCombineBwdWarps + 1) * 32);
     const size_t sm = combine_backward_smem(p.slots, p.slot_units);
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     const cudaError_t e = d.k == 8   ? launch_kernel(k_combine_backward<8>, g, b, sm, st, ctx->pdl, p)
