@@ -16,7 +16,7 @@ struct CombineParams {
     uint4 *y;                    // [T, H/8]
     int T, k, hv;
     const int32_t *dst_row;      // [T*k]
-    const float *topk_weights;   // [T,k]; NULL = every coefficient is 1 (gradient of the scatter)
+    const float *topk_weights;   // [T,k]
     const int32_t *topk_slot;    // [T,k]
     const float *slot_scale;     // [P]
     // Expert parallelism over several GPUs: the rows of slot p live in the receive buffer of
@@ -77,7 +77,7 @@ __global__ void __launch_bounds__(kCombineThreads) k_combine_vec(CombineParams p
             const int r = __ldg(p.dst_row + i);
             if ((unsigned)slot < (unsigned)p.P && r >= 0 && r < p.row_limit) {
                 my_row = r;
-                my_coef = p.topk_weights ? __fmul_rn(__ldg(p.topk_weights + i), __ldg(p.slot_scale + slot)) : 1.0f;
+                my_coef = __fmul_rn(__ldg(p.topk_weights + i), __ldg(p.slot_scale + slot));
             } else {
                 my_row = -1;                               // not placed: contributes nothing
             }
@@ -146,7 +146,7 @@ __device__ __forceinline__ void combine_fetch_index(const CombineParams &p, int 
         if ((unsigned)slot < (unsigned)p.P && r >= 0 && r < p.row_limit) {
             const uint4 *base = p.peer_bufs ? p.peer_bufs[slot / p.slots_per_gpu] : p.buf;
             row = base + (size_t)r * p.hv;
-            coef = p.topk_weights ? __fmul_rn(__ldg(p.topk_weights + i), __ldg(p.slot_scale + slot)) : 1.0f;
+            coef = __fmul_rn(__ldg(p.topk_weights + i), __ldg(p.slot_scale + slot));
         }
     }
 }

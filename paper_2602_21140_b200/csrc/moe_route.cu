@@ -409,17 +409,6 @@ moe_status enqueue_combine_bulk(moe_ctx *ctx, const CombineParams &cp, cudaStrea
     return cudaGetLastError() == cudaSuccess ? MOE_OK : MOE_ERR_CUDA;
 }
 
-// The combine kernel of the context's choice.
-moe_status enqueue_combine(moe_ctx *ctx, const CombineParams &cp, cudaStream_t st)
-{
-    if (ctx->combine_impl == 1) return enqueue_combine_bulk(ctx, cp, st);
-    const int chunks = (cp.hv + kCombineChunk - 1) / kCombineChunk;
-    const long long items = (long long)cp.T * chunks;
-    const long long want = (items + kCombineThreads / 32 - 1) / (kCombineThreads / 32);
-    const int grid = (int)std::min<long long>(want, (long long)ctx->sm_count * ctx->combine_blocks_per_sm);
-    return launch_combine(cp, grid, st) == cudaSuccess ? MOE_OK : MOE_ERR_CUDA;
-}
-
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 // Rebuild the live-replica lists from the bitmaps and the replica table, on the stream,
@@ -494,9 +483,12 @@ bool set_kernel_attributes_once()
           && cudaFuncSetAttribute(k_combine_bulk<1, 0>, at, sm) == cudaSuccess
           && cudaFuncSetAttribute(k_combine_bulk<2, 0>, at, sm) == cudaSuccess
           && cudaFuncSetAttribute(k_combine_bulk<4, 0>, at, sm) == cudaSuccess
-          && cudaFuncSetAttribute(k_combine_backward<8>, at, 112 * 1024) == cudaSuccess
-          && cudaFuncSetAttribute(k_combine_backward<2>, at, 112 * 1024) == cudaSuccess
-          && cudaFuncSetAttribute(k_combine_backward<0>, at, 112 * 1024) == cudaSuccess;
+          && cudaFuncSetAttribute(k_backward<true, 8>, at, 112 * 1024) == cudaSuccess
+          && cudaFuncSetAttribute(k_backward<false, 8>, at, 112 * 1024) == cudaSuccess
+          && cudaFuncSetAttribute(k_backward<true, 2>, at, 112 * 1024) == cudaSuccess
+          && cudaFuncSetAttribute(k_backward<false, 2>, at, 112 * 1024) == cudaSuccess
+          && cudaFuncSetAttribute(k_backward<true, 0>, at, 112 * 1024) == cudaSuccess
+          && cudaFuncSetAttribute(k_backward<false, 0>, at, 112 * 1024) == cudaSuccess;
     });
     return ok;
 }
@@ -581,6 +573,75 @@ void free_ctx(moe_ctx *ctx)
         if (ctx->stage_done[s]) cudaEventDestroy(ctx->stage_done[s]);
     }
     delete ctx;
+}
+
+// ---- 4-bit rows and the gradients of the routed step
+
+// The context's device for the duration of a call, whatever device the caller has current.
+struct DeviceScope {
+    int before = -1;
+    bool ok = true;
+    explicit DeviceScope(int device)
+    {
+        ok = cudaGetDevice(&before) == cudaSuccess;
+        if (ok && before != device) ok = cudaSetDevice(device) == cudaSuccess;
+        else before = -1;
+    }
+    ~DeviceScope() { if (before >= 0) cudaSetDevice(before); }
+};
+
+// Rows read and written by an expert product: common checks.
+moe_status check_product(const moe_ctx *ctx, const uint8_t *a_codes, const uint8_t *a_scales, int64_t rows,
+                         const int32_t *slot_counts, const int32_t *slot_offsets, const uint8_t *w_codes,
+                         const uint8_t *w_scales, int32_t n_out, int32_t n_in)
+{
+    if (!ctx || rows < 0 || n_out < 1 || n_in < kMxBlock || n_in % kMxBlock != 0) return MOE_ERR_INVALID_ARG;
+    // 32-bit tile numbers and tensor-map strides (2^40 bytes)
+    const long long feats = ((long long)n_out + 127) / 128;
+    if (rows > (1ll << 30) || feats * (ctx->d.P + rows / 32) > (1ll << 30)) return MOE_ERR_CAPACITY;
+    if ((long long)n_out * (n_in / 2) >= (1ll << 40)) return MOE_ERR_CAPACITY;
+    if (rows == 0) return MOE_OK;
+    if (!a_codes || !a_scales || !slot_counts || !slot_offsets || !w_codes || !w_scales) return MOE_ERR_INVALID_ARG;
+    if (!aligned16(a_codes) || !aligned16(a_scales) || !aligned16(w_codes) || !aligned16(w_scales)) return MOE_ERR_INVALID_ARG;
+    return MOE_OK;
+}
+
+MxProductArgs product_args(const moe_ctx *ctx, const uint8_t *a_codes, const uint8_t *a_scales, int64_t rows,
+                           const int32_t *slot_counts, const int32_t *slot_offsets, const uint8_t *w_codes,
+                           const uint8_t *w_scales, int32_t n_out, int32_t n_in)
+{
+    MxProductArgs a = {};
+    a.a_codes = a_codes; a.a_scales = a_scales; a.rows = rows;
+    a.slot_counts = slot_counts; a.slot_offsets = slot_offsets; a.P = ctx->d.P;
+    a.w_codes = w_codes; a.w_scales = w_scales; a.N = n_out; a.K = n_in;
+    a.ctl = ctx->d_ctl; a.spin_limit = ctx->spin_limit; a.sm_count = ctx->sm_count; a.pdl = ctx->pdl;
+    return a;
+}
+
+// What both gradients take from the latest dispatch.
+BackwardParams backward_params(const moe_ctx *ctx, int32_t T)
+{
+    const Derived &d = ctx->d;
+    BackwardParams p = {};
+    p.T = T; p.k = d.k; p.hv = d.H / 8; p.P = d.P;
+    p.dst_row = ctx->last_dst_row; p.topk_weights = ctx->last_weights; p.topk_slot = ctx->last_slot;
+    p.zero_row = ctx->d_zero_row; p.ctl = ctx->d_ctl; p.spin_limit = ctx->spin_limit;
+    // two CTAs per SM, each with a ring of half the shared memory (less what the kernel itself declares)
+    p.slot_units = std::min(p.hv, kBwdSlotUnits);
+    const size_t half = (227 * 1024 - 2 * 6 * 1024) / 2;
+    p.slots = std::min<int>(kBwdMaxSlots, (int)((half - 128) / ((size_t)p.slot_units * 16)));
+    return p;
+}
+
+template <bool COMBINE>
+moe_status enqueue_backward(const moe_ctx *ctx, const BackwardParams &p, cudaStream_t st)
+{
+    const dim3 g(p.T), b(backward_threads(COMBINE));           // a CTA per token; resident ones take over the rest
+    const size_t sm = backward_smem(p.slots, p.slot_units);
+    const cudaError_t e = p.k == 8   ? launch_kernel(k_backward<COMBINE, 8>, g, b, sm, st, ctx->pdl, p)
+                          : p.k == 2 ? launch_kernel(k_backward<COMBINE, 2>, g, b, sm, st, ctx->pdl, p)
+                                     : launch_kernel(k_backward<COMBINE, 0>, g, b, sm, st, ctx->pdl, p);
+    return e == cudaSuccess ? MOE_OK : MOE_ERR_CUDA;
 }
 
 }  // namespace
@@ -905,7 +966,13 @@ moe_status moe_combine(moe_ctx *ctx, const void *expert_buf, int32_t T, void *y,
     cp.slot_scale = ctx->d_slot_scale;
     cp.peer_bufs = nullptr; cp.slots_per_gpu = 0;
     cp.P = d.P; cp.row_limit = (long long)T * d.k; cp.zero_row = ctx->d_zero_row; cp.spin_limit = ctx->spin_limit;
-    return enqueue_combine(ctx, cp, st);
+    if (ctx->combine_impl == 1) return enqueue_combine_bulk(ctx, cp, st);
+    const int chunks = (cp.hv + kCombineChunk - 1) / kCombineChunk;
+    const long long items = (long long)T * chunks;
+    const long long want = (items + kCombineThreads / 32 - 1) / (kCombineThreads / 32);
+    const int grid = (int)std::min<long long>(want, (long long)ctx->sm_count * ctx->combine_blocks_per_sm);
+    if (launch_combine(cp, grid, st) != cudaSuccess) return MOE_ERR_CUDA;
+    return MOE_OK;
 }
 
 // ---------------------------------------------------------------------------
@@ -1052,51 +1119,6 @@ moe_status moe_ep_combine(moe_ctx *ctx, int32_t T, void *y, void *cuda_stream)
 // 4-bit rows and the gradients of the routed step
 // ---------------------------------------------------------------------------
 
-namespace {
-
-// The context's device for the duration of a call, whatever device the caller has current.
-struct DeviceScope {
-    int before = -1;
-    bool ok = true;
-    explicit DeviceScope(int device)
-    {
-        ok = cudaGetDevice(&before) == cudaSuccess;
-        if (ok && before != device) ok = cudaSetDevice(device) == cudaSuccess;
-        else before = -1;
-    }
-    ~DeviceScope() { if (before >= 0) cudaSetDevice(before); }
-};
-
-// Rows read and written by an expert product: common checks.
-moe_status check_product(const moe_ctx *ctx, const uint8_t *a_codes, const uint8_t *a_scales, int64_t rows,
-                         const int32_t *slot_counts, const int32_t *slot_offsets, const uint8_t *w_codes,
-                         const uint8_t *w_scales, int32_t n_out, int32_t n_in)
-{
-    if (!ctx || rows < 0 || n_out < 1 || n_in < kMxBlock || n_in % kMxBlock != 0) return MOE_ERR_INVALID_ARG;
-    // 32-bit tile numbers and tensor-map strides (2^40 bytes)
-    const long long feats = ((long long)n_out + 127) / 128;
-    if (rows > (1ll << 30) || feats * (ctx->d.P + rows / 32) > (1ll << 30)) return MOE_ERR_CAPACITY;
-    if ((long long)n_out * (n_in / 2) >= (1ll << 40)) return MOE_ERR_CAPACITY;
-    if (rows == 0) return MOE_OK;
-    if (!a_codes || !a_scales || !slot_counts || !slot_offsets || !w_codes || !w_scales) return MOE_ERR_INVALID_ARG;
-    if (!aligned16(a_codes) || !aligned16(a_scales) || !aligned16(w_codes) || !aligned16(w_scales)) return MOE_ERR_INVALID_ARG;
-    return MOE_OK;
-}
-
-MxProductArgs product_args(const moe_ctx *ctx, const uint8_t *a_codes, const uint8_t *a_scales, int64_t rows,
-                           const int32_t *slot_counts, const int32_t *slot_offsets, const uint8_t *w_codes,
-                           const uint8_t *w_scales, int32_t n_out, int32_t n_in)
-{
-    MxProductArgs a = {};
-    a.a_codes = a_codes; a.a_scales = a_scales; a.rows = rows;
-    a.slot_counts = slot_counts; a.slot_offsets = slot_offsets; a.P = ctx->d.P;
-    a.w_codes = w_codes; a.w_scales = w_scales; a.N = n_out; a.K = n_in;
-    a.ctl = ctx->d_ctl; a.spin_limit = ctx->spin_limit; a.sm_count = ctx->sm_count; a.pdl = ctx->pdl;
-    return a;
-}
-
-}  // namespace
-
 moe_status moe_mx_dispatch(moe_ctx *ctx, const float *logits, const void *x, int32_t T, const moe_dispatch_out *out,
                            uint8_t *send_codes, uint8_t *send_scales, void *cuda_stream)
 {
@@ -1181,25 +1203,11 @@ moe_status moe_combine_backward(moe_ctx *ctx, const void *expert_buf, const void
     if (expert_buf == d_expert_buf) return MOE_ERR_INVALID_ARG;   // rows are read ahead of the ones written
     DeviceScope scope(ctx->device);
     if (!scope.ok) return MOE_ERR_CUDA;
-    const Derived &d = ctx->d;
-    CombineBackwardParams p;
-    p.buf = static_cast<const uint4 *>(expert_buf); p.dy = static_cast<const uint4 *>(dy);
-    p.d_buf = static_cast<uint4 *>(d_expert_buf); p.d_weights = d_weights;
-    p.T = T; p.k = d.k; p.hv = d.H / 8; p.P = d.P;
-    p.dst_row = ctx->last_dst_row; p.topk_weights = ctx->last_weights; p.topk_slot = ctx->last_slot;
+    BackwardParams p = backward_params(ctx, T);
+    p.rows = static_cast<const uint4 *>(expert_buf); p.dy = static_cast<const uint4 *>(dy);
+    p.out = static_cast<uint4 *>(d_expert_buf); p.d_weights = d_weights;
     p.slot_scale = ctx->d_slot_scale;
-    p.zero_row = ctx->d_zero_row; p.ctl = ctx->d_ctl; p.spin_limit = ctx->spin_limit;
-    // two CTAs per SM, each with a ring of half the shared memory
-    p.slot_units = std::min(p.hv, kCombineBwdSlotUnits);
-    const size_t half = (227 * 1024 - 2 * 6 * 1024) / 2;
-    p.slots = std::min<int>(kCombineBwdMaxSlots, (int)((half - 128) / ((size_t)p.slot_units * 16)));
-    const dim3 g(T), b((kCombineBwdWarps + 1) * 32);
-    const size_t sm = combine_backward_smem(p.slots, p.slot_units);
-    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    const cudaError_t e = d.k == 8   ? launch_kernel(k_combine_backward<8>, g, b, sm, st, ctx->pdl, p)
-                          : d.k == 2 ? launch_kernel(k_combine_backward<2>, g, b, sm, st, ctx->pdl, p)
-                                     : launch_kernel(k_combine_backward<0>, g, b, sm, st, ctx->pdl, p);
-    return e == cudaSuccess ? MOE_OK : MOE_ERR_CUDA;
+    return enqueue_backward<true>(ctx, p, static_cast<cudaStream_t>(cuda_stream));
 }
 
 moe_status moe_dispatch_backward(moe_ctx *ctx, const float *logits, const void *d_send_buf, const float *d_weights, int32_t T,
@@ -1215,26 +1223,13 @@ moe_status moe_dispatch_backward(moe_ctx *ctx, const float *logits, const void *
     if (d_logits && (!aligned16(d_logits) || (ctx->cfg.score_func == MOE_SCORE_SIGMOID && !logits))) return MOE_ERR_INVALID_ARG;
     DeviceScope scope(ctx->device);
     if (!scope.ok) return MOE_ERR_CUDA;
-    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    const Derived &d = ctx->d;
-    if (d_logits) {
-        RouteBackwardParams rp;
-        rp.logits = logits; rp.topk_ids = ctx->last_ids; rp.topk_weights = ctx->last_weights; rp.d_weights = d_weights;
-        rp.d_logits = d_logits; rp.T = T; rp.E = d.E; rp.k = d.k;
-        rp.sigmoid = ctx->cfg.score_func == MOE_SCORE_SIGMOID;
-        rp.inv_scale = 1.0f / ctx->cfg.route_scale;
-        const int warps = kRouteBwdThreads / 32;
-        const int grid = std::min((T + warps - 1) / warps, ctx->sm_count * 8);
-        if (launch_kernel(k_route_backward, dim3(grid), dim3(kRouteBwdThreads), 0, st, ctx->pdl, rp) != cudaSuccess) return MOE_ERR_CUDA;
-    }
-    CombineParams cp;
-    cp.buf = static_cast<const uint4 *>(d_send_buf); cp.y = static_cast<uint4 *>(dx);
-    cp.T = T; cp.k = d.k; cp.hv = d.H / 8;
-    cp.dst_row = ctx->last_dst_row; cp.topk_weights = nullptr; cp.topk_slot = ctx->last_slot;
-    cp.slot_scale = ctx->d_slot_scale;
-    cp.peer_bufs = nullptr; cp.slots_per_gpu = 0;
-    cp.P = d.P; cp.row_limit = (long long)T * d.k; cp.zero_row = ctx->d_zero_row; cp.spin_limit = ctx->spin_limit;
-    return enqueue_combine(ctx, cp, st);
+    BackwardParams p = backward_params(ctx, T);
+    p.rows = static_cast<const uint4 *>(d_send_buf); p.out = static_cast<uint4 *>(dx);
+    p.d_weights = const_cast<float *>(d_weights); p.d_logits = d_logits;
+    p.topk_ids = ctx->last_ids; p.logits = logits; p.E = ctx->d.E;
+    p.sigmoid = ctx->cfg.score_func == MOE_SCORE_SIGMOID;
+    p.inv_scale = 1.0f / ctx->cfg.route_scale;
+    return enqueue_backward<false>(ctx, p, static_cast<cudaStream_t>(cuda_stream));
 }
 
 moe_status moe_step_host_async(moe_ctx *ctx, const float *logits_host, const void *x_host, int32_t T,
