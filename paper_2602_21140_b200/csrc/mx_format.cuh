@@ -77,19 +77,65 @@ __device__ __forceinline__ void mx_unpack8(uint32_t c, float (&v)[8])
     }
 }
 
-__device__ __forceinline__ void bf16x8_to_f32(const uint4 &u, float (&v)[8])
+__device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b)
 {
-    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        v[2 * q] = __uint_as_float(w[q] << 16);
-        v[2 * q + 1] = __uint_as_float(w[q] & 0xffff0000u);
-    }
+    uint32_t r;
+    asm("max.u16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+
+// Largest magnitude of the block as the bit pattern of its 16-bit type: eight elements of this lane, two to a
+// word, over the four lanes of an aligned quad.  Magnitudes of 16-bit floats compare like their bit patterns too,
+// so this is two instructions per word.
+__device__ __forceinline__ uint32_t mx_amax16(const uint4 &u)
+{
+    uint32_t m = max_u16x2(max_u16x2(u.x & 0x7fff7fffu, u.y & 0x7fff7fffu), max_u16x2(u.z & 0x7fff7fffu, u.w & 0x7fff7fffu));
+    m = max_u16x2(m, __shfl_xor_sync(0xffffffffu, m, 1));
+    m = max_u16x2(m, __shfl_xor_sync(0xffffffffu, m, 2));
+    return max(m & 0xffffu, m >> 16);
 }
 
 // Quantise eight consecutive elements held by this lane; the four lanes of an aligned quad hold one
 // block.  Every lane of the warp must call it.
-__device__ __forceinline__ uint32_t mx_quantize8(float (&v)[8], uint32_t &scale)
+
+// bf16: a bf16 number times a power of two is a bf16 number (down to its subnormals, which are far below half the
+// smallest code), so the scaling is done two at a time before they are taken apart.
+__device__ __forceinline__ uint32_t mx_quantize8_bf16(const uint4 &u, uint32_t &scale)
+{
+    scale = mx_scale_byte(mx_amax16(u) << 16);
+    const uint32_t inv_bits = __float_as_uint(mx_inverse_scale(scale)) >> 16;
+    const uint32_t inv2_bits = inv_bits | (inv_bits << 16);
+    const __nv_bfloat162 inv2 = *reinterpret_cast<const __nv_bfloat162 *>(&inv2_bits);
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+    float v[8];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const __nv_bfloat162 h = __hmul2(*reinterpret_cast<const __nv_bfloat162 *>(&w[q]), inv2);
+        const uint32_t b = *reinterpret_cast<const uint32_t *>(&h);
+        v[2 * q] = __uint_as_float(b << 16);
+        v[2 * q + 1] = __uint_as_float(b & 0xffff0000u);
+    }
+    const uint32_t c = mx_pack8(v);
+    return scale == 255u ? 0u : c;
+}
+
+// fp16: scaled in fp32, whose range the scale may need.
+__device__ __forceinline__ uint32_t mx_quantize8_f16(const uint4 &u, uint32_t &scale)
+{
+    scale = mx_scale_byte(__float_as_uint(__half2float(__ushort_as_half((unsigned short)mx_amax16(u)))) & 0x7fffffffu);
+    const float inv = mx_inverse_scale(scale);
+    const __half2 *h = reinterpret_cast<const __half2 *>(&u);
+    float v[8];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const float2 f = __half22float2(h[q]);
+        v[2 * q] = f.x * inv; v[2 * q + 1] = f.y * inv;
+    }
+    const uint32_t c = mx_pack8(v);
+    return scale == 255u ? 0u : c;
+}
+
+__device__ __forceinline__ uint32_t mx_quantize8_f32(float (&v)[8], uint32_t &scale)
 {
     uint32_t a = 0;
 #pragma unroll

@@ -56,11 +56,7 @@ __global__ void __launch_bounds__(kScatterThreads) k_mx_scatter(MxScatterParams 
         for (int c = c_first; c < c_last; ++c) {
             uint32_t w[4], s[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                float v[8];
-                bf16x8_to_f32(in[i], v);
-                w[i] = mx_quantize8(v, s[i]);
-            }
+            for (int i = 0; i < 4; ++i) w[i] = mx_quantize8_bf16(in[i], s[i]);
             if (c + 1 < c_last) {                            // the next piece is on its way while this one is stored
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {

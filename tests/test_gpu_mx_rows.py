@@ -61,6 +61,18 @@ def test_special_values():
     assert torch.isnan(y[:4]).all() and (y[4:6] == 0).all()
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_every_16_bit_pattern(dtype):
+    """All 65536 bit patterns, NaN, infinities and subnormals among them: one to a block of ordinary numbers, and
+    as blocks of neighbours."""
+    bits = torch.arange(65536, dtype=torch.int32).to(torch.int16)
+    alone = torch.from_numpy(M.random_rows(65536, 32, 1)).to(dtype)
+    alone[torch.arange(65536), torch.arange(65536) % 32] = bits.view(dtype)
+    for x in (alone, bits.view(dtype).view(2048, 32), bits.view(dtype).view(32, 2048).t().contiguous()):
+        x = x.cuda()
+        _check(x, B.mx_quantize(x))
+
+
 def test_leading_dimensions_and_strided_rows():
     x = torch.randn(3, 5, 64, device="cuda", dtype=torch.float16)
     m = B.mx_quantize(x)
