@@ -150,4 +150,21 @@ __device__ __forceinline__ uint32_t mx_quantize8_f32(float (&v)[8], uint32_t &sc
     return scale == 255u ? 0u : c;
 }
 
+// 4 x 4 transpose in a quad of lanes.  Before: w[i] and s[i] belong to this lane's quarter of block 8 i + (lane / 4)
+// of the warp's 32 blocks.  After: w holds the whole 16 bytes of block mx_block_of_lane(lane), the result is its scale.
+__device__ __forceinline__ int mx_block_of_lane(int lane) { return 8 * (lane & 3) + (lane >> 2); }
+
+__device__ __forceinline__ uint32_t mx_transpose(uint32_t (&w)[4], const uint32_t (&s)[4], int lane)
+{
+    const unsigned full = 0xffffffffu;
+    uint32_t x0 = (lane & 1) ? w[0] : w[1], x1 = (lane & 1) ? w[2] : w[3];
+    x0 = __shfl_xor_sync(full, x0, 1); x1 = __shfl_xor_sync(full, x1, 1);
+    if (lane & 1) { w[0] = x0; w[2] = x1; } else { w[1] = x0; w[3] = x1; }
+    x0 = (lane & 2) ? w[0] : w[2]; x1 = (lane & 2) ? w[1] : w[3];
+    x0 = __shfl_xor_sync(full, x0, 2); x1 = __shfl_xor_sync(full, x1, 2);
+    if (lane & 2) { w[0] = x0; w[1] = x1; } else { w[2] = x0; w[3] = x1; }
+    const int sub = lane & 3;
+    return sub == 0 ? s[0] : sub == 1 ? s[1] : sub == 2 ? s[2] : s[3];
+}
+
 }  // namespace moe

@@ -3,7 +3,7 @@
 // Both are one pass over the data and bound by HBM: n elements of `size` bytes are read (written)
 // once and n * 17/32 bytes written (read).  A thread owns eight consecutive elements (one 16-byte
 // access of a 16-bit type) and four neighbouring lanes own a block, so the block's largest
-// magnitude takes two shuffles and a warp writes 128 contiguous bytes of codes.  Units of eight
+// magnitude takes two shuffles.  Units of eight
 // elements are numbered through all rows, so short rows fill the warps as well as long ones.
 #include "../../include/moe_route.h"
 
@@ -78,41 +78,61 @@ __device__ __forceinline__ UnitBase unit_base(const RowParams &p, long long firs
     return b;
 }
 
-template <int DT, int UN>
+__device__ __forceinline__ void store_scale(const RowParams &p, long long row, unsigned block, uint32_t s)
+{
+    uint8_t *dst = p.scales + row * p.pitch;
+    dst[block] = (uint8_t)s;
+    if ((int)block * 4 + 4 == p.upr)                          // the row's last block also clears the padding
+        for (int q = p.upr / 4; q < p.pitch; ++q) dst[q] = 0;
+}
+
+// Large calls: a warp takes 128 units (32 blocks), four per lane, and trades code words within its quads of lanes
+// so that a lane stores the 16 bytes and the scale of one block.
+template <int DT>
 __global__ void __launch_bounds__(kRowThreads) k_mx_quantize(RowParams p)
 {
-    const long long first = (long long)blockIdx.x * (kRowThreads * UN);
+    const long long first = (long long)blockIdx.x * (kRowThreads * 4);
     const UnitBase b = unit_base(p, first);
-    uint4 in[UN][Elem<DT>::kVec];
-    long long row[UN]; unsigned col[UN];
+    const int lane = threadIdx.x & 31, w0 = (threadIdx.x >> 5) * 128;
+    uint4 in[4][Elem<DT>::kVec];
 #pragma unroll
-    for (int i = 0; i < UN; ++i) {
-        const unsigned off = b.col + i * kRowThreads + threadIdx.x;
+    for (int i = 0; i < 4; ++i) {
+        const unsigned u = w0 + 32 * i + lane, off = b.col + u;
         const unsigned dr = __umulhi(off, p.magic) >> p.shift;
-        row[i] = b.row + dr; col[i] = off - dr * p.upr;
-        if (first + i * kRowThreads + threadIdx.x < p.units) {
-            const uint4 *src = reinterpret_cast<const uint4 *>(p.x + row[i] * p.stride) + (size_t)col[i] * Elem<DT>::kVec;
+        const uint4 *src = reinterpret_cast<const uint4 *>(p.x + (b.row + dr) * p.stride) + (size_t)(off - dr * p.upr) * Elem<DT>::kVec;
 #pragma unroll
-            for (int q = 0; q < Elem<DT>::kVec; ++q) in[i][q] = __ldg(src + q);
-        } else {
-#pragma unroll
-            for (int q = 0; q < Elem<DT>::kVec; ++q) in[i][q] = make_uint4(0u, 0u, 0u, 0u);
-        }
+        for (int q = 0; q < Elem<DT>::kVec; ++q) in[i][q] = first + u < p.units ? __ldg(src + q) : make_uint4(0u, 0u, 0u, 0u);
     }
+    uint32_t w[4], s[4];
 #pragma unroll
-    for (int i = 0; i < UN; ++i) {
-        uint32_t s;
-        const uint32_t c = quantize8<DT>(in[i], s);
-        const long long u = first + i * kRowThreads + threadIdx.x;
-        if (u < p.units) {
-            reinterpret_cast<uint32_t *>(p.codes)[u] = c;
-            if ((col[i] & 3u) == 0u) {
-                uint8_t *dst = p.scales + row[i] * p.pitch;
-                dst[col[i] >> 2] = (uint8_t)s;
-                if ((int)col[i] + 4 == p.upr)                 // the row's last block also clears the padding
-                    for (int q = p.upr / 4; q < p.pitch; ++q) dst[q] = 0;
-            }
-        }
+    for (int i = 0; i < 4; ++i) w[i] = quantize8<DT>(in[i], s[i]);
+    const uint32_t scale = mx_transpose(w, s, lane);
+    const unsigned u = w0 + 4 * mx_block_of_lane(lane), off = b.col + u;     // first unit of this lane's block
+    if (first + u < p.units) {
+        reinterpret_cast<uint4 *>(p.codes)[(first + u) >> 2] = make_uint4(w[0], w[1], w[2], w[3]);
+        const unsigned dr = __umulhi(off, p.magic) >> p.shift;
+        store_scale(p, b.row + dr, (off - dr * p.upr) >> 2, scale);
+    }
+}
+
+// Small calls: a unit per thread, so that there are as many CTAs as possible.
+template <int DT>
+__global__ void __launch_bounds__(kRowThreads) k_mx_quantize_small(RowParams p)
+{
+    const long long first = (long long)blockIdx.x * kRowThreads, u = first + threadIdx.x;
+    const UnitBase b = unit_base(p, first);
+    const unsigned off = b.col + threadIdx.x;
+    const unsigned dr = __umulhi(off, p.magic) >> p.shift;
+    const unsigned col = off - dr * p.upr;
+    const uint4 *src = reinterpret_cast<const uint4 *>(p.x + (b.row + dr) * p.stride) + (size_t)col * Elem<DT>::kVec;
+    uint4 in[Elem<DT>::kVec];
+#pragma unroll
+    for (int q = 0; q < Elem<DT>::kVec; ++q) in[q] = u < p.units ? __ldg(src + q) : make_uint4(0u, 0u, 0u, 0u);
+    uint32_t s;
+    const uint32_t c = quantize8<DT>(in, s);
+    if (u < p.units) {
+        reinterpret_cast<uint32_t *>(p.codes)[u] = c;
+        if ((col & 3u) == 0u) store_scale(p, b.row + dr, col >> 2, s);
     }
 }
 
@@ -189,9 +209,9 @@ template <int DT>
 void launch_quantize(const RowParams &p, cudaStream_t st)
 {
     if (p.units <= kFewUnits)
-        k_mx_quantize<DT, 1><<<(unsigned)((p.units + kRowThreads - 1) / kRowThreads), kRowThreads, 0, st>>>(p);
+        k_mx_quantize_small<DT><<<(unsigned)((p.units + kRowThreads - 1) / kRowThreads), kRowThreads, 0, st>>>(p);
     else
-        k_mx_quantize<DT, 4><<<(unsigned)((p.units + 4 * kRowThreads - 1) / (4 * kRowThreads)), kRowThreads, 0, st>>>(p);
+        k_mx_quantize<DT><<<(unsigned)((p.units + 4 * kRowThreads - 1) / (4 * kRowThreads)), kRowThreads, 0, st>>>(p);
 }
 
 template <int DT>

@@ -26,7 +26,7 @@ __global__ void __launch_bounds__(kScatterThreads) k_mx_scatter(MxScatterParams 
 {
     const unsigned full = 0xffffffffu;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    const int lane = lane_id(), quad = lane >> 2, sub = lane & 3;
+    const int lane = lane_id();
     const int hv = p.s.hv;                                   // units of eight elements per row
     const int all = (hv + 127) / 128;                        // pieces per row
     const int per_row = (all + p.pieces - 1) / p.pieces;     // work items per row
@@ -64,17 +64,8 @@ __global__ void __launch_bounds__(kScatterThreads) k_mx_scatter(MxScatterParams 
                     in[i] = u < hv ? ld_stream_v4(src + u) : make_uint4(0u, 0u, 0u, 0u);
                 }
             }
-            // 4 x 4 transpose in the quad: lane `sub` ends with the four words of block 8 * sub + quad
-            {
-                uint32_t x0 = (lane & 1) ? w[0] : w[1], x1 = (lane & 1) ? w[2] : w[3];
-                x0 = __shfl_xor_sync(full, x0, 1); x1 = __shfl_xor_sync(full, x1, 1);
-                if (lane & 1) { w[0] = x0; w[2] = x1; } else { w[1] = x0; w[3] = x1; }
-                x0 = (lane & 2) ? w[0] : w[2]; x1 = (lane & 2) ? w[1] : w[3];
-                x0 = __shfl_xor_sync(full, x0, 2); x1 = __shfl_xor_sync(full, x1, 2);
-                if (lane & 2) { w[0] = x0; w[1] = x1; } else { w[2] = x0; w[3] = x1; }
-            }
-            const uint32_t scale = sub == 0 ? s[0] : sub == 1 ? s[1] : sub == 2 ? s[2] : s[3];
-            const int block = c * 32 + 8 * sub + quad;       // block of the row
+            const uint32_t scale = mx_transpose(w, s, lane);
+            const int block = c * 32 + mx_block_of_lane(lane);   // block of the row
             const bool inside = block * 4 < hv;
             const bool pad = !inside && block < p.pitch;     // padding of the row of scales: written as 0
             const uint4 out = make_uint4(w[0], w[1], w[2], w[3]);
