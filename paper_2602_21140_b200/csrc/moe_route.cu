@@ -1149,11 +1149,7 @@ moe_status moe_mx_dispatch(moe_ctx *ctx, const float *logits, const void *x, int
     sp.topk_slot = out->topk_slot; sp.slot_offsets = out->slot_offsets; sp.pos_in_slot = ctx->d_pos;
     sp.dst_row = out->dst_row; sp.src_index = out->src_index; sp.ctl = ctx->d_ctl;
     mp.codes = send_codes; mp.scales = send_scales; mp.pitch = mx_scale_pitch(d.H);
-    // A warp takes a whole row when there are rows enough for every SM's warps, and single 1024-column
-    // pieces otherwise.
-    const int pieces = (sp.hv + 127) / 128;
-    mp.pieces = T >= ctx->sm_count * 16 ? pieces : 1;
-    const long long items = (long long)T * ((pieces + mp.pieces - 1) / mp.pieces);
+    const long long items = (long long)T * ((sp.hv + 127) / 128);
     const long long want = (items + kScatterThreads / 32 - 1) / (kScatterThreads / 32);
     const int grid = (int)std::min<long long>(want, (long long)ctx->sm_count * 8);
     if (launch_kernel(k_mx_scatter, dim3(grid), dim3(kScatterThreads), 0, st, ctx->pdl, mp) != cudaSuccess) return MOE_ERR_CUDA;
