@@ -1151,8 +1151,7 @@ moe_status moe_mx_dispatch(moe_ctx *ctx, const float *logits, const void *x, int
     mp.codes = send_codes; mp.scales = send_scales; mp.pitch = mx_scale_pitch(d.H);
     const long long items = (long long)T * ((sp.hv + 127) / 128);
     const long long want = (items + kScatterThreads / 32 - 1) / (kScatterThreads / 32);
-    const int grid = (int)std::min<long long>(want, (long long)ctx->sm_count * 8);
-    if (launch_kernel(k_mx_scatter, dim3(grid), dim3(kScatterThreads), 0, st, ctx->pdl, mp) != cudaSuccess) return MOE_ERR_CUDA;
+    if (launch_kernel(k_mx_scatter, dim3((unsigned)want), dim3(kScatterThreads), 0, st, ctx->pdl, mp) != cudaSuccess) return MOE_ERR_CUDA;
     return MOE_OK;
 }
 
