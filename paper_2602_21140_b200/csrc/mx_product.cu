@@ -295,11 +295,10 @@ __device__ __forceinline__ Tile tile_at(const KernelParams &p, const int *ends, 
     return t;
 }
 
-// Shared memory of the epilogue: a group's two planes of the gated form, shared out to its four warps; the
-// plain form needs 2 KB per warp.
-constexpr int kPlane = 32 * 32 + 8;
-constexpr int kEpiWarpBytes = (2 * kPlane * 4 / 4 + 127) / 128 * 128;
-static_assert(kEpiWarpBytes >= 2048, "plain epilogue");
+// Shared memory of the epilogue, per group of warps: two boxes of bf16 rows (store_plain) or two planes of fp32
+// (store_gated); twice, used in turn behind one barrier each, where many rows make the epilogue as long as the
+// products.
+constexpr int kPlane = 32 * 32 + 8, kPlaneBytes = (2 * kPlane * 4 + 127) / 128 * 128, kBoxBytes = 2 * 4096;
 
 // The tiles of a CTA (or pair of CTAs) of a grid of `step`, first, first + step, ..., as a warp sees them.  Finding a tile is a chain of
 // dependent reads, so the lanes find the next 32 of them side by side and hand them out one by one.
@@ -349,7 +348,7 @@ __device__ __forceinline__ bool next_uniform(TileStream<NT, CG> &stream, Tile &t
     return true;
 }
 
-template <int NT, int STAGES, int CG>
+template <int NT, int STAGES, int CG, bool GATED>
 struct Layout {
     static constexpr int kBTile = (NT / CG + 31) / 32 * 32 * kRowBytes;   // this CTA's rows, in boxes of 32
     static constexpr int kRB = (NT + 127) / 128;              // 128-row scale blocks of the row operand
@@ -360,7 +359,8 @@ struct Layout {
     static constexpr int kStageOff = 0;
     static constexpr int kSfOff = STAGES * kStage;
     static constexpr int kEpiOff = kSfOff + STAGES * kSf;
-    static constexpr int kEpiBytes = kEpiWarps * kEpiWarpBytes;
+    static constexpr int kEpiBufs = NT > 64 ? 2 : 1, kEpiBuf = GATED ? kPlaneBytes : kBoxBytes;
+    static constexpr int kEpiBytes = 2 * kEpiBufs * kEpiBuf;
     static constexpr int kBarOff = kEpiOff + kEpiBytes;
     static constexpr int kBars = 2 * STAGES + 5;
     static constexpr int kEndsOff = kBarOff + ((kBars * 8 + 32 + 15) & ~15);
@@ -390,40 +390,52 @@ __device__ __forceinline__ bool group_all(int group, bool ok)
 
 __device__ __forceinline__ void group_sync(int group) { asm volatile("barrier.cta.sync %0, 128;" ::"r"(group + 1) : "memory"); }
 
-// 32 features x 32 rows of the accumulator as bf16 rows, through 2 KB of shared memory of this warp,
-// [32 rows][32 features].  The accumulator is read in the fragment layout (lane / 4 = feature, two
-// neighbouring rows per register pair), so that a pair is one bf16x2 and stmatrix writes it transposed: 16
-// conversions and 4 stores where one value at a time takes 32 of each.  The 16-byte pieces of a row are
-// swizzled over the banks; they leave as 16-byte stores, four lanes to a row's 64 bytes.  The fp32 sum is
-// rounded once.
-__device__ __forceinline__ void store_plain(const KernelParams &p, const Tile &t, int c0, const uint32_t (&v)[32],
-                                            unsigned char *buf, int quarter, int lane)
+// 128 features (four warps) x 32 rows of the accumulator as bf16 rows, through 8 KB of shared memory of this
+// group: two boxes of [32 rows][64 features], 128-byte swizzle.  The accumulator is read in the fragment layout
+// (lane / 4 = feature, two neighbouring rows per register pair), so that a pair is one bf16x2 and stmatrix writes
+// it transposed.  32 rows that all belong to the segment leave as two TMA stores, which cost the warps nothing;
+// the last rows of a segment leave as 16-byte stores, so that the rows behind it stay as they are.  (Every load or
+// store instruction of these warps has to queue for the shared memory that the products keep busy: with their own
+// stores of 64-byte pieces they were the limit of products with short K.)  The fp32 sum is rounded once.
+__device__ __forceinline__ void store_plain(const KernelParams &p, const CUtensorMap *map_y, const Tile &t, int c0, const uint32_t (&v)[32],
+                                            unsigned char *buf, int group, int quarter, int lane)
 {
-    const uint32_t base = smem_addr(buf);
+    const uint32_t base = smem_addr(buf) + (quarter >> 1) * 4096;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         uint32_t m[4];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {                          // features 8q .. 8q + 7
+        for (int q = 0; q < 4; ++q) {                          // features 8q .. 8q + 7 of the warp's 32
             const int at = (q >> 1) * 16 + 4 * i + (q & 1) * 2;
             const __nv_bfloat162 h = __floats2bfloat162_rn(__uint_as_float(v[at]), __uint_as_float(v[at + 1]));
             m[q] = *reinterpret_cast<const uint32_t *>(&h);
         }
-        const int r = 8 * i + (lane & 7);                      // lane names row r, piece lane / 8
-        const uint32_t at = base + r * 64 + ((((uint32_t)lane >> 3) ^ ((r >> 1) & 3)) << 4);
-        asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(m[0]), "r"(m[1]),
-                     "r"(m[2]), "r"(m[3])
+        const int r = 8 * i + (lane & 7), piece = (quarter & 1) * 4 + (lane >> 3);   // this lane's row and 16-byte piece
+        asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(base + r * 128 + ((piece ^ (r & 7)) << 4)),
+                     "r"(m[0]), "r"(m[1]), "r"(m[2]), "r"(m[3])
                      : "memory");
     }
-    __syncwarp();
-    const int f = t.feat + quarter * 32 + (lane & 3) * 8;
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        const int r = q * 8 + (lane >> 2);
-        const uint4 o = *reinterpret_cast<const uint4 *>(buf + r * 64 + (((lane & 3) ^ ((r >> 1) & 3)) << 4));
-        if (c0 + r < t.rows && f < p.N) *reinterpret_cast<uint4 *>(p.y + (size_t)(t.row + c0 + r) * p.N + f) = o;
+    fence_async_shared();
+    const bool leader = quarter == 0 && lane == 0;
+    if (leader) bulk_wait_read<0>();                           // the other buffer's stores have left it
+    group_sync(group);
+    const int left = t.rows - c0;
+    if (left >= 32) {
+        if (leader) {
+            for (int h = 0; h < 2; ++h)
+                if (t.feat + 64 * h < p.N)
+                    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map_y),
+                                 "r"(t.feat + 64 * h), "r"(t.row + c0), "r"(smem_addr(buf) + 4096 * h)
+                                 : "memory");
+            bulk_commit();
+        }
+    } else {
+        const int tid = quarter * 32 + lane, piece = tid & 15, f = t.feat + piece * 8;
+        for (int r = tid >> 4; r < left; r += 8) {
+            const uint4 o = *reinterpret_cast<const uint4 *>(buf + (piece >> 3) * 4096 + r * 128 + (((piece & 7) ^ (r & 7)) << 4));
+            if (f < p.N) *reinterpret_cast<uint4 *>(p.y + (size_t)(t.row + c0 + r) * p.N + f) = o;
+        }
     }
-    __syncwarp();
 }
 
 // SwiGLU and quantisation of 128 weight rows (64 pairs of a gate and its up-projection, in even and odd
@@ -466,7 +478,6 @@ __device__ __forceinline__ void store_gated(const KernelParams &p, const Tile &t
             a = max(a, __float_as_uint(e[i]) & 0x7fffffffu);
         }
     }
-    group_sync(group);                                         // the planes are free for the next 32 rows
     a = max(a, __shfl_xor_sync(0xffffffffu, a, 1));
     const uint32_t s = mx_scale_byte(a);
     const float inv = mx_inverse_scale(s);
@@ -486,11 +497,11 @@ __device__ __forceinline__ void store_gated(const KernelParams &p, const Tile &t
 }
 
 template <int NT, int STAGES, int CG, bool GATED>
-__global__ void __launch_bounds__(Layout<NT, STAGES, CG>::kThreads, 1)
+__global__ void __launch_bounds__(Layout<NT, STAGES, CG, GATED>::kThreads, 1)
 k_mx_product(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_big,
-             const KernelParams p)
+             const __grid_constant__ CUtensorMap map_y, const KernelParams p)
 {
-    using L = Layout<NT, STAGES, CG>;
+    using L = Layout<NT, STAGES, CG, GATED>;
     constexpr int kBox = 32, kBig = NT / CG;                   // rows per TMA load of the row operand
     extern __shared__ unsigned char raw[];
     unsigned char *base = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
@@ -517,6 +528,7 @@ k_mx_product(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
         asm volatile("prefetch.tensormap [%0];" ::"l"(&map_w));
         asm volatile("prefetch.tensormap [%0];" ::"l"(&map_a));
         asm volatile("prefetch.tensormap [%0];" ::"l"(&map_big));
+        if (!GATED) asm volatile("prefetch.tensormap [%0];" ::"l"(&map_y));
     }
     if (warp == kMmaWarp) tmem_alloc<CG>(tmem_slot, 512);
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -764,12 +776,12 @@ k_mx_product(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
     } else if (warp < kEpiWarps) {
         // epilogue: TMEM lane = feature of the tile, column = row
         const int group = warp >> 2, quarter = warp & 3;
-        int buf = 0;
+        int buf = 0, epi_turn = 0;
         unsigned acc_parity = 0;
         Tile t;
         for (TileStream<NT, CG> stream(p, ends, tiles); stream.next(t);) {
             bool ok = wait_for(&acc_full[buf], acc_parity, quit, p.spin_limit);
-            ok = GATED ? group_all(group, ok) : __all_sync(0xffffffffu, ok);   // the gated epilogue's warps meet at barriers
+            ok = group_all(group, ok);                          // the group's warps meet at barriers below
             if (!ok) break;
             tc_fence_after();
             const uint32_t acc = tmem + buf * NT + ((uint32_t)(quarter * 32) << 16);
@@ -784,13 +796,21 @@ k_mx_product(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
                     __syncwarp();
                     if (lane == 0) mbar_arrive_lead<CG>(&acc_empty[buf]);
                 }
-                if (GATED) store_gated(p, t, c0, v, reinterpret_cast<float *>(epi + group * 4 * kEpiWarpBytes), group, quarter, lane);
-                else store_plain(p, t, c0, v, epi + warp * kEpiWarpBytes, quarter, lane);
+                unsigned char *epi_buf = epi + (group * L::kEpiBufs + epi_turn) * L::kEpiBuf;
+                if (GATED) store_gated(p, t, c0, v, reinterpret_cast<float *>(epi_buf), group, quarter, lane);
+                else store_plain(p, &map_y, t, c0, v, epi_buf, group, quarter, lane);
+                if (L::kEpiBufs == 2) {
+                    epi_turn ^= 1;
+                } else {                                        // one buffer: free before the next 32 rows are written
+                    if (!GATED && quarter == 0 && lane == 0) bulk_wait_read<0>();
+                    group_sync(group);
+                }
             }
             if (group * 32 >= t.rows && lane == 0) mbar_arrive_lead<CG>(&acc_empty[buf]);
             buf ^= 1;
             if (buf == 0) acc_parity ^= 1u;
         }
+        if (!GATED && quarter == 0 && lane == 0) bulk_wait_all();   // the last stores have left shared memory
     }
 
     __syncwarp();
@@ -824,18 +844,18 @@ EncodeTiled encode_fn()
     return fn;
 }
 
-bool encode(CUtensorMap *map, const uint8_t *ptr, int rank, const cuuint64_t *dims, const cuuint64_t *strides, int box_rows)
+bool encode(CUtensorMap *map, CUtensorMapDataType type, const void *ptr, int rank, const cuuint64_t *dims, const cuuint64_t *strides,
+            int box_cols, int box_rows)
 {
-    const cuuint32_t box[3] = {(cuuint32_t)kRowBytes, (cuuint32_t)box_rows, 1u}, one[3] = {1u, 1u, 1u};
-    return encode_fn()(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, rank, const_cast<uint8_t *>(ptr), dims, strides, box, one,
-                       CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                       CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    const cuuint32_t box[3] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows, 1u}, one[3] = {1u, 1u, 1u};
+    return encode_fn()(map, type, rank, const_cast<void *>(ptr), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                       CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 template <int NT, int STAGES, int CG, bool GATED>
 cudaError_t launch(const MxProductArgs &a, cudaStream_t st)
 {
-    using L = Layout<NT, STAGES, CG>;
+    using L = Layout<NT, STAGES, CG, GATED>;
     static_assert(L::kEndsOff + 1024 + kMaxP * 4 <= 227 * 1024, "shared memory");
     static_assert(NT >= 32 && NT % 32 == 0, "row boxes and epilogue chunks are 32 rows");
     const auto kernel = k_mx_product<NT, STAGES, CG, GATED>;
@@ -846,13 +866,18 @@ cudaError_t launch(const MxProductArgs &a, cudaStream_t st)
     });
     if (attr != cudaSuccess) return attr;
     if (!encode_fn()) return cudaErrorNotSupported;
-    CUtensorMap map_w, map_a, map_big;
+    CUtensorMap map_w, map_a, map_big, map_y = {};
     const cuuint64_t row = (cuuint64_t)a.K / 2;
     const cuuint64_t wd[3] = {row, (cuuint64_t)a.N, (cuuint64_t)a.P}, ws[2] = {row, row * (cuuint64_t)a.N};
     const cuuint64_t ad[2] = {row, (cuuint64_t)a.rows}, as[1] = {row};
-    if (!encode(&map_w, a.w_codes, 3, wd, ws, kFeat) || !encode(&map_a, a.a_codes, 2, ad, as, 32) ||
-        !encode(&map_big, a.a_codes, 2, ad, as, NT / CG))
-        return cudaErrorInvalidValue;
+    const CUtensorMapDataType u8 = CU_TENSOR_MAP_DATA_TYPE_UINT8;
+    bool ok = encode(&map_w, u8, a.w_codes, 3, wd, ws, kRowBytes, kFeat) && encode(&map_a, u8, a.a_codes, 2, ad, as, kRowBytes, 32) &&
+              encode(&map_big, u8, a.a_codes, 2, ad, as, kRowBytes, NT / CG);
+    if (!GATED) {
+        const cuuint64_t yd[2] = {(cuuint64_t)a.N, (cuuint64_t)a.rows}, ys[1] = {2 * (cuuint64_t)a.N};
+        ok = ok && encode(&map_y, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, a.y, 2, yd, ys, 64, 32);
+    }
+    if (!ok) return cudaErrorInvalidValue;
     KernelParams p;
     p.a_scales = a.a_scales; p.w_scales = a.w_scales; p.slot_counts = a.slot_counts; p.slot_offsets = a.slot_offsets;
     p.rows = a.rows; p.P = a.P; p.N = a.N; p.K = a.K; p.y = static_cast<__nv_bfloat16 *>(a.y);
@@ -869,7 +894,7 @@ cudaError_t launch(const MxProductArgs &a, cudaStream_t st)
     at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at; cfg.numAttrs = a.pdl ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, kernel, map_w, map_a, map_big, p);
+    return cudaLaunchKernelEx(&cfg, kernel, map_w, map_a, map_big, map_y, p);
 }
 
 template <bool GATED>
