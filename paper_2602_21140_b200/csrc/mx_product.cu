@@ -16,8 +16,8 @@
 //   warps 10-   scales, a warp per 128 rows: HBM -> registers -> the 32 x 16-byte blocks tcgen05.cp wants
 // The accumulator is double buffered, so the epilogue of a tile runs under the products of the next.
 //
-// Tiles are dealt slot by slot, feature tile by feature tile, row tile innermost: CTAs that work at the
-// same time share a weight tile (through L2) as often as possible.
+// Tiles are dealt feature tile by feature tile of a slot, row tile innermost: CTAs that work at the same time
+// share a weight tile (through L2) as often as possible.  How slots are ordered: see Order.
 #include "mx_product.h"
 
 #include <cuda.h>
@@ -35,7 +35,7 @@ constexpr int kFeat = 128;                 // features per CTA and tile
 constexpr int kStageK = 256;               // elements of K per stage
 constexpr int kRowBytes = kStageK / 2;     // bytes of a code row per stage
 constexpr int kATile = kFeat * kRowBytes;  // 16 KB
-constexpr int kMaxP = 4096;
+constexpr int kMaxP = 4096, kFullTableP = kMaxP / 4;   // slots up to which the tables of Order fit in full
 constexpr int kEpiWarps = 8, kTmaWarp = kEpiWarps, kMmaWarp = kEpiWarps + 1, kScaleWarp = kEpiWarps + 2;
 
 // ------------------------------------------------------------------ tcgen05 in PTX
@@ -274,9 +274,30 @@ __device__ __forceinline__ int segment(const KernelParams &p, int s, int &first)
 template <int NT>
 __device__ __forceinline__ int row_tiles(int c) { return (c + NT - 1) / NT; }
 
+// Sums of tile counts stop here.  Segments that do not overlap stay below it (the host checks that); counts left
+// behind by a dispatch that gave up may not.
+constexpr int kTooManyTiles = 1 << 30;
+__device__ __forceinline__ int tiles_sum(int a, int b) { return min(a + b, kTooManyTiles); }
+
+// The order of the tiles.  A slot whose rows fit one tile is bound by its weights (HBM), one with several row tiles by
+// the products (its weights come from L2 after the first), and neighbours in the order run at the same time.  So the
+// tiles of both kinds are merged in proportion, each kind in its own order, instead of slot by slot: with a
+// popularity skew HBM then works all the time and not in turn with the tensor cores.
+struct Order {
+    const int *many, *one;     // inclusive prefix over the slots of the tiles of either kind
+    const int2 *segments;      // first row and rows of every slot; NULL = read them again
+    int n_many, n_all;
+};
+
 template <int NT, int CG>
-__device__ __forceinline__ Tile tile_at(const KernelParams &p, const int *ends, int index)
+__device__ __forceinline__ Tile tile_at(const KernelParams &p, const Order &o, int index)
 {
+    const int *ends = o.one;
+    if (o.n_many > 0) {                              // tiles before `index` that are of the first kind, and whether this one is
+        const int m = (int)((long long)index * o.n_many / o.n_all), m1 = (int)(((long long)index + 1) * o.n_many / o.n_all);
+        if (m1 > m) ends = o.many;
+        index = m1 > m ? m : index - m;
+    }
     int lo = 0, hi = p.P - 1;                        // first slot whose inclusive end is beyond the index
     while (lo < hi) {
         const int mid = (lo + hi) >> 1;
@@ -284,8 +305,9 @@ __device__ __forceinline__ Tile tile_at(const KernelParams &p, const int *ends, 
     }
     const int local = index - (lo ? ends[lo - 1] : 0);
     Tile t;
-    int first;
-    const int c = segment(p, lo, first);
+    int first, c;
+    if (o.segments) { const int2 sg = o.segments[lo]; first = sg.x; c = sg.y; }
+    else c = segment(p, lo, first);
     const int nt = row_tiles<NT>(c);
     const int f = local / nt, r = local - f * nt;
     const int size = ((c + nt - 1) / nt + 15) & ~15;
@@ -305,12 +327,12 @@ constexpr int kPlane = 32 * 32 + 8, kPlaneBytes = (2 * kPlane * 4 + 127) / 128 *
 template <int NT, int CG>
 struct TileStream {
     const KernelParams &p;
-    const int *ends;
+    const Order &o;
     const int tiles;
     int base, at;
     Tile mine;
-    __device__ TileStream(const KernelParams &p_, const int *ends_, int tiles_)
-        : p(p_), ends(ends_), tiles(tiles_), base(blockIdx.x / CG), at(32), mine{}
+    __device__ TileStream(const KernelParams &p_, const Order &o_, int tiles_)
+        : p(p_), o(o_), tiles(tiles_), base(blockIdx.x / CG), at(32), mine{}
     {
     }
     __device__ bool next(Tile &t)                    // false when there are no more
@@ -320,7 +342,7 @@ struct TileStream {
                 if (base >= tiles) return false;
                 const int step = (int)gridDim.x / CG, i = base + (int)(threadIdx.x & 31) * step;
                 mine.rows = 0; mine.slot = -1;
-                if (i < tiles) mine = tile_at<NT, CG>(p, ends, i);
+                if (i < tiles) mine = tile_at<NT, CG>(p, o, i);
                 base += 32 * step;
                 at = 0;
                 __syncwarp();
@@ -364,7 +386,7 @@ struct Layout {
     static constexpr int kBarOff = kEpiOff + kEpiBytes;
     static constexpr int kBars = 2 * STAGES + 5;
     static constexpr int kEndsOff = kBarOff + ((kBars * 8 + 32 + 15) & ~15);
-    static size_t bytes(int P) { return 1024 + kEndsOff + (size_t)P * 4; }
+    static size_t bytes(int P) { return 1024 + kEndsOff + (size_t)P * (P <= kFullTableP ? 16 : 4); }
 };
 
 // Bounded wait.  `quit` is shared by the CTA: the first role that gives up sets it, the others follow.
@@ -534,27 +556,46 @@ k_mx_product(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
 
-    // inclusive prefix over the slots of their tile counts
+    // inclusive prefixes over the slots of their tile counts: with up to kFullTableP slots for both kinds (see
+    // Order), and the segments beside them, with more all slots as one kind
     const int feats = (p.N + CG * kFeat - 1) / (CG * kFeat);
+    const bool merge = p.P <= kFullTableP;
+    int2 *segments = reinterpret_cast<int2 *>(ends);           // with the full tables: [P] segments, [P] many, [P] one
+    int *many = ends + 2 * p.P;
+    if (merge) ends += 3 * p.P;
     {
         const int chunk = (p.P + L::kThreads - 1) / L::kThreads;
         const int s0 = tid * chunk, s1 = min(p.P, s0 + chunk);
-        int sum = 0;
+        int sum[2] = {0, 0};
         for (int s = s0; s < s1; ++s) {
             int first;
-            sum += feats * row_tiles<NT>(segment(p, s, first));
-            ends[s] = sum;
+            const int c = segment(p, s, first), nt = row_tiles<NT>(c);
+            if (merge) segments[s] = make_int2(first, c);
+            if (merge && nt > 1) sum[1] = tiles_sum(sum[1], feats * nt);
+            else sum[0] = tiles_sum(sum[0], feats * nt);
+            ends[s] = sum[0];
+            if (merge) many[s] = sum[1];
         }
-        int incl = sum;
-        for (int off = 1; off < 32; off <<= 1) {
-            const int o = __shfl_up_sync(0xffffffffu, incl, off);
-            if (lane >= off) incl += o;
+        int before[2];
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            int incl = sum[q];
+            for (int off = 1; off < 32; off <<= 1) {
+                const int o = __shfl_up_sync(0xffffffffu, incl, off);
+                if (lane >= off) incl = tiles_sum(incl, o);
+            }
+            if (lane == 31) warp_sums[2 * warp + q] = incl;
+            before[q] = __shfl_up_sync(0xffffffffu, incl, 1);
+            if (lane == 0) before[q] = 0;
         }
-        if (lane == 31) warp_sums[warp] = incl;
         __syncthreads();
-        int before = incl - sum;
-        for (int w = 0; w < warp; ++w) before += warp_sums[w];
-        for (int s = s0; s < s1; ++s) ends[s] += before;
+        for (int w = 0; w < warp; ++w) {
+            before[0] = tiles_sum(before[0], warp_sums[2 * w]); before[1] = tiles_sum(before[1], warp_sums[2 * w + 1]);
+        }
+        for (int s = s0; s < s1; ++s) {
+            ends[s] = tiles_sum(ends[s], before[0]);
+            if (merge) many[s] = tiles_sum(many[s], before[1]);
+        }
     }
     __syncwarp();
     tc_fence_before();
@@ -566,7 +607,11 @@ k_mx_product(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
     constexpr uint32_t tmem = 0;
     const bool whole = *tmem_slot == 0;
     if (tid == 0 && !whole) *quit = 1;
-    const int tiles = whole ? ends[p.P - 1] : 0;
+    const int n_many = merge ? many[p.P - 1] : 0, n_all = tiles_sum(ends[p.P - 1], n_many);
+    const Order order = {many, ends, merge ? segments : nullptr, n_many, n_all};
+    const bool sane = n_all < kTooManyTiles;                   // else counts that no dispatch writes: nothing is touched
+    if (tid == 0 && !sane) report_status(p.ctl, kDevCapacity);
+    const int tiles = whole && sane ? n_all : 0;
     const int steps = (p.K + kStageK - 1) / kStageK;
     constexpr uint32_t kSfCol = 2 * NT;                        // scale columns follow the two accumulators
     constexpr uint32_t kSfaCols = 8, kSfbCols = 8 * L::kRB;    // per stage parity
@@ -582,7 +627,7 @@ k_mx_product(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
         unsigned parity = 1;                                   // a fresh barrier passes the wait for parity 1
         bool ok = true;
         Tile t;
-        for (TileStream<NT, CG> stream(p, ends, tiles); ok && next_uniform(stream, t);) {
+        for (TileStream<NT, CG> stream(p, order, tiles); ok && next_uniform(stream, t);) {
             const int half = t.n() / CG;                       // rows of the tile in this CTA
             // each TMA instruction costs its warp some 80 cycles: many rows come in one box, few in boxes of 32
             const bool big = half > 2 * kBox;
@@ -620,7 +665,7 @@ k_mx_product(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
         bool ok = true;
         const uint64_t stage_desc = desc_codes(smem_addr(stage)), sf_desc = desc_scales(smem_addr(sf));
         Tile t;
-        for (TileStream<NT, CG> stream(p, ends, tiles); ok && next_uniform(stream, t);) {
+        for (TileStream<NT, CG> stream(p, order, tiles); ok && next_uniform(stream, t);) {
             ok = __all_sync(0xffffffffu, wait_for(&acc_empty[buf], acc_parity, quit, p.spin_limit));
             if (!ok) break;
             tc_fence_after();
@@ -687,7 +732,7 @@ k_mx_product(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
         uint4 ring[kPieces][4];
         bool valid[kPieces];
         const uint8_t *src[4];
-        TileStream<NT, CG> stream(p, ends, tiles);
+        TileStream<NT, CG> stream(p, order, tiles);
         int piece = 0;
         int whose = 0;                                         // turn of the next piece
         auto fetch = [&](uint4 (&v)[4]) {                      // this warp's next piece, over all tiles; false when there is none
@@ -779,7 +824,7 @@ k_mx_product(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
         int buf = 0, epi_turn = 0;
         unsigned acc_parity = 0;
         Tile t;
-        for (TileStream<NT, CG> stream(p, ends, tiles); stream.next(t);) {
+        for (TileStream<NT, CG> stream(p, order, tiles); stream.next(t);) {
             bool ok = wait_for(&acc_full[buf], acc_parity, quit, p.spin_limit);
             ok = group_all(group, ok);                          // the group's warps meet at barriers below
             if (!ok) break;
@@ -862,7 +907,7 @@ cudaError_t launch(const MxProductArgs &a, cudaStream_t st)
     static std::once_flag once;
     static cudaError_t attr = cudaSuccess;
     std::call_once(once, [&] {
-        attr = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)L::bytes(kMaxP));
+        attr = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)std::max(L::bytes(kMaxP), L::bytes(kFullTableP)));
     });
     if (attr != cudaSuccess) return attr;
     if (!encode_fn()) return cudaErrorNotSupported;

@@ -17,7 +17,7 @@ pytestmark = pytest.mark.gpu
 
 def _router(P, k=1):
     E = P
-    cfg = B.make_config(min(E, 512), k, 64, 16, 1 if P <= 512 else P // 512, P if P <= 512 else 512, 8)
+    cfg = B.make_config(min(E, 512), k, 64, 16, P, 1, 8)          # P ranks of one slot
     return B.MoeRouter(cfg, [p % cfg.num_experts for p in range(P)], None, [1.0] * P)
 
 
@@ -116,6 +116,88 @@ def _pack(codes, sb):
     return packed, s
 
 
+@pytest.mark.parametrize("P", [1024, 1025, 1536])
+def test_many_slots(P):
+    """Around the number of slots up to which the kernel keeps its full tables, most of them empty."""
+    counts = np.zeros(P, np.int32)
+    rng = np.random.default_rng(P)
+    counts[rng.choice(P, 40, replace=False)] = rng.integers(1, 9, 40)
+    counts[P - 1], counts[0], counts[P // 2] = 70, 0, 230
+    N, K = 136, 96
+    r = _router(P)
+    n = int(counts.sum())
+    a, w = _mx(M.random_rows(n, K, 1)), _weights(P, N, K, 2)
+    c, o = M.segments(counts)
+    y = r.mx_expert_product(a, _dev(c), _dev(o), w)
+    want, mag = _sums(_vals(a), _vals(w), c, o, n)
+    assert ((y.double() - want).abs() <= (K / 64 + 64) * 2.0 ** -23 * mag + 2.0 ** -8 * want.abs()).all()
+    # the same rows in few slots' worth of the wide kernel: many rows a slot on average
+    big = np.zeros(P, np.int32)
+    big[[3, P - 2]] = [32 * P, 33 * P + 7]
+    c, o = M.segments(big)
+    n = int(big.sum())
+    a = _mx(M.random_rows(n, K, 3))
+    y = r.mx_expert_product(a, _dev(c), _dev(o), w)
+    want, mag = _sums(_vals(a), _vals(w), c, o, n)
+    assert ((y.double() - want).abs() <= (K / 64 + 64) * 2.0 ** -23 * mag + 2.0 ** -8 * want.abs()).all()
+    assert r.device_status() == 0
+    r.close()
+
+
+@pytest.mark.parametrize("seed", range(6))
+def test_skewed_slots_in_any_order(seed):
+    """A few slots with many row tiles among slots with one or none, laid out in a random order with gaps."""
+    rng = np.random.default_rng(seed)
+    P = int(rng.integers(2, 14))
+    counts = np.where(rng.random(P) < 0.3, rng.integers(225, 1500, P), rng.integers(0, 200, P)).astype(np.int32)
+    N, K = int(rng.integers(1, 60)) * 8, int(rng.integers(1, 40)) * 32
+    order = rng.permutation(P)
+    offsets, at = np.zeros(P + 1, np.int32), 0
+    for p in order:
+        at += int(rng.integers(0, 40))
+        offsets[p] = at
+        at += counts[p]
+    n = at + int(rng.integers(0, 50))
+    r = _router(P)
+    a, w = _mx(M.random_rows(n, K, seed, 1.0)), _weights(P, N, K, seed + 50)
+    y = torch.full((n, N), -7.0, dtype=torch.bfloat16, device="cuda")
+    r.mx_expert_product(a, _dev(counts), _dev(offsets), w, y)
+    want, mag = _sums(_vals(a), _vals(w), counts, offsets, n)
+    own = ~torch.isnan(want[:, 0])
+    assert (y[~own] == -7).all()
+    tol = (K / 64 + 64) * 2.0 ** -23 * mag + 2.0 ** -8 * want.abs()
+    assert ((y.double() - want).abs() <= tol)[own].all()
+    assert r.device_status() == 0
+    r.close()
+
+
+def test_refusals():
+    r = _router(2)
+    a, w, z = _mx(M.random_rows(4, 64, 1)), _weights(2, 128, 64, 1), _dev([2, 2])
+    o = _dev([0, 2, 4])
+    ok = lambda **k: r.mx_expert_product(**{**dict(rows=a, slot_counts=z, slot_offsets=o, weight=w), **k})   # noqa: E731
+    ok()
+    for bad in (dict(weight=_weights(3, 128, 64, 1)), dict(weight=_weights(2, 128, 32, 1)), dict(weight=_weights(2, 132, 64, 1)),
+                dict(slot_counts=z.long()), dict(slot_counts=_dev([1, 1, 2])), dict(slot_offsets=o[:1]), dict(slot_counts=z.cpu()),
+                dict(rows=B.MxRows(a.codes[:, :16], a.scales)), dict(rows=B.MxRows(a.codes, a.scales[:3])),
+                dict(rows=B.MxRows(a.codes.float(), a.scales)), dict(y=torch.empty(4, 120, dtype=torch.bfloat16, device="cuda")),
+                dict(y=torch.empty(4, 128, device="cuda"))):
+        with pytest.raises(B.MoeError):
+            ok(**bad)
+    with pytest.raises(B.MoeError):                                   # gate and up rows come in pairs of 32 features
+        r.mx_expert_gated(a, z, o, _weights(2, 96, 64, 1))
+    p = a.codes.data_ptr()
+    args = [r._ctx, p, a.scales.data_ptr(), 4, z.data_ptr(), o.data_ptr(), w.codes.data_ptr(), w.scales.data_ptr(), 128, 64, p]
+    for i, v in ((1, p + 8), (2, 0), (3, -1), (4, 0), (5, 0), (6, p + 1), (7, 0), (8, 0), (8, 12), (9, 16), (10, p + 4), (10, 0)):
+        bad = list(args)
+        bad[i] = v
+        assert B.moe_mx_expert_product(*bad) == B.MOE_ERR_INVALID_ARG, i
+    args[3] = (1 << 30) + 1                                           # more rows than the call takes
+    assert B.moe_mx_expert_product(*args) == B.MOE_ERR_CAPACITY
+    torch.cuda.synchronize()
+    r.close()
+
+
 def test_rows_outside_segments_stay():
     """Gaps between segments, slots in another order, and rows behind the last segment."""
     P, N, K, rows = 4, 136, 256, 200
@@ -147,6 +229,19 @@ def test_segments_that_leave_the_buffer_are_cut():
     own = ~torch.isnan(want[:, 0])
     tol = (K / 64 + 64) * 2.0 ** -23 * mag + 2.0 ** -8 * want.abs()
     assert ((y.double() - want).abs() <= tol)[own].all()
+    r.close()
+
+
+def test_segments_that_overlap_stay_inside():
+    """Not a dispatch's output, but it must not reach outside of y: every slot claims every row."""
+    P, N, K, rows = 40, 128, 64, 300
+    r = _router(P)
+    a, w = _mx(M.random_rows(rows, K, 3)), _weights(P, N, K, 4)
+    guard = torch.full((rows + 64, N), -7.0, dtype=torch.bfloat16, device="cuda")
+    r.mx_expert_product(a, _dev([2 ** 31 - 1] * P), _dev([0] * P), w, guard[32:32 + rows])
+    torch.cuda.synchronize()
+    assert r.device_status() == 0
+    assert (guard[:32] == -7).all() and (guard[32 + rows:] == -7).all()
     r.close()
 
 
