@@ -475,21 +475,26 @@ def mx_empty(*shape, device="cuda") -> MxRows:
                   torch.empty((*lead, _mx_pitch(cols)), dtype=torch.uint8, device=device))
 
 
+def _mx_like(x: torch.Tensor, lead, cols: int) -> MxRows:
+    """As mx_empty, on the device of ``x``."""
+    return MxRows(x.new_empty((*lead, cols // 2), dtype=torch.uint8), x.new_empty((*lead, _mx_pitch(cols)), dtype=torch.uint8))
+
+
 def mx_quantize(x: torch.Tensor, out: MxRows | None = None) -> MxRows:
     """Rows of ``x`` ([..., cols], bf16 / fp16 / fp32) in 4 bits, on the current stream of its device.
     A 2-D ``x`` may have any row stride that keeps its rows 16-byte aligned; others are contiguous."""
-    _require(x.is_cuda and x.dtype in _DTYPE_CODE and x.dim() >= 1 and x.shape[-1] > 0 and x.shape[-1] % 32 == 0, "mx_quantize")
-    flat = x.is_contiguous()
-    _require(flat or (x.dim() == 2 and x.stride(1) == 1), "mx_quantize")
-    cols, index = x.shape[-1], x.get_device()
+    shape, code = x.shape, _DTYPE_CODE.get(x.dtype)
+    _require(x.is_cuda and code is not None and len(shape) > 0 and shape[-1] > 0 and shape[-1] % 32 == 0, "mx_quantize")
+    cols, index, stride = shape[-1], x.get_device(), shape[-1]
+    if not x.is_contiguous():
+        _require(len(shape) == 2 and x.stride(1) == 1, "mx_quantize")
+        stride = x.stride(0)
     if out is None:
-        out = mx_empty(*x.shape, device=x.device)
+        out = _mx_like(x, shape[:-1], cols)
     else:
-        _require(_is_mx(out, x.get_device(), x.shape[:-1]) and out.cols == cols, "mx_quantize")
-    rows = x.numel() // cols
-    stride = cols if flat else x.stride(0)
-    st = _on_device(index, moe_mx_quantize, x.data_ptr(), _DTYPE_CODE[x.dtype], rows, cols, stride,
-                    out.codes.data_ptr(), out.scales.data_ptr(), _raw_stream(index))
+        _require(_is_mx(out, index, shape[:-1]) and out.cols == cols, "mx_quantize")
+    st = _on_device(index, moe_mx_quantize, x.data_ptr(), code, x.numel() // cols, cols, stride, out.codes.data_ptr(),
+                    out.scales.data_ptr(), _raw_stream(index))
     if st != MOE_OK:
         raise MoeError(st, "moe_mx_quantize")
     return out
@@ -502,7 +507,7 @@ def mx_dequantize(m: MxRows, dtype: torch.dtype = torch.bfloat16, out: torch.Ten
     shape, cols = (*m.codes.shape[:-1], m.cols), m.cols
     stride = cols
     if out is None:
-        out = torch.empty(shape, dtype=dtype, device=m.codes.device)
+        out = m.codes.new_empty(shape, dtype=dtype)
     else:
         flat = out.is_contiguous()
         _require(out.shape == shape and out.dtype is dtype and out.is_cuda and out.get_device() == index
@@ -618,7 +623,7 @@ class MoeRouter:
         if out is None:
             out = self.alloc_outputs(T, send_buf=False)
         if rows is None:
-            rows = mx_empty(T * c.top_k, H, device=self.device)
+            rows = _mx_like(x, (T * c.top_k,), H)
         else:
             _require(_is_mx(rows, dev, (T * c.top_k,)) and rows.cols == H, "mx_dispatch")
         st = moe_mx_dispatch(self._ctx, logits.data_ptr(), x.data_ptr(), T, out.as_struct(), rows.codes.data_ptr(),
@@ -641,7 +646,7 @@ class MoeRouter:
         _require(self._segments_ok(rows, slot_counts, slot_offsets, weight, dev), "mx_expert_product")
         n, n_out = rows.codes.shape[0], weight.codes.shape[1]
         if y is None:
-            y = torch.empty((n, n_out), dtype=torch.bfloat16, device=self.device)
+            y = rows.codes.new_empty((n, n_out), dtype=torch.bfloat16)
         else:
             _require(_is_dense(y, torch.bfloat16, (n, n_out), dev), "mx_expert_product")
         st = moe_mx_expert_product(self._ctx, rows.codes.data_ptr(), rows.scales.data_ptr(), n, slot_counts.data_ptr(),
@@ -659,7 +664,7 @@ class MoeRouter:
                  and gate_up.codes.shape[1] > 0, "mx_expert_gated")
         n, n_hidden = rows.codes.shape[0], gate_up.codes.shape[1] // 2
         if out is None:
-            out = mx_empty(n, n_hidden, device=self.device)
+            out = _mx_like(rows.codes, (n,), n_hidden)
         else:
             _require(_is_mx(out, dev, (n,)) and out.cols == n_hidden, "mx_expert_gated")
         st = moe_mx_expert_gated(self._ctx, rows.codes.data_ptr(), rows.scales.data_ptr(), n, slot_counts.data_ptr(),
@@ -691,11 +696,11 @@ class MoeRouter:
         H, k = c.hidden, c.top_k
         ok = _is_dense(expert_buf, torch.bfloat16, (T * k, H), dev) and _is_dense(dy, torch.bfloat16, (T, H), dev)
         if d_expert_buf is None:
-            d_expert_buf = torch.empty((T * k, H), dtype=torch.bfloat16, device=self.device)
+            d_expert_buf = torch.empty_like(expert_buf)
         else:
             ok = ok and _is_dense(d_expert_buf, torch.bfloat16, (T * k, H), dev)
         if d_weights is None:
-            d_weights = torch.empty((T, k), dtype=torch.float32, device=self.device)
+            d_weights = dy.new_empty((T, k), dtype=torch.float32)
         else:
             ok = ok and _is_dense(d_weights, torch.float32, (T, k), dev)
         _require(ok, "combine_backward")
@@ -713,13 +718,13 @@ class MoeRouter:
         H, k, E = c.hidden, c.top_k, c.num_experts
         ok = _is_dense(d_send_buf, torch.bfloat16, (T * k, H), dev)
         if dx is None:
-            dx = torch.empty((T, H), dtype=torch.bfloat16, device=self.device)
+            dx = d_send_buf.new_empty((T, H))
         else:
             ok = ok and _is_dense(dx, torch.bfloat16, (T, H), dev)
         if d_weights is not None:
             ok = ok and _is_dense(d_weights, torch.float32, (T, k), dev)
             if d_logits is None:
-                d_logits = torch.empty((T, E), dtype=torch.float32, device=self.device)
+                d_logits = d_weights.new_empty((T, E))
         if d_logits is not None:
             ok = ok and _is_dense(d_logits, torch.float32, (T, E), dev)
         ok = ok and (logits is None or _is_dense(logits, torch.float32, (T, E), dev))

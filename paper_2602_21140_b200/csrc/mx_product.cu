@@ -281,24 +281,26 @@ __device__ __forceinline__ int tiles_sum(int a, int b) { return min(a + b, kTooM
 
 // The order of the tiles.  A slot whose rows fit one tile is bound by its weights (HBM), one with several row tiles by
 // the products (its weights come from L2 after the first), and neighbours in the order run at the same time.  So the
-// tiles of both kinds are merged in proportion, each kind in its own order, instead of slot by slot: with a
-// popularity skew HBM then works all the time and not in turn with the tensor cores.
+// tiles of both kinds are merged in proportion, each kind in its own order, instead of slot by slot: with a popularity
+// skew HBM then works all the time and not in turn with the tensor cores.  (Everything here is kept short: between
+// two launches the weights push this code out of L2, and in a call of 20 us every line of it is fetched anew.)
 struct Order {
     const int *many, *one;     // inclusive prefix over the slots of the tiles of either kind
     const int2 *segments;      // first row and rows of every slot; NULL = read them again
-    int n_many, n_all;
+    unsigned share;            // 2^32 * (tiles of the first kind) / (all tiles), rounded up; 0 = all are of the second
 };
 
 template <int NT, int CG>
 __device__ __forceinline__ Tile tile_at(const KernelParams &p, const Order &o, int index)
 {
     const int *ends = o.one;
-    if (o.n_many > 0) {                              // tiles before `index` that are of the first kind, and whether this one is
-        const int m = (int)((long long)index * o.n_many / o.n_all), m1 = (int)(((long long)index + 1) * o.n_many / o.n_all);
+    if (o.share) {                                   // tiles before `index` that are of the first kind, and whether this one is
+        const int m = (int)__umulhi(index, o.share), m1 = (int)__umulhi(index + 1, o.share);
         if (m1 > m) ends = o.many;
         index = m1 > m ? m : index - m;
     }
     int lo = 0, hi = p.P - 1;                        // first slot whose inclusive end is beyond the index
+#pragma unroll 1
     while (lo < hi) {
         const int mid = (lo + hi) >> 1;
         if (ends[mid] > index) hi = mid; else lo = mid + 1;
@@ -567,6 +569,7 @@ k_mx_product(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
         const int chunk = (p.P + L::kThreads - 1) / L::kThreads;
         const int s0 = tid * chunk, s1 = min(p.P, s0 + chunk);
         int sum[2] = {0, 0};
+#pragma unroll 1
         for (int s = s0; s < s1; ++s) {
             int first;
             const int c = segment(p, s, first), nt = row_tiles<NT>(c);
@@ -578,8 +581,9 @@ k_mx_product(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
         }
         int before[2];
 #pragma unroll
-        for (int q = 0; q < 2; ++q) {
+        for (int q = 0; q < 2; ++q) {                          // (loops that are run once are not unrolled)
             int incl = sum[q];
+#pragma unroll 1
             for (int off = 1; off < 32; off <<= 1) {
                 const int o = __shfl_up_sync(0xffffffffu, incl, off);
                 if (lane >= off) incl = tiles_sum(incl, o);
@@ -589,9 +593,11 @@ k_mx_product(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
             if (lane == 0) before[q] = 0;
         }
         __syncthreads();
+#pragma unroll 1
         for (int w = 0; w < warp; ++w) {
             before[0] = tiles_sum(before[0], warp_sums[2 * w]); before[1] = tiles_sum(before[1], warp_sums[2 * w + 1]);
         }
+#pragma unroll 1
         for (int s = s0; s < s1; ++s) {
             ends[s] = tiles_sum(ends[s], before[0]);
             if (merge) many[s] = tiles_sum(many[s], before[1]);
@@ -608,7 +614,10 @@ k_mx_product(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
     const bool whole = *tmem_slot == 0;
     if (tid == 0 && !whole) *quit = 1;
     const int n_many = merge ? many[p.P - 1] : 0, n_all = tiles_sum(ends[p.P - 1], n_many);
-    const Order order = {many, ends, merge ? segments : nullptr, n_many, n_all};
+    Order order = {many, ends, merge ? segments : nullptr, 0u};
+    if (n_many == n_all) order.one = many;                     // only that kind
+    // share * n_all / 2^32 is n_many and a fraction: exactly n_many of the n_all tiles are of the first kind
+    else if (n_many > 0) order.share = (unsigned)(((unsigned long long)n_many << 32) / (unsigned)n_all) + 1u;
     const bool sane = n_all < kTooManyTiles;                   // else counts that no dispatch writes: nothing is touched
     if (tid == 0 && !sane) report_status(p.ctl, kDevCapacity);
     const int tiles = whole && sane ? n_all : 0;
@@ -722,13 +731,16 @@ k_mx_product(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
         // l, l + 32, l + 64 and l + 96.
         // tcgen05.cp wants, for each K = 128, [32 lanes][4 rows][4 scales]: word w of the lane's four rows is
         // one 16-byte store, so nothing is transposed and no two lanes meet in a bank.
-        constexpr int kPieces = 3;
+        constexpr int kPieces = 2;
         const int blk = (warp - kScaleWarp) % (1 + L::kRB);    // 0: weights; 1 + rb: data rows [128 rb, 128 rb + 128)
         const int turn = (warp - kScaleWarp) / (1 + L::kRB);   // this warp's pieces: even or odd ones
         const int pitch = mx_scale_pitch(p.K);
         const int pieces = (steps + 1) / 2;
         const int left = p.K / kMxBlock - (pieces - 1) * 16;   // scales of the last piece; the padding counts as 1
         const uint32_t one = 0x7f7f7f7fu;                      // scale 1: for rows that do not exist
+        uint32_t keep[4];
+#pragma unroll
+        for (int x = 0; x < 4; ++x) keep[x] = 0xffffffffu >> min(31, max(0, 32 - 8 * (left - 4 * x))) & (left > 4 * x ? 0xffffffffu : 0u);
         uint4 ring[kPieces][4];
         bool valid[kPieces];
         const uint8_t *src[4];
@@ -776,16 +788,9 @@ k_mx_product(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
                 uint4 (&v)[4] = ring[d];
                 if (at == pieces - 1 && left < 16) {
 #pragma unroll
-                    for (int g = 0; g < 4; ++g) {
-                        uint32_t w[4] = {v[g].x, v[g].y, v[g].z, v[g].w};
-#pragma unroll
-                        for (int x = 0; x < 4; ++x) {
-                            const int keep = min(4, max(0, left - 4 * x));
-                            const uint32_t mask = keep == 4 ? 0xffffffffu : (1u << (8 * keep)) - 1u;
-                            w[x] = (w[x] & mask) | (one & ~mask);
-                        }
-                        v[g] = make_uint4(w[0], w[1], w[2], w[3]);
-                    }
+                    for (int g = 0; g < 4; ++g)
+                        v[g] = make_uint4((v[g].x & keep[0]) | (one & ~keep[0]), (v[g].y & keep[1]) | (one & ~keep[1]),
+                                          (v[g].z & keep[2]) | (one & ~keep[2]), (v[g].w & keep[3]) | (one & ~keep[3]));
                 }
                 // both stages of the piece behind one proxy fence
                 const bool two = at * 2 + 1 < steps;
