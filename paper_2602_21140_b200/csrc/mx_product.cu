@@ -270,7 +270,8 @@ __device__ __forceinline__ int segment(const KernelParams &p, int s, int &first)
     return (int)min(c, p.rows - first);
 }
 
-// A segment of c rows is cut into the fewest tiles of at most NT rows, of equal size.
+// A segment of c rows is cut into the fewest tiles of at most NT rows, of equal size (to whole pieces of the
+// epilogue, 32 rows: only a segment's last tile leaves part of one).
 template <int NT>
 __device__ __forceinline__ int row_tiles(int c) { return (c + NT - 1) / NT; }
 
@@ -312,7 +313,7 @@ __device__ __forceinline__ Tile tile_at(const KernelParams &p, const Order &o, i
     else c = segment(p, lo, first);
     const int nt = row_tiles<NT>(c);
     const int f = local / nt, r = local - f * nt;
-    const int size = ((c + nt - 1) / nt + 15) & ~15;
+    const int size = ((c + nt - 1) / nt + 31) & ~31;
     t.slot = lo; t.feat = f * (CG * kFeat);
     t.row = first + r * size;
     t.rows = min(size, c - r * size);                // may be <= 0 for the last tile of an uneven cut
@@ -455,9 +456,16 @@ __device__ __forceinline__ void store_plain(const KernelParams &p, const CUtenso
         }
     } else {
         const int tid = quarter * 32 + lane, piece = tid & 15, f = t.feat + piece * 8;
-        for (int r = tid >> 4; r < left; r += 8) {
-            const uint4 o = *reinterpret_cast<const uint4 *>(buf + (piece >> 3) * 4096 + r * 128 + (((piece & 7) ^ (r & 7)) << 4));
-            if (f < p.N) *reinterpret_cast<uint4 *>(p.y + (size_t)(t.row + c0 + r) * p.N + f) = o;
+        uint4 o[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int r = (tid >> 4) + 8 * i;
+            o[i] = *reinterpret_cast<const uint4 *>(buf + (piece >> 3) * 4096 + r * 128 + (((piece & 7) ^ (r & 7)) << 4));
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int r = (tid >> 4) + 8 * i;
+            if (r < left && f < p.N) *reinterpret_cast<uint4 *>(p.y + (size_t)(t.row + c0 + r) * p.N + f) = o[i];
         }
     }
 }
