@@ -320,10 +320,10 @@ __device__ __forceinline__ Tile tile_at(const KernelParams &p, const Order &o, i
     return t;
 }
 
-// Shared memory of the epilogue, per group of warps: two boxes of bf16 rows (store_plain) or two planes of fp32
-// (store_gated); twice, used in turn behind one barrier each, where many rows make the epilogue as long as the
+// Shared memory of the epilogue: a box of bf16 rows per pair of warps (store_plain) or two planes of fp32 per group of four
+// (store_gated); twice, used in turn, where many rows make the epilogue as long as the
 // products.
-constexpr int kPlane = 32 * 32 + 8, kPlaneBytes = (2 * kPlane * 4 + 127) / 128 * 128, kBoxBytes = 2 * 4096;
+constexpr int kPlane = 32 * 32 + 8, kPlaneBytes = (2 * kPlane * 4 + 127) / 128 * 128, kBoxBytes = 4096;
 
 // The tiles of a CTA (or pair of CTAs) of a grid of `step`, first, first + step, ..., as a warp sees them.  Finding a tile is a chain of
 // dependent reads, so the lanes find the next 32 of them side by side and hand them out one by one.
@@ -384,7 +384,7 @@ struct Layout {
     static constexpr int kStageOff = 0;
     static constexpr int kSfOff = STAGES * kStage;
     static constexpr int kEpiOff = kSfOff + STAGES * kSf;
-    static constexpr int kEpiBufs = NT > 64 ? 2 : 1, kEpiBuf = GATED ? kPlaneBytes : kBoxBytes;
+    static constexpr int kEpiBufs = NT > 64 ? 2 : 1, kEpiBuf = GATED ? kPlaneBytes : 2 * kBoxBytes;
     static constexpr int kEpiBytes = 2 * kEpiBufs * kEpiBuf;
     static constexpr int kBarOff = kEpiOff + kEpiBytes;
     static constexpr int kBars = 2 * STAGES + 5;
@@ -404,28 +404,32 @@ __device__ __forceinline__ bool wait_for(uint64_t *bar, unsigned parity, volatil
 
 // ---------------------------------------------------------------------- epilogue
 
-// Verdict of the four warps of an epilogue group: true if it is true for all of them.
-__device__ __forceinline__ bool group_all(int group, bool ok)
+// Verdict of the warps that share a barrier: true if it is true for all of them.
+__device__ __forceinline__ bool warps_all(int barrier, int threads, bool ok)
 {
     uint32_t r;
-    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.and.pred q, %2, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
-                 : "=r"(r) : "r"((uint32_t)ok), "r"(group + 1) : "memory");
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.and.pred q, %2, %3, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                 : "=r"(r) : "r"((uint32_t)ok), "r"(barrier), "r"(threads) : "memory");
     return r != 0;
 }
 
 __device__ __forceinline__ void group_sync(int group) { asm volatile("barrier.cta.sync %0, 128;" ::"r"(group + 1) : "memory"); }
 
-// 128 features (four warps) x 32 rows of the accumulator as bf16 rows, through 8 KB of shared memory of this
-// group: two boxes of [32 rows][64 features], 128-byte swizzle.  The accumulator is read in the fragment layout
-// (lane / 4 = feature, two neighbouring rows per register pair), so that a pair is one bf16x2 and stmatrix writes
-// it transposed.  32 rows that all belong to the segment leave as two TMA stores, which cost the warps nothing;
-// the last rows of a segment leave as 16-byte stores, so that the rows behind it stay as they are.  (Every load or
-// store instruction of these warps has to queue for the shared memory that the products keep busy: with their own
-// stores of 64-byte pieces they were the limit of products with short K.)  The fp32 sum is rounded once.
+// 64 features (two warps) x 32 rows of the accumulator as bf16 rows, through 4 KB of shared memory: a box of
+// [32 rows][64 features], 128-byte swizzle.  The accumulator is read in the fragment layout (lane / 4 = feature, two
+// neighbouring rows per register pair), so that a pair is one bf16x2 and stmatrix writes it transposed.  32 rows
+// that all belong to the segment leave as a TMA store, which costs the warps nothing; the last rows of a segment leave
+// as 16-byte stores, so that the rows behind it stay as they are.  (Every load or store of these warps has to queue
+// for the shared memory that the products keep busy, and warps that wait for one another wait for the slowest: boxes
+// of four warps were 10 % slower with short K.  Boxes of one warp, 64 bytes to a row, cost 8 % in L2 with long rows.)
+// The fp32 sum is rounded once.
+__device__ __forceinline__ void pair_sync(int pair) { asm volatile("barrier.cta.sync %0, 64;" ::"r"(pair + 1) : "memory"); }
+
+template <int BUFS>
 __device__ __forceinline__ void store_plain(const KernelParams &p, const CUtensorMap *map_y, const Tile &t, int c0, const uint32_t (&v)[32],
-                                            unsigned char *buf, int group, int quarter, int lane)
+                                            unsigned char *buf, int pair, int half, int lane)
 {
-    const uint32_t base = smem_addr(buf) + (quarter >> 1) * 4096;
+    const uint32_t base = smem_addr(buf);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         uint32_t m[4];
@@ -435,38 +439,40 @@ __device__ __forceinline__ void store_plain(const KernelParams &p, const CUtenso
             const __nv_bfloat162 h = __floats2bfloat162_rn(__uint_as_float(v[at]), __uint_as_float(v[at + 1]));
             m[q] = *reinterpret_cast<const uint32_t *>(&h);
         }
-        const int r = 8 * i + (lane & 7), piece = (quarter & 1) * 4 + (lane >> 3);   // this lane's row and 16-byte piece
+        const int r = 8 * i + (lane & 7), piece = half * 4 + (lane >> 3);   // this lane's row and 16-byte piece
         asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(base + r * 128 + ((piece ^ (r & 7)) << 4)),
                      "r"(m[0]), "r"(m[1]), "r"(m[2]), "r"(m[3])
                      : "memory");
     }
     fence_async_shared();
-    const bool leader = quarter == 0 && lane == 0;
-    if (leader) bulk_wait_read<0>();                           // the other buffer's stores have left it
-    group_sync(group);
-    const int left = t.rows - c0;
+    const bool leader = half == 0 && lane == 0;
+    if (leader && BUFS == 2) bulk_wait_read<0>();              // the other buffer's store has left it
+    pair_sync(pair);
+    const int left = t.rows - c0, f = t.feat + (pair & 1) * 64;
     if (left >= 32) {
-        if (leader) {
-            for (int h = 0; h < 2; ++h)
-                if (t.feat + 64 * h < p.N)
-                    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map_y),
-                                 "r"(t.feat + 64 * h), "r"(t.row + c0), "r"(smem_addr(buf) + 4096 * h)
-                                 : "memory");
+        if (leader && f < p.N) {
+            asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map_y), "r"(f),
+                         "r"(t.row + c0), "r"(base)
+                         : "memory");
             bulk_commit();
         }
     } else {
-        const int tid = quarter * 32 + lane, piece = tid & 15, f = t.feat + piece * 8;
+        const int tid = half * 32 + lane, piece = tid & 7;
         uint4 o[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int r = (tid >> 4) + 8 * i;
-            o[i] = *reinterpret_cast<const uint4 *>(buf + (piece >> 3) * 4096 + r * 128 + (((piece & 7) ^ (r & 7)) << 4));
+            const int r = (tid >> 3) + 8 * i;
+            o[i] = *reinterpret_cast<const uint4 *>(buf + r * 128 + ((piece ^ (r & 7)) << 4));
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int r = (tid >> 4) + 8 * i;
-            if (r < left && f < p.N) *reinterpret_cast<uint4 *>(p.y + (size_t)(t.row + c0 + r) * p.N + f) = o[i];
+            const int r = (tid >> 3) + 8 * i;
+            if (r < left && f + piece * 8 < p.N) *reinterpret_cast<uint4 *>(p.y + (size_t)(t.row + c0 + r) * p.N + f + piece * 8) = o[i];
         }
+    }
+    if (BUFS == 1) {                                           // one buffer: free before the next 32 rows are written
+        if (leader) bulk_wait_read<0>();
+        pair_sync(pair);
     }
 }
 
@@ -839,7 +845,7 @@ k_mx_product(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
         Tile t;
         for (TileStream<NT, CG> stream(p, order, tiles); stream.next(t);) {
             bool ok = wait_for(&acc_full[buf], acc_parity, quit, p.spin_limit);
-            ok = group_all(group, ok);                          // the group's warps meet at barriers below
+            ok = GATED ? warps_all(group + 1, 128, ok) : warps_all((warp >> 1) + 1, 64, ok);   // they meet at barriers below
             if (!ok) break;
             tc_fence_after();
             const uint32_t acc = tmem + buf * NT + ((uint32_t)(quarter * 32) << 16);
@@ -854,21 +860,17 @@ k_mx_product(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
                     __syncwarp();
                     if (lane == 0) mbar_arrive_lead<CG>(&acc_empty[buf]);
                 }
-                unsigned char *epi_buf = epi + (group * L::kEpiBufs + epi_turn) * L::kEpiBuf;
+                unsigned char *epi_buf = epi + (group * L::kEpiBufs + epi_turn) * L::kEpiBuf;   // of the group
                 if (GATED) store_gated(p, t, c0, v, reinterpret_cast<float *>(epi_buf), group, quarter, lane);
-                else store_plain(p, &map_y, t, c0, v, epi_buf, group, quarter, lane);
-                if (L::kEpiBufs == 2) {
-                    epi_turn ^= 1;
-                } else {                                        // one buffer: free before the next 32 rows are written
-                    if (!GATED && quarter == 0 && lane == 0) bulk_wait_read<0>();
-                    group_sync(group);
-                }
+                else store_plain<L::kEpiBufs>(p, &map_y, t, c0, v, epi_buf + (quarter >> 1) * kBoxBytes, warp >> 1, quarter & 1, lane);
+                if (L::kEpiBufs == 2) epi_turn ^= 1;
+                else if (GATED) group_sync(group);              // one set of planes: free before the next 32 rows are written
             }
             if (group * 32 >= t.rows && lane == 0) mbar_arrive_lead<CG>(&acc_empty[buf]);
             buf ^= 1;
             if (buf == 0) acc_parity ^= 1u;
         }
-        if (!GATED && quarter == 0 && lane == 0) bulk_wait_all();   // the last stores have left shared memory
+        if (!GATED && (quarter & 1) == 0 && lane == 0) bulk_wait_all();   // the last stores have left shared memory
     }
 
     __syncwarp();
@@ -902,12 +904,12 @@ EncodeTiled encode_fn()
     return fn;
 }
 
-bool encode(CUtensorMap *map, CUtensorMapDataType type, const void *ptr, int rank, const cuuint64_t *dims, const cuuint64_t *strides,
-            int box_cols, int box_rows)
+bool encode(CUtensorMap *map, CUtensorMapDataType type, CUtensorMapSwizzle swizzle, const void *ptr, int rank, const cuuint64_t *dims,
+            const cuuint64_t *strides, int box_cols, int box_rows)
 {
     const cuuint32_t box[3] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows, 1u}, one[3] = {1u, 1u, 1u};
     return encode_fn()(map, type, rank, const_cast<void *>(ptr), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                       CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+                       swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 template <int NT, int STAGES, int CG, bool GATED>
@@ -929,11 +931,12 @@ cudaError_t launch(const MxProductArgs &a, cudaStream_t st)
     const cuuint64_t wd[3] = {row, (cuuint64_t)a.N, (cuuint64_t)a.P}, ws[2] = {row, row * (cuuint64_t)a.N};
     const cuuint64_t ad[2] = {row, (cuuint64_t)a.rows}, as[1] = {row};
     const CUtensorMapDataType u8 = CU_TENSOR_MAP_DATA_TYPE_UINT8;
-    bool ok = encode(&map_w, u8, a.w_codes, 3, wd, ws, kRowBytes, kFeat) && encode(&map_a, u8, a.a_codes, 2, ad, as, kRowBytes, 32) &&
-              encode(&map_big, u8, a.a_codes, 2, ad, as, kRowBytes, NT / CG);
+    const CUtensorMapSwizzle sw = CU_TENSOR_MAP_SWIZZLE_128B;
+    bool ok = encode(&map_w, u8, sw, a.w_codes, 3, wd, ws, kRowBytes, kFeat) && encode(&map_a, u8, sw, a.a_codes, 2, ad, as, kRowBytes, 32) &&
+              encode(&map_big, u8, sw, a.a_codes, 2, ad, as, kRowBytes, NT / CG);
     if (!GATED) {
         const cuuint64_t yd[2] = {(cuuint64_t)a.N, (cuuint64_t)a.rows}, ys[1] = {2 * (cuuint64_t)a.N};
-        ok = ok && encode(&map_y, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, a.y, 2, yd, ys, 64, 32);
+        ok = ok && encode(&map_y, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, sw, a.y, 2, yd, ys, 64, 32);
     }
     if (!ok) return cudaErrorInvalidValue;
     KernelParams p;
