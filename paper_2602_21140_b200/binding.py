@@ -686,7 +686,7 @@ class MoeRouter:
         out, rows = self.mx_dispatch(logits, x, out)
         buf = self.mx_expert_ffn(rows, out.slot_counts, out.slot_offsets, gate_up, down)
         _require(buf.shape[1] == self.cfg.hidden, "mx_step")
-        return self.combine(buf, x.shape[0], y)
+        return _on_device(self._index(), self.combine, buf, x.shape[0], y)
 
     # -- gradients of the routed step ----------------------------------------
     def combine_backward(self, expert_buf: torch.Tensor, dy: torch.Tensor, d_expert_buf: torch.Tensor | None = None,

@@ -464,13 +464,16 @@ bool alloc_scan_scratch(moe_ctx *ctx, cudaStream_t st)
 }
 
 // The kernels with rings in dynamic shared memory may use all of it.  The attribute belongs to
-// the function, not to a context, so it is set once per process to the largest size any
-// context can ask for.
-bool set_kernel_attributes_once()
+// the function, not to a context, so it is set once per process and device to the largest
+// size any context can ask for.
+bool set_kernel_attributes_once(int device)
 {
-    static std::once_flag once;
-    static bool ok = false;
-    std::call_once(once, [] {
+    constexpr int kDevices = 64;
+    static std::once_flag once[kDevices];
+    static bool done[kDevices];
+    if (device < 0 || device >= kDevices) return false;
+    bool &ok = done[device];
+    std::call_once(once[device], [&ok] {
         const cudaFuncAttribute at = cudaFuncAttributeMaxDynamicSharedMemorySize;
         const int sm = (int)(kMaxSmem - 1024);
         ok = cudaFuncSetAttribute(k_scatter_bulk, at, sm) == cudaSuccess
@@ -614,7 +617,8 @@ MxProductArgs product_args(const moe_ctx *ctx, const uint8_t *a_codes, const uin
     a.a_codes = a_codes; a.a_scales = a_scales; a.rows = rows;
     a.slot_counts = slot_counts; a.slot_offsets = slot_offsets; a.P = ctx->d.P;
     a.w_codes = w_codes; a.w_scales = w_scales; a.N = n_out; a.K = n_in;
-    a.ctl = ctx->d_ctl; a.spin_limit = ctx->spin_limit; a.sm_count = ctx->sm_count; a.pdl = ctx->pdl;
+    a.ctl = ctx->d_ctl; a.spin_limit = ctx->spin_limit; a.sm_count = ctx->sm_count; a.device = ctx->device;
+    a.pdl = ctx->pdl;
     return a;
 }
 
@@ -761,7 +765,7 @@ moe_status moe_route_init(const moe_config *cfg, const int32_t *slot_to_expert, 
              enqueue_derive(ctx, st) == MOE_OK &&
              cudaStreamSynchronize(st) == cudaSuccess;
     }
-    ok = ok && set_kernel_attributes_once();
+    ok = ok && set_kernel_attributes_once(ctx->device);
     if (ok) configure_launch(ctx);
     if (!ok) {
         cudaGetLastError();

@@ -10,10 +10,10 @@
 //
 // One persistent CTA per SM:
 //   warps 0-7   epilogue, two groups of four (a warp reads one quarter of the TMEM lanes): TMEM -> registers ->
-//               shared memory (transposed) -> HBM, 32 rows at a time, the groups taking turns
+//               shared memory -> HBM, 32 rows at a time, the groups taking turns
 //   warp 8      TMA loads of the code tiles (weights 128 x 128 B, rows n x 128 B, 128-byte swizzle)
 //   warp 9      scales shared -> TMEM (tcgen05.cp) and the MMAs, from one thread
-//   warps 10-   scales, a warp per 128 rows: HBM -> registers -> the 32 x 16-byte blocks tcgen05.cp wants
+//   warps 10-   scales, two warps per 128 rows: HBM -> registers -> the 32 x 16-byte blocks tcgen05.cp wants
 // The accumulator is double buffered, so the epilogue of a tile runs under the products of the next.
 //
 // Tiles are dealt feature tile by feature tile of a slot, row tile innermost: CTAs that work at the same time
@@ -320,13 +320,12 @@ __device__ __forceinline__ Tile tile_at(const KernelParams &p, const Order &o, i
     return t;
 }
 
-// Shared memory of the epilogue: a box of bf16 rows per pair of warps (store_plain) or two planes of fp32 per group of four
-// (store_gated); twice, used in turn, where many rows make the epilogue as long as the
-// products.
+// Shared memory of the epilogue: a box of bf16 rows per pair of warps (store_plain) or two planes of fp32 per group
+// of four (store_gated); twice, used in turn, where many rows make the epilogue as long as the products.
 constexpr int kPlane = 32 * 32 + 8, kPlaneBytes = (2 * kPlane * 4 + 127) / 128 * 128, kBoxBytes = 4096;
 
-// The tiles of a CTA (or pair of CTAs) of a grid of `step`, first, first + step, ..., as a warp sees them.  Finding a tile is a chain of
-// dependent reads, so the lanes find the next 32 of them side by side and hand them out one by one.
+// The tiles of a CTA (or pair of CTAs) of a grid of `step`, first, first + step, ..., as a warp sees them.  Finding a
+// tile is a chain of dependent reads, so the lanes find the next 32 of them side by side and hand them out one by one.
 template <int NT, int CG>
 struct TileStream {
     const KernelParams &p;
@@ -415,6 +414,8 @@ __device__ __forceinline__ bool warps_all(int barrier, int threads, bool ok)
 
 __device__ __forceinline__ void group_sync(int group) { asm volatile("barrier.cta.sync %0, 128;" ::"r"(group + 1) : "memory"); }
 
+__device__ __forceinline__ void pair_sync(int pair) { asm volatile("barrier.cta.sync %0, 64;" ::"r"(pair + 1) : "memory"); }
+
 // 64 features (two warps) x 32 rows of the accumulator as bf16 rows, through 4 KB of shared memory: a box of
 // [32 rows][64 features], 128-byte swizzle.  The accumulator is read in the fragment layout (lane / 4 = feature, two
 // neighbouring rows per register pair), so that a pair is one bf16x2 and stmatrix writes it transposed.  32 rows
@@ -423,8 +424,6 @@ __device__ __forceinline__ void group_sync(int group) { asm volatile("barrier.ct
 // for the shared memory that the products keep busy, and warps that wait for one another wait for the slowest: boxes
 // of four warps were 10 % slower with short K.  Boxes of one warp, 64 bytes to a row, cost 8 % in L2 with long rows.)
 // The fp32 sum is rounded once.
-__device__ __forceinline__ void pair_sync(int pair) { asm volatile("barrier.cta.sync %0, 64;" ::"r"(pair + 1) : "memory"); }
-
 template <int BUFS>
 __device__ __forceinline__ void store_plain(const KernelParams &p, const CUtensorMap *map_y, const Tile &t, int c0, const uint32_t (&v)[32],
                                             unsigned char *buf, int pair, int half, int lane)
@@ -476,13 +475,6 @@ __device__ __forceinline__ void store_plain(const KernelParams &p, const CUtenso
     }
 }
 
-// SwiGLU and quantisation of 128 weight rows (64 pairs of a gate and its up-projection, in even and odd
-// lanes) x 32 rows.  Neighbouring lanes trade one value so that an even lane holds both halves of its
-// pair for the even row of two and an odd lane for the odd one; the 64 results of a row then go through
-// shared memory, two planes (blocks of 32 features) of [32 rows][32] with the halves of odd rows swapped
-// (no two lanes of a store meet in a bank), where each half block is taken by one thread and the block's
-// largest magnitude by one shuffle.  Everything before the one rounding to 4 bits is fp32; exp and the
-// reciprocal are the hardware's approximations (2 and 1 units in the last place), far below a 4-bit step.
 __device__ __forceinline__ float silu(float g)
 {
     float r;
@@ -490,6 +482,13 @@ __device__ __forceinline__ float silu(float g)
     return g * r;
 }
 
+// SwiGLU and quantisation of 128 weight rows (64 pairs of a gate and its up-projection, in even and odd
+// lanes) x 32 rows.  Neighbouring lanes trade one value so that an even lane holds both halves of its
+// pair for the even row of two and an odd lane for the odd one; the 64 results of a row then go through
+// shared memory, two planes (blocks of 32 features) of [32 rows][32] with the halves of odd rows swapped
+// (no two lanes of a store meet in a bank), where each half block is taken by one thread and the block's
+// largest magnitude by one shuffle.  Everything before the one rounding to 4 bits is fp32; exp and the
+// reciprocal are the hardware's approximations (2 and 1 units in the last place), far below a 4-bit step.
 __device__ __forceinline__ void store_gated(const KernelParams &p, const Tile &t, int c0, const uint32_t (&v)[32], float *buf,
                                             int group, int quarter, int lane)
 {
@@ -735,10 +734,6 @@ k_mx_product(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
         __syncwarp();
         unsigned spins = 0;
         while (!mbar_try_wait(drained, 0) && ++spins < p.spin_limit) {}
-    } else if (warp == kMmaWarp) {
-        // the second CTA of a pair: stay until the last arrival from the first has come in
-        unsigned spins = 0;
-        while (!mbar_try_wait(drained, 0) && ++spins < p.spin_limit) __nanosleep(256);
     } else if (warp >= kScaleWarp) {
         // Two warps per 128-row block of scales (the weight rows, then the data rows), which take the pieces of
         // 16 bytes a row (K = 512, two stages) in turn, each reading kPieces of its own ahead.  Lane l owns rows
@@ -879,6 +874,11 @@ k_mx_product(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
     else __syncthreads();
     if (tid == 0 && *quit) report_status(p.ctl, kDevTimeout);
     if (warp == kMmaWarp) {
+        if (CG == 2 && rank == 1) {                            // the first CTA's last arrival is on its way here as well
+            unsigned spins = 0;
+            while (!mbar_try_wait(drained, 0) && ++spins < p.spin_limit) {}
+            __syncwarp();
+        }
         tc_fence_after();
         tmem_dealloc<CG>(tmem, 512);
     }
@@ -919,12 +919,16 @@ cudaError_t launch(const MxProductArgs &a, cudaStream_t st)
     static_assert(L::kEndsOff + 1024 + kMaxP * 4 <= 227 * 1024, "shared memory");
     static_assert(NT >= 32 && NT % 32 == 0, "row boxes and epilogue chunks are 32 rows");
     const auto kernel = k_mx_product<NT, STAGES, CG, GATED>;
-    static std::once_flag once;
-    static cudaError_t attr = cudaSuccess;
-    std::call_once(once, [&] {
-        attr = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)std::max(L::bytes(kMaxP), L::bytes(kFullTableP)));
+    // a function's attributes are those of one device
+    constexpr int kDevices = 64;
+    static std::once_flag once[kDevices];
+    static cudaError_t attr[kDevices];
+    if (a.device < 0 || a.device >= kDevices) return cudaErrorInvalidDevice;
+    std::call_once(once[a.device], [&] {
+        attr[a.device] = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                              (int)std::max(L::bytes(kMaxP), L::bytes(kFullTableP)));
     });
-    if (attr != cudaSuccess) return attr;
+    if (attr[a.device] != cudaSuccess) return attr[a.device];
     if (!encode_fn()) return cudaErrorNotSupported;
     CUtensorMap map_w, map_a, map_big, map_y = {};
     const cuuint64_t row = (cuuint64_t)a.K / 2;

@@ -22,6 +22,7 @@ struct MxProductArgs {
     Control *ctl;
     unsigned spin_limit;
     int sm_count;
+    int device;                          // the current one
     bool pdl;
 };
 

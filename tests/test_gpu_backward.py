@@ -86,6 +86,45 @@ def test_dispatch_backward(name, T, H, route_scale):
     router.close()
 
 
+@pytest.mark.parametrize("E,k,H,T", [(16, 1, 40, 70), (24, 3, 8200, 9), (64, 6, 2048, 333), (32, 16, 264, 41), (8, 8, 64, 5)])
+def test_any_number_of_experts_per_token(E, k, H, T):
+    """The kernels that are not built for one k, one token with every expert, rows of more than one ring slot; on a
+    stream of its own."""
+    cfg = B.make_config(E, k, H, T, E, 1, 1, B.MOE_SCORE_SIGMOID, route_scale=1.5)
+    scale = np.linspace(0.5, 1.5, E).astype(np.float32)
+    router = B.MoeRouter(cfg, range(E), np.zeros(E, np.float32), scale)
+    g = torch.Generator(device="cuda").manual_seed(E)
+    logits = torch.randn(T, E, device="cuda", generator=g)
+    x, dy = (torch.randn(T, H, device="cuda", generator=g).bfloat16() for _ in range(2))
+    buf, d_send = (torch.randn(T * k, H, device="cuda", generator=g).bfloat16() for _ in range(2))
+    d_w = torch.randn(T, k, device="cuda", generator=g)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        out = router.dispatch(logits, x)
+        d_buf, got_w = router.combine_backward(buf, dy)
+        dx, d_logits = router.dispatch_backward(logits, d_send, d_w)
+    side.synchronize()
+    assert router.device_status() == 0
+    dst, ids = out.dst_row.long().view(T, k), out.topk_ids.long()
+    sc = torch.from_numpy(scale).cuda().double()[out.topk_slot.long()]
+    prod = buf.double()[dst] * dy.double()[:, None]
+    assert ((got_w.double() - sc * prod.sum(-1)).abs() <= (H / 256 + 34) * 2.0 ** -24 * sc * prod.abs().sum(-1)).all()
+    want = torch.empty(T * k, H, dtype=torch.float64, device="cuda")
+    want[dst.flatten()] = ((out.topk_weights.double() * sc)[..., None] * dy.double()[:, None]).flatten(0, 1)
+    assert ((d_buf.double() - want).abs() <= 2.0 ** -8 * want.abs()).all()
+    rows = d_send.double()[dst]
+    assert ((dx.double() - rows.sum(1)).abs() <= 2.0 ** -8 * rows.sum(1).abs() + k * 2.0 ** -24 * rows.abs().sum(1)).all()
+    leaf = logits.double().requires_grad_()
+    w = _weights(leaf, ids, True, 1.5)
+    (w * d_w.double()).sum().backward()
+    wm, gm = w.detach(), d_w.double().abs()
+    tol = torch.zeros(T, E, dtype=torch.float64, device="cuda").scatter_(
+        1, ids, wm * (gm + (wm * gm).sum(1, keepdim=True) / 1.5) * (16 * k * 2.0 ** -24 + 3e-7))
+    assert ((d_logits.double() - leaf.grad).abs() <= tol).all()
+    router.close()
+
+
 def test_formula_against_differences():
     """d loss / d logits and d x by central differences of the forward formula in 64 bits (T, E small)."""
     for name in ("tiny", "dsv3"):

@@ -174,3 +174,32 @@ def test_two_graphs_and_two_streams():
     for router, _, _, y, want, _ in made:
         assert torch.equal(y, want) and router.device_status() == 0
         router.close()
+
+
+def test_two_graphs_of_one_context():
+    """Two layers' steps captured from one context, of different lengths, replayed in turn on one stream."""
+    wl = W.WORKLOADS["tiny"]
+    H, I = 256, 64
+    inp = W.make_inputs(wl, T=128, H=H)
+    router = make_router(wl, inp, max_tokens=128, hidden=H)
+    (gate_up, _), (down, _) = _layer(wl, inp, 128, H, I, 5)
+    made = []
+    s = torch.cuda.Stream()
+    for T in (128, 37):
+        logits, x = to_dev(inp["logits"][:T]), to_dev(inp["x"][:T], torch.bfloat16)
+        want = router.mx_step(logits, x, gate_up, down).clone()
+        y, out = torch.zeros_like(want), router.alloc_outputs(T, send_buf=False)
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=s):
+            router.mx_step(logits, x, gate_up, down, out, y)
+        made.append((g, y, want, logits, x, out))
+    for _ in range(5):
+        for g, *_ in made:
+            g.replay()
+        torch.cuda.synchronize()
+        for _, y, want, *_ in made:
+            assert torch.equal(y, want)
+            y.zero_()
+    assert router.device_status() == 0
+    router.close()
