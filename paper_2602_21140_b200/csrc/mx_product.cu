@@ -567,6 +567,8 @@ k_mx_product(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
         asm volatile("prefetch.tensormap [%0];" ::"l"(&map_big));
         if (!GATED) asm volatile("prefetch.tensormap [%0];" ::"l"(&map_y));
     }
+    // hints while the previous kernel drains: its weights have pushed these out of L2 (a hint returns nothing stale)
+    if (tid * 32 < p.P) { prefetch_l2(p.slot_counts + tid * 32); prefetch_l2(p.slot_offsets + tid * 32); }
     if (warp == kMmaWarp) tmem_alloc<CG>(tmem_slot, 512);
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
