@@ -477,8 +477,9 @@ __device__ __forceinline__ void store_plain(const KernelParams &p, const CUtenso
 
 __device__ __forceinline__ float silu(float g)
 {
-    float r;
-    asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(1.0f + __expf(-g)));
+    float e, r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(g * -1.44269504f));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + e));
     return g * r;
 }
 
