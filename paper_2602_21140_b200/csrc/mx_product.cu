@@ -100,18 +100,6 @@ __device__ __forceinline__ void cp_scales(uint32_t tmem, uint64_t desc)
     else asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
 }
 
-__device__ __forceinline__ void tmem_ld32(uint32_t addr, uint32_t (&r)[32])
-{
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
-          "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
-          "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-        : "r"(addr));
-}
-
 // 32 lanes x 32 columns as two halves of 16 lanes in the fragment layout: v[16 h + 4 i + 2 j + e] is lane
 // 16 h + 8 j + (thread / 4), column 8 i + 2 (thread % 4) + e
 __device__ __forceinline__ void tmem_ld_fragments(uint32_t addr, uint32_t (&r)[32])
@@ -209,6 +197,24 @@ __device__ __forceinline__ void tma_3d(void *dst, const CUtensorMap *map, int x,
             "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(
                 smem_addr(dst)),
             "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
+            : "memory");
+}
+
+// weight rows in the order of weight_row: sixteens of {8 even, 8 odd} rows
+template <int CG>
+__device__ __forceinline__ void tma_pairs(void *dst, const CUtensorMap *map, int x, int sixteen, int slot, uint32_t bar)
+{
+    if (CG == 1)
+        asm volatile(
+            "cp.async.bulk.tensor.5d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %5, %5, %3, %4}], [%6];" ::"r"(
+                smem_addr(dst)),
+            "l"(map), "r"(x), "r"(sixteen), "r"(slot), "r"(0), "r"(bar)
+            : "memory");
+    else
+        asm volatile(
+            "cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %5, %5, %3, %4}], [%6];" ::"r"(
+                smem_addr(dst)),
+            "l"(map), "r"(x), "r"(sixteen), "r"(slot), "r"(0), "r"(bar)
             : "memory");
 }
 
@@ -372,6 +378,10 @@ __device__ __forceinline__ bool next_uniform(TileStream<NT, CG> &stream, Tile &t
     return true;
 }
 
+// Row of a gated tile's weights that lies at place r: of each sixteen first the even rows (gates), then the odd ones
+// (up-projections)
+__device__ __forceinline__ int weight_row(int r) { return (r & ~15) + 2 * (r & 7) + ((r >> 3) & 1); }
+
 template <int NT, int STAGES, int CG, bool GATED>
 struct Layout {
     static constexpr int kBTile = (NT / CG + 31) / 32 * 32 * kRowBytes;   // this CTA's rows, in boxes of 32
@@ -477,38 +487,49 @@ __device__ __forceinline__ void store_plain(const KernelParams &p, const CUtenso
 
 __device__ __forceinline__ float silu(float g)
 {
+    // both flush to zero: below g = -87 the result is 0 where the formula leaves less than 88 * 2^-126
     float e, r;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(g * -1.44269504f));
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + e));
     return g * r;
 }
 
-// SwiGLU and quantisation of 128 weight rows (64 pairs of a gate and its up-projection, in even and odd
-// lanes) x 32 rows.  Neighbouring lanes trade one value so that an even lane holds both halves of its
-// pair for the even row of two and an odd lane for the odd one; the 64 results of a row then go through
-// shared memory, two planes (blocks of 32 features) of [32 rows][32] with the halves of odd rows swapped
-// (no two lanes of a store meet in a bank), where each half block is taken by one thread and the block's
-// largest magnitude by one shuffle.  Everything before the one rounding to 4 bits is fp32; exp and the
-// reciprocal are the hardware's approximations (2 and 1 units in the last place), far below a 4-bit step.
+// SwiGLU and quantisation of 128 weight rows (64 pairs of a gate and its up-projection) x 32 rows.  The weight rows of
+// a sixteen lie in the order of weight_row, so that the fragment layout gives a thread both halves of its pairs: of
+// feature lane / 4 (and 8 more) for the rows 8 j + 2 (lane % 4) and one more.  The 64 results of a row then go through
+// shared memory, two planes (blocks of 32 features) of [32 rows][32], where each half block is taken by one thread and
+// the block's largest magnitude by one shuffle.  In a plane the eights of a row are swapped by row / 2 % 4 and their
+// fours by row % 2: no two lanes of a store or of a load of 16 bytes meet in a bank.  (Weight rows in their own
+// order, pairs in neighbouring lanes that trade a value by shuffle: 73.4 us instead of 71.4 for 4096 rows over 8 experts
+// of 4096 x 4096, 711 instead of 706 for 65536 over 16 of 7168 x 2048.)  Everything before the one rounding to 4 bits
+// is fp32; exp and the reciprocal are the hardware's approximations (2 and 1 units in the last place), far below a
+// 4-bit step.
 __device__ __forceinline__ void store_gated(const KernelParams &p, const Tile &t, int c0, const uint32_t (&v)[32], float *buf,
                                             int group, int quarter, int lane)
 {
-    const bool odd = lane & 1;
-    float *w = buf + (quarter >> 1) * kPlane + ((((quarter & 1) ^ (odd ? 1 : 0)) << 4) | (lane >> 1)) + (odd ? 32 : 0);
+    float *w = buf + (quarter >> 1) * kPlane + (lane & 3) * 64;
 #pragma unroll
-    for (int j = 0; j < 16; ++j) {
-        const uint32_t other = __shfl_xor_sync(0xffffffffu, odd ? v[2 * j] : v[2 * j + 1], 1);
-        const float gate = __uint_as_float(odd ? other : v[2 * j]), up = __uint_as_float(odd ? v[2 * j + 1] : other);
-        w[64 * j] = silu(gate) * up;
+    for (int e = 0; e < 2; ++e) {
+        const int eight = (((quarter & 1) * 2 + e) ^ (lane & 3)) * 8;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            float *at = w + i * 32 + eight + ((lane >> 2) ^ (4 * i));
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float gate = __uint_as_float(v[16 * e + 4 * j + i]), up = __uint_as_float(v[16 * e + 4 * j + 2 + i]);
+                at[256 * j] = silu(gate) * up;
+            }
+        }
     }
     group_sync(group);
     const int tid = quarter * 32 + lane, r = tid >> 2, blk = (tid >> 1) & 1, half = tid & 1;
-    const float4 *src = reinterpret_cast<const float4 *>(buf + blk * kPlane + r * 32 + ((half ^ (r & 1)) << 4));
+    const float *src = buf + blk * kPlane + r * 32;
+    const int swap = (half * 16) ^ (((r >> 1) & 3) * 8) ^ ((r & 1) * 4);
     float x[2][8];
     uint32_t a = 0;
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-        const float4 f = src[q];
+        const float4 f = *reinterpret_cast<const float4 *>(src + (swap ^ (4 * q)));
         const float e[4] = {f.x, f.y, f.z, f.w};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -666,7 +687,8 @@ k_mx_product(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
                     // the first CTA's barrier counts the bytes of both
                     if (rank == 0) mbar_expect_tx(&full[s], bytes);
                     const uint32_t bar = lead + s * 8;
-                    tma_3d<CG>(a, &map_w, k * kRowBytes, t.feat + rank * kFeat, t.slot, bar);
+                    if (GATED) tma_pairs<CG>(a, &map_w, k * kRowBytes, (t.feat + rank * kFeat) / 16, t.slot, bar);
+                    else tma_3d<CG>(a, &map_w, k * kRowBytes, t.feat + rank * kFeat, t.slot, bar);
                     if (big) tma_2d<CG>(b, &map_big, k * kRowBytes, t.row + rank * half, bar);
                     else for (int l = 0; l < loads; ++l)
                         tma_2d<CG>(b + l * kBox * kRowBytes, &map_a, k * kRowBytes, t.row + rank * half + l * kBox, bar);
@@ -769,7 +791,8 @@ k_mx_product(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
 #pragma unroll
                     for (int g = 0; g < 4; ++g) {
                         const int r = lane + 32 * g + (blk > 0 ? (blk - 1) * 128 : 0);
-                        if (blk == 0) src[g] = t.feat + r < p.N ? p.w_scales + ((size_t)t.slot * p.N + t.feat + r) * pitch : nullptr;
+                        const int f = t.feat + (GATED ? weight_row(r) : r);
+                        if (blk == 0) src[g] = f < p.N ? p.w_scales + ((size_t)t.slot * p.N + f) * pitch : nullptr;
                         else src[g] = r < t.rows ? p.a_scales + (size_t)(t.row + r) * pitch : nullptr;
                     }
                 }
@@ -850,8 +873,7 @@ k_mx_product(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
             t.feat += rank * kFeat;
             for (int c0 = group * 32; c0 < t.rows; c0 += 64) {
                 uint32_t v[32];
-                if (GATED) tmem_ld32(acc + c0, v);
-                else tmem_ld_fragments(acc + c0, v);
+                tmem_ld_fragments(acc + c0, v);
                 tmem_wait_ld();
                 if (c0 + 64 >= t.rows) {                        // this warp's last look at the accumulator
                     tc_fence_before();
@@ -908,9 +930,9 @@ EncodeTiled encode_fn()
 }
 
 bool encode(CUtensorMap *map, CUtensorMapDataType type, CUtensorMapSwizzle swizzle, const void *ptr, int rank, const cuuint64_t *dims,
-            const cuuint64_t *strides, int box_cols, int box_rows)
+            const cuuint64_t *strides, int box_cols, int box_rows, int box_2 = 1, int box_3 = 1)
 {
-    const cuuint32_t box[3] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows, 1u}, one[3] = {1u, 1u, 1u};
+    const cuuint32_t box[5] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows, (cuuint32_t)box_2, (cuuint32_t)box_3, 1u}, one[5] = {1u, 1u, 1u, 1u, 1u};
     return encode_fn()(map, type, rank, const_cast<void *>(ptr), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
                        swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
@@ -939,8 +961,11 @@ cudaError_t launch(const MxProductArgs &a, cudaStream_t st)
     const cuuint64_t ad[2] = {row, (cuuint64_t)a.rows}, as[1] = {row};
     const CUtensorMapDataType u8 = CU_TENSOR_MAP_DATA_TYPE_UINT8;
     const CUtensorMapSwizzle sw = CU_TENSOR_MAP_SWIZZLE_128B;
-    bool ok = encode(&map_w, u8, sw, a.w_codes, 3, wd, ws, kRowBytes, kFeat) && encode(&map_a, u8, sw, a.a_codes, 2, ad, as, kRowBytes, 32) &&
-              encode(&map_big, u8, sw, a.a_codes, 2, ad, as, kRowBytes, NT / CG);
+    // the order of weight_row: a row's bytes, the eight rows of one parity, the two parities, the sixteens, the slots
+    const cuuint64_t pd[5] = {row, 8, 2, (cuuint64_t)a.N / 16, (cuuint64_t)a.P}, ps[4] = {2 * row, row, 16 * row, row * (cuuint64_t)a.N};
+    bool ok = (GATED ? encode(&map_w, u8, sw, a.w_codes, 5, pd, ps, kRowBytes, 8, 2, kFeat / 16)
+                     : encode(&map_w, u8, sw, a.w_codes, 3, wd, ws, kRowBytes, kFeat)) &&
+              encode(&map_a, u8, sw, a.a_codes, 2, ad, as, kRowBytes, 32) && encode(&map_big, u8, sw, a.a_codes, 2, ad, as, kRowBytes, NT / CG);
     if (!GATED) {
         const cuuint64_t yd[2] = {(cuuint64_t)a.N, (cuuint64_t)a.rows}, ys[1] = {2 * (cuuint64_t)a.N};
         ok = ok && encode(&map_y, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, sw, a.y, 2, yd, ys, 64, 32);
