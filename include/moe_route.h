@@ -378,7 +378,7 @@ moe_status moe_mx_expert_gated(moe_ctx *ctx, const uint8_t *a_codes, const uint8
  * ---- Gradients of the routed step ---------------------------------------------------
  * (No counterpart in the paper.)  For tuning the router and the experts that are left after a
  * failure.  Both use the topk_*, dst_row buffers of the latest moe_dispatch or moe_mx_dispatch on this
- * context, like moe_combine, and the same T; INVALID_ARG otherwise, and after moe_ep_route.  The
+ * context, like moe_combine (the caller keeps them until then), and the same T; INVALID_ARG otherwise, and after moe_ep_route.  The
  * selection itself, the replica pick and the 4-bit rounding have no gradient (the last is passed through).
  *
  * moe_combine_backward — from dy device [T,H] bf16 and the expert_buf [T*k,H] bf16 of the forward:

@@ -535,6 +535,7 @@ class MoeRouter:
         if self.device.type != "cuda":
             raise RuntimeError("MoeRouter needs a CUDA device; there is no CPU path")
         self._ctx = None
+        self._latest = None      # what the context still points at: see _keep
         with torch.cuda.device(self.device):
             st, ctx = moe_route_init(cfg, slot_to_expert, bias, slot_scale, self._stream())
         if st != MOE_OK:
@@ -544,6 +545,12 @@ class MoeRouter:
     # -- helpers ----------------------------------------------------------
     def _stream(self) -> int:
         return torch.cuda.current_stream(self.device).cuda_stream
+
+    def _keep(self, out: DispatchBuffers, status: int) -> None:
+        """Hold the buffers that a later combine or gradient of this dispatch reads: the context has their addresses,
+        and the caller may drop ``out`` (mx_step returns y alone).  A call that was refused changed nothing."""
+        if status not in (MOE_ERR_INVALID_ARG, MOE_ERR_CAPACITY):
+            self._latest = (out.topk_ids, out.topk_weights, out.topk_slot, out.dst_row)
 
     @property
     def num_slots(self) -> int:
@@ -595,6 +602,7 @@ class MoeRouter:
             out = self.alloc_outputs(T)
         struct = out.as_struct()
         st = moe_dispatch(self._ctx, logits.data_ptr(), x.data_ptr(), T, struct, self._stream())
+        self._keep(out, st)
         if st != MOE_OK:
             raise MoeError(st, "moe_dispatch")
         return out
@@ -628,6 +636,7 @@ class MoeRouter:
             _require(_is_mx(rows, dev, (T * c.top_k,)) and rows.cols == H, "mx_dispatch")
         st = moe_mx_dispatch(self._ctx, logits.data_ptr(), x.data_ptr(), T, out.as_struct(), rows.codes.data_ptr(),
                              rows.scales.data_ptr(), _raw_stream(dev))
+        self._keep(out, st)
         if st != MOE_OK:
             raise MoeError(st, "moe_mx_dispatch")
         return out, rows
@@ -746,6 +755,7 @@ class MoeRouter:
         T = logits.shape[0]
         assert logits.dtype == torch.float32 and logits.is_contiguous() and logits.shape[1] == self.cfg.num_experts
         st = moe_ep_route(self._ctx, logits.data_ptr(), T, out.as_struct(), self._stream())
+        self._keep(out, st)
         if st != MOE_OK:
             raise MoeError(st, "moe_ep_route")
         return out
@@ -775,6 +785,7 @@ class MoeRouter:
         st = moe_step_host(self._ctx, logits_host.data_ptr(), x_host.data_ptr(), T, out.as_struct(),
                            logits_dev.data_ptr(), x_dev.data_ptr(), y_dev.data_ptr(),
                            y_host.data_ptr(), self._stream())
+        self._keep(out, st)
         if st != MOE_OK:
             raise MoeError(st, "moe_step_host")
 
@@ -786,6 +797,7 @@ class MoeRouter:
         st = moe_step_host_async(self._ctx, logits_host.data_ptr(), x_host.data_ptr(), T, out.as_struct(),
                                  logits_dev.data_ptr(), x_dev.data_ptr(), y_dev.data_ptr(),
                                  y_host.data_ptr(), self._stream())
+        self._keep(out, st)
         if st != MOE_OK:
             raise MoeError(st, "moe_step_host_async")
 
@@ -814,7 +826,7 @@ class MoeRouter:
     def close(self) -> None:
         if self._ctx is not None:
             moe_route_destroy(self._ctx)
-            self._ctx = None
+            self._ctx = self._latest = None
 
     def __del__(self):
         try:
