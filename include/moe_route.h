@@ -394,7 +394,11 @@ moe_status moe_combine_backward(moe_ctx *ctx, const void *expert_buf, const void
  *   dx[t,:] = bf16( sum_j d_send_buf[dst_row[t*k+j], :] )                                  [T,H] bf16 out
  *   d_logits[t, id_j] = w_j * (d_weights_j - sum_i w_i * d_weights_i / route_scale)        [T,E] f32 out
  *                       (times 1 - sigmoid(logit) for sigmoid scores), 0 for every other expert
- * logits: those of the forward, read for sigmoid scores only.  d_weights and d_logits may both be
+ * Where -inf logits left a token fewer than k selectable experts (see moe_get_device_status), the picks that
+ * routing filled weigh in as the constant score they were given, the best pick's for softmax and 1 for sigmoid, and
+ * have no gradient; with softmax the best pick's own value is then minus the sum of the other selected picks'.
+ * logits: those of the forward.  NULL is allowed for softmax scores, and says that no token ran out of
+ * experts in that way.  d_weights and d_logits may both be
  * NULL; they must be for MOE_ROUTE_DENSE_TP, whose weights are constants.  d_send_buf, dx and
  * d_logits 16-byte aligned.
  */

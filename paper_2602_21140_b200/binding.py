@@ -383,7 +383,7 @@ def moe_combine_backward(ctx, expert_buf_ptr: int, dy_ptr: int, T: int, d_expert
 
 def moe_dispatch_backward(ctx, logits_ptr: int, d_send_buf_ptr: int, d_weights_ptr: int, T: int, dx_ptr: int,
                           d_logits_ptr: int, cuda_stream: int = 0) -> int:
-    """d_weights_ptr and d_logits_ptr may both be 0; logits_ptr may be 0 unless the scores are sigmoids."""
+    """d_weights_ptr and d_logits_ptr may both be 0; logits_ptr may be 0 for softmax scores if no token ran out of experts."""
     return _lib().moe_dispatch_backward(ctx, logits_ptr or None, d_send_buf_ptr, d_weights_ptr or None, T, dx_ptr,
                                         d_logits_ptr or None, cuda_stream)
 
@@ -721,7 +721,8 @@ class MoeRouter:
 
     def dispatch_backward(self, logits: torch.Tensor | None, d_send_buf: torch.Tensor, d_weights: torch.Tensor | None = None,
                           dx: torch.Tensor | None = None, d_logits: torch.Tensor | None = None):
-        """Gradients of the latest dispatch: (dx, d_logits).  d_logits is None without d_weights."""
+        """Gradients of the latest dispatch: (dx, d_logits).  d_logits is None without d_weights.  ``logits``: those of the
+        dispatch; None is for softmax scores when no -inf mask left a token with fewer than top_k experts."""
         c, dev = self.cfg, self._index()
         T = d_send_buf.shape[0] // c.top_k
         H, k, E = c.hidden, c.top_k, c.num_experts

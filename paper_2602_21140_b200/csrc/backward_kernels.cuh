@@ -8,6 +8,11 @@
 //   w_j = c * u_j / sum_i u_i with u = exp(l) or u = sigmoid(l), c = route_scale:
 //   d_l_j           = w_j * (g_j - sum_i w_i g_i / c) * (1 for softmax, 1 - sigmoid(l_j) = sigmoid(-l_j) for sigmoid)
 //   and zero for every expert that was not chosen (the selection itself has no gradient).
+//   Where -inf logits leave a token fewer than k selectable experts, routing fills its last picks with some expert
+//   and the constant u = 1 (for softmax u = exp(l - l_0), l_0 the best pick's logit, so 1 is the best pick's own
+//   score).  Filled picks take part in the sums and get no gradient; for softmax the selected picks then move
+//   against l_0 alone: d_l_0 = - (sum of the other selected picks' d_l), which is the formula above where nothing
+//   was filled.
 #pragma once
 
 #include "combine_kernels.cuh"
@@ -26,9 +31,10 @@ struct BackwardParams {
     const float *slot_scale;     // [P]        combine only
     // gate (dispatch only)
     const int32_t *topk_ids;     // [T,k]
-    const float *logits;         // [T,E], read for sigmoid scores only
+    const float *logits;         // [T,E]; NULL (softmax only) = no token ran out of experts
     float *d_logits;             // [T,E]
     int E, sigmoid;
+    int topk_group, group_size;  // group-limited selection; topk_group 0 = none
     float inv_scale;             // 1 / route_scale
     const uint4 *zero_row;       // [H/8] zeros: stands in for a row that was not placed
     Control *ctl;
@@ -80,20 +86,37 @@ struct BackwardTable {                                     // one token's assign
 inline size_t backward_smem(int slots, int slot_units) { return (size_t)slots * slot_units * 16 + 128; }
 
 // Gradient of the gate for one token, by one warp: lanes j < k form the k values, the row of d_logits is cleared
-// and the values written into it (__syncwarp orders the two).  Lanes that name the same expert (possible only
-// where routing ran out of experts and reported it) all write the sum of their values.
+// and the values written into it (__syncwarp orders the two).
+//
+// Which picks were filled follows from what was picked.  Selected picks come first, are distinct and not masked.
+// Filled ones all name one expert that has a live replica.  If that expert is masked, its logit says so.  If not,
+// it either was selected before (so the pick repeats an earlier one), or its group was not kept; then every kept
+// group had a selectable expert and, as routing ran out, all of those were picked: the earlier picks lie in
+// topk_group groups and this one in yet another.  No selected pick has any of the three marks.
 __device__ __forceinline__ void route_backward(const BackwardParams &p, int t, int lane)
 {
     const unsigned full = 0xffffffffu;
     float w = 0.0f, g = 0.0f, slope = 1.0f;
     int id = -1;
+    bool filled = false;
     if (lane < p.k) {
         const size_t i = (size_t)t * p.k + lane;
         id = __ldg(p.topk_ids + i);
         w = __ldg(p.topk_weights + i);
         g = __ldg(p.d_weights + i);
         if ((unsigned)id >= (unsigned)p.E) id = -1;
-        if (p.sigmoid && id >= 0) slope = sigmoid_spec(-__ldg(p.logits + (size_t)t * p.E + id));   // 1 - sigmoid(l) without cancellation
+    }
+    // A filled last pick has the largest score there is: unless no pick weighs more than the last one, there is
+    // nothing to look for (and with softmax no need to fetch logits behind the ids).
+    const float w_last = __shfl_sync(full, w, p.k - 1);
+    const bool look = __all_sync(full, lane >= p.k || w <= w_last);
+    if ((look || p.sigmoid) && lane < p.k) {
+        filled = id < 0;
+        if (p.logits && id >= 0) {
+            const float l = __ldg(p.logits + (size_t)t * p.E + id);
+            filled = l == __int_as_float(0xff800000);
+            if (p.sigmoid) slope = sigmoid_spec(-l);           // 1 - sigmoid(l) without cancellation
+        }
     }
     // g_j - sum_i p_i g_i as sum_i p_i (g_j - g_i) (the p_i = w_i / route_scale add up to 1): nothing
     // cancels where one expert has nearly all of the weight
@@ -102,12 +125,22 @@ __device__ __forceinline__ void route_backward(const BackwardParams &p, int t, i
         const float wi = __shfl_sync(full, w, i), gi = __shfl_sync(full, g, i);
         diff += wi * p.inv_scale * (g - gi);
     }
-    const float d = w * diff * slope;
-    float sum = 0.0f;
-    for (int j = 0; j < p.k; ++j) {
-        const int oid = __shfl_sync(full, id, j);
-        const float od = __shfl_sync(full, d, j);
-        sum += oid == id ? od : 0.0f;
+    float d = w * diff * slope;
+    int selected = p.k;
+    if (look) {
+        filled |= (__match_any_sync(full, id) & lanemask_lt()) != 0u;
+        if (p.topk_group) {
+            const bool new_group = (__match_any_sync(full, id / p.group_size) & lanemask_lt()) == 0u;
+            const unsigned firsts = __ballot_sync(full, new_group && lane < p.k);
+            filled |= new_group && __popc(firsts & lanemask_lt()) >= p.topk_group;
+        }
+        const unsigned marks = __ballot_sync(full, filled && lane < p.k);
+        if (marks) {
+            selected = __ffs(marks) - 1;
+            float others = 0.0f;
+            for (int i = 1; i < selected; ++i) others += __shfl_sync(full, d, i);
+            if (lane == 0 && !p.sigmoid) d = 0.0f - others;
+        }
     }
     float *row = p.d_logits + (size_t)t * p.E;
     if ((p.E & 3) == 0) {
@@ -116,7 +149,7 @@ __device__ __forceinline__ void route_backward(const BackwardParams &p, int t, i
         for (int e = lane; e < p.E; e += 32) row[e] = 0.0f;
     }
     __syncwarp();
-    if (id >= 0) row[id] = sum;
+    if (lane < selected && id >= 0) row[id] = d;
 }
 
 // Both gradients: a CTA per token, and as many tokens per CTA as it gets done.  One warp asks the TMA engine for

@@ -1227,6 +1227,8 @@ moe_status moe_dispatch_backward(moe_ctx *ctx, const float *logits, const void *
     p.d_weights = const_cast<float *>(d_weights); p.d_logits = d_logits;
     p.topk_ids = ctx->last_ids; p.logits = logits; p.E = ctx->d.E;
     p.sigmoid = ctx->cfg.score_func == MOE_SCORE_SIGMOID;
+    p.topk_group = ctx->cfg.n_group > 1 ? ctx->cfg.topk_group : 0;
+    p.group_size = p.topk_group ? ctx->d.E / ctx->cfg.n_group : ctx->d.E;
     p.inv_scale = 1.0f / ctx->cfg.route_scale;
     return enqueue_backward<false>(ctx, p, static_cast<cudaStream_t>(cuda_stream));
 }
