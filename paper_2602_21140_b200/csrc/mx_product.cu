@@ -281,11 +281,6 @@ __device__ __forceinline__ int segment(const KernelParams &p, int s, int &first)
 template <int NT>
 __device__ __forceinline__ int row_tiles(int c) { return (c + NT - 1) / NT; }
 
-// Sums of tile counts stop here.  Segments that do not overlap stay below it (the host checks that); counts left
-// behind by a dispatch that gave up may not.
-constexpr int kTooManyTiles = 1 << 30;
-__device__ __forceinline__ int tiles_sum(int a, int b) { return min(a + b, kTooManyTiles); }
-
 // The order of the tiles.  A slot whose rows fit one tile is bound by its weights (HBM), one with several row tiles by
 // the products (its weights come from L2 after the first), and neighbours in the order run at the same time.  So the
 // tiles of both kinds are merged in proportion, each kind in its own order, instead of slot by slot: with a popularity

@@ -8,6 +8,11 @@
 
 namespace moe {
 
+// Sums of tile counts stop at kTooManyTiles.  Segments that do not overlap stay below it (the host checks that); counts
+// left behind by a dispatch that gave up may not.  Two sums that have both stopped there still add up to an int.
+constexpr int kTooManyTiles = 1 << 29;
+__host__ __device__ inline int tiles_sum(int a, int b) { return min(a + b, kTooManyTiles); }
+
 struct MxProductArgs {
     const uint8_t *a_codes, *a_scales;   // [rows, K/2], [rows, pitch(K)]
     long long rows;
