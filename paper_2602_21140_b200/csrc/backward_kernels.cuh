@@ -260,11 +260,9 @@ __global__ void __launch_bounds__(backward_threads(COMBINE), 2) k_backward(Backw
         if (!ok) {
             if (lane == 0) report_status(p.ctl, kDevTimeout);
             // the answer and the copies in flight still land in this CTA's shared memory: a bounded wait for each
-            for (unsigned spins = 0; !mbar_try_wait(&clc_bar, clc_parity) && ++spins < p.spin_limit;) {}
-            for (int m = max(0, issued - S); m < issued; ++m) {
-                unsigned spins = 0;
-                while (!mbar_try_wait(&full[m % S], (unsigned)(m / S) & 1u) && ++spins < p.spin_limit) {}
-            }
+            unsigned long long until = 0;
+            for (int m = max(0, issued - S); m < issued; ++m) drain_wait(&full[m % S], (unsigned)(m / S) & 1u, until);
+            drain_wait(&clc_bar, clc_parity, until);           // last: with nothing asked for, this one runs out
         }
         return;
     }

@@ -278,10 +278,8 @@ __global__ void __launch_bounds__(kCombineBulkMaxWarps * 32) k_combine_bulk(Comb
         if (lane == 0) report_status(ctl, kDevTimeout);
         // copies issued for items n .. n+stages-1 may still be landing in this CTA's shared
         // memory: give each a bounded chance to finish before the memory is released
-        for (int m = n; m < min(n_mine, n + stages); ++m) {
-            unsigned spins = 0;
-            while (!mbar_try_wait(&full[m % stages], (unsigned)(m / stages) & 1u) && ++spins < p.spin_limit) {}
-        }
+        unsigned long long until = 0;
+        for (int m = n; m < min(n_mine, n + stages); ++m) drain_wait(&full[m % stages], (unsigned)(m / stages) & 1u, until);
     }
 }
 

@@ -216,6 +216,22 @@ __device__ __forceinline__ bool mbar_try_wait(uint64_t *bar, unsigned parity)
     return ok != 0;
 }
 
+// A role that gives up still has copies (or products) in flight, which land in shared memory or TMEM of a CTA that is
+// about to leave.  The waits for them have a limit of their own, in time, whatever the polls of the waits that
+// gave up (a context may set those to any number): a copy takes microseconds.  `until` starts at 0 and is shared
+// by the drains of a role, whose barriers may be ones that never complete.
+constexpr unsigned long long kDrainNs = 20ull * 1000 * 1000;
+constexpr unsigned kDrainPolls = 1u << 22;             // ends the wait even if the timer stood still
+__device__ __forceinline__ void drain_wait(uint64_t *bar, unsigned parity, unsigned long long &until)
+{
+    for (unsigned polls = 0; !mbar_try_wait(bar, parity) && polls < kDrainPolls; ++polls) {
+        unsigned long long now;
+        asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(now));
+        if (until == 0) until = now + kDrainNs;
+        else if (now > until) break;
+    }
+}
+
 // global -> shared bulk copy, completion counted in bytes on an mbarrier
 __device__ __forceinline__ void bulk_load(void *smem_dst, const void *gsrc, unsigned bytes,
                                           uint64_t *bar)

@@ -694,12 +694,10 @@ k_mx_product(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
             }
         }
         if (!ok) {
-            // loads in flight still land in this CTA's shared memory: a bounded wait for each (their barriers also
-            // count the scales, so they may not complete, but the wait outlasts any copy)
-            for (int m = max(0, issued - STAGES); m < issued; ++m) {
-                unsigned spins = 0;
-                while (!mbar_try_wait(&full[m % STAGES], (unsigned)(m / STAGES) & 1u) && ++spins < p.spin_limit) {}
-            }
+            // loads in flight still land in this CTA's shared memory: a bounded wait for them (their barriers also
+            // count the scales, or are the other CTA's, so they may not complete, but the wait outlasts any copy)
+            unsigned long long until = 0;
+            for (int m = max(0, issued - STAGES); m < issued; ++m) drain_wait(&full[m % STAGES], (unsigned)(m / STAGES) & 1u, until);
         }
     } else if (warp == kMmaWarp && rank == 0) {
         int s = 0, buf = 0;
@@ -752,8 +750,8 @@ k_mx_product(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
         // everything issued has left the tensor core before TMEM is given back
         if (elect_one()) mma_commit<CG>(drained);
         __syncwarp();
-        unsigned spins = 0;
-        while (!mbar_try_wait(drained, 0) && ++spins < p.spin_limit) {}
+        unsigned long long until = 0;
+        drain_wait(drained, 0, until);
     } else if (warp >= kScaleWarp) {
         // Two warps per 128-row block of scales (the weight rows, then the data rows), which take the pieces of
         // 16 bytes a row (K = 512, two stages) in turn, each reading kPieces of its own ahead.  Lane l owns rows
@@ -895,8 +893,8 @@ k_mx_product(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
     if (tid == 0 && *quit) report_status(p.ctl, kDevTimeout);
     if (warp == kMmaWarp) {
         if (CG == 2 && rank == 1) {                            // the first CTA's last arrival is on its way here as well
-            unsigned spins = 0;
-            while (!mbar_try_wait(drained, 0) && ++spins < p.spin_limit) {}
+            unsigned long long until = 0;
+            drain_wait(drained, 0, until);
             __syncwarp();
         }
         tc_fence_after();

@@ -166,10 +166,9 @@ __global__ void __launch_bounds__(kBulkThreads) k_scatter_bulk(ScatterParams p, 
         if (lane == 0) report_status(p.ctl, kDevTimeout);
         // loads requested for tokens n_failed_at .. n_failed_at+stages-1 may still be landing in this
         // CTA's shared memory: give each a bounded chance to finish before the memory is released
-        for (int m = n_failed_at; m < min(n_mine, n_failed_at + stages); ++m) {
-            unsigned spins = 0;
-            while (!mbar_try_wait(&full_bar[m % stages], (unsigned)(m / stages) & 1u) && ++spins < p.spin_limit) {}
-        }
+        unsigned long long until = 0;
+        for (int m = n_failed_at; m < min(n_mine, n_failed_at + stages); ++m)
+            drain_wait(&full_bar[m % stages], (unsigned)(m / stages) & 1u, until);
     }
     bulk_wait_all();   // nothing of this CTA may still read the ring or write HBM at exit
 }
