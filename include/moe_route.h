@@ -352,7 +352,7 @@ moe_status moe_mx_dispatch(moe_ctx *ctx, const float *logits, const void *x, int
  *     cut at `rows`; segments must not overlap.
  *   w_codes, w_scales device [P, n_out] 4-bit rows of n_in elements, P slots of this context
  *   y device out [rows, n_out] bf16, 16-byte aligned
- * n_in % 32 == 0, n_out % 8 == 0, rows <= 2^30.  rows = 0 launches nothing.  Allocates nothing, does not wait;
+ * n_in % 32 == 0, n_out % 8 == 0; CAPACITY if rows or n_out exceed 2^30.  rows = 0 launches nothing.  Allocates nothing, does not wait;
  * a bounded wait that gives up sets the context's device status.
  */
 moe_status moe_mx_expert_product(moe_ctx *ctx, const uint8_t *a_codes, const uint8_t *a_scales, int64_t rows,

@@ -599,10 +599,7 @@ moe_status check_product(const moe_ctx *ctx, const uint8_t *a_codes, const uint8
                          const uint8_t *w_scales, int32_t n_out, int32_t n_in)
 {
     if (!ctx || rows < 0 || n_out < 1 || n_in < kMxBlock || n_in % kMxBlock != 0) return MOE_ERR_INVALID_ARG;
-    // 32-bit tile numbers and tensor-map strides (2^40 bytes)
-    const long long feats = ((long long)n_out + 127) / 128;
-    if (rows > (1ll << 30) || feats * (ctx->d.P + rows / 32) >= kTooManyTiles) return MOE_ERR_CAPACITY;
-    if ((long long)n_out * (n_in / 2) >= (1ll << 40)) return MOE_ERR_CAPACITY;
+    if (!product_fits(rows, n_out, n_in, ctx->d.P)) return MOE_ERR_CAPACITY;
     if (rows == 0) return MOE_OK;
     if (!a_codes || !a_scales || !slot_counts || !slot_offsets || !w_codes || !w_scales) return MOE_ERR_INVALID_ARG;
     if (!aligned16(a_codes) || !aligned16(a_scales) || !aligned16(w_codes) || !aligned16(w_scales)) return MOE_ERR_INVALID_ARG;

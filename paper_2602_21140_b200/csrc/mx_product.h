@@ -13,6 +13,15 @@ namespace moe {
 constexpr int kTooManyTiles = 1 << 29;
 __host__ __device__ inline int tiles_sum(int a, int b) { return min(a + b, kTooManyTiles); }
 
+// Whether the sizes of a product fit the kernels' numbers: features are counted in int, rounded up to the two tiles
+// of a pair; rows are coordinates of a tensor map; tile numbers stay below kTooManyTiles; strides below 2^40 bytes.
+constexpr int kMaxFeatures = 1 << 30, kMaxRows = 1 << 30;
+inline bool product_fits(long long rows, long long n_out, long long n_in, int P)
+{
+    if (rows > kMaxRows || n_out > kMaxFeatures) return false;
+    return (n_out + 127) / 128 * (P + rows / 32) < kTooManyTiles && n_out * (n_in / 2) < (1ll << 40);
+}
+
 struct MxProductArgs {
     const uint8_t *a_codes, *a_scales;   // [rows, K/2], [rows, pitch(K)]
     long long rows;

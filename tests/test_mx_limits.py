@@ -35,3 +35,15 @@ def test_sums_of_tiles_saturate(tmp_path):
     printf("%d %d %d\n", v[0], total, sorted);''')
     assert [int(x) for x in got[:len(cases)]] == [min(a + b, limit) for a, b in cases]
     assert got[len(cases):] == [str(1 << 26), str(limit), "1"]
+
+
+def test_sizes_that_the_kernels_numbers_cannot_hold_are_refused(tmp_path):
+    """Whatever is accepted, the rounding up to a pair of tiles (2 x 128 features) and the first feature of the last
+    tile stay ints, and so do rows rounded up to a tile."""
+    top = 2 ** 31 - 1
+    cases = [(1, 8, 32, 1, 1), (1, 1 << 30, 32, 1, 1), (1 << 30, 8, 32, 1, 1),
+             (1, top - 7, 32, 1, 0), (1, top - 255, 32, 1, 0), (1, top, 32, 4, 0), (1, (1 << 30) + 8, 32, 1, 0),
+             ((1 << 30) + 1, 8, 32, 1, 0), (1 << 30, 1 << 30, 32, 1, 0), (1, 1 << 30, 2048, 1, 0), (1, 1 << 25, 32, 4096, 0)]
+    got = _run(tmp_path, "\n".join(f'printf("%d\\n", (int)product_fits({r}ll, {n}ll, {k}ll, {p}));' for r, n, k, p, _ in cases) + """
+    printf("%d\\n", (int)((long long)kMaxFeatures + 2 * 2 * 128 < (1ll << 31) && (long long)kMaxRows + 2 * 224 < (1ll << 31)));""")
+    assert [int(x) for x in got] == [c[4] for c in cases] + [1]
