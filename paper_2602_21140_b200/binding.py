@@ -630,6 +630,8 @@ class MoeRouter:
         _require(_is_dense(logits, torch.float32, (T, c.num_experts), dev) and _is_dense(x, torch.bfloat16, (T, H), dev), "mx_dispatch")
         if out is None:
             out = self.alloc_outputs(T, send_buf=False)
+        else:
+            _require(self._outputs_ok(out, T, dev), "mx_dispatch")
         if rows is None:
             rows = _mx_like(x, (T * c.top_k,), H)
         else:
@@ -640,6 +642,20 @@ class MoeRouter:
         if st != MOE_OK:
             raise MoeError(st, "moe_mx_dispatch")
         return out, rows
+
+    def _outputs_ok(self, out: DispatchBuffers, T: int, dev: int) -> bool:
+        """The index buffers have room for a dispatch of T tokens (send_buf is not among them): the C call takes their
+        sizes on trust.  (2 of the 12 microseconds that a small call takes on the host.)"""
+        c = self.cfg
+        R, n, i32, weights = c.num_ranks, T * c.top_k, torch.int32, out.topk_weights
+        P = R * c.slots_per_rank
+        if weights.dtype is not torch.float32:
+            return False
+        for t, least in ((weights, n), (out.topk_ids, n), (out.topk_slot, n), (out.dst_row, n), (out.src_index, n), (out.slot_counts, P),
+                         (out.slot_offsets, P + 1), (out.rank_counts, R), (out.rank_offsets, R + 1)):
+            if t.numel() < least or not t.is_contiguous() or t.get_device() != dev or (t.dtype is not i32 and t is not weights):
+                return False
+        return True
 
     def _segments_ok(self, rows: MxRows, slot_counts, slot_offsets, weight: MxRows, dev: int) -> bool:
         P, w = self.num_slots, weight.codes.shape

@@ -24,3 +24,27 @@ def test_features_that_an_int_cannot_round_up():
     torch.cuda.synchronize()
     assert (y == -7).all() and r.device_status() == 0
     r.close()
+
+
+def test_buffers_of_a_smaller_dispatch():
+    """test_mx_binding shows on the CPU that such a call does not reach the library."""
+    r = _router(4)
+    logits, x = torch.randn(9, 4, device="cuda"), torch.randn(9, 64, device="cuda").bfloat16()
+    whole = torch.full((64,), -7, dtype=torch.int32, device="cuda")
+    out = r.alloc_outputs(8, send_buf=False)
+    out.dst_row = whole[:8]
+    with pytest.raises(B.MoeError):
+        r.mx_dispatch(logits, x, out)
+    gate_up, down = (B.mx_quantize(torch.randn(4, 64, cols, device="cuda")) for cols in (64, 32))
+    with pytest.raises(B.MoeError):
+        r.mx_step(logits, x, gate_up, down, out)
+    torch.cuda.synchronize()
+    assert (whole == -7).all()
+    large = r.alloc_outputs(12, send_buf=False)              # room for more tokens is fine
+    r.mx_dispatch(logits, x, large)
+    want, _ = r.mx_dispatch(logits, x)
+    torch.cuda.synchronize()
+    for f in ("topk_ids", "topk_slot", "dst_row", "src_index"):
+        a = getattr(want, f).flatten()
+        assert torch.equal(getattr(large, f).flatten()[:a.numel()], a), f
+    r.close()

@@ -1,0 +1,87 @@
+"""CPU-only: what the binding of the 4-bit dispatch lets through to the C call, which cannot know a buffer's size.
+Tensors are stand-ins that claim to be on a device; the C calls are replaced and only note that they were reached."""
+import dataclasses
+
+import pytest
+import torch
+
+from paper_2602_21140_b200 import binding as B
+
+
+class Fake:
+    """As much of a CUDA tensor as the binding looks at."""
+
+    def __init__(self, shape, dtype, device=0, contiguous=True):
+        self.shape, self.dtype, self._device, self._contiguous = torch.Size(shape), dtype, device, contiguous
+        self.is_cuda = device >= 0
+
+    def is_contiguous(self):
+        return self._contiguous
+
+    def get_device(self):
+        return self._device
+
+    def data_ptr(self):
+        return 1 << 20
+
+    def numel(self):
+        return self.shape.numel()
+
+    def dim(self):
+        return len(self.shape)
+
+    def new_empty(self, shape, dtype=None):
+        return Fake(shape, dtype or self.dtype, self._device)
+
+
+T, H, E, K, R, S = 8, 64, 8, 2, 4, 2
+
+
+@pytest.fixture
+def router(monkeypatch):
+    r = B.MoeRouter.__new__(B.MoeRouter)
+    r.cfg = B.make_config(E, K, H, 64, R, S)
+    r.device, r._ctx, r._latest = torch.device("cuda", 0), None, None
+    reached = []
+    for name in ("moe_mx_dispatch", "moe_mx_expert_gated", "moe_mx_expert_product", "moe_combine"):
+        monkeypatch.setattr(B, name, lambda *a, _n=name: reached.append(_n) or B.MOE_OK)
+    monkeypatch.setattr(B, "_raw_stream", lambda index: 0)
+    monkeypatch.setattr(B, "_on_device", lambda index, call, *args: call(*args))
+    monkeypatch.setattr(B.MoeRouter, "_stream", lambda self: 0)
+    r.reached = reached
+    return r
+
+
+def _out(tokens=T, device=0, ranks=R, slots=R * S, k=K):
+    i, f, n = torch.int32, torch.float32, tokens * k
+    return B.DispatchBuffers(Fake((tokens, k), i, device), Fake((tokens, k), f, device), Fake((tokens, k), i, device),
+                             Fake((slots,), i, device), Fake((slots + 1,), i, device), Fake((ranks,), i, device),
+                             Fake((ranks + 1,), i, device), Fake((n,), i, device), Fake((n,), i, device), None)
+
+
+def _inputs():
+    return Fake((T, E), torch.float32), Fake((T, H), torch.bfloat16)
+
+
+def test_buffers_of_this_dispatch_pass(router):
+    router.mx_dispatch(*_inputs(), _out())
+    router.mx_dispatch(*_inputs(), _out(tokens=T + 3))       # allocated for more tokens than come this time
+    assert router.reached == ["moe_mx_dispatch"] * 2
+
+
+@pytest.mark.parametrize("out", [_out(tokens=T - 1), _out(device=1), _out(device=-1), _out(ranks=2), _out(slots=7),
+                                 _out(k=1)], ids=["smaller T", "other device", "CPU", "fewer ranks", "fewer slots", "smaller k"])
+def test_buffers_of_another_dispatch_are_refused(router, out):
+    with pytest.raises(B.MoeError):
+        router.mx_dispatch(*_inputs(), out)
+    assert router.reached == []
+
+
+@pytest.mark.parametrize("field", [f.name for f in dataclasses.fields(B.DispatchBuffers) if f.name != "send_buf"])
+def test_every_buffer_is_looked_at(router, field):
+    good = getattr(_out(), field)
+    for bad in (Fake(good.shape, torch.int64), Fake(good.shape, good.dtype, contiguous=False), Fake(good.shape, good.dtype, device=1),
+                Fake(tuple(good.shape)[:-1] + (good.shape[-1] - 1,), good.dtype)):
+        with pytest.raises(B.MoeError):
+            router.mx_dispatch(*_inputs(), dataclasses.replace(_out(), **{field: bad}))
+    assert router.reached == []
