@@ -708,9 +708,13 @@ class MoeRouter:
     def mx_step(self, logits: torch.Tensor, x: torch.Tensor, gate_up: MxRows, down: MxRows, out: DispatchBuffers | None = None,
                 y: torch.Tensor | None = None) -> torch.Tensor:
         """One whole layer: 4-bit dispatch, the experts, and the combine (times slot_scale, as always)."""
+        H, P, g, d = self.cfg.hidden, self.num_slots, gate_up.codes.shape, down.codes.shape
+        # before the first launch: the combine takes the size of y on trust, and a step that is refused halfway has
+        # already replaced the latest dispatch
+        _require(len(g) == 3 and g[1] > 0 and g[1] % 64 == 0 and tuple(g) == (P, g[1], H // 2) and tuple(d) == (P, H, g[1] // 4)
+                 and (y is None or _is_dense(y, torch.bfloat16, (x.shape[0], H), self._index())), "mx_step")
         out, rows = self.mx_dispatch(logits, x, out)
         buf = self.mx_expert_ffn(rows, out.slot_counts, out.slot_offsets, gate_up, down)
-        _require(buf.shape[1] == self.cfg.hidden, "mx_step")
         return _on_device(self._index(), self.combine, buf, x.shape[0], y)
 
     # -- gradients of the routed step ----------------------------------------

@@ -48,3 +48,19 @@ def test_buffers_of_a_smaller_dispatch():
         a = getattr(want, f).flatten()
         assert torch.equal(getattr(large, f).flatten()[:a.numel()], a), f
     r.close()
+
+
+def test_a_step_into_a_shorter_y():
+    """test_mx_binding shows on the CPU that nothing is launched."""
+    r = _router(4)
+    logits, x = torch.randn(9, 4, device="cuda"), torch.randn(9, 64, device="cuda").bfloat16()
+    gate_up, down = (B.mx_quantize(torch.randn(4, 64, cols, device="cuda")) for cols in (64, 32))
+    whole = torch.full((9, 64), -7.0, dtype=torch.bfloat16, device="cuda")
+    for y in (whole[:8], whole[:, :32], whole.float(), whole.cpu()):
+        with pytest.raises(B.MoeError):
+            r.mx_step(logits, x, gate_up, down, y=y)
+    torch.cuda.synchronize()
+    assert (whole == -7).all()
+    want = r.mx_step(logits, x, gate_up, down)
+    assert torch.equal(r.mx_step(logits, x, gate_up, down, y=whole), want)
+    r.close()

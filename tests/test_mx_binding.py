@@ -85,3 +85,35 @@ def test_every_buffer_is_looked_at(router, field):
         with pytest.raises(B.MoeError):
             router.mx_dispatch(*_inputs(), dataclasses.replace(_out(), **{field: bad}))
     assert router.reached == []
+
+
+def _rows(*shape):
+    pitch = (shape[-1] // 32 + 15) // 16 * 16
+    return B.MxRows(Fake((*shape[:-1], shape[-1] // 2), torch.uint8), Fake((*shape[:-1], pitch), torch.uint8))
+
+
+I = 96
+
+
+def _step(router, y=None, gate_up=None, down=None):
+    router.mx_step(*_inputs(), gate_up or _rows(R * S, 2 * I, H), down or _rows(R * S, H, I), _out(), y)
+
+
+def test_a_whole_step_passes(router):
+    _step(router, Fake((T, H), torch.bfloat16))
+    assert router.reached == ["moe_mx_dispatch", "moe_mx_expert_gated", "moe_mx_expert_product", "moe_combine"]
+
+
+@pytest.mark.parametrize("args", [
+    dict(y=Fake((T - 1, H), torch.bfloat16)), dict(y=Fake((T, H - 32), torch.bfloat16)), dict(y=Fake((T, H), torch.float32)),
+    dict(y=Fake((T, H), torch.bfloat16, device=1)), dict(y=Fake((T, H), torch.bfloat16, contiguous=False)),
+    dict(down=_rows(R * S, H - 32, I)), dict(down=_rows(R * S, H, I - 32)), dict(gate_up=_rows(R * S * 2 * I, H)),
+    dict(down=_rows(R * S * H, I)), dict(gate_up=_rows(R * S - 1, 2 * I, H)), dict(gate_up=_rows(R * S, 2 * I, H + 32)),
+    dict(gate_up=_rows(R * S, 2 * I - 32, H))],
+    ids=["rows of y", "columns of y", "type of y", "device of y", "strides of y", "features", "hidden", "flat gate_up", "flat down", "slots", "columns",
+         "half a block of pairs"])
+def test_a_step_is_refused_before_its_first_launch(router, args):
+    """Above all a y that the combine, which takes its size on trust, would write past its end."""
+    with pytest.raises(B.MoeError):
+        _step(router, **args)
+    assert router.reached == []
