@@ -320,7 +320,8 @@ int32_t moe_mx_scale_pitch(int32_t cols);
  * weights ([experts, features, cols] flattened to rows).
  *   x device [rows, cols] of `dtype`, `row_stride` elements from row to row (>= cols, rows 16-byte
  *     aligned); codes, scales device out, as above (the padding of the scales is written as 0)
- * rows = 0 succeeds and launches nothing.  CAPACITY beyond 2^40 elements.  Allocates nothing, does not wait.
+ * rows = 0 succeeds and launches nothing.  CAPACITY beyond 2^40 elements.  x, codes and scales may not overlap (nor
+ * may they in moe_mx_dequantize): INVALID_ARG.  Allocates nothing, does not wait.
  */
 moe_status moe_mx_quantize(const void *x, int32_t dtype, int64_t rows, int32_t cols, int64_t row_stride,
                            uint8_t *codes, uint8_t *scales, void *cuda_stream);

@@ -2,6 +2,7 @@
 #pragma once
 
 #include <cuda_runtime.h>
+#include <stddef.h>
 #include <stdint.h>
 
 namespace moe {
@@ -24,6 +25,24 @@ struct Control {
     int status;          // kDev* code, sticky until the host clears it
     int pad;
 };
+
+// Host side: whether two buffers share a byte (an operator whose output lies on its input would read what other CTAs
+// have already written), and whether rows `stride` bytes apart (>= row_bytes) share one with a buffer.
+inline bool ranges_overlap(const void *a, size_t a_bytes, const void *b, size_t b_bytes)
+{
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return x <= y ? y - x < a_bytes && b_bytes > 0 : x - y < b_bytes && a_bytes > 0;
+}
+
+inline bool rows_overlap(const void *a, long long rows, size_t row_bytes, size_t stride, const void *b, size_t b_bytes)
+{
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    if (rows <= 0 || b_bytes == 0) return false;
+    if (y < x) return x - y < b_bytes;
+    // the first row that ends behind the start of b
+    const size_t off = y - x, i = off < row_bytes ? 0 : (off - row_bytes) / stride + 1;
+    return i < (size_t)rows && i * stride < off + b_bytes;
+}
 
 // Programmatic dependent launch: let the next kernel of the stream be scheduled while this
 // one is still running, and hold this kernel until the previous one has completed and its

@@ -186,6 +186,12 @@ moe_status fill(RowParams *p, const void *x, int32_t dtype, long long rows, int3
     if (rows == 0) return MOE_OK;
     if (!x || !codes || !scales || !aligned(x, 16) || !aligned(codes, 16) || !aligned(scales, 16)) return MOE_ERR_INVALID_ARG;
     if (rows > 1 && (row_stride * size) % 16 != 0) return MOE_ERR_INVALID_ARG;
+    // One side is read while the other is written, in no particular order.
+    const size_t row_bytes = (size_t)cols * size, stride_bytes = rows > 1 ? (size_t)row_stride * size : row_bytes;
+    if (rows_overlap(x, rows, row_bytes, stride_bytes, codes, (size_t)rows * (cols / 2)) ||
+        rows_overlap(x, rows, row_bytes, stride_bytes, scales, (size_t)rows * mx_scale_pitch(cols)) ||
+        ranges_overlap(codes, (size_t)rows * (cols / 2), scales, (size_t)rows * mx_scale_pitch(cols)))
+        return MOE_ERR_INVALID_ARG;
     p->x = static_cast<char *>(const_cast<void *>(x));
     p->stride = row_stride * size;
     p->codes = const_cast<uint8_t *>(codes);
