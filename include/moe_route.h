@@ -338,7 +338,7 @@ moe_status moe_mx_dequantize(const uint8_t *codes, const uint8_t *scales, int64_
  * each token's row is quantised once and its codes and scales are written to its k rows.
  *   out->send_buf is not used and may be NULL
  *   send_codes device out [T*k, H/2], send_scales device out [T*k, moe_mx_scale_pitch(H)]
- * INVALID_ARG if H % 32 != 0, otherwise as moe_dispatch.  moe_combine and the gradients may follow it.
+ * INVALID_ARG if H % 32 != 0 or if x and the send buffers overlap, otherwise as moe_dispatch.  moe_combine and the gradients may follow it.
  */
 moe_status moe_mx_dispatch(moe_ctx *ctx, const float *logits, const void *x, int32_t T,
                            const moe_dispatch_out *out, uint8_t *send_codes, uint8_t *send_scales,
@@ -352,7 +352,7 @@ moe_status moe_mx_dispatch(moe_ctx *ctx, const float *logits, const void *x, int
  *   slot_counts, slot_offsets device [P] (of a dispatch; a longer slot_offsets is fine).  Segments are
  *     cut at `rows`; segments must not overlap.
  *   w_codes, w_scales device [P, n_out] 4-bit rows of n_in elements, P slots of this context
- *   y device out [rows, n_out] bf16, 16-byte aligned
+ *   y device out [rows, n_out] bf16, 16-byte aligned; INVALID_ARG if it overlaps an input
  * n_in % 32 == 0, n_out % 8 == 0; CAPACITY if rows or n_out exceed 2^30.  rows = 0 launches nothing.  Allocates nothing, does not wait;
  * a bounded wait that gives up sets the context's device status.
  */
@@ -367,7 +367,8 @@ moe_status moe_mx_expert_product(moe_ctx *ctx, const uint8_t *a_codes, const uin
  * in fp32, then quantised.  Row 2i of a slot's matrix is the gate of feature i, row 2i + 1 its
  * up-projection.
  *   w_codes, w_scales device [P, 2 * n_hidden] 4-bit rows of n_in elements
- *   h_codes, h_scales device out: `rows` 4-bit rows of n_hidden elements (the padding of the scales is not written)
+ *   h_codes, h_scales device out: `rows` 4-bit rows of n_hidden elements (the padding of the scales is not written);
+ *     INVALID_ARG if they overlap an input
  * n_hidden % 32 == 0; otherwise as moe_mx_expert_product, which takes h to the expert's output.
  */
 moe_status moe_mx_expert_gated(moe_ctx *ctx, const uint8_t *a_codes, const uint8_t *a_scales, int64_t rows,

@@ -606,6 +606,15 @@ moe_status check_product(const moe_ctx *ctx, const uint8_t *a_codes, const uint8
     return MOE_OK;
 }
 
+// Whether an output of a product shares a byte with what other CTAs still read: the rows, the weights, the segments.
+bool over_inputs(const MxProductArgs &a, const void *out, size_t bytes)
+{
+    const size_t k = (size_t)a.K, rows = (size_t)a.rows, feats = (size_t)a.P * a.N, pitch = (size_t)mx_scale_pitch(a.K);
+    return ranges_overlap(out, bytes, a.a_codes, rows * (k / 2)) || ranges_overlap(out, bytes, a.a_scales, rows * pitch) ||
+           ranges_overlap(out, bytes, a.w_codes, feats * (k / 2)) || ranges_overlap(out, bytes, a.w_scales, feats * pitch) ||
+           ranges_overlap(out, bytes, a.slot_counts, (size_t)a.P * 4) || ranges_overlap(out, bytes, a.slot_offsets, (size_t)a.P * 4);
+}
+
 MxProductArgs product_args(const moe_ctx *ctx, const uint8_t *a_codes, const uint8_t *a_scales, int64_t rows,
                            const int32_t *slot_counts, const int32_t *slot_offsets, const uint8_t *w_codes,
                            const uint8_t *w_scales, int32_t n_out, int32_t n_in)
@@ -1132,6 +1141,10 @@ moe_status moe_mx_dispatch(moe_ctx *ctx, const float *logits, const void *x, int
             return MOE_ERR_INVALID_ARG;
         if (!x || (!logits && ctx->cfg.score_func != MOE_ROUTE_DENSE_TP)) return MOE_ERR_INVALID_ARG;
         if (!aligned16(x) || !aligned16(logits) || !aligned16(send_codes) || !aligned16(send_scales)) return MOE_ERR_INVALID_ARG;
+        const size_t n = (size_t)T * ctx->d.k, H = (size_t)ctx->d.H, codes = n * (H / 2), scales = n * mx_scale_pitch(ctx->d.H);
+        if (ranges_overlap(send_codes, codes, x, T * H * 2) || ranges_overlap(send_scales, scales, x, T * H * 2) ||
+            ranges_overlap(send_codes, codes, send_scales, scales))
+            return MOE_ERR_INVALID_ARG;
     }
     ctx->last_ids = out->topk_ids; ctx->last_weights = out->topk_weights; ctx->last_slot = out->topk_slot;
     ctx->last_dst_row = out->dst_row; ctx->last_T = T;
@@ -1165,10 +1178,11 @@ moe_status moe_mx_expert_product(moe_ctx *ctx, const uint8_t *a_codes, const uin
     if (n_out % 8 != 0) return MOE_ERR_INVALID_ARG;
     if (rows == 0) return MOE_OK;
     if (!y || !aligned16(y)) return MOE_ERR_INVALID_ARG;
-    DeviceScope scope(ctx->device);
-    if (!scope.ok) return MOE_ERR_CUDA;
     MxProductArgs a = product_args(ctx, a_codes, a_scales, rows, slot_counts, slot_offsets, w_codes, w_scales, n_out, n_in);
     a.gated = false; a.y = y;
+    if (over_inputs(a, y, (size_t)rows * n_out * 2)) return MOE_ERR_INVALID_ARG;
+    DeviceScope scope(ctx->device);
+    if (!scope.ok) return MOE_ERR_CUDA;
     return mx_product_launch(a, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? MOE_OK : MOE_ERR_CUDA;
 }
 
@@ -1181,10 +1195,14 @@ moe_status moe_mx_expert_gated(moe_ctx *ctx, const uint8_t *a_codes, const uint8
     const moe_status ms = check_product(ctx, a_codes, a_scales, rows, slot_counts, slot_offsets, w_codes, w_scales, 2 * n_hidden, n_in);
     if (ms != MOE_OK || rows == 0) return ms;
     if (!h_codes || !h_scales || !aligned16(h_codes) || !aligned16(h_scales)) return MOE_ERR_INVALID_ARG;
-    DeviceScope scope(ctx->device);
-    if (!scope.ok) return MOE_ERR_CUDA;
     MxProductArgs a = product_args(ctx, a_codes, a_scales, rows, slot_counts, slot_offsets, w_codes, w_scales, 2 * n_hidden, n_in);
     a.gated = true; a.h_codes = h_codes; a.h_scales = h_scales;
+    const size_t code_bytes = (size_t)rows * (n_hidden / 2), scale_bytes = (size_t)rows * mx_scale_pitch(n_hidden);
+    if (over_inputs(a, h_codes, code_bytes) || over_inputs(a, h_scales, scale_bytes) ||
+        ranges_overlap(h_codes, code_bytes, h_scales, scale_bytes))
+        return MOE_ERR_INVALID_ARG;
+    DeviceScope scope(ctx->device);
+    if (!scope.ok) return MOE_ERR_CUDA;
     return mx_product_launch(a, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? MOE_OK : MOE_ERR_CUDA;
 }
 
