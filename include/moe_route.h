@@ -386,7 +386,8 @@ moe_status moe_mx_expert_gated(moe_ctx *ctx, const uint8_t *a_codes, const uint8
  * moe_combine_backward — from dy device [T,H] bf16 and the expert_buf [T*k,H] bf16 of the forward:
  *   d_expert_buf[dst_row[t*k+j], :] = bf16( (w[t,j] * slot_scale[slot]) * dy[t,:] )       [T*k,H] bf16 out
  *   d_weights[t,j] = slot_scale[slot] * sum_c expert_buf[dst_row[t*k+j], c] * dy[t,c]     [T,k] f32 out
- * fp32 sums in a fixed order.  expert_buf, dy and d_expert_buf 16-byte aligned; d_expert_buf may not be expert_buf.
+ * fp32 sums in a fixed order.  expert_buf, dy and d_expert_buf 16-byte aligned; INVALID_ARG if an output overlaps
+ * an input or the other output.
  */
 moe_status moe_combine_backward(moe_ctx *ctx, const void *expert_buf, const void *dy, int32_t T,
                                 void *d_expert_buf, float *d_weights, void *cuda_stream);
@@ -402,7 +403,7 @@ moe_status moe_combine_backward(moe_ctx *ctx, const void *expert_buf, const void
  * logits: those of the forward.  NULL is allowed for softmax scores, and says that no token ran out of
  * experts in that way.  d_weights and d_logits may both be
  * NULL; they must be for MOE_ROUTE_DENSE_TP, whose weights are constants.  d_send_buf, dx and
- * d_logits 16-byte aligned.
+ * d_logits 16-byte aligned; INVALID_ARG if an output overlaps an input or the other output.
  */
 moe_status moe_dispatch_backward(moe_ctx *ctx, const float *logits, const void *d_send_buf, const float *d_weights,
                                  int32_t T, void *dx, float *d_logits, void *cuda_stream);

@@ -1214,7 +1214,12 @@ moe_status moe_combine_backward(moe_ctx *ctx, const void *expert_buf, const void
     if (T == 0) return MOE_OK;
     if (!expert_buf || !dy || !d_expert_buf || !d_weights) return MOE_ERR_INVALID_ARG;
     if (!aligned16(expert_buf) || !aligned16(dy) || !aligned16(d_expert_buf)) return MOE_ERR_INVALID_ARG;
-    if (expert_buf == d_expert_buf) return MOE_ERR_INVALID_ARG;   // rows are read ahead of the ones written
+    // rows are read ahead of the ones written
+    const size_t row = (size_t)ctx->d.H * 2, tokens = (size_t)T * row, all = tokens * ctx->d.k, weights = (size_t)T * ctx->d.k * 4;
+    if (ranges_overlap(d_expert_buf, all, expert_buf, all) || ranges_overlap(d_expert_buf, all, dy, tokens) ||
+        ranges_overlap(d_weights, weights, expert_buf, all) || ranges_overlap(d_weights, weights, dy, tokens) ||
+        ranges_overlap(d_weights, weights, d_expert_buf, all))
+        return MOE_ERR_INVALID_ARG;
     DeviceScope scope(ctx->device);
     if (!scope.ok) return MOE_ERR_CUDA;
     BackwardParams p = backward_params(ctx, T);
@@ -1235,6 +1240,12 @@ moe_status moe_dispatch_backward(moe_ctx *ctx, const float *logits, const void *
     if (T == 0) return MOE_OK;
     if (!d_send_buf || !dx || !aligned16(d_send_buf) || !aligned16(dx)) return MOE_ERR_INVALID_ARG;
     if (d_logits && (!aligned16(d_logits) || (ctx->cfg.score_func == MOE_SCORE_SIGMOID && !logits))) return MOE_ERR_INVALID_ARG;
+    const size_t tokens = (size_t)T * ctx->d.H * 2, all = tokens * ctx->d.k, scores = (size_t)T * ctx->d.E * 4, weights = (size_t)T * ctx->d.k * 4;
+    if (ranges_overlap(dx, tokens, d_send_buf, all)) return MOE_ERR_INVALID_ARG;
+    if (d_logits && (ranges_overlap(d_logits, scores, d_send_buf, all) || ranges_overlap(d_logits, scores, dx, tokens) ||
+                     ranges_overlap(d_logits, scores, d_weights, weights) || ranges_overlap(dx, tokens, d_weights, weights) ||
+                     (logits && (ranges_overlap(d_logits, scores, logits, scores) || ranges_overlap(dx, tokens, logits, scores)))))
+        return MOE_ERR_INVALID_ARG;
     DeviceScope scope(ctx->device);
     if (!scope.ok) return MOE_ERR_CUDA;
     BackwardParams p = backward_params(ctx, T);
