@@ -534,6 +534,8 @@ class MoeRouter:
         self.device = torch.device(device)
         if self.device.type != "cuda":
             raise RuntimeError("MoeRouter needs a CUDA device; there is no CPU path")
+        if self.device.index is None:            # the device that is current now is the context's from here on
+            self.device = torch.device("cuda", torch.cuda.current_device())
         self._ctx = None
         self._latest = None      # what the context still points at: see _keep
         with torch.cuda.device(self.device):
@@ -618,8 +620,6 @@ class MoeRouter:
 
     # -- 4-bit rows: dispatch and the experts' products ----------------------
     def _index(self) -> int:
-        if self.device.index is None:
-            self.device = torch.device("cuda", torch.cuda.current_device())
         return self.device.index
 
     def mx_dispatch(self, logits: torch.Tensor, x: torch.Tensor, out: DispatchBuffers | None = None,

@@ -117,3 +117,18 @@ def test_a_step_is_refused_before_its_first_launch(router, args):
     with pytest.raises(B.MoeError):
         _step(router, **args)
     assert router.reached == []
+
+
+def test_a_router_stays_on_the_device_that_it_was_made_on(monkeypatch):
+    """device="cuda" means the device that is current when the context is made, not at the first 4-bit call."""
+    import contextlib
+    current = [1]
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: current[0])
+    monkeypatch.setattr(torch.cuda, "device", lambda d: contextlib.nullcontext())
+    monkeypatch.setattr(B.MoeRouter, "_stream", lambda self: 0)
+    monkeypatch.setattr(B, "moe_route_init", lambda *a: (B.MOE_OK, object()))
+    monkeypatch.setattr(B, "moe_route_destroy", lambda ctx: B.MOE_OK)
+    r = B.MoeRouter(B.make_config(E, K, H, 64, R, S), range(R * S), None, [1.0] * (R * S), device="cuda")
+    current[0] = 0
+    assert r._index() == 1 and r.device == torch.device("cuda", 1)
+    r.close()
