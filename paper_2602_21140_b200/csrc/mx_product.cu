@@ -150,9 +150,11 @@ __device__ __forceinline__ uint32_t lead_addr(uint64_t *bar)
     return r;
 }
 
-// Arrival at the first CTA's barrier.  What it announces lies in this CTA's shared memory or TMEM and has
-// been ordered before it (proxy fence, tcgen05 fence), so it needs no release over the cluster: that
-// one waits for the thread's loads and stores in global memory, which took 1500 cycles a stage here.
+// Arrival at the first CTA's barrier.  What it announces lies in this CTA's shared memory or TMEM, behind a proxy
+// fence or a tcgen05 fence, and is read there by asynchronous units alone.  The PTX memory model orders it for the
+// issuing thread of the other CTA only with a release of cluster scope, which also waits for this thread's loads and
+// stores in global memory (1500 cycles a stage here).  So this relies on how the hardware does it: the fence has
+// completed before the arrival leaves.  The tests compare pairs with single CTAs bit for bit.
 template <int CG>
 __device__ __forceinline__ void mbar_arrive_lead(uint64_t *bar)
 {
@@ -482,7 +484,8 @@ __device__ __forceinline__ void store_plain(const KernelParams &p, const CUtenso
 
 __device__ __forceinline__ float silu(float g)
 {
-    // both flush to zero: below g = -87 the result is 0 where the formula leaves less than 88 * 2^-126
+    // Both flush to zero: below g = -87.3, where the sigmoid is less than 2^-126, the result is 0.  (The formula in 32
+    // bits does the same from g = -88.7 on, where exp overflows.)
     float e, r;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(g * -1.44269504f));
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + e));
@@ -497,8 +500,8 @@ __device__ __forceinline__ float silu(float g)
 // fours by row % 2: no two lanes of a store or of a load of 16 bytes meet in a bank.  (Weight rows in their own
 // order, pairs in neighbouring lanes that trade a value by shuffle: 73.4 us instead of 71.4 for 4096 rows over 8 experts
 // of 4096 x 4096, 711 instead of 706 for 65536 over 16 of 7168 x 2048.)  Everything before the one rounding to 4 bits
-// is fp32; exp and the reciprocal are the hardware's approximations (2 and 1 units in the last place), far below a
-// 4-bit step.
+// is fp32; exp and the reciprocal are the hardware's approximations (2 and 1 units in the last place), and the rounded
+// argument of exp costs up to |g| 2^-24 relative besides, all far below a 4-bit step.
 __device__ __forceinline__ void store_gated(const KernelParams &p, const Tile &t, int c0, const uint32_t (&v)[32], float *buf,
                                             int group, int quarter, int lane)
 {
@@ -989,6 +992,11 @@ cudaError_t launch_for(const MxProductArgs &a, cudaStream_t st)
     // With few rows a slot the weights dominate, and a narrow tile of one CTA leaves shared memory for more
     // stages of them.  With many rows the products do, and a pair of CTAs halves what each holds of the row operand in
     // shared memory (a stage of 256 is written once and read once): 524 clocks a stage, of which the products need 448.
+    // Up to 64 rows a slot the two are within 5 % (32 slots of 8 to 64 rows, H 4096, 2048 features: gated 67.6-69.6 us
+    // narrow, 67.6-69.7 wide; down 38.9-41.2 and 38.9-41.0).  The host knows the buffer's rows but not the counts, so the
+    // mean over all slots, empty ones included, decides.  Where the rows fall on a few slots that costs up to half
+    // (n rows on 8 of 288 slots, H 7168, 2048 features, narrow and wide: gated 51.2 and 45.1 us for n = 1024, 125 and 72
+    // for 4096, 436 and 182 for 16384; down 32.8 and 28.7, 76 and 43, 256 and 105).
     if (a.rows <= 64ll * a.P) return launch<64, 7, 1, GATED>(a, st);
     return launch<224, 5, 2, GATED>(a, st);
 }
