@@ -161,8 +161,13 @@ __device__ __forceinline__ void route_backward(const BackwardParams &p, int t, i
 // token's rows coming while the present one ends.  Tokens are taken as CTAs get free, because SMs do not get
 // equal shares of HBM: dealt out in advance, the SMs were busy for 83 % of the kernel (combine, 8192 tokens of
 // 7168, k = 8: 350 us; 304 us like this, 6.56 TB/s).
+// Short rows are another matter: a slot holds one piece of one row whatever its length, one lane asks for the rows one
+// after the other, and at H = 512 at most 15 KB per CTA are in flight (share of the bytes' time at 300 MB of rows,
+// combine and dispatch: H = 512 k = 8 0.22 and 0.12, 1024 0.42 and 0.22, 2048 0.72 and 0.41, 4096 0.91 and 0.70).
 // Dot products are summed per thread, over the warp and over the warps, always in the same order.
-// K = top_k known at compile time, 0 = any.
+// K = top_k known at compile time, 0 = any: 8 and 2, the values of the framework's workloads, as in the combine.  The
+// variant for any k spills 8 bytes for combine and keeps up (H = 7168, share of the bytes' time: k = 1 0.87, 4 0.91, 6
+// 0.89 against 0.93 for 2 and 0.91 for 8).
 template <bool COMBINE, int K>
 __global__ void __launch_bounds__(backward_threads(COMBINE), 2) k_backward(BackwardParams p)
 {
