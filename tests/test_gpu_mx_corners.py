@@ -141,15 +141,20 @@ def test_launches_without_overlap():
     router.close()
 
 
-def _free(gib):
+@pytest.fixture
+def gib():
+    """gib(n): skip unless n GiB are free; what the test took goes back to the device afterwards."""
+    def need(n):
+        if torch.cuda.mem_get_info()[0] < n * 2 ** 30:
+            pytest.skip("not enough free device memory")
     torch.cuda.empty_cache()
-    if torch.cuda.mem_get_info()[0] < gib * 2 ** 30:
-        pytest.skip("not enough free device memory")
+    yield need
+    torch.cuda.empty_cache()
 
 
-def test_rows_past_32_bits():
+def test_rows_past_32_bits(gib):
     """9 GB of bf16 rows, 2.4 GB of codes; the last rows lie past 2^32 elements."""
-    _free(24)
+    gib(24)
     rows, K = 70000, 65536
     x = torch.zeros(rows, K, dtype=torch.bfloat16, device="cuda")
     at = [0, 32767, 32768, 65535, 65536, 69999]
@@ -164,9 +169,9 @@ def test_rows_past_32_bits():
     assert (x[1:32767] == 0).all() and (x[65537:69999] == 0).all()
 
 
-def test_products_past_32_bits():
+def test_products_past_32_bits(gib):
     """Weights of 4.3 GB, of which three slots are used, and 4.6 GB of y."""
-    _free(24)
+    gib(24)
     P, N, K, rows = 66, 32768, 4096, 70000
     r = B.MoeRouter(B.make_config(P, 1, 64, 16, P, 1, 1), range(P), None, [1.0] * P)
     w = B.MxRows(torch.full((P, N, K // 2), 0x22, dtype=torch.uint8, device="cuda"), torch.full((P, N, M.pitch(K)), 127, dtype=torch.uint8, device="cuda"))
@@ -206,9 +211,9 @@ def test_products_past_32_bits():
     r.close()
 
 
-def test_dispatch_and_gradients_past_32_bits():
+def test_dispatch_and_gradients_past_32_bits(gib):
     """A send buffer of 4.8 GB of codes, rows of 4.6 GB in the gradients."""
-    _free(60)
+    gib(60)
     E, k, H = 16, 8, 7168
     T = 42000
     r = B.MoeRouter(B.make_config(E, k, H, T, E, 1, 1), range(E), None, [1.0] * E)
