@@ -296,7 +296,7 @@ def _own(st):
         y = r.expert_ffn(st["rows"], st["counts"], st["offsets"], st["gate_up"], st["down"], z=z)
         return {"y": y, "z": B.mx8_dequantize(z) if c["kept"] == "8" else z}
     if c["op"] == "weight_grad":
-        return r.expert_weight_grad(st["d_out"], st["rows"], st["counts"], st["offsets"], dtype=getattr(torch, c["grad"]))
+        return r.expert_weight_backward(st["d_out"], st["rows"], st["counts"], st["offsets"], dtype=getattr(torch, c["grad"]))
     z = B.Mx8Rows(*st["z"]) if c["kept"] == "8" else st["z"]
     got = r.expert_ffn_backward(st["dy"], st["rows"], st["counts"], st["offsets"], st["gate_up"], st["down"], z)
     return dict(zip(("d_rows", "d_gate_up", "d_down"), got))
