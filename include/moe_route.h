@@ -409,6 +409,64 @@ moe_status moe_dispatch_backward(moe_ctx *ctx, const float *logits, const void *
                                  int32_t T, void *dx, float *d_logits, void *cuda_stream);
 
 /*
+ * ---- Experts in 16 bits and their gradients -------------------------------------------
+ * (No counterpart in the paper.)  The experts' gated feed-forward networks on bf16 rows, for serving them as they were
+ * trained and for training them: what lies between moe_dispatch and moe_combine, and between moe_combine_backward and
+ * moe_dispatch_backward.  Throughout,
+ *   rows, slot_counts, slot_offsets: as in moe_mx_expert_product.  Segments are cut at `rows` and must not overlap; rows
+ *     outside every segment are left as they are (outputs) and not looked at (inputs)
+ *   matrices: device bf16, one per physical slot, contiguous: [P, n_out, n_in].  The copies of an expert on several slots
+ *     are matrices of their own, and so are their gradients: training adds those up
+ * All sums are fp32 on the tensor cores and rounded once.  Feature counts are multiples of 8 (n_hidden of 16), at least that;
+ * buffers 16-byte aligned; INVALID_ARG otherwise, or if an output overlaps an input or another output.  CAPACITY if rows or features
+ * exceed 2^30.  Nothing is allocated, nothing waits; a bounded wait that gives up sets the context's device status.
+ *
+ * moe_expert_product — y[r, f] = sum_c a[r, c] * w[p, f, c]; a [rows, n_in] bf16, y [rows, n_out] bf16 out.
+ */
+moe_status moe_expert_product(moe_ctx *ctx, const void *a, int64_t rows, const int32_t *slot_counts, const int32_t *slot_offsets,
+                              const void *w, int32_t n_out, int32_t n_in, void *y, void *cuda_stream);
+
+/*
+ * moe_expert_gated — first half of a gated feed-forward expert: with z[r, f] = sum_c a[r, c] * w[p, f, c],
+ *   h[r, i] = silu(z[r, 2i]) * z[r, 2i + 1],  silu(g) = g / (1 + exp(-g))
+ *   w [P, 2 * n_hidden, n_in]: row 2i of a slot's matrix is the gate of feature i, row 2i + 1 its up-projection
+ *   h [rows, n_hidden] bf16 out
+ *   z, z_scales: what moe_expert_gated_backward needs.  Both NULL: nothing is kept.  z alone: [rows, 2 * n_hidden] bf16.
+ *     Both: 8-bit rows (moe_mx8_dequantize), codes [rows, 2 * n_hidden] and scales [rows, moe_mx_scale_pitch(2 * n_hidden)];
+ *     the padding of the scales is not written
+ */
+moe_status moe_expert_gated(moe_ctx *ctx, const void *a, int64_t rows, const int32_t *slot_counts, const int32_t *slot_offsets,
+                            const void *w, int32_t n_hidden, int32_t n_in, void *h, void *z, uint8_t *z_scales, void *cuda_stream);
+
+/*
+ * moe_expert_rows_backward — gradient of a product by its rows: da[r, c] = sum_f dy[r, f] * w[p, f, c];
+ * dy [rows, n_out] bf16, da [rows, n_in] bf16 out.
+ */
+moe_status moe_expert_rows_backward(moe_ctx *ctx, const void *dy, int64_t rows, const int32_t *slot_counts, const int32_t *slot_offsets,
+                                    const void *w, int32_t n_out, int32_t n_in, void *da, void *cuda_stream);
+
+/*
+ * moe_expert_gated_backward — through the down product and the gate: with dh[r, i] = sum_f dy[r, f] * w[p, f, i], the kept
+ * g = z[r, 2i] and u = z[r, 2i + 1], and s = 1 / (1 + exp(-g)),
+ *   dz[r, 2i] = dh * u * s * (1 + g * (1 - s)),  dz[r, 2i + 1] = dh * g * s      [rows, 2 * n_hidden] bf16 out
+ *   h[r, i] = g * s * u, once more, for the gradient of w                        [rows, n_hidden] bf16 out
+ *   dy [rows, n_out] bf16, w [P, n_out, n_hidden] the down matrices, z and z_scales as moe_expert_gated wrote them
+ *   (z_scales NULL: z is bf16)
+ */
+moe_status moe_expert_gated_backward(moe_ctx *ctx, const void *dy, int64_t rows, const int32_t *slot_counts, const int32_t *slot_offsets,
+                                     const void *w, int32_t n_out, int32_t n_hidden, const void *z, const uint8_t *z_scales, void *dz,
+                                     void *h, void *cuda_stream);
+
+/*
+ * moe_expert_weight_backward — gradient of a product by its matrices: dw[p, f, c] = sum over the slot's segment of
+ * dy[r, f] * a[r, c]; dy [rows, n_out] bf16, a [rows, n_in] bf16, dw [P, n_out, n_in] of `dtype` out (MOE_DTYPE_BF16 or
+ * MOE_DTYPE_F32).  Slots without rows get zeros.  add != 0 (fp32 only): the sums are added to what dw holds.
+ */
+moe_status moe_expert_weight_backward(moe_ctx *ctx, const void *dy, const void *a, int64_t rows, const int32_t *slot_counts,
+                                      const int32_t *slot_offsets, int32_t n_out, int32_t n_in, void *dw, int32_t dtype, int32_t add,
+                                      void *cuda_stream);
+
+/*
  * moe_step_host — one dispatch + combine fed from HOST memory, for callers
  * that hold activations on the CPU: copies logits and x to the given device
  * staging buffers, runs moe_dispatch and moe_combine (expert_buf = the send

@@ -51,6 +51,7 @@ EXPORTED_SYMBOLS = (
     "moe_set_tuning", "moe_debug_skip_ticket",
     "moe_mx_scale_pitch", "moe_mx_quantize", "moe_mx_dequantize", "moe_mx_dispatch", "moe_mx_expert_product",
     "moe_mx_expert_gated", "moe_combine_backward", "moe_dispatch_backward",
+    "moe_expert_product", "moe_expert_gated", "moe_expert_rows_backward", "moe_expert_gated_backward", "moe_expert_weight_backward",
 )
 
 
@@ -158,6 +159,16 @@ def _lib():
         lib.moe_combine_backward.argtypes = [vp, vp, vp, i32, vp, vp, vp]
         lib.moe_dispatch_backward.restype = ctypes.c_int
         lib.moe_dispatch_backward.argtypes = [vp, vp, vp, vp, i32, vp, vp, vp]
+        lib.moe_expert_product.restype = ctypes.c_int
+        lib.moe_expert_product.argtypes = [vp, vp, i64, vp, vp, vp, i32, i32, vp, vp]
+        lib.moe_expert_gated.restype = ctypes.c_int
+        lib.moe_expert_gated.argtypes = [vp, vp, i64, vp, vp, vp, i32, i32, vp, vp, vp, vp]
+        lib.moe_expert_rows_backward.restype = ctypes.c_int
+        lib.moe_expert_rows_backward.argtypes = [vp, vp, i64, vp, vp, vp, i32, i32, vp, vp]
+        lib.moe_expert_gated_backward.restype = ctypes.c_int
+        lib.moe_expert_gated_backward.argtypes = [vp, vp, i64, vp, vp, vp, i32, i32, vp, vp, vp, vp, vp]
+        lib.moe_expert_weight_backward.restype = ctypes.c_int
+        lib.moe_expert_weight_backward.argtypes = [vp, vp, vp, i64, vp, vp, i32, i32, vp, i32, i32, vp]
         lib.moe_status_string.restype = ctypes.c_char_p
         lib.moe_status_string.argtypes = [ctypes.c_int]
         _lib_handle = lib
@@ -388,6 +399,36 @@ def moe_dispatch_backward(ctx, logits_ptr: int, d_send_buf_ptr: int, d_weights_p
                                         d_logits_ptr or None, cuda_stream)
 
 
+def moe_expert_product(ctx, a_ptr: int, rows: int, slot_counts_ptr: int, slot_offsets_ptr: int, w_ptr: int, n_out: int, n_in: int,
+                       y_ptr: int, cuda_stream: int = 0) -> int:
+    return _lib().moe_expert_product(ctx, a_ptr, rows, slot_counts_ptr, slot_offsets_ptr, w_ptr, n_out, n_in, y_ptr, cuda_stream)
+
+
+def moe_expert_gated(ctx, a_ptr: int, rows: int, slot_counts_ptr: int, slot_offsets_ptr: int, w_ptr: int, n_hidden: int, n_in: int,
+                     h_ptr: int, z_ptr: int = 0, z_scales_ptr: int = 0, cuda_stream: int = 0) -> int:
+    """z_ptr and z_scales_ptr may both be 0 (nothing is kept), or z_scales_ptr alone (kept in bf16)."""
+    return _lib().moe_expert_gated(ctx, a_ptr, rows, slot_counts_ptr, slot_offsets_ptr, w_ptr, n_hidden, n_in, h_ptr, z_ptr or None,
+                                   z_scales_ptr or None, cuda_stream)
+
+
+def moe_expert_rows_backward(ctx, dy_ptr: int, rows: int, slot_counts_ptr: int, slot_offsets_ptr: int, w_ptr: int, n_out: int, n_in: int,
+                             da_ptr: int, cuda_stream: int = 0) -> int:
+    return _lib().moe_expert_rows_backward(ctx, dy_ptr, rows, slot_counts_ptr, slot_offsets_ptr, w_ptr, n_out, n_in, da_ptr, cuda_stream)
+
+
+def moe_expert_gated_backward(ctx, dy_ptr: int, rows: int, slot_counts_ptr: int, slot_offsets_ptr: int, w_ptr: int, n_out: int,
+                              n_hidden: int, z_ptr: int, z_scales_ptr: int, dz_ptr: int, h_ptr: int, cuda_stream: int = 0) -> int:
+    """z_scales_ptr may be 0: z is bf16."""
+    return _lib().moe_expert_gated_backward(ctx, dy_ptr, rows, slot_counts_ptr, slot_offsets_ptr, w_ptr, n_out, n_hidden, z_ptr,
+                                            z_scales_ptr or None, dz_ptr, h_ptr, cuda_stream)
+
+
+def moe_expert_weight_backward(ctx, dy_ptr: int, a_ptr: int, rows: int, slot_counts_ptr: int, slot_offsets_ptr: int, n_out: int,
+                               n_in: int, dw_ptr: int, dtype: int, add: int, cuda_stream: int = 0) -> int:
+    return _lib().moe_expert_weight_backward(ctx, dy_ptr, a_ptr, rows, slot_counts_ptr, slot_offsets_ptr, n_out, n_in, dw_ptr, dtype,
+                                             add, cuda_stream)
+
+
 def moe_route_destroy(ctx) -> int:
     return _lib().moe_route_destroy(ctx)
 
@@ -428,6 +469,18 @@ class MxRows:
         return 2 * self.codes.shape[-1]
 
 
+@dataclass
+class Mx8Rows:
+    """8-bit rows (format: include/moe_route.h), in which activations are kept for a backward pass: any leading
+    dimensions, contiguous."""
+    codes: torch.Tensor      # uint8 [..., cols]
+    scales: torch.Tensor     # uint8 [..., moe_mx_scale_pitch(cols)]
+
+    @property
+    def cols(self) -> int:
+        return self.codes.shape[-1]
+
+
 _DTYPE_CODE = {torch.bfloat16: MOE_DTYPE_BF16, torch.float16: MOE_DTYPE_F16, torch.float32: MOE_DTYPE_F32}
 
 
@@ -447,6 +500,13 @@ def _is_mx(m: MxRows, index: int, lead=None) -> bool:
     return (c.dtype is torch.uint8 and s.dtype is torch.uint8 and c.is_contiguous() and s.is_contiguous() and c.is_cuda and s.is_cuda
             and c.get_device() == index and s.get_device() == index and len(cs) > 0 and cs[-1] % 16 == 0 and cs[:-1] == ss[:-1]
             and ss[-1] == _mx_pitch(2 * cs[-1]) and (lead is None or cs[:-1] == lead))
+
+
+def _is_mx8(m: Mx8Rows, index: int, shape) -> bool:
+    """8-bit rows of the given logical shape on CUDA device `index`."""
+    shape = tuple(shape)
+    return (isinstance(m, Mx8Rows) and shape[-1] > 0 and shape[-1] % 32 == 0 and _is_dense(m.codes, torch.uint8, shape, index)
+            and _is_dense(m.scales, torch.uint8, (*shape[:-1], _mx_pitch(shape[-1])), index))
 
 
 def _is_dense(t: torch.Tensor, dtype: torch.dtype, shape, index: int) -> bool:
@@ -473,6 +533,14 @@ def mx_empty(*shape, device="cuda") -> MxRows:
     _require(cols > 0 and cols % 32 == 0, "mx_empty")
     return MxRows(torch.empty((*lead, cols // 2), dtype=torch.uint8, device=device),
                   torch.empty((*lead, _mx_pitch(cols)), dtype=torch.uint8, device=device))
+
+
+def mx8_empty(*shape, device="cuda") -> Mx8Rows:
+    """Uninitialised 8-bit rows of the given shape (last dimension: elements of a row)."""
+    lead, cols = shape[:-1], shape[-1]
+    _require(cols > 0 and cols % 32 == 0, "mx8_empty")
+    return Mx8Rows(torch.empty((*lead, cols), dtype=torch.uint8, device=device),
+                   torch.empty((*lead, _mx_pitch(cols)), dtype=torch.uint8, device=device))
 
 
 def _mx_like(x: torch.Tensor, lead, cols: int) -> MxRows:
@@ -765,6 +833,131 @@ class MoeRouter:
         if st != MOE_OK:
             raise MoeError(st, "moe_dispatch_backward")
         return dx, d_logits
+
+    # -- experts in 16 bits and their gradients --------------------------------
+    def _expert_ok(self, rows: torch.Tensor, cols: int, slot_counts, slot_offsets, weight: torch.Tensor, dev: int) -> bool:
+        """Rows [n, cols] and one matrix [P, n_out, n_in] per slot, in bf16."""
+        P = self.num_slots
+        return (rows.dim() == 2 and weight.dim() == 3 and weight.shape[0] == P and _is_dense(rows, torch.bfloat16, (rows.shape[0], cols), dev)
+                and _is_dense(weight, torch.bfloat16, weight.shape, dev) and self._slots_ok(slot_counts, slot_offsets, dev))
+
+    def _slots_ok(self, slot_counts: torch.Tensor, slot_offsets: torch.Tensor, dev: int) -> bool:
+        P = self.num_slots
+        return (_is_dense(slot_counts, torch.int32, (P,), dev) and slot_offsets.dim() == 1 and slot_offsets.shape[0] >= P
+                and _is_dense(slot_offsets, torch.int32, slot_offsets.shape, dev))
+
+    @staticmethod
+    def _kept_ok(z, n: int, cols: int, dev: int) -> bool:
+        return _is_mx8(z, dev, (n, cols)) if isinstance(z, Mx8Rows) else _is_dense(z, torch.bfloat16, (n, cols), dev)
+
+    @staticmethod
+    def _kept_ptrs(z):
+        return (z.codes.data_ptr(), z.scales.data_ptr()) if isinstance(z, Mx8Rows) else (0 if z is None else z.data_ptr(), 0)
+
+    def expert_product(self, rows: torch.Tensor, slot_counts: torch.Tensor, slot_offsets: torch.Tensor, weight: torch.Tensor,
+                       y: torch.Tensor | None = None) -> torch.Tensor:
+        """y[r] = weight[slot of r] @ rows[r]: weight [P, n_out, cols], rows [n, cols], y [n, n_out], all bf16."""
+        dev = self._index()
+        _require(weight.dim() == 3 and self._expert_ok(rows, weight.shape[2], slot_counts, slot_offsets, weight, dev), "expert_product")
+        n, (_, n_out, n_in) = rows.shape[0], weight.shape
+        if y is None:
+            y = rows.new_empty((n, n_out))
+        else:
+            _require(_is_dense(y, torch.bfloat16, (n, n_out), dev), "expert_product")
+        st = moe_expert_product(self._ctx, rows.data_ptr(), n, slot_counts.data_ptr(), slot_offsets.data_ptr(), weight.data_ptr(), n_out,
+                                n_in, y.data_ptr(), _raw_stream(dev))
+        if st != MOE_OK:
+            raise MoeError(st, "moe_expert_product")
+        return y
+
+    def expert_gated(self, rows: torch.Tensor, slot_counts: torch.Tensor, slot_offsets: torch.Tensor, gate_up: torch.Tensor,
+                     h: torch.Tensor | None = None, z: "torch.Tensor | Mx8Rows | None" = None) -> torch.Tensor:
+        """silu(gate) * up [n, n_hidden].  gate_up [P, 2 * n_hidden, cols]: row 2i is the gate of feature i, row 2i + 1 its
+        up-projection.  ``z`` [n, 2 * n_hidden]: bf16 or 8-bit rows that keep the projections for the backward pass."""
+        dev = self._index()
+        _require(gate_up.dim() == 3 and gate_up.shape[1] % 32 == 0
+                 and self._expert_ok(rows, gate_up.shape[2], slot_counts, slot_offsets, gate_up, dev), "expert_gated")
+        n, (_, cols, n_in) = rows.shape[0], gate_up.shape
+        if h is None:
+            h = rows.new_empty((n, cols // 2))
+        _require(_is_dense(h, torch.bfloat16, (n, cols // 2), dev) and (z is None or self._kept_ok(z, n, cols, dev)), "expert_gated")
+        st = moe_expert_gated(self._ctx, rows.data_ptr(), n, slot_counts.data_ptr(), slot_offsets.data_ptr(), gate_up.data_ptr(),
+                              cols // 2, n_in, h.data_ptr(), *self._kept_ptrs(z), _raw_stream(dev))
+        if st != MOE_OK:
+            raise MoeError(st, "moe_expert_gated")
+        return h
+
+    def expert_ffn(self, rows: torch.Tensor, slot_counts: torch.Tensor, slot_offsets: torch.Tensor, gate_up: torch.Tensor,
+                   down: torch.Tensor, y: torch.Tensor | None = None, h: torch.Tensor | None = None,
+                   z: "torch.Tensor | Mx8Rows | None" = None) -> torch.Tensor:
+        """The gated feed-forward expert of every slot on its rows: expert_gated, then expert_product."""
+        h = self.expert_gated(rows, slot_counts, slot_offsets, gate_up, h, z)
+        return self.expert_product(h, slot_counts, slot_offsets, down, y)
+
+    def expert_rows_backward(self, dy: torch.Tensor, slot_counts: torch.Tensor, slot_offsets: torch.Tensor, weight: torch.Tensor,
+                             d_rows: torch.Tensor | None = None) -> torch.Tensor:
+        """Gradient of expert_product by its rows: dy [n, n_out] -> [n, cols]."""
+        dev = self._index()
+        _require(weight.dim() == 3 and self._expert_ok(dy, weight.shape[1], slot_counts, slot_offsets, weight, dev), "expert_rows_backward")
+        n, (_, n_out, n_in) = dy.shape[0], weight.shape
+        if d_rows is None:
+            d_rows = dy.new_empty((n, n_in))
+        else:
+            _require(_is_dense(d_rows, torch.bfloat16, (n, n_in), dev), "expert_rows_backward")
+        st = moe_expert_rows_backward(self._ctx, dy.data_ptr(), n, slot_counts.data_ptr(), slot_offsets.data_ptr(), weight.data_ptr(),
+                                      n_out, n_in, d_rows.data_ptr(), _raw_stream(dev))
+        if st != MOE_OK:
+            raise MoeError(st, "moe_expert_rows_backward")
+        return d_rows
+
+    def expert_gated_backward(self, dy: torch.Tensor, slot_counts: torch.Tensor, slot_offsets: torch.Tensor, down: torch.Tensor,
+                              z: "torch.Tensor | Mx8Rows", dz: torch.Tensor | None = None, h: torch.Tensor | None = None):
+        """From the gradient of an expert's output [n, n_out] and the kept projections: (dz [n, 2 * n_hidden], h [n, n_hidden]),
+        the projections' gradient and the hidden rows of the forward pass."""
+        dev = self._index()
+        _require(down.dim() == 3 and down.shape[2] % 16 == 0 and self._expert_ok(dy, down.shape[1], slot_counts, slot_offsets, down, dev),
+                 "expert_gated_backward")
+        n, (_, n_out, n_hidden) = dy.shape[0], down.shape
+        dz = dy.new_empty((n, 2 * n_hidden)) if dz is None else dz
+        h = dy.new_empty((n, n_hidden)) if h is None else h
+        _require(_is_dense(dz, torch.bfloat16, (n, 2 * n_hidden), dev) and _is_dense(h, torch.bfloat16, (n, n_hidden), dev)
+                 and self._kept_ok(z, n, 2 * n_hidden, dev), "expert_gated_backward")
+        st = moe_expert_gated_backward(self._ctx, dy.data_ptr(), n, slot_counts.data_ptr(), slot_offsets.data_ptr(), down.data_ptr(),
+                                       n_out, n_hidden, *self._kept_ptrs(z), dz.data_ptr(), h.data_ptr(), _raw_stream(dev))
+        if st != MOE_OK:
+            raise MoeError(st, "moe_expert_gated_backward")
+        return dz, h
+
+    def expert_weight_backward(self, dy: torch.Tensor, rows: torch.Tensor, slot_counts: torch.Tensor, slot_offsets: torch.Tensor,
+                               d_weight: torch.Tensor | None = None, add: bool = False, dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
+        """Gradient of expert_product by its matrices: dy [n, n_out], rows [n, cols] -> [P, n_out, cols] in bf16 or fp32 (``dtype``
+        where no ``d_weight`` is given); with ``add`` (fp32) added to ``d_weight``.  Copies of one expert have one each."""
+        dev, P = self._index(), self.num_slots
+        _require(dy.dim() == 2 and rows.dim() == 2 and _is_dense(dy, torch.bfloat16, dy.shape, dev)
+                 and _is_dense(rows, torch.bfloat16, (dy.shape[0], rows.shape[1]), dev) and self._slots_ok(slot_counts, slot_offsets, dev)
+                 and not (add and d_weight is None), "expert_weight_backward")
+        shape = (P, dy.shape[1], rows.shape[1])
+        if d_weight is None:
+            _require(dtype in (torch.bfloat16, torch.float32), "expert_weight_backward")
+            d_weight = dy.new_empty(shape, dtype=dtype)
+        _require(d_weight.dtype in (torch.bfloat16, torch.float32) and _is_dense(d_weight, d_weight.dtype, shape, dev), "expert_weight_backward")
+        st = moe_expert_weight_backward(self._ctx, dy.data_ptr(), rows.data_ptr(), dy.shape[0], slot_counts.data_ptr(),
+                                        slot_offsets.data_ptr(), shape[1], shape[2], d_weight.data_ptr(), _DTYPE_CODE[d_weight.dtype],
+                                        int(add), _raw_stream(dev))
+        if st != MOE_OK:
+            raise MoeError(st, "moe_expert_weight_backward")
+        return d_weight
+
+    def expert_ffn_backward(self, dy: torch.Tensor, rows: torch.Tensor, slot_counts: torch.Tensor, slot_offsets: torch.Tensor,
+                            gate_up: torch.Tensor, down: torch.Tensor, z: "torch.Tensor | Mx8Rows", d_rows: torch.Tensor | None = None,
+                            d_gate_up: torch.Tensor | None = None, d_down: torch.Tensor | None = None, add: bool = False,
+                            grad_dtype: torch.dtype = torch.bfloat16):
+        """Gradients of expert_ffn with the projections ``z`` that it kept: (d_rows, d_gate_up, d_down).  ``add``: as in
+        expert_weight_backward, for both matrices."""
+        dz, h = self.expert_gated_backward(dy, slot_counts, slot_offsets, down, z)
+        d_down = self.expert_weight_backward(dy, h, slot_counts, slot_offsets, d_down, add, grad_dtype)
+        d_gate_up = self.expert_weight_backward(dz, rows, slot_counts, slot_offsets, d_gate_up, add, grad_dtype)
+        return self.expert_rows_backward(dz, slot_counts, slot_offsets, gate_up, d_rows), d_gate_up, d_down
 
     # -- expert parallelism over several GPUs -------------------------------
     def ep_attach(self, world: int, rank: int, recv_buf_ptrs, recv_rows: int) -> None:

@@ -1,0 +1,832 @@
+// The experts' products on bf16 rows and their gradients, on tcgen05.mma kind::f16 (fp32 accumulation).  For every physical
+// slot p and the rows r of its segment:
+//     kProduct         y[r, n] = sum_k a[r, k] w[p, n, k]
+//     kGated           the same sums z over the pairs of rows 2i, 2i + 1 of w, and h[r, i] = silu(z[2i]) z[2i + 1]
+//     kTransposed      y[r, n] = sum_k a[r, k] w[p, k, n]                       (gradient by the rows)
+//     kGatedBackward   the same sums dh, and with g = z[2i], u = z[2i + 1], s = 1 / (1 + exp(-g)):
+//                      dz[2i] = dh u s (1 + g (1 - s)), dz[2i + 1] = dh g s, h = g s u
+//     kWeightGrad      y[p, m, n] = sum_r a[r, m] b[r, n]                       (gradient by the weights)
+//
+// Weights are the M operand and rows the N operand of the first four, so a segment costs its own length rounded up to 16 or 32,
+// from one token to hundreds, and a tile's accumulator is [128 lanes = features] x [columns = rows] in TMEM.  The weight
+// gradient has the features of a as M, those of b as N, and rows as K.  K goes in stages of 64: a K-major operand (w, a of
+// the products) has 128 bytes of a row, one 128-byte swizzle span; an operand that runs along M or N in memory (w of the
+// transposed products, both of the weight gradient) has 64 lines of 64 features, with the same swizzle.
+//
+// One persistent CTA per SM, or a pair of CTAs per two SMs on one MMA (cta_group::2):
+//   warps 0-7   epilogue, two groups of four (a warp reads one quarter of the TMEM lanes): TMEM -> registers ->
+//               shared memory -> HBM, 32 columns at a time, the groups taking turns
+//   warp 8      TMA loads
+//   warp 9      the MMAs, from one thread
+// The accumulator is double buffered, so the epilogue of a tile runs under the products of the next.
+#include "expert_product.h"
+
+#include <algorithm>
+#include <mutex>
+
+#include "mx8_format.cuh"
+#include "tcgen05.cuh"
+
+namespace {
+
+using namespace moe;
+
+constexpr int kFeat = 128;                 // features (M) per CTA and tile
+constexpr int kStageK = 64;                // elements of K per stage
+constexpr int kLine = 128;                 // bytes of a line of an operand tile: 64 elements
+constexpr int kChunk = 64 * kLine;         // 64 features x 64 K of an operand that runs along its features
+constexpr int kATile = kFeat * kLine;      // 16 KB
+constexpr int kEpiWarps = 8, kTmaWarp = kEpiWarps, kMmaWarp = kEpiWarps + 1, kThreads = 32 * (kEpiWarps + 2);
+constexpr int kMaxStages = 10;
+constexpr int kBand = 8;                   // tiles of rows (or of n) that are worked on side by side, see tile_at
+
+// ------------------------------------------------------------------ tcgen05 in PTX (the rest: tcgen05.cuh)
+
+template <int CG>
+__device__ __forceinline__ void mma_bf16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool accumulate)
+{
+    if (CG == 1)
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                     "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc),
+                     "r"((uint32_t)accumulate)
+                     : "memory");
+    else
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                     "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc),
+                     "r"((uint32_t)accumulate)
+                     : "memory");
+}
+
+// 32 lanes x 32 columns: v[c] is column c of lane threadIdx.x % 32
+__device__ __forceinline__ void tmem_ld_lanes(uint32_t addr, uint32_t (&r)[32])
+{
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, "
+        "%19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]),
+          "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]),
+          "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(addr));
+}
+
+// As mbar_try_wait, for a barrier that a thread of the other CTA arrives on.
+__device__ __forceinline__ bool mbar_try_wait_cluster(uint64_t *bar, unsigned parity)
+{
+    unsigned ok;
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                 : "=r"(ok) : "r"(smem_addr(bar)), "r"(parity) : "memory");
+    return ok != 0;
+}
+
+__device__ __forceinline__ void mbar_arrive_lead_release(uint64_t *bar)
+{
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(lead_addr<2>(bar)) : "memory");
+}
+
+// Shared-memory matrix descriptors: start and strides in 16-byte units, version 1 (sm_100), 128-byte swizzle.
+// Along K: eight rows of 128 bytes are an atom, atoms 1024 bytes apart.  Along M or N: eight lines (K) of 64 elements
+// are an atom, the next eight of K 1024 bytes on, the next 64 elements a chunk on.
+template <bool ALONG_K>
+__device__ __forceinline__ uint64_t desc_tile(uint32_t addr)
+{
+    const uint64_t lead = ALONG_K ? 1 : kChunk >> 4;
+    return (uint64_t)((addr >> 4) & 0x3fffu) | (lead << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61);
+}
+// bytes from one K = 16 of a tile to the next, in the descriptor's units
+template <bool ALONG_K>
+constexpr uint32_t kDescStep = (ALONG_K ? 16 * 2 : 16 * kLine) >> 4;
+
+// Instruction descriptor of kind::f16: fp32 accumulators (1 at bit 4), A and B bf16 (1 at 7 and 10), operands that run
+// along M or N (15 and 16), N / 8 at bit 17, M / 16 at bit 24.
+template <int CG, bool A_ALONG_K, bool B_ALONG_K>
+__device__ __forceinline__ uint32_t idesc_bf16(int n)
+{
+    return (1u << 4) | (1u << 7) | (1u << 10) | (A_ALONG_K ? 0u : 1u << 15) | (B_ALONG_K ? 0u : 1u << 16) | ((uint32_t)(n >> 3) << 17) |
+           ((uint32_t)(CG * kFeat >> 4) << 24);
+}
+
+// ------------------------------------------------------------------------ tiles
+
+struct KernelParams {
+    const int32_t *slot_counts, *slot_offsets;
+    long long rows;
+    int P, N, K, M;
+    int stages;
+    __nv_bfloat16 *y;              // kGated, kGatedBackward: h
+    void *z;
+    uint8_t *z_scales;
+    __nv_bfloat16 *dz;
+    int add;
+    Control *ctl;
+    unsigned spin_limit;
+};
+
+// feat: first feature (M) of the tile; row, rows: first row and rows, of the tile (products) or of its whole segment (weight
+// gradient); col: first column of a weight gradient's tile
+struct Tile {
+    int slot, feat, row, rows, col;
+};
+
+// Rows of slot p that can be worked on: counts and offsets come from device memory, so a segment
+// that leaves the row buffer is cut (or dropped) instead of followed.
+__device__ __forceinline__ int segment(const KernelParams &p, int s, int &first)
+{
+    first = __ldg(p.slot_offsets + s);
+    const long long c = __ldg(p.slot_counts + s);
+    if (first < 0 || c <= 0 || first >= p.rows) return 0;
+    return (int)min(c, p.rows - first);
+}
+
+// A segment of c rows is cut into the fewest tiles of at most NT rows, of equal size (to whole pieces of the
+// epilogue, 32 rows: only a segment's last tile leaves part of one).
+template <int NT>
+__device__ __forceinline__ int row_tiles(int c) { return (c + NT - 1) / NT; }
+
+// Neighbours in the order of the tiles run at the same time and share what they read through L2.  So the nt tiles of
+// rows of a slot are dealt in bands of kBand, and in a band all feature tiles one after the other, rows innermost: 74
+// pairs work on 8 tiles of rows by 9 of features, and a band's rows stay in L2 while the weights go by.  (All rows of a
+// segment innermost would read the rows from HBM again for every tile of features, once they outgrow L2.)
+__device__ __forceinline__ void in_bands(int local, int feats, int nt, int &f, int &r)
+{
+    const int band = local / (feats * kBand), wide = min(kBand, nt - band * kBand);
+    local -= band * feats * kBand;
+    f = local / wide;
+    r = band * kBand + local - f * wide;
+}
+
+template <ExpertOp OP, int NT, int CG>
+__device__ __forceinline__ Tile tile_at(const KernelParams &p, const int *ends, int index)
+{
+    Tile t;
+    int f, r;
+    if (OP == ExpertOp::kWeightGrad) {
+        const int mt = (p.M + CG * kFeat - 1) / (CG * kFeat), nt = (p.N + NT - 1) / NT;
+        t.slot = index / (mt * nt);
+        in_bands(index - t.slot * mt * nt, mt, nt, f, r);
+        t.rows = segment(p, t.slot, t.row);
+        t.feat = f * (CG * kFeat); t.col = r * NT;
+        return t;
+    }
+    int lo = 0, hi = p.P - 1;                        // first slot whose inclusive end is beyond the index
+#pragma unroll 1
+    while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (ends[mid] > index) hi = mid; else lo = mid + 1;
+    }
+    int first;
+    const int c = segment(p, lo, first), nt = row_tiles<NT>(c), size = ((c + nt - 1) / nt + 31) & ~31;
+    in_bands(index - (lo ? ends[lo - 1] : 0), (p.N + CG * kFeat - 1) / (CG * kFeat), nt, f, r);
+    t.slot = lo; t.feat = f * (CG * kFeat); t.col = 0;
+    t.row = first + r * size;
+    t.rows = min(size, c - r * size);                // may be <= 0 for the last tile of an uneven cut
+    return t;
+}
+
+// N of a tile's MMAs: its rows (weight gradient: columns) rounded up to what the instruction takes
+template <ExpertOp OP, int NT, int CG>
+__device__ __forceinline__ int tile_n(const KernelParams &p, const Tile &t)
+{
+    const int n = OP == ExpertOp::kWeightGrad ? min(NT, p.N - t.col) : t.rows;
+    return (n + 16 * CG - 1) & -(16 * CG);
+}
+
+// The tiles of a CTA (or pair of CTAs) of a grid of `step`, first, first + step, ..., as a warp sees them.  Finding a
+// tile is a chain of dependent reads, so the lanes find the next 32 of them side by side and hand them out one by one.
+// The fields and the verdict are in uniform registers (a warp reduction writes those): what tcgen05 and TMA
+// instructions take comes from uniform registers.
+template <ExpertOp OP, int NT, int CG>
+struct TileStream {
+    const KernelParams &p;
+    const int *ends;
+    const int tiles;
+    int base, at;
+    Tile mine;
+    __device__ TileStream(const KernelParams &p_, const int *ends_, int tiles_)
+        : p(p_), ends(ends_), tiles(tiles_), base(blockIdx.x / CG), at(32), mine{}
+    {
+    }
+    __device__ bool next(Tile &t)                    // false when there are no more
+    {
+        while (true) {
+            if (at == 32) {
+                if (base >= tiles) return false;
+                const int step = (int)gridDim.x / CG, i = base + (int)(threadIdx.x & 31) * step;
+                mine.rows = 0; mine.slot = -1;
+                if (i < tiles) mine = tile_at<OP, NT, CG>(p, ends, i);
+                base += 32 * step;
+                at = 0;
+                __syncwarp();
+            }
+            const int slot = __shfl_sync(0xffffffffu, mine.slot, at);
+            t.feat = (int)__reduce_max_sync(0xffffffffu, (unsigned)__shfl_sync(0xffffffffu, mine.feat, at));
+            t.row = (int)__reduce_max_sync(0xffffffffu, (unsigned)__shfl_sync(0xffffffffu, mine.row, at));
+            t.col = (int)__reduce_max_sync(0xffffffffu, (unsigned)__shfl_sync(0xffffffffu, mine.col, at));
+            t.rows = __reduce_max_sync(0xffffffffu, __shfl_sync(0xffffffffu, mine.rows, at));
+            ++at;
+            if (!__any_sync(0xffffffffu, slot >= 0)) return false;
+            t.slot = (int)__reduce_max_sync(0xffffffffu, (unsigned)slot);
+            // a slot without rows has no tiles of products, and a gradient of zeros
+            if (OP == ExpertOp::kWeightGrad || t.rows > 0) return true;
+        }
+    }
+};
+
+template <ExpertOp OP, int NT, int CG>
+struct Layout {
+    static constexpr bool kGrad = OP == ExpertOp::kWeightGrad;
+    static constexpr bool kAAlongK = OP == ExpertOp::kProduct || OP == ExpertOp::kGated;   // see desc_tile
+    static constexpr bool kBAlongK = !kGrad;
+    static constexpr int kN = NT / CG;                        // rows (or columns) of a tile in this CTA
+    static constexpr int kBTile = kN * kLine;
+    static constexpr int kStage = kATile + kBTile;            // multiples of 1024: swizzle alignment
+    static constexpr int kEpiWarp = 32 * 32 * 4;              // a plane of fp32 sums, or a box of a weight gradient
+    static constexpr int kBars = 3 * kMaxStages + 5;
+    static constexpr int kEpiOff = 0, kBarOff = kEpiWarps * kEpiWarp;
+    static constexpr int kEndsOff = kBarOff + ((kBars * 8 + 16 + 4 * (kThreads / 32) + 15) & ~15);
+    static constexpr int kSmem = 227 * 1024;
+    static size_t fixed(int P) { return (kEndsOff + (kGrad ? 0 : (size_t)P * 4) + 1023) / 1024 * 1024; }
+    static int stages(int P) { return std::min<int>(kMaxStages, (int)((kSmem - 1024 - fixed(P)) / kStage)); }
+    static size_t bytes(int P) { return 1024 + fixed(P) + (size_t)stages(P) * kStage; }
+};
+
+// Bounded wait.  `quit` is shared by the CTA: the first role that gives up sets it, the others follow.
+template <bool CLUSTER = false>
+__device__ __forceinline__ bool wait_for(uint64_t *bar, unsigned parity, volatile int *quit, unsigned limit)
+{
+    unsigned spins = 0;
+    while (!(CLUSTER ? mbar_try_wait_cluster(bar, parity) : mbar_try_wait(bar, parity))) {
+        if (++spins > limit || ((spins & 63u) == 0 && *quit)) { *quit = 1; return false; }
+    }
+    return true;
+}
+
+// ---------------------------------------------------------------------- epilogue
+
+// s = 1 / (1 + exp(-g)), by the hardware's exp and reciprocal (2 and 1 units in the last place; the rounded argument of
+// exp costs up to |g| 2^-24 relative besides: far below the bf16 that its results are rounded to).  Both flush to zero: below
+// g = -87.3, where s is less than 2^-126, it is 0.  (The formula in 32 bits does the same from g = -88.7 on.)
+__device__ __forceinline__ float sigmoid(float g)
+{
+    float e, r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(g * -1.44269504f));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + e));
+    return r;
+}
+
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b)
+{
+    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
+
+// A warp's 32 features x 32 rows, turned round in shared memory: lane l of the accumulator is a feature, and afterwards
+// lane l holds eight neighbouring features of row 8 i + l / 4, so that four lanes have 32 features of a row in a run.
+// The 16-byte units of a row are permuted by the row, so that neither the stores (32 lanes of one row) nor the loads of 16
+// bytes (two rows, every other unit) meet in a bank.
+__device__ __forceinline__ void write_plane(float *plane, const uint32_t (&v)[32], int lane)
+{
+#pragma unroll
+    for (int r = 0; r < 32; ++r) plane[r * 32 + (lane ^ ((r & 7) << 2))] = __uint_as_float(v[r]);
+    __syncwarp();
+}
+
+__device__ __forceinline__ void read_eight(const float *plane, int i, int lane, float (&x)[8])
+{
+    const float4 *row = reinterpret_cast<const float4 *>(plane + (8 * i + (lane >> 2)) * 32);
+    const int unit = ((lane & 3) * 2) ^ (lane >> 2);           // row % 8 = lane / 4
+    const float4 a = row[unit], b = row[unit ^ 1];
+    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+}
+
+// f: first of the warp's features, left: rows of the segment from the piece's first one, `row`, on.  The fp32 sums
+// are rounded once.
+__device__ __forceinline__ void store_rows(const KernelParams &p, const float *plane, int f, long long row, int left, int lane)
+{
+    f += (lane & 3) * 8;
+    if (f >= p.N) return;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int r = 8 * i + (lane >> 2);
+        float x[8];
+        read_eight(plane, i, lane, x);
+        if (r < left)
+            *reinterpret_cast<uint4 *>(p.y + (row + r) * p.N + f) =
+                make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
+    }
+}
+
+// SwiGLU of 16 pairs x 32 rows, and the sums themselves where they are kept, in bf16 or in 8 bits (the warp's 32 sums of a
+// row are one block).
+__device__ __forceinline__ void store_gated(const KernelParams &p, const float *plane, int f, long long row, int left, int lane)
+{
+    const bool inside = f < p.N;                               // N is a multiple of 32: all of the block or nothing
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int r = 8 * i + (lane >> 2), at = f + (lane & 3) * 8;
+        float x[8];
+        read_eight(plane, i, lane, x);
+        uint32_t amax = mx8_amax(x);                           // before anything is masked: all lanes take part
+        amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
+        amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
+        if (r >= left || !inside) continue;
+        float h[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) h[q] = x[2 * q] * sigmoid(x[2 * q]) * x[2 * q + 1];
+        *reinterpret_cast<uint2 *>(p.y + (row + r) * (p.N / 2) + at / 2) = make_uint2(pack_bf16(h[0], h[1]), pack_bf16(h[2], h[3]));
+        if (p.z_scales) {
+            const uint32_t s = mx8_scale_byte(amax);
+            *reinterpret_cast<uint2 *>(static_cast<uint8_t *>(p.z) + (row + r) * p.N + at) = mx8_quantize8(x, s);
+            if ((lane & 3) == 0) p.z_scales[(row + r) * mx_scale_pitch(p.N) + f / kMxBlock] = (uint8_t)s;
+        } else if (p.z) {
+            *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(p.z) + (row + r) * p.N + at) =
+                make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
+        }
+    }
+}
+
+// The kept sums of eight features (16 of them) of a row, asked for before the product of the piece is there.
+struct Kept {
+    uint4 v[2];
+    uint32_t s;
+};
+
+__device__ __forceinline__ void load_kept(const KernelParams &p, int f, long long row, int left, int lane, Kept (&k)[4])
+{
+    const int at = 2 * (f + (lane & 3) * 8), cols = 2 * p.N;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int r = 8 * i + (lane >> 2);
+        k[i].v[0] = k[i].v[1] = make_uint4(0u, 0u, 0u, 0u);
+        k[i].s = 0u;
+        if (r >= left || at >= cols) continue;
+        if (p.z_scales) {
+            k[i].v[0] = __ldg(reinterpret_cast<const uint4 *>(static_cast<const uint8_t *>(p.z) + (row + r) * cols + at));
+            k[i].s = __ldg(p.z_scales + (row + r) * mx_scale_pitch(cols) + at / kMxBlock);
+        } else {
+            const uint4 *src = reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(p.z) + (row + r) * cols + at);
+            k[i].v[0] = __ldg(src);
+            k[i].v[1] = __ldg(src + 1);
+        }
+    }
+}
+
+// Gradient of SwiGLU for 32 features x 32 rows, and its output once more for the gradient of the down matrix.
+__device__ __forceinline__ void store_gated_backward(const KernelParams &p, const float *plane, int f, long long row, int left, int lane,
+                                                     const Kept (&k)[4])
+{
+    f += (lane & 3) * 8;
+    if (f >= p.N) return;                                      // N is a multiple of 16
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int r = 8 * i + (lane >> 2);
+        if (r >= left) continue;
+        float dh[8], z[16], h[8];
+        read_eight(plane, i, lane, dh);
+        if (p.z_scales) {
+            const float scale = mx_scale_value(k[i].s);
+            const uint32_t c[4] = {k[i].v[0].x, k[i].v[0].y, k[i].v[0].z, k[i].v[0].w};
+#pragma unroll
+            for (int q = 0; q < 4; ++q) mx8_unpack4(c[q], z + 4 * q);
+#pragma unroll
+            for (int q = 0; q < 16; ++q) z[q] *= scale;
+        } else {
+            const uint32_t c[8] = {k[i].v[0].x, k[i].v[0].y, k[i].v[0].z, k[i].v[0].w, k[i].v[1].x, k[i].v[1].y, k[i].v[1].z, k[i].v[1].w};
+#pragma unroll
+            for (int q = 0; q < 8; ++q) { z[2 * q] = __uint_as_float(c[q] << 16); z[2 * q + 1] = __uint_as_float(c[q] & 0xffff0000u); }
+        }
+        uint32_t d[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+            const float g = z[2 * q], u = z[2 * q + 1], s = sigmoid(g), a = g * s;
+            h[q] = a * u;
+            d[q] = pack_bf16(dh[q] * u * s * (1.0f + g * (1.0f - s)), dh[q] * a);
+        }
+        uint4 *dst = reinterpret_cast<uint4 *>(p.dz + (row + r) * (2 * p.N) + 2 * f);
+        dst[0] = make_uint4(d[0], d[1], d[2], d[3]);
+        dst[1] = make_uint4(d[4], d[5], d[6], d[7]);
+        *reinterpret_cast<uint4 *>(p.y + (row + r) * p.N + f) =
+            make_uint4(pack_bf16(h[0], h[1]), pack_bf16(h[2], h[3]), pack_bf16(h[4], h[5]), pack_bf16(h[6], h[7]));
+    }
+}
+
+// 32 features x 32 (fp32) or 64 (bf16) columns of a weight gradient leave as one TMA store from a box of 32 lines of
+// 128 bytes, 128-byte swizzle; what lies outside the matrix is cut by the store.  An addition is done by the memory
+// system, one for each element, so its order is no question.
+template <bool F32>
+__device__ __forceinline__ void store_grad(const KernelParams &p, const CUtensorMap *map, const Tile &t, int f, int col, const uint4 (&v)[8],
+                                           unsigned char *box, int lane)
+{
+    if (lane == 0) bulk_wait_read<0>();                        // the store before has left the box
+    __syncwarp();
+#pragma unroll
+    for (int q = 0; q < 8; ++q) *reinterpret_cast<uint4 *>(box + lane * kLine + ((q ^ (lane & 7)) << 4)) = v[q];
+    fence_async_shared();
+    __syncwarp();
+    if (lane == 0) {
+        if (F32 && p.add)
+            asm volatile("cp.reduce.async.bulk.tensor.3d.global.shared::cta.add.tile.bulk_group [%0, {%1, %2, %3}], [%4];" ::"l"(map), "r"(col),
+                         "r"(f), "r"(t.slot), "r"(smem_addr(box))
+                         : "memory");
+        else
+            asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%1, %2, %3}], [%4];" ::"l"(map), "r"(col), "r"(f),
+                         "r"(t.slot), "r"(smem_addr(box))
+                         : "memory");
+        bulk_commit();
+    }
+}
+
+// ------------------------------------------------------------------------ kernel
+
+template <ExpertOp OP, int NT, int CG, bool F32>
+__global__ void __launch_bounds__(kThreads, 1)
+k_expert_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_big,
+                 const __grid_constant__ CUtensorMap map_y, const KernelParams p)
+{
+    // map_a: the M operand (weights, or the left operand of a weight gradient); map_b, map_big: the N operand
+    using L = Layout<OP, NT, CG>;
+    constexpr bool kGrad = L::kGrad;
+    constexpr int kBox = 32;                                   // rows per TMA load of few rows
+    extern __shared__ unsigned char raw[];
+    unsigned char *base = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
+    unsigned char *epi = base + L::kEpiOff;
+    uint64_t *bars = reinterpret_cast<uint64_t *>(base + L::kBarOff);
+    uint64_t *full = bars, *empty = bars + kMaxStages, *peer = bars + 2 * kMaxStages;
+    uint64_t *acc_full = bars + 3 * kMaxStages, *acc_empty = acc_full + 2, *drained = acc_full + 4;
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(bars + L::kBars);
+    volatile int *quit = reinterpret_cast<volatile int *>(tmem_slot + 1);
+    int *warp_sums = reinterpret_cast<int *>(tmem_slot + 4);
+    int *ends = reinterpret_cast<int *>(base + L::kEndsOff);
+    unsigned char *stage = base + ((L::kEndsOff + (kGrad ? 0 : p.P * 4) + 1023) & ~1023);
+
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, stages = p.stages;
+    const int rank = CG == 2 ? (int)cluster_rank() : 0;
+    if (tid == 0) {
+        for (int s = 0; s < stages; ++s) {
+            mbar_init(&full[s], 1); mbar_init(&empty[s], 1);
+            mbar_init(&peer[s], 1);
+        }
+        for (int b = 0; b < 2; ++b) { mbar_init(&acc_full[b], 1); mbar_init(&acc_empty[b], CG * kEpiWarps); }
+        mbar_init(drained, 1);
+        *quit = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&map_a));
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&map_b));
+        if (!kGrad) asm volatile("prefetch.tensormap [%0];" ::"l"(&map_big));
+        if (kGrad) asm volatile("prefetch.tensormap [%0];" ::"l"(&map_y));
+    }
+    // hints while the previous kernel drains: its weights have pushed these out of L2 (a hint returns nothing stale)
+    if (tid * 32 < p.P) { prefetch_l2(p.slot_counts + tid * 32); prefetch_l2(p.slot_offsets + tid * 32); }
+    if (warp == kMmaWarp) tmem_alloc<CG>(tmem_slot, 512);
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+
+    int tiles = 0;
+    const int feats = ((kGrad ? p.M : p.N) + CG * kFeat - 1) / (CG * kFeat);
+    if (kGrad) {
+        tiles = p.P * feats * ((p.N + NT - 1) / NT);           // the host has seen that this is an int
+        __syncthreads();
+    } else {
+        // inclusive prefix over the slots of their tile counts
+        const int chunk = (p.P + kThreads - 1) / kThreads, s0 = tid * chunk, s1 = min(p.P, s0 + chunk);
+        int sum = 0;
+#pragma unroll 1
+        for (int s = s0; s < s1; ++s) {
+            int first;
+            sum = tiles_sum(sum, feats * row_tiles<NT>(segment(p, s, first)));
+            ends[s] = sum;
+        }
+        int incl = sum;
+#pragma unroll 1
+        for (int off = 1; off < 32; off <<= 1) {
+            const int o = __shfl_up_sync(0xffffffffu, incl, off);
+            if (lane >= off) incl = tiles_sum(incl, o);
+        }
+        if (lane == 31) warp_sums[warp] = incl;
+        int before = __shfl_up_sync(0xffffffffu, incl, 1);
+        if (lane == 0) before = 0;
+        __syncthreads();
+#pragma unroll 1
+        for (int w = 0; w < warp; ++w) before = tiles_sum(before, warp_sums[w]);
+#pragma unroll 1
+        for (int s = s0; s < s1; ++s) ends[s] = tiles_sum(ends[s], before);
+    }
+    __syncwarp();
+    tc_fence_before();
+    if (CG == 2) cluster_sync();                               // the peer's barriers are set up before anything arrives on them
+    else __syncthreads();
+    tc_fence_after();
+    // All 512 columns belong to this CTA, so they start at 0: a constant in every TMEM address.  (Anything else
+    // would be reported and no tile touched.)
+    constexpr uint32_t tmem = 0;
+    const bool whole = *tmem_slot == 0;
+    if (tid == 0 && !whole) *quit = 1;
+    if (!kGrad) {
+        tiles = ends[p.P - 1];
+        // counts that no dispatch writes: nothing is touched
+        if (tiles >= kTooManyTiles) {
+            if (tid == 0) report_status(p.ctl, kDevCapacity);
+            tiles = 0;
+        }
+    }
+    if (!whole) tiles = 0;
+
+    // The two issuing warps run their loops with all lanes, so that everything the asynchronous instructions
+    // take is uniform over the warp, and issue from one elected lane.
+    if (warp == kTmaWarp) {
+        int issued = 0, s = 0;
+        // products: the first CTA's barrier counts the bytes of both; weight gradient: each CTA's its own
+        const uint32_t lead = kGrad ? smem_addr(full) : lead_addr<CG>(full);
+        unsigned parity = 1;                                   // a fresh barrier passes the wait for parity 1
+        bool ok = true;
+        Tile t;
+        for (TileStream<OP, NT, CG> stream(p, ends, tiles); ok && stream.next(t);) {
+            const int n = tile_n<OP, NT, CG>(p, t), half = n / CG;   // rows (or columns) of the tile in this CTA
+            // each TMA instruction costs its warp some 80 cycles: many rows come in one box, few in boxes of 32
+            const bool big = half > 2 * kBox;
+            const int loads = big ? 1 : (half + kBox - 1) / kBox;
+            const uint32_t bytes = kGrad ? L::kStage : CG * (kATile + (big ? L::kN : loads * kBox) * kLine);
+            const int steps = ((kGrad ? t.rows : p.K) + kStageK - 1) / kStageK;
+            const int feat = t.feat + rank * kFeat;
+            for (int k = 0; k < steps; ++k) {
+                ok = __all_sync(0xffffffffu, wait_for(&empty[s], parity, quit, p.spin_limit));
+                if (!ok) break;
+                unsigned char *a = stage + s * L::kStage, *b = a + kATile;
+                if (elect_one()) {
+                    const uint32_t bar = lead + s * 8;
+                    if (kGrad || rank == 0) mbar_expect_tx(&full[s], bytes);
+                    if (kGrad) {
+                        const int r = t.row + k * kStageK, col = t.col + rank * half;
+#pragma unroll
+                        for (int q = 0; q < kFeat / 64; ++q) tma_2d<1>(a + q * kChunk, &map_a, feat + q * 64, r, bar);
+#pragma unroll
+                        for (int q = 0; q < L::kN / 64; ++q) tma_2d<1>(b + q * kChunk, &map_b, col + q * 64, r, bar);
+                    } else {
+                        if (L::kAAlongK) tma_3d<CG>(a, &map_a, k * kStageK, feat, t.slot, bar);
+                        else {
+#pragma unroll
+                            for (int q = 0; q < kFeat / 64; ++q) tma_3d<CG>(a + q * kChunk, &map_a, feat + q * 64, k * kStageK, t.slot, bar);
+                        }
+                        if (big) tma_2d<CG>(b, &map_big, k * kStageK, t.row + rank * half, bar);
+                        else for (int l = 0; l < loads; ++l)
+                            tma_2d<CG>(b + l * kBox * kLine, &map_b, k * kStageK, t.row + rank * half + l * kBox, bar);
+                    }
+                }
+                __syncwarp();
+                ++issued;
+                if (++s == stages) { s = 0; parity ^= 1u; }
+            }
+        }
+        if (!ok) {
+            // loads in flight still land in this CTA's shared memory: a bounded wait for them (the barriers may be the
+            // other CTA's, so they may not complete, but the wait outlasts any copy)
+            unsigned long long until = 0;
+            for (int m = max(0, issued - stages); m < issued; ++m) drain_wait(&full[m % stages], (unsigned)(m / stages) & 1u, until);
+        }
+    } else if (warp == kMmaWarp && (rank == 0 || kGrad)) {
+        int s = 0, buf = 0;
+        unsigned parity = 0, acc_parity = 1;
+        bool ok = true;
+        const uint64_t a_desc = desc_tile<L::kAAlongK>(smem_addr(stage)), b_desc = desc_tile<L::kBAlongK>(smem_addr(stage + kATile));
+        Tile t;
+        for (TileStream<OP, NT, CG> stream(p, ends, tiles); ok && stream.next(t);) {
+            if (rank == 0) {
+                ok = __all_sync(0xffffffffu, wait_for(&acc_empty[buf], acc_parity, quit, p.spin_limit));
+                if (!ok) break;
+                tc_fence_after();
+            }
+            const uint32_t d = tmem + buf * NT;
+            const uint32_t idesc = idesc_bf16<CG, L::kAAlongK, L::kBAlongK>(tile_n<OP, NT, CG>(p, t));
+            const int steps = ((kGrad ? t.rows : p.K) + kStageK - 1) / kStageK;
+            bool ready = steps > 0 && __all_sync(0xffffffffu, mbar_test_wait(&full[s], parity));
+            for (int k = 0; k < steps; ++k) {
+                if (!ready) {
+                    ok = __all_sync(0xffffffffu, wait_for(&full[s], parity, quit, p.spin_limit));
+                    if (!ok) break;
+                }
+                // ask for the next stage's barrier now: the answer arrives while this stage is issued
+                const int s_next = s + 1 == stages ? 0 : s + 1;
+                const bool next_full = mbar_test_wait(&full[s_next], s_next ? parity : parity ^ 1u);
+                int parts = kStageK / 16;
+                if (kGrad) {
+                    // The last rows of a segment: whole 16s are multiplied, and of the last 16 the lines behind the
+                    // segment, which hold the next one's rows, are made zero in both operands (a NaN there times a
+                    // zero would still be one).  A line is 128 bytes of one k in each of the stage's chunks.
+                    const int left = t.rows - k * kStageK;
+                    if (left < kStageK) {
+                        parts = (left + 15) / 16;
+                        if (left & 15) {
+                            unsigned char *lines = stage + s * L::kStage + (lane & 7) * 16;
+                            for (int i = left; i < parts * 16; ++i)
+                                for (int q = lane >> 3; q < L::kStage / kChunk; q += 4)
+                                    *reinterpret_cast<uint4 *>(lines + q * kChunk + i * kLine) = make_uint4(0u, 0u, 0u, 0u);
+                            fence_async_shared();
+                            __syncwarp();
+                        }
+                    }
+                    if (CG == 2) {
+                        // the second CTA's operands are there (and its last lines zero): it says so, the first one waits for it
+                        if (rank == 1) {
+                            if (lane == 0) mbar_arrive_lead_release(&peer[s]);
+                        } else {
+                            ok = __all_sync(0xffffffffu, wait_for<true>(&peer[s], parity, quit, p.spin_limit));
+                            if (!ok) break;
+                        }
+                    }
+                }
+                if (rank == 0) {
+                    tc_fence_after();
+                    // descriptors count in 16-byte units
+                    const uint64_t a = a_desc + (uint32_t)(s * (L::kStage >> 4)), b = b_desc + (uint32_t)(s * (L::kStage >> 4));
+                    if (elect_one()) {
+#pragma unroll
+                        for (int q = 0; q < kStageK / 16; ++q)
+                            if (!kGrad || q < parts)
+                                mma_bf16<CG>(d, a + q * kDescStep<L::kAAlongK>, b + q * kDescStep<L::kBAlongK>, idesc, k > 0 || q > 0);
+                        mma_commit<CG>(&empty[s]);
+                    }
+                }
+                ready = __all_sync(0xffffffffu, next_full);
+                s = s_next;
+                if (s == 0) parity ^= 1u;
+            }
+            if (!ok) break;
+            if (rank == 0 && elect_one()) mma_commit<CG>(&acc_full[buf]);
+            __syncwarp();
+            buf ^= 1;
+            if (buf == 0) acc_parity ^= 1u;
+        }
+        if (rank == 0) {
+            // everything issued has left the tensor core before TMEM is given back
+            if (elect_one()) mma_commit<CG>(drained);
+            __syncwarp();
+            unsigned long long until = 0;
+            drain_wait(drained, 0, until);
+        }
+    } else if (warp < kEpiWarps) {
+        // epilogue: TMEM lane = feature of the tile, column = row (weight gradient: column)
+        const int group = warp >> 2, quarter = warp & 3;
+        unsigned char *mine = epi + warp * L::kEpiWarp;
+        int buf = 0;
+        unsigned acc_parity = 0;
+        Tile t;
+        for (TileStream<OP, NT, CG> stream(p, ends, tiles); stream.next(t);) {
+            if (!__all_sync(0xffffffffu, wait_for(&acc_full[buf], acc_parity, quit, p.spin_limit))) break;
+            tc_fence_after();
+            const uint32_t acc = tmem + buf * NT + ((uint32_t)(quarter * 32) << 16);
+            const int f = t.feat + rank * kFeat + quarter * 32;
+            if (kGrad) {
+                constexpr int kCols = F32 ? 32 : 64;           // of a box
+                const int cols = min(NT, p.N - t.col);
+                const bool any = f < p.M && (t.rows > 0 || !p.add);
+                for (int c0 = group * kCols; c0 < cols && any; c0 += 2 * kCols) {
+                    uint4 box[8] = {};
+                    if (t.rows > 0) {
+                        uint32_t v[kCols / 32][32];
+#pragma unroll
+                        for (int q = 0; q < kCols / 32; ++q) tmem_ld_lanes(acc + c0 + 32 * q, v[q]);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int q = 0; q < 8; ++q) {
+                            if (F32) box[q] = make_uint4(v[0][4 * q], v[0][4 * q + 1], v[0][4 * q + 2], v[0][4 * q + 3]);
+                            else {
+                                const uint32_t *w = &v[kCols / 32 - 1 ? q >> 2 : 0][8 * (q & 3)];
+                                box[q] = make_uint4(pack_bf16(__uint_as_float(w[0]), __uint_as_float(w[1])),
+                                                    pack_bf16(__uint_as_float(w[2]), __uint_as_float(w[3])),
+                                                    pack_bf16(__uint_as_float(w[4]), __uint_as_float(w[5])),
+                                                    pack_bf16(__uint_as_float(w[6]), __uint_as_float(w[7])));
+                            }
+                        }
+                    }
+                    store_grad<F32>(p, &map_y, t, f, t.col + c0, box, mine, lane);
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_lead<CG>(&acc_empty[buf]);
+            } else {
+                float *plane = reinterpret_cast<float *>(mine);
+                for (int c0 = group * 32; c0 < t.rows; c0 += 64) {
+                    const long long row = t.row + c0;
+                    const int left = t.rows - c0;
+                    Kept kept[4];
+                    if (OP == ExpertOp::kGatedBackward) load_kept(p, f, row, left, lane, kept);
+                    uint32_t v[32];
+                    tmem_ld_lanes(acc + c0, v);
+                    tmem_wait_ld();
+                    if (c0 + 64 >= t.rows) {                   // this warp's last look at the accumulator
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive_lead<CG>(&acc_empty[buf]);
+                    }
+                    write_plane(plane, v, lane);
+                    if (OP == ExpertOp::kGated) store_gated(p, plane, f, row, left, lane);
+                    else if (OP == ExpertOp::kGatedBackward) store_gated_backward(p, plane, f, row, left, lane, kept);
+                    else store_rows(p, plane, f, row, left, lane);
+                    __syncwarp();                              // the plane is free before the next 32 rows are written
+                }
+                if (group * 32 >= t.rows && lane == 0) mbar_arrive_lead<CG>(&acc_empty[buf]);
+            }
+            buf ^= 1;
+            if (buf == 0) acc_parity ^= 1u;
+        }
+        if (kGrad && lane == 0) bulk_wait_all();               // the last stores have left shared memory
+    }
+
+    __syncwarp();
+    tc_fence_before();
+    if (CG == 2) cluster_sync();                               // the pair leaves together: neither arrives on a CTA that is gone
+    else __syncthreads();
+    if (tid == 0 && *quit) report_status(p.ctl, kDevTimeout);
+    if (warp == kMmaWarp) {
+        if (CG == 2 && rank == 1) {                            // the first CTA's last arrival is on its way here as well
+            unsigned long long until = 0;
+            drain_wait(drained, 0, until);
+            __syncwarp();
+        }
+        tc_fence_after();
+        tmem_dealloc<CG>(tmem, 512);
+    }
+}
+
+// ------------------------------------------------------------------------- host
+
+template <ExpertOp OP, int NT, int CG, bool F32 = false>
+cudaError_t launch(const ExpertArgs &a, cudaStream_t st)
+{
+    using L = Layout<OP, NT, CG>;
+    static_assert(L::kN % 64 == 0 && NT % 32 == 0 && 2 * NT <= 512, "boxes of the row operand, pieces of the epilogue, TMEM columns");
+    const auto kernel = k_expert_product<OP, NT, CG, F32>;
+    // a function's attributes are those of one device
+    constexpr int kDevices = 64;
+    static std::once_flag once[kDevices];
+    static cudaError_t attr[kDevices];
+    if (a.device < 0 || a.device >= kDevices) return cudaErrorInvalidDevice;
+    std::call_once(once[a.device], [&] { attr[a.device] = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kSmem); });
+    if (attr[a.device] != cudaSuccess) return attr[a.device];
+    if (!encode_fn()) return cudaErrorNotSupported;
+    const CUtensorMapDataType bf16 = CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, f32 = CU_TENSOR_MAP_DATA_TYPE_FLOAT32;
+    const CUtensorMapSwizzle sw = CU_TENSOR_MAP_SWIZZLE_128B;
+    CUtensorMap map_a, map_b, map_big = {}, map_y = {};
+    bool ok;
+    if (L::kGrad) {
+        const cuuint64_t ad[2] = {(cuuint64_t)a.M, (cuuint64_t)a.rows}, as[1] = {2 * (cuuint64_t)a.M};
+        const cuuint64_t bd[2] = {(cuuint64_t)a.N, (cuuint64_t)a.rows}, bs[1] = {2 * (cuuint64_t)a.N};
+        const cuuint64_t size = F32 ? 4 : 2;
+        const cuuint64_t yd[3] = {(cuuint64_t)a.N, (cuuint64_t)a.M, (cuuint64_t)a.P}, ys[2] = {size * a.N, size * a.N * (cuuint64_t)a.M};
+        ok = encode(&map_a, bf16, sw, a.a, 2, ad, as, 64, kStageK) && encode(&map_b, bf16, sw, a.b, 2, bd, bs, 64, kStageK) &&
+             encode(&map_y, F32 ? f32 : bf16, sw, a.y, 3, yd, ys, F32 ? 32 : 64, 32);
+    } else {
+        const cuuint64_t inner = L::kAAlongK ? a.K : a.N, outer = L::kAAlongK ? a.N : a.K;
+        const cuuint64_t wd[3] = {inner, outer, (cuuint64_t)a.P}, ws[2] = {2 * inner, 2 * inner * outer};
+        const cuuint64_t ad[2] = {(cuuint64_t)a.K, (cuuint64_t)a.rows}, as[1] = {2 * (cuuint64_t)a.K};
+        ok = encode(&map_a, bf16, sw, a.w, 3, wd, ws, 64, L::kAAlongK ? kFeat : kStageK) && encode(&map_b, bf16, sw, a.a, 2, ad, as, 64, 32) &&
+             encode(&map_big, bf16, sw, a.a, 2, ad, as, 64, L::kN);
+    }
+    if (!ok) return cudaErrorInvalidValue;
+    KernelParams p;
+    p.slot_counts = a.slot_counts; p.slot_offsets = a.slot_offsets; p.rows = a.rows;
+    p.P = a.P; p.N = a.N; p.K = a.K; p.M = a.M; p.stages = L::stages(a.P);
+    p.y = static_cast<__nv_bfloat16 *>(a.y); p.z = a.z; p.z_scales = a.z_scales; p.dz = static_cast<__nv_bfloat16 *>(a.dz);
+    p.add = a.add; p.ctl = a.ctl; p.spin_limit = a.spin_limit;
+    // no more CTAs than there can be tiles (the counts are on the device)
+    const long long feats = ((L::kGrad ? a.M : a.N) + CG * kFeat - 1) / (CG * kFeat);
+    const long long most = L::kGrad ? feats * ((a.N + NT - 1) / NT) * a.P : feats * (std::min<long long>(a.P, a.rows) + a.rows / NT);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(CG * std::min<long long>(a.sm_count / CG, most)));
+    cfg.blockDim = dim3(kThreads); cfg.dynamicSmemBytes = L::bytes(a.P); cfg.stream = st;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = CG; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
+    at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at; cfg.numAttrs = a.pdl ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, kernel, map_a, map_b, map_big, map_y, p);
+}
+
+// With few rows a slot the weights dominate, and a narrow tile of one CTA leaves shared memory for more stages of them.
+// With many rows the products do, and a pair of CTAs halves what each holds of the row operand.  The host knows the
+// buffer's rows but not the counts, so the mean over all slots, empty ones included, decides.
+template <ExpertOp OP>
+cudaError_t launch_for(const ExpertArgs &a, cudaStream_t st)
+{
+    if (a.rows <= 64ll * a.P) return launch<OP, 64, 1>(a, st);
+    return launch<OP, 256, 2>(a, st);
+}
+
+}  // namespace
+
+namespace moe {
+
+cudaError_t expert_product_launch(const ExpertArgs &a, cudaStream_t st)
+{
+    switch (a.op) {
+    case ExpertOp::kProduct: return launch_for<ExpertOp::kProduct>(a, st);
+    case ExpertOp::kGated: return launch_for<ExpertOp::kGated>(a, st);
+    case ExpertOp::kTransposed: return launch_for<ExpertOp::kTransposed>(a, st);
+    case ExpertOp::kGatedBackward: return launch_for<ExpertOp::kGatedBackward>(a, st);
+    case ExpertOp::kWeightGrad: return a.f32 ? launch<ExpertOp::kWeightGrad, 256, 2, true>(a, st) : launch<ExpertOp::kWeightGrad, 256, 2>(a, st);
+    }
+    return cudaErrorInvalidValue;
+}
+
+}  // namespace moe

@@ -8,6 +8,7 @@
 
 #include <algorithm>
 #include <cstring>
+#include <initializer_list>
 #include <mutex>
 #include <new>
 #include <vector>
@@ -15,6 +16,7 @@
 #include "backward_kernels.cuh"
 #include "combine_kernels.cuh"
 #include "ep_kernels.cuh"
+#include "expert_product.h"
 #include "mx_product.h"
 #include "mx_scatter.cuh"
 #include "route_kernels.cuh"
@@ -626,6 +628,54 @@ MxProductArgs product_args(const moe_ctx *ctx, const uint8_t *a_codes, const uin
     a.ctl = ctx->d_ctl; a.spin_limit = ctx->spin_limit; a.sm_count = ctx->sm_count; a.device = ctx->device;
     a.pdl = ctx->pdl;
     return a;
+}
+
+// A buffer of a call, for the question whether an output shares a byte with an input or with another output.
+struct Span {
+    const void *at;
+    size_t bytes;
+};
+
+bool spans_meet(std::initializer_list<Span> outputs, std::initializer_list<Span> inputs)
+{
+    for (const Span *o = outputs.begin(); o != outputs.end(); ++o) {
+        for (const Span *q = outputs.begin(); q != o; ++q)
+            if (ranges_overlap(o->at, o->bytes, q->at, q->bytes)) return true;
+        for (const Span &i : inputs)
+            if (ranges_overlap(o->at, o->bytes, i.at, i.bytes)) return true;
+    }
+    return false;
+}
+
+// Common checks of the products on bf16 rows: `rows` rows of n_in elements and matrices of [n_out, n_in] (n and k of
+// the kernel in either order).
+moe_status check_expert(const moe_ctx *ctx, const void *a, int64_t rows, const int32_t *slot_counts, const int32_t *slot_offsets,
+                        const void *w, int32_t n_out, int32_t n_in)
+{
+    if (!ctx || rows < 0 || n_out < 8 || n_out % 8 != 0 || n_in < 8 || n_in % 8 != 0) return MOE_ERR_INVALID_ARG;
+    if (!expert_product_fits(rows, n_out, n_in, ctx->d.P) || !expert_product_fits(rows, n_in, n_out, ctx->d.P)) return MOE_ERR_CAPACITY;
+    if (rows == 0) return MOE_OK;
+    if (!a || !slot_counts || !slot_offsets || !w || !aligned16(a) || !aligned16(w)) return MOE_ERR_INVALID_ARG;
+    return MOE_OK;
+}
+
+ExpertArgs expert_args(const moe_ctx *ctx, ExpertOp op, const void *a, int64_t rows, const int32_t *slot_counts, const int32_t *slot_offsets,
+                       const void *w, int32_t n, int32_t k)
+{
+    ExpertArgs e = {};
+    e.op = op; e.a = a; e.rows = rows;
+    e.slot_counts = slot_counts; e.slot_offsets = slot_offsets; e.P = ctx->d.P;
+    e.w = w; e.N = n; e.K = k;
+    e.ctl = ctx->d_ctl; e.spin_limit = ctx->spin_limit; e.sm_count = ctx->sm_count; e.device = ctx->device;
+    e.pdl = ctx->pdl;
+    return e;
+}
+
+moe_status enqueue_expert(const moe_ctx *ctx, const ExpertArgs &e, void *cuda_stream)
+{
+    DeviceScope scope(ctx->device);
+    if (!scope.ok) return MOE_ERR_CUDA;
+    return expert_product_launch(e, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? MOE_OK : MOE_ERR_CUDA;
 }
 
 // What both gradients take from the latest dispatch.
@@ -1257,6 +1307,95 @@ moe_status moe_dispatch_backward(moe_ctx *ctx, const float *logits, const void *
     p.group_size = p.topk_group ? ctx->d.E / ctx->cfg.n_group : ctx->d.E;
     p.inv_scale = 1.0f / ctx->cfg.route_scale;
     return enqueue_backward<false>(ctx, p, static_cast<cudaStream_t>(cuda_stream));
+}
+
+// ---------------------------------------------------------------------------
+// experts in 16 bits and their gradients
+// ---------------------------------------------------------------------------
+
+moe_status moe_expert_product(moe_ctx *ctx, const void *a, int64_t rows, const int32_t *slot_counts, const int32_t *slot_offsets,
+                              const void *w, int32_t n_out, int32_t n_in, void *y, void *cuda_stream)
+{
+    const moe_status ms = check_expert(ctx, a, rows, slot_counts, slot_offsets, w, n_out, n_in);
+    if (ms != MOE_OK || rows == 0) return ms;
+    if (!y || !aligned16(y)) return MOE_ERR_INVALID_ARG;
+    const size_t P = ctx->d.P, n = rows;
+    if (spans_meet({{y, n * n_out * 2}}, {{a, n * n_in * 2}, {w, P * n_out * n_in * 2}, {slot_counts, P * 4}, {slot_offsets, P * 4}}))
+        return MOE_ERR_INVALID_ARG;
+    ExpertArgs e = expert_args(ctx, ExpertOp::kProduct, a, rows, slot_counts, slot_offsets, w, n_out, n_in);
+    e.y = y;
+    return enqueue_expert(ctx, e, cuda_stream);
+}
+
+moe_status moe_expert_gated(moe_ctx *ctx, const void *a, int64_t rows, const int32_t *slot_counts, const int32_t *slot_offsets,
+                            const void *w, int32_t n_hidden, int32_t n_in, void *h, void *z, uint8_t *z_scales, void *cuda_stream)
+{
+    if (n_hidden < 16 || n_hidden % 16 != 0 || n_hidden > (1 << 29)) return MOE_ERR_INVALID_ARG;
+    const moe_status ms = check_expert(ctx, a, rows, slot_counts, slot_offsets, w, 2 * n_hidden, n_in);
+    if (ms != MOE_OK || rows == 0) return ms;
+    if (!h || !aligned16(h) || (z_scales && !z) || !aligned16(z) || !aligned16(z_scales)) return MOE_ERR_INVALID_ARG;
+    const size_t P = ctx->d.P, n = rows, cols = 2 * (size_t)n_hidden;
+    const Span sz = {z, z ? n * cols * (z_scales ? 1 : 2) : 0}, ss = {z_scales, z_scales ? n * mx_scale_pitch((int)cols) : 0};
+    if (spans_meet({{h, n * cols}, sz, ss}, {{a, n * n_in * 2}, {w, P * cols * n_in * 2}, {slot_counts, P * 4}, {slot_offsets, P * 4}}))
+        return MOE_ERR_INVALID_ARG;
+    ExpertArgs e = expert_args(ctx, ExpertOp::kGated, a, rows, slot_counts, slot_offsets, w, 2 * n_hidden, n_in);
+    e.y = h; e.z = z; e.z_scales = z_scales;
+    return enqueue_expert(ctx, e, cuda_stream);
+}
+
+moe_status moe_expert_rows_backward(moe_ctx *ctx, const void *dy, int64_t rows, const int32_t *slot_counts, const int32_t *slot_offsets,
+                                    const void *w, int32_t n_out, int32_t n_in, void *da, void *cuda_stream)
+{
+    const moe_status ms = check_expert(ctx, dy, rows, slot_counts, slot_offsets, w, n_out, n_in);
+    if (ms != MOE_OK || rows == 0) return ms;
+    if (!da || !aligned16(da)) return MOE_ERR_INVALID_ARG;
+    const size_t P = ctx->d.P, n = rows;
+    if (spans_meet({{da, n * n_in * 2}}, {{dy, n * n_out * 2}, {w, P * n_out * n_in * 2}, {slot_counts, P * 4}, {slot_offsets, P * 4}}))
+        return MOE_ERR_INVALID_ARG;
+    ExpertArgs e = expert_args(ctx, ExpertOp::kTransposed, dy, rows, slot_counts, slot_offsets, w, n_in, n_out);
+    e.y = da;
+    return enqueue_expert(ctx, e, cuda_stream);
+}
+
+moe_status moe_expert_gated_backward(moe_ctx *ctx, const void *dy, int64_t rows, const int32_t *slot_counts, const int32_t *slot_offsets,
+                                     const void *w, int32_t n_out, int32_t n_hidden, const void *z, const uint8_t *z_scales, void *dz,
+                                     void *h, void *cuda_stream)
+{
+    if (n_hidden < 16 || n_hidden % 16 != 0 || n_hidden > (1 << 29)) return MOE_ERR_INVALID_ARG;
+    const moe_status ms = check_expert(ctx, dy, rows, slot_counts, slot_offsets, w, n_out, n_hidden);
+    if (ms != MOE_OK || rows == 0) return ms;
+    if (!z || !dz || !h || !aligned16(z) || !aligned16(z_scales) || !aligned16(dz) || !aligned16(h)) return MOE_ERR_INVALID_ARG;
+    const size_t P = ctx->d.P, n = rows, cols = 2 * (size_t)n_hidden;
+    if (spans_meet({{dz, n * cols * 2}, {h, n * cols}},
+                   {{dy, n * n_out * 2}, {w, P * n_out * cols}, {z, n * cols * (z_scales ? 1 : 2)},
+                    {z_scales, z_scales ? n * mx_scale_pitch((int)cols) : 0}, {slot_counts, P * 4}, {slot_offsets, P * 4}}))
+        return MOE_ERR_INVALID_ARG;
+    ExpertArgs e = expert_args(ctx, ExpertOp::kGatedBackward, dy, rows, slot_counts, slot_offsets, w, n_hidden, n_out);
+    e.y = h; e.z = const_cast<void *>(z); e.z_scales = const_cast<uint8_t *>(z_scales); e.dz = dz;
+    return enqueue_expert(ctx, e, cuda_stream);
+}
+
+moe_status moe_expert_weight_backward(moe_ctx *ctx, const void *dy, const void *a, int64_t rows, const int32_t *slot_counts,
+                                      const int32_t *slot_offsets, int32_t n_out, int32_t n_in, void *dw, int32_t dtype, int32_t add,
+                                      void *cuda_stream)
+{
+    if (!ctx || rows < 0 || n_out < 8 || n_out % 8 != 0 || n_in < 8 || n_in % 8 != 0) return MOE_ERR_INVALID_ARG;
+    if ((dtype != MOE_DTYPE_BF16 && dtype != MOE_DTYPE_F32) || (add && dtype != MOE_DTYPE_F32)) return MOE_ERR_INVALID_ARG;
+    if (!weight_grad_fits(rows, n_out, n_in, ctx->d.P)) return MOE_ERR_CAPACITY;
+    if (!dw || !aligned16(dw)) return MOE_ERR_INVALID_ARG;
+    const size_t P = ctx->d.P, n = rows, bytes = P * n_out * n_in * (dtype == MOE_DTYPE_F32 ? 4 : 2);
+    if (rows == 0) {                                           // no segment has a row: a gradient of zeros
+        if (add) return MOE_OK;
+        DeviceScope scope(ctx->device);
+        if (!scope.ok) return MOE_ERR_CUDA;
+        return cudaMemsetAsync(dw, 0, bytes, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? MOE_OK : MOE_ERR_CUDA;
+    }
+    if (!dy || !a || !slot_counts || !slot_offsets || !aligned16(dy) || !aligned16(a)) return MOE_ERR_INVALID_ARG;
+    if (spans_meet({{dw, bytes}}, {{dy, n * n_out * 2}, {a, n * n_in * 2}, {slot_counts, P * 4}, {slot_offsets, P * 4}}))
+        return MOE_ERR_INVALID_ARG;
+    ExpertArgs e = expert_args(ctx, ExpertOp::kWeightGrad, dy, rows, slot_counts, slot_offsets, nullptr, n_in, 0);
+    e.M = n_out; e.b = a; e.y = dw; e.f32 = dtype == MOE_DTYPE_F32; e.add = add != 0;
+    return enqueue_expert(ctx, e, cuda_stream);
 }
 
 moe_status moe_step_host_async(moe_ctx *ctx, const float *logits_host, const void *x_host, int32_t T,
