@@ -334,6 +334,19 @@ moe_status moe_mx_dequantize(const uint8_t *codes, const uint8_t *scales, int64_
                              int32_t dtype, int64_t row_stride, void *cuda_stream);
 
 /*
+ * Eight-bit rows, in which activations are kept for a backward pass (written by moe_rms_norm and moe_expert_gated, read by
+ * moe_redispatch and moe_expert_gated_backward):
+ *   codes  [cols] u8: e4m3 floats (a sign, four exponent bits with bias 7, three bits of mantissa, largest 448)
+ *   scales [moe_mx_scale_pitch(cols)] u8 as above
+ * A block's scale is the smallest power of two, at least 2^-127, under which its largest magnitude is at most 448, 255 for a block
+ * with a NaN or an infinity; elements are rounded to the nearest code, ties to even.
+ *
+ * moe_mx8_dequantize — the values that 8-bit rows stand for, as moe_mx_dequantize.
+ */
+moe_status moe_mx8_dequantize(const uint8_t *codes, const uint8_t *scales, int64_t rows, int32_t cols, void *y, int32_t dtype,
+                              int64_t row_stride, void *cuda_stream);
+
+/*
  * moe_mx_dispatch — moe_dispatch with a send buffer of 4-bit rows: the same routing and permutation;
  * each token's row is quantised once and its codes and scales are written to its k rows.
  *   out->send_buf is not used and may be NULL
@@ -407,6 +420,46 @@ moe_status moe_combine_backward(moe_ctx *ctx, const void *expert_buf, const void
  */
 moe_status moe_dispatch_backward(moe_ctx *ctx, const float *logits, const void *d_send_buf, const float *d_weights,
                                  int32_t T, void *dx, float *d_logits, void *cuda_stream);
+
+/*
+ * moe_rms_norm — the norm in front of a layer (no context: any rows on the current device):
+ *   h = x + residual, rounded to the rows' type;  rstd = 1 / sqrt(mean(h^2) + eps);  y = h * rstd * weight
+ *   x, residual  device [rows, cols] of `dtype`, x_stride and residual_stride elements from row to row (>= cols, rows 16-byte
+ *     aligned).  residual may be NULL: then h = x, and h need not be given
+ *   weight       device [cols] of `weight_dtype`: `dtype` or MOE_DTYPE_F32
+ *   h, y         device out [rows, cols] of `dtype`, contiguous.  h may be x or residual itself where that is contiguous
+ *   rstd         device out [rows] f32, or NULL: needed by moe_rms_norm_backward
+ *   codes, scales device out: y (before it is rounded to `dtype`) as 8-bit rows, with the padding of the scales as 0; or both NULL
+ * cols % 8 == 0 (% 32 with codes), 8 <= cols <= 32768.  Sums are fp32, in an order that depends on the sizes alone; each output is
+ * rounded once.  rows = 0 launches nothing.  CAPACITY beyond 2^31 - 1 rows.  INVALID_ARG if an output overlaps an input
+ * (but as said for h) or another output.  Allocates nothing, does not wait.
+ */
+moe_status moe_rms_norm(const void *x, int64_t x_stride, const void *residual, int64_t residual_stride, int32_t dtype, int64_t rows,
+                        int32_t cols, const void *weight, int32_t weight_dtype, float eps, void *h, void *y, float *rstd, uint8_t *codes,
+                        uint8_t *scales, void *cuda_stream);
+
+/*
+ * moe_rms_norm_backward — with n = h * rstd and g = dy * weight:
+ *   dx = rstd * (g - n * mean(g * n)) + dh      [rows, cols] of `dtype` out: the gradient of x, and of the residual
+ *   d_weight = sum over the rows of dy * n      [cols] f32 out (zeros for rows = 0)
+ *   dy, dh, h device [rows, cols] of `dtype`, contiguous: the gradients of y and (or NULL) of h, and the forward's h
+ *   workspace device, moe_rms_norm_backward_workspace(rows, cols) bytes, 16-byte aligned, contents irrelevant: the call's own
+ *     until its work has run.  CAPACITY if workspace_bytes is less
+ * dx may be dy, dh or h itself; otherwise as moe_rms_norm.  d_weight's sums are fp32 in a fixed order.
+ */
+size_t moe_rms_norm_backward_workspace(int64_t rows, int32_t cols);
+moe_status moe_rms_norm_backward(const void *dy, const void *dh, const void *h, const float *rstd, int32_t dtype, int64_t rows,
+                                 int32_t cols, const void *weight, int32_t weight_dtype, void *dx, float *d_weight, void *workspace,
+                                 size_t workspace_bytes, void *cuda_stream);
+
+/*
+ * moe_redispatch — the bf16 send buffer of the latest moe_dispatch or moe_mx_dispatch once more, from its tokens' rows in 8
+ * bits: send_buf[dst_row[t*k+j], :] = the values of row t, rounded to bf16 (exact unless a scale leaves its range).
+ *   codes [T, H], scales [T, moe_mx_scale_pitch(H)] device; send_buf device out [T*k, H] bf16; 16-byte aligned
+ * H % 32 == 0; T as in that dispatch, whose dst_row buffer is read (the caller keeps it).  INVALID_ARG otherwise, after
+ * moe_ep_route, and if send_buf overlaps an input.
+ */
+moe_status moe_redispatch(moe_ctx *ctx, const uint8_t *codes, const uint8_t *scales, int32_t T, void *send_buf, void *cuda_stream);
 
 /*
  * ---- Experts in 16 bits and their gradients -------------------------------------------

@@ -52,6 +52,7 @@ EXPORTED_SYMBOLS = (
     "moe_mx_scale_pitch", "moe_mx_quantize", "moe_mx_dequantize", "moe_mx_dispatch", "moe_mx_expert_product",
     "moe_mx_expert_gated", "moe_combine_backward", "moe_dispatch_backward",
     "moe_expert_product", "moe_expert_gated", "moe_expert_rows_backward", "moe_expert_gated_backward", "moe_expert_weight_backward",
+    "moe_mx8_dequantize", "moe_rms_norm", "moe_rms_norm_backward", "moe_rms_norm_backward_workspace", "moe_redispatch",
 )
 
 
@@ -169,6 +170,16 @@ def _lib():
         lib.moe_expert_gated_backward.argtypes = [vp, vp, i64, vp, vp, vp, i32, i32, vp, vp, vp, vp, vp]
         lib.moe_expert_weight_backward.restype = ctypes.c_int
         lib.moe_expert_weight_backward.argtypes = [vp, vp, vp, i64, vp, vp, i32, i32, vp, i32, i32, vp]
+        lib.moe_mx8_dequantize.restype = ctypes.c_int
+        lib.moe_mx8_dequantize.argtypes = [vp, vp, i64, i32, vp, i32, i64, vp]
+        lib.moe_rms_norm.restype = ctypes.c_int
+        lib.moe_rms_norm.argtypes = [vp, i64, vp, i64, i32, i64, i32, vp, i32, ctypes.c_float, vp, vp, vp, vp, vp, vp]
+        lib.moe_rms_norm_backward_workspace.restype = ctypes.c_size_t
+        lib.moe_rms_norm_backward_workspace.argtypes = [i64, i32]
+        lib.moe_rms_norm_backward.restype = ctypes.c_int
+        lib.moe_rms_norm_backward.argtypes = [vp, vp, vp, vp, i32, i64, i32, vp, i32, vp, vp, vp, ctypes.c_size_t, vp]
+        lib.moe_redispatch.restype = ctypes.c_int
+        lib.moe_redispatch.argtypes = [vp, vp, vp, i32, vp, vp]
         lib.moe_status_string.restype = ctypes.c_char_p
         lib.moe_status_string.argtypes = [ctypes.c_int]
         _lib_handle = lib
@@ -399,6 +410,35 @@ def moe_dispatch_backward(ctx, logits_ptr: int, d_send_buf_ptr: int, d_weights_p
                                         d_logits_ptr or None, cuda_stream)
 
 
+def moe_mx8_dequantize(codes_ptr: int, scales_ptr: int, rows: int, cols: int, y_ptr: int, dtype: int, row_stride: int,
+                       cuda_stream: int = 0) -> int:
+    return _lib().moe_mx8_dequantize(codes_ptr, scales_ptr, rows, cols, y_ptr, dtype, row_stride, cuda_stream)
+
+
+def moe_rms_norm(x_ptr: int, x_stride: int, residual_ptr: int, residual_stride: int, dtype: int, rows: int, cols: int, weight_ptr: int,
+                 weight_dtype: int, eps: float, h_ptr: int, y_ptr: int, rstd_ptr: int, codes_ptr: int, scales_ptr: int,
+                 cuda_stream: int = 0) -> int:
+    """residual_ptr, h_ptr, rstd_ptr may be 0, and codes_ptr and scales_ptr together (include/moe_route.h)."""
+    return _lib().moe_rms_norm(x_ptr, x_stride, residual_ptr or None, residual_stride, dtype, rows, cols, weight_ptr, weight_dtype, eps,
+                               h_ptr or None, y_ptr, rstd_ptr or None, codes_ptr or None, scales_ptr or None, cuda_stream)
+
+
+def moe_rms_norm_backward_workspace(rows: int, cols: int) -> int:
+    return int(_lib().moe_rms_norm_backward_workspace(rows, cols))
+
+
+def moe_rms_norm_backward(dy_ptr: int, dh_ptr: int, h_ptr: int, rstd_ptr: int, dtype: int, rows: int, cols: int, weight_ptr: int,
+                          weight_dtype: int, dx_ptr: int, d_weight_ptr: int, workspace_ptr: int, workspace_bytes: int,
+                          cuda_stream: int = 0) -> int:
+    """dh_ptr may be 0."""
+    return _lib().moe_rms_norm_backward(dy_ptr, dh_ptr or None, h_ptr, rstd_ptr, dtype, rows, cols, weight_ptr, weight_dtype, dx_ptr,
+                                        d_weight_ptr, workspace_ptr, workspace_bytes, cuda_stream)
+
+
+def moe_redispatch(ctx, codes_ptr: int, scales_ptr: int, T: int, send_buf_ptr: int, cuda_stream: int = 0) -> int:
+    return _lib().moe_redispatch(ctx, codes_ptr, scales_ptr, T, send_buf_ptr, cuda_stream)
+
+
 def moe_expert_product(ctx, a_ptr: int, rows: int, slot_counts_ptr: int, slot_offsets_ptr: int, w_ptr: int, n_out: int, n_in: int,
                        y_ptr: int, cuda_stream: int = 0) -> int:
     return _lib().moe_expert_product(ctx, a_ptr, rows, slot_counts_ptr, slot_offsets_ptr, w_ptr, n_out, n_in, y_ptr, cuda_stream)
@@ -586,6 +626,95 @@ def mx_dequantize(m: MxRows, dtype: torch.dtype = torch.bfloat16, out: torch.Ten
     if st != MOE_OK:
         raise MoeError(st, "moe_mx_dequantize")
     return out
+
+
+def mx8_dequantize(m: Mx8Rows, dtype: torch.dtype = torch.bfloat16, out: torch.Tensor | None = None) -> torch.Tensor:
+    """The values that 8-bit rows stand for."""
+    index, shape, cols = m.codes.get_device(), m.codes.shape, m.cols
+    _require(dtype in _DTYPE_CODE and len(shape) > 0 and _is_mx8(m, index, shape), "mx8_dequantize")
+    stride = cols
+    if out is None:
+        out = m.codes.new_empty(shape, dtype=dtype)
+    else:
+        flat = out.is_contiguous()
+        _require(out.shape == shape and out.dtype is dtype and out.is_cuda and out.get_device() == index
+                 and (flat or (out.dim() == 2 and out.stride(1) == 1)), "mx8_dequantize")
+        stride = cols if flat else out.stride(0)
+    st = _on_device(index, moe_mx8_dequantize, m.codes.data_ptr(), m.scales.data_ptr(), out.numel() // cols, cols, out.data_ptr(),
+                    _DTYPE_CODE[dtype], stride, _raw_stream(index))
+    if st != MOE_OK:
+        raise MoeError(st, "moe_mx8_dequantize")
+    return out
+
+
+@dataclass
+class RmsNormOut:
+    """What a norm writes; reusable as its ``out``."""
+    y: torch.Tensor                  # the normed rows
+    h: torch.Tensor                  # x + residual, x itself without a residual
+    rstd: torch.Tensor               # fp32, one per row
+    y8: Mx8Rows | None = None        # the normed rows in 8 bits, where they are kept
+
+
+def _row_stride(t: torch.Tensor, cols: int) -> int:
+    """Elements from row to row of [..., cols], or -1: a 2-D tensor may have gaps between its rows, others are contiguous."""
+    if t.is_contiguous():
+        return cols
+    return t.stride(0) if t.dim() == 2 and t.stride(1) == 1 else -1
+
+
+def rms_norm(x: torch.Tensor, weight: torch.Tensor, residual: torch.Tensor | None = None, eps: float = 1e-6, keep: bool = False,
+             out: RmsNormOut | None = None) -> RmsNormOut:
+    """Root-mean-square norm of ``x`` + ``residual`` ([..., cols], bf16 / fp16 / fp32) times ``weight`` (the same type or fp32), on the
+    current stream of its device.  ``keep``: also in 8 bits, for a backward pass.  ``out.h`` may be ``residual``
+    itself."""
+    shape, dtype, index = x.shape, x.dtype, x.get_device()
+    code = _DTYPE_CODE.get(dtype)
+    _require(x.is_cuda and code is not None and len(shape) > 0 and shape[-1] > 0, "rms_norm")
+    cols, lead = shape[-1], shape[:-1]
+    n = x.numel() // cols
+    x_stride = _row_stride(x, cols)
+    r_stride = cols if residual is None else _row_stride(residual, cols)
+    _require(x_stride >= 0 and r_stride >= 0 and weight.dtype in (dtype, torch.float32) and _is_dense(weight, weight.dtype, (cols,), index)
+             and (residual is None or (residual.shape == shape and residual.dtype is dtype and residual.get_device() == index)), "rms_norm")
+    if out is None:
+        h = x if residual is None else x.new_empty(shape)
+        y8 = Mx8Rows(x.new_empty(shape, dtype=torch.uint8), x.new_empty((*lead, _mx_pitch(cols)), dtype=torch.uint8)) if keep else None
+        out = RmsNormOut(x.new_empty(shape), h, x.new_empty(lead, dtype=torch.float32), y8)
+    else:
+        _require(_is_dense(out.y, dtype, shape, index) and (residual is None or _is_dense(out.h, dtype, shape, index))
+                 and _is_dense(out.rstd, torch.float32, lead, index) and (not keep or _is_mx8(out.y8, index, shape)), "rms_norm")
+        if residual is None:
+            out.h = x
+    st = _on_device(index, moe_rms_norm, x.data_ptr(), x_stride, 0 if residual is None else residual.data_ptr(), r_stride, code, n, cols,
+                    weight.data_ptr(), _DTYPE_CODE[weight.dtype], eps, 0 if residual is None else out.h.data_ptr(), out.y.data_ptr(),
+                    out.rstd.data_ptr(), out.y8.codes.data_ptr() if keep else 0, out.y8.scales.data_ptr() if keep else 0, _raw_stream(index))
+    if st != MOE_OK:
+        raise MoeError(st, "moe_rms_norm")
+    return out
+
+
+def rms_norm_backward(dy: torch.Tensor, h: torch.Tensor, rstd: torch.Tensor, weight: torch.Tensor, dh: torch.Tensor | None = None,
+                      dx: torch.Tensor | None = None, d_weight: torch.Tensor | None = None):
+    """Gradient of rms_norm: (dx, d_weight), dx by x and by the residual alike, d_weight in fp32.  ``h`` and ``rstd``: of the
+    forward; ``dh``: the gradient that comes to h past the norm.  ``dx`` may be dy, dh or h itself."""
+    shape, dtype, index = dy.shape, dy.dtype, dy.get_device()
+    code = _DTYPE_CODE.get(dtype)
+    _require(dy.is_cuda and code is not None and len(shape) > 0 and shape[-1] > 0, "rms_norm_backward")
+    cols = shape[-1]
+    n = dy.numel() // cols
+    dx = torch.empty_like(dy) if dx is None else dx
+    d_weight = dy.new_empty(cols, dtype=torch.float32) if d_weight is None else d_weight
+    _require(all(_is_dense(t, dtype, shape, index) for t in ((dy, h, dx) if dh is None else (dy, h, dx, dh)))
+             and _is_dense(rstd, torch.float32, shape[:-1], index) and weight.dtype in (dtype, torch.float32)
+             and _is_dense(weight, weight.dtype, (cols,), index) and _is_dense(d_weight, torch.float32, (cols,), index), "rms_norm_backward")
+    ws = dy.new_empty(moe_rms_norm_backward_workspace(n, cols), dtype=torch.uint8)
+    st = _on_device(index, moe_rms_norm_backward, dy.data_ptr(), 0 if dh is None else dh.data_ptr(), h.data_ptr(), rstd.data_ptr(), code, n,
+                    cols, weight.data_ptr(), _DTYPE_CODE[weight.dtype], dx.data_ptr(), d_weight.data_ptr(), ws.data_ptr(), ws.numel(),
+                    _raw_stream(index))
+    if st != MOE_OK:
+        raise MoeError(st, "moe_rms_norm_backward")
+    return dx, d_weight
 
 
 def make_config(num_experts, top_k, hidden, max_tokens, num_ranks, slots_per_rank, max_replicas=2,
@@ -835,6 +964,20 @@ class MoeRouter:
         return dx, d_logits
 
     # -- experts in 16 bits and their gradients --------------------------------
+    def redispatch(self, x8: Mx8Rows, send_buf: torch.Tensor | None = None) -> torch.Tensor:
+        """The send buffer [T * k, H] of the latest dispatch once more, from its tokens' rows [T, H] in 8 bits."""
+        c, dev = self.cfg, self._index()
+        T, H = x8.codes.shape[0], c.hidden
+        _require(H % 32 == 0 and _is_mx8(x8, dev, (T, H)), "redispatch")
+        if send_buf is None:
+            send_buf = x8.codes.new_empty((T * c.top_k, H), dtype=torch.bfloat16)
+        else:
+            _require(_is_dense(send_buf, torch.bfloat16, (T * c.top_k, H), dev), "redispatch")
+        st = moe_redispatch(self._ctx, x8.codes.data_ptr(), x8.scales.data_ptr(), T, send_buf.data_ptr(), _raw_stream(dev))
+        if st != MOE_OK:
+            raise MoeError(st, "moe_redispatch")
+        return send_buf
+
     def _expert_ok(self, rows: torch.Tensor, cols: int, slot_counts, slot_offsets, weight: torch.Tensor, dev: int) -> bool:
         """Rows [n, cols] and one matrix [P, n_out, n_in] per slot, in bf16."""
         P = self.num_slots

@@ -8,10 +8,10 @@ import sys
 _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(CSRC, "libmoe_route.so")
-SOURCES = ["moe_route.cu", "permute_static.cu", "mx_rows.cu", "mx_product.cu", "expert_product.cu"]
+SOURCES = ["moe_route.cu", "permute_static.cu", "mx_rows.cu", "mx_product.cu", "expert_product.cu", "norm_rows.cu"]
 HEADERS = ["device_utils.cuh", "route_kernels.cuh", "scatter_kernels.cuh", "combine_kernels.cuh", "ep_kernels.cuh",
            "backward_kernels.cuh", "mx_format.cuh", "mx_scatter.cuh", "mx_product.h", "expert_product.h",
-           "mx8_format.cuh", "tcgen05.cuh",
+           "mx8_format.cuh", "tcgen05.cuh", "redispatch_kernels.cuh",
            os.path.join("..", "..", "include", "moe_route.h")]
 
 

@@ -19,6 +19,7 @@
 #include "expert_product.h"
 #include "mx_product.h"
 #include "mx_scatter.cuh"
+#include "redispatch_kernels.cuh"
 #include "route_kernels.cuh"
 #include "scatter_kernels.cuh"
 
@@ -1312,6 +1313,29 @@ moe_status moe_dispatch_backward(moe_ctx *ctx, const float *logits, const void *
 // ---------------------------------------------------------------------------
 // experts in 16 bits and their gradients
 // ---------------------------------------------------------------------------
+
+moe_status moe_redispatch(moe_ctx *ctx, const uint8_t *codes, const uint8_t *scales, int32_t T, void *send_buf, void *cuda_stream)
+{
+    if (!ctx || T < 0 || ctx->d.H % kMxBlock != 0) return MOE_ERR_INVALID_ARG;
+    if (ctx->last_T < 0 || T != ctx->last_T || ctx->ep_routed) return MOE_ERR_INVALID_ARG;
+    if (T == 0) return MOE_OK;
+    if (!codes || !scales || !send_buf || !aligned16(codes) || !aligned16(scales) || !aligned16(send_buf)) return MOE_ERR_INVALID_ARG;
+    const Derived &d = ctx->d;
+    const size_t n = (size_t)T * d.k, H = d.H;
+    if (spans_meet({{send_buf, n * H * 2}}, {{codes, T * H}, {scales, (size_t)T * mx_scale_pitch(d.H)}, {ctx->last_dst_row, n * 4}}))
+        return MOE_ERR_INVALID_ARG;
+    DeviceScope scope(ctx->device);
+    if (!scope.ok) return MOE_ERR_CUDA;
+    RedispatchParams p;
+    p.codes = reinterpret_cast<const uint2 *>(codes); p.scales = scales; p.dst_row = ctx->last_dst_row;
+    p.send = static_cast<uint4 *>(send_buf); p.T = T; p.k = d.k; p.hv = d.H / 8; p.pitch = mx_scale_pitch(d.H);
+    const auto launch = [&](auto kernel, int u) {
+        const long long items = (long long)T * ((p.hv + 32 * u - 1) / (32 * u));
+        const long long ctas = (items + kScatterThreads / 32 - 1) / (kScatterThreads / 32);
+        return launch_kernel(kernel, dim3((unsigned)ctas), dim3(kScatterThreads), 0, static_cast<cudaStream_t>(cuda_stream), ctx->pdl, p);
+    };
+    return launch(k_redispatch<4>, 4) == cudaSuccess ? MOE_OK : MOE_ERR_CUDA;
+}
 
 moe_status moe_expert_product(moe_ctx *ctx, const void *a, int64_t rows, const int32_t *slot_counts, const int32_t *slot_offsets,
                               const void *w, int32_t n_out, int32_t n_in, void *y, void *cuda_stream)

@@ -1,4 +1,4 @@
-// moe_mx_quantize / moe_mx_dequantize: rows to the microscaled 4-bit format and back.
+// moe_mx_quantize / moe_mx_dequantize: rows to the microscaled 4-bit format and back; moe_mx8_dequantize: back from 8 bits.
 //
 // Both are one pass over the data and bound by HBM: n elements of `size` bytes are read (written)
 // once and n * 17/32 bytes written (read).  A thread owns eight consecutive elements (one 16-byte
@@ -7,7 +7,7 @@
 // elements are numbered through all rows, so short rows fill the warps as well as long ones.
 #include "../../include/moe_route.h"
 
-#include "mx_format.cuh"
+#include "mx8_format.cuh"
 
 namespace {
 
@@ -57,7 +57,7 @@ __device__ __forceinline__ void from_f32(const float (&v)[8], uint4 (&u)[Elem<DT
 struct RowParams {
     char *x;             // rows of `stride` bytes
     long long stride;
-    uint8_t *codes;      // [rows, cols/2]
+    uint8_t *codes;      // [rows, cols/2], of 8 bits [rows, cols]
     uint8_t *scales;     // [rows, pitch]
     long long units;     // rows * cols/8
     int upr;             // units per row
@@ -136,12 +136,21 @@ __global__ void __launch_bounds__(kRowThreads) k_mx_quantize_small(RowParams p)
     }
 }
 
-template <int DT, int UN>
+// The codes of a unit of eight elements and their values.
+template <int BITS> struct Codes;
+template <> struct Codes<4> { typedef uint32_t Word; };
+template <> struct Codes<8> { typedef uint2 Word; };
+__device__ __forceinline__ void unpack8(uint32_t c, float (&v)[8]) { mx_unpack8(c, v); }
+__device__ __forceinline__ void unpack8(uint2 c, float (&v)[8]) { mx8_unpack4(c.x, v); mx8_unpack4(c.y, v + 4); }
+
+template <int DT, int UN, int BITS>
 __global__ void __launch_bounds__(kRowThreads) k_mx_dequantize(RowParams p)
 {
+    typedef typename Codes<BITS>::Word Word;
     const long long first = (long long)blockIdx.x * (kRowThreads * UN);
     const UnitBase b = unit_base(p, first);
-    uint32_t c[UN], s[UN];
+    Word c[UN];
+    uint32_t s[UN];
     long long row[UN]; unsigned col[UN];
 #pragma unroll
     for (int i = 0; i < UN; ++i) {
@@ -150,7 +159,7 @@ __global__ void __launch_bounds__(kRowThreads) k_mx_dequantize(RowParams p)
         row[i] = b.row + dr; col[i] = off - dr * p.upr;
         const long long u = first + i * kRowThreads + threadIdx.x;
         if (u < p.units) {
-            c[i] = __ldg(reinterpret_cast<const uint32_t *>(p.codes) + u);
+            c[i] = __ldg(reinterpret_cast<const Word *>(p.codes) + u);
             s[i] = __ldg(p.scales + row[i] * p.pitch + (col[i] >> 2));
         }
     }
@@ -158,7 +167,7 @@ __global__ void __launch_bounds__(kRowThreads) k_mx_dequantize(RowParams p)
     for (int i = 0; i < UN; ++i) {
         if (first + i * kRowThreads + threadIdx.x >= p.units) continue;
         float v[8];
-        mx_unpack8(c[i], v);
+        unpack8(c[i], v);
         const float scale = mx_scale_value(s[i]);
 #pragma unroll
         for (int q = 0; q < 8; ++q) v[q] *= scale;            // exact unless the type's range is left
@@ -174,7 +183,7 @@ bool aligned(const void *p, unsigned a) { return (reinterpret_cast<uintptr_t>(p)
 
 // Checks shared by both directions; fills everything but the launch shape.
 moe_status fill(RowParams *p, const void *x, int32_t dtype, long long rows, int32_t cols, long long row_stride,
-                const uint8_t *codes, const uint8_t *scales)
+                const uint8_t *codes, const uint8_t *scales, int bits = 4)
 {
     if (rows < 0 || cols < kMxBlock || cols % kMxBlock != 0) return MOE_ERR_INVALID_ARG;
     if (dtype != MOE_DTYPE_BF16 && dtype != MOE_DTYPE_F16 && dtype != MOE_DTYPE_F32) return MOE_ERR_INVALID_ARG;
@@ -187,10 +196,10 @@ moe_status fill(RowParams *p, const void *x, int32_t dtype, long long rows, int3
     if (!x || !codes || !scales || !aligned(x, 16) || !aligned(codes, 16) || !aligned(scales, 16)) return MOE_ERR_INVALID_ARG;
     if (rows > 1 && (row_stride * size) % 16 != 0) return MOE_ERR_INVALID_ARG;
     // One side is read while the other is written, in no particular order.
-    const size_t row_bytes = (size_t)cols * size, stride_bytes = rows > 1 ? (size_t)row_stride * size : row_bytes;
-    if (rows_overlap(x, rows, row_bytes, stride_bytes, codes, (size_t)rows * (cols / 2)) ||
+    const size_t row_bytes = (size_t)cols * size, code_bytes = (size_t)rows * cols * bits / 8, stride_bytes = rows > 1 ? (size_t)row_stride * size : row_bytes;
+    if (rows_overlap(x, rows, row_bytes, stride_bytes, codes, code_bytes) ||
         rows_overlap(x, rows, row_bytes, stride_bytes, scales, (size_t)rows * mx_scale_pitch(cols)) ||
-        ranges_overlap(codes, (size_t)rows * (cols / 2), scales, (size_t)rows * mx_scale_pitch(cols)))
+        ranges_overlap(codes, code_bytes, scales, (size_t)rows * mx_scale_pitch(cols)))
         return MOE_ERR_INVALID_ARG;
     p->x = static_cast<char *>(const_cast<void *>(x));
     p->stride = row_stride * size;
@@ -220,13 +229,27 @@ void launch_quantize(const RowParams &p, cudaStream_t st)
         k_mx_quantize<DT><<<(unsigned)((p.units + 4 * kRowThreads - 1) / (4 * kRowThreads)), kRowThreads, 0, st>>>(p);
 }
 
-template <int DT>
+template <int DT, int BITS>
 void launch_dequantize(const RowParams &p, cudaStream_t st)
 {
     if (p.units <= kFewUnits)
-        k_mx_dequantize<DT, 1><<<(unsigned)((p.units + kRowThreads - 1) / kRowThreads), kRowThreads, 0, st>>>(p);
+        k_mx_dequantize<DT, 1, BITS><<<(unsigned)((p.units + kRowThreads - 1) / kRowThreads), kRowThreads, 0, st>>>(p);
     else
-        k_mx_dequantize<DT, 4><<<(unsigned)((p.units + 4 * kRowThreads - 1) / (4 * kRowThreads)), kRowThreads, 0, st>>>(p);
+        k_mx_dequantize<DT, 4, BITS><<<(unsigned)((p.units + 4 * kRowThreads - 1) / (4 * kRowThreads)), kRowThreads, 0, st>>>(p);
+}
+
+template <int BITS>
+moe_status dequantize(const uint8_t *codes, const uint8_t *scales, int64_t rows, int32_t cols, void *y, int32_t dtype, int64_t row_stride,
+                      void *cuda_stream)
+{
+    RowParams p;
+    const moe_status ms = fill(&p, y, dtype, rows, cols, row_stride, codes, scales, BITS);
+    if (ms != MOE_OK || p.units == 0) return ms;
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    if (dtype == MOE_DTYPE_BF16) launch_dequantize<MOE_DTYPE_BF16, BITS>(p, st);
+    else if (dtype == MOE_DTYPE_F16) launch_dequantize<MOE_DTYPE_F16, BITS>(p, st);
+    else launch_dequantize<MOE_DTYPE_F32, BITS>(p, st);
+    return cudaGetLastError() == cudaSuccess ? MOE_OK : MOE_ERR_CUDA;
 }
 
 }  // namespace
@@ -254,14 +277,13 @@ moe_status moe_mx_quantize(const void *x, int32_t dtype, int64_t rows, int32_t c
 moe_status moe_mx_dequantize(const uint8_t *codes, const uint8_t *scales, int64_t rows, int32_t cols, void *y, int32_t dtype,
                              int64_t row_stride, void *cuda_stream)
 {
-    RowParams p;
-    const moe_status ms = fill(&p, y, dtype, rows, cols, row_stride, codes, scales);
-    if (ms != MOE_OK || p.units == 0) return ms;
-    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    if (dtype == MOE_DTYPE_BF16) launch_dequantize<MOE_DTYPE_BF16>(p, st);
-    else if (dtype == MOE_DTYPE_F16) launch_dequantize<MOE_DTYPE_F16>(p, st);
-    else launch_dequantize<MOE_DTYPE_F32>(p, st);
-    return cudaGetLastError() == cudaSuccess ? MOE_OK : MOE_ERR_CUDA;
+    return dequantize<4>(codes, scales, rows, cols, y, dtype, row_stride, cuda_stream);
+}
+
+moe_status moe_mx8_dequantize(const uint8_t *codes, const uint8_t *scales, int64_t rows, int32_t cols, void *y, int32_t dtype,
+                              int64_t row_stride, void *cuda_stream)
+{
+    return dequantize<8>(codes, scales, rows, cols, y, dtype, row_stride, cuda_stream);
 }
 
 }  // extern "C"

@@ -1,0 +1,427 @@
+// moe_rms_norm / moe_rms_norm_backward: the norm in front of a layer, with the residual's addition, and its gradient.
+//
+//   h = x + residual (rounded to the rows' type), rstd = 1 / sqrt(mean(h^2) + eps), y = h * rstd * weight,
+//   and y in 8 bits (mx8_format.cuh) where it is kept for a backward pass
+//   backward, with n = h * rstd and g = dy * weight:  dx = rstd * (g - n * mean(g * n)) + dh,  d_weight = sum over rows of dy * n
+//
+// Both are one pass over the rows and bound by HBM.  A row is taken by TPR threads, which hold it in registers between the
+// reduction and the result: a warp up to 1024 columns, a CTA of 256 or 1024 threads above.  A thread owns units of eight
+// consecutive elements (one 16-byte access of a 16-bit type), so four neighbouring lanes own a block of the 8-bit form.  All
+// sums are fp32, in an order that depends on the sizes alone; every output is rounded once.
+#include "../../include/moe_route.h"
+
+#include <algorithm>
+
+#include "mx8_format.cuh"
+
+namespace {
+
+using namespace moe;
+
+constexpr int kUnits = 4;                  // units of eight elements per thread
+constexpr int kMaxCols = 1024 * kUnits * 8;
+constexpr int kNormCtas = 296;             // CTAs of a backward pass, each with a row of partial sums of d_weight
+
+template <int DT> constexpr int kVec = DT == MOE_DTYPE_F32 ? 2 : 1;   // 16-byte words of a unit
+
+// Rows are read once.  (Not through the read-only path: an output may take the place of an input.)
+__device__ __forceinline__ uint4 load_v4(const uint4 *p)
+{
+    uint4 v;
+    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory");
+    return v;
+}
+
+template <int DT>
+__device__ __forceinline__ void to_f32(const uint4 (&u)[kVec<DT>], float (&v)[8])
+{
+    if constexpr (DT == MOE_DTYPE_F32) {
+        const uint32_t w[8] = {u[0].x, u[0].y, u[0].z, u[0].w, u[1].x, u[1].y, u[1].z, u[1].w};
+#pragma unroll
+        for (int q = 0; q < 8; ++q) v[q] = __uint_as_float(w[q]);
+    } else {
+        const uint32_t w[4] = {u[0].x, u[0].y, u[0].z, u[0].w};
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            if constexpr (DT == MOE_DTYPE_BF16) {
+                v[2 * q] = __uint_as_float(w[q] << 16);
+                v[2 * q + 1] = __uint_as_float(w[q] & 0xffff0000u);
+            } else {
+                const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&w[q]));
+                v[2 * q] = f.x; v[2 * q + 1] = f.y;
+            }
+        }
+    }
+}
+
+template <int DT>
+__device__ __forceinline__ void from_f32(const float (&v)[8], uint4 (&u)[kVec<DT>])
+{
+    uint32_t *w = reinterpret_cast<uint32_t *>(&u[0]);
+    if constexpr (DT == MOE_DTYPE_F32) {
+#pragma unroll
+        for (int q = 0; q < 8; ++q) w[q] = __float_as_uint(v[q]);
+    } else {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            if constexpr (DT == MOE_DTYPE_BF16) {
+                const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * q], v[2 * q + 1]);
+                w[q] = *reinterpret_cast<const uint32_t *>(&h);
+            } else {
+                const __half2 h = __floats2half2_rn(v[2 * q], v[2 * q + 1]);
+                w[q] = *reinterpret_cast<const uint32_t *>(&h);
+            }
+        }
+    }
+}
+
+// Eight elements of the weight, of the rows' type or fp32.
+template <int DT>
+__device__ __forceinline__ void weight8(const void *weight, bool f32, int unit, float (&v)[8])
+{
+    if (f32) {
+        uint4 u[2];
+        u[0] = __ldg(static_cast<const uint4 *>(weight) + 2 * unit);
+        u[1] = __ldg(static_cast<const uint4 *>(weight) + 2 * unit + 1);
+        to_f32<MOE_DTYPE_F32>(u, v);
+    } else {
+        uint4 u[kVec<DT>];
+#pragma unroll
+        for (int q = 0; q < kVec<DT>; ++q) u[q] = __ldg(static_cast<const uint4 *>(weight) + kVec<DT> * unit + q);
+        to_f32<DT>(u, v);
+    }
+}
+
+// Sum over the TPR threads of a row; `scratch` holds a float per warp, and every thread passes the same `turn`, 0 and 1 in turn.
+template <int TPR>
+__device__ __forceinline__ float row_sum(float v, float *scratch, int turn)
+{
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) v += __shfl_xor_sync(0xffffffffu, v, off);
+    if (TPR == 32) return v;
+    constexpr int kWarps = TPR / 32;
+    scratch += turn * kWarps;
+    if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = v;
+    __syncthreads();
+    v = (threadIdx.x & 31) < kWarps ? scratch[threadIdx.x & 31] : 0.0f;
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) v += __shfl_xor_sync(0xffffffffu, v, off);
+    return v;
+}
+
+struct NormParams {
+    const uint4 *x, *residual;     // rows of x_stride and r_stride words of 16 bytes; residual may be NULL
+    long long x_stride, r_stride;
+    const void *weight;
+    bool weight_f32;
+    float eps;
+    long long rows;
+    int units;                     // of a row
+    uint4 *h, *y;                  // h may be NULL
+    float *rstd;                   // may be NULL
+    uint8_t *codes, *scales;       // may be NULL
+    int pitch;
+};
+
+template <int TPR> constexpr int kBlock = TPR < 256 ? 256 : TPR;
+
+template <int DT, int TPR>
+__global__ void __launch_bounds__(kBlock<TPR>) k_rms_norm(NormParams p)
+{
+    constexpr int V = kVec<DT>;
+    __shared__ float scratch[32];
+    const int tid = threadIdx.x % TPR;
+    const long long row = (long long)blockIdx.x * (kBlock<TPR> / TPR) + threadIdx.x / TPR;
+    if (TPR < kBlock<TPR> && row >= p.rows) return;            // whole warps
+    const uint4 *x = p.x + row * p.x_stride, *res = p.residual ? p.residual + row * p.r_stride : nullptr;
+    uint4 in[kUnits][V], add[kUnits][V];
+#pragma unroll
+    for (int i = 0; i < kUnits; ++i) {
+        const int u = i * TPR + tid;
+#pragma unroll
+        for (int q = 0; q < V; ++q) {
+            in[i][q] = u < p.units ? load_v4(x + u * V + q) : make_uint4(0u, 0u, 0u, 0u);
+            if (res) add[i][q] = u < p.units ? load_v4(res + u * V + q) : make_uint4(0u, 0u, 0u, 0u);
+        }
+    }
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kUnits; ++i) {
+        float a[8];
+        to_f32<DT>(in[i], a);
+        if (res) {
+            float b[8];
+            to_f32<DT>(add[i], b);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) a[q] += b[q];
+            from_f32<DT>(a, in[i]);                            // the norm is that of the stored sum
+            to_f32<DT>(in[i], a);
+        }
+#pragma unroll
+        for (int q = 0; q < 8; ++q) sum += a[q] * a[q];
+        const int u = i * TPR + tid;
+        if (p.h && u < p.units)
+#pragma unroll
+            for (int q = 0; q < V; ++q) p.h[(row * p.units + u) * V + q] = in[i][q];
+    }
+    const float rstd = rsqrtf(row_sum<TPR>(sum, scratch, 0) / (float)(p.units * 8) + p.eps);
+    if (p.rstd && tid == 0) p.rstd[row] = rstd;
+#pragma unroll
+    for (int i = 0; i < kUnits; ++i) {
+        const int u = i * TPR + tid;
+        const bool inside = u < p.units;                       // with an 8-bit form whole blocks: all four lanes of one or none
+        float a[8], w[8];
+        to_f32<DT>(in[i], a);
+        if (inside) weight8<DT>(p.weight, p.weight_f32, u, w);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) a[q] = inside ? a[q] * rstd * w[q] : 0.0f;
+        if (inside) {
+            uint4 o[V];
+            from_f32<DT>(a, o);
+#pragma unroll
+            for (int q = 0; q < V; ++q) p.y[(row * p.units + u) * V + q] = o[q];
+        }
+        if (p.codes) {
+            uint32_t amax = mx8_amax(a);
+            amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
+            amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
+            const uint32_t s = mx8_scale_byte(amax);
+            if (inside) *reinterpret_cast<uint2 *>(p.codes + (row * p.units + u) * 8) = mx8_quantize8(a, s);
+            // the padding of the scales is written as 0
+            if ((u & 3) == 0 && u / 4 < p.pitch) p.scales[row * p.pitch + u / 4] = inside ? (uint8_t)s : (uint8_t)0;
+        }
+    }
+}
+
+struct NormBackwardParams {
+    const uint4 *dy, *dh, *h;      // dh may be NULL
+    const float *rstd;
+    const void *weight;
+    bool weight_f32;
+    long long rows;
+    int units;
+    uint4 *dx;
+    float *partial;                // [CTAs, cols]
+};
+
+template <int DT, int TPR>
+__global__ void __launch_bounds__(kBlock<TPR>) k_rms_norm_backward(NormBackwardParams p)
+{
+    constexpr int V = kVec<DT>, kRows = kBlock<TPR> / TPR;
+    __shared__ float scratch[64];
+    extern __shared__ float sums[];                            // [kRows, cols], where a CTA has several rows at a time
+    const int tid = threadIdx.x % TPR, sub = threadIdx.x / TPR;
+    float acc[kUnits][8] = {};
+    int turn = 0;
+    for (long long row = (long long)blockIdx.x * kRows + sub; row < p.rows; row += (long long)gridDim.x * kRows) {
+        uint4 a[kUnits][V], b[kUnits][V];
+#pragma unroll
+        for (int i = 0; i < kUnits; ++i) {
+            const int u = i * TPR + tid;
+#pragma unroll
+            for (int q = 0; q < V; ++q) {
+                a[i][q] = u < p.units ? load_v4(p.dy + (row * p.units + u) * V + q) : make_uint4(0u, 0u, 0u, 0u);
+                b[i][q] = u < p.units ? load_v4(p.h + (row * p.units + u) * V + q) : make_uint4(0u, 0u, 0u, 0u);
+            }
+        }
+        const float rstd = __ldg(p.rstd + row);
+        float sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kUnits; ++i) {
+            const int u = i * TPR + tid;
+            if (u >= p.units) continue;
+            float dy[8], n[8], w[8];
+            to_f32<DT>(a[i], dy); to_f32<DT>(b[i], n);
+            weight8<DT>(p.weight, p.weight_f32, u, w);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+                n[q] *= rstd;
+                sum += dy[q] * w[q] * n[q];
+                acc[i][q] += dy[q] * n[q];
+            }
+        }
+        const float mean = row_sum<TPR>(sum, scratch, turn) / (float)(p.units * 8);
+        turn ^= 1;
+#pragma unroll
+        for (int i = 0; i < kUnits; ++i) {
+            const int u = i * TPR + tid;
+            if (u >= p.units) continue;
+            float dy[8], n[8], w[8], d[8];
+            to_f32<DT>(a[i], dy); to_f32<DT>(b[i], n);
+            weight8<DT>(p.weight, p.weight_f32, u, w);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) d[q] = rstd * (dy[q] * w[q] - n[q] * rstd * mean);
+            if (p.dh) {
+                uint4 c[V];
+                float past[8];
+#pragma unroll
+                for (int q = 0; q < V; ++q) c[q] = load_v4(p.dh + (row * p.units + u) * V + q);
+                to_f32<DT>(c, past);
+#pragma unroll
+                for (int q = 0; q < 8; ++q) d[q] += past[q];
+            }
+            uint4 o[V];
+            from_f32<DT>(d, o);
+#pragma unroll
+            for (int q = 0; q < V; ++q) p.dx[(row * p.units + u) * V + q] = o[q];
+        }
+    }
+    const int cols = p.units * 8;
+    float *mine = kRows > 1 ? sums + sub * cols : p.partial + (size_t)blockIdx.x * cols;
+#pragma unroll
+    for (int i = 0; i < kUnits; ++i) {
+        const int u = i * TPR + tid;
+        if (u >= p.units) continue;
+        float4 *dst = reinterpret_cast<float4 *>(mine + u * 8);
+        dst[0] = make_float4(acc[i][0], acc[i][1], acc[i][2], acc[i][3]);
+        dst[1] = make_float4(acc[i][4], acc[i][5], acc[i][6], acc[i][7]);
+    }
+    if (kRows > 1) {
+        __syncthreads();
+        for (int c = threadIdx.x; c < cols; c += kBlock<TPR>) {
+            float s = 0.0f;
+#pragma unroll
+            for (int r = 0; r < kRows; ++r) s += sums[r * cols + c];
+            p.partial[(size_t)blockIdx.x * cols + c] = s;
+        }
+    }
+}
+
+// d_weight: the CTAs' sums added up, 32 of them side by side for each four columns.
+__global__ void __launch_bounds__(1024) k_norm_weight(const float4 *partial, int ctas, int quads, float4 *d_weight)
+{
+    __shared__ float4 sums[32][33];
+    const int lane = threadIdx.x & 31, slice = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
+    float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    if (c < quads)
+        for (int i = slice; i < ctas; i += 32) {
+            const float4 v = __ldcg(partial + (size_t)i * quads + c);
+            s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+        }
+    sums[slice][lane] = s;
+    __syncthreads();
+    if (slice != 0 || c >= quads) return;
+    for (int i = 1; i < 32; ++i) {
+        const float4 v = sums[i][lane];
+        s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+    }
+    d_weight[c] = s;
+}
+
+bool aligned(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+bool is_dtype(int32_t d) { return d == MOE_DTYPE_BF16 || d == MOE_DTYPE_F16 || d == MOE_DTYPE_F32; }
+
+// f(type, threads of a row) for the kernel that rows of `units` units of this type take
+template <typename F>
+void with_kernel(int32_t dtype, int units, F f)
+{
+    const auto by_width = [&](auto dt) {
+        if (units <= 32 * kUnits) f(dt, std::integral_constant<int, 32>());
+        else if (units <= 256 * kUnits) f(dt, std::integral_constant<int, 256>());
+        else f(dt, std::integral_constant<int, 1024>());
+    };
+    if (dtype == MOE_DTYPE_BF16) by_width(std::integral_constant<int, MOE_DTYPE_BF16>());
+    else if (dtype == MOE_DTYPE_F16) by_width(std::integral_constant<int, MOE_DTYPE_F16>());
+    else by_width(std::integral_constant<int, MOE_DTYPE_F32>());
+}
+
+moe_status check_norm(int32_t dtype, int32_t weight_dtype, int64_t rows, int32_t cols)
+{
+    if (rows < 0 || cols < 8 || cols % 8 != 0 || cols > kMaxCols || !is_dtype(dtype)) return MOE_ERR_INVALID_ARG;
+    if (weight_dtype != dtype && weight_dtype != MOE_DTYPE_F32) return MOE_ERR_INVALID_ARG;
+    return rows > (1ll << 31) - 1 ? MOE_ERR_CAPACITY : MOE_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+moe_status moe_rms_norm(const void *x, int64_t x_stride, const void *residual, int64_t residual_stride, int32_t dtype, int64_t rows,
+                        int32_t cols, const void *weight, int32_t weight_dtype, float eps, void *h, void *y, float *rstd, uint8_t *codes,
+                        uint8_t *scales, void *cuda_stream)
+{
+    const moe_status ms = check_norm(dtype, weight_dtype, rows, cols);
+    if (ms != MOE_OK) return ms;
+    if (!(eps >= 0.0f) || (codes == nullptr) != (scales == nullptr) || (codes && cols % kMxBlock != 0)) return MOE_ERR_INVALID_ARG;
+    if (rows == 0) return MOE_OK;
+    const long long size = dtype == MOE_DTYPE_F32 ? 4 : 2;
+    if (rows > 1 && (x_stride < cols || x_stride > (1ll << 40) || x_stride * size % 16 != 0)) return MOE_ERR_INVALID_ARG;
+    if (rows > 1 && residual && (residual_stride < cols || residual_stride > (1ll << 40) || residual_stride * size % 16 != 0))
+        return MOE_ERR_INVALID_ARG;
+    if (!x || !weight || !y || (residual && !h) || !aligned(x) || !aligned(residual) || !aligned(weight) || !aligned(h) || !aligned(y) ||
+        !aligned(codes) || !aligned(scales))
+        return MOE_ERR_INVALID_ARG;
+    // Outputs may not lie on inputs or on one another, but for h in the place of x or of the residual: a thread
+    // has read what it overwrites there.
+    const size_t n = rows, row = (size_t)cols * size;
+    const struct { const void *at; size_t bytes; } out[5] = {
+        {y, n * row}, {codes, codes ? n * cols : 0}, {scales, codes ? n * mx_scale_pitch(cols) : 0}, {rstd, rstd ? n * 4 : 0}, {h, h ? n * row : 0}};
+    for (int i = 0; i < 5; ++i) {
+        for (int j = 0; j < i; ++j)
+            if (ranges_overlap(out[i].at, out[i].bytes, out[j].at, out[j].bytes)) return MOE_ERR_INVALID_ARG;
+        if (ranges_overlap(out[i].at, out[i].bytes, weight, (size_t)cols * (weight_dtype == MOE_DTYPE_F32 ? 4 : 2))) return MOE_ERR_INVALID_ARG;
+        const bool same_x = i == 4 && h == x && (rows == 1 || x_stride == cols);
+        const bool same_r = i == 4 && h == residual && (rows == 1 || residual_stride == cols);
+        if (!same_x && rows_overlap(x, rows, row, rows > 1 ? x_stride * size : row, out[i].at, out[i].bytes)) return MOE_ERR_INVALID_ARG;
+        if (residual && !same_r && rows_overlap(residual, rows, row, rows > 1 ? residual_stride * size : row, out[i].at, out[i].bytes))
+            return MOE_ERR_INVALID_ARG;
+    }
+    NormParams p;
+    p.x = static_cast<const uint4 *>(x); p.residual = static_cast<const uint4 *>(residual);
+    p.x_stride = x_stride * size / 16; p.r_stride = residual_stride * size / 16;
+    p.weight = weight; p.weight_f32 = weight_dtype == MOE_DTYPE_F32; p.eps = eps; p.rows = rows; p.units = cols / 8;
+    p.h = static_cast<uint4 *>(h); p.y = static_cast<uint4 *>(y); p.rstd = rstd; p.codes = codes; p.scales = scales;
+    p.pitch = mx_scale_pitch(cols);
+    with_kernel(dtype, p.units, [&](auto dt, auto tpr) {
+        constexpr int kRows = kBlock<tpr> / tpr;
+        k_rms_norm<dt, tpr><<<(unsigned)((rows + kRows - 1) / kRows), kBlock<tpr>, 0, static_cast<cudaStream_t>(cuda_stream)>>>(p);
+    });
+    return cudaGetLastError() == cudaSuccess ? MOE_OK : MOE_ERR_CUDA;
+}
+
+size_t moe_rms_norm_backward_workspace(int64_t rows, int32_t cols)
+{
+    return rows < 1 || cols < 8 || cols % 8 != 0 || cols > kMaxCols ? 0 : (size_t)std::min<int64_t>(rows, kNormCtas) * cols * 4;
+}
+
+moe_status moe_rms_norm_backward(const void *dy, const void *dh, const void *h, const float *rstd, int32_t dtype, int64_t rows,
+                                 int32_t cols, const void *weight, int32_t weight_dtype, void *dx, float *d_weight, void *workspace,
+                                 size_t workspace_bytes, void *cuda_stream)
+{
+    const moe_status ms = check_norm(dtype, weight_dtype, rows, cols);
+    if (ms != MOE_OK) return ms;
+    if (!d_weight || !aligned(d_weight)) return MOE_ERR_INVALID_ARG;
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    if (rows == 0) return cudaMemsetAsync(d_weight, 0, (size_t)cols * 4, st) == cudaSuccess ? MOE_OK : MOE_ERR_CUDA;
+    if (!dy || !h || !rstd || !weight || !dx || !workspace || !aligned(dy) || !aligned(dh) || !aligned(h) || !aligned(weight) || !aligned(dx) ||
+        !aligned(workspace))
+        return MOE_ERR_INVALID_ARG;
+    const size_t need = moe_rms_norm_backward_workspace(rows, cols);
+    if (workspace_bytes < need) return MOE_ERR_CAPACITY;
+    // dx may take the place of dy, of dh or of h: a thread has read what it overwrites there
+    const size_t n = rows, bytes = n * cols * (dtype == MOE_DTYPE_F32 ? 4 : 2), w = (size_t)cols * (weight_dtype == MOE_DTYPE_F32 ? 4 : 2);
+    const struct { const void *at; size_t bytes; } out[3] = {{dx, bytes}, {d_weight, (size_t)cols * 4}, {workspace, need}},
+        in[5] = {{dy, bytes}, {dh, dh ? bytes : 0}, {h, bytes}, {rstd, n * 4}, {weight, w}};
+    for (int i = 0; i < 3; ++i) {
+        for (int j = 0; j < i; ++j)
+            if (ranges_overlap(out[i].at, out[i].bytes, out[j].at, out[j].bytes)) return MOE_ERR_INVALID_ARG;
+        for (int j = 0; j < 5; ++j)
+            if (!(i == 0 && j < 3 && dx == in[j].at) && ranges_overlap(out[i].at, out[i].bytes, in[j].at, in[j].bytes)) return MOE_ERR_INVALID_ARG;
+    }
+    NormBackwardParams p;
+    p.dy = static_cast<const uint4 *>(dy); p.dh = static_cast<const uint4 *>(dh); p.h = static_cast<const uint4 *>(h);
+    p.rstd = rstd; p.weight = weight; p.weight_f32 = weight_dtype == MOE_DTYPE_F32; p.rows = rows; p.units = cols / 8;
+    p.dx = static_cast<uint4 *>(dx); p.partial = static_cast<float *>(workspace);
+    int ctas = 0;
+    with_kernel(dtype, p.units, [&](auto dt, auto tpr) {
+        constexpr int kRows = kBlock<tpr> / tpr;
+        ctas = (int)std::min<int64_t>((rows + kRows - 1) / kRows, kNormCtas);
+        k_rms_norm_backward<dt, tpr><<<ctas, kBlock<tpr>, kRows > 1 ? (size_t)kRows * cols * 4 : 0, st>>>(p);
+    });
+    if (cudaGetLastError() != cudaSuccess) return MOE_ERR_CUDA;
+    k_norm_weight<<<(cols / 4 + 31) / 32, 1024, 0, st>>>(static_cast<const float4 *>(workspace), ctas, cols / 4, reinterpret_cast<float4 *>(d_weight));
+    return cudaGetLastError() == cudaSuccess ? MOE_OK : MOE_ERR_CUDA;
+}
+
+}  // extern "C"
