@@ -241,7 +241,7 @@ struct Layout {
     static constexpr int kBTile = kN * kLine;
     static constexpr int kStage = kATile + kBTile;            // multiples of 1024: swizzle alignment
     static constexpr int kEpiWarp = 32 * 32 * 4;              // a plane of fp32 sums, or a box of a weight gradient
-    static constexpr int kBars = 3 * kMaxStages + 5;
+    static constexpr int kBars = 4 * kMaxStages + 5;
     static constexpr int kEpiOff = 0, kBarOff = kEpiWarps * kEpiWarp;
     static constexpr int kEndsOff = kBarOff + ((kBars * 8 + 16 + 4 * (kThreads / 32) + 15) & ~15);
     static constexpr int kSmem = 227 * 1024;
@@ -249,6 +249,31 @@ struct Layout {
     static int stages(int P) { return std::min<int>(kMaxStages, (int)((kSmem - 1024 - fixed(P)) / kStage)); }
     static size_t bytes(int P) { return 1024 + fixed(P) + (size_t)stages(P) * kStage; }
 };
+
+// Whether the last of `left` rows of a weight gradient's segment end inside a K = 16 of this stage.
+__device__ __forceinline__ bool has_tail(int left) { return left < kStageK && (left & 15) != 0; }
+
+// Both operands of a stage of a weight gradient, 64 features by 64 rows at a time.
+template <int CG, int N>
+__device__ __forceinline__ void load_grad(unsigned char *a, unsigned char *b, const CUtensorMap *map_a, const CUtensorMap *map_b, int feat, int col,
+                                          int row, uint32_t bar)
+{
+#pragma unroll
+    for (int q = 0; q < kFeat / 64; ++q) tma_2d<CG>(a + q * kChunk, map_a, feat + q * 64, row, bar);
+#pragma unroll
+    for (int q = 0; q < N / 64; ++q) tma_2d<CG>(b + q * kChunk, map_b, col + q * 64, row, bar);
+}
+
+// The lines of a stage behind a segment, up to a whole K = 16, are made zero in both operands: they hold the next segment's rows
+// (and a NaN there times a zero would still be one).  A line is 128 bytes of one k in each of the stage's chunks.
+__device__ __forceinline__ void clear_tail(unsigned char *stage, int bytes, int left, int lane)
+{
+    unsigned char *lines = stage + (lane & 7) * 16;
+    for (int i = left; i < ((left + 15) & ~15); ++i)
+        for (int q = (lane >> 3) * kChunk; q < bytes; q += 4 * kChunk) *reinterpret_cast<uint4 *>(lines + q + i * kLine) = make_uint4(0u, 0u, 0u, 0u);
+    fence_async_shared();
+    __syncwarp();
+}
 
 // Bounded wait.  `quit` is shared by the CTA: the first role that gives up sets it, the others follow.
 template <bool CLUSTER = false>
@@ -410,27 +435,35 @@ __device__ __forceinline__ void store_gated_backward(const KernelParams &p, cons
     }
 }
 
+// Stages after which a tile of a weight gradient in fp32 goes on in another accumulator, whose sums are added to the first
+// one's in memory.  The tensor core cuts off what it adds, which shrinks a sum by some 2e-8 of itself with each K = 16
+// (1.0e-6 off after 1024 rows, 1.6e-5 after 16384): sums of 2048 rows stay at 2e-6.  A sum that is rounded to bf16 needs no such care.
+template <bool F32> constexpr int kAccSteps = F32 ? 2048 / kStageK : 1 << 30;
+
 // 32 features x 32 (fp32) or 64 (bf16) columns of a weight gradient leave as one TMA store from a box of 32 lines of
 // 128 bytes, 128-byte swizzle; what lies outside the matrix is cut by the store.  An addition is done by the memory
 // system, one for each element, so its order is no question.
 template <bool F32>
-__device__ __forceinline__ void store_grad(const KernelParams &p, const CUtensorMap *map, const Tile &t, int f, int col, const uint4 (&v)[8],
-                                           unsigned char *box, int lane)
+__device__ __forceinline__ void store_grad(const CUtensorMap *map, int slot, int f, int col, const uint4 (&v)[8], unsigned char *box, int lane,
+                                           bool add, bool more)
 {
-    if (lane == 0) bulk_wait_read<0>();                        // the store before has left the box
+    if (lane == 0) {
+        if (F32 && more) bulk_wait_all();                      // the sums of the rows before are where these are added
+        else bulk_wait_read<0>();                              // the store before has left the box
+    }
     __syncwarp();
 #pragma unroll
     for (int q = 0; q < 8; ++q) *reinterpret_cast<uint4 *>(box + lane * kLine + ((q ^ (lane & 7)) << 4)) = v[q];
     fence_async_shared();
     __syncwarp();
     if (lane == 0) {
-        if (F32 && p.add)
+        if (F32 && (add || more))
             asm volatile("cp.reduce.async.bulk.tensor.3d.global.shared::cta.add.tile.bulk_group [%0, {%1, %2, %3}], [%4];" ::"l"(map), "r"(col),
-                         "r"(f), "r"(t.slot), "r"(smem_addr(box))
+                         "r"(f), "r"(slot), "r"(smem_addr(box))
                          : "memory");
         else
             asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%1, %2, %3}], [%4];" ::"l"(map), "r"(col), "r"(f),
-                         "r"(t.slot), "r"(smem_addr(box))
+                         "r"(slot), "r"(smem_addr(box))
                          : "memory");
         bulk_commit();
     }
@@ -451,8 +484,8 @@ k_expert_product(const __grid_constant__ CUtensorMap map_a, const __grid_constan
     unsigned char *base = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
     unsigned char *epi = base + L::kEpiOff;
     uint64_t *bars = reinterpret_cast<uint64_t *>(base + L::kBarOff);
-    uint64_t *full = bars, *empty = bars + kMaxStages, *peer = bars + 2 * kMaxStages;
-    uint64_t *acc_full = bars + 3 * kMaxStages, *acc_empty = acc_full + 2, *drained = acc_full + 4;
+    uint64_t *full = bars, *empty = bars + kMaxStages, *tail = bars + 2 * kMaxStages, *peer = bars + 3 * kMaxStages;
+    uint64_t *acc_full = bars + 4 * kMaxStages, *acc_empty = acc_full + 2, *drained = acc_full + 4;
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(bars + L::kBars);
     volatile int *quit = reinterpret_cast<volatile int *>(tmem_slot + 1);
     int *warp_sums = reinterpret_cast<int *>(tmem_slot + 4);
@@ -464,7 +497,7 @@ k_expert_product(const __grid_constant__ CUtensorMap map_a, const __grid_constan
     if (tid == 0) {
         for (int s = 0; s < stages; ++s) {
             mbar_init(&full[s], 1); mbar_init(&empty[s], 1);
-            mbar_init(&peer[s], 1);
+            mbar_init(&tail[s], 1); mbar_init(&peer[s], 1);
         }
         for (int b = 0; b < 2; ++b) { mbar_init(&acc_full[b], 1); mbar_init(&acc_empty[b], CG * kEpiWarps); }
         mbar_init(drained, 1);
@@ -535,8 +568,7 @@ k_expert_product(const __grid_constant__ CUtensorMap map_a, const __grid_constan
     // take is uniform over the warp, and issue from one elected lane.
     if (warp == kTmaWarp) {
         int issued = 0, s = 0;
-        // products: the first CTA's barrier counts the bytes of both; weight gradient: each CTA's its own
-        const uint32_t lead = kGrad ? smem_addr(full) : lead_addr<CG>(full);
+        const uint32_t lead = lead_addr<CG>(full);             // the first CTA's barrier counts the bytes of both
         unsigned parity = 1;                                   // a fresh barrier passes the wait for parity 1
         bool ok = true;
         Tile t;
@@ -545,7 +577,7 @@ k_expert_product(const __grid_constant__ CUtensorMap map_a, const __grid_constan
             // each TMA instruction costs its warp some 80 cycles: many rows come in one box, few in boxes of 32
             const bool big = half > 2 * kBox;
             const int loads = big ? 1 : (half + kBox - 1) / kBox;
-            const uint32_t bytes = kGrad ? L::kStage : CG * (kATile + (big ? L::kN : loads * kBox) * kLine);
+            const uint32_t bytes = CG * (kATile + (kGrad || big ? L::kN : loads * kBox) * kLine);
             const int steps = ((kGrad ? t.rows : p.K) + kStageK - 1) / kStageK;
             const int feat = t.feat + rank * kFeat;
             for (int k = 0; k < steps; ++k) {
@@ -553,15 +585,20 @@ k_expert_product(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                 if (!ok) break;
                 unsigned char *a = stage + s * L::kStage, *b = a + kATile;
                 if (elect_one()) {
-                    const uint32_t bar = lead + s * 8;
-                    if (kGrad || rank == 0) mbar_expect_tx(&full[s], bytes);
+                    uint32_t bar = lead + s * 8;
                     if (kGrad) {
                         const int r = t.row + k * kStageK, col = t.col + rank * half;
-#pragma unroll
-                        for (int q = 0; q < kFeat / 64; ++q) tma_2d<1>(a + q * kChunk, &map_a, feat + q * 64, r, bar);
-#pragma unroll
-                        for (int q = 0; q < L::kN / 64; ++q) tma_2d<1>(b + q * kChunk, &map_b, col + q * 64, r, bar);
+                        // a stage whose last lines have to be made zero: the second CTA counts its own bytes
+                        const bool own = CG == 2 && has_tail(t.rows - k * kStageK);
+                        if (rank == 0) mbar_expect_tx(&full[s], own ? bytes / CG : bytes);
+                        else if (own) {
+                            mbar_expect_tx(&tail[s], bytes / CG);
+                            bar = smem_addr(&tail[s]);
+                        }
+                        if (own) load_grad<1, L::kN>(a, b, &map_a, &map_b, feat, col, r, bar);
+                        else load_grad<CG, L::kN>(a, b, &map_a, &map_b, feat, col, r, bar);
                     } else {
+                        if (rank == 0) mbar_expect_tx(&full[s], bytes);
                         if (L::kAAlongK) tma_3d<CG>(a, &map_a, k * kStageK, feat, t.slot, bar);
                         else {
 #pragma unroll
@@ -583,85 +620,85 @@ k_expert_product(const __grid_constant__ CUtensorMap map_a, const __grid_constan
             unsigned long long until = 0;
             for (int m = max(0, issued - stages); m < issued; ++m) drain_wait(&full[m % stages], (unsigned)(m / stages) & 1u, until);
         }
-    } else if (warp == kMmaWarp && (rank == 0 || kGrad)) {
+    } else if (warp == kMmaWarp && rank == 0) {
         int s = 0, buf = 0;
-        unsigned parity = 0, acc_parity = 1;
+        unsigned parity = 0, acc_parity = 1, peer_parity = 0;  // peer_parity: a bit per stage, of its next use
         bool ok = true;
         const uint64_t a_desc = desc_tile<L::kAAlongK>(smem_addr(stage)), b_desc = desc_tile<L::kBAlongK>(smem_addr(stage + kATile));
         Tile t;
         for (TileStream<OP, NT, CG> stream(p, ends, tiles); ok && stream.next(t);) {
-            if (rank == 0) {
+            const uint32_t idesc = idesc_bf16<CG, L::kAAlongK, L::kBAlongK>(tile_n<OP, NT, CG>(p, t));
+            const int steps = ((kGrad ? t.rows : p.K) + kStageK - 1) / kStageK;
+            int k = 0;
+            do {                                               // once for every accumulator that the tile takes
                 ok = __all_sync(0xffffffffu, wait_for(&acc_empty[buf], acc_parity, quit, p.spin_limit));
                 if (!ok) break;
                 tc_fence_after();
-            }
-            const uint32_t d = tmem + buf * NT;
-            const uint32_t idesc = idesc_bf16<CG, L::kAAlongK, L::kBAlongK>(tile_n<OP, NT, CG>(p, t));
-            const int steps = ((kGrad ? t.rows : p.K) + kStageK - 1) / kStageK;
-            bool ready = steps > 0 && __all_sync(0xffffffffu, mbar_test_wait(&full[s], parity));
-            for (int k = 0; k < steps; ++k) {
-                if (!ready) {
-                    ok = __all_sync(0xffffffffu, wait_for(&full[s], parity, quit, p.spin_limit));
-                    if (!ok) break;
-                }
-                // ask for the next stage's barrier now: the answer arrives while this stage is issued
-                const int s_next = s + 1 == stages ? 0 : s + 1;
-                const bool next_full = mbar_test_wait(&full[s_next], s_next ? parity : parity ^ 1u);
-                int parts = kStageK / 16;
-                if (kGrad) {
-                    // The last rows of a segment: whole 16s are multiplied, and of the last 16 the lines behind the
-                    // segment, which hold the next one's rows, are made zero in both operands (a NaN there times a
-                    // zero would still be one).  A line is 128 bytes of one k in each of the stage's chunks.
-                    const int left = t.rows - k * kStageK;
-                    if (left < kStageK) {
-                        parts = (left + 15) / 16;
-                        if (left & 15) {
-                            unsigned char *lines = stage + s * L::kStage + (lane & 7) * 16;
-                            for (int i = left; i < parts * 16; ++i)
-                                for (int q = lane >> 3; q < L::kStage / kChunk; q += 4)
-                                    *reinterpret_cast<uint4 *>(lines + q * kChunk + i * kLine) = make_uint4(0u, 0u, 0u, 0u);
-                            fence_async_shared();
-                            __syncwarp();
-                        }
+                const uint32_t d = tmem + buf * NT;
+                const int first = k, last = kAccSteps<F32> < steps - k ? k + kAccSteps<F32> : steps;
+                bool ready = steps > 0 && __all_sync(0xffffffffu, mbar_test_wait(&full[s], parity));
+                for (; k < last; ++k) {
+                    if (!ready) {
+                        ok = __all_sync(0xffffffffu, wait_for(&full[s], parity, quit, p.spin_limit));
+                        if (!ok) break;
                     }
-                    if (CG == 2) {
-                        // the second CTA's operands are there (and its last lines zero): it says so, the first one waits for it
-                        if (rank == 1) {
-                            if (lane == 0) mbar_arrive_lead_release(&peer[s]);
-                        } else {
-                            ok = __all_sync(0xffffffffu, wait_for<true>(&peer[s], parity, quit, p.spin_limit));
+                    // ask for the next stage's barrier now: the answer arrives while this stage is issued
+                    const int s_next = s + 1 == stages ? 0 : s + 1;
+                    const bool next_full = mbar_test_wait(&full[s_next], s_next ? parity : parity ^ 1u);
+                    const int left = t.rows - k * kStageK;     // of a weight gradient
+                    if (kGrad && has_tail(left)) {
+                        clear_tail(stage + s * L::kStage, L::kStage, left, lane);
+                        if (CG == 2) {                         // so has the second CTA
+                            ok = __all_sync(0xffffffffu, wait_for<true>(&peer[s], (peer_parity >> s) & 1u, quit, p.spin_limit));
                             if (!ok) break;
+                            peer_parity ^= 1u << s;
                         }
                     }
-                }
-                if (rank == 0) {
                     tc_fence_after();
                     // descriptors count in 16-byte units
                     const uint64_t a = a_desc + (uint32_t)(s * (L::kStage >> 4)), b = b_desc + (uint32_t)(s * (L::kStage >> 4));
                     if (elect_one()) {
 #pragma unroll
                         for (int q = 0; q < kStageK / 16; ++q)
-                            if (!kGrad || q < parts)
-                                mma_bf16<CG>(d, a + q * kDescStep<L::kAAlongK>, b + q * kDescStep<L::kBAlongK>, idesc, k > 0 || q > 0);
+                            if (!kGrad || q * 16 < left)
+                                mma_bf16<CG>(d, a + q * kDescStep<L::kAAlongK>, b + q * kDescStep<L::kBAlongK>, idesc, k > first || q > 0);
                         mma_commit<CG>(&empty[s]);
+                        if (k == last - 1) mma_commit<CG>(&acc_full[buf]);
                     }
+                    ready = __all_sync(0xffffffffu, next_full);
+                    s = s_next;
+                    if (s == 0) parity ^= 1u;
                 }
-                ready = __all_sync(0xffffffffu, next_full);
-                s = s_next;
-                if (s == 0) parity ^= 1u;
-            }
-            if (!ok) break;
-            if (rank == 0 && elect_one()) mma_commit<CG>(&acc_full[buf]);
-            __syncwarp();
-            buf ^= 1;
-            if (buf == 0) acc_parity ^= 1u;
+                if (!ok) break;
+                if (kGrad && steps == 0 && elect_one()) mma_commit<CG>(&acc_full[buf]);   // nothing to wait for
+                buf ^= 1;
+                if (buf == 0) acc_parity ^= 1u;
+            } while (k < steps);
         }
-        if (rank == 0) {
-            // everything issued has left the tensor core before TMEM is given back
-            if (elect_one()) mma_commit<CG>(drained);
-            __syncwarp();
-            unsigned long long until = 0;
-            drain_wait(drained, 0, until);
+        // everything issued has left the tensor core before TMEM is given back
+        if (elect_one()) mma_commit<CG>(drained);
+        __syncwarp();
+        unsigned long long until = 0;
+        drain_wait(drained, 0, until);
+    } else if (warp == kMmaWarp && kGrad) {
+        // The second CTA of a pair: its share of the stages that end a segment within a K = 16 (see clear_tail).  The first
+        // CTA's thread issues the MMA that reads these lines, so the arrival is a release of cluster scope: it takes some 1500
+        // cycles, but runs stages ahead.  (On every stage it bound the whole kernel: 510 TFLOP/s.)
+        int s = 0;
+        unsigned tail_parity = 0;                              // a bit per stage, of its next use
+        bool ok = true;
+        Tile t;
+        for (TileStream<OP, NT, CG> stream(p, ends, tiles); ok && stream.next(t);) {
+            const int steps = (t.rows + kStageK - 1) / kStageK, left = t.rows - (steps - 1) * kStageK;
+            if (steps > 0 && has_tail(left)) {
+                const int at = (s + steps - 1) % stages;
+                ok = __all_sync(0xffffffffu, wait_for(&tail[at], (tail_parity >> at) & 1u, quit, p.spin_limit));
+                if (!ok) break;
+                tail_parity ^= 1u << at;
+                clear_tail(stage + at * L::kStage, L::kStage, left, lane);
+                if (lane == 0) mbar_arrive_lead_release(&peer[at]);
+            }
+            s = (s + steps) % stages;
         }
     } else if (warp < kEpiWarps) {
         // epilogue: TMEM lane = feature of the tile, column = row (weight gradient: column)
@@ -670,12 +707,16 @@ k_expert_product(const __grid_constant__ CUtensorMap map_a, const __grid_constan
         int buf = 0;
         unsigned acc_parity = 0;
         Tile t;
-        for (TileStream<OP, NT, CG> stream(p, ends, tiles); stream.next(t);) {
-            if (!__all_sync(0xffffffffu, wait_for(&acc_full[buf], acc_parity, quit, p.spin_limit))) break;
+        bool ok = true;
+        int k = 0;                                             // of a weight gradient: stages of the tile that are done
+        for (TileStream<OP, NT, CG> stream(p, ends, tiles); ok && (k > 0 || stream.next(t));) {
+            ok = __all_sync(0xffffffffu, wait_for(&acc_full[buf], acc_parity, quit, p.spin_limit));
+            if (!ok) break;
             tc_fence_after();
             const uint32_t acc = tmem + buf * NT + ((uint32_t)(quarter * 32) << 16);
             const int f = t.feat + rank * kFeat + quarter * 32;
             if (kGrad) {
+                const bool more = k > 0;                       // sums of the same elements have been stored
                 constexpr int kCols = F32 ? 32 : 64;           // of a box
                 const int cols = min(NT, p.N - t.col);
                 const bool any = f < p.M && (t.rows > 0 || !p.add);
@@ -698,8 +739,9 @@ k_expert_product(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                             }
                         }
                     }
-                    store_grad<F32>(p, &map_y, t, f, t.col + c0, box, mine, lane);
+                    store_grad<F32>(&map_y, t.slot, f, t.col + c0, box, mine, lane, p.add, more);
                 }
+                k = F32 && t.rows - k * kStageK > kAccSteps<F32> * kStageK ? k + kAccSteps<F32> : 0;
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive_lead<CG>(&acc_empty[buf]);
