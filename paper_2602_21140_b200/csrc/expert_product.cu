@@ -70,20 +70,6 @@ __device__ __forceinline__ void tmem_ld_lanes(uint32_t addr, uint32_t (&r)[32])
         : "r"(addr));
 }
 
-// As mbar_try_wait, for a barrier that a thread of the other CTA arrives on.
-__device__ __forceinline__ bool mbar_try_wait_cluster(uint64_t *bar, unsigned parity)
-{
-    unsigned ok;
-    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-                 : "=r"(ok) : "r"(smem_addr(bar)), "r"(parity) : "memory");
-    return ok != 0;
-}
-
-__device__ __forceinline__ void mbar_arrive_lead_release(uint64_t *bar)
-{
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(lead_addr<2>(bar)) : "memory");
-}
-
 // Shared-memory matrix descriptors: start and strides in 16-byte units, version 1 (sm_100), 128-byte swizzle.
 // Along K: eight rows of 128 bytes are an atom, atoms 1024 bytes apart.  Along M or N: eight lines (K) of 64 elements
 // are an atom, the next eight of K 1024 bytes on, the next 64 elements a chunk on.
@@ -113,7 +99,7 @@ struct KernelParams {
     long long rows;
     int P, N, K, M;
     int stages;
-    __nv_bfloat16 *y;              // kGated, kGatedBackward: h
+    void *y;                       // kGated, kGatedBackward: h
     void *z;
     uint8_t *z_scales;
     __nv_bfloat16 *dz;
@@ -240,7 +226,7 @@ struct Layout {
     static constexpr int kN = NT / CG;                        // rows (or columns) of a tile in this CTA
     static constexpr int kBTile = kN * kLine;
     static constexpr int kStage = kATile + kBTile;            // multiples of 1024: swizzle alignment
-    static constexpr int kEpiWarp = 32 * 32 * 4;              // a plane of fp32 sums, or a box of a weight gradient
+    static constexpr int kEpiWarp = 32 * kLine;               // a plane of 32 x 32 fp32 or 32 x 64 bf16
     static constexpr int kBars = 4 * kMaxStages + 5;
     static constexpr int kEpiOff = 0, kBarOff = kEpiWarps * kEpiWarp;
     static constexpr int kEndsOff = kBarOff + ((kBars * 8 + 16 + 4 * (kThreads / 32) + 15) & ~15);
@@ -276,11 +262,10 @@ __device__ __forceinline__ void clear_tail(unsigned char *stage, int bytes, int 
 }
 
 // Bounded wait.  `quit` is shared by the CTA: the first role that gives up sets it, the others follow.
-template <bool CLUSTER = false>
 __device__ __forceinline__ bool wait_for(uint64_t *bar, unsigned parity, volatile int *quit, unsigned limit)
 {
     unsigned spins = 0;
-    while (!(CLUSTER ? mbar_try_wait_cluster(bar, parity) : mbar_try_wait(bar, parity))) {
+    while (!mbar_try_wait(bar, parity)) {
         if (++spins > limit || ((spins & 63u) == 0 && *quit)) { *quit = 1; return false; }
     }
     return true;
@@ -336,7 +321,7 @@ __device__ __forceinline__ void store_rows(const KernelParams &p, const float *p
         float x[8];
         read_eight(plane, i, lane, x);
         if (r < left)
-            *reinterpret_cast<uint4 *>(p.y + (row + r) * p.N + f) =
+            *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(p.y) + (row + r) * p.N + f) =
                 make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
     }
 }
@@ -358,7 +343,7 @@ __device__ __forceinline__ void store_gated(const KernelParams &p, const float *
         float h[4];
 #pragma unroll
         for (int q = 0; q < 4; ++q) h[q] = x[2 * q] * sigmoid(x[2 * q]) * x[2 * q + 1];
-        *reinterpret_cast<uint2 *>(p.y + (row + r) * (p.N / 2) + at / 2) = make_uint2(pack_bf16(h[0], h[1]), pack_bf16(h[2], h[3]));
+        *reinterpret_cast<uint2 *>(static_cast<__nv_bfloat16 *>(p.y) + (row + r) * (p.N / 2) + at / 2) = make_uint2(pack_bf16(h[0], h[1]), pack_bf16(h[2], h[3]));
         if (p.z_scales) {
             const uint32_t s = mx8_scale_byte(amax);
             *reinterpret_cast<uint2 *>(static_cast<uint8_t *>(p.z) + (row + r) * p.N + at) = mx8_quantize8(x, s);
@@ -430,7 +415,7 @@ __device__ __forceinline__ void store_gated_backward(const KernelParams &p, cons
         uint4 *dst = reinterpret_cast<uint4 *>(p.dz + (row + r) * (2 * p.N) + 2 * f);
         dst[0] = make_uint4(d[0], d[1], d[2], d[3]);
         dst[1] = make_uint4(d[4], d[5], d[6], d[7]);
-        *reinterpret_cast<uint4 *>(p.y + (row + r) * p.N + f) =
+        *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(p.y) + (row + r) * p.N + f) =
             make_uint4(pack_bf16(h[0], h[1]), pack_bf16(h[2], h[3]), pack_bf16(h[4], h[5]), pack_bf16(h[6], h[7]));
     }
 }
@@ -440,33 +425,39 @@ __device__ __forceinline__ void store_gated_backward(const KernelParams &p, cons
 // (1.0e-6 off after 1024 rows, 1.6e-5 after 16384): sums of 2048 rows stay at 2e-6.  A sum that is rounded to bf16 needs no such care.
 template <bool F32> constexpr int kAccSteps = F32 ? 2048 / kStageK : 1 << 30;
 
-// 32 features x 32 (fp32) or 64 (bf16) columns of a weight gradient leave as one TMA store from a box of 32 lines of
-// 128 bytes, 128-byte swizzle; what lies outside the matrix is cut by the store.  An addition is done by the memory
-// system, one for each element, so its order is no question.
+// 32 features (lanes) x 32 (fp32) or 64 (bf16) columns of a weight gradient, through 4 KB of shared memory: a lane writes
+// its feature's 128 bytes, 16-byte units permuted by the feature, and then eight lanes store the 128 bytes of one feature, so
+// that whole lines leave and nothing waits.  (By TMA stores the box has to be read before it is filled again, and they queue
+// with the loads, which already keep the TMA unit busy: a stage is 256 lines in 512 clocks.)  `add`: to what is there, which
+// this thread or an earlier kernel stored.
 template <bool F32>
-__device__ __forceinline__ void store_grad(const CUtensorMap *map, int slot, int f, int col, const uint4 (&v)[8], unsigned char *box, int lane,
-                                           bool add, bool more)
+__device__ __forceinline__ void store_grad(const KernelParams &p, const Tile &t, int f, int col, const uint4 (&v)[8], unsigned char *plane,
+                                           int lane, bool add)
 {
-    if (lane == 0) {
-        if (F32 && more) bulk_wait_all();                      // the sums of the rows before are where these are added
-        else bulk_wait_read<0>();                              // the store before has left the box
-    }
-    __syncwarp();
 #pragma unroll
-    for (int q = 0; q < 8; ++q) *reinterpret_cast<uint4 *>(box + lane * kLine + ((q ^ (lane & 7)) << 4)) = v[q];
-    fence_async_shared();
+    for (int q = 0; q < 8; ++q) *reinterpret_cast<uint4 *>(plane + lane * kLine + ((q ^ (lane & 7)) << 4)) = v[q];
     __syncwarp();
-    if (lane == 0) {
-        if (F32 && (add || more))
-            asm volatile("cp.reduce.async.bulk.tensor.3d.global.shared::cta.add.tile.bulk_group [%0, {%1, %2, %3}], [%4];" ::"l"(map), "r"(col),
-                         "r"(f), "r"(slot), "r"(smem_addr(box))
-                         : "memory");
-        else
-            asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%1, %2, %3}], [%4];" ::"l"(map), "r"(col), "r"(f),
-                         "r"(slot), "r"(smem_addr(box))
-                         : "memory");
-        bulk_commit();
+    constexpr int kWord = F32 ? 4 : 8;                         // columns of 16 bytes
+    const int unit = lane & 7, c = col + unit * kWord;
+    char *dst = static_cast<char *>(p.y) + (((size_t)t.slot * p.M + f) * p.N + c) * (16 / kWord);
+    const size_t pitch = (size_t)p.N * (16 / kWord);
+    const int left = c < p.N ? p.M - f : 0;                    // N is a multiple of 8
+    float4 before[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int r = 4 * i + (lane >> 3);
+        if (F32 && add && r < left) before[i] = *reinterpret_cast<const float4 *>(dst + r * pitch);
     }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int r = 4 * i + (lane >> 3);
+        uint4 o = *reinterpret_cast<const uint4 *>(plane + r * kLine + ((unit ^ (r & 7)) << 4));
+        if (F32 && add)
+            o = make_uint4(__float_as_uint(__uint_as_float(o.x) + before[i].x), __float_as_uint(__uint_as_float(o.y) + before[i].y),
+                           __float_as_uint(__uint_as_float(o.z) + before[i].z), __float_as_uint(__uint_as_float(o.w) + before[i].w));
+        if (r < left) *reinterpret_cast<uint4 *>(dst + r * pitch) = o;
+    }
+    __syncwarp();                                              // the plane is free again
 }
 
 // ------------------------------------------------------------------------ kernel
@@ -474,7 +465,7 @@ __device__ __forceinline__ void store_grad(const CUtensorMap *map, int slot, int
 template <ExpertOp OP, int NT, int CG, bool F32>
 __global__ void __launch_bounds__(kThreads, 1)
 k_expert_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_big,
-                 const __grid_constant__ CUtensorMap map_y, const KernelParams p)
+                 const KernelParams p)
 {
     // map_a: the M operand (weights, or the left operand of a weight gradient); map_b, map_big: the N operand
     using L = Layout<OP, NT, CG>;
@@ -506,7 +497,6 @@ k_expert_product(const __grid_constant__ CUtensorMap map_a, const __grid_constan
         asm volatile("prefetch.tensormap [%0];" ::"l"(&map_a));
         asm volatile("prefetch.tensormap [%0];" ::"l"(&map_b));
         if (!kGrad) asm volatile("prefetch.tensormap [%0];" ::"l"(&map_big));
-        if (kGrad) asm volatile("prefetch.tensormap [%0];" ::"l"(&map_y));
     }
     // hints while the previous kernel drains: its weights have pushed these out of L2 (a hint returns nothing stale)
     if (tid * 32 < p.P) { prefetch_l2(p.slot_counts + tid * 32); prefetch_l2(p.slot_offsets + tid * 32); }
@@ -649,7 +639,7 @@ k_expert_product(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                     if (kGrad && has_tail(left)) {
                         clear_tail(stage + s * L::kStage, L::kStage, left, lane);
                         if (CG == 2) {                         // so has the second CTA
-                            ok = __all_sync(0xffffffffu, wait_for<true>(&peer[s], (peer_parity >> s) & 1u, quit, p.spin_limit));
+                            ok = __all_sync(0xffffffffu, wait_for(&peer[s], (peer_parity >> s) & 1u, quit, p.spin_limit));
                             if (!ok) break;
                             peer_parity ^= 1u << s;
                         }
@@ -681,9 +671,9 @@ k_expert_product(const __grid_constant__ CUtensorMap map_a, const __grid_constan
         unsigned long long until = 0;
         drain_wait(drained, 0, until);
     } else if (warp == kMmaWarp && kGrad) {
-        // The second CTA of a pair: its share of the stages that end a segment within a K = 16 (see clear_tail).  The first
-        // CTA's thread issues the MMA that reads these lines, so the arrival is a release of cluster scope: it takes some 1500
-        // cycles, but runs stages ahead.  (On every stage it bound the whole kernel: 510 TFLOP/s.)
+        // The second CTA of a pair: its share of the stages that end a segment within a K = 16 (see clear_tail), announced to the
+        // first one, whose thread issues the MMA that reads these lines, as in mbar_arrive_lead.  (With a release of cluster scope:
+        // 128 x 511 rows 1488 us instead of 1054; such an arrival on every stage: 510 TFLOP/s.)
         int s = 0;
         unsigned tail_parity = 0;                              // a bit per stage, of its next use
         bool ok = true;
@@ -696,7 +686,7 @@ k_expert_product(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                 if (!ok) break;
                 tail_parity ^= 1u << at;
                 clear_tail(stage + at * L::kStage, L::kStage, left, lane);
-                if (lane == 0) mbar_arrive_lead_release(&peer[at]);
+                if (lane == 0) mbar_arrive_lead<CG>(&peer[at]);
             }
             s = (s + steps) % stages;
         }
@@ -716,32 +706,30 @@ k_expert_product(const __grid_constant__ CUtensorMap map_a, const __grid_constan
             const uint32_t acc = tmem + buf * NT + ((uint32_t)(quarter * 32) << 16);
             const int f = t.feat + rank * kFeat + quarter * 32;
             if (kGrad) {
-                const bool more = k > 0;                       // sums of the same elements have been stored
+                const int cols = min(NT, p.N - t.col), steps = (t.rows + kStageK - 1) / kStageK;
+                const bool add = F32 && (p.add || k > 0);      // k > 0: sums of the same elements have been stored
+                const bool any = f < p.M && !(add && steps == 0);
                 constexpr int kCols = F32 ? 32 : 64;           // of a box
-                const int cols = min(NT, p.N - t.col);
-                const bool any = f < p.M && (t.rows > 0 || !p.add);
                 for (int c0 = group * kCols; c0 < cols && any; c0 += 2 * kCols) {
                     uint4 box[8] = {};
-                    if (t.rows > 0) {
+                    if (steps > 0) {
                         uint32_t v[kCols / 32][32];
 #pragma unroll
                         for (int q = 0; q < kCols / 32; ++q) tmem_ld_lanes(acc + c0 + 32 * q, v[q]);
                         tmem_wait_ld();
 #pragma unroll
                         for (int q = 0; q < 8; ++q) {
-                            if (F32) box[q] = make_uint4(v[0][4 * q], v[0][4 * q + 1], v[0][4 * q + 2], v[0][4 * q + 3]);
-                            else {
-                                const uint32_t *w = &v[kCols / 32 - 1 ? q >> 2 : 0][8 * (q & 3)];
-                                box[q] = make_uint4(pack_bf16(__uint_as_float(w[0]), __uint_as_float(w[1])),
-                                                    pack_bf16(__uint_as_float(w[2]), __uint_as_float(w[3])),
-                                                    pack_bf16(__uint_as_float(w[4]), __uint_as_float(w[5])),
-                                                    pack_bf16(__uint_as_float(w[6]), __uint_as_float(w[7])));
-                            }
+                            const uint32_t *w = F32 ? &v[0][4 * q] : &v[(kCols / 32 - 1) & (q >> 2)][8 * (q & 3)];
+                            box[q] = F32 ? make_uint4(w[0], w[1], w[2], w[3])
+                                         : make_uint4(pack_bf16(__uint_as_float(w[0]), __uint_as_float(w[1])),
+                                                      pack_bf16(__uint_as_float(w[2]), __uint_as_float(w[3])),
+                                                      pack_bf16(__uint_as_float(w[4]), __uint_as_float(w[5])),
+                                                      pack_bf16(__uint_as_float(w[6]), __uint_as_float(w[7])));
                         }
                     }
-                    store_grad<F32>(&map_y, t.slot, f, t.col + c0, box, mine, lane, p.add, more);
+                    store_grad<F32>(p, t, f, t.col + c0, box, mine, lane, add);
                 }
-                k = F32 && t.rows - k * kStageK > kAccSteps<F32> * kStageK ? k + kAccSteps<F32> : 0;
+                k = F32 && steps - k > kAccSteps<F32> ? k + kAccSteps<F32> : 0;
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive_lead<CG>(&acc_empty[buf]);
@@ -771,7 +759,6 @@ k_expert_product(const __grid_constant__ CUtensorMap map_a, const __grid_constan
             buf ^= 1;
             if (buf == 0) acc_parity ^= 1u;
         }
-        if (kGrad && lane == 0) bulk_wait_all();               // the last stores have left shared memory
     }
 
     __syncwarp();
@@ -806,17 +793,14 @@ cudaError_t launch(const ExpertArgs &a, cudaStream_t st)
     std::call_once(once[a.device], [&] { attr[a.device] = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kSmem); });
     if (attr[a.device] != cudaSuccess) return attr[a.device];
     if (!encode_fn()) return cudaErrorNotSupported;
-    const CUtensorMapDataType bf16 = CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, f32 = CU_TENSOR_MAP_DATA_TYPE_FLOAT32;
+    const CUtensorMapDataType bf16 = CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
     const CUtensorMapSwizzle sw = CU_TENSOR_MAP_SWIZZLE_128B;
-    CUtensorMap map_a, map_b, map_big = {}, map_y = {};
+    CUtensorMap map_a, map_b, map_big = {};
     bool ok;
     if (L::kGrad) {
         const cuuint64_t ad[2] = {(cuuint64_t)a.M, (cuuint64_t)a.rows}, as[1] = {2 * (cuuint64_t)a.M};
         const cuuint64_t bd[2] = {(cuuint64_t)a.N, (cuuint64_t)a.rows}, bs[1] = {2 * (cuuint64_t)a.N};
-        const cuuint64_t size = F32 ? 4 : 2;
-        const cuuint64_t yd[3] = {(cuuint64_t)a.N, (cuuint64_t)a.M, (cuuint64_t)a.P}, ys[2] = {size * a.N, size * a.N * (cuuint64_t)a.M};
-        ok = encode(&map_a, bf16, sw, a.a, 2, ad, as, 64, kStageK) && encode(&map_b, bf16, sw, a.b, 2, bd, bs, 64, kStageK) &&
-             encode(&map_y, F32 ? f32 : bf16, sw, a.y, 3, yd, ys, F32 ? 32 : 64, 32);
+        ok = encode(&map_a, bf16, sw, a.a, 2, ad, as, 64, kStageK) && encode(&map_b, bf16, sw, a.b, 2, bd, bs, 64, kStageK);
     } else {
         const cuuint64_t inner = L::kAAlongK ? a.K : a.N, outer = L::kAAlongK ? a.N : a.K;
         const cuuint64_t wd[3] = {inner, outer, (cuuint64_t)a.P}, ws[2] = {2 * inner, 2 * inner * outer};
@@ -828,7 +812,7 @@ cudaError_t launch(const ExpertArgs &a, cudaStream_t st)
     KernelParams p;
     p.slot_counts = a.slot_counts; p.slot_offsets = a.slot_offsets; p.rows = a.rows;
     p.P = a.P; p.N = a.N; p.K = a.K; p.M = a.M; p.stages = L::stages(a.P);
-    p.y = static_cast<__nv_bfloat16 *>(a.y); p.z = a.z; p.z_scales = a.z_scales; p.dz = static_cast<__nv_bfloat16 *>(a.dz);
+    p.y = a.y; p.z = a.z; p.z_scales = a.z_scales; p.dz = static_cast<__nv_bfloat16 *>(a.dz);
     p.add = a.add; p.ctl = a.ctl; p.spin_limit = a.spin_limit;
     // no more CTAs than there can be tiles (the counts are on the device)
     const long long feats = ((L::kGrad ? a.M : a.N) + CG * kFeat - 1) / (CG * kFeat);
@@ -842,7 +826,7 @@ cudaError_t launch(const ExpertArgs &a, cudaStream_t st)
     at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at; cfg.numAttrs = a.pdl ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, kernel, map_a, map_b, map_big, map_y, p);
+    return cudaLaunchKernelEx(&cfg, kernel, map_a, map_b, map_big, p);
 }
 
 // With few rows a slot the weights dominate, and a narrow tile of one CTA leaves shared memory for more stages of them.
