@@ -430,7 +430,7 @@ moe_status moe_dispatch_backward(moe_ctx *ctx, const float *logits, const void *
  *   h, y         device out [rows, cols] of `dtype`, contiguous.  h may be x or residual itself where that is contiguous
  *   rstd         device out [rows] f32, or NULL: needed by moe_rms_norm_backward
  *   codes, scales device out: y (before it is rounded to `dtype`) as 8-bit rows, with the padding of the scales as 0; or both NULL
- * cols % 8 == 0 (% 32 with codes), 8 <= cols <= 32768.  Sums are fp32, in an order that depends on the sizes alone; each output is
+ * cols % 8 == 0 (% 32 with codes), 8 <= cols <= 16384.  Sums are fp32, in an order that depends on the sizes alone; each output is
  * rounded once.  rows = 0 launches nothing.  CAPACITY beyond 2^31 - 1 rows.  INVALID_ARG if an output overlaps an input
  * (but as said for h) or another output.  Allocates nothing, does not wait.
  */

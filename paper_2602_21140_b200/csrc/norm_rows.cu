@@ -4,13 +4,16 @@
 //   and y in 8 bits (mx8_format.cuh) where it is kept for a backward pass
 //   backward, with n = h * rstd and g = dy * weight:  dx = rstd * (g - n * mean(g * n)) + dh,  d_weight = sum over rows of dy * n
 //
-// Both are one pass over the rows and bound by HBM.  A row is taken by TPR threads, which hold it in registers between the
-// reduction and the result: a warp up to 1024 columns, a CTA of 256 or 1024 threads above.  A thread owns units of eight
-// consecutive elements (one 16-byte access of a 16-bit type), so four neighbouring lanes own a block of the 8-bit form.  All
-// sums are fp32, in an order that depends on the sizes alone; every output is rounded once.
+// Both are one pass over the rows and bound by HBM.  A row is taken by a warp up to 1024 columns, by a CTA above, with as many
+// warps as make four units a thread (a fixed 256 threads lost half of the bandwidth at 1536 columns).  A thread owns units of eight consecutive elements (one 16-byte access of a 16-bit type), so four
+// neighbouring lanes own a block of the 8-bit form.  The forward pass holds a row in registers between the reduction and the
+// result and has a CTA per row.  The backward pass has as many CTAs as fit, because each also sums d_weight over its rows; its
+// next rows are on their way to shared memory meanwhile (k_rms_norm_backward_ring).  All sums are fp32, in an order that
+// depends on the sizes alone; every output is rounded once.
 #include "../../include/moe_route.h"
 
 #include <algorithm>
+#include <type_traits>
 
 #include "mx8_format.cuh"
 
@@ -19,8 +22,10 @@ namespace {
 using namespace moe;
 
 constexpr int kUnits = 4;                  // units of eight elements per thread
-constexpr int kMaxCols = 1024 * kUnits * 8;
-constexpr int kNormCtas = 296;             // CTAs of a backward pass, each with a row of partial sums of d_weight
+constexpr int kMaxThreads = 512;           // of a CTA that has a row
+constexpr int kMaxCols = kMaxThreads * kUnits * 8;
+constexpr int kSms = 148;
+constexpr int kRingBytes = 220 * 1024;     // shared memory of an SM for the rows of a backward pass
 
 template <int DT> constexpr int kVec = DT == MOE_DTYPE_F32 ? 2 : 1;   // 16-byte words of a unit
 
@@ -92,21 +97,22 @@ __device__ __forceinline__ void weight8(const void *weight, bool f32, int unit, 
     }
 }
 
-// Sum over the TPR threads of a row; `scratch` holds a float per warp, and every thread passes the same `turn`, 0 and 1 in turn.
-template <int TPR>
-__device__ __forceinline__ float row_sum(float v, float *scratch, int turn)
+__device__ __forceinline__ float warp_sum(float v)
 {
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) v += __shfl_xor_sync(0xffffffffu, v, off);
-    if (TPR == 32) return v;
-    constexpr int kWarps = TPR / 32;
-    scratch += turn * kWarps;
-    if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = v;
-    __syncthreads();
-    v = (threadIdx.x & 31) < kWarps ? scratch[threadIdx.x & 31] : 0.0f;
-#pragma unroll
-    for (int off = 16; off > 0; off >>= 1) v += __shfl_xor_sync(0xffffffffu, v, off);
     return v;
+}
+
+// Sum over the CTA; `scratch` holds two sets of a float per warp, which calls take in turn.
+__device__ __forceinline__ float cta_sum(float v, float *scratch, int turn)
+{
+    const int lane = threadIdx.x & 31;
+    v = warp_sum(v);
+    scratch += turn * (kMaxThreads / 32);
+    if (lane == 0) scratch[threadIdx.x >> 5] = v;
+    __syncthreads();
+    return warp_sum(lane < (int)blockDim.x / 32 ? scratch[lane] : 0.0f);
 }
 
 struct NormParams {
@@ -123,21 +129,20 @@ struct NormParams {
     int pitch;
 };
 
-template <int TPR> constexpr int kBlock = TPR < 256 ? 256 : TPR;
-
-template <int DT, int TPR>
-__global__ void __launch_bounds__(kBlock<TPR>) k_rms_norm(NormParams p)
+// UN units per thread; WARP: eight rows to a CTA, a warp each, and not one to the CTA.
+template <int DT, int UN, bool WARP>
+__global__ void __launch_bounds__(WARP ? 256 : kMaxThreads) k_rms_norm(NormParams p)
 {
     constexpr int V = kVec<DT>;
-    __shared__ float scratch[32];
-    const int tid = threadIdx.x % TPR;
-    const long long row = (long long)blockIdx.x * (kBlock<TPR> / TPR) + threadIdx.x / TPR;
-    if (TPR < kBlock<TPR> && row >= p.rows) return;            // whole warps
+    __shared__ float scratch[2 * kMaxThreads / 32];
+    const int tid = WARP ? threadIdx.x & 31 : threadIdx.x, threads = WARP ? 32 : blockDim.x;
+    const long long row = WARP ? (long long)blockIdx.x * 8 + (threadIdx.x >> 5) : blockIdx.x;
+    if (WARP && row >= p.rows) return;
     const uint4 *x = p.x + row * p.x_stride, *res = p.residual ? p.residual + row * p.r_stride : nullptr;
-    uint4 in[kUnits][V], add[kUnits][V];
+    uint4 in[UN][V], add[UN][V];
 #pragma unroll
-    for (int i = 0; i < kUnits; ++i) {
-        const int u = i * TPR + tid;
+    for (int i = 0; i < UN; ++i) {
+        const int u = i * threads + tid;
 #pragma unroll
         for (int q = 0; q < V; ++q) {
             in[i][q] = u < p.units ? load_v4(x + u * V + q) : make_uint4(0u, 0u, 0u, 0u);
@@ -146,7 +151,7 @@ __global__ void __launch_bounds__(kBlock<TPR>) k_rms_norm(NormParams p)
     }
     float sum = 0.0f;
 #pragma unroll
-    for (int i = 0; i < kUnits; ++i) {
+    for (int i = 0; i < UN; ++i) {
         float a[8];
         to_f32<DT>(in[i], a);
         if (res) {
@@ -159,16 +164,16 @@ __global__ void __launch_bounds__(kBlock<TPR>) k_rms_norm(NormParams p)
         }
 #pragma unroll
         for (int q = 0; q < 8; ++q) sum += a[q] * a[q];
-        const int u = i * TPR + tid;
+        const int u = i * threads + tid;
         if (p.h && u < p.units)
 #pragma unroll
             for (int q = 0; q < V; ++q) p.h[(row * p.units + u) * V + q] = in[i][q];
     }
-    const float rstd = rsqrtf(row_sum<TPR>(sum, scratch, 0) / (float)(p.units * 8) + p.eps);
+    const float rstd = rsqrtf((WARP ? warp_sum(sum) : cta_sum(sum, scratch, 0)) / (float)(p.units * 8) + p.eps);
     if (p.rstd && tid == 0) p.rstd[row] = rstd;
 #pragma unroll
-    for (int i = 0; i < kUnits; ++i) {
-        const int u = i * TPR + tid;
+    for (int i = 0; i < UN; ++i) {
+        const int u = i * threads + tid;
         const bool inside = u < p.units;                       // with an 8-bit form whole blocks: all four lanes of one or none
         float a[8], w[8];
         to_f32<DT>(in[i], a);
@@ -204,62 +209,71 @@ struct NormBackwardParams {
     float *partial;                // [CTAs, cols]
 };
 
-template <int DT, int TPR>
-__global__ void __launch_bounds__(kBlock<TPR>) k_rms_norm_backward(NormBackwardParams p)
+// One row's unit: n = h * rstd, and what the row's mean and d_weight take from it.
+__device__ __forceinline__ void norm_sums(const float (&dy)[8], float (&n)[8], const float (&w)[8], float rstd, float &sum, float (&acc)[8])
 {
-    constexpr int V = kVec<DT>, kRows = kBlock<TPR> / TPR;
-    __shared__ float scratch[64];
-    extern __shared__ float sums[];                            // [kRows, cols], where a CTA has several rows at a time
-    const int tid = threadIdx.x % TPR, sub = threadIdx.x / TPR;
-    float acc[kUnits][8] = {};
-    int turn = 0;
-    for (long long row = (long long)blockIdx.x * kRows + sub; row < p.rows; row += (long long)gridDim.x * kRows) {
-        uint4 a[kUnits][V], b[kUnits][V];
 #pragma unroll
-        for (int i = 0; i < kUnits; ++i) {
-            const int u = i * TPR + tid;
+    for (int q = 0; q < 8; ++q) {
+        n[q] *= rstd;
+        sum += dy[q] * w[q] * n[q];
+        acc[q] += dy[q] * n[q];
+    }
+}
+
+__device__ __forceinline__ void norm_gradient(const float (&dy)[8], const float (&n)[8], const float (&w)[8], float rstd, float mean, float (&d)[8])
+{
+#pragma unroll
+    for (int q = 0; q < 8; ++q) d[q] = rstd * (dy[q] * w[q] - n[q] * mean);
+}
+
+// Rows of up to 1024 columns: a warp each, eight to a CTA, whose sums of d_weight meet in shared memory.
+template <int DT, int UN>
+__global__ void __launch_bounds__(256) k_rms_norm_backward(NormBackwardParams p)
+{
+    constexpr int V = kVec<DT>, kRows = 8;
+    extern __shared__ float sums[];                            // [kRows, cols]
+    const int lane = threadIdx.x & 31, sub = threadIdx.x >> 5;
+    float acc[UN][8] = {}, w[UN][8] = {};
+#pragma unroll
+    for (int i = 0; i < UN; ++i)
+        if (i * 32 + lane < p.units) weight8<DT>(p.weight, p.weight_f32, i * 32 + lane, w[i]);
+    for (long long row = (long long)blockIdx.x * kRows + sub; row < p.rows; row += (long long)gridDim.x * kRows) {
+        uint4 a[UN][V], b[UN][V], c[UN][V];
+#pragma unroll
+        for (int i = 0; i < UN; ++i) {
+            const int u = i * 32 + lane;
 #pragma unroll
             for (int q = 0; q < V; ++q) {
-                a[i][q] = u < p.units ? load_v4(p.dy + (row * p.units + u) * V + q) : make_uint4(0u, 0u, 0u, 0u);
-                b[i][q] = u < p.units ? load_v4(p.h + (row * p.units + u) * V + q) : make_uint4(0u, 0u, 0u, 0u);
+                const long long at = (row * p.units + u) * V + q;
+                a[i][q] = b[i][q] = c[i][q] = make_uint4(0u, 0u, 0u, 0u);
+                if (u < p.units) {
+                    a[i][q] = load_v4(p.dy + at);
+                    b[i][q] = load_v4(p.h + at);
+                    if (p.dh) c[i][q] = load_v4(p.dh + at);
+                }
             }
         }
         const float rstd = __ldg(p.rstd + row);
         float sum = 0.0f;
 #pragma unroll
-        for (int i = 0; i < kUnits; ++i) {
-            const int u = i * TPR + tid;
-            if (u >= p.units) continue;
-            float dy[8], n[8], w[8];
+        for (int i = 0; i < UN; ++i) {
+            float dy[8], n[8];
             to_f32<DT>(a[i], dy); to_f32<DT>(b[i], n);
-            weight8<DT>(p.weight, p.weight_f32, u, w);
-#pragma unroll
-            for (int q = 0; q < 8; ++q) {
-                n[q] *= rstd;
-                sum += dy[q] * w[q] * n[q];
-                acc[i][q] += dy[q] * n[q];
-            }
+            norm_sums(dy, n, w[i], rstd, sum, acc[i]);
         }
-        const float mean = row_sum<TPR>(sum, scratch, turn) / (float)(p.units * 8);
-        turn ^= 1;
+        const float mean = warp_sum(sum) / (float)(p.units * 8);
 #pragma unroll
-        for (int i = 0; i < kUnits; ++i) {
-            const int u = i * TPR + tid;
+        for (int i = 0; i < UN; ++i) {
+            const int u = i * 32 + lane;
             if (u >= p.units) continue;
-            float dy[8], n[8], w[8], d[8];
-            to_f32<DT>(a[i], dy); to_f32<DT>(b[i], n);
-            weight8<DT>(p.weight, p.weight_f32, u, w);
+            float dy[8], n[8], past[8], d[8];
+            to_f32<DT>(a[i], dy); to_f32<DT>(b[i], n); to_f32<DT>(c[i], past);
 #pragma unroll
-            for (int q = 0; q < 8; ++q) d[q] = rstd * (dy[q] * w[q] - n[q] * rstd * mean);
-            if (p.dh) {
-                uint4 c[V];
-                float past[8];
-#pragma unroll
-                for (int q = 0; q < V; ++q) c[q] = load_v4(p.dh + (row * p.units + u) * V + q);
-                to_f32<DT>(c, past);
+            for (int q = 0; q < 8; ++q) n[q] *= rstd;
+            norm_gradient(dy, n, w[i], rstd, mean, d);
+            if (p.dh)
 #pragma unroll
                 for (int q = 0; q < 8; ++q) d[q] += past[q];
-            }
             uint4 o[V];
             from_f32<DT>(d, o);
 #pragma unroll
@@ -267,23 +281,113 @@ __global__ void __launch_bounds__(kBlock<TPR>) k_rms_norm_backward(NormBackwardP
         }
     }
     const int cols = p.units * 8;
-    float *mine = kRows > 1 ? sums + sub * cols : p.partial + (size_t)blockIdx.x * cols;
 #pragma unroll
-    for (int i = 0; i < kUnits; ++i) {
-        const int u = i * TPR + tid;
+    for (int i = 0; i < UN; ++i) {
+        const int u = i * 32 + lane;
         if (u >= p.units) continue;
-        float4 *dst = reinterpret_cast<float4 *>(mine + u * 8);
+        float4 *dst = reinterpret_cast<float4 *>(sums + sub * cols + u * 8);
         dst[0] = make_float4(acc[i][0], acc[i][1], acc[i][2], acc[i][3]);
         dst[1] = make_float4(acc[i][4], acc[i][5], acc[i][6], acc[i][7]);
     }
-    if (kRows > 1) {
-        __syncthreads();
-        for (int c = threadIdx.x; c < cols; c += kBlock<TPR>) {
-            float s = 0.0f;
+    __syncthreads();
+    for (int c = threadIdx.x; c < cols; c += 256) {
+        float s = 0.0f;
 #pragma unroll
-            for (int r = 0; r < kRows; ++r) s += sums[r * cols + c];
-            p.partial[(size_t)blockIdx.x * cols + c] = s;
+        for (int r = 0; r < kRows; ++r) s += sums[r * cols + c];
+        p.partial[(size_t)blockIdx.x * cols + c] = s;
+    }
+}
+
+// Longer rows: a CTA each.  Its rows of dy, h and dh come by asynchronous copies, STAGES - 1 rows ahead, into a ring in shared
+// memory; every thread reads back what it copied itself, so a wait for its own copies is all that a stage takes.  (With
+// loads to registers and two CTAs per SM: 254 us for 16384 x 7168 in bf16, whose bytes take 143.)
+template <int DT, int STAGES>
+__global__ void __launch_bounds__(kMaxThreads) k_rms_norm_backward_ring(NormBackwardParams p)
+{
+    constexpr int V = kVec<DT>;
+    __shared__ float scratch[2 * kMaxThreads / 32];
+    extern __shared__ uint4 ring[];                            // [STAGES][dy, h, dh][units * V]
+    const int tid = threadIdx.x, threads = blockDim.x, words = p.units * V, tensors = p.dh ? 3 : 2;
+    float acc[kUnits][8] = {}, w[kUnits][8] = {};
+#pragma unroll
+    for (int i = 0; i < kUnits; ++i)
+        if (i * threads + tid < p.units) weight8<DT>(p.weight, p.weight_f32, i * threads + tid, w[i]);
+    const auto ask = [&](long long row, uint4 *stage) {
+        if (row < p.rows)
+#pragma unroll
+            for (int i = 0; i < kUnits; ++i) {
+                const int u = i * threads + tid;
+                if (u >= p.units) continue;
+#pragma unroll
+                for (int q = 0; q < V; ++q) {
+                    const long long at = row * words + u * V + q;
+                    cp_async_16(stage + u * V + q, p.dy + at);
+                    cp_async_16(stage + words + u * V + q, p.h + at);
+                    if (tensors == 3) cp_async_16(stage + 2 * words + u * V + q, p.dh + at);
+                }
+            }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    const long long step = gridDim.x;
+    const int stage_words = tensors * words;
+    int fill = 0, take = 0, turn = 0;
+#pragma unroll
+    for (int s = 0; s < STAGES - 1; ++s) ask(blockIdx.x + s * step, ring + s * stage_words);
+    fill = (STAGES - 1) * stage_words;
+    for (long long row = blockIdx.x; row < p.rows; row += step) {
+        ask(row + (STAGES - 1) * step, ring + fill);
+        fill = fill == (STAGES - 1) * stage_words ? 0 : fill + stage_words;
+        const float rstd = __ldg(p.rstd + row);
+        asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 1) : "memory");
+        const uint4 *in = ring + take;
+        take = take == (STAGES - 1) * stage_words ? 0 : take + stage_words;
+        float sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kUnits; ++i) {
+            const int u = i * threads + tid;
+            if (u >= p.units) continue;
+            uint4 a[V], b[V];
+#pragma unroll
+            for (int q = 0; q < V; ++q) { a[q] = in[u * V + q]; b[q] = in[words + u * V + q]; }
+            float dy[8], n[8];
+            to_f32<DT>(a, dy); to_f32<DT>(b, n);
+            norm_sums(dy, n, w[i], rstd, sum, acc[i]);
         }
+        const float mean = cta_sum(sum, scratch, turn) / (float)(p.units * 8);
+        turn ^= 1;
+#pragma unroll
+        for (int i = 0; i < kUnits; ++i) {
+            const int u = i * threads + tid;
+            if (u >= p.units) continue;
+            uint4 a[V], b[V], c[V];
+#pragma unroll
+            for (int q = 0; q < V; ++q) { a[q] = in[u * V + q]; b[q] = in[words + u * V + q]; }
+            float dy[8], n[8], d[8];
+            to_f32<DT>(a, dy); to_f32<DT>(b, n);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) n[q] *= rstd;
+            norm_gradient(dy, n, w[i], rstd, mean, d);
+            if (tensors == 3) {
+                float past[8];
+#pragma unroll
+                for (int q = 0; q < V; ++q) c[q] = in[2 * words + u * V + q];
+                to_f32<DT>(c, past);
+#pragma unroll
+                for (int q = 0; q < 8; ++q) d[q] += past[q];
+            }
+            uint4 o[V];
+            from_f32<DT>(d, o);
+#pragma unroll
+            for (int q = 0; q < V; ++q) p.dx[row * words + u * V + q] = o[q];
+        }
+    }
+    float4 *dst = reinterpret_cast<float4 *>(p.partial + (size_t)blockIdx.x * p.units * 8);
+#pragma unroll
+    for (int i = 0; i < kUnits; ++i) {
+        const int u = i * threads + tid;
+        if (u >= p.units) continue;
+        dst[2 * u] = make_float4(acc[i][0], acc[i][1], acc[i][2], acc[i][3]);
+        dst[2 * u + 1] = make_float4(acc[i][4], acc[i][5], acc[i][6], acc[i][7]);
     }
 }
 
@@ -312,18 +416,31 @@ bool aligned(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0
 
 bool is_dtype(int32_t d) { return d == MOE_DTYPE_BF16 || d == MOE_DTYPE_F16 || d == MOE_DTYPE_F32; }
 
-// f(type, threads of a row) for the kernel that rows of `units` units of this type take
+// f(type, units per thread, whether a row is a warp's) for the kernel that rows of `units` units of this type take
 template <typename F>
 void with_kernel(int32_t dtype, int units, F f)
 {
+    using std::integral_constant;
     const auto by_width = [&](auto dt) {
-        if (units <= 32 * kUnits) f(dt, std::integral_constant<int, 32>());
-        else if (units <= 256 * kUnits) f(dt, std::integral_constant<int, 256>());
-        else f(dt, std::integral_constant<int, 1024>());
+        if (units <= 32) f(dt, integral_constant<int, 1>(), std::true_type());
+        else if (units <= 64) f(dt, integral_constant<int, 2>(), std::true_type());
+        else if (units <= 32 * kUnits) f(dt, integral_constant<int, kUnits>(), std::true_type());
+        else f(dt, integral_constant<int, kUnits>(), std::false_type());
     };
-    if (dtype == MOE_DTYPE_BF16) by_width(std::integral_constant<int, MOE_DTYPE_BF16>());
-    else if (dtype == MOE_DTYPE_F16) by_width(std::integral_constant<int, MOE_DTYPE_F16>());
-    else by_width(std::integral_constant<int, MOE_DTYPE_F32>());
+    if (dtype == MOE_DTYPE_BF16) by_width(integral_constant<int, MOE_DTYPE_BF16>());
+    else if (dtype == MOE_DTYPE_F16) by_width(integral_constant<int, MOE_DTYPE_F16>());
+    else by_width(integral_constant<int, MOE_DTYPE_F32>());
+}
+
+// Threads of the CTA that takes a row.
+int row_threads(int units) { return (units + 32 * kUnits - 1) / (32 * kUnits) * 32; }
+
+// CTAs of a backward pass at most, each with a row of partial sums of d_weight: 512 threads of CTAs with a row (their
+// registers fill an SM), two CTAs of eight warps with a row each.
+int64_t backward_ctas(int64_t rows, int units)
+{
+    if (units <= 32 * kUnits) return std::min<int64_t>((rows + 7) / 8, 2 * kSms);
+    return std::min<int64_t>(rows, std::min(8, kMaxThreads / row_threads(units)) * kSms);
 }
 
 moe_status check_norm(int32_t dtype, int32_t weight_dtype, int64_t rows, int32_t cols)
@@ -373,16 +490,16 @@ moe_status moe_rms_norm(const void *x, int64_t x_stride, const void *residual, i
     p.weight = weight; p.weight_f32 = weight_dtype == MOE_DTYPE_F32; p.eps = eps; p.rows = rows; p.units = cols / 8;
     p.h = static_cast<uint4 *>(h); p.y = static_cast<uint4 *>(y); p.rstd = rstd; p.codes = codes; p.scales = scales;
     p.pitch = mx_scale_pitch(cols);
-    with_kernel(dtype, p.units, [&](auto dt, auto tpr) {
-        constexpr int kRows = kBlock<tpr> / tpr;
-        k_rms_norm<dt, tpr><<<(unsigned)((rows + kRows - 1) / kRows), kBlock<tpr>, 0, static_cast<cudaStream_t>(cuda_stream)>>>(p);
+    with_kernel(dtype, p.units, [&](auto dt, auto un, auto warp) {
+        k_rms_norm<dt, un, warp><<<(unsigned)(warp ? (rows + 7) / 8 : rows), warp ? 256 : row_threads(p.units), 0,
+                                   static_cast<cudaStream_t>(cuda_stream)>>>(p);
     });
     return cudaGetLastError() == cudaSuccess ? MOE_OK : MOE_ERR_CUDA;
 }
 
 size_t moe_rms_norm_backward_workspace(int64_t rows, int32_t cols)
 {
-    return rows < 1 || cols < 8 || cols % 8 != 0 || cols > kMaxCols ? 0 : (size_t)std::min<int64_t>(rows, kNormCtas) * cols * 4;
+    return rows < 1 || cols < 8 || cols % 8 != 0 || cols > kMaxCols ? 0 : (size_t)backward_ctas(rows, cols / 8) * cols * 4;
 }
 
 moe_status moe_rms_norm_backward(const void *dy, const void *dh, const void *h, const float *rstd, int32_t dtype, int64_t rows,
@@ -413,13 +530,32 @@ moe_status moe_rms_norm_backward(const void *dy, const void *dh, const void *h, 
     p.dy = static_cast<const uint4 *>(dy); p.dh = static_cast<const uint4 *>(dh); p.h = static_cast<const uint4 *>(h);
     p.rstd = rstd; p.weight = weight; p.weight_f32 = weight_dtype == MOE_DTYPE_F32; p.rows = rows; p.units = cols / 8;
     p.dx = static_cast<uint4 *>(dx); p.partial = static_cast<float *>(workspace);
-    int ctas = 0;
-    with_kernel(dtype, p.units, [&](auto dt, auto tpr) {
-        constexpr int kRows = kBlock<tpr> / tpr;
-        ctas = (int)std::min<int64_t>((rows + kRows - 1) / kRows, kNormCtas);
-        k_rms_norm_backward<dt, tpr><<<ctas, kBlock<tpr>, kRows > 1 ? (size_t)kRows * cols * 4 : 0, st>>>(p);
+    int ctas = (int)backward_ctas(rows, p.units);
+    cudaError_t e = cudaSuccess;
+    with_kernel(dtype, p.units, [&](auto dt, auto un, auto warp) {
+        if constexpr (warp) {
+            k_rms_norm_backward<dt, un><<<ctas, 256, (size_t)8 * cols * 4, st>>>(p);
+            e = cudaGetLastError();
+        } else {
+            // As many CTAs as the registers hold, with two or three rows each in the ring; fewer where not even two fit.  (One CTA
+            // of 224 threads with three rows: 255 us for 16384 x 7168 in bf16.)
+            const size_t stage = (size_t)cols * (dtype == MOE_DTYPE_F32 ? 4 : 2) * (dh ? 3 : 2);
+            int per_sm = std::min(8, kMaxThreads / row_threads(p.units));
+            while (per_sm > 1 && kRingBytes / per_sm < 2 * stage) --per_sm;
+            const int stages = (int)std::min<size_t>(3, kRingBytes / per_sm / stage);
+            ctas = (int)std::min<int64_t>(ctas, per_sm * kSms);
+            const auto launch = [&](auto kernel) {
+                e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kRingBytes);
+                if (e != cudaSuccess) return;
+                kernel<<<ctas, row_threads(p.units), stages * stage, st>>>(p);
+                e = cudaGetLastError();
+            };
+            if (stages == 3) launch(k_rms_norm_backward_ring<dt, 3>);
+            else if (stages == 2) launch(k_rms_norm_backward_ring<dt, 2>);
+            else launch(k_rms_norm_backward_ring<dt, 1>);
+        }
     });
-    if (cudaGetLastError() != cudaSuccess) return MOE_ERR_CUDA;
+    if (e != cudaSuccess) return MOE_ERR_CUDA;
     k_norm_weight<<<(cols / 4 + 31) / 32, 1024, 0, st>>>(static_cast<const float4 *>(workspace), ctas, cols / 4, reinterpret_cast<float4 *>(d_weight));
     return cudaGetLastError() == cudaSuccess ? MOE_OK : MOE_ERR_CUDA;
 }
