@@ -1102,6 +1102,48 @@ class MoeRouter:
         d_gate_up = self.expert_weight_backward(dz, rows, slot_counts, slot_offsets, d_gate_up, add, grad_dtype)
         return self.expert_rows_backward(dz, slot_counts, slot_offsets, gate_up, d_rows), d_gate_up, d_down
 
+    def _networks_ok(self, gate_up: torch.Tensor, down: torch.Tensor) -> bool:
+        H, P, dev = self.cfg.hidden, self.num_slots, self._index()
+        return (gate_up.dim() == 3 and gate_up.shape[1] > 0 and gate_up.shape[1] % 32 == 0
+                and _is_dense(gate_up, torch.bfloat16, (P, gate_up.shape[1], H), dev)
+                and _is_dense(down, torch.bfloat16, (P, H, gate_up.shape[1] // 2), dev))
+
+    def expert_step(self, logits: torch.Tensor, x: torch.Tensor, gate_up: torch.Tensor, down: torch.Tensor,
+                    out: DispatchBuffers | None = None, y: torch.Tensor | None = None, buf: torch.Tensor | None = None,
+                    z: "torch.Tensor | Mx8Rows | None" = None) -> torch.Tensor:
+        """One whole layer with experts in 16 bits: dispatch, the experts, and the combine (times slot_scale, as always).
+        For expert_step_backward keep ``out``, the experts' outputs ``buf`` [T * k, H] and their projections ``z``."""
+        T, H, k, dev = x.shape[0], self.cfg.hidden, self.cfg.top_k, self._index()
+        # before the first launch: dispatch and combine take the sizes of their buffers on trust
+        _require(self._networks_ok(gate_up, down) and _is_dense(x, torch.bfloat16, (T, H), dev)
+                 and _is_dense(logits, torch.float32, (T, self.cfg.num_experts), dev)
+                 and (y is None or _is_dense(y, torch.bfloat16, (T, H), dev)) and (buf is None or _is_dense(buf, torch.bfloat16, (T * k, H), dev))
+                 and (z is None or self._kept_ok(z, T * k, gate_up.shape[1], dev))
+                 and (out is None or (self._outputs_ok(out, T, dev) and out.send_buf is not None
+                                      and _is_dense(out.send_buf, torch.bfloat16, (T * k, H), dev))), "expert_step")
+        out = _on_device(dev, self.dispatch, logits, x, out)
+        buf = self.expert_ffn(out.send_buf, out.slot_counts, out.slot_offsets, gate_up, down, buf, z=z)
+        return _on_device(dev, self.combine, buf, T, y)
+
+    def expert_step_backward(self, logits: torch.Tensor, dy: torch.Tensor, rows: "torch.Tensor | Mx8Rows", out: DispatchBuffers,
+                             buf: torch.Tensor, z: "torch.Tensor | Mx8Rows", gate_up: torch.Tensor, down: torch.Tensor,
+                             d_gate_up: torch.Tensor | None = None, d_down: torch.Tensor | None = None, add: bool = False,
+                             grad_dtype: torch.dtype = torch.bfloat16):
+        """Gradients of the latest expert_step: (dx, d_logits, d_gate_up, d_down).  ``rows``: its send buffer, or its tokens' rows
+        x in 8 bits (rms_norm's ``y8``).  d_logits is None for dense-FFN routing, whose weights are constants."""
+        T, H, dev = dy.shape[0], self.cfg.hidden, self._index()
+        _require(self._networks_ok(gate_up, down) and _is_dense(dy, torch.bfloat16, (T, H), dev) and self._outputs_ok(out, T, dev)
+                 and self._kept_ok(z, T * self.cfg.top_k, gate_up.shape[1], dev), "expert_step_backward")
+        d_buf, d_weights = self.combine_backward(buf, dy)
+        if isinstance(rows, Mx8Rows):
+            rows = self.redispatch(rows)
+        d_rows, d_gate_up, d_down = self.expert_ffn_backward(d_buf, rows, out.slot_counts, out.slot_offsets, gate_up, down, z, None,
+                                                             d_gate_up, d_down, add, grad_dtype)
+        if self.cfg.score_func == MOE_ROUTE_DENSE_TP:
+            d_weights = None
+        dx, d_logits = self.dispatch_backward(logits, d_rows, d_weights)
+        return dx, d_logits, d_gate_up, d_down
+
     # -- expert parallelism over several GPUs -------------------------------
     def ep_attach(self, world: int, rank: int, recv_buf_ptrs, recv_rows: int) -> None:
         st = moe_ep_attach(self._ctx, world, rank, recv_buf_ptrs, recv_rows, self._stream())

@@ -192,10 +192,11 @@ __global__ void __launch_bounds__(WARP ? 256 : kMaxThreads) k_rms_norm(NormParam
             amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
             const uint32_t s = mx8_scale_byte(amax);
             if (inside) *reinterpret_cast<uint2 *>(p.codes + (row * p.units + u) * 8) = mx8_quantize8(a, s);
-            // the padding of the scales is written as 0
-            if ((u & 3) == 0 && u / 4 < p.pitch) p.scales[row * p.pitch + u / 4] = inside ? (uint8_t)s : (uint8_t)0;
+            if ((u & 3) == 0 && inside) p.scales[row * p.pitch + u / 4] = (uint8_t)s;
         }
     }
+    if (p.codes)                                               // the padding of the scales is written as 0
+        for (int b = p.units / 4 + tid; b < p.pitch; b += threads) p.scales[row * p.pitch + b] = 0;
 }
 
 struct NormBackwardParams {
