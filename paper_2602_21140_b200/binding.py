@@ -1018,7 +1018,7 @@ class MoeRouter:
         """silu(gate) * up [n, n_hidden].  gate_up [P, 2 * n_hidden, cols]: row 2i is the gate of feature i, row 2i + 1 its
         up-projection.  ``z`` [n, 2 * n_hidden]: bf16 or 8-bit rows that keep the projections for the backward pass."""
         dev = self._index()
-        _require(gate_up.dim() == 3 and gate_up.shape[1] % 32 == 0
+        _require(gate_up.dim() == 3 and gate_up.shape[1] > 0 and gate_up.shape[1] % 32 == 0
                  and self._expert_ok(rows, gate_up.shape[2], slot_counts, slot_offsets, gate_up, dev), "expert_gated")
         n, (_, cols, n_in) = rows.shape[0], gate_up.shape
         if h is None:
@@ -1058,7 +1058,7 @@ class MoeRouter:
         """From the gradient of an expert's output [n, n_out] and the kept projections: (dz [n, 2 * n_hidden], h [n, n_hidden]),
         the projections' gradient and the hidden rows of the forward pass."""
         dev = self._index()
-        _require(down.dim() == 3 and down.shape[2] % 16 == 0 and self._expert_ok(dy, down.shape[1], slot_counts, slot_offsets, down, dev),
+        _require(down.dim() == 3 and down.shape[2] > 0 and down.shape[2] % 16 == 0 and self._expert_ok(dy, down.shape[1], slot_counts, slot_offsets, down, dev),
                  "expert_gated_backward")
         n, (_, n_out, n_hidden) = dy.shape[0], down.shape
         dz = dy.new_empty((n, 2 * n_hidden)) if dz is None else dz
