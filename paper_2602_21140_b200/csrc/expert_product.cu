@@ -36,7 +36,7 @@ constexpr int kStageK = 64;                // elements of K per stage
 constexpr int kLine = 128;                 // bytes of a line of an operand tile: 64 elements
 constexpr int kChunk = 64 * kLine;         // 64 features x 64 K of an operand that runs along its features
 constexpr int kATile = kFeat * kLine;      // 16 KB
-constexpr int kEpiWarps = 8, kTmaWarp = kEpiWarps, kMmaWarp = kEpiWarps + 1, kThreads = 32 * (kEpiWarps + 2);
+constexpr int kEpiWarps = 8, kTmaWarp = kEpiWarps, kMmaWarp = kEpiWarps + 1;
 constexpr int kMaxStages = 10;
 constexpr int kBand = 8;                   // tiles of rows (or of n) that are worked on side by side, see tile_at
 
@@ -67,6 +67,16 @@ __device__ __forceinline__ void tmem_ld_lanes(uint32_t addr, uint32_t (&r)[32])
           "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]),
           "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]),
           "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(addr));
+}
+
+// 32 lanes x 16 columns
+__device__ __forceinline__ void tmem_ld_lanes(uint32_t addr, uint32_t (&r)[16])
+{
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
         : "r"(addr));
 }
 
@@ -218,8 +228,14 @@ struct TileStream {
     }
 };
 
-template <ExpertOp OP, int NT, int CG>
+// Threads of a CTA.  Where the epilogue keeps sums in registers (FINE, a wide tile: 128 of a thread), the two issuing warps are
+// filled up to a warpgroup, which hands registers to the two of the epilogue: 72 + 2 * 216 = 3 * 168, what the launch gives.
+template <int NT, bool FINE> constexpr bool kSplitRegs = FINE && NT > 64;
+template <int NT, bool FINE> constexpr int kThreadsOf = kSplitRegs<NT, FINE> ? 384 : 32 * (kEpiWarps + 2);
+
+template <ExpertOp OP, int NT, int CG, bool FINE>
 struct Layout {
+    static constexpr int kThreads = kThreadsOf<NT, FINE>;
     static constexpr bool kGrad = OP == ExpertOp::kWeightGrad;
     static constexpr bool kAAlongK = OP == ExpertOp::kProduct || OP == ExpertOp::kGated;   // see desc_tile
     static constexpr bool kBAlongK = !kGrad;
@@ -327,30 +343,37 @@ __device__ __forceinline__ void store_rows(const KernelParams &p, const float *p
 }
 
 // SwiGLU of 16 pairs x 32 rows, and the sums themselves where they are kept, in bf16 or in 8 bits (the warp's 32 sums of a
-// row are one block).
+// row are one block).  Rows behind the segment are computed as the others and not stored: branches would keep the four
+// rows of a lane from running side by side.
 __device__ __forceinline__ void store_gated(const KernelParams &p, const float *plane, int f, long long row, int left, int lane)
 {
     const bool inside = f < p.N;                               // N is a multiple of 32: all of the block or nothing
+    const int at = f + (lane & 3) * 8;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const int r = 8 * i + (lane >> 2), at = f + (lane & 3) * 8;
-        float x[8];
+        const int r = 8 * i + (lane >> 2);
+        const bool store = r < left && inside;
+        float x[8], h[4];
         read_eight(plane, i, lane, x);
-        uint32_t amax = mx8_amax(x);                           // before anything is masked: all lanes take part
-        amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
-        amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
-        if (r >= left || !inside) continue;
-        float h[4];
 #pragma unroll
         for (int q = 0; q < 4; ++q) h[q] = x[2 * q] * sigmoid(x[2 * q]) * x[2 * q + 1];
-        *reinterpret_cast<uint2 *>(static_cast<__nv_bfloat16 *>(p.y) + (row + r) * (p.N / 2) + at / 2) = make_uint2(pack_bf16(h[0], h[1]), pack_bf16(h[2], h[3]));
+        if (store)
+            *reinterpret_cast<uint2 *>(static_cast<__nv_bfloat16 *>(p.y) + (row + r) * (p.N / 2) + at / 2) =
+                make_uint2(pack_bf16(h[0], h[1]), pack_bf16(h[2], h[3]));
         if (p.z_scales) {
+            uint32_t amax = mx8_amax(x);
+            amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
+            amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
             const uint32_t s = mx8_scale_byte(amax);
-            *reinterpret_cast<uint2 *>(static_cast<uint8_t *>(p.z) + (row + r) * p.N + at) = mx8_quantize8(x, s);
-            if ((lane & 3) == 0) p.z_scales[(row + r) * mx_scale_pitch(p.N) + f / kMxBlock] = (uint8_t)s;
+            const uint2 codes = mx8_quantize8(x, s);
+            if (store) {
+                *reinterpret_cast<uint2 *>(static_cast<uint8_t *>(p.z) + (row + r) * p.N + at) = codes;
+                if ((lane & 3) == 0) p.z_scales[(row + r) * mx_scale_pitch(p.N) + f / kMxBlock] = (uint8_t)s;
+            }
         } else if (p.z) {
-            *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(p.z) + (row + r) * p.N + at) =
-                make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
+            if (store)
+                *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(p.z) + (row + r) * p.N + at) =
+                    make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
         }
     }
 }
@@ -390,7 +413,6 @@ __device__ __forceinline__ void store_gated_backward(const KernelParams &p, cons
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int r = 8 * i + (lane >> 2);
-        if (r >= left) continue;
         float dh[8], z[16], h[8];
         read_eight(plane, i, lane, dh);
         if (p.z_scales) {
@@ -412,6 +434,7 @@ __device__ __forceinline__ void store_gated_backward(const KernelParams &p, cons
             h[q] = a * u;
             d[q] = pack_bf16(dh[q] * u * s * (1.0f + g * (1.0f - s)), dh[q] * a);
         }
+        if (r >= left) continue;
         uint4 *dst = reinterpret_cast<uint4 *>(p.dz + (row + r) * (2 * p.N) + 2 * f);
         dst[0] = make_uint4(d[0], d[1], d[2], d[3]);
         dst[1] = make_uint4(d[4], d[5], d[6], d[7]);
@@ -420,19 +443,21 @@ __device__ __forceinline__ void store_gated_backward(const KernelParams &p, cons
     }
 }
 
-// Stages after which a tile of a weight gradient in fp32 goes on in another accumulator, whose sums are added to the first
-// one's in memory.  The tensor core cuts off what it adds, which shrinks a sum by some 2e-8 of itself with each K = 16
-// (1.0e-6 off after 1024 rows, 1.6e-5 after 16384): sums of 2048 rows stay at 2e-6.  A sum that is rounded to bf16 needs no such care.
-template <bool F32> constexpr int kAccSteps = F32 ? 2048 / kStageK : 1 << 30;
+// Stages after which a tile goes on in another accumulator, whose sums the epilogue adds up in registers, where sums are
+// given in fp32 (FINE: the weight gradient) or rounded to 8 bits (the gated product).  The tensor core cuts off what it adds,
+// which shrinks a sum by some 2e-8 of itself with each K = 16: 1.0e-6 after 1024, 1.6e-5 after 16384; with 1024 at a time it stays
+// there.  (960 for the gradients, which then are within 1e-6.  Of the 8-bit codes of sums over K = 7168 in one accumulator, one in 5000 falls the other way.)  512 at a time keep the
+// epilogue, which has to add before it can store, from running under the products: 10-19 % more time for the gated product.  A
+// sum that is rounded to bf16 needs no such care.
+template <ExpertOp OP, bool FINE> constexpr int kAccSteps = !FINE ? 1 << 30 : (OP == ExpertOp::kWeightGrad ? 960 : 1024) / kStageK;
 
 // 32 features (lanes) x 32 (fp32) or 64 (bf16) columns of a weight gradient, through 4 KB of shared memory: a lane writes
 // its feature's 128 bytes, 16-byte units permuted by the feature, and then eight lanes store the 128 bytes of one feature, so
 // that whole lines leave and nothing waits.  (By TMA stores the box has to be read before it is filled again, and they queue
-// with the loads, which already keep the TMA unit busy: a stage is 256 lines in 512 clocks.)  `add`: to what is there, which
-// this thread or an earlier kernel stored.
+// with the loads, which already keep the TMA unit busy: a stage is 256 lines in 512 clocks.)
 template <bool F32>
 __device__ __forceinline__ void store_grad(const KernelParams &p, const Tile &t, int f, int col, const uint4 (&v)[8], unsigned char *plane,
-                                           int lane, bool add)
+                                           int lane)
 {
 #pragma unroll
     for (int q = 0; q < 8; ++q) *reinterpret_cast<uint4 *>(plane + lane * kLine + ((q ^ (lane & 7)) << 4)) = v[q];
@@ -442,33 +467,36 @@ __device__ __forceinline__ void store_grad(const KernelParams &p, const Tile &t,
     char *dst = static_cast<char *>(p.y) + (((size_t)t.slot * p.M + f) * p.N + c) * (16 / kWord);
     const size_t pitch = (size_t)p.N * (16 / kWord);
     const int left = c < p.N ? p.M - f : 0;                    // N is a multiple of 8
-    float4 before[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const int r = 4 * i + (lane >> 3);
-        if (F32 && add && r < left) before[i] = *reinterpret_cast<const float4 *>(dst + r * pitch);
-    }
+    for (int half = 0; half < 2; ++half) {                     // four loads on their way at a time
+        float4 before[4];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const int r = 4 * i + (lane >> 3);
-        uint4 o = *reinterpret_cast<const uint4 *>(plane + r * kLine + ((unit ^ (r & 7)) << 4));
-        if (F32 && add)
-            o = make_uint4(__float_as_uint(__uint_as_float(o.x) + before[i].x), __float_as_uint(__uint_as_float(o.y) + before[i].y),
-                           __float_as_uint(__uint_as_float(o.z) + before[i].z), __float_as_uint(__uint_as_float(o.w) + before[i].w));
-        if (r < left) *reinterpret_cast<uint4 *>(dst + r * pitch) = o;
+        for (int i = 0; i < 4; ++i) {
+            const int r = 16 * half + 4 * i + (lane >> 3);
+            if (F32 && p.add && r < left) before[i] = *reinterpret_cast<const float4 *>(dst + r * pitch);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int r = 16 * half + 4 * i + (lane >> 3);
+            uint4 o = *reinterpret_cast<const uint4 *>(plane + r * kLine + ((unit ^ (r & 7)) << 4));
+            if (F32 && p.add)
+                o = make_uint4(__float_as_uint(__uint_as_float(o.x) + before[i].x), __float_as_uint(__uint_as_float(o.y) + before[i].y),
+                               __float_as_uint(__uint_as_float(o.z) + before[i].z), __float_as_uint(__uint_as_float(o.w) + before[i].w));
+            if (r < left) *reinterpret_cast<uint4 *>(dst + r * pitch) = o;
+        }
     }
     __syncwarp();                                              // the plane is free again
 }
 
 // ------------------------------------------------------------------------ kernel
 
-template <ExpertOp OP, int NT, int CG, bool F32>
-__global__ void __launch_bounds__(kThreads, 1)
+template <ExpertOp OP, int NT, int CG, bool FINE, bool F32>
+__global__ void __launch_bounds__(kThreadsOf<NT, FINE>, 1)
 k_expert_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_big,
                  const KernelParams p)
 {
     // map_a: the M operand (weights, or the left operand of a weight gradient); map_b, map_big: the N operand
-    using L = Layout<OP, NT, CG>;
+    using L = Layout<OP, NT, CG, FINE>;
     constexpr bool kGrad = L::kGrad;
     constexpr int kBox = 32;                                   // rows per TMA load of few rows
     extern __shared__ unsigned char raw[];
@@ -511,7 +539,7 @@ k_expert_product(const __grid_constant__ CUtensorMap map_a, const __grid_constan
         __syncthreads();
     } else {
         // inclusive prefix over the slots of their tile counts
-        const int chunk = (p.P + kThreads - 1) / kThreads, s0 = tid * chunk, s1 = min(p.P, s0 + chunk);
+        const int chunk = (p.P + L::kThreads - 1) / L::kThreads, s0 = tid * chunk, s1 = min(p.P, s0 + chunk);
         int sum = 0;
 #pragma unroll 1
         for (int s = s0; s < s1; ++s) {
@@ -556,208 +584,270 @@ k_expert_product(const __grid_constant__ CUtensorMap map_a, const __grid_constan
 
     // The two issuing warps run their loops with all lanes, so that everything the asynchronous instructions
     // take is uniform over the warp, and issue from one elected lane.
-    if (warp == kTmaWarp) {
-        int issued = 0, s = 0;
-        const uint32_t lead = lead_addr<CG>(full);             // the first CTA's barrier counts the bytes of both
-        unsigned parity = 1;                                   // a fresh barrier passes the wait for parity 1
-        bool ok = true;
-        Tile t;
-        for (TileStream<OP, NT, CG> stream(p, ends, tiles); ok && stream.next(t);) {
-            const int n = tile_n<OP, NT, CG>(p, t), half = n / CG;   // rows (or columns) of the tile in this CTA
-            // each TMA instruction costs its warp some 80 cycles: many rows come in one box, few in boxes of 32
-            const bool big = half > 2 * kBox;
-            const int loads = big ? 1 : (half + kBox - 1) / kBox;
-            const uint32_t bytes = CG * (kATile + (kGrad || big ? L::kN : loads * kBox) * kLine);
-            const int steps = ((kGrad ? t.rows : p.K) + kStageK - 1) / kStageK;
-            const int feat = t.feat + rank * kFeat;
-            for (int k = 0; k < steps; ++k) {
-                ok = __all_sync(0xffffffffu, wait_for(&empty[s], parity, quit, p.spin_limit));
-                if (!ok) break;
-                unsigned char *a = stage + s * L::kStage, *b = a + kATile;
-                if (elect_one()) {
-                    uint32_t bar = lead + s * 8;
-                    if (kGrad) {
-                        const int r = t.row + k * kStageK, col = t.col + rank * half;
-                        // a stage whose last lines have to be made zero: the second CTA counts its own bytes
-                        const bool own = CG == 2 && has_tail(t.rows - k * kStageK);
-                        if (rank == 0) mbar_expect_tx(&full[s], own ? bytes / CG : bytes);
-                        else if (own) {
-                            mbar_expect_tx(&tail[s], bytes / CG);
-                            bar = smem_addr(&tail[s]);
-                        }
-                        if (own) load_grad<1, L::kN>(a, b, &map_a, &map_b, feat, col, r, bar);
-                        else load_grad<CG, L::kN>(a, b, &map_a, &map_b, feat, col, r, bar);
-                    } else {
-                        if (rank == 0) mbar_expect_tx(&full[s], bytes);
-                        if (L::kAAlongK) tma_3d<CG>(a, &map_a, k * kStageK, feat, t.slot, bar);
-                        else {
-#pragma unroll
-                            for (int q = 0; q < kFeat / 64; ++q) tma_3d<CG>(a + q * kChunk, &map_a, feat + q * 64, k * kStageK, t.slot, bar);
-                        }
-                        if (big) tma_2d<CG>(b, &map_big, k * kStageK, t.row + rank * half, bar);
-                        else for (int l = 0; l < loads; ++l)
-                            tma_2d<CG>(b + l * kBox * kLine, &map_b, k * kStageK, t.row + rank * half + l * kBox, bar);
-                    }
-                }
-                __syncwarp();
-                ++issued;
-                if (++s == stages) { s = 0; parity ^= 1u; }
-            }
-        }
-        if (!ok) {
-            // loads in flight still land in this CTA's shared memory: a bounded wait for them (the barriers may be the
-            // other CTA's, so they may not complete, but the wait outlasts any copy)
-            unsigned long long until = 0;
-            for (int m = max(0, issued - stages); m < issued; ++m) drain_wait(&full[m % stages], (unsigned)(m / stages) & 1u, until);
-        }
-    } else if (warp == kMmaWarp && rank == 0) {
-        int s = 0, buf = 0;
-        unsigned parity = 0, acc_parity = 1, peer_parity = 0;  // peer_parity: a bit per stage, of its next use
-        bool ok = true;
-        const uint64_t a_desc = desc_tile<L::kAAlongK>(smem_addr(stage)), b_desc = desc_tile<L::kBAlongK>(smem_addr(stage + kATile));
-        Tile t;
-        for (TileStream<OP, NT, CG> stream(p, ends, tiles); ok && stream.next(t);) {
-            const uint32_t idesc = idesc_bf16<CG, L::kAAlongK, L::kBAlongK>(tile_n<OP, NT, CG>(p, t));
-            const int steps = ((kGrad ? t.rows : p.K) + kStageK - 1) / kStageK;
-            int k = 0;
-            do {                                               // once for every accumulator that the tile takes
-                ok = __all_sync(0xffffffffu, wait_for(&acc_empty[buf], acc_parity, quit, p.spin_limit));
-                if (!ok) break;
-                tc_fence_after();
-                const uint32_t d = tmem + buf * NT;
-                const int first = k, last = kAccSteps<F32> < steps - k ? k + kAccSteps<F32> : steps;
-                bool ready = steps > 0 && __all_sync(0xffffffffu, mbar_test_wait(&full[s], parity));
-                for (; k < last; ++k) {
-                    if (!ready) {
-                        ok = __all_sync(0xffffffffu, wait_for(&full[s], parity, quit, p.spin_limit));
-                        if (!ok) break;
-                    }
-                    // ask for the next stage's barrier now: the answer arrives while this stage is issued
-                    const int s_next = s + 1 == stages ? 0 : s + 1;
-                    const bool next_full = mbar_test_wait(&full[s_next], s_next ? parity : parity ^ 1u);
-                    const int left = t.rows - k * kStageK;     // of a weight gradient
-                    if (kGrad && has_tail(left)) {
-                        clear_tail(stage + s * L::kStage, L::kStage, left, lane);
-                        if (CG == 2) {                         // so has the second CTA
-                            ok = __all_sync(0xffffffffu, wait_for(&peer[s], (peer_parity >> s) & 1u, quit, p.spin_limit));
-                            if (!ok) break;
-                            peer_parity ^= 1u << s;
-                        }
-                    }
-                    tc_fence_after();
-                    // descriptors count in 16-byte units
-                    const uint64_t a = a_desc + (uint32_t)(s * (L::kStage >> 4)), b = b_desc + (uint32_t)(s * (L::kStage >> 4));
-                    if (elect_one()) {
-#pragma unroll
-                        for (int q = 0; q < kStageK / 16; ++q)
-                            if (!kGrad || q * 16 < left)
-                                mma_bf16<CG>(d, a + q * kDescStep<L::kAAlongK>, b + q * kDescStep<L::kBAlongK>, idesc, k > first || q > 0);
-                        mma_commit<CG>(&empty[s]);
-                        if (k == last - 1) mma_commit<CG>(&acc_full[buf]);
-                    }
-                    ready = __all_sync(0xffffffffu, next_full);
-                    s = s_next;
-                    if (s == 0) parity ^= 1u;
-                }
-                if (!ok) break;
-                if (kGrad && steps == 0 && elect_one()) mma_commit<CG>(&acc_full[buf]);   // nothing to wait for
-                buf ^= 1;
-                if (buf == 0) acc_parity ^= 1u;
-            } while (k < steps);
-        }
-        // everything issued has left the tensor core before TMEM is given back
-        if (elect_one()) mma_commit<CG>(drained);
-        __syncwarp();
-        unsigned long long until = 0;
-        drain_wait(drained, 0, until);
-    } else if (warp == kMmaWarp && kGrad) {
-        // The second CTA of a pair: its share of the stages that end a segment within a K = 16 (see clear_tail), announced to the
-        // first one, whose thread issues the MMA that reads these lines, as in mbar_arrive_lead.  (With a release of cluster scope:
-        // 128 x 511 rows 1488 us instead of 1054; such an arrival on every stage: 510 TFLOP/s.)
-        int s = 0;
-        unsigned tail_parity = 0;                              // a bit per stage, of its next use
-        bool ok = true;
-        Tile t;
-        for (TileStream<OP, NT, CG> stream(p, ends, tiles); ok && stream.next(t);) {
-            const int steps = (t.rows + kStageK - 1) / kStageK, left = t.rows - (steps - 1) * kStageK;
-            if (steps > 0 && has_tail(left)) {
-                const int at = (s + steps - 1) % stages;
-                ok = __all_sync(0xffffffffu, wait_for(&tail[at], (tail_parity >> at) & 1u, quit, p.spin_limit));
-                if (!ok) break;
-                tail_parity ^= 1u << at;
-                clear_tail(stage + at * L::kStage, L::kStage, left, lane);
-                if (lane == 0) mbar_arrive_lead<CG>(&peer[at]);
-            }
-            s = (s + steps) % stages;
-        }
-    } else if (warp < kEpiWarps) {
+    if (warp < kEpiWarps) {
+        if (kSplitRegs<NT, FINE>) asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
         // epilogue: TMEM lane = feature of the tile, column = row (weight gradient: column)
         const int group = warp >> 2, quarter = warp & 3;
         unsigned char *mine = epi + warp * L::kEpiWarp;
+        constexpr int kPieces = NT / 64;                       // of 32 columns, of this warp: c0 = group * 32, then every 64
         int buf = 0;
         unsigned acc_parity = 0;
         Tile t;
         bool ok = true;
-        int k = 0;                                             // of a weight gradient: stages of the tile that are done
-        for (TileStream<OP, NT, CG> stream(p, ends, tiles); ok && (k > 0 || stream.next(t));) {
-            ok = __all_sync(0xffffffffu, wait_for(&acc_full[buf], acc_parity, quit, p.spin_limit));
-            if (!ok) break;
-            tc_fence_after();
-            const uint32_t acc = tmem + buf * NT + ((uint32_t)(quarter * 32) << 16);
+        for (TileStream<OP, NT, CG> stream(p, ends, tiles); ok && stream.next(t);) {
             const int f = t.feat + rank * kFeat + quarter * 32;
-            if (kGrad) {
-                const int cols = min(NT, p.N - t.col), steps = (t.rows + kStageK - 1) / kStageK;
-                const bool add = F32 && (p.add || k > 0);      // k > 0: sums of the same elements have been stored
-                const bool any = f < p.M && !(add && steps == 0);
-                constexpr int kCols = F32 ? 32 : 64;           // of a box
-                for (int c0 = group * kCols; c0 < cols && any; c0 += 2 * kCols) {
-                    uint4 box[8] = {};
-                    if (steps > 0) {
-                        uint32_t v[kCols / 32][32];
-#pragma unroll
-                        for (int q = 0; q < kCols / 32; ++q) tmem_ld_lanes(acc + c0 + 32 * q, v[q]);
-                        tmem_wait_ld();
-#pragma unroll
-                        for (int q = 0; q < 8; ++q) {
-                            const uint32_t *w = F32 ? &v[0][4 * q] : &v[(kCols / 32 - 1) & (q >> 2)][8 * (q & 3)];
-                            box[q] = F32 ? make_uint4(w[0], w[1], w[2], w[3])
-                                         : make_uint4(pack_bf16(__uint_as_float(w[0]), __uint_as_float(w[1])),
-                                                      pack_bf16(__uint_as_float(w[2]), __uint_as_float(w[3])),
-                                                      pack_bf16(__uint_as_float(w[4]), __uint_as_float(w[5])),
-                                                      pack_bf16(__uint_as_float(w[6]), __uint_as_float(w[7])));
-                        }
-                    }
-                    store_grad<F32>(p, t, f, t.col + c0, box, mine, lane, add);
-                }
-                k = F32 && steps - k > kAccSteps<F32> ? k + kAccSteps<F32> : 0;
+            const int cols = kGrad ? min(NT, p.N - t.col) : t.rows, steps = ((kGrad ? t.rows : p.K) + kStageK - 1) / kStageK;
+            const auto wait_acc = [&] {
+                ok = __all_sync(0xffffffffu, wait_for(&acc_full[buf], acc_parity, quit, p.spin_limit));
+                tc_fence_after();
+                return ok;
+            };
+            const auto release_acc = [&] {                     // after this warp's last look at the accumulator
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive_lead<CG>(&acc_empty[buf]);
+            };
+            const auto next_acc = [&] {
+                buf ^= 1;
+                if (buf == 0) acc_parity ^= 1u;
+            };
+            const auto acc_at = [&](int c0) { return tmem + buf * NT + c0 + ((uint32_t)(quarter * 32) << 16); };
+            uint32_t sum[FINE ? kPieces : 1][32];
+            const auto next_piece = [&] {                      // to the front: a piece's number is no register's
+#pragma unroll
+                for (int n = 1; n < kPieces; ++n)
+#pragma unroll
+                    for (int c = 0; c < 32; ++c) sum[FINE ? n - 1 : 0][c] = sum[FINE ? n : 0][c];
+            };
+            const bool one = !FINE || steps <= kAccSteps<OP, FINE>;   // accumulator: its pieces are read as they are stored
+            if (!one) {                                        // all of the tile's accumulators added up
+                int k = 0;
+#pragma unroll
+                for (int q = 0; q < kPieces; ++q)
+#pragma unroll
+                    for (int c = 0; c < 32; ++c) sum[q][c] = 0u;
+                do {
+                    if (!wait_acc()) break;
+#pragma unroll
+                    for (int q = 0; q < kPieces; ++q) {
+                        if (group * 32 + 64 * q >= cols) break;
+                        const uint32_t at = acc_at(group * 32 + 64 * q);
+#pragma unroll
+                        for (int half = 0; half < 32; half += 16) {
+                            uint32_t v[16];
+                            tmem_ld_lanes(at + half, v);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int c = 0; c < 16; ++c)
+                                sum[q][half + c] = __float_as_uint(__uint_as_float(sum[q][half + c]) + __uint_as_float(v[c]));
+                        }
+                    }
+                    release_acc();
+                    next_acc();
+                    k += kAccSteps<OP, FINE>;
+                } while (k < steps);
+                if (!ok) break;
+            } else if (!wait_acc()) {
+                break;
+            }
+            if (kGrad && !F32) {
+                for (int c0 = group * 64; c0 < cols && f < p.M; c0 += 128) {
+                    uint4 box[8] = {};
+                    if (steps > 0) {
+                        uint32_t v[2][32];
+                        tmem_ld_lanes(acc_at(c0), v[0]);
+                        tmem_ld_lanes(acc_at(c0 + 32), v[1]);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int q = 0; q < 8; ++q) {
+                            const uint32_t *w = &v[q >> 2][8 * (q & 3)];
+                            box[q] = make_uint4(pack_bf16(__uint_as_float(w[0]), __uint_as_float(w[1])),
+                                                pack_bf16(__uint_as_float(w[2]), __uint_as_float(w[3])),
+                                                pack_bf16(__uint_as_float(w[4]), __uint_as_float(w[5])),
+                                                pack_bf16(__uint_as_float(w[6]), __uint_as_float(w[7])));
+                        }
+                    }
+                    store_grad<false>(p, t, f, t.col + c0, box, mine, lane);
+                }
+                release_acc();
+            } else if (kGrad) {
+#pragma unroll 1
+                for (int q = 0; q < kPieces; ++q) {
+                    const int c0 = group * 32 + 64 * q;
+                    if (c0 >= cols || f >= p.M || (p.add && steps == 0)) break;
+                    if (one && steps > 0) {
+                        tmem_ld_lanes(acc_at(c0), sum[0]);
+                        tmem_wait_ld();
+                    }
+                    uint4 box[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) 
+                        box[i] = steps > 0 ? make_uint4(sum[0][4 * i], sum[0][4 * i + 1], sum[0][4 * i + 2], sum[0][4 * i + 3]) : make_uint4(0u, 0u, 0u, 0u);
+                    store_grad<true>(p, t, f, t.col + c0, box, mine, lane);
+                    if (!one) next_piece();
+                }
+                if (one) release_acc();
             } else {
                 float *plane = reinterpret_cast<float *>(mine);
-                for (int c0 = group * 32; c0 < t.rows; c0 += 64) {
+#pragma unroll 1
+                for (int q = 0; q < kPieces; ++q) {
+                    const int c0 = group * 32 + 64 * q, left = cols - c0;
+                    if (left <= 0) break;
                     const long long row = t.row + c0;
-                    const int left = t.rows - c0;
                     Kept kept[4];
                     if (OP == ExpertOp::kGatedBackward) load_kept(p, f, row, left, lane, kept);
-                    uint32_t v[32];
-                    tmem_ld_lanes(acc + c0, v);
-                    tmem_wait_ld();
-                    if (c0 + 64 >= t.rows) {                   // this warp's last look at the accumulator
-                        tc_fence_before();
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive_lead<CG>(&acc_empty[buf]);
+                    if (one) {
+                        tmem_ld_lanes(acc_at(c0), sum[0]);
+                        tmem_wait_ld();
+                        if (left <= 64) release_acc();
                     }
-                    write_plane(plane, v, lane);
+                    write_plane(plane, sum[0], lane);
                     if (OP == ExpertOp::kGated) store_gated(p, plane, f, row, left, lane);
                     else if (OP == ExpertOp::kGatedBackward) store_gated_backward(p, plane, f, row, left, lane, kept);
                     else store_rows(p, plane, f, row, left, lane);
                     __syncwarp();                              // the plane is free before the next 32 rows are written
+                    if (!one) next_piece();
                 }
-                if (group * 32 >= t.rows && lane == 0) mbar_arrive_lead<CG>(&acc_empty[buf]);
+                if (one && group * 32 >= cols) release_acc();
             }
-            buf ^= 1;
-            if (buf == 0) acc_parity ^= 1u;
+            if (one) next_acc();
+        }
+    } else {
+        if (kSplitRegs<NT, FINE>) asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+        if (warp == kTmaWarp) {
+            int issued = 0, s = 0;
+            const uint32_t lead = lead_addr<CG>(full);             // the first CTA's barrier counts the bytes of both
+            unsigned parity = 1;                                   // a fresh barrier passes the wait for parity 1
+            bool ok = true;
+            Tile t;
+            for (TileStream<OP, NT, CG> stream(p, ends, tiles); ok && stream.next(t);) {
+                const int n = tile_n<OP, NT, CG>(p, t), half = n / CG;   // rows (or columns) of the tile in this CTA
+                // each TMA instruction costs its warp some 80 cycles: many rows come in one box, few in boxes of 32
+                const bool big = half > 2 * kBox;
+                const int loads = big ? 1 : (half + kBox - 1) / kBox;
+                const uint32_t bytes = CG * (kATile + (kGrad || big ? L::kN : loads * kBox) * kLine);
+                const int steps = ((kGrad ? t.rows : p.K) + kStageK - 1) / kStageK;
+                const int feat = t.feat + rank * kFeat;
+                for (int k = 0; k < steps; ++k) {
+                    ok = __all_sync(0xffffffffu, wait_for(&empty[s], parity, quit, p.spin_limit));
+                    if (!ok) break;
+                    unsigned char *a = stage + s * L::kStage, *b = a + kATile;
+                    if (elect_one()) {
+                        uint32_t bar = lead + s * 8;
+                        if (kGrad) {
+                            const int r = t.row + k * kStageK, col = t.col + rank * half;
+                            // a stage whose last lines have to be made zero: the second CTA counts its own bytes
+                            const bool own = CG == 2 && has_tail(t.rows - k * kStageK);
+                            if (rank == 0) mbar_expect_tx(&full[s], own ? bytes / CG : bytes);
+                            else if (own) {
+                                mbar_expect_tx(&tail[s], bytes / CG);
+                                bar = smem_addr(&tail[s]);
+                            }
+                            if (own) load_grad<1, L::kN>(a, b, &map_a, &map_b, feat, col, r, bar);
+                            else load_grad<CG, L::kN>(a, b, &map_a, &map_b, feat, col, r, bar);
+                        } else {
+                            if (rank == 0) mbar_expect_tx(&full[s], bytes);
+                            if (L::kAAlongK) tma_3d<CG>(a, &map_a, k * kStageK, feat, t.slot, bar);
+                            else {
+    #pragma unroll
+                                for (int q = 0; q < kFeat / 64; ++q) tma_3d<CG>(a + q * kChunk, &map_a, feat + q * 64, k * kStageK, t.slot, bar);
+                            }
+                            if (big) tma_2d<CG>(b, &map_big, k * kStageK, t.row + rank * half, bar);
+                            else for (int l = 0; l < loads; ++l)
+                                tma_2d<CG>(b + l * kBox * kLine, &map_b, k * kStageK, t.row + rank * half + l * kBox, bar);
+                        }
+                    }
+                    __syncwarp();
+                    ++issued;
+                    if (++s == stages) { s = 0; parity ^= 1u; }
+                }
+            }
+            if (!ok) {
+                // loads in flight still land in this CTA's shared memory: a bounded wait for them (the barriers may be the
+                // other CTA's, so they may not complete, but the wait outlasts any copy)
+                unsigned long long until = 0;
+                for (int m = max(0, issued - stages); m < issued; ++m) drain_wait(&full[m % stages], (unsigned)(m / stages) & 1u, until);
+            }
+        } else if (warp == kMmaWarp && rank == 0) {
+            int s = 0, buf = 0;
+            unsigned parity = 0, acc_parity = 1, peer_parity = 0;  // peer_parity: a bit per stage, of its next use
+            bool ok = true;
+            const uint64_t a_desc = desc_tile<L::kAAlongK>(smem_addr(stage)), b_desc = desc_tile<L::kBAlongK>(smem_addr(stage + kATile));
+            Tile t;
+            for (TileStream<OP, NT, CG> stream(p, ends, tiles); ok && stream.next(t);) {
+                const uint32_t idesc = idesc_bf16<CG, L::kAAlongK, L::kBAlongK>(tile_n<OP, NT, CG>(p, t));
+                const int steps = ((kGrad ? t.rows : p.K) + kStageK - 1) / kStageK;
+                int k = 0;
+                do {                                               // once for every accumulator that the tile takes
+                    ok = __all_sync(0xffffffffu, wait_for(&acc_empty[buf], acc_parity, quit, p.spin_limit));
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint32_t d = tmem + buf * NT;
+                    const int first = k, last = kAccSteps<OP, FINE> < steps - k ? k + kAccSteps<OP, FINE> : steps;
+                    bool ready = steps > 0 && __all_sync(0xffffffffu, mbar_test_wait(&full[s], parity));
+                    for (; k < last; ++k) {
+                        if (!ready) {
+                            ok = __all_sync(0xffffffffu, wait_for(&full[s], parity, quit, p.spin_limit));
+                            if (!ok) break;
+                        }
+                        // ask for the next stage's barrier now: the answer arrives while this stage is issued
+                        const int s_next = s + 1 == stages ? 0 : s + 1;
+                        const bool next_full = mbar_test_wait(&full[s_next], s_next ? parity : parity ^ 1u);
+                        const int left = t.rows - k * kStageK;     // of a weight gradient
+                        if (kGrad && has_tail(left)) {
+                            clear_tail(stage + s * L::kStage, L::kStage, left, lane);
+                            if (CG == 2) {                         // so has the second CTA
+                                ok = __all_sync(0xffffffffu, wait_for(&peer[s], (peer_parity >> s) & 1u, quit, p.spin_limit));
+                                if (!ok) break;
+                                peer_parity ^= 1u << s;
+                            }
+                        }
+                        tc_fence_after();
+                        // descriptors count in 16-byte units
+                        const uint64_t a = a_desc + (uint32_t)(s * (L::kStage >> 4)), b = b_desc + (uint32_t)(s * (L::kStage >> 4));
+                        if (elect_one()) {
+    #pragma unroll
+                            for (int q = 0; q < kStageK / 16; ++q)
+                                if (!kGrad || q * 16 < left)
+                                    mma_bf16<CG>(d, a + q * kDescStep<L::kAAlongK>, b + q * kDescStep<L::kBAlongK>, idesc, k > first || q > 0);
+                            mma_commit<CG>(&empty[s]);
+                            if (k == last - 1) mma_commit<CG>(&acc_full[buf]);
+                        }
+                        ready = __all_sync(0xffffffffu, next_full);
+                        s = s_next;
+                        if (s == 0) parity ^= 1u;
+                    }
+                    if (!ok) break;
+                    if (kGrad && steps == 0 && elect_one()) mma_commit<CG>(&acc_full[buf]);   // nothing to wait for
+                    buf ^= 1;
+                    if (buf == 0) acc_parity ^= 1u;
+                } while (k < steps);
+            }
+            // everything issued has left the tensor core before TMEM is given back
+            if (elect_one()) mma_commit<CG>(drained);
+            __syncwarp();
+            unsigned long long until = 0;
+            drain_wait(drained, 0, until);
+        } else if (warp == kMmaWarp && kGrad) {
+            // The second CTA of a pair: its share of the stages that end a segment within a K = 16 (see clear_tail), announced to the
+            // first one, whose thread issues the MMA that reads these lines, as in mbar_arrive_lead.  (With a release of cluster scope:
+            // 128 x 511 rows 1488 us instead of 1054; such an arrival on every stage: 510 TFLOP/s.)
+            int s = 0;
+            unsigned tail_parity = 0;                              // a bit per stage, of its next use
+            bool ok = true;
+            Tile t;
+            for (TileStream<OP, NT, CG> stream(p, ends, tiles); ok && stream.next(t);) {
+                const int steps = (t.rows + kStageK - 1) / kStageK, left = t.rows - (steps - 1) * kStageK;
+                if (steps > 0 && has_tail(left)) {
+                    const int at = (s + steps - 1) % stages;
+                    ok = __all_sync(0xffffffffu, wait_for(&tail[at], (tail_parity >> at) & 1u, quit, p.spin_limit));
+                    if (!ok) break;
+                    tail_parity ^= 1u << at;
+                    clear_tail(stage + at * L::kStage, L::kStage, left, lane);
+                    if (lane == 0) mbar_arrive_lead<CG>(&peer[at]);
+                }
+                s = (s + steps) % stages;
+            }
         }
     }
 
@@ -779,12 +869,12 @@ k_expert_product(const __grid_constant__ CUtensorMap map_a, const __grid_constan
 
 // ------------------------------------------------------------------------- host
 
-template <ExpertOp OP, int NT, int CG, bool F32 = false>
+template <ExpertOp OP, int NT, int CG, bool FINE = false, bool F32 = false>
 cudaError_t launch(const ExpertArgs &a, cudaStream_t st)
 {
-    using L = Layout<OP, NT, CG>;
+    using L = Layout<OP, NT, CG, FINE>;
     static_assert(L::kN % 64 == 0 && NT % 32 == 0 && 2 * NT <= 512, "boxes of the row operand, pieces of the epilogue, TMEM columns");
-    const auto kernel = k_expert_product<OP, NT, CG, F32>;
+    const auto kernel = k_expert_product<OP, NT, CG, FINE, F32>;
     // a function's attributes are those of one device
     constexpr int kDevices = 64;
     static std::once_flag once[kDevices];
@@ -819,7 +909,7 @@ cudaError_t launch(const ExpertArgs &a, cudaStream_t st)
     const long long most = L::kGrad ? feats * ((a.N + NT - 1) / NT) * a.P : feats * (std::min<long long>(a.P, a.rows) + a.rows / NT);
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(CG * std::min<long long>(a.sm_count / CG, most)));
-    cfg.blockDim = dim3(kThreads); cfg.dynamicSmemBytes = L::bytes(a.P); cfg.stream = st;
+    cfg.blockDim = dim3(L::kThreads); cfg.dynamicSmemBytes = L::bytes(a.P); cfg.stream = st;
     cudaLaunchAttribute at[2];
     at[0].id = cudaLaunchAttributeClusterDimension;
     at[0].val.clusterDim.x = CG; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
@@ -835,8 +925,9 @@ cudaError_t launch(const ExpertArgs &a, cudaStream_t st)
 template <ExpertOp OP>
 cudaError_t launch_for(const ExpertArgs &a, cudaStream_t st)
 {
-    if (a.rows <= 64ll * a.P) return launch<OP, 64, 1>(a, st);
-    return launch<OP, 256, 2>(a, st);
+    const bool narrow = a.rows <= 64ll * a.P;
+    constexpr bool kFine = OP == ExpertOp::kGated;             // its output does not depend on what is kept
+    return narrow ? launch<OP, 64, 1, kFine>(a, st) : launch<OP, 256, 2, kFine>(a, st);
 }
 
 }  // namespace
@@ -850,7 +941,12 @@ cudaError_t expert_product_launch(const ExpertArgs &a, cudaStream_t st)
     case ExpertOp::kGated: return launch_for<ExpertOp::kGated>(a, st);
     case ExpertOp::kTransposed: return launch_for<ExpertOp::kTransposed>(a, st);
     case ExpertOp::kGatedBackward: return launch_for<ExpertOp::kGatedBackward>(a, st);
-    case ExpertOp::kWeightGrad: return a.f32 ? launch<ExpertOp::kWeightGrad, 256, 2, true>(a, st) : launch<ExpertOp::kWeightGrad, 256, 2>(a, st);
+    case ExpertOp::kWeightGrad:
+        if (!a.f32) return launch<ExpertOp::kWeightGrad, 256, 2>(a, st);
+        // no segment is longer than the buffer: one accumulator will do, and the kernel without the sums is 5-10 % faster where
+        // the stores bound it (24 slots of 45 rows, 4096 x 1024: 82 and 90 us)
+        if (a.rows <= kAccSteps<ExpertOp::kWeightGrad, true> * kStageK) return launch<ExpertOp::kWeightGrad, 256, 2, false, true>(a, st);
+        return launch<ExpertOp::kWeightGrad, 256, 2, true, true>(a, st);
     }
     return cudaErrorInvalidValue;
 }

@@ -129,23 +129,21 @@ def test_backward(counts, H, I, kept):
             want, half = left.T @ right, U.HALF[got.dtype]
             bound = U.sum_bound(e - s, left.abs().T @ right.abs())
             U.within(got, want, (1 + half) * bound + half * want.abs())
-        # k pieces of 2048 rows: `added` takes k additions and the plain gradient k - 1, each rounded by at most 2^-24 of its
-        # result, and no partial sum is larger than the sum of magnitudes (and what was there)
-        k = -(-(e - s) // 2048)
-        most = before[p].double().abs() + d.abs().T @ a[s:e].double().abs()
-        U.within(added[p], grads[1][p].double() + before[p].double(), (2 * k - 1) * 2.0 ** -24 * (1 + 2.0 ** -10) * most)
+        # one rounding of the sum with what was there
+        total = grads[1][p].double() + before[p].double()
+        U.within(added[p], total, 2.0 ** -24 * total.abs())
     r.close()
 
 
 def test_fp32_gradients_of_many_rows():
-    """Sums of 2048 rows at a time: 20000 rows are as near as cutting off in 128 steps of K = 16 leaves them, plus a rounding for
-    each of the ten pieces.  (In one accumulator they would be off by ten times as much.)"""
+    """Sums of 960 rows at a time: 20000 rows are as near as cutting off in 60 steps of K = 16 leaves them, plus a rounding for
+    each of the 21 pieces.  (In one accumulator they would be off by twenty times as much.)"""
     r = U.make_router(1)
     n_, off, n = U.layout([20000])
     dy, a = U.bf16(n, 64, seed=1).abs(), U.bf16(n, 72, seed=2).abs()      # all of one sign: cutting off adds up
     got = r.expert_weight_backward(dy, a, n_, off, dtype=torch.float32)[0].double()
     want = dy.double().T @ a.double()
-    assert ((got - want).abs() <= (U.sum_bound(2048, 1.0) + 10 * 2.0 ** -24) * want).all()
+    assert ((got - want).abs() <= (U.sum_bound(960, 1.0) + 21 * 2.0 ** -24) * want).all()
     r.close()
 
 
