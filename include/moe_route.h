@@ -426,7 +426,7 @@ moe_status moe_dispatch_backward(moe_ctx *ctx, const float *logits, const void *
  *   h = x + residual, rounded to the rows' type;  rstd = 1 / sqrt(mean(h^2) + eps);  y = h * rstd * weight
  *   x, residual  device [rows, cols] of `dtype`, x_stride and residual_stride elements from row to row (>= cols, rows 16-byte
  *     aligned).  residual may be NULL: then h = x, and h need not be given
- *   weight       device [cols] of `weight_dtype`: `dtype` or MOE_DTYPE_F32
+ *   weight       device [cols] of `weight_dtype`, any of the types
  *   h, y         device out [rows, cols] of `dtype`, contiguous.  h may be x or residual itself where that is contiguous
  *   rstd         device out [rows] f32, or NULL: needed by moe_rms_norm_backward
  *   codes, scales device out: y (before it is rounded to `dtype`) as 8-bit rows, with the padding of the scales as 0; or both NULL

@@ -15,6 +15,7 @@ Two layers:
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from dataclasses import dataclass
 
@@ -435,6 +436,11 @@ def moe_rms_norm_backward(dy_ptr: int, dh_ptr: int, h_ptr: int, rstd_ptr: int, d
                                         d_weight_ptr, workspace_ptr, workspace_bytes, cuda_stream)
 
 
+@functools.lru_cache(maxsize=256)
+def _norm_workspace(rows: int, cols: int) -> int:
+    return moe_rms_norm_backward_workspace(rows, cols)
+
+
 def moe_redispatch(ctx, codes_ptr: int, scales_ptr: int, T: int, send_buf_ptr: int, cuda_stream: int = 0) -> int:
     return _lib().moe_redispatch(ctx, codes_ptr, scales_ptr, T, send_buf_ptr, cuda_stream)
 
@@ -665,30 +671,30 @@ def _row_stride(t: torch.Tensor, cols: int) -> int:
 
 def rms_norm(x: torch.Tensor, weight: torch.Tensor, residual: torch.Tensor | None = None, eps: float = 1e-6, keep: bool = False,
              out: RmsNormOut | None = None) -> RmsNormOut:
-    """Root-mean-square norm of ``x`` + ``residual`` ([..., cols], bf16 / fp16 / fp32) times ``weight`` (the same type or fp32), on the
+    """Root-mean-square norm of ``x`` + ``residual`` ([..., cols], bf16 / fp16 / fp32) times ``weight`` (any of these types), on the
     current stream of its device.  ``keep``: also in 8 bits, for a backward pass.  ``out.h`` may be ``residual``
     itself."""
     shape, dtype, index = x.shape, x.dtype, x.get_device()
-    code = _DTYPE_CODE.get(dtype)
-    _require(x.is_cuda and code is not None and len(shape) > 0 and shape[-1] > 0, "rms_norm")
-    cols, lead = shape[-1], shape[:-1]
-    n = x.numel() // cols
-    x_stride = _row_stride(x, cols)
-    r_stride = cols if residual is None else _row_stride(residual, cols)
-    _require(x_stride >= 0 and r_stride >= 0 and weight.dtype in (dtype, torch.float32) and _is_dense(weight, weight.dtype, (cols,), index)
-             and (residual is None or (residual.shape == shape and residual.dtype is dtype and residual.get_device() == index)), "rms_norm")
+    code, w_code = _DTYPE_CODE.get(dtype), _DTYPE_CODE.get(weight.dtype)
+    _require(index >= 0 and code is not None and w_code is not None and len(shape) > 0 and shape[-1] > 0, "rms_norm")
+    cols, x_stride, r_stride = shape[-1], _row_stride(x, shape[-1]), 0
+    ok = (x_stride >= 0 and weight.get_device() == index and weight.dim() == 1 and weight.shape[0] == cols and weight.is_contiguous())
+    if residual is not None:
+        r_stride = _row_stride(residual, cols)
+        ok = ok and r_stride >= 0 and residual.shape == shape and residual.dtype is dtype and residual.get_device() == index
+    _require(ok, "rms_norm")
     if out is None:
-        h = x if residual is None else x.new_empty(shape)
-        y8 = Mx8Rows(x.new_empty(shape, dtype=torch.uint8), x.new_empty((*lead, _mx_pitch(cols)), dtype=torch.uint8)) if keep else None
-        out = RmsNormOut(x.new_empty(shape), h, x.new_empty(lead, dtype=torch.float32), y8)
+        y8 = Mx8Rows(x.new_empty(shape, dtype=torch.uint8), x.new_empty((*shape[:-1], _mx_pitch(cols)), dtype=torch.uint8)) if keep else None
+        out = RmsNormOut(x.new_empty(shape), x if residual is None else x.new_empty(shape), x.new_empty(shape[:-1], dtype=torch.float32), y8)
     else:
         _require(_is_dense(out.y, dtype, shape, index) and (residual is None or _is_dense(out.h, dtype, shape, index))
-                 and _is_dense(out.rstd, torch.float32, lead, index) and (not keep or _is_mx8(out.y8, index, shape)), "rms_norm")
+                 and _is_dense(out.rstd, torch.float32, shape[:-1], index) and (not keep or _is_mx8(out.y8, index, shape)), "rms_norm")
         if residual is None:
             out.h = x
-    st = _on_device(index, moe_rms_norm, x.data_ptr(), x_stride, 0 if residual is None else residual.data_ptr(), r_stride, code, n, cols,
-                    weight.data_ptr(), _DTYPE_CODE[weight.dtype], eps, 0 if residual is None else out.h.data_ptr(), out.y.data_ptr(),
-                    out.rstd.data_ptr(), out.y8.codes.data_ptr() if keep else 0, out.y8.scales.data_ptr() if keep else 0, _raw_stream(index))
+    r_ptr, h_ptr = (0, 0) if residual is None else (residual.data_ptr(), out.h.data_ptr())
+    c_ptr, s_ptr = (out.y8.codes.data_ptr(), out.y8.scales.data_ptr()) if keep else (0, 0)
+    st = _on_device(index, moe_rms_norm, x.data_ptr(), x_stride, r_ptr, r_stride, code, x.numel() // cols, cols, weight.data_ptr(), w_code, eps,
+                    h_ptr, out.y.data_ptr(), out.rstd.data_ptr(), c_ptr, s_ptr, _raw_stream(index))
     if st != MOE_OK:
         raise MoeError(st, "moe_rms_norm")
     return out
@@ -700,15 +706,15 @@ def rms_norm_backward(dy: torch.Tensor, h: torch.Tensor, rstd: torch.Tensor, wei
     forward; ``dh``: the gradient that comes to h past the norm.  ``dx`` may be dy, dh or h itself."""
     shape, dtype, index = dy.shape, dy.dtype, dy.get_device()
     code = _DTYPE_CODE.get(dtype)
-    _require(dy.is_cuda and code is not None and len(shape) > 0 and shape[-1] > 0, "rms_norm_backward")
+    _require(index >= 0 and code is not None and len(shape) > 0 and shape[-1] > 0, "rms_norm_backward")
     cols = shape[-1]
     n = dy.numel() // cols
     dx = torch.empty_like(dy) if dx is None else dx
     d_weight = dy.new_empty(cols, dtype=torch.float32) if d_weight is None else d_weight
     _require(all(_is_dense(t, dtype, shape, index) for t in ((dy, h, dx) if dh is None else (dy, h, dx, dh)))
-             and _is_dense(rstd, torch.float32, shape[:-1], index) and weight.dtype in (dtype, torch.float32)
+             and _is_dense(rstd, torch.float32, shape[:-1], index) and weight.dtype in _DTYPE_CODE
              and _is_dense(weight, weight.dtype, (cols,), index) and _is_dense(d_weight, torch.float32, (cols,), index), "rms_norm_backward")
-    ws = dy.new_empty(moe_rms_norm_backward_workspace(n, cols), dtype=torch.uint8)
+    ws = dy.new_empty(_norm_workspace(n, cols), dtype=torch.uint8)
     st = _on_device(index, moe_rms_norm_backward, dy.data_ptr(), 0 if dh is None else dh.data_ptr(), h.data_ptr(), rstd.data_ptr(), code, n,
                     cols, weight.data_ptr(), _DTYPE_CODE[weight.dtype], dx.data_ptr(), d_weight.data_ptr(), ws.data_ptr(), ws.numel(),
                     _raw_stream(index))

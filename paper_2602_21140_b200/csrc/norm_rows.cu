@@ -13,6 +13,7 @@
 #include "../../include/moe_route.h"
 
 #include <algorithm>
+#include <mutex>
 #include <type_traits>
 
 #include "mx8_format.cuh"
@@ -80,20 +81,17 @@ __device__ __forceinline__ void from_f32(const float (&v)[8], uint4 (&u)[kVec<DT
     }
 }
 
-// Eight elements of the weight, of the rows' type or fp32.
-template <int DT>
-__device__ __forceinline__ void weight8(const void *weight, bool f32, int unit, float (&v)[8])
+// Eight elements of the weight, of any of the types.
+__device__ __forceinline__ void weight8(const void *weight, int dtype, int unit, float (&v)[8])
 {
-    if (f32) {
-        uint4 u[2];
-        u[0] = __ldg(static_cast<const uint4 *>(weight) + 2 * unit);
-        u[1] = __ldg(static_cast<const uint4 *>(weight) + 2 * unit + 1);
+    const uint4 *src = static_cast<const uint4 *>(weight);
+    if (dtype == MOE_DTYPE_F32) {
+        const uint4 u[2] = {__ldg(src + 2 * unit), __ldg(src + 2 * unit + 1)};
         to_f32<MOE_DTYPE_F32>(u, v);
     } else {
-        uint4 u[kVec<DT>];
-#pragma unroll
-        for (int q = 0; q < kVec<DT>; ++q) u[q] = __ldg(static_cast<const uint4 *>(weight) + kVec<DT> * unit + q);
-        to_f32<DT>(u, v);
+        const uint4 u[1] = {__ldg(src + unit)};
+        if (dtype == MOE_DTYPE_BF16) to_f32<MOE_DTYPE_BF16>(u, v);
+        else to_f32<MOE_DTYPE_F16>(u, v);
     }
 }
 
@@ -119,7 +117,7 @@ struct NormParams {
     const uint4 *x, *residual;     // rows of x_stride and r_stride words of 16 bytes; residual may be NULL
     long long x_stride, r_stride;
     const void *weight;
-    bool weight_f32;
+    int weight_dtype;
     float eps;
     long long rows;
     int units;                     // of a row
@@ -177,7 +175,7 @@ __global__ void __launch_bounds__(WARP ? 256 : kMaxThreads) k_rms_norm(NormParam
         const bool inside = u < p.units;                       // with an 8-bit form whole blocks: all four lanes of one or none
         float a[8], w[8];
         to_f32<DT>(in[i], a);
-        if (inside) weight8<DT>(p.weight, p.weight_f32, u, w);
+        if (inside) weight8(p.weight, p.weight_dtype, u, w);
 #pragma unroll
         for (int q = 0; q < 8; ++q) a[q] = inside ? a[q] * rstd * w[q] : 0.0f;
         if (inside) {
@@ -203,7 +201,7 @@ struct NormBackwardParams {
     const uint4 *dy, *dh, *h;      // dh may be NULL
     const float *rstd;
     const void *weight;
-    bool weight_f32;
+    int weight_dtype;
     long long rows;
     int units;
     uint4 *dx;
@@ -237,7 +235,7 @@ __global__ void __launch_bounds__(256) k_rms_norm_backward(NormBackwardParams p)
     float acc[UN][8] = {}, w[UN][8] = {};
 #pragma unroll
     for (int i = 0; i < UN; ++i)
-        if (i * 32 + lane < p.units) weight8<DT>(p.weight, p.weight_f32, i * 32 + lane, w[i]);
+        if (i * 32 + lane < p.units) weight8(p.weight, p.weight_dtype, i * 32 + lane, w[i]);
     for (long long row = (long long)blockIdx.x * kRows + sub; row < p.rows; row += (long long)gridDim.x * kRows) {
         uint4 a[UN][V], b[UN][V], c[UN][V];
 #pragma unroll
@@ -281,6 +279,7 @@ __global__ void __launch_bounds__(256) k_rms_norm_backward(NormBackwardParams p)
             for (int q = 0; q < V; ++q) p.dx[(row * p.units + u) * V + q] = o[q];
         }
     }
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int cols = p.units * 8;
 #pragma unroll
     for (int i = 0; i < UN; ++i) {
@@ -312,7 +311,7 @@ __global__ void __launch_bounds__(kMaxThreads) k_rms_norm_backward_ring(NormBack
     float acc[kUnits][8] = {}, w[kUnits][8] = {};
 #pragma unroll
     for (int i = 0; i < kUnits; ++i)
-        if (i * threads + tid < p.units) weight8<DT>(p.weight, p.weight_f32, i * threads + tid, w[i]);
+        if (i * threads + tid < p.units) weight8(p.weight, p.weight_dtype, i * threads + tid, w[i]);
     const auto ask = [&](long long row, uint4 *stage) {
         if (row < p.rows)
 #pragma unroll
@@ -382,6 +381,7 @@ __global__ void __launch_bounds__(kMaxThreads) k_rms_norm_backward_ring(NormBack
             for (int q = 0; q < V; ++q) p.dx[row * words + u * V + q] = o[q];
         }
     }
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     float4 *dst = reinterpret_cast<float4 *>(p.partial + (size_t)blockIdx.x * p.units * 8);
 #pragma unroll
     for (int i = 0; i < kUnits; ++i) {
@@ -397,6 +397,7 @@ __global__ void __launch_bounds__(1024) k_norm_weight(const float4 *partial, int
 {
     __shared__ float4 sums[32][33];
     const int lane = threadIdx.x & 31, slice = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
+    asm volatile("griddepcontrol.wait;" ::: "memory");         // launched while the rows' kernel drains
     float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     if (c < quads)
         for (int i = slice; i < ctas; i += 32) {
@@ -444,10 +445,24 @@ int64_t backward_ctas(int64_t rows, int units)
     return std::min<int64_t>(rows, std::min(8, kMaxThreads / row_threads(units)) * kSms);
 }
 
+// A function's attributes are those of one device: set at its first use there.
+template <int DT, int STAGES>
+cudaError_t allow_ring()
+{
+    constexpr int kDevices = 64;
+    static std::once_flag once[kDevices];
+    static cudaError_t attr[kDevices];
+    int device;
+    const cudaError_t e = cudaGetDevice(&device);
+    if (e != cudaSuccess) return e;
+    if (device >= kDevices) return cudaErrorInvalidDevice;
+    std::call_once(once[device], [&] { attr[device] = cudaFuncSetAttribute(k_rms_norm_backward_ring<DT, STAGES>, cudaFuncAttributeMaxDynamicSharedMemorySize, kRingBytes); });
+    return attr[device];
+}
+
 moe_status check_norm(int32_t dtype, int32_t weight_dtype, int64_t rows, int32_t cols)
 {
-    if (rows < 0 || cols < 8 || cols % 8 != 0 || cols > kMaxCols || !is_dtype(dtype)) return MOE_ERR_INVALID_ARG;
-    if (weight_dtype != dtype && weight_dtype != MOE_DTYPE_F32) return MOE_ERR_INVALID_ARG;
+    if (rows < 0 || cols < 8 || cols % 8 != 0 || cols > kMaxCols || !is_dtype(dtype) || !is_dtype(weight_dtype)) return MOE_ERR_INVALID_ARG;
     return rows > (1ll << 31) - 1 ? MOE_ERR_CAPACITY : MOE_OK;
 }
 
@@ -488,7 +503,7 @@ moe_status moe_rms_norm(const void *x, int64_t x_stride, const void *residual, i
     NormParams p;
     p.x = static_cast<const uint4 *>(x); p.residual = static_cast<const uint4 *>(residual);
     p.x_stride = x_stride * size / 16; p.r_stride = residual_stride * size / 16;
-    p.weight = weight; p.weight_f32 = weight_dtype == MOE_DTYPE_F32; p.eps = eps; p.rows = rows; p.units = cols / 8;
+    p.weight = weight; p.weight_dtype = weight_dtype; p.eps = eps; p.rows = rows; p.units = cols / 8;
     p.h = static_cast<uint4 *>(h); p.y = static_cast<uint4 *>(y); p.rstd = rstd; p.codes = codes; p.scales = scales;
     p.pitch = mx_scale_pitch(cols);
     with_kernel(dtype, p.units, [&](auto dt, auto un, auto warp) {
@@ -529,7 +544,7 @@ moe_status moe_rms_norm_backward(const void *dy, const void *dh, const void *h, 
     }
     NormBackwardParams p;
     p.dy = static_cast<const uint4 *>(dy); p.dh = static_cast<const uint4 *>(dh); p.h = static_cast<const uint4 *>(h);
-    p.rstd = rstd; p.weight = weight; p.weight_f32 = weight_dtype == MOE_DTYPE_F32; p.rows = rows; p.units = cols / 8;
+    p.rstd = rstd; p.weight = weight; p.weight_dtype = weight_dtype; p.rows = rows; p.units = cols / 8;
     p.dx = static_cast<uint4 *>(dx); p.partial = static_cast<float *>(workspace);
     int ctas = (int)backward_ctas(rows, p.units);
     cudaError_t e = cudaSuccess;
@@ -545,20 +560,26 @@ moe_status moe_rms_norm_backward(const void *dy, const void *dh, const void *h, 
             while (per_sm > 1 && kRingBytes / per_sm < 2 * stage) --per_sm;
             const int stages = (int)std::min<size_t>(3, kRingBytes / per_sm / stage);
             ctas = (int)std::min<int64_t>(ctas, per_sm * kSms);
-            const auto launch = [&](auto kernel) {
-                e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kRingBytes);
+            const auto launch = [&](auto n) {
+                e = allow_ring<dt, n>();
                 if (e != cudaSuccess) return;
-                kernel<<<ctas, row_threads(p.units), stages * stage, st>>>(p);
+                k_rms_norm_backward_ring<dt, n><<<ctas, row_threads(p.units), stages * stage, st>>>(p);
                 e = cudaGetLastError();
             };
-            if (stages == 3) launch(k_rms_norm_backward_ring<dt, 3>);
-            else if (stages == 2) launch(k_rms_norm_backward_ring<dt, 2>);
-            else launch(k_rms_norm_backward_ring<dt, 1>);
+            if (stages == 3) launch(std::integral_constant<int, 3>());
+            else if (stages == 2) launch(std::integral_constant<int, 2>());
+            else launch(std::integral_constant<int, 1>());
         }
     });
     if (e != cudaSuccess) return MOE_ERR_CUDA;
-    k_norm_weight<<<(cols / 4 + 31) / 32, 1024, 0, st>>>(static_cast<const float4 *>(workspace), ctas, cols / 4, reinterpret_cast<float4 *>(d_weight));
-    return cudaGetLastError() == cudaSuccess ? MOE_OK : MOE_ERR_CUDA;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((cols / 4 + 31) / 32); cfg.blockDim = dim3(1024); cfg.stream = st;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at; cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, k_norm_weight, static_cast<const float4 *>(workspace), ctas, cols / 4, reinterpret_cast<float4 *>(d_weight)) ==
+                   cudaSuccess ? MOE_OK : MOE_ERR_CUDA;
 }
 
 }  // extern "C"

@@ -162,7 +162,7 @@ def test_norm_arguments(router):
     router_reached = router.reached
     B.rms_norm(x, w, keep=True)
     B.rms_norm(Row((T, H), BF, contiguous=False), Row((H,), F32), x)
-    for bad in ((Row((T, H), torch.int32), w, None), (x, Row((H - 1,), BF), None), (x, Row((H,), torch.float16), None), (x, w, Row((T, H), F32)),
+    for bad in ((Row((T, H), torch.int32), w, None), (x, Row((H - 1,), BF), None), (x, Row((H,), torch.float64), None), (x, w, Row((T, H), F32)),
                 (x, w, Row((T - 1, H), BF)), (x, w, Row((T, H), BF, device=1)), (Row((T, H), BF, device=-1), w, None),
                 (Row((2, T, H), BF, contiguous=False), w, None)):
         with pytest.raises(B.MoeError):
@@ -195,7 +195,7 @@ def _back(dy=A, dh=0, h=A + (1 << 20), rstd=A + (2 << 20), dt=0, rows=4, cols=64
 
 
 @pytest.mark.parametrize("args", [dict(dt=3), dict(dt=-1), dict(rows=-1), dict(cols=0), dict(cols=12), dict(cols=16392, xs=16392), dict(xs=63), dict(xs=68),
-                                  dict(wdt=1), dict(dt=2, wdt=0), dict(eps=-1.0), dict(eps=float("nan")), dict(x=0), dict(w=0), dict(y=0), dict(x=A + 8),
+                                  dict(wdt=3), dict(wdt=-1), dict(eps=-1.0), dict(eps=float("nan")), dict(x=0), dict(w=0), dict(y=0), dict(x=A + 8),
                                   dict(y=A + (2 << 20) + 2), dict(c=A + 8192), dict(s=A + 8192), dict(c=A + 8192, s=A + 16384, cols=40, xs=40),
                                   dict(res=A + 4096), dict(res=A + 4096, h=A + 8192, rs=60), dict(y=A + 496), dict(y=A), dict(rstd=A + 16), dict(h=A + 16),
                                   dict(h=A, xs=128), dict(c=A + 8192, s=A + 8192 + 240), dict(y=A + (1 << 20) - 400), dict(res=A + 4096, h=A + 4096 + 16)])
@@ -203,7 +203,7 @@ def test_norm_is_refused(built, args):
     assert _norm(**args) == BAD
 
 
-@pytest.mark.parametrize("args", [dict(dt=3), dict(cols=12), dict(cols=16392), dict(wdt=1), dict(dy=0), dict(h=0), dict(rstd=0), dict(w=0), dict(dx=0),
+@pytest.mark.parametrize("args", [dict(dt=3), dict(cols=12), dict(cols=16392), dict(wdt=3), dict(dy=0), dict(h=0), dict(rstd=0), dict(w=0), dict(dx=0),
                                   dict(dw=0), dict(ws=0), dict(ws=A + (6 << 20) + 8), dict(dx=A + 16), dict(dx=A + (1 << 20) - 16), dict(dw=A + 64),
                                   dict(dw=A + (4 << 20) + 64), dict(ws=A + (5 << 20)), dict(dx=A + (3 << 20)), dict(rows=0, dw=0)])
 def test_norm_backward_is_refused(built, args):

@@ -33,7 +33,7 @@ SUM = 48 * 2.0 ** -24
 @pytest.mark.parametrize("rows,cols", SIZES)
 def test_forward(rows, cols, dtype):
     half = U.HALF[dtype]
-    for residual, wtype, strided in ((True, dtype, False), (False, torch.float32, True), (True, torch.float32, True)):
+    for residual, wtype, strided in ((True, dtype, False), (False, torch.float32, True), (True, torch.bfloat16, True), (False, torch.float16, False)):
         stride = cols + 24 if strided else None
         x = _rows(rows, cols, dtype, 1, stride)
         res = _rows(rows, cols, dtype, 2, stride) if residual else None
@@ -105,7 +105,7 @@ def test_rows_that_are_not_numbers():
 @pytest.mark.parametrize("rows,cols", SIZES)
 def test_backward(rows, cols, dtype):
     half = U.HALF[dtype]
-    h, w = _rows(rows, cols, dtype, 1), _weight(cols, dtype if rows % 2 else torch.float32)
+    h, w = _rows(rows, cols, dtype, 1), _weight(cols, TYPES[rows % 3])
     h = h.contiguous()
     rstd = torch.rsqrt(h.double().square().mean(1) + 1e-5).float()
     dy, dh = (torch.randn(rows, cols, device="cuda", generator=torch.Generator(device="cuda").manual_seed(s)).to(dtype) for s in (5, 6))
