@@ -454,7 +454,7 @@ template <ExpertOp OP, bool FINE> constexpr int kAccSteps = !FINE ? 1 << 30 : (O
 // 32 features (lanes) x 32 (fp32) or 64 (bf16) columns of a weight gradient, through 4 KB of shared memory: a lane writes
 // its feature's 128 bytes, 16-byte units permuted by the feature, and then eight lanes store the 128 bytes of one feature, so
 // that whole lines leave and nothing waits.  (By TMA stores the box has to be read before it is filled again, and they queue
-// with the loads, which already keep the TMA unit busy: a stage is 256 lines in 512 clocks.)
+// with the loads, which already keep the TMA unit busy: a stage is 256 lines in 512 clocks.  See store_box.)
 template <bool F32>
 __device__ __forceinline__ void store_grad(const KernelParams &p, const Tile &t, int f, int col, const uint4 (&v)[8], unsigned char *plane,
                                            int lane)
@@ -488,12 +488,33 @@ __device__ __forceinline__ void store_grad(const KernelParams &p, const Tile &t,
     __syncwarp();                                              // the plane is free again
 }
 
+// The same for 64 columns in bf16 as one TMA store, from a box of 32 lines of 128 bytes with the 128-byte swizzle; what lies
+// outside the matrix is cut by the store.  For tiles of few stages, whose stores bound them: the TMA unit has time then, and
+// reads the box once where warps would read it and store it (128 slots of 100 rows, 2048 x 4096: 520 us, 585 by the warps; of 511
+// rows: 992 and 933).
+constexpr int kFewSteps = 4;
+__device__ __forceinline__ void store_box(const CUtensorMap *map, int slot, int f, int col, const uint4 (&v)[8], unsigned char *box, int lane)
+{
+    if (lane == 0) bulk_wait_read<0>();                        // the store before has left the box
+    __syncwarp();
+#pragma unroll
+    for (int q = 0; q < 8; ++q) *reinterpret_cast<uint4 *>(box + lane * kLine + ((q ^ (lane & 7)) << 4)) = v[q];
+    fence_async_shared();
+    __syncwarp();
+    if (lane == 0) {
+        asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%1, %2, %3}], [%4];" ::"l"(map), "r"(col), "r"(f),
+                     "r"(slot), "r"(smem_addr(box))
+                     : "memory");
+        bulk_commit();
+    }
+}
+
 // ------------------------------------------------------------------------ kernel
 
 template <ExpertOp OP, int NT, int CG, bool FINE, bool F32>
 __global__ void __launch_bounds__(kThreadsOf<NT, FINE>, 1)
 k_expert_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_big,
-                 const KernelParams p)
+                 const __grid_constant__ CUtensorMap map_y, const KernelParams p)
 {
     // map_a: the M operand (weights, or the left operand of a weight gradient); map_b, map_big: the N operand
     using L = Layout<OP, NT, CG, FINE>;
@@ -667,7 +688,12 @@ k_expert_product(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                                                 pack_bf16(__uint_as_float(w[6]), __uint_as_float(w[7])));
                         }
                     }
-                    store_grad<false>(p, t, f, t.col + c0, box, mine, lane);
+                    if (steps <= kFewSteps) store_box(&map_y, t.slot, f, t.col + c0, box, mine, lane);
+                    else {
+                        if (lane == 0) bulk_wait_read<0>();    // of an earlier tile
+                        __syncwarp();
+                        store_grad<false>(p, t, f, t.col + c0, box, mine, lane);
+                    }
                 }
                 release_acc();
             } else if (kGrad) {
@@ -712,6 +738,7 @@ k_expert_product(const __grid_constant__ CUtensorMap map_a, const __grid_constan
             }
             if (one) next_acc();
         }
+        if (kGrad && !F32 && lane == 0) bulk_wait_all();       // the last stores have left shared memory
     } else {
         if (kSplitRegs<NT, FINE>) asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
         if (warp == kTmaWarp) {
@@ -885,12 +912,16 @@ cudaError_t launch(const ExpertArgs &a, cudaStream_t st)
     if (!encode_fn()) return cudaErrorNotSupported;
     const CUtensorMapDataType bf16 = CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
     const CUtensorMapSwizzle sw = CU_TENSOR_MAP_SWIZZLE_128B;
-    CUtensorMap map_a, map_b, map_big = {};
+    CUtensorMap map_a, map_b, map_big = {}, map_y = {};
     bool ok;
     if (L::kGrad) {
         const cuuint64_t ad[2] = {(cuuint64_t)a.M, (cuuint64_t)a.rows}, as[1] = {2 * (cuuint64_t)a.M};
         const cuuint64_t bd[2] = {(cuuint64_t)a.N, (cuuint64_t)a.rows}, bs[1] = {2 * (cuuint64_t)a.N};
         ok = encode(&map_a, bf16, sw, a.a, 2, ad, as, 64, kStageK) && encode(&map_b, bf16, sw, a.b, 2, bd, bs, 64, kStageK);
+        if (!F32) {
+            const cuuint64_t yd[3] = {(cuuint64_t)a.N, (cuuint64_t)a.M, (cuuint64_t)a.P}, ys[2] = {2 * (cuuint64_t)a.N, 2 * (cuuint64_t)a.N * a.M};
+            ok = ok && encode(&map_y, bf16, sw, a.y, 3, yd, ys, 64, 32);
+        }
     } else {
         const cuuint64_t inner = L::kAAlongK ? a.K : a.N, outer = L::kAAlongK ? a.N : a.K;
         const cuuint64_t wd[3] = {inner, outer, (cuuint64_t)a.P}, ws[2] = {2 * inner, 2 * inner * outer};
@@ -916,7 +947,7 @@ cudaError_t launch(const ExpertArgs &a, cudaStream_t st)
     at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at; cfg.numAttrs = a.pdl ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, kernel, map_a, map_b, map_big, p);
+    return cudaLaunchKernelEx(&cfg, kernel, map_a, map_b, map_big, map_y, p);
 }
 
 // With few rows a slot the weights dominate, and a narrow tile of one CTA leaves shared memory for more stages of them.

@@ -17,6 +17,8 @@ BF, F32, I32, U8 = torch.bfloat16, torch.float32, torch.int32, torch.uint8
 
 
 class Row(Fake):
+    device = None
+
     def stride(self, d):
         return 1 if d else self.shape[-1] + 8
 
@@ -157,7 +159,9 @@ def test_a_step_is_refused_before_its_first_launch(router):
     assert router.reached == []
 
 
-def test_norm_arguments(router):
+def test_norm_arguments(router, monkeypatch):
+    monkeypatch.setattr(torch, "empty_like", lambda t: Row(t.shape, t.dtype))
+    monkeypatch.setattr(torch, "empty", lambda shape, dtype, device: Row((shape,) if isinstance(shape, int) else shape, dtype))
     x, w = Row((T, H), BF), Row((H,), BF)
     router_reached = router.reached
     B.rms_norm(x, w, keep=True)
@@ -173,7 +177,17 @@ def test_norm_arguments(router):
     for field, bad in (("y", Row((T, H), F32)), ("h", Row((T - 1, H), BF)), ("rstd", Row((T,), BF))):
         with pytest.raises(B.MoeError):
             B.rms_norm(x, w, x, out=B.RmsNormOut(**{**vars(out), field: bad}))
-    assert router_reached == ["moe_rms_norm"] * 2
+    args = (x, Row((T, H), BF), Row((T,), F32), Row((H,), F32))
+    B.rms_norm_backward(*args, dh=x)
+    for i, t in enumerate(args):
+        for what, bad in variants(t):
+            if (i, what) != (3, "type"):
+                with pytest.raises((B.MoeError, ValueError)):
+                    B.rms_norm_backward(*args[:i], Row(bad.shape, bad.dtype, bad._device, bad._contiguous), *args[i + 1:])
+    for more in (dict(dh=Row((T, H), F32)), dict(dx=Row((T - 1, H), BF)), dict(d_weight=Row((H,), BF)), dict(d_weight=Row((H + 8,), F32))):
+        with pytest.raises(B.MoeError):
+            B.rms_norm_backward(*args, **more)
+    assert router_reached == ["moe_rms_norm"] * 2 + ["moe_rms_norm_backward"]
 
 
 A = 1 << 30                  # 16-byte aligned; refused calls never look at it
