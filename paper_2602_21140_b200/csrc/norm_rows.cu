@@ -208,21 +208,87 @@ struct NormBackwardParams {
     float *partial;                // [CTAs, cols]
 };
 
-// One row's unit: n = h * rstd, and what the row's mean and d_weight take from it.
-__device__ __forceinline__ void norm_sums(const float (&dy)[8], float (&n)[8], const float (&w)[8], float rstd, float &sum, float (&acc)[8])
+// Two fp32 in one 64-bit register: sm_100 multiplies and adds them with one instruction, rounded as two.
+typedef unsigned long long Pair;
+
+__device__ __forceinline__ Pair pair(float a, float b)
+{
+    Pair r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+
+__device__ __forceinline__ void split(Pair p, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(p)); }
+
+__device__ __forceinline__ Pair mul2(Pair a, Pair b)
+{
+    Pair r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+
+__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c)
+{
+    Pair r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+
+template <int DT>
+__device__ __forceinline__ void to_pairs(const uint4 (&u)[kVec<DT>], Pair (&v)[4])
+{
+    float f[8];
+    to_f32<DT>(u, f);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) v[q] = pair(f[2 * q], f[2 * q + 1]);
+}
+
+__device__ __forceinline__ void weight_pairs(const NormBackwardParams &p, int unit, Pair (&w)[4])
+{
+    float f[8];
+    weight8(p.weight, p.weight_dtype, unit, f);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) w[q] = pair(f[2 * q], f[2 * q + 1]);
+}
+
+// A unit of a row: n = h * rstd, and what the row's mean and d_weight take from it.
+__device__ __forceinline__ void norm_sums(const Pair (&dy)[4], const Pair (&h)[4], const Pair (&w)[4], Pair rstd, Pair &sum, Pair (&acc)[4])
 {
 #pragma unroll
-    for (int q = 0; q < 8; ++q) {
-        n[q] *= rstd;
-        sum += dy[q] * w[q] * n[q];
-        acc[q] += dy[q] * n[q];
+    for (int q = 0; q < 4; ++q) {
+        const Pair n = mul2(h[q], rstd);
+        sum = fma2(mul2(dy[q], w[q]), n, sum);
+        acc[q] = fma2(dy[q], n, acc[q]);
     }
 }
 
-__device__ __forceinline__ void norm_gradient(const float (&dy)[8], const float (&n)[8], const float (&w)[8], float rstd, float mean, float (&d)[8])
+// rstd * (dy * w - n * mean) + past, in the rows' type
+template <int DT>
+__device__ __forceinline__ void norm_gradient(const Pair (&dy)[4], const Pair (&h)[4], const Pair (&w)[4], Pair rstd, Pair minus_mean,
+                                              const Pair (&past)[4], uint4 (&out)[kVec<DT>])
+{
+    float d[8];
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+        split(fma2(fma2(mul2(h[q], rstd), minus_mean, mul2(dy[q], w[q])), rstd, past[q]), d[2 * q], d[2 * q + 1]);
+    from_f32<DT>(d, out);
+}
+
+__device__ __forceinline__ float sum_of(Pair p)
+{
+    float a, b;
+    split(p, a, b);
+    return a + b;
+}
+
+__device__ __forceinline__ void store_sums(float *dst, const Pair (&acc)[4])
 {
 #pragma unroll
-    for (int q = 0; q < 8; ++q) d[q] = rstd * (dy[q] * w[q] - n[q] * mean);
+    for (int q = 0; q < 4; q += 2) {
+        float4 v;
+        split(acc[q], v.x, v.y); split(acc[q + 1], v.z, v.w);
+        reinterpret_cast<float4 *>(dst)[q / 2] = v;
+    }
 }
 
 // Rows of up to 1024 columns: a warp each, eight to a CTA, whose sums of d_weight meet in shared memory.
@@ -232,10 +298,10 @@ __global__ void __launch_bounds__(256) k_rms_norm_backward(NormBackwardParams p)
     constexpr int V = kVec<DT>, kRows = 8;
     extern __shared__ float sums[];                            // [kRows, cols]
     const int lane = threadIdx.x & 31, sub = threadIdx.x >> 5;
-    float acc[UN][8] = {}, w[UN][8] = {};
+    Pair acc[UN][4] = {}, w[UN][4] = {};                       // two +0 are 64 bits of zero
 #pragma unroll
     for (int i = 0; i < UN; ++i)
-        if (i * 32 + lane < p.units) weight8(p.weight, p.weight_dtype, i * 32 + lane, w[i]);
+        if (i * 32 + lane < p.units) weight_pairs(p, i * 32 + lane, w[i]);
     for (long long row = (long long)blockIdx.x * kRows + sub; row < p.rows; row += (long long)gridDim.x * kRows) {
         uint4 a[UN][V], b[UN][V], c[UN][V];
 #pragma unroll
@@ -252,29 +318,25 @@ __global__ void __launch_bounds__(256) k_rms_norm_backward(NormBackwardParams p)
                 }
             }
         }
-        const float rstd = __ldg(p.rstd + row);
-        float sum = 0.0f;
+        const float r = __ldg(p.rstd + row);
+        const Pair rstd = pair(r, r);
+        Pair sum = 0;
 #pragma unroll
         for (int i = 0; i < UN; ++i) {
-            float dy[8], n[8];
-            to_f32<DT>(a[i], dy); to_f32<DT>(b[i], n);
-            norm_sums(dy, n, w[i], rstd, sum, acc[i]);
+            Pair dy[4], h[4];
+            to_pairs<DT>(a[i], dy); to_pairs<DT>(b[i], h);
+            norm_sums(dy, h, w[i], rstd, sum, acc[i]);
         }
-        const float mean = warp_sum(sum) / (float)(p.units * 8);
+        const float mean = warp_sum(sum_of(sum)) / (float)(p.units * 8);
+        const Pair minus_mean = pair(-mean, -mean);
 #pragma unroll
         for (int i = 0; i < UN; ++i) {
             const int u = i * 32 + lane;
             if (u >= p.units) continue;
-            float dy[8], n[8], past[8], d[8];
-            to_f32<DT>(a[i], dy); to_f32<DT>(b[i], n); to_f32<DT>(c[i], past);
-#pragma unroll
-            for (int q = 0; q < 8; ++q) n[q] *= rstd;
-            norm_gradient(dy, n, w[i], rstd, mean, d);
-            if (p.dh)
-#pragma unroll
-                for (int q = 0; q < 8; ++q) d[q] += past[q];
+            Pair dy[4], h[4], past[4];
+            to_pairs<DT>(a[i], dy); to_pairs<DT>(b[i], h); to_pairs<DT>(c[i], past);
             uint4 o[V];
-            from_f32<DT>(d, o);
+            norm_gradient<DT>(dy, h, w[i], rstd, minus_mean, past, o);
 #pragma unroll
             for (int q = 0; q < V; ++q) p.dx[(row * p.units + u) * V + q] = o[q];
         }
@@ -282,13 +344,8 @@ __global__ void __launch_bounds__(256) k_rms_norm_backward(NormBackwardParams p)
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int cols = p.units * 8;
 #pragma unroll
-    for (int i = 0; i < UN; ++i) {
-        const int u = i * 32 + lane;
-        if (u >= p.units) continue;
-        float4 *dst = reinterpret_cast<float4 *>(sums + sub * cols + u * 8);
-        dst[0] = make_float4(acc[i][0], acc[i][1], acc[i][2], acc[i][3]);
-        dst[1] = make_float4(acc[i][4], acc[i][5], acc[i][6], acc[i][7]);
-    }
+    for (int i = 0; i < UN; ++i)
+        if (i * 32 + lane < p.units) store_sums(sums + sub * cols + (i * 32 + lane) * 8, acc[i]);
     __syncthreads();
     for (int c = threadIdx.x; c < cols; c += 256) {
         float s = 0.0f;
@@ -308,10 +365,10 @@ __global__ void __launch_bounds__(kMaxThreads) k_rms_norm_backward_ring(NormBack
     __shared__ float scratch[2 * kMaxThreads / 32];
     extern __shared__ uint4 ring[];                            // [STAGES][dy, h, dh][units * V]
     const int tid = threadIdx.x, threads = blockDim.x, words = p.units * V, tensors = p.dh ? 3 : 2;
-    float acc[kUnits][8] = {}, w[kUnits][8] = {};
+    Pair acc[kUnits][4] = {}, w[kUnits][4] = {};               // two +0 are 64 bits of zero
 #pragma unroll
     for (int i = 0; i < kUnits; ++i)
-        if (i * threads + tid < p.units) weight8(p.weight, p.weight_dtype, i * threads + tid, w[i]);
+        if (i * threads + tid < p.units) weight_pairs(p, i * threads + tid, w[i]);
     const auto ask = [&](long long row, uint4 *stage) {
         if (row < p.rows)
 #pragma unroll
@@ -337,11 +394,12 @@ __global__ void __launch_bounds__(kMaxThreads) k_rms_norm_backward_ring(NormBack
     for (long long row = blockIdx.x; row < p.rows; row += step) {
         ask(row + (STAGES - 1) * step, ring + fill);
         fill = fill == (STAGES - 1) * stage_words ? 0 : fill + stage_words;
-        const float rstd = __ldg(p.rstd + row);
+        const float r = __ldg(p.rstd + row);
+        const Pair rstd = pair(r, r);
         asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 1) : "memory");
         const uint4 *in = ring + take;
         take = take == (STAGES - 1) * stage_words ? 0 : take + stage_words;
-        float sum = 0.0f;
+        Pair sum = 0;
 #pragma unroll
         for (int i = 0; i < kUnits; ++i) {
             const int u = i * threads + tid;
@@ -349,11 +407,12 @@ __global__ void __launch_bounds__(kMaxThreads) k_rms_norm_backward_ring(NormBack
             uint4 a[V], b[V];
 #pragma unroll
             for (int q = 0; q < V; ++q) { a[q] = in[u * V + q]; b[q] = in[words + u * V + q]; }
-            float dy[8], n[8];
-            to_f32<DT>(a, dy); to_f32<DT>(b, n);
-            norm_sums(dy, n, w[i], rstd, sum, acc[i]);
+            Pair dy[4], h[4];
+            to_pairs<DT>(a, dy); to_pairs<DT>(b, h);
+            norm_sums(dy, h, w[i], rstd, sum, acc[i]);
         }
-        const float mean = cta_sum(sum, scratch, turn) / (float)(p.units * 8);
+        const float mean = cta_sum(sum_of(sum), scratch, turn) / (float)(p.units * 8);
+        const Pair minus_mean = pair(-mean, -mean);
         turn ^= 1;
 #pragma unroll
         for (int i = 0; i < kUnits; ++i) {
@@ -361,35 +420,22 @@ __global__ void __launch_bounds__(kMaxThreads) k_rms_norm_backward_ring(NormBack
             if (u >= p.units) continue;
             uint4 a[V], b[V], c[V];
 #pragma unroll
-            for (int q = 0; q < V; ++q) { a[q] = in[u * V + q]; b[q] = in[words + u * V + q]; }
-            float dy[8], n[8], d[8];
-            to_f32<DT>(a, dy); to_f32<DT>(b, n);
-#pragma unroll
-            for (int q = 0; q < 8; ++q) n[q] *= rstd;
-            norm_gradient(dy, n, w[i], rstd, mean, d);
-            if (tensors == 3) {
-                float past[8];
-#pragma unroll
-                for (int q = 0; q < V; ++q) c[q] = in[2 * words + u * V + q];
-                to_f32<DT>(c, past);
-#pragma unroll
-                for (int q = 0; q < 8; ++q) d[q] += past[q];
+            for (int q = 0; q < V; ++q) {
+                a[q] = in[u * V + q]; b[q] = in[words + u * V + q];
+                c[q] = tensors == 3 ? in[2 * words + u * V + q] : make_uint4(0u, 0u, 0u, 0u);
             }
+            Pair dy[4], h[4], past[4];
+            to_pairs<DT>(a, dy); to_pairs<DT>(b, h); to_pairs<DT>(c, past);
             uint4 o[V];
-            from_f32<DT>(d, o);
+            norm_gradient<DT>(dy, h, w[i], rstd, minus_mean, past, o);
 #pragma unroll
             for (int q = 0; q < V; ++q) p.dx[row * words + u * V + q] = o[q];
         }
     }
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    float4 *dst = reinterpret_cast<float4 *>(p.partial + (size_t)blockIdx.x * p.units * 8);
 #pragma unroll
-    for (int i = 0; i < kUnits; ++i) {
-        const int u = i * threads + tid;
-        if (u >= p.units) continue;
-        dst[2 * u] = make_float4(acc[i][0], acc[i][1], acc[i][2], acc[i][3]);
-        dst[2 * u + 1] = make_float4(acc[i][4], acc[i][5], acc[i][6], acc[i][7]);
-    }
+    for (int i = 0; i < kUnits; ++i)
+        if (i * threads + tid < p.units) store_sums(p.partial + ((size_t)blockIdx.x * p.units + i * threads + tid) * 8, acc[i]);
 }
 
 // d_weight: the CTAs' sums added up, 32 of them side by side for each four columns.
