@@ -7,18 +7,26 @@
 //                      dz[2i] = dh u s (1 + g (1 - s)), dz[2i + 1] = dh g s, h = g s u
 //     kWeightGrad      y[p, m, n] = sum_r a[r, m] b[r, n]                       (gradient by the weights)
 //
-// Weights are the M operand and rows the N operand of the first four, so a segment costs its own length rounded up to 16 or 32,
+// Weights are the M operand and rows the N operand of the first four, so a segment costs its own length rounded up to 32,
 // from one token to hundreds, and a tile's accumulator is [128 lanes = features] x [columns = rows] in TMEM.  The weight
 // gradient has the features of a as M, those of b as N, and rows as K.  K goes in stages of 64: a K-major operand (w, a of
 // the products) has 128 bytes of a row, one 128-byte swizzle span; an operand that runs along M or N in memory (w of the
 // transposed products, both of the weight gradient) has 64 lines of 64 features, with the same swizzle.
 //
-// One persistent CTA per SM, or a pair of CTAs per two SMs on one MMA (cta_group::2):
+// A pair of persistent CTAs per two SMs works on one MMA (cta_group::2): each has 128 of a tile's 256 features in its TMEM and
+// shared memory, and half of its rows.  In each CTA
 //   warps 0-7   epilogue, two groups of four (a warp reads one quarter of the TMEM lanes): TMEM -> registers ->
 //               shared memory -> HBM, 32 columns at a time, the groups taking turns
 //   warp 8      TMA loads
 //   warp 9      the MMAs, from one thread
 // The accumulator is double buffered, so the epilogue of a tile runs under the products of the next.
+//
+// What bounds it: with many rows the tensor cores, under the power cap (at 32 slots of 1024 rows, 4096 x 1024, they are busy for
+// 92 % of the gated product and of the gradient by the rows, at 1.39 GHz).  A stage of 64 is 32 KB a CTA in the 512 clocks of its
+// MMAs, all that an SM gets from L2, so nothing else may use that path: prefetching stages into L2 by TMA cost 15 %.  The
+// gradient of the gate (78 %) and the weights' (83 %, in fp32 67 %) move as many bytes of HBM as products, and wait for loads.
+// With few rows HBM: one row for 8 slots of 7168 x 2048 takes 77 + 46 us, whose weights take 72 + 36.  Single CTAs with tiles of
+// 64 rows were as fast up to 64 rows a slot and took up to 2.4 times as long with 200.
 #include "expert_product.h"
 
 #include <algorithm>
@@ -31,6 +39,8 @@ namespace {
 
 using namespace moe;
 
+constexpr int CG = 2;                      // CTAs of a pair, which work on one MMA
+constexpr int NT = 256;                    // rows (N) of a tile at most
 constexpr int kFeat = 128;                 // features (M) per CTA and tile
 constexpr int kStageK = 64;                // elements of K per stage
 constexpr int kLine = 128;                 // bytes of a line of an operand tile: 64 elements
@@ -42,19 +52,11 @@ constexpr int kBand = 8;                   // tiles of rows (or of n) that are w
 
 // ------------------------------------------------------------------ tcgen05 in PTX (the rest: tcgen05.cuh)
 
-template <int CG>
 __device__ __forceinline__ void mma_bf16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool accumulate)
 {
-    if (CG == 1)
-        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-                     "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc),
-                     "r"((uint32_t)accumulate)
-                     : "memory");
-    else
-        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-                     "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc),
-                     "r"((uint32_t)accumulate)
-                     : "memory");
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                 "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)accumulate)
+                 : "memory");
 }
 
 // 32 lanes x 32 columns: v[c] is column c of lane threadIdx.x % 32
@@ -95,7 +97,7 @@ constexpr uint32_t kDescStep = (ALONG_K ? 16 * 2 : 16 * kLine) >> 4;
 
 // Instruction descriptor of kind::f16: fp32 accumulators (1 at bit 4), A and B bf16 (1 at 7 and 10), operands that run
 // along M or N (15 and 16), N / 8 at bit 17, M / 16 at bit 24.
-template <int CG, bool A_ALONG_K, bool B_ALONG_K>
+template <bool A_ALONG_K, bool B_ALONG_K>
 __device__ __forceinline__ uint32_t idesc_bf16(int n)
 {
     return (1u << 4) | (1u << 7) | (1u << 10) | (A_ALONG_K ? 0u : 1u << 15) | (B_ALONG_K ? 0u : 1u << 16) | ((uint32_t)(n >> 3) << 17) |
@@ -108,7 +110,7 @@ struct KernelParams {
     const int32_t *slot_counts, *slot_offsets;
     long long rows;
     int P, N, K, M;
-    int stages;
+    int ring;                      // bytes
     void *y;                       // kGated, kGatedBackward: h
     void *z;
     uint8_t *z_scales;
@@ -136,7 +138,6 @@ __device__ __forceinline__ int segment(const KernelParams &p, int s, int &first)
 
 // A segment of c rows is cut into the fewest tiles of at most NT rows, of equal size (to whole pieces of the
 // epilogue, 32 rows: only a segment's last tile leaves part of one).
-template <int NT>
 __device__ __forceinline__ int row_tiles(int c) { return (c + NT - 1) / NT; }
 
 // Neighbours in the order of the tiles run at the same time and share what they read through L2.  So the nt tiles of
@@ -151,7 +152,7 @@ __device__ __forceinline__ void in_bands(int local, int feats, int nt, int &f, i
     r = band * kBand + local - f * wide;
 }
 
-template <ExpertOp OP, int NT, int CG>
+template <ExpertOp OP>
 __device__ __forceinline__ Tile tile_at(const KernelParams &p, const int *ends, int index)
 {
     Tile t;
@@ -171,7 +172,7 @@ __device__ __forceinline__ Tile tile_at(const KernelParams &p, const int *ends, 
         if (ends[mid] > index) hi = mid; else lo = mid + 1;
     }
     int first;
-    const int c = segment(p, lo, first), nt = row_tiles<NT>(c), size = ((c + nt - 1) / nt + 31) & ~31;
+    const int c = segment(p, lo, first), nt = row_tiles(c), size = ((c + nt - 1) / nt + 31) & ~31;
     in_bands(index - (lo ? ends[lo - 1] : 0), (p.N + CG * kFeat - 1) / (CG * kFeat), nt, f, r);
     t.slot = lo; t.feat = f * (CG * kFeat); t.col = 0;
     t.row = first + r * size;
@@ -180,7 +181,7 @@ __device__ __forceinline__ Tile tile_at(const KernelParams &p, const int *ends, 
 }
 
 // N of a tile's MMAs: its rows (weight gradient: columns) rounded up to what the instruction takes
-template <ExpertOp OP, int NT, int CG>
+template <ExpertOp OP>
 __device__ __forceinline__ int tile_n(const KernelParams &p, const Tile &t)
 {
     const int n = OP == ExpertOp::kWeightGrad ? min(NT, p.N - t.col) : t.rows;
@@ -191,7 +192,7 @@ __device__ __forceinline__ int tile_n(const KernelParams &p, const Tile &t)
 // tile is a chain of dependent reads, so the lanes find the next 32 of them side by side and hand them out one by one.
 // The fields and the verdict are in uniform registers (a warp reduction writes those): what tcgen05 and TMA
 // instructions take comes from uniform registers.
-template <ExpertOp OP, int NT, int CG>
+template <ExpertOp OP>
 struct TileStream {
     const KernelParams &p;
     const int *ends;
@@ -209,7 +210,7 @@ struct TileStream {
                 if (base >= tiles) return false;
                 const int step = (int)gridDim.x / CG, i = base + (int)(threadIdx.x & 31) * step;
                 mine.rows = 0; mine.slot = -1;
-                if (i < tiles) mine = tile_at<OP, NT, CG>(p, ends, i);
+                if (i < tiles) mine = tile_at<OP>(p, ends, i);
                 base += 32 * step;
                 at = 0;
                 __syncwarp();
@@ -228,42 +229,40 @@ struct TileStream {
     }
 };
 
-// Threads of a CTA.  Where the epilogue keeps sums in registers (FINE, a wide tile: 128 of a thread), the two issuing warps are
+// Threads of a CTA.  Where the epilogue keeps sums in registers (FINE: 128 of a thread), the two issuing warps are
 // filled up to a warpgroup, which hands registers to the two of the epilogue: 72 + 2 * 216 = 3 * 168, what the launch gives.
-template <int NT, bool FINE> constexpr bool kSplitRegs = FINE && NT > 64;
-template <int NT, bool FINE> constexpr int kThreadsOf = kSplitRegs<NT, FINE> ? 384 : 32 * (kEpiWarps + 2);
+template <bool FINE> constexpr int kThreadsOf = FINE ? 384 : 32 * (kEpiWarps + 2);
 
-template <ExpertOp OP, int NT, int CG, bool FINE>
+template <ExpertOp OP, bool FINE>
 struct Layout {
-    static constexpr int kThreads = kThreadsOf<NT, FINE>;
+    static constexpr int kThreads = kThreadsOf<FINE>;
     static constexpr bool kGrad = OP == ExpertOp::kWeightGrad;
     static constexpr bool kAAlongK = OP == ExpertOp::kProduct || OP == ExpertOp::kGated;   // see desc_tile
     static constexpr bool kBAlongK = !kGrad;
     static constexpr int kN = NT / CG;                        // rows (or columns) of a tile in this CTA
-    static constexpr int kBTile = kN * kLine;
-    static constexpr int kStage = kATile + kBTile;            // multiples of 1024: swizzle alignment
+    static constexpr int kStage = kATile + kN * kLine;        // multiples of 1024: swizzle alignment
     static constexpr int kEpiWarp = 32 * kLine;               // a plane of 32 x 32 fp32 or 32 x 64 bf16
     static constexpr int kBars = 4 * kMaxStages + 5;
     static constexpr int kEpiOff = 0, kBarOff = kEpiWarps * kEpiWarp;
-    static constexpr int kEndsOff = kBarOff + ((kBars * 8 + 16 + 4 * (kThreads / 32) + 15) & ~15);
+    static constexpr int kEndsOff = kBarOff + ((kBars * 8 + 16 + 8 * (kThreads / 32) + 15) & ~15);
     static constexpr int kSmem = 227 * 1024;
     static size_t fixed(int P) { return (kEndsOff + (kGrad ? 0 : (size_t)P * 4) + 1023) / 1024 * 1024; }
-    static int stages(int P) { return std::min<int>(kMaxStages, (int)((kSmem - 1024 - fixed(P)) / kStage)); }
-    static size_t bytes(int P) { return 1024 + fixed(P) + (size_t)stages(P) * kStage; }
+    static int ring(int P) { return (int)(kSmem - 1024 - fixed(P)) / kStage * kStage; }   // its bytes: whole stages at their largest
+    static size_t bytes(int P) { return 1024 + fixed(P) + (size_t)ring(P); }
 };
 
 // Whether the last of `left` rows of a weight gradient's segment end inside a K = 16 of this stage.
 __device__ __forceinline__ bool has_tail(int left) { return left < kStageK && (left & 15) != 0; }
 
-// Both operands of a stage of a weight gradient, 64 features by 64 rows at a time.
-template <int CG, int N>
+// Both operands of a stage of a weight gradient, 64 features by 64 rows at a time; PEER: `bar` is in the first CTA.
+template <bool PEER>
 __device__ __forceinline__ void load_grad(unsigned char *a, unsigned char *b, const CUtensorMap *map_a, const CUtensorMap *map_b, int feat, int col,
                                           int row, uint32_t bar)
 {
 #pragma unroll
-    for (int q = 0; q < kFeat / 64; ++q) tma_2d<CG>(a + q * kChunk, map_a, feat + q * 64, row, bar);
+    for (int q = 0; q < kFeat / 64; ++q) tma_2d<PEER ? CG : 1>(a + q * kChunk, map_a, feat + q * 64, row, bar);
 #pragma unroll
-    for (int q = 0; q < N / 64; ++q) tma_2d<CG>(b + q * kChunk, map_b, col + q * 64, row, bar);
+    for (int q = 0; q < NT / CG / 64; ++q) tma_2d<PEER ? CG : 1>(b + q * kChunk, map_b, col + q * 64, row, bar);
 }
 
 // The lines of a stage behind a segment, up to a whole K = 16, are made zero in both operands: they hold the next segment's rows
@@ -511,13 +510,13 @@ __device__ __forceinline__ void store_box(const CUtensorMap *map, int slot, int 
 
 // ------------------------------------------------------------------------ kernel
 
-template <ExpertOp OP, int NT, int CG, bool FINE, bool F32>
-__global__ void __launch_bounds__(kThreadsOf<NT, FINE>, 1)
+template <ExpertOp OP, bool FINE, bool F32>
+__global__ void __launch_bounds__(kThreadsOf<FINE>, 1)
 k_expert_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_big,
                  const __grid_constant__ CUtensorMap map_y, const KernelParams p)
 {
     // map_a: the M operand (weights, or the left operand of a weight gradient); map_b, map_big: the N operand
-    using L = Layout<OP, NT, CG, FINE>;
+    using L = Layout<OP, FINE>;
     constexpr bool kGrad = L::kGrad;
     constexpr int kBox = 32;                                   // rows per TMA load of few rows
     extern __shared__ unsigned char raw[];
@@ -528,14 +527,14 @@ k_expert_product(const __grid_constant__ CUtensorMap map_a, const __grid_constan
     uint64_t *acc_full = bars + 4 * kMaxStages, *acc_empty = acc_full + 2, *drained = acc_full + 4;
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(bars + L::kBars);
     volatile int *quit = reinterpret_cast<volatile int *>(tmem_slot + 1);
-    int *warp_sums = reinterpret_cast<int *>(tmem_slot + 4);
+    int *warp_sums = reinterpret_cast<int *>(tmem_slot + 4), *warp_most = warp_sums + L::kThreads / 32;
     int *ends = reinterpret_cast<int *>(base + L::kEndsOff);
     unsigned char *stage = base + ((L::kEndsOff + (kGrad ? 0 : p.P * 4) + 1023) & ~1023);
 
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, stages = p.stages;
-    const int rank = CG == 2 ? (int)cluster_rank() : 0;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int rank = (int)cluster_rank();
     if (tid == 0) {
-        for (int s = 0; s < stages; ++s) {
+        for (int s = 0; s < kMaxStages; ++s) {
             mbar_init(&full[s], 1); mbar_init(&empty[s], 1);
             mbar_init(&tail[s], 1); mbar_init(&peer[s], 1);
         }
@@ -553,7 +552,7 @@ k_expert_product(const __grid_constant__ CUtensorMap map_a, const __grid_constan
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
 
-    int tiles = 0;
+    int tiles = 0, most_rows = 0;                              // most_rows: of the longest segment
     const int feats = ((kGrad ? p.M : p.N) + CG * kFeat - 1) / (CG * kFeat);
     if (kGrad) {
         tiles = p.P * feats * ((p.N + NT - 1) / NT);           // the host has seen that this is an int
@@ -561,13 +560,17 @@ k_expert_product(const __grid_constant__ CUtensorMap map_a, const __grid_constan
     } else {
         // inclusive prefix over the slots of their tile counts
         const int chunk = (p.P + L::kThreads - 1) / L::kThreads, s0 = tid * chunk, s1 = min(p.P, s0 + chunk);
-        int sum = 0;
+        int sum = 0, longest = 0;
 #pragma unroll 1
         for (int s = s0; s < s1; ++s) {
             int first;
-            sum = tiles_sum(sum, feats * row_tiles<NT>(segment(p, s, first)));
+            const int c = segment(p, s, first);
+            longest = max(longest, c);
+            sum = tiles_sum(sum, feats * row_tiles(c));
             ends[s] = sum;
         }
+        longest = __reduce_max_sync(0xffffffffu, longest);
+        if (lane == 0) warp_most[warp] = longest;
         int incl = sum;
 #pragma unroll 1
         for (int off = 1; off < 32; off <<= 1) {
@@ -582,11 +585,12 @@ k_expert_product(const __grid_constant__ CUtensorMap map_a, const __grid_constan
         for (int w = 0; w < warp; ++w) before = tiles_sum(before, warp_sums[w]);
 #pragma unroll 1
         for (int s = s0; s < s1; ++s) ends[s] = tiles_sum(ends[s], before);
+#pragma unroll 1
+        for (int w = 0; w < L::kThreads / 32; ++w) most_rows = max(most_rows, warp_most[w]);
     }
     __syncwarp();
     tc_fence_before();
-    if (CG == 2) cluster_sync();                               // the peer's barriers are set up before anything arrives on them
-    else __syncthreads();
+    cluster_sync();                                            // the peer's barriers are set up before anything arrives on them
     tc_fence_after();
     // All 512 columns belong to this CTA, so they start at 0: a constant in every TMEM address.  (Anything else
     // would be reported and no tile touched.)
@@ -602,11 +606,17 @@ k_expert_product(const __grid_constant__ CUtensorMap map_a, const __grid_constan
         }
     }
     if (!whole) tiles = 0;
+    // Where no segment has more than 64 (128) rows, a stage holds 32 (64) of a CTA's and the ring has room for nine (eight)
+    // stages and not six: the weights bound the kernel then, and more of them are on their way (one row for 8 slots of
+    // 7168 x 2048: gated 97 us instead of 99, down 60 instead of 63).  Weights that run along their features are better off
+    // with six (32 slots of 64 rows, 4096 x 2048: gradient by the rows 184 us, with nine 190).
+    const int stage_bytes = !L::kAAlongK || most_rows > 128 ? L::kStage : kATile + (most_rows > 64 ? 64 : 32) * kLine;
+    const int stages = min(kMaxStages, p.ring / stage_bytes);
 
     // The two issuing warps run their loops with all lanes, so that everything the asynchronous instructions
     // take is uniform over the warp, and issue from one elected lane.
     if (warp < kEpiWarps) {
-        if (kSplitRegs<NT, FINE>) asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+        if (FINE) asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
         // epilogue: TMEM lane = feature of the tile, column = row (weight gradient: column)
         const int group = warp >> 2, quarter = warp & 3;
         unsigned char *mine = epi + warp * L::kEpiWarp;
@@ -615,7 +625,7 @@ k_expert_product(const __grid_constant__ CUtensorMap map_a, const __grid_constan
         unsigned acc_parity = 0;
         Tile t;
         bool ok = true;
-        for (TileStream<OP, NT, CG> stream(p, ends, tiles); ok && stream.next(t);) {
+        for (TileStream<OP> stream(p, ends, tiles); ok && stream.next(t);) {
             const int f = t.feat + rank * kFeat + quarter * 32;
             const int cols = kGrad ? min(NT, p.N - t.col) : t.rows, steps = ((kGrad ? t.rows : p.K) + kStageK - 1) / kStageK;
             const auto wait_acc = [&] {
@@ -740,15 +750,15 @@ k_expert_product(const __grid_constant__ CUtensorMap map_a, const __grid_constan
         }
         if (kGrad && !F32 && lane == 0) bulk_wait_all();       // the last stores have left shared memory
     } else {
-        if (kSplitRegs<NT, FINE>) asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+        if (FINE) asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
         if (warp == kTmaWarp) {
             int issued = 0, s = 0;
             const uint32_t lead = lead_addr<CG>(full);             // the first CTA's barrier counts the bytes of both
             unsigned parity = 1;                                   // a fresh barrier passes the wait for parity 1
             bool ok = true;
             Tile t;
-            for (TileStream<OP, NT, CG> stream(p, ends, tiles); ok && stream.next(t);) {
-                const int n = tile_n<OP, NT, CG>(p, t), half = n / CG;   // rows (or columns) of the tile in this CTA
+            for (TileStream<OP> stream(p, ends, tiles); ok && stream.next(t);) {
+                const int n = tile_n<OP>(p, t), half = n / CG;   // rows (or columns) of the tile in this CTA
                 // each TMA instruction costs its warp some 80 cycles: many rows come in one box, few in boxes of 32
                 const bool big = half > 2 * kBox;
                 const int loads = big ? 1 : (half + kBox - 1) / kBox;
@@ -758,20 +768,20 @@ k_expert_product(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                 for (int k = 0; k < steps; ++k) {
                     ok = __all_sync(0xffffffffu, wait_for(&empty[s], parity, quit, p.spin_limit));
                     if (!ok) break;
-                    unsigned char *a = stage + s * L::kStage, *b = a + kATile;
+                    unsigned char *a = stage + s * stage_bytes, *b = a + kATile;
                     if (elect_one()) {
                         uint32_t bar = lead + s * 8;
                         if (kGrad) {
                             const int r = t.row + k * kStageK, col = t.col + rank * half;
                             // a stage whose last lines have to be made zero: the second CTA counts its own bytes
-                            const bool own = CG == 2 && has_tail(t.rows - k * kStageK);
+                            const bool own = has_tail(t.rows - k * kStageK);
                             if (rank == 0) mbar_expect_tx(&full[s], own ? bytes / CG : bytes);
                             else if (own) {
                                 mbar_expect_tx(&tail[s], bytes / CG);
                                 bar = smem_addr(&tail[s]);
                             }
-                            if (own) load_grad<1, L::kN>(a, b, &map_a, &map_b, feat, col, r, bar);
-                            else load_grad<CG, L::kN>(a, b, &map_a, &map_b, feat, col, r, bar);
+                            if (own) load_grad<false>(a, b, &map_a, &map_b, feat, col, r, bar);
+                            else load_grad<true>(a, b, &map_a, &map_b, feat, col, r, bar);
                         } else {
                             if (rank == 0) mbar_expect_tx(&full[s], bytes);
                             if (L::kAAlongK) tma_3d<CG>(a, &map_a, k * kStageK, feat, t.slot, bar);
@@ -801,8 +811,8 @@ k_expert_product(const __grid_constant__ CUtensorMap map_a, const __grid_constan
             bool ok = true;
             const uint64_t a_desc = desc_tile<L::kAAlongK>(smem_addr(stage)), b_desc = desc_tile<L::kBAlongK>(smem_addr(stage + kATile));
             Tile t;
-            for (TileStream<OP, NT, CG> stream(p, ends, tiles); ok && stream.next(t);) {
-                const uint32_t idesc = idesc_bf16<CG, L::kAAlongK, L::kBAlongK>(tile_n<OP, NT, CG>(p, t));
+            for (TileStream<OP> stream(p, ends, tiles); ok && stream.next(t);) {
+                const uint32_t idesc = idesc_bf16<L::kAAlongK, L::kBAlongK>(tile_n<OP>(p, t));
                 const int steps = ((kGrad ? t.rows : p.K) + kStageK - 1) / kStageK;
                 int k = 0;
                 do {                                               // once for every accumulator that the tile takes
@@ -822,8 +832,8 @@ k_expert_product(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                         const bool next_full = mbar_test_wait(&full[s_next], s_next ? parity : parity ^ 1u);
                         const int left = t.rows - k * kStageK;     // of a weight gradient
                         if (kGrad && has_tail(left)) {
-                            clear_tail(stage + s * L::kStage, L::kStage, left, lane);
-                            if (CG == 2) {                         // so has the second CTA
+                            clear_tail(stage + s * stage_bytes, stage_bytes, left, lane);
+                            {                                      // so has the second CTA
                                 ok = __all_sync(0xffffffffu, wait_for(&peer[s], (peer_parity >> s) & 1u, quit, p.spin_limit));
                                 if (!ok) break;
                                 peer_parity ^= 1u << s;
@@ -831,12 +841,12 @@ k_expert_product(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                         }
                         tc_fence_after();
                         // descriptors count in 16-byte units
-                        const uint64_t a = a_desc + (uint32_t)(s * (L::kStage >> 4)), b = b_desc + (uint32_t)(s * (L::kStage >> 4));
+                        const uint64_t a = a_desc + (uint32_t)(s * (stage_bytes >> 4)), b = b_desc + (uint32_t)(s * (stage_bytes >> 4));
                         if (elect_one()) {
     #pragma unroll
                             for (int q = 0; q < kStageK / 16; ++q)
                                 if (!kGrad || q * 16 < left)
-                                    mma_bf16<CG>(d, a + q * kDescStep<L::kAAlongK>, b + q * kDescStep<L::kBAlongK>, idesc, k > first || q > 0);
+                                    mma_bf16(d, a + q * kDescStep<L::kAAlongK>, b + q * kDescStep<L::kBAlongK>, idesc, k > first || q > 0);
                             mma_commit<CG>(&empty[s]);
                             if (k == last - 1) mma_commit<CG>(&acc_full[buf]);
                         }
@@ -863,14 +873,14 @@ k_expert_product(const __grid_constant__ CUtensorMap map_a, const __grid_constan
             unsigned tail_parity = 0;                              // a bit per stage, of its next use
             bool ok = true;
             Tile t;
-            for (TileStream<OP, NT, CG> stream(p, ends, tiles); ok && stream.next(t);) {
+            for (TileStream<OP> stream(p, ends, tiles); ok && stream.next(t);) {
                 const int steps = (t.rows + kStageK - 1) / kStageK, left = t.rows - (steps - 1) * kStageK;
                 if (steps > 0 && has_tail(left)) {
                     const int at = (s + steps - 1) % stages;
                     ok = __all_sync(0xffffffffu, wait_for(&tail[at], (tail_parity >> at) & 1u, quit, p.spin_limit));
                     if (!ok) break;
                     tail_parity ^= 1u << at;
-                    clear_tail(stage + at * L::kStage, L::kStage, left, lane);
+                    clear_tail(stage + at * stage_bytes, stage_bytes, left, lane);
                     if (lane == 0) mbar_arrive_lead<CG>(&peer[at]);
                 }
                 s = (s + steps) % stages;
@@ -880,11 +890,10 @@ k_expert_product(const __grid_constant__ CUtensorMap map_a, const __grid_constan
 
     __syncwarp();
     tc_fence_before();
-    if (CG == 2) cluster_sync();                               // the pair leaves together: neither arrives on a CTA that is gone
-    else __syncthreads();
+    cluster_sync();                                            // the pair leaves together: neither arrives on a CTA that is gone
     if (tid == 0 && *quit) report_status(p.ctl, kDevTimeout);
     if (warp == kMmaWarp) {
-        if (CG == 2 && rank == 1) {                            // the first CTA's last arrival is on its way here as well
+        if (rank == 1) {                                       // the first CTA's last arrival is on its way here as well
             unsigned long long until = 0;
             drain_wait(drained, 0, until);
             __syncwarp();
@@ -896,12 +905,12 @@ k_expert_product(const __grid_constant__ CUtensorMap map_a, const __grid_constan
 
 // ------------------------------------------------------------------------- host
 
-template <ExpertOp OP, int NT, int CG, bool FINE = false, bool F32 = false>
+template <ExpertOp OP, bool FINE = false, bool F32 = false>
 cudaError_t launch(const ExpertArgs &a, cudaStream_t st)
 {
-    using L = Layout<OP, NT, CG, FINE>;
+    using L = Layout<OP, FINE>;
     static_assert(L::kN % 64 == 0 && NT % 32 == 0 && 2 * NT <= 512, "boxes of the row operand, pieces of the epilogue, TMEM columns");
-    const auto kernel = k_expert_product<OP, NT, CG, FINE, F32>;
+    const auto kernel = k_expert_product<OP, FINE, F32>;
     // a function's attributes are those of one device
     constexpr int kDevices = 64;
     static std::once_flag once[kDevices];
@@ -932,7 +941,7 @@ cudaError_t launch(const ExpertArgs &a, cudaStream_t st)
     if (!ok) return cudaErrorInvalidValue;
     KernelParams p;
     p.slot_counts = a.slot_counts; p.slot_offsets = a.slot_offsets; p.rows = a.rows;
-    p.P = a.P; p.N = a.N; p.K = a.K; p.M = a.M; p.stages = L::stages(a.P);
+    p.P = a.P; p.N = a.N; p.K = a.K; p.M = a.M; p.ring = L::ring(a.P);
     p.y = a.y; p.z = a.z; p.z_scales = a.z_scales; p.dz = static_cast<__nv_bfloat16 *>(a.dz);
     p.add = a.add; p.ctl = a.ctl; p.spin_limit = a.spin_limit;
     // no more CTAs than there can be tiles (the counts are on the device)
@@ -950,17 +959,6 @@ cudaError_t launch(const ExpertArgs &a, cudaStream_t st)
     return cudaLaunchKernelEx(&cfg, kernel, map_a, map_b, map_big, map_y, p);
 }
 
-// With few rows a slot the weights dominate, and a narrow tile of one CTA leaves shared memory for more stages of them.
-// With many rows the products do, and a pair of CTAs halves what each holds of the row operand.  The host knows the
-// buffer's rows but not the counts, so the mean over all slots, empty ones included, decides.
-template <ExpertOp OP>
-cudaError_t launch_for(const ExpertArgs &a, cudaStream_t st)
-{
-    const bool narrow = a.rows <= 64ll * a.P;
-    constexpr bool kFine = OP == ExpertOp::kGated;             // its output does not depend on what is kept
-    return narrow ? launch<OP, 64, 1, kFine>(a, st) : launch<OP, 256, 2, kFine>(a, st);
-}
-
 }  // namespace
 
 namespace moe {
@@ -968,16 +966,16 @@ namespace moe {
 cudaError_t expert_product_launch(const ExpertArgs &a, cudaStream_t st)
 {
     switch (a.op) {
-    case ExpertOp::kProduct: return launch_for<ExpertOp::kProduct>(a, st);
-    case ExpertOp::kGated: return launch_for<ExpertOp::kGated>(a, st);
-    case ExpertOp::kTransposed: return launch_for<ExpertOp::kTransposed>(a, st);
-    case ExpertOp::kGatedBackward: return launch_for<ExpertOp::kGatedBackward>(a, st);
+    case ExpertOp::kProduct: return launch<ExpertOp::kProduct>(a, st);
+    case ExpertOp::kGated: return launch<ExpertOp::kGated, true>(a, st);      // its output does not depend on what is kept
+    case ExpertOp::kTransposed: return launch<ExpertOp::kTransposed>(a, st);
+    case ExpertOp::kGatedBackward: return launch<ExpertOp::kGatedBackward>(a, st);
     case ExpertOp::kWeightGrad:
-        if (!a.f32) return launch<ExpertOp::kWeightGrad, 256, 2>(a, st);
+        if (!a.f32) return launch<ExpertOp::kWeightGrad>(a, st);
         // no segment is longer than the buffer: one accumulator will do, and the kernel without the sums is 5-10 % faster where
         // the stores bound it (24 slots of 45 rows, 4096 x 1024: 82 and 90 us)
-        if (a.rows <= kAccSteps<ExpertOp::kWeightGrad, true> * kStageK) return launch<ExpertOp::kWeightGrad, 256, 2, false, true>(a, st);
-        return launch<ExpertOp::kWeightGrad, 256, 2, true, true>(a, st);
+        if (a.rows <= kAccSteps<ExpertOp::kWeightGrad, true> * kStageK) return launch<ExpertOp::kWeightGrad, false, true>(a, st);
+        return launch<ExpertOp::kWeightGrad, true, true>(a, st);
     }
     return cudaErrorInvalidValue;
 }

@@ -8,8 +8,8 @@ from paper_2602_21140_b200 import binding as B
 
 pytestmark = pytest.mark.gpu
 
-# (rows of each slot, n_in = n_out = H, n_hidden = I).  Up to 64 rows a slot on average single CTAs with tiles of 64 rows
-# run, above pairs with tiles of 256; weight gradients always take pairs.
+# (rows of each slot, n_in = n_out = H, n_hidden = I): tiles have 256 features and at most 256 rows, stages 64 of K; up to 64 and
+# up to 128 rows in the longest segment the ring is another one.
 SIZES = [
     ([1], 8, 16), ([0, 1, 0], 64, 16), ([3, 0, 64, 17, 1], 136, 48), ([65, 20, 5], 264, 144), ([15, 16, 17, 31, 33], 512, 128),
     ([66], 8, 16), ([130, 0, 257], 72, 272), ([700, 3, 129, 1], 1032, 80), ([256, 255, 512, 511], 256, 128), ([2100], 64, 32), ([0, 300, 0], 320, 640),
@@ -218,7 +218,7 @@ def test_no_rows():
     r.close()
 
 
-@pytest.mark.parametrize("counts", [[40, 3, 0, 17], [300, 30, 700, 1]], ids=["single CTAs", "pairs"])
+@pytest.mark.parametrize("counts", [[40, 3, 0, 17], [300, 30, 700, 1]], ids=["short", "long"])
 def test_calls_repeat_bit_for_bit_and_in_graphs(counts):
     """Eagerly, on another stream, and captured and replayed over other counts, between eager calls of the same context."""
     r = U.make_router(4)
@@ -258,24 +258,23 @@ def test_calls_repeat_bit_for_bit_and_in_graphs(counts):
     r.close()
 
 
-def test_pairs_and_single_cta_give_the_same_bits():
-    """The same segments in a buffer with few rows (single CTAs) and in one with many (pairs): a row's sums do not depend on
-    its tile.  What the second CTA of a pair announces to the first one would show here if it came too early."""
+def test_a_rows_sums_do_not_depend_on_its_tile():
+    """The same segments beside one that makes the ring another one, and in a longer buffer."""
     P, H, I = 6, 520, 176
     r = U.make_router(P)
-    counts = [5, 64, 33, 0, 100, 17]
-    n_, off, n = U.layout(counts)
-    extra = 64 * P - n + 200
-    a = U.bf16(n + extra, H, seed=1)
+    short, extra = [5, 64, 33, 0, 17], 700
+    n1, off1, n = U.layout(short + [0])
+    n2, off2, m = U.layout(short + [extra])
+    a = U.bf16(m + 50, H, seed=1)
     gate_up, down = U.bf16(P, 2 * I, H, seed=3, scale=H ** -0.5), U.bf16(P, H, I, seed=4, scale=I ** -0.5)
-    assert n <= 64 * P < n + extra
-    z1, z2 = (torch.empty(m, 2 * I, dtype=torch.bfloat16, device="cuda") for m in (n, n + extra))
-    y1, y2 = (r.expert_ffn(a[:m], n_, off, gate_up, down, z=z) for m, z in ((n, z1), (n + extra, z2)))
-    dz1, h1 = r.expert_gated_backward(a[:n], n_, off, down, z1)
-    dz2, h2 = r.expert_gated_backward(a, n_, off, down, z2)
-    d1, d2 = (r.expert_rows_backward(d, n_, off, gate_up) for d in (dz1, dz2))
+    calls = []
+    for rows, counts, off in ((a[:n], n1, off1), (a, n2, off2)):
+        z = torch.empty(rows.shape[0], 2 * I, dtype=torch.bfloat16, device="cuda")
+        y = r.expert_ffn(rows, counts, off, gate_up, down, z=z)
+        dz, h = r.expert_gated_backward(rows, counts, off, down, z)
+        calls.append((z, y, dz, h, r.expert_rows_backward(dz, counts, off, gate_up)))
     torch.cuda.synchronize()
-    for one, two in ((z1, z2), (y1, y2), (dz1, dz2), (h1, h2), (d1, d2)):
+    for one, two in zip(*calls):
         assert torch.equal(one, two[:n])
     r.close()
 
