@@ -450,6 +450,15 @@ __device__ __forceinline__ void store_gated_backward(const KernelParams &p, cons
 // sum that is rounded to bf16 needs no such care.
 template <ExpertOp OP, bool FINE> constexpr int kAccSteps = !FINE ? 1 << 30 : (OP == ExpertOp::kWeightGrad ? 960 : 1024) / kStageK;
 
+// Stages of each of a tile's accumulators: as few accumulators as that allows, of equal length.
+template <ExpertOp OP, bool FINE>
+__device__ __forceinline__ int acc_steps(int steps)
+{
+    if (!FINE || steps <= kAccSteps<OP, FINE>) return steps;
+    const int n = (steps + kAccSteps<OP, FINE> - 1) / kAccSteps<OP, FINE>;
+    return (steps + n - 1) / n;
+}
+
 // 32 features (lanes) x 32 (fp32) or 64 (bf16) columns of a weight gradient, through 4 KB of shared memory: a lane writes
 // its feature's 128 bytes, 16-byte units permuted by the feature, and then eight lanes store the 128 bytes of one feature, so
 // that whole lines leave and nothing waits.  (By TMA stores the box has to be read before it is filled again, and they queue
@@ -650,7 +659,8 @@ k_expert_product(const __grid_constant__ CUtensorMap map_a, const __grid_constan
 #pragma unroll
                     for (int c = 0; c < 32; ++c) sum[FINE ? n - 1 : 0][c] = sum[FINE ? n : 0][c];
             };
-            const bool one = !FINE || steps <= kAccSteps<OP, FINE>;   // accumulator: its pieces are read as they are stored
+            const int each = acc_steps<OP, FINE>(steps);
+            const bool one = !FINE || each == steps;           // accumulator: its pieces are read as they are stored
             if (!one) {                                        // all of the tile's accumulators added up
                 int k = 0;
 #pragma unroll
@@ -675,7 +685,7 @@ k_expert_product(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                     }
                     release_acc();
                     next_acc();
-                    k += kAccSteps<OP, FINE>;
+                    k += each;
                 } while (k < steps);
                 if (!ok) break;
             } else if (!wait_acc()) {
@@ -814,13 +824,14 @@ k_expert_product(const __grid_constant__ CUtensorMap map_a, const __grid_constan
             for (TileStream<OP> stream(p, ends, tiles); ok && stream.next(t);) {
                 const uint32_t idesc = idesc_bf16<L::kAAlongK, L::kBAlongK>(tile_n<OP>(p, t));
                 const int steps = ((kGrad ? t.rows : p.K) + kStageK - 1) / kStageK;
+                const int each = acc_steps<OP, FINE>(steps);
                 int k = 0;
                 do {                                               // once for every accumulator that the tile takes
                     ok = __all_sync(0xffffffffu, wait_for(&acc_empty[buf], acc_parity, quit, p.spin_limit));
                     if (!ok) break;
                     tc_fence_after();
                     const uint32_t d = tmem + buf * NT;
-                    const int first = k, last = kAccSteps<OP, FINE> < steps - k ? k + kAccSteps<OP, FINE> : steps;
+                    const int first = k, last = min(steps, k + each);
                     bool ready = steps > 0 && __all_sync(0xffffffffu, mbar_test_wait(&full[s], parity));
                     for (; k < last; ++k) {
                         if (!ready) {
