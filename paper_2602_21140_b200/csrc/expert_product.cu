@@ -444,10 +444,10 @@ __device__ __forceinline__ void store_gated_backward(const KernelParams &p, cons
 
 // Stages after which a tile goes on in another accumulator, whose sums the epilogue adds up in registers, where sums are
 // given in fp32 (FINE: the weight gradient) or rounded to 8 bits (the gated product).  The tensor core cuts off what it adds,
-// which shrinks a sum by some 2e-8 of itself with each K = 16: 1.0e-6 after 1024, 1.6e-5 after 16384; with 1024 at a time it stays
-// there.  (960 for the gradients, which then are within 1e-6.  Of the 8-bit codes of sums over K = 7168 in one accumulator, one in 5000 falls the other way.)  512 at a time keep the
-// epilogue, which has to add before it can store, from running under the products: 10-19 % more time for the gated product.  A
-// sum that is rounded to bf16 needs no such care.
+// which shrinks a sum by some 2e-8 of itself with each K = 16: 1.0e-6 after 1024, 1.6e-5 after 16384.  With 960 at a time the
+// gradients are within 1e-6 of their magnitude, and of the 8-bit codes one in 30000 falls the other way (one in 5000 with K = 7168
+// in one accumulator).  512 at a time keep the epilogue, which has to add before it can store, from running under the
+// products: 10-19 % more time for the gated product.  A sum that is rounded to bf16 needs no such care.
 template <ExpertOp OP, bool FINE> constexpr int kAccSteps = !FINE ? 1 << 30 : (OP == ExpertOp::kWeightGrad ? 960 : 1024) / kStageK;
 
 // Stages of each of a tile's accumulators: as few accumulators as that allows, of equal length.
@@ -622,8 +622,6 @@ k_expert_product(const __grid_constant__ CUtensorMap map_a, const __grid_constan
     const int stage_bytes = !L::kAAlongK || most_rows > 128 ? L::kStage : kATile + (most_rows > 64 ? 64 : 32) * kLine;
     const int stages = min(kMaxStages, p.ring / stage_bytes);
 
-    // The two issuing warps run their loops with all lanes, so that everything the asynchronous instructions
-    // take is uniform over the warp, and issue from one elected lane.
     if (warp < kEpiWarps) {
         if (FINE) asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
         // epilogue: TMEM lane = feature of the tile, column = row (weight gradient: column)
@@ -727,7 +725,7 @@ k_expert_product(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                     }
                     uint4 box[8];
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) 
+                    for (int i = 0; i < 8; ++i)
                         box[i] = steps > 0 ? make_uint4(sum[0][4 * i], sum[0][4 * i + 1], sum[0][4 * i + 2], sum[0][4 * i + 3]) : make_uint4(0u, 0u, 0u, 0u);
                     store_grad<true>(p, t, f, t.col + c0, box, mine, lane);
                     if (!one) next_piece();
@@ -760,6 +758,8 @@ k_expert_product(const __grid_constant__ CUtensorMap map_a, const __grid_constan
         }
         if (kGrad && !F32 && lane == 0) bulk_wait_all();       // the last stores have left shared memory
     } else {
+        // The two issuing warps run their loops with all lanes, so that everything the asynchronous instructions
+        // take is uniform over the warp, and issue from one elected lane.
         if (FINE) asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
         if (warp == kTmaWarp) {
             int issued = 0, s = 0;
@@ -796,7 +796,7 @@ k_expert_product(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                             if (rank == 0) mbar_expect_tx(&full[s], bytes);
                             if (L::kAAlongK) tma_3d<CG>(a, &map_a, k * kStageK, feat, t.slot, bar);
                             else {
-    #pragma unroll
+#pragma unroll
                                 for (int q = 0; q < kFeat / 64; ++q) tma_3d<CG>(a + q * kChunk, &map_a, feat + q * 64, k * kStageK, t.slot, bar);
                             }
                             if (big) tma_2d<CG>(b, &map_big, k * kStageK, t.row + rank * half, bar);
@@ -844,17 +844,16 @@ k_expert_product(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                         const int left = t.rows - k * kStageK;     // of a weight gradient
                         if (kGrad && has_tail(left)) {
                             clear_tail(stage + s * stage_bytes, stage_bytes, left, lane);
-                            {                                      // so has the second CTA
-                                ok = __all_sync(0xffffffffu, wait_for(&peer[s], (peer_parity >> s) & 1u, quit, p.spin_limit));
-                                if (!ok) break;
-                                peer_parity ^= 1u << s;
-                            }
+                            // so has the second CTA
+                            ok = __all_sync(0xffffffffu, wait_for(&peer[s], (peer_parity >> s) & 1u, quit, p.spin_limit));
+                            if (!ok) break;
+                            peer_parity ^= 1u << s;
                         }
                         tc_fence_after();
                         // descriptors count in 16-byte units
                         const uint64_t a = a_desc + (uint32_t)(s * (stage_bytes >> 4)), b = b_desc + (uint32_t)(s * (stage_bytes >> 4));
                         if (elect_one()) {
-    #pragma unroll
+#pragma unroll
                             for (int q = 0; q < kStageK / 16; ++q)
                                 if (!kGrad || q * 16 < left)
                                     mma_bf16(d, a + q * kDescStep<L::kAAlongK>, b + q * kDescStep<L::kBAlongK>, idesc, k > first || q > 0);
