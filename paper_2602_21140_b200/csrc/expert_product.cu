@@ -442,20 +442,21 @@ __device__ __forceinline__ void store_gated_backward(const KernelParams &p, cons
     }
 }
 
-// Stages after which a tile goes on in another accumulator, whose sums the epilogue adds up in registers, where sums are
-// given in fp32 (FINE: the weight gradient) or rounded to 8 bits (the gated product).  The tensor core cuts off what it adds,
-// which shrinks a sum by some 2e-8 of itself with each K = 16: 1.0e-6 after 1024, 1.6e-5 after 16384.  With 960 at a time the
-// gradients are within 1e-6 of their magnitude, and of the 8-bit codes one in 30000 falls the other way (one in 5000 with K = 7168
-// in one accumulator).  512 at a time keep the epilogue, which has to add before it can store, from running under the
-// products: 10-19 % more time for the gated product.  A sum that is rounded to bf16 needs no such care.
-template <ExpertOp OP, bool FINE> constexpr int kAccSteps = !FINE ? 1 << 30 : (OP == ExpertOp::kWeightGrad ? 960 : 1024) / kStageK;
-
-// Stages of each of a tile's accumulators: as few accumulators as that allows, of equal length.
+// Stages of each of a tile's accumulators.  Where sums are given in fp32 (FINE: the weight gradient) or rounded to 8 bits (the
+// gated product), a long sum goes on in another accumulator, and the epilogue adds them up in registers: the tensor core cuts
+// off what it adds, which shrinks a sum by some 2e-8 of itself with each K = 16, 1.0e-6 after 1024 and 1.6e-5 after 16384.  With
+// 960 at a time fp32 gradients are within 1e-6 of their magnitude.  With 1024 at a time one in 25000 of the 8-bit codes falls the
+// other way, whatever the length (one in 5000 with K = 7168 in one accumulator; one in 33000 with a chain of fp32 additions, and
+// one in 100000 with K = 1024).  Shorter pieces keep the epilogue, which has to add before it can store, from running under
+// the products: two and three for K of 1024 and 2048 take 16-21 % more time, 512 throughout 10-19 %.  A sum that is rounded to
+// bf16 needs no such care.
+constexpr int kGradSteps = 960 / kStageK;
 template <ExpertOp OP, bool FINE>
 __device__ __forceinline__ int acc_steps(int steps)
 {
-    if (!FINE || steps <= kAccSteps<OP, FINE>) return steps;
-    const int n = (steps + kAccSteps<OP, FINE> - 1) / kAccSteps<OP, FINE>;
+    if (!FINE) return steps;
+    constexpr int kMost = OP == ExpertOp::kWeightGrad ? kGradSteps : 1024 / kStageK;
+    const int n = max(1, (steps + kMost - 1) / kMost);         // as few pieces as that allows, of equal length
     return (steps + n - 1) / n;
 }
 
@@ -984,7 +985,7 @@ cudaError_t expert_product_launch(const ExpertArgs &a, cudaStream_t st)
         if (!a.f32) return launch<ExpertOp::kWeightGrad>(a, st);
         // no segment is longer than the buffer: one accumulator will do, and the kernel without the sums is 5-10 % faster where
         // the stores bound it (24 slots of 45 rows, 4096 x 1024: 82 and 90 us)
-        if (a.rows <= kAccSteps<ExpertOp::kWeightGrad, true> * kStageK) return launch<ExpertOp::kWeightGrad, false, true>(a, st);
+        if (a.rows <= kGradSteps * kStageK) return launch<ExpertOp::kWeightGrad, false, true>(a, st);
         return launch<ExpertOp::kWeightGrad, true, true>(a, st);
     }
     return cudaErrorInvalidValue;
