@@ -1000,6 +1000,8 @@ class MoeRouter:
 
     @staticmethod
     def _kept_ok(z, n: int, cols: int, dev: int) -> bool:
+        if z is None:
+            return False
         return _is_mx8(z, dev, (n, cols)) if isinstance(z, Mx8Rows) else _is_dense(z, torch.bfloat16, (n, cols), dev)
 
     @staticmethod

@@ -636,8 +636,10 @@ k_expert_product(const __grid_constant__ CUtensorMap map_a, const __grid_constan
         for (TileStream<OP> stream(p, ends, tiles); ok && stream.next(t);) {
             const int f = t.feat + rank * kFeat + quarter * 32;
             const int cols = kGrad ? min(NT, p.N - t.col) : t.rows, steps = ((kGrad ? t.rows : p.K) + kStageK - 1) / kStageK;
+            const int each = acc_steps<OP, FINE>(steps);
             const auto wait_acc = [&] {
-                ok = __all_sync(0xffffffffu, wait_for(&acc_full[buf], acc_parity, quit, p.spin_limit));
+                // a stage takes 512 clocks, a poll 20 or more: a long sum is no reason to give up
+                ok = __all_sync(0xffffffffu, wait_for(&acc_full[buf], acc_parity, quit, p.spin_limit + 64u * each));
                 tc_fence_after();
                 return ok;
             };
@@ -658,7 +660,6 @@ k_expert_product(const __grid_constant__ CUtensorMap map_a, const __grid_constan
 #pragma unroll
                     for (int c = 0; c < 32; ++c) sum[FINE ? n - 1 : 0][c] = sum[FINE ? n : 0][c];
             };
-            const int each = acc_steps<OP, FINE>(steps);
             const bool one = !FINE || each == steps;           // accumulator: its pieces are read as they are stored
             if (!one) {                                        // all of the tile's accumulators added up
                 int k = 0;

@@ -320,6 +320,63 @@ def test_two_contexts_at_once():
         r.close()
 
 
+def test_thousands_of_slots_and_wide_matrices():
+    """As many slots as a context takes at 512 experts, few of them with rows, where their table takes a stage's place; and more
+    features than a wave has tiles."""
+    P, H, I = 2000, 72, 48
+    r = B.MoeRouter(B.make_config(512, 1, H, 16, P // 8, 8, 8), [p % 512 if p < 2000 else -1 for p in range(P)], None, [1.0] * P)
+    counts = [0] * P
+    for p, n in ((0, 3), (7, 300), (1023, 1), (1024, 65), (1999, 40)):
+        counts[p] = n
+    n_, off, n = U.layout(counts)
+    a, gate_up, down = U.bf16(n, H, seed=1), U.bf16(P, 2 * I, H, seed=2, scale=H ** -0.5), U.bf16(P, H, I, seed=3, scale=I ** -0.5)
+    z = torch.empty(n, 2 * I, dtype=torch.bfloat16, device="cuda")
+    y = r.expert_ffn(a, n_, off, gate_up, down, z=z)
+    d_rows, d_gate_up, d_down = r.expert_ffn_backward(a, a, n_, off, gate_up, down, z, grad_dtype=torch.float32)
+    torch.cuda.synchronize()
+    assert r.device_status() == 0
+    few = U.make_router(5)
+    at = torch.tensor([0, 7, 1023, 1024, 1999], device="cuda")
+    args = (n_[at].contiguous(), off[at].contiguous())
+    y2 = few.expert_ffn(a, *args, gate_up[at].contiguous(), down[at].contiguous())
+    want = few.expert_ffn_backward(a, a, *args, gate_up[at].contiguous(), down[at].contiguous(), z, grad_dtype=torch.float32)
+    assert torch.equal(y, y2) and torch.equal(d_rows, want[0]) and torch.equal(d_gate_up[at], want[1]) and torch.equal(d_down[at], want[2])
+    rest = torch.ones(P, dtype=torch.bool, device="cuda")
+    rest[at] = False
+    assert not d_gate_up[rest].any() and not d_down[rest].any()
+    few.close(); r.close()
+    r = U.make_router(1)
+    n_, off, n = U.layout([130])
+    a, w = U.bf16(n, 40, seed=1), U.bf16(1, 40_008, 40, seed=2)
+    y = r.expert_product(a, n_, off, w)
+    back = r.expert_rows_backward(y, n_, off, w)
+    dw = r.expert_weight_backward(y, a, n_, off)
+    torch.cuda.synchronize()
+    x, m, t = a.double(), w[0].double(), y.double()
+    U.within(y, x @ m.T, U.sum_bound(40, x.abs() @ m.abs().T) * 1.01 + 2.0 ** -8 * (x @ m.T).abs())
+    U.within(back, t @ m, U.sum_bound(40_008, t.abs() @ m.abs()) * 1.01 + 2.0 ** -8 * (t @ m).abs())
+    U.within(dw[0], t.T @ x, U.sum_bound(130, t.abs().T @ x.abs()) * 1.01 + 2.0 ** -8 * (t.T @ x).abs())
+    assert r.device_status() == 0
+    r.close()
+
+
+def test_a_long_sum_is_no_reason_to_give_up():
+    """8 million rows in one segment: a tile takes longer than most steps, and the waits for it are counted in polls."""
+    r = U.make_router(1)
+    n_, off, n = U.layout([8_000_001])
+    a, dy = (torch.ones(n, 8, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    dy[:, 3] = 0
+    for dtype in (torch.float32, torch.bfloat16):
+        dw = r.expert_weight_backward(dy, a, n_, off, dtype=dtype)[0].double()
+        torch.cuda.synchronize()
+        assert r.device_status() == 0 and not dw[3].any()
+        # whole numbers below 2^24: nothing is cut off
+        assert ((dw[:3] - 8_000_001).abs() <= U.HALF[dtype] * 8_000_001).all() and (dw[4:] == dw[0, 0]).all()
+    r.close()
+    del a, dy
+    torch.cuda.empty_cache()
+
+
 def test_offsets_past_32_bits():
     """A segment at the end of row buffers of 5 GB, and a slot at the end of 9 GB of matrices."""
     H, I, n = 4096, 2056, 600_000
