@@ -714,9 +714,10 @@ def rms_norm_backward(dy: torch.Tensor, h: torch.Tensor, rstd: torch.Tensor, wei
     n = dy.numel() // cols
     dx = torch.empty_like(dy) if dx is None else dx
     d_weight = torch.empty(cols, dtype=torch.float32, device=dy.device) if d_weight is None else d_weight
-    _require(all(_is_dense(t, dtype, shape, index) for t in ((dy, h, dx) if dh is None else (dy, h, dx, dh)))
-             and _is_dense(rstd, torch.float32, shape[:-1], index) and weight.dtype in _DTYPE_CODE
-             and _is_dense(weight, weight.dtype, (cols,), index) and _is_dense(d_weight, torch.float32, (cols,), index), "rms_norm_backward")
+    _require(dy.is_contiguous() and _is_dense(h, dtype, shape, index) and _is_dense(dx, dtype, shape, index)
+             and (dh is None or _is_dense(dh, dtype, shape, index)) and _is_dense(rstd, torch.float32, shape[:-1], index)
+             and weight.dtype in _DTYPE_CODE and _is_dense(weight, weight.dtype, (cols,), index)
+             and _is_dense(d_weight, torch.float32, (cols,), index), "rms_norm_backward")
     ws = torch.empty(_norm_workspace(n, cols), dtype=torch.uint8, device=dy.device)
     st = _on_device(index, moe_rms_norm_backward, dy.data_ptr(), 0 if dh is None else dh.data_ptr(), h.data_ptr(), rstd.data_ptr(), code, n,
                     cols, weight.data_ptr(), _DTYPE_CODE[weight.dtype], dx.data_ptr(), d_weight.data_ptr(), ws.data_ptr(), ws.numel(),
