@@ -341,9 +341,9 @@ moe_status moe_mx_dequantize(const uint8_t *codes, const uint8_t *scales, int64_
  * A block's scale is the smallest power of two, at least 2^-127, under which its largest magnitude is at most 448, 255 for a block
  * with a NaN or an infinity; elements are rounded to the nearest code, ties to even.
  *
- * moe_mx8_dequantize — the values that 8-bit rows stand for, as moe_mx_dequantize.
+ * moe_kept_dequantize — the values that 8-bit rows stand for, as moe_mx_dequantize.
  */
-moe_status moe_mx8_dequantize(const uint8_t *codes, const uint8_t *scales, int64_t rows, int32_t cols, void *y, int32_t dtype,
+moe_status moe_kept_dequantize(const uint8_t *codes, const uint8_t *scales, int64_t rows, int32_t cols, void *y, int32_t dtype,
                               int64_t row_stride, void *cuda_stream);
 
 /*
@@ -485,7 +485,7 @@ moe_status moe_expert_product(moe_ctx *ctx, const void *a, int64_t rows, const i
  *   w [P, 2 * n_hidden, n_in]: row 2i of a slot's matrix is the gate of feature i, row 2i + 1 its up-projection
  *   h [rows, n_hidden] bf16 out
  *   z, z_scales: what moe_expert_gated_backward needs.  Both NULL: nothing is kept.  z alone: [rows, 2 * n_hidden] bf16.
- *     Both: 8-bit rows (moe_mx8_dequantize), codes [rows, 2 * n_hidden] and scales [rows, moe_mx_scale_pitch(2 * n_hidden)];
+ *     Both: 8-bit rows (moe_kept_dequantize), codes [rows, 2 * n_hidden] and scales [rows, moe_mx_scale_pitch(2 * n_hidden)];
  *     the padding of the scales is not written
  */
 moe_status moe_expert_gated(moe_ctx *ctx, const void *a, int64_t rows, const int32_t *slot_counts, const int32_t *slot_offsets,

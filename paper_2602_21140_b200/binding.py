@@ -53,7 +53,7 @@ EXPORTED_SYMBOLS = (
     "moe_mx_scale_pitch", "moe_mx_quantize", "moe_mx_dequantize", "moe_mx_dispatch", "moe_mx_expert_product",
     "moe_mx_expert_gated", "moe_combine_backward", "moe_dispatch_backward",
     "moe_expert_product", "moe_expert_gated", "moe_expert_rows_backward", "moe_expert_gated_backward", "moe_expert_weight_backward",
-    "moe_mx8_dequantize", "moe_rms_norm", "moe_rms_norm_backward", "moe_rms_norm_backward_workspace", "moe_redispatch",
+    "moe_kept_dequantize", "moe_rms_norm", "moe_rms_norm_backward", "moe_rms_norm_backward_workspace", "moe_redispatch",
 )
 
 
@@ -171,8 +171,8 @@ def _lib():
         lib.moe_expert_gated_backward.argtypes = [vp, vp, i64, vp, vp, vp, i32, i32, vp, vp, vp, vp, vp]
         lib.moe_expert_weight_backward.restype = ctypes.c_int
         lib.moe_expert_weight_backward.argtypes = [vp, vp, vp, i64, vp, vp, i32, i32, vp, i32, i32, vp]
-        lib.moe_mx8_dequantize.restype = ctypes.c_int
-        lib.moe_mx8_dequantize.argtypes = [vp, vp, i64, i32, vp, i32, i64, vp]
+        lib.moe_kept_dequantize.restype = ctypes.c_int
+        lib.moe_kept_dequantize.argtypes = [vp, vp, i64, i32, vp, i32, i64, vp]
         lib.moe_rms_norm.restype = ctypes.c_int
         lib.moe_rms_norm.argtypes = [vp, i64, vp, i64, i32, i64, i32, vp, i32, ctypes.c_float, vp, vp, vp, vp, vp, vp]
         lib.moe_rms_norm_backward_workspace.restype = ctypes.c_size_t
@@ -411,9 +411,9 @@ def moe_dispatch_backward(ctx, logits_ptr: int, d_send_buf_ptr: int, d_weights_p
                                         d_logits_ptr or None, cuda_stream)
 
 
-def moe_mx8_dequantize(codes_ptr: int, scales_ptr: int, rows: int, cols: int, y_ptr: int, dtype: int, row_stride: int,
+def moe_kept_dequantize(codes_ptr: int, scales_ptr: int, rows: int, cols: int, y_ptr: int, dtype: int, row_stride: int,
                        cuda_stream: int = 0) -> int:
-    return _lib().moe_mx8_dequantize(codes_ptr, scales_ptr, rows, cols, y_ptr, dtype, row_stride, cuda_stream)
+    return _lib().moe_kept_dequantize(codes_ptr, scales_ptr, rows, cols, y_ptr, dtype, row_stride, cuda_stream)
 
 
 def moe_rms_norm(x_ptr: int, x_stride: int, residual_ptr: int, residual_stride: int, dtype: int, rows: int, cols: int, weight_ptr: int,
@@ -646,10 +646,10 @@ def mx8_dequantize(m: Mx8Rows, dtype: torch.dtype = torch.bfloat16, out: torch.T
         _require(out.shape == shape and out.dtype is dtype and out.is_cuda and out.get_device() == index
                  and (flat or (out.dim() == 2 and out.stride(1) == 1)), "mx8_dequantize")
         stride = cols if flat else out.stride(0)
-    st = _on_device(index, moe_mx8_dequantize, m.codes.data_ptr(), m.scales.data_ptr(), out.numel() // cols, cols, out.data_ptr(),
+    st = _on_device(index, moe_kept_dequantize, m.codes.data_ptr(), m.scales.data_ptr(), out.numel() // cols, cols, out.data_ptr(),
                     _DTYPE_CODE[dtype], stride, _raw_stream(index))
     if st != MOE_OK:
-        raise MoeError(st, "moe_mx8_dequantize")
+        raise MoeError(st, "moe_kept_dequantize")
     return out
 
 

@@ -1,4 +1,4 @@
-// moe_mx_quantize / moe_mx_dequantize: rows to the microscaled 4-bit format and back; moe_mx8_dequantize: back from 8 bits.
+// moe_mx_quantize / moe_mx_dequantize: rows to the microscaled 4-bit format and back; moe_kept_dequantize: back from 8 bits.
 //
 // Both are one pass over the data and bound by HBM: n elements of `size` bytes are read (written)
 // once and n * 17/32 bytes written (read).  A thread owns eight consecutive elements (one 16-byte
@@ -280,7 +280,7 @@ moe_status moe_mx_dequantize(const uint8_t *codes, const uint8_t *scales, int64_
     return dequantize<4>(codes, scales, rows, cols, y, dtype, row_stride, cuda_stream);
 }
 
-moe_status moe_mx8_dequantize(const uint8_t *codes, const uint8_t *scales, int64_t rows, int32_t cols, void *y, int32_t dtype,
+moe_status moe_kept_dequantize(const uint8_t *codes, const uint8_t *scales, int64_t rows, int32_t cols, void *y, int32_t dtype,
                               int64_t row_stride, void *cuda_stream)
 {
     return dequantize<8>(codes, scales, rows, cols, y, dtype, row_stride, cuda_stream);

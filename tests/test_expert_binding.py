@@ -246,7 +246,7 @@ def test_context_calls_without_a_context(built):
     assert B.moe_redispatch(None, A, A, 1, A) == BAD
     for args, status in (((A, A, 1, 40, A, 0, 40), BAD), ((A, A, 1, 32, A + 2, 0, 32), BAD), ((A, A, 1, 32, A + 16, 0, 32), BAD), ((A, A, 0, 32, 0, 0, 32), OK),
                          ((A, A + 4096, 1 << 40, 32, A, 0, 32), CAP)):
-        assert B.moe_mx8_dequantize(*args) == status
+        assert B.moe_kept_dequantize(*args) == status
 
 
 def test_every_other_wait_gives_up():
