@@ -559,6 +559,10 @@ k_expert_product(const __grid_constant__ CUtensorMap map_a, const __grid_constan
     // hints while the previous kernel drains: its weights have pushed these out of L2 (a hint returns nothing stale)
     if (tid * 32 < p.P) { prefetch_l2(p.slot_counts + tid * 32); prefetch_l2(p.slot_offsets + tid * 32); }
     if (warp == kMmaWarp) tmem_alloc<CG>(tmem_slot, 512);
+    __syncwarp();
+    tc_fence_before();
+    cluster_sync();                                            // the peer's barriers are set up before anything arrives on them
+    tc_fence_after();
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
 
@@ -566,7 +570,6 @@ k_expert_product(const __grid_constant__ CUtensorMap map_a, const __grid_constan
     const int feats = ((kGrad ? p.M : p.N) + CG * kFeat - 1) / (CG * kFeat);
     if (kGrad) {
         tiles = p.P * feats * ((p.N + NT - 1) / NT);           // the host has seen that this is an int
-        __syncthreads();
     } else {
         // inclusive prefix over the slots of their tile counts
         const int chunk = (p.P + L::kThreads - 1) / L::kThreads, s0 = tid * chunk, s1 = min(p.P, s0 + chunk);
@@ -591,17 +594,15 @@ k_expert_product(const __grid_constant__ CUtensorMap map_a, const __grid_constan
         int before = __shfl_up_sync(0xffffffffu, incl, 1);
         if (lane == 0) before = 0;
         __syncthreads();
-#pragma unroll 1
-        for (int w = 0; w < warp; ++w) before = tiles_sum(before, warp_sums[w]);
+        int others = lane < warp ? warp_sums[lane] : 0;        // of the warps before
+#pragma unroll
+        for (int off = 1; off < 16; off <<= 1) others = tiles_sum(others, __shfl_xor_sync(0xffffffffu, others, off));
+        before = tiles_sum(before, __shfl_sync(0xffffffffu, others, 0));
+        most_rows = __reduce_max_sync(0xffffffffu, lane < L::kThreads / 32 ? warp_most[lane] : 0);
 #pragma unroll 1
         for (int s = s0; s < s1; ++s) ends[s] = tiles_sum(ends[s], before);
-#pragma unroll 1
-        for (int w = 0; w < L::kThreads / 32; ++w) most_rows = max(most_rows, warp_most[w]);
+        __syncthreads();
     }
-    __syncwarp();
-    tc_fence_before();
-    cluster_sync();                                            // the peer's barriers are set up before anything arrives on them
-    tc_fence_after();
     // All 512 columns belong to this CTA, so they start at 0: a constant in every TMEM address.  (Anything else
     // would be reported and no tile touched.)
     constexpr uint32_t tmem = 0;
