@@ -438,21 +438,27 @@ __global__ void __launch_bounds__(kMaxThreads) k_rms_norm_backward_ring(NormBack
         if (i * threads + tid < p.units) store_sums(p.partial + ((size_t)blockIdx.x * p.units + i * threads + tid) * 8, acc[i]);
 }
 
-// d_weight: the CTAs' sums added up, 32 of them side by side for each four columns.
+// d_weight: the CTAs' sums added up, 64 of them side by side for each four columns (two in a warp, whose loads are lines).
+constexpr int kWeightQuads = 16;           // of a CTA
 __global__ void __launch_bounds__(1024) k_norm_weight(const float4 *partial, int ctas, int quads, float4 *d_weight)
 {
-    __shared__ float4 sums[32][33];
-    const int lane = threadIdx.x & 31, slice = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
+    __shared__ float4 sums[32][kWeightQuads];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x * kWeightQuads + (lane & 15);
     asm volatile("griddepcontrol.wait;" ::: "memory");         // launched while the rows' kernel drains
     float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    if (c < quads)
-        for (int i = slice; i < ctas; i += 32) {
+    if (c < quads) {
+#pragma unroll 4
+        for (int i = 2 * warp + (lane >> 4); i < ctas; i += 64) {
             const float4 v = __ldcg(partial + (size_t)i * quads + c);
             s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
         }
-    sums[slice][lane] = s;
+    }
+    s.x += __shfl_down_sync(0xffffffffu, s.x, 16); s.y += __shfl_down_sync(0xffffffffu, s.y, 16);
+    s.z += __shfl_down_sync(0xffffffffu, s.z, 16); s.w += __shfl_down_sync(0xffffffffu, s.w, 16);
+    if (lane < 16) sums[warp][lane] = s;
     __syncthreads();
-    if (slice != 0 || c >= quads) return;
+    if (threadIdx.x >= kWeightQuads || c >= quads) return;
+#pragma unroll 8
     for (int i = 1; i < 32; ++i) {
         const float4 v = sums[i][lane];
         s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
@@ -488,7 +494,9 @@ int row_threads(int units) { return (units + 32 * kUnits - 1) / (32 * kUnits) * 
 int64_t backward_ctas(int64_t rows, int units)
 {
     if (units <= 32 * kUnits) return std::min<int64_t>((rows + 7) / 8, 2 * kSms);
-    return std::min<int64_t>(rows, std::min(8, kMaxThreads / row_threads(units)) * kSms);
+    // but not for fewer than four rows where one CTA an SM has as many: their sums are written and read again
+    const int64_t most = std::min(8, kMaxThreads / row_threads(units)) * kSms, few = std::max(std::min<int64_t>(rows, kSms), (rows + 3) / 4);
+    return std::min(most, few);
 }
 
 // A function's attributes are those of one device: set at its first use there.
@@ -619,7 +627,7 @@ moe_status moe_rms_norm_backward(const void *dy, const void *dh, const void *h, 
     });
     if (e != cudaSuccess) return MOE_ERR_CUDA;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((cols / 4 + 31) / 32); cfg.blockDim = dim3(1024); cfg.stream = st;
+    cfg.gridDim = dim3((cols / 4 + kWeightQuads - 1) / kWeightQuads); cfg.blockDim = dim3(1024); cfg.stream = st;
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;
