@@ -548,6 +548,18 @@ def _is_mx(m: MxRows, index: int, lead=None) -> bool:
             and ss[-1] == _mx_pitch(2 * cs[-1]) and (lead is None or cs[:-1] == lead))
 
 
+def _apart(outputs, inputs) -> bool:
+    """Whether contiguous output tensors (None: not given) share no byte with inputs or with one another."""
+    taken = [(t.data_ptr(), t.data_ptr() + t.numel() * t.element_size()) for t in inputs if t is not None]
+    for t in outputs:
+        if t is not None:
+            at, end = t.data_ptr(), t.data_ptr() + t.numel() * t.element_size()
+            if any(at < e and b < end for b, e in taken):
+                return False
+            taken.append((at, end))
+    return True
+
+
 def _is_mx8(m: Mx8Rows, index: int, shape) -> bool:
     """8-bit rows of the given logical shape on CUDA device `index`."""
     shape = tuple(shape)
@@ -556,7 +568,7 @@ def _is_mx8(m: Mx8Rows, index: int, shape) -> bool:
 
 
 def _is_dense(t: torch.Tensor, dtype: torch.dtype, shape, index: int) -> bool:
-    return t.dtype is dtype and t.shape == shape and t.is_contiguous() and t.is_cuda and t.get_device() == index
+    return t.dtype is dtype and t.shape == shape and t.get_device() == index and t.is_contiguous()      # (-1 on the CPU)
 
 
 # The current stream of a device as the integer that the C entry points take.  (torch.cuda.current_stream builds
@@ -1006,6 +1018,10 @@ class MoeRouter:
         return _is_mx8(z, dev, (n, cols)) if isinstance(z, Mx8Rows) else _is_dense(z, torch.bfloat16, (n, cols), dev)
 
     @staticmethod
+    def _kept_tensors(z):
+        return (z.codes, z.scales) if isinstance(z, Mx8Rows) else (z,)
+
+    @staticmethod
     def _kept_ptrs(z):
         return (z.codes.data_ptr(), z.scales.data_ptr()) if isinstance(z, Mx8Rows) else (0 if z is None else z.data_ptr(), 0)
 
@@ -1045,9 +1061,28 @@ class MoeRouter:
     def expert_ffn(self, rows: torch.Tensor, slot_counts: torch.Tensor, slot_offsets: torch.Tensor, gate_up: torch.Tensor,
                    down: torch.Tensor, y: torch.Tensor | None = None, h: torch.Tensor | None = None,
                    z: "torch.Tensor | Mx8Rows | None" = None) -> torch.Tensor:
-        """The gated feed-forward expert of every slot on its rows: expert_gated, then expert_product."""
-        h = self.expert_gated(rows, slot_counts, slot_offsets, gate_up, h, z)
-        return self.expert_product(h, slot_counts, slot_offsets, down, y)
+        """The gated feed-forward expert of every slot on its rows: expert_gated, then expert_product, refused before the
+        first launch where either would be."""
+        dev, n, bf16 = self._index(), rows.shape[0], torch.bfloat16
+        P, cols, n_in = gate_up.shape if gate_up.dim() == 3 else (0, 0, 0)
+        n_out, n_hidden = down.shape[1] if down.dim() == 3 else 0, cols // 2
+        _require(P == self.num_slots and cols > 0 and cols % 32 == 0 and _is_dense(gate_up, bf16, (P, cols, n_in), dev)
+                 and _is_dense(down, bf16, (P, n_out, n_hidden), dev) and _is_dense(rows, bf16, (n, n_in), dev)
+                 and self._slots_ok(slot_counts, slot_offsets, dev) and (z is None or self._kept_ok(z, n, cols, dev))
+                 and (y is None or (_is_dense(y, bf16, (n, n_out), dev) and _apart((y,), self._kept_tensors(z))))
+                 and (h is None or _is_dense(h, bf16, (n, n_hidden), dev)), "expert_ffn")
+        if h is None:
+            h = rows.new_empty((n, n_hidden))
+        if y is None:
+            y = torch.empty_like(rows) if n_out == n_in else rows.new_empty((n, n_out))
+        counts, offsets, stream = slot_counts.data_ptr(), slot_offsets.data_ptr(), _raw_stream(dev)
+        st = moe_expert_gated(self._ctx, rows.data_ptr(), n, counts, offsets, gate_up.data_ptr(), n_hidden, n_in, h.data_ptr(),
+                              *self._kept_ptrs(z), stream)
+        if st == MOE_OK:
+            st = moe_expert_product(self._ctx, h.data_ptr(), n, counts, offsets, down.data_ptr(), n_out, n_hidden, y.data_ptr(), stream)
+        if st != MOE_OK:
+            raise MoeError(st, "expert_ffn")
+        return y
 
     def expert_rows_backward(self, dy: torch.Tensor, slot_counts: torch.Tensor, slot_offsets: torch.Tensor, weight: torch.Tensor,
                              d_rows: torch.Tensor | None = None) -> torch.Tensor:
@@ -1108,11 +1143,41 @@ class MoeRouter:
                             d_gate_up: torch.Tensor | None = None, d_down: torch.Tensor | None = None, add: bool = False,
                             grad_dtype: torch.dtype = torch.bfloat16):
         """Gradients of expert_ffn with the projections ``z`` that it kept: (d_rows, d_gate_up, d_down).  ``add``: as in
-        expert_weight_backward, for both matrices."""
-        dz, h = self.expert_gated_backward(dy, slot_counts, slot_offsets, down, z)
-        d_down = self.expert_weight_backward(dy, h, slot_counts, slot_offsets, d_down, add, grad_dtype)
-        d_gate_up = self.expert_weight_backward(dz, rows, slot_counts, slot_offsets, d_gate_up, add, grad_dtype)
-        return self.expert_rows_backward(dz, slot_counts, slot_offsets, gate_up, d_rows), d_gate_up, d_down
+        expert_weight_backward, for both matrices.  Refused before the first launch where one of the four operators would be, and
+        where a given output shares a byte with an input of any of them."""
+        dev, n, bf16, f32 = self._index(), dy.shape[0], torch.bfloat16, torch.float32
+        P, cols, n_in = gate_up.shape if gate_up.dim() == 3 else (0, 0, 0)
+        n_out, n_hidden = down.shape[1] if down.dim() == 3 else 0, cols // 2
+        apart = ((d_rows is None and d_gate_up is None and d_down is None)
+                 or _apart((d_rows, d_gate_up, d_down), (dy, rows, gate_up, down, slot_counts, slot_offsets, *self._kept_tensors(z))))
+        add_ok = not add or (d_gate_up is not None and d_down is not None and d_gate_up.dtype is f32 and d_down.dtype is f32)
+        if d_gate_up is None:
+            d_gate_up = torch.empty_like(gate_up, dtype=grad_dtype) if grad_dtype is not bf16 else torch.empty_like(gate_up)
+        if d_down is None:
+            d_down = torch.empty_like(down, dtype=grad_dtype) if grad_dtype is not bf16 else torch.empty_like(down)
+        g_type, d_type = d_gate_up.dtype, d_down.dtype
+        _require(P == self.num_slots and cols > 0 and cols % 32 == 0 and _is_dense(gate_up, bf16, (P, cols, n_in), dev)
+                 and _is_dense(down, bf16, (P, n_out, n_hidden), dev) and _is_dense(dy, bf16, (n, n_out), dev) and _is_dense(rows, bf16, (n, n_in), dev)
+                 and self._slots_ok(slot_counts, slot_offsets, dev) and self._kept_ok(z, n, cols, dev)
+                 and (d_rows is None or _is_dense(d_rows, bf16, (n, n_in), dev)) and g_type in (bf16, f32) and d_type in (bf16, f32)
+                 and _is_dense(d_gate_up, g_type, (P, cols, n_in), dev) and _is_dense(d_down, d_type, (P, n_out, n_hidden), dev)
+                 and add_ok and apart, "expert_ffn_backward")
+        if d_rows is None:
+            d_rows = torch.empty_like(rows)
+        dz, h = dy.new_empty((n, cols)), dy.new_empty((n, n_hidden))
+        ctx, counts, offsets, stream = self._ctx, slot_counts.data_ptr(), slot_offsets.data_ptr(), _raw_stream(dev)
+        dy_ptr, dz_ptr, h_ptr, add = dy.data_ptr(), dz.data_ptr(), h.data_ptr(), int(add)
+        st = moe_expert_gated_backward(ctx, dy_ptr, n, counts, offsets, down.data_ptr(), n_out, n_hidden, *self._kept_ptrs(z), dz_ptr, h_ptr, stream)
+        if st == MOE_OK:
+            st = moe_expert_weight_backward(ctx, dy_ptr, h_ptr, n, counts, offsets, n_out, n_hidden, d_down.data_ptr(), _DTYPE_CODE[d_type], add, stream)
+        if st == MOE_OK:
+            st = moe_expert_weight_backward(ctx, dz_ptr, rows.data_ptr(), n, counts, offsets, cols, n_in, d_gate_up.data_ptr(), _DTYPE_CODE[g_type], add,
+                                            stream)
+        if st == MOE_OK:
+            st = moe_expert_rows_backward(ctx, dz_ptr, n, counts, offsets, gate_up.data_ptr(), cols, n_in, d_rows.data_ptr(), stream)
+        if st != MOE_OK:
+            raise MoeError(st, "expert_ffn_backward")
+        return d_rows, d_gate_up, d_down
 
     def _networks_ok(self, gate_up: torch.Tensor, down: torch.Tensor) -> bool:
         H, P, dev = self.cfg.hidden, self.num_slots, self._index()
@@ -1144,7 +1209,9 @@ class MoeRouter:
         """Gradients of the latest expert_step: (dx, d_logits, d_gate_up, d_down).  ``rows``: its send buffer, or its tokens' rows
         x in 8 bits (rms_norm's ``y8``).  d_logits is None for dense-FFN routing, whose weights are constants."""
         T, H, dev = dy.shape[0], self.cfg.hidden, self._index()
-        _require(self._networks_ok(gate_up, down) and _is_dense(dy, torch.bfloat16, (T, H), dev) and self._outputs_ok(out, T, dev)
+        # the gradients of combine and dispatch take the context's latest dispatch: it has to be this one
+        _require(self._latest is not None and self._latest[3] is out.dst_row
+                 and self._networks_ok(gate_up, down) and _is_dense(dy, torch.bfloat16, (T, H), dev) and self._outputs_ok(out, T, dev)
                  and self._kept_ok(z, T * self.cfg.top_k, gate_up.shape[1], dev), "expert_step_backward")
         d_buf, d_weights = self.combine_backward(buf, dy)
         if isinstance(rows, Mx8Rows):

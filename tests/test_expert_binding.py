@@ -9,11 +9,30 @@ import torch
 import test_drains
 from paper_2602_21140_b200 import binding as B
 from paper_2602_21140_b200 import build as build_mod
-from test_mx_binding import Fake
+from test_mx_binding import Fake as FakeTensor
 
 T, H, E, K, R, S, I = 8, 64, 8, 2, 4, 2, 48
 P, N = R * S, T * K
 BF, F32, I32, U8 = torch.bfloat16, torch.float32, torch.int32, torch.uint8
+
+
+class Fake(FakeTensor):
+    """Each somewhere else."""
+    _next = 1 << 30
+
+    def __init__(self, *args, **kwargs):
+        super().__init__(*args, **kwargs)
+        Fake._next += 1 << 30
+        self._at = Fake._next
+
+    def data_ptr(self):
+        return self._at
+
+    def element_size(self):
+        return {U8: 1, BF: 2, torch.float16: 2}.get(self.dtype, 4)
+
+    def new_empty(self, shape, dtype=None):
+        return Fake(shape, dtype or self.dtype, self._device)
 
 
 class Row(Fake):
@@ -22,12 +41,10 @@ class Row(Fake):
     def stride(self, d):
         return 1 if d else self.shape[-1] + 8
 
-    def element_size(self):
-        return 2 if self.dtype in (BF, torch.float16) else 4
-
 
 @pytest.fixture
 def router(monkeypatch):
+    monkeypatch.setattr(torch, "empty_like", lambda t, dtype=None: type(t)(t.shape, dtype or t.dtype))
     r = B.MoeRouter.__new__(B.MoeRouter)
     r.cfg = B.make_config(E, K, H, 64, R, S)
     r.device, r._ctx, r._latest = torch.device("cuda", 0), None, None
@@ -123,6 +140,59 @@ def test_weight_gradients(router):
     assert router.reached == ["moe_expert_weight_backward"] * 2
 
 
+def test_a_network_is_refused_before_its_first_launch(router):
+    g = good()
+    dy = Fake((N, H), BF)
+    args = dict(rows=g["rows"], slot_counts=g["slot_counts"], slot_offsets=g["slot_offsets"], gate_up=g["gate_up"], down=g["down"])
+    outs = dict(y=Fake((N, H), BF), h=Fake((N, I), BF), z=rows8(N, 2 * I))
+    router.expert_ffn(**args)
+    router.expert_ffn(**args, **outs)
+    assert router.reached == ["moe_expert_gated", "moe_expert_product"] * 2
+    router.reached.clear()
+    for name, t in [*args.items(), *outs.items()]:
+        for what, bad in variants(t) if name != "z" else [("rows", rows8(N - 1, 2 * I)), ("columns", rows8(N, 4 * I)), ("a tensor", Fake((N, I), BF))]:
+            if (name, what) in (("slot_offsets", "dimension 0"), ("down", "dimension 1")):
+                continue
+            with pytest.raises((B.MoeError, ValueError, AttributeError)):
+                router.expert_ffn(**{**args, **outs, name: bad})
+    whole = Fake((2 * N, 2 * I), BF)
+    y = Fake((N, H), BF)
+    y._at = whole._at + 64
+    with pytest.raises(B.MoeError):                             # y over what is kept
+        router.expert_ffn(**args, y=y, z=_at((N, 2 * I), whole._at))
+    assert router.reached == []
+    args = dict(dy=dy, **args, z=rows8(N, 2 * I))
+    outs = dict(d_rows=Fake((N, H), BF), d_gate_up=Fake((P, 2 * I, H), F32), d_down=Fake((P, H, I), F32))
+    router.expert_ffn_backward(**args)
+    router.expert_ffn_backward(**args, **outs, add=True)
+    router.expert_ffn_backward(**args, grad_dtype=F32)
+    steps = ["moe_expert_gated_backward", "moe_expert_weight_backward", "moe_expert_weight_backward", "moe_expert_rows_backward"]
+    assert router.reached == steps * 3
+    router.reached.clear()
+    for name, t in [*args.items(), *outs.items()]:
+        for what, bad in variants(t) if name != "z" else [("rows", rows8(N - 1, 2 * I)), ("columns", rows8(N, 4 * I)), ("none", None)]:
+            if (name, what) in (("slot_offsets", "dimension 0"), ("d_gate_up", "type"), ("d_down", "type")):
+                continue
+            with pytest.raises((B.MoeError, ValueError, AttributeError)):
+                router.expert_ffn_backward(**{**args, **outs, name: bad})
+    for bad in (dict(add=True), dict(add=True, grad_dtype=F32), dict(add=True, d_down=outs["d_down"]), dict(grad_dtype=torch.float16),
+                dict(add=True, d_gate_up=Fake((P, 2 * I, H), BF), d_down=outs["d_down"])):
+        with pytest.raises(B.MoeError):
+            router.expert_ffn_backward(**args, **bad)
+    for name, t in outs.items():                                # over any input or another output
+        for other in [*args.values(), *[o for o in outs.values() if o is not t]]:
+            place = _at(t.shape, (other.codes if isinstance(other, B.Mx8Rows) else other)._at, t.dtype)
+            with pytest.raises(B.MoeError):
+                router.expert_ffn_backward(**{**args, **outs, name: place})
+    assert router.reached == []
+
+
+def _at(shape, address, dtype=BF):
+    t = Fake(shape, dtype)
+    t._at = address
+    return t
+
+
 def _out(tokens=T):
     n = tokens * K
     return B.DispatchBuffers(Fake((tokens, K), I32), Fake((tokens, K), F32), Fake((tokens, K), I32), Fake((P,), I32), Fake((P + 1,), I32),
@@ -160,7 +230,6 @@ def test_a_step_is_refused_before_its_first_launch(router):
 
 
 def test_norm_arguments(router, monkeypatch):
-    monkeypatch.setattr(torch, "empty_like", lambda t: Row(t.shape, t.dtype))
     monkeypatch.setattr(torch, "empty", lambda shape, dtype, device: Row((shape,) if isinstance(shape, int) else shape, dtype))
     x, w = Row((T, H), BF), Row((H,), BF)
     router_reached = router.reached

@@ -163,6 +163,21 @@ def test_a_backward_pass_captured_while_an_eager_graph_of_the_same_leaves_lives(
     r.close()
 
 
+def test_another_dispatch_in_between_is_refused():
+    r, _, (gate_up, down) = _layer(32)
+    logits, x, dy = torch.randn(32, E, device="cuda"), U.bf16(32, H, seed=3), U.bf16(32, H, seed=4)
+    out, buf, z = r.alloc_outputs(32), torch.empty(32 * K, H, dtype=torch.bfloat16, device="cuda"), B.mx8_empty(32 * K, 2 * I)
+    r.expert_step(logits, x, gate_up, down, out, buf=buf, z=z)
+    want = r.expert_step_backward(logits, dy, out.send_buf, out, buf, z, gate_up, down)
+    r.dispatch(logits.flip(0).contiguous(), x)
+    with pytest.raises(B.MoeError):
+        r.expert_step_backward(logits, dy, out.send_buf, out, buf, z, gate_up, down)
+    r.expert_step(logits, x, gate_up, down, out, buf=buf, z=z)
+    got = r.expert_step_backward(logits, dy, out.send_buf, out, buf, z, gate_up, down)
+    assert all(torch.equal(a, b) for a, b in zip(want, got))
+    r.close()
+
+
 def test_no_tokens_and_dense_routing():
     r, _, (gate_up, down) = _layer(8)
     logits, x = torch.randn(0, E, device="cuda"), torch.empty(0, H, dtype=torch.bfloat16, device="cuda")
