@@ -239,6 +239,7 @@ struct Layout {
     static constexpr bool kGrad = OP == ExpertOp::kWeightGrad;
     static constexpr bool kAAlongK = OP == ExpertOp::kProduct || OP == ExpertOp::kGated;   // see desc_tile
     static constexpr bool kBAlongK = !kGrad;
+    static constexpr bool kFragments = OP == ExpertOp::kGated;   // how the epilogue reads an accumulator
     static constexpr int kN = NT / CG;                        // rows (or columns) of a tile in this CTA
     static constexpr int kStage = kATile + kN * kLine;        // multiples of 1024: swizzle alignment
     static constexpr int kEpiWarp = 32 * kLine;               // a plane of 32 x 32 fp32 or 32 x 64 bf16
@@ -341,38 +342,117 @@ __device__ __forceinline__ void store_rows(const KernelParams &p, const float *p
     }
 }
 
-// SwiGLU of 16 pairs x 32 rows, and the sums themselves where they are kept, in bf16 or in 8 bits (the warp's 32 sums of a
-// row are one block).  Rows behind the segment are computed as the others and not stored: branches would keep the four
-// rows of a lane from running side by side.
-__device__ __forceinline__ void store_gated(const KernelParams &p, const float *plane, int f, long long row, int left, int lane)
+// 8 pairs x 32 rows of 16-bit values in the fragment layout, m[i] being rows 8 i + 2 (lane % 4) and the next: written
+// as rows, `addr` being that of this lane's row.
+__device__ __forceinline__ void store_transposed(uint32_t addr, const uint32_t (&m)[4])
 {
-    const bool inside = f < p.N;                               // N is a multiple of 32: all of the block or nothing
-    const int at = f + (lane & 3) * 8;
+    asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(m[0]), "r"(m[1]), "r"(m[2]), "r"(m[3])
+                 : "memory");
+}
+
+// Rows of 16 pairs, 2 bytes each, in shared memory: where the eight of half c lie.
+__device__ __forceinline__ int pairs_at(int r, int c) { return r * 32 + ((c ^ ((r >> 2) & 1)) << 4); }
+
+// SwiGLU of 16 pairs x 32 rows, and the sums themselves where they are kept, in bf16 or in 8 bits (the warp's 32 sums of a
+// row are one block).  The features of a gated product lie in TMEM as sixteens of 8 gates and their 8 up-projections, so that a thread has
+// both of a pair: v[16 h + 4 i + e] and v[16 h + 4 i + 2 + e] for pair 8 h + lane / 4 and row 8 i + 2 (lane % 4) + e.  Two rows of a pair of
+// codes or of outputs are a register, which stmatrix turns round.  (Through a plane of fp32, as in store_rows, the epilogue bounds short K: 32
+// slots of 2048 rows, 1024 x 1024, 200 us and 246 with 8-bit sums instead of 169 and 222.  Rows without a gate have less to gain and
+// were 2 % slower by fragments.)
+__device__ __forceinline__ void store_gated(const KernelParams &p, const uint32_t (&v)[32], unsigned char *box, int f, long long row, int left,
+                                            int lane)
+{
+    const uint32_t base = smem_addr(box);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int r = 8 * i + (lane >> 2);
-        const bool store = r < left && inside;
-        float x[8], h[4];
-        read_eight(plane, i, lane, x);
+    for (int h = 0; h < 2; ++h) {
+        uint32_t m[4];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) h[q] = x[2 * q] * sigmoid(x[2 * q]) * x[2 * q + 1];
-        if (store)
-            *reinterpret_cast<uint2 *>(static_cast<__nv_bfloat16 *>(p.y) + (row + r) * (p.N / 2) + at / 2) =
-                make_uint2(pack_bf16(h[0], h[1]), pack_bf16(h[2], h[3]));
-        if (p.z_scales) {
-            uint32_t amax = mx8_amax(x);
-            amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
-            amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
-            const uint32_t s = mx8_scale_byte(amax);
-            const uint2 codes = mx8_quantize8(x, s);
-            if (store) {
-                *reinterpret_cast<uint2 *>(static_cast<uint8_t *>(p.z) + (row + r) * p.N + at) = codes;
-                if ((lane & 3) == 0) p.z_scales[(row + r) * mx_scale_pitch(p.N) + f / kMxBlock] = (uint8_t)s;
+        for (int i = 0; i < 4; ++i) {
+            float o[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const float g = __uint_as_float(v[16 * h + 4 * i + e]);
+                o[e] = g * sigmoid(g) * __uint_as_float(v[16 * h + 4 * i + 2 + e]);
             }
+            m[i] = pack_bf16(o[0], o[1]);
+        }
+        store_transposed(base + pairs_at(lane, h), m);
+    }
+    unsigned char *codes = box + 1024, *gates = box + 1024, *ups = box + 2048;
+    if (p.z_scales) {
+        uint32_t most[4];                                      // of two rows each, in 16 bits
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            uint32_t a[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                a[e] = 0;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) a[e] = max(a[e], v[16 * (q >> 1) + 4 * i + 2 * (q & 1) + e] & 0x7fffffffu);
+                // Rounded up to a bf16, two to a register: all that the scale asks is whether the mantissa is above 1.75, which
+                // is one.  (Not up to infinity: the largest bf16 has the scale of all that lies between.)
+                a[e] = a[e] >= 0x7f800000u ? a[e] >> 16 : min((a[e] + 0xffffu) >> 16, 0x7f7fu);
+            }
+            most[i] = a[0] | a[1] << 16;
+#pragma unroll
+            for (int off = 4; off < 32; off <<= 1) {
+                const uint32_t o = __shfl_xor_sync(0xffffffffu, most[i], off);
+                asm("max.u16x2 %0, %0, %1;" : "+r"(most[i]) : "r"(o));
+            }
+        }
+        float inv[4][2];
+        uint32_t keep[4];                                      // a block with a NaN or infinity has codes of 0
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t s0 = mx8_scale_byte(most[i] << 16), s1 = mx8_scale_byte(most[i] & 0xffff0000u);
+            inv[i][0] = mx_inverse_scale(s0); inv[i][1] = mx_inverse_scale(s1);
+            keep[i] = (s0 == 255u ? 0u : 0xffffu) | (s1 == 255u ? 0u : 0xffff0000u);
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            uint32_t m[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t *w = &v[16 * h + 4 * i];
+                m[i] = mx8_pack4(__uint_as_float(w[0]) * inv[i][0], __uint_as_float(w[2]) * inv[i][0], __uint_as_float(w[1]) * inv[i][1],
+                                 __uint_as_float(w[3]) * inv[i][1]) & keep[i];
+            }
+            store_transposed(smem_addr(codes) + pairs_at(lane, h), m);
+        }
+        const int r = 8 * (lane >> 3) + 2 * (lane & 3) + ((lane >> 2) & 1);   // every row's scale by one lane
+        const uint32_t two = lane < 16 ? (lane < 8 ? most[0] : most[1]) : (lane < 24 ? most[2] : most[3]);
+        if (r < left && f < p.N)
+            p.z_scales[(row + r) * mx_scale_pitch(p.N) + f / kMxBlock] = (uint8_t)mx8_scale_byte(lane & 4 ? two & 0xffff0000u : two << 16);
+    } else if (p.z) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            uint32_t g[4], u[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t *w = &v[16 * h + 4 * i];
+                g[i] = pack_bf16(__uint_as_float(w[0]), __uint_as_float(w[1]));
+                u[i] = pack_bf16(__uint_as_float(w[2]), __uint_as_float(w[3]));
+            }
+            store_transposed(smem_addr(gates) + pairs_at(lane, h), g);
+            store_transposed(smem_addr(ups) + pairs_at(lane, h), u);
+        }
+    }
+    __syncwarp();
+    const int c = lane & 1;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int r = 16 * i + (lane >> 1);
+        if (r >= left || f >= p.N) continue;                   // N is a multiple of 32: all of the block or nothing
+        *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(p.y) + (row + r) * (p.N / 2) + f / 2 + 8 * c) =
+            *reinterpret_cast<const uint4 *>(box + pairs_at(r, c));
+        if (p.z_scales) {
+            *reinterpret_cast<uint4 *>(static_cast<uint8_t *>(p.z) + (row + r) * p.N + f + 16 * c) =
+                *reinterpret_cast<const uint4 *>(codes + pairs_at(r, c));
         } else if (p.z) {
-            if (store)
-                *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(p.z) + (row + r) * p.N + at) =
-                    make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
+            const uint4 g = *reinterpret_cast<const uint4 *>(gates + pairs_at(r, c)), u = *reinterpret_cast<const uint4 *>(ups + pairs_at(r, c));
+            uint4 *dst = reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(p.z) + (row + r) * p.N + f + 16 * c);
+            dst[0] = make_uint4(__byte_perm(g.x, u.x, 0x5410), __byte_perm(g.x, u.x, 0x7632), __byte_perm(g.y, u.y, 0x5410), __byte_perm(g.y, u.y, 0x7632));
+            dst[1] = make_uint4(__byte_perm(g.z, u.z, 0x5410), __byte_perm(g.z, u.z, 0x7632), __byte_perm(g.w, u.w, 0x5410), __byte_perm(g.w, u.w, 0x7632));
         }
     }
 }
@@ -448,7 +528,7 @@ __device__ __forceinline__ void store_gated_backward(const KernelParams &p, cons
 // 960 at a time fp32 gradients are within 1e-6 of their magnitude.  With 1024 at a time one in 25000 of the 8-bit codes falls the
 // other way, whatever the length (one in 5000 with K = 7168 in one accumulator; one in 33000 with a chain of fp32 additions, and
 // one in 100000 with K = 1024).  Shorter pieces keep the epilogue, which has to add before it can store, from running under
-// the products: two and three for K of 1024 and 2048 take 16-21 % more time, 512 throughout 10-19 %.  A sum that is rounded to
+// the products: two and three for K of 1024 and 2048 take 15 % more time, 512 throughout 8-26 %.  A sum that is rounded to
 // bf16 needs no such care.
 constexpr int kGradSteps = 960 / kStageK;
 template <ExpertOp OP, bool FINE>
@@ -677,7 +757,8 @@ k_expert_product(const __grid_constant__ CUtensorMap map_a, const __grid_constan
 #pragma unroll
                         for (int half = 0; half < 32; half += 16) {
                             uint32_t v[16];
-                            tmem_ld_lanes(at + half, v);
+                            if (L::kFragments) tmem_ld_fragment(at + ((uint32_t)half << 16), v);
+                            else tmem_ld_lanes(at + half, v);
                             tmem_wait_ld();
 #pragma unroll
                             for (int c = 0; c < 16; ++c)
@@ -744,12 +825,13 @@ k_expert_product(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                     Kept kept[4];
                     if (OP == ExpertOp::kGatedBackward) load_kept(p, f, row, left, lane, kept);
                     if (one) {
-                        tmem_ld_lanes(acc_at(c0), sum[0]);
+                        if (L::kFragments) tmem_ld_fragments(acc_at(c0), sum[0]);
+                        else tmem_ld_lanes(acc_at(c0), sum[0]);
                         tmem_wait_ld();
                         if (left <= 64) release_acc();
                     }
-                    write_plane(plane, sum[0], lane);
-                    if (OP == ExpertOp::kGated) store_gated(p, plane, f, row, left, lane);
+                    if (!L::kFragments) write_plane(plane, sum[0], lane);
+                    if (OP == ExpertOp::kGated) store_gated(p, sum[0], mine, f, row, left, lane);
                     else if (OP == ExpertOp::kGatedBackward) store_gated_backward(p, plane, f, row, left, lane, kept);
                     else store_rows(p, plane, f, row, left, lane);
                     __syncwarp();                              // the plane is free before the next 32 rows are written
@@ -797,7 +879,8 @@ k_expert_product(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                             else load_grad<true>(a, b, &map_a, &map_b, feat, col, r, bar);
                         } else {
                             if (rank == 0) mbar_expect_tx(&full[s], bytes);
-                            if (L::kAAlongK) tma_3d<CG>(a, &map_a, k * kStageK, feat, t.slot, bar);
+                            if (OP == ExpertOp::kGated) tma_pairs<CG>(a, &map_a, k * kStageK, feat / 16, t.slot, bar);
+                            else if (L::kAAlongK) tma_3d<CG>(a, &map_a, k * kStageK, feat, t.slot, bar);
                             else {
 #pragma unroll
                                 for (int q = 0; q < kFeat / 64; ++q) tma_3d<CG>(a + q * kChunk, &map_a, feat + q * 64, k * kStageK, t.slot, bar);
@@ -948,7 +1031,12 @@ cudaError_t launch(const ExpertArgs &a, cudaStream_t st)
         const cuuint64_t inner = L::kAAlongK ? a.K : a.N, outer = L::kAAlongK ? a.N : a.K;
         const cuuint64_t wd[3] = {inner, outer, (cuuint64_t)a.P}, ws[2] = {2 * inner, 2 * inner * outer};
         const cuuint64_t ad[2] = {(cuuint64_t)a.K, (cuuint64_t)a.rows}, as[1] = {2 * (cuuint64_t)a.K};
-        ok = encode(&map_a, bf16, sw, a.w, 3, wd, ws, 64, L::kAAlongK ? kFeat : kStageK) && encode(&map_b, bf16, sw, a.a, 2, ad, as, 64, 32) &&
+        // a row, eight rows of one parity, the parities, the sixteens, the slots
+        const cuuint64_t pd[5] = {(cuuint64_t)a.K, 8, 2, (cuuint64_t)a.N / 16, (cuuint64_t)a.P};
+        const cuuint64_t ps[4] = {4 * (cuuint64_t)a.K, 2 * (cuuint64_t)a.K, 32 * (cuuint64_t)a.K, 2 * (cuuint64_t)a.K * a.N};
+        ok = (OP == ExpertOp::kGated ? encode(&map_a, bf16, sw, a.w, 5, pd, ps, 64, 8, 2, kFeat / 16)
+                                     : encode(&map_a, bf16, sw, a.w, 3, wd, ws, 64, L::kAAlongK ? kFeat : kStageK)) &&
+             encode(&map_b, bf16, sw, a.a, 2, ad, as, 64, 32) &&
              encode(&map_big, bf16, sw, a.a, 2, ad, as, 64, L::kN);
     }
     if (!ok) return cudaErrorInvalidValue;

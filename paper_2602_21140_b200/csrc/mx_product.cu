@@ -65,39 +65,6 @@ __device__ __forceinline__ void cp_scales(uint32_t tmem, uint64_t desc)
     else asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
 }
 
-// 32 lanes x 32 columns as two halves of 16 lanes in the fragment layout: v[16 h + 4 i + 2 j + e] is lane
-// 16 h + 8 j + (thread / 4), column 8 i + 2 (thread % 4) + e
-__device__ __forceinline__ void tmem_ld_fragments(uint32_t addr, uint32_t (&r)[32])
-{
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-        asm volatile(
-            "tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-            : "=r"(r[16 * h + 0]), "=r"(r[16 * h + 1]), "=r"(r[16 * h + 2]), "=r"(r[16 * h + 3]), "=r"(r[16 * h + 4]),
-              "=r"(r[16 * h + 5]), "=r"(r[16 * h + 6]), "=r"(r[16 * h + 7]), "=r"(r[16 * h + 8]), "=r"(r[16 * h + 9]),
-              "=r"(r[16 * h + 10]), "=r"(r[16 * h + 11]), "=r"(r[16 * h + 12]), "=r"(r[16 * h + 13]), "=r"(r[16 * h + 14]),
-              "=r"(r[16 * h + 15])
-            : "r"(addr + ((uint32_t)(16 * h) << 16)));
-}
-
-// weight rows in the order of weight_row: sixteens of {8 even, 8 odd} rows
-template <int CG>
-__device__ __forceinline__ void tma_pairs(void *dst, const CUtensorMap *map, int x, int sixteen, int slot, uint32_t bar)
-{
-    if (CG == 1)
-        asm volatile(
-            "cp.async.bulk.tensor.5d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %5, %5, %3, %4}], [%6];" ::"r"(
-                smem_addr(dst)),
-            "l"(map), "r"(x), "r"(sixteen), "r"(slot), "r"(0), "r"(bar)
-            : "memory");
-    else
-        asm volatile(
-            "cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %5, %5, %3, %4}], [%6];" ::"r"(
-                smem_addr(dst)),
-            "l"(map), "r"(x), "r"(sixteen), "r"(slot), "r"(0), "r"(bar)
-            : "memory");
-}
-
 // Shared-memory matrix descriptor: start and strides in 16-byte units, version 1 (sm_100).
 // Code tiles: K-major, 128-byte swizzle, 8-row groups 1024 bytes apart.
 // Scale blocks: no swizzle, 8-row groups (8 x 16 bytes) 128 bytes apart.

@@ -43,6 +43,23 @@ __device__ __forceinline__ void mma_commit(uint64_t *bar)
                      : "memory");
 }
 
+// 16 lanes x 32 columns in the fragment layout: v[4 i + 2 j + e] is lane 8 j + (thread / 4), column 8 i + 2 (thread % 4) + e
+__device__ __forceinline__ void tmem_ld_fragment(uint32_t addr, uint32_t *r)
+{
+    asm volatile(
+        "tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(addr));
+}
+
+// 32 lanes: v[16 h + ...] for the lanes from 16 h on
+__device__ __forceinline__ void tmem_ld_fragments(uint32_t addr, uint32_t (&r)[32])
+{
+#pragma unroll
+    for (int h = 0; h < 2; ++h) tmem_ld_fragment(addr + ((uint32_t)(16 * h) << 16), r + 16 * h);
+}
+
 __device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
@@ -127,6 +144,25 @@ __device__ __forceinline__ void tma_3d(void *dst, const CUtensorMap *map, int x,
             "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(
                 smem_addr(dst)),
             "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
+            : "memory");
+}
+
+// Weight rows as sixteens of {8 even, 8 odd} rows, of a map over {a row, eight rows of one parity, the parities, the sixteens,
+// the slots}
+template <int CG>
+__device__ __forceinline__ void tma_pairs(void *dst, const CUtensorMap *map, int x, int sixteen, int slot, uint32_t bar)
+{
+    if (CG == 1)
+        asm volatile(
+            "cp.async.bulk.tensor.5d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %5, %5, %3, %4}], [%6];" ::"r"(
+                smem_addr(dst)),
+            "l"(map), "r"(x), "r"(sixteen), "r"(slot), "r"(0), "r"(bar)
+            : "memory");
+    else
+        asm volatile(
+            "cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %5, %5, %3, %4}], [%6];" ::"r"(
+                smem_addr(dst)),
+            "l"(map), "r"(x), "r"(sixteen), "r"(slot), "r"(0), "r"(bar)
             : "memory");
 }
 

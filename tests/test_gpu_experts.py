@@ -178,6 +178,29 @@ def test_values_at_the_edge():
     r.close()
 
 
+@pytest.mark.parametrize("most", [1.75, 1.0, 1.9921875])
+def test_scales_of_kept_sums_at_their_steps(most):
+    """The largest sum of a block, at every place of it, a little below, at and above `most` times a power of two, up to the
+    largest that is finite: the scale is the smallest that will do.  The sums are exact: two terms that 24 bits hold."""
+    P, I = 32, 16                                            # slot p has its largest at p
+    rows = [(2.0 ** e, s * 2.0 ** e) for e in (-100, -7, 0, 1, 120, 127) for s in (-1, 0, 1)]
+    r = U.make_router(P)
+    n_, off, n = U.layout([len(rows)] * P)
+    a = torch.zeros(n, 16, device="cuda").bfloat16()
+    a[:, :2] = torch.tensor(rows * P)
+    gate_up = torch.zeros(P, 2 * I, 16, device="cuda").bfloat16()
+    gate_up[:, :, 0] = 0.25
+    gate_up[torch.arange(P), torch.arange(P), 0] = most
+    gate_up[torch.arange(P), torch.arange(P), 1] = 2.0 ** -20
+    z = B.mx8_empty(n, 2 * I)
+    r.expert_gated(a, n_, off, gate_up, z=z)
+    torch.cuda.synchronize()
+    want = torch.bmm(a.double().view(P, -1, 16), gate_up.double().transpose(1, 2)).view(n, 2 * I)
+    assert want.float().isfinite().all() and (want.float() == want).all()
+    U.check8(z, want, torch.zeros_like(want))
+    r.close()
+
+
 def test_segments_from_device_memory_are_cut():
     """Counts and offsets that leave the row buffer: segments are cut or dropped, nothing beyond the buffers is touched."""
     r = U.make_router(4)
