@@ -568,7 +568,7 @@ def _is_mx8(m: Mx8Rows, index: int, shape) -> bool:
 
 
 def _is_dense(t: torch.Tensor, dtype: torch.dtype, shape, index: int) -> bool:
-    return t.dtype is dtype and t.shape == shape and t.get_device() == index and t.is_contiguous()      # (-1 on the CPU)
+    return t.dtype is dtype and t.shape == shape and t.get_device() == index >= 0 and t.is_contiguous()   # (-1 on the CPU)
 
 
 # The current stream of a device as the integer that the C entry points take.  (torch.cuda.current_stream builds

@@ -259,6 +259,17 @@ def test_norm_arguments(router, monkeypatch):
     assert router_reached == ["moe_rms_norm"] * 2 + ["moe_rms_norm_backward"]
 
 
+def test_values_of_8_bit_rows(router):
+    m = rows8(T, H)
+    B.mx8_dequantize(m, out=Row((T, H), BF, contiguous=False))
+    for bad, out in ((rows8(T, H), Row((T, H), F32)), (rows8(T, H), Row((T, H + 32), BF)), (rows8(T, H), Row((T, H), BF, device=-1)),
+                     (B.Mx8Rows(Fake((T, H), U8), Fake((T, H // 32), U8)), None), (B.mx_empty(T, H, device="cpu"), None), (B.mx8_empty(T, H, device="cpu"), None),
+                     (B.mx8_empty(T, H, device="cpu"), torch.empty(T, H, dtype=BF))):
+        with pytest.raises(B.MoeError):
+            B.mx8_dequantize(bad, out=out)
+    assert router.reached == ["moe_kept_dequantize"]
+
+
 A = 1 << 30                  # 16-byte aligned; refused calls never look at it
 BAD, OK, CAP, CUDA = B.MOE_ERR_INVALID_ARG, B.MOE_OK, B.MOE_ERR_CAPACITY, B.MOE_ERR_CUDA
 
