@@ -31,6 +31,7 @@
 
 #include <algorithm>
 #include <mutex>
+#include <type_traits>
 
 #include "mx8_format.cuh"
 #include "tcgen05.cuh"
@@ -531,13 +532,29 @@ __device__ __forceinline__ void store_gated_backward(const KernelParams &p, cons
 // the products: two and three for K of 1024 and 2048 take 15 % more time, 512 throughout 8-26 %.  A sum that is rounded to
 // bf16 needs no such care.
 constexpr int kGradSteps = 960 / kStageK;
+template <ExpertOp OP> constexpr int kMostSteps = OP == ExpertOp::kWeightGrad ? kGradSteps : 1024 / kStageK;
 template <ExpertOp OP, bool FINE>
 __device__ __forceinline__ int acc_steps(int steps)
 {
     if (!FINE) return steps;
-    constexpr int kMost = OP == ExpertOp::kWeightGrad ? kGradSteps : 1024 / kStageK;
-    const int n = max(1, (steps + kMost - 1) / kMost);         // as few pieces as that allows, of equal length
+    const int n = max(1, (steps + kMostSteps<OP> - 1) / kMostSteps<OP>);   // as few pieces as that allows, of equal length
     return (steps + n - 1) / n;
+}
+
+// Whether a sum of this call takes more than one accumulator.
+template <ExpertOp OP>
+__device__ __forceinline__ bool any_split(const KernelParams &p, int lane)
+{
+    int longest = p.K;
+    if (OP == ExpertOp::kWeightGrad) {
+        longest = 0;
+        for (int s = lane; s < p.P; s += 32) {
+            int first;
+            longest = max(longest, segment(p, s, first));
+        }
+        longest = __reduce_max_sync(0xffffffffu, longest);
+    }
+    return longest > kMostSteps<OP> * kStageK;
 }
 
 // 32 features (lanes) x 32 (fp32) or 64 (bf16) columns of a weight gradient, through 4 KB of shared memory: a lane writes
@@ -710,137 +727,147 @@ k_expert_product(const __grid_constant__ CUtensorMap map_a, const __grid_constan
         const int group = warp >> 2, quarter = warp & 3;
         unsigned char *mine = epi + warp * L::kEpiWarp;
         constexpr int kPieces = NT / 64;                       // of 32 columns, of this warp: c0 = group * 32, then every 64
-        int buf = 0;
-        unsigned acc_parity = 0;
-        Tile t;
-        bool ok = true;
-        for (TileStream<OP> stream(p, ends, tiles); ok && stream.next(t);) {
-            const int f = t.feat + rank * kFeat + quarter * 32;
-            const int cols = kGrad ? min(NT, p.N - t.col) : t.rows, steps = ((kGrad ? t.rows : p.K) + kStageK - 1) / kStageK;
-            const int each = acc_steps<OP, FINE>(steps);
-            const auto wait_acc = [&] {
-                // a stage takes 512 clocks, a poll 20 or more: a long sum is no reason to give up
-                ok = __all_sync(0xffffffffu, wait_for(&acc_full[buf], acc_parity, quit, p.spin_limit + 64u * each));
-                tc_fence_after();
-                return ok;
-            };
-            const auto release_acc = [&] {                     // after this warp's last look at the accumulator
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive_lead<CG>(&acc_empty[buf]);
-            };
-            const auto next_acc = [&] {
-                buf ^= 1;
-                if (buf == 0) acc_parity ^= 1u;
-            };
-            const auto acc_at = [&](int c0) { return tmem + buf * NT + c0 + ((uint32_t)(quarter * 32) << 16); };
-            uint32_t sum[FINE ? kPieces : 1][32];
-            const auto next_piece = [&] {                      // to the front: a piece's number is no register's
+        const auto epilogue = [&](auto split) {
+            constexpr bool kSplit = decltype(split)::value;
+            int buf = 0;
+            unsigned acc_parity = 0;
+            Tile t;
+            bool ok = true;
+            for (TileStream<OP> stream(p, ends, tiles); ok && stream.next(t);) {
+                const int f = t.feat + rank * kFeat + quarter * 32;
+                const int cols = kGrad ? min(NT, p.N - t.col) : t.rows, steps = ((kGrad ? t.rows : p.K) + kStageK - 1) / kStageK;
+                const int each = acc_steps<OP, FINE>(steps);
+                const auto wait_acc = [&] {
+                    // a stage takes 512 clocks, a poll 20 or more: a long sum is no reason to give up
+                    ok = __all_sync(0xffffffffu, wait_for(&acc_full[buf], acc_parity, quit, p.spin_limit + 64u * each));
+                    tc_fence_after();
+                    return ok;
+                };
+                const auto release_acc = [&] {                     // after this warp's last look at the accumulator
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_lead<CG>(&acc_empty[buf]);
+                };
+                const auto next_acc = [&] {
+                    buf ^= 1;
+                    if (buf == 0) acc_parity ^= 1u;
+                };
+                const auto acc_at = [&](int c0) { return tmem + buf * NT + c0 + ((uint32_t)(quarter * 32) << 16); };
+                uint32_t sum[kSplit ? kPieces : 1][32];
+                const auto next_piece = [&] {                      // to the front: a piece's number is no register's
 #pragma unroll
-                for (int n = 1; n < kPieces; ++n)
+                    for (int n = 1; n < kPieces; ++n)
 #pragma unroll
-                    for (int c = 0; c < 32; ++c) sum[FINE ? n - 1 : 0][c] = sum[FINE ? n : 0][c];
-            };
-            const bool one = !FINE || each == steps;           // accumulator: its pieces are read as they are stored
-            if (!one) {                                        // all of the tile's accumulators added up
-                int k = 0;
+                        for (int c = 0; c < 32; ++c) sum[kSplit ? n - 1 : 0][c] = sum[kSplit ? n : 0][c];
+                };
+                const bool one = !kSplit || each == steps;          // accumulator: its pieces are read as they are stored
+                if (!one) {                                        // all of the tile's accumulators added up
+                    int k = 0;
 #pragma unroll
-                for (int q = 0; q < kPieces; ++q)
+                    for (int q = 0; q < kPieces; ++q)
 #pragma unroll
-                    for (int c = 0; c < 32; ++c) sum[q][c] = 0u;
-                do {
-                    if (!wait_acc()) break;
+                        for (int c = 0; c < 32; ++c) sum[q][c] = 0u;
+                    do {
+                        if (!wait_acc()) break;
 #pragma unroll
-                    for (int q = 0; q < kPieces; ++q) {
-                        if (group * 32 + 64 * q >= cols) break;
-                        const uint32_t at = acc_at(group * 32 + 64 * q);
+                        for (int q = 0; q < kPieces; ++q) {
+                            if (group * 32 + 64 * q >= cols) break;
+                            const uint32_t at = acc_at(group * 32 + 64 * q);
 #pragma unroll
-                        for (int half = 0; half < 32; half += 16) {
-                            uint32_t v[16];
-                            if (L::kFragments) tmem_ld_fragment(at + ((uint32_t)half << 16), v);
-                            else tmem_ld_lanes(at + half, v);
+                            for (int half = 0; half < 32; half += 16) {
+                                uint32_t v[16];
+                                if (L::kFragments) tmem_ld_fragment(at + ((uint32_t)half << 16), v);
+                                else tmem_ld_lanes(at + half, v);
+                                tmem_wait_ld();
+#pragma unroll
+                                for (int c = 0; c < 16; ++c)
+                                    sum[q][half + c] = __float_as_uint(__uint_as_float(sum[q][half + c]) + __uint_as_float(v[c]));
+                            }
+                        }
+                        release_acc();
+                        next_acc();
+                        k += each;
+                    } while (k < steps);
+                    if (!ok) break;
+                } else if (!wait_acc()) {
+                    break;
+                }
+                if (kGrad && !F32) {
+                    for (int c0 = group * 64; c0 < cols && f < p.M; c0 += 128) {
+                        uint4 box[8] = {};
+                        if (steps > 0) {
+                            uint32_t v[2][32];
+                            tmem_ld_lanes(acc_at(c0), v[0]);
+                            tmem_ld_lanes(acc_at(c0 + 32), v[1]);
                             tmem_wait_ld();
 #pragma unroll
-                            for (int c = 0; c < 16; ++c)
-                                sum[q][half + c] = __float_as_uint(__uint_as_float(sum[q][half + c]) + __uint_as_float(v[c]));
+                            for (int q = 0; q < 8; ++q) {
+                                const uint32_t *w = &v[q >> 2][8 * (q & 3)];
+                                box[q] = make_uint4(pack_bf16(__uint_as_float(w[0]), __uint_as_float(w[1])),
+                                                    pack_bf16(__uint_as_float(w[2]), __uint_as_float(w[3])),
+                                                    pack_bf16(__uint_as_float(w[4]), __uint_as_float(w[5])),
+                                                    pack_bf16(__uint_as_float(w[6]), __uint_as_float(w[7])));
+                            }
+                        }
+                        if (steps <= kFewSteps) store_box(&map_y, t.slot, f, t.col + c0, box, mine, lane);
+                        else {
+                            if (lane == 0) bulk_wait_read<0>();    // of an earlier tile
+                            __syncwarp();
+                            store_grad<false>(p, t, f, t.col + c0, box, mine, lane);
                         }
                     }
                     release_acc();
-                    next_acc();
-                    k += each;
-                } while (k < steps);
-                if (!ok) break;
-            } else if (!wait_acc()) {
-                break;
-            }
-            if (kGrad && !F32) {
-                for (int c0 = group * 64; c0 < cols && f < p.M; c0 += 128) {
-                    uint4 box[8] = {};
-                    if (steps > 0) {
-                        uint32_t v[2][32];
-                        tmem_ld_lanes(acc_at(c0), v[0]);
-                        tmem_ld_lanes(acc_at(c0 + 32), v[1]);
-                        tmem_wait_ld();
-#pragma unroll
-                        for (int q = 0; q < 8; ++q) {
-                            const uint32_t *w = &v[q >> 2][8 * (q & 3)];
-                            box[q] = make_uint4(pack_bf16(__uint_as_float(w[0]), __uint_as_float(w[1])),
-                                                pack_bf16(__uint_as_float(w[2]), __uint_as_float(w[3])),
-                                                pack_bf16(__uint_as_float(w[4]), __uint_as_float(w[5])),
-                                                pack_bf16(__uint_as_float(w[6]), __uint_as_float(w[7])));
+                } else if (kGrad) {
+#pragma unroll 1
+                    for (int q = 0; q < kPieces; ++q) {
+                        const int c0 = group * 32 + 64 * q;
+                        if (c0 >= cols || f >= p.M || (p.add && steps == 0)) break;
+                        if (one && steps > 0) {
+                            tmem_ld_lanes(acc_at(c0), sum[0]);
+                            tmem_wait_ld();
                         }
-                    }
-                    if (steps <= kFewSteps) store_box(&map_y, t.slot, f, t.col + c0, box, mine, lane);
-                    else {
-                        if (lane == 0) bulk_wait_read<0>();    // of an earlier tile
-                        __syncwarp();
-                        store_grad<false>(p, t, f, t.col + c0, box, mine, lane);
-                    }
-                }
-                release_acc();
-            } else if (kGrad) {
-#pragma unroll 1
-                for (int q = 0; q < kPieces; ++q) {
-                    const int c0 = group * 32 + 64 * q;
-                    if (c0 >= cols || f >= p.M || (p.add && steps == 0)) break;
-                    if (one && steps > 0) {
-                        tmem_ld_lanes(acc_at(c0), sum[0]);
-                        tmem_wait_ld();
-                    }
-                    uint4 box[8];
+                        uint4 box[8];
 #pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        box[i] = steps > 0 ? make_uint4(sum[0][4 * i], sum[0][4 * i + 1], sum[0][4 * i + 2], sum[0][4 * i + 3]) : make_uint4(0u, 0u, 0u, 0u);
-                    store_grad<true>(p, t, f, t.col + c0, box, mine, lane);
-                    if (!one) next_piece();
-                }
-                if (one) release_acc();
-            } else {
-                float *plane = reinterpret_cast<float *>(mine);
-#pragma unroll 1
-                for (int q = 0; q < kPieces; ++q) {
-                    const int c0 = group * 32 + 64 * q, left = cols - c0;
-                    if (left <= 0) break;
-                    const long long row = t.row + c0;
-                    Kept kept[4];
-                    if (OP == ExpertOp::kGatedBackward) load_kept(p, f, row, left, lane, kept);
-                    if (one) {
-                        if (L::kFragments) tmem_ld_fragments(acc_at(c0), sum[0]);
-                        else tmem_ld_lanes(acc_at(c0), sum[0]);
-                        tmem_wait_ld();
-                        if (left <= 64) release_acc();
+                        for (int i = 0; i < 8; ++i)
+                            box[i] = steps > 0 ? make_uint4(sum[0][4 * i], sum[0][4 * i + 1], sum[0][4 * i + 2], sum[0][4 * i + 3]) : make_uint4(0u, 0u, 0u, 0u);
+                        store_grad<true>(p, t, f, t.col + c0, box, mine, lane);
+                        if (!one) next_piece();
                     }
-                    if (!L::kFragments) write_plane(plane, sum[0], lane);
-                    if (OP == ExpertOp::kGated) store_gated(p, sum[0], mine, f, row, left, lane);
-                    else if (OP == ExpertOp::kGatedBackward) store_gated_backward(p, plane, f, row, left, lane, kept);
-                    else store_rows(p, plane, f, row, left, lane);
-                    __syncwarp();                              // the plane is free before the next 32 rows are written
-                    if (!one) next_piece();
+                    if (one) release_acc();
+                } else {
+                    float *plane = reinterpret_cast<float *>(mine);
+#pragma unroll 1
+                    for (int q = 0; q < kPieces; ++q) {
+                        const int c0 = group * 32 + 64 * q, left = cols - c0;
+                        if (left <= 0) break;
+                        const long long row = t.row + c0;
+                        Kept kept[4];
+                        if (OP == ExpertOp::kGatedBackward) load_kept(p, f, row, left, lane, kept);
+                        if (one) {
+                            if (L::kFragments) tmem_ld_fragments(acc_at(c0), sum[0]);
+                            else tmem_ld_lanes(acc_at(c0), sum[0]);
+                            tmem_wait_ld();
+                            if (left <= 64) release_acc();
+                        }
+                        if (!L::kFragments) write_plane(plane, sum[0], lane);
+                        if (OP == ExpertOp::kGated) store_gated(p, sum[0], mine, f, row, left, lane);
+                        else if (OP == ExpertOp::kGatedBackward) store_gated_backward(p, plane, f, row, left, lane, kept);
+                        else store_rows(p, plane, f, row, left, lane);
+                        __syncwarp();                              // the plane is free before the next 32 rows are written
+                        if (!one) next_piece();
+                    }
+                    if (one && group * 32 >= cols) release_acc();
                 }
-                if (one && group * 32 >= cols) release_acc();
+                if (one) next_acc();
             }
-            if (one) next_acc();
-        }
+        };
+        // Two epilogues: where every sum is one accumulator's, registers that hold sums would only be in the way (fp32 gradients of
+        // 24 slots of 45 rows, 4096 x 1024: 90 us and 119; of 128 slots of 511 rows: 1363 and 1487; gated, 32 slots of 2048 rows, 1024 x
+        // 1024, 8-bit sums: 205 and 218).
+        if constexpr (FINE) {
+            if (any_split<OP>(p, lane)) epilogue(std::true_type());
+            else epilogue(std::false_type());
+        } else epilogue(std::false_type());
         if (kGrad && !F32 && lane == 0) bulk_wait_all();       // the last stores have left shared memory
     } else {
         // The two issuing warps run their loops with all lanes, so that everything the asynchronous instructions
@@ -1073,8 +1100,8 @@ cudaError_t expert_product_launch(const ExpertArgs &a, cudaStream_t st)
     case ExpertOp::kGatedBackward: return launch<ExpertOp::kGatedBackward>(a, st);
     case ExpertOp::kWeightGrad:
         if (!a.f32) return launch<ExpertOp::kWeightGrad>(a, st);
-        // no segment is longer than the buffer: one accumulator will do, and the kernel without the sums is 5-10 % faster where
-        // the stores bound it (24 slots of 45 rows, 4096 x 1024: 82 and 90 us)
+        // no segment is longer than the buffer: one accumulator will do, without a look at the segments (2 % of 24 slots of 45 rows,
+        // 4096 x 1024)
         if (a.rows <= kGradSteps * kStageK) return launch<ExpertOp::kWeightGrad, false, true>(a, st);
         return launch<ExpertOp::kWeightGrad, true, true>(a, st);
     }
