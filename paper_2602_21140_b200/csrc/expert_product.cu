@@ -22,9 +22,9 @@
 // The accumulator is double buffered, so the epilogue of a tile runs under the products of the next.
 //
 // What bounds it: with many rows the tensor cores, under the power cap (at 32 slots of 1024 rows, 4096 x 1024, they are busy for
-// 92 % of the gated product and of the gradient by the rows, at 1.39 GHz).  A stage of 64 is 32 KB a CTA in the 512 clocks of its
+// 90 % of the gated product and 92 % of the gradient by the rows, at 1.39 GHz).  A stage of 64 is 32 KB a CTA in the 512 clocks of its
 // MMAs, all that an SM gets from L2, so nothing else may use that path: prefetching stages into L2 by TMA cost 15 %.  The
-// gradient of the gate (78 %) and the weights' (83 %, in fp32 67 %) move as many bytes of HBM as products, and wait for loads.
+// gradient of the gate (77 %) and the weights' (85 %, in fp32 66 %) move as many bytes of HBM as products, and wait for loads.
 // With few rows HBM: one row for 8 slots of 7168 x 2048 takes 77 + 46 us, whose weights take 72 + 36.  Single CTAs with tiles of
 // 64 rows were as fast up to 64 rows a slot and took up to 2.4 times as long with 200.
 #include "expert_product.h"

@@ -5,8 +5,8 @@
 //   backward, with n = h * rstd and g = dy * weight:  dx = rstd * (g - n * mean(g * n)) + dh,  d_weight = sum over rows of dy * n
 //
 // Both are one pass over the rows and bound by HBM.  A row is taken by a warp up to 1024 columns, by a CTA above, with as many
-// warps as make four units a thread (a fixed 256 threads lost half of the bandwidth at 1536 columns).  A thread owns units of eight consecutive elements (one 16-byte access of a 16-bit type), so four
-// neighbouring lanes own a block of the 8-bit form.  The forward pass holds a row in registers between the reduction and the
+// warps as make four units a thread (a fixed 256 threads lost half of the bandwidth at 1536 columns).  A thread owns units of eight
+// consecutive elements (one 16-byte access of a 16-bit type), so four neighbouring lanes own a block of the 8-bit form.  The forward pass holds a row in registers between the reduction and the
 // result and has a CTA per row.  The backward pass has as many CTAs as fit, because each also sums d_weight over its rows; its
 // next rows are on their way to shared memory meanwhile (k_rms_norm_backward_ring).  All sums are fp32, in an order that
 // depends on the sizes alone; every output is rounded once.
