@@ -147,6 +147,31 @@ def test_fp32_gradients_of_many_rows():
     r.close()
 
 
+def test_fp32_gradients_beside_longer_segments():
+    """Segments of one piece beside ones of two, of none, and alone in a call: the same bits, whichever way the call's sums go."""
+    counts = [961, 0, 45, 960, 1500, 1, 530]
+    P = len(counts)
+    r = U.make_router(P)
+    n_, off, n = U.layout(counts, gap=3)
+    dy, a = U.bf16(n, 272, seed=1), U.bf16(n, 520, seed=2)
+    before = torch.randn(P, 272, 520, device="cuda")
+    got = r.expert_weight_backward(dy, a, n_, off, dtype=torch.float32)
+    added = r.expert_weight_backward(dy, a, n_, off, before.clone(), add=True)
+    assert torch.equal(added, torch.where(torch.tensor(counts, device="cuda")[:, None, None] > 0, got + before, before))
+    short = torch.where(n_ > 960, torch.zeros_like(n_), n_)       # the same buffer, no segment of two pieces
+    alone = r.expert_weight_backward(dy, a, short, off, dtype=torch.float32)
+    for p, s, e in _spans(counts, off):
+        if e - s <= 960:
+            assert torch.equal(got[p], alone[p])
+            few, where = torch.zeros_like(n_), torch.zeros_like(off)   # a buffer that no segment of two pieces fits
+            few[p] = e - s
+            assert torch.equal(got[p], r.expert_weight_backward(dy[s:e], a[s:e], few, where, dtype=torch.float32)[p])
+        want, size = dy[s:e].double().T @ a[s:e].double(), dy[s:e].double().abs().T @ a[s:e].double().abs()
+        U.within(got[p], want, (1 + 2.0 ** -24) * (U.sum_bound(min(e - s, 960), size) + 2 * 2.0 ** -24 * size) + 2.0 ** -24 * want.abs())
+    assert r.device_status() == 0
+    r.close()
+
+
 def test_values_at_the_edge():
     """Gates beyond exp's range, infinities and NaN stay in their row; a large gate is the identity, a very negative one 0."""
     r = U.make_router(1)
