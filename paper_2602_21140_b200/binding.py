@@ -17,7 +17,7 @@ from __future__ import annotations
 import ctypes
 import functools
 import os
-from dataclasses import dataclass
+from dataclasses import dataclass, field
 
 import numpy as np
 import torch
@@ -671,7 +671,10 @@ class RmsNormOut:
     y: torch.Tensor                  # the normed rows
     h: torch.Tensor                  # x + residual, x itself without a residual
     rstd: torch.Tensor               # fp32, one per row
-    y8: Mx8Rows | None = None        # the normed rows in 8 bits, where they are kept
+    y8: Mx8Rows | None = None        # the normed rows in 8 bits (a call that does not keep them leaves these as they were)
+    # An x that stands in h is the caller's and no later call's output: which one it is, and the buffer whose place it took.
+    lent: torch.Tensor | None = field(default=None, repr=False, compare=False)
+    own_h: torch.Tensor | None = field(default=None, repr=False, compare=False)
 
 
 def _row_stride(t: torch.Tensor, cols: int) -> int:
@@ -695,23 +698,29 @@ def rms_norm(x: torch.Tensor, weight: torch.Tensor, residual: torch.Tensor | Non
         r_stride = _row_stride(residual, cols)
         ok = ok and r_stride >= 0 and residual.shape == shape and residual.dtype is dtype and residual.get_device() == index
     _require(ok, "rms_norm")
+    # (empty_like of a contiguous tensor: a third of the time on the host that a shape takes)
+    like = x if x_stride == cols and x.is_contiguous() else None
     if out is None:
         y8 = Mx8Rows(x.new_empty(shape, dtype=torch.uint8), x.new_empty((*shape[:-1], _mx_pitch(cols)), dtype=torch.uint8)) if keep else None
-        # (like a contiguous tensor: a third of the time on the host that a shape takes)
-        like = x if x_stride == cols and x.is_contiguous() else x.new_empty(shape)
-        out = RmsNormOut(torch.empty_like(like), x if residual is None else torch.empty_like(like),
+        h = None
+        out = RmsNormOut(x.new_empty(shape) if like is None else torch.empty_like(like), None,
                          torch.empty(shape[:-1], dtype=torch.float32, device=x.device), y8)
     else:
-        _require(_is_dense(out.y, dtype, shape, index) and (residual is None or _is_dense(out.h, dtype, shape, index))
+        h = out.h if out.lent is None or out.h is not out.lent else out.own_h
+        _require(_is_dense(out.y, dtype, shape, index) and (residual is None or h is None or _is_dense(h, dtype, shape, index))
                  and _is_dense(out.rstd, torch.float32, shape[:-1], index) and (not keep or _is_mx8(out.y8, index, shape)), "rms_norm")
-        if residual is None:
-            out.h = x
-    r_ptr, h_ptr = (0, 0) if residual is None else (residual.data_ptr(), out.h.data_ptr())
+    r_ptr, h_ptr = 0, 0
+    if residual is not None:
+        if h is None:
+            h = x.new_empty(shape) if like is None else torch.empty_like(like)
+        r_ptr, h_ptr = residual.data_ptr(), h.data_ptr()
     c_ptr, s_ptr = (out.y8.codes.data_ptr(), out.y8.scales.data_ptr()) if keep else (0, 0)
     st = _on_device(index, moe_rms_norm, x.data_ptr(), x_stride, r_ptr, r_stride, code, x.numel() // cols, cols, weight.data_ptr(), w_code, eps,
                     h_ptr, out.y.data_ptr(), out.rstd.data_ptr(), c_ptr, s_ptr, _raw_stream(index))
     if st != MOE_OK:
         raise MoeError(st, "moe_rms_norm")
+    out.own_h = h
+    out.h, out.lent = (x, x) if residual is None else (h, None)
     return out
 
 
