@@ -560,6 +560,22 @@ def _apart(outputs, inputs) -> bool:
     return True
 
 
+def _aligned16(*tensors) -> bool:
+    return not any(t is not None and t.data_ptr() & 15 for t in tensors)
+
+
+@functools.lru_cache(maxsize=256)
+def _network_status(n: int, n_in: int, cols: int, n_out: int, slots: int) -> int:
+    """What the C calls of a gated network on n rows say to its sizes (rows of n_in, two projections of cols / 2, n_out)."""
+    if n_in < 8 or n_in % 8 or cols < 32 or cols % 32 or n_out < 8 or n_out % 8:
+        return MOE_ERR_INVALID_ARG
+    most, tiles = 1 << 30, 1 << 29                              # expert_product_fits in csrc/expert_product.h
+    for a, b in ((cols, n_in), (n_out, cols // 2)):
+        if max(n, a, b) > most or a * b * 2 >= 1 << 39 or (max(a, b) + 127) // 128 * (slots + n // 32) >= tiles:
+            return MOE_ERR_CAPACITY
+    return MOE_OK
+
+
 def _is_mx8(m: Mx8Rows, index: int, shape) -> bool:
     """8-bit rows of the given logical shape on CUDA device `index`."""
     shape = tuple(shape)
@@ -1071,15 +1087,22 @@ class MoeRouter:
                    down: torch.Tensor, y: torch.Tensor | None = None, h: torch.Tensor | None = None,
                    z: "torch.Tensor | Mx8Rows | None" = None) -> torch.Tensor:
         """The gated feed-forward expert of every slot on its rows: expert_gated, then expert_product, refused before the
-        first launch where either would be."""
+        first launch where either would be, and where an output shares a byte with an input of either (``y`` may take the place
+        of ``rows``) or with another output."""
         dev, n, bf16 = self._index(), rows.shape[0], torch.bfloat16
         P, cols, n_in = gate_up.shape if gate_up.dim() == 3 else (0, 0, 0)
         n_out, n_hidden = down.shape[1] if down.dim() == 3 else 0, cols // 2
         _require(P == self.num_slots and cols > 0 and cols % 32 == 0 and _is_dense(gate_up, bf16, (P, cols, n_in), dev)
                  and _is_dense(down, bf16, (P, n_out, n_hidden), dev) and _is_dense(rows, bf16, (n, n_in), dev)
                  and self._slots_ok(slot_counts, slot_offsets, dev) and (z is None or self._kept_ok(z, n, cols, dev))
-                 and (y is None or (_is_dense(y, bf16, (n, n_out), dev) and _apart((y,), self._kept_tensors(z))))
-                 and (h is None or _is_dense(h, bf16, (n, n_hidden), dev)), "expert_ffn")
+                 and (y is None or _is_dense(y, bf16, (n, n_out), dev)) and (h is None or _is_dense(h, bf16, (n, n_hidden), dev)), "expert_ffn")
+        st = _network_status(n, n_in, cols, n_out, P)
+        if st != MOE_OK:
+            raise MoeError(st, "expert_ffn")
+        kept, read = self._kept_tensors(z), (gate_up, down, slot_counts, slot_offsets)
+        _require(n == 0 or (_aligned16(rows, gate_up, down, y, h, *kept)
+                            and ((z is None and h is None) or _apart((h, *kept), (rows, *read)))
+                            and (y is None or _apart((y,), (h, *kept, *read)))), "expert_ffn")
         if h is None:
             h = rows.new_empty((n, n_hidden))
         if y is None:

@@ -1,0 +1,173 @@
+"""CPU-only: calls that launch several operators are refused before the first launch where any of them would be, or where one of
+them would write what another reads.  Tensors are stand-ins, and so are the C calls, which refuse as the C code does."""
+import itertools
+import os
+import subprocess
+
+import pytest
+import torch
+
+from paper_2602_21140_b200 import binding as B
+from test_expert_binding import BF, E, F32, H, I, I32, K, N, P, T, U8, Fake, _at, _out, good, router, rows8  # noqa: F401
+
+OK, BAD, CAP = B.MOE_OK, B.MOE_ERR_INVALID_ARG, B.MOE_ERR_CAPACITY
+
+
+def _meet(outputs, inputs):
+    spans = [(a, a + n) for a, n in inputs if a]
+    for a, n in outputs:
+        if a and n:
+            if any(a < e and s < a + n for s, e in spans if s < e):
+                return True
+            spans.append((a, a + n))
+    return False
+
+
+def _askew(*pointers):
+    return any(p and p % 16 for p in pointers)
+
+
+def _sizes(rows, n_out, n_in):
+    if n_out < 8 or n_out % 8 or n_in < 8 or n_in % 8:
+        return BAD
+    for n, k in ((n_out, n_in), (n_in, n_out)):
+        if max(rows, n, k) > 1 << 30 or (n + 127) // 128 * (P + rows // 32) >= 1 << 29 or n * k * 2 >= 1 << 39:
+            return CAP
+    return OK
+
+
+def _kept(rows, cols, z, s):
+    return [(z or 0, rows * cols * (1 if s else 2)), (s or 0, rows * B._mx_pitch(cols) if s else 0)]
+
+
+class C:
+    """The C entry points of a network, as far as they refuse."""
+
+    def __init__(self):
+        self.launched = []
+
+    def _done(self, name, st):
+        if st == OK:
+            self.launched.append(name)
+        return st
+
+    def gated(self, ctx, a, rows, counts, offsets, w, hidden, n_in, h, z=0, s=0, stream=0):
+        st = _sizes(rows, 2 * hidden, n_in) if hidden >= 16 and hidden % 16 == 0 else BAD
+        if st == OK and rows:
+            bad = not h or _askew(a, w, h, z, s) or _meet([(h, rows * hidden * 2), *_kept(rows, 2 * hidden, z, s)],
+                                                          [(a, rows * n_in * 2), (w, P * hidden * n_in * 4), (counts, P * 4), (offsets, P * 4)])
+            st = BAD if bad else OK
+        return self._done("gated", st)
+
+    def product(self, ctx, a, rows, counts, offsets, w, n_out, n_in, y, stream=0):
+        st = _sizes(rows, n_out, n_in)
+        if st == OK and rows:
+            bad = not y or _askew(a, w, y) or _meet([(y, rows * n_out * 2)], [(a, rows * n_in * 2), (w, P * n_out * n_in * 2), (counts, P * 4), (offsets, P * 4)])
+            st = BAD if bad else OK
+        return self._done("product", st)
+
+
+@pytest.fixture
+def c(router, monkeypatch):  # noqa: F811
+    c = C()
+    monkeypatch.setattr(B, "moe_expert_gated", c.gated)
+    monkeypatch.setattr(B, "moe_expert_product", c.product)
+    return c
+
+
+def _forward():
+    g = good()
+    return {**g, "y": Fake((N, H), BF), "h": Fake((N, I), BF), "z": rows8(N, 2 * I)}
+
+
+def _moved(args, name, address):
+    """The same arguments, with `name` (of 8-bit rows "z.codes", "z.scales") at another address."""
+    key, _, part = name.partition(".")
+    t = getattr(args[key], part) if part else args[key]
+    moved = _at(t.shape, address, t.dtype)
+    if part:
+        z = args[key]
+        moved = B.Mx8Rows(moved, z.scales) if part == "codes" else B.Mx8Rows(z.codes, moved)
+    return {**args, key: moved}
+
+
+def _tensor(args, name):
+    key, _, part = name.partition(".")
+    return getattr(args[key], part) if part else args[key]
+
+
+def test_a_network_runs_with_its_buffers_apart(router, c):  # noqa: F811
+    for more in itertools.product((False, True), (False, True), (None, "8", "16")):
+        args = _forward()
+        y, h, kept = more
+        args["y"], args["h"] = args["y"] if y else None, args["h"] if h else None
+        args["z"] = {None: None, "8": args["z"], "16": Fake((N, 2 * I), BF)}[kept]
+        router.expert_ffn(**args)
+    assert c.launched == ["gated", "product"] * 12
+    args = _forward()
+    router.expert_ffn(**{**args, "y": args["rows"]})           # y in the place of the rows, which are read no more
+    empty = dict(rows=Fake((0, H), BF), y=_at((0, H), args["down"]._at), z=None, h=None)
+    router.expert_ffn(**{**args, **empty})                      # a buffer without rows shares no byte
+    assert c.launched == ["gated", "product"] * 14
+
+
+@pytest.mark.parametrize("kept", ["8", "16"])
+def test_a_networks_outputs_lie_nowhere_else(router, c, kept):  # noqa: F811
+    args = _forward()
+    outputs = ["y", "h"] + (["z.codes", "z.scales"] if kept == "8" else ["z"])
+    if kept == "16":
+        args["z"] = Fake((N, 2 * I), BF)
+    for out in outputs:
+        for other in ["rows", "gate_up", "down", "slot_counts", "slot_offsets"] + [o for o in outputs if o != out]:
+            t = _tensor(args, other)
+            for address in (t._at, t._at + t.numel() * t.element_size() - 16, t._at - 16):
+                if (out, other) == ("y", "rows") or address % 16:
+                    continue
+                with pytest.raises(B.MoeError):
+                    router.expert_ffn(**_moved(args, out, address))
+    assert c.launched == []
+
+
+def test_a_networks_alignment_and_sizes(router, c):  # noqa: F811
+    args = _forward()
+    for name in ("rows", "gate_up", "down", "y", "h", "z.codes", "z.scales"):
+        for off in (2, 8):
+            with pytest.raises(B.MoeError):
+                router.expert_ffn(**_moved(args, name, _tensor(args, name)._at + off))
+    router.expert_ffn(**_moved(args, "slot_counts", args["slot_counts"]._at + 4))
+    assert c.launched == ["gated", "product"]
+    c.launched.clear()
+    plain = {k: args[k] for k in ("rows", "slot_counts", "slot_offsets", "gate_up", "down")}
+    for n_out in (12, 4, 0, 7):
+        with pytest.raises(B.MoeError):
+            router.expert_ffn(**{**plain, "down": Fake((P, n_out, I), BF)})
+    for n_in in (12, 4, 0):
+        with pytest.raises(B.MoeError):
+            router.expert_ffn(**{**plain, "rows": Fake((N, n_in), BF), "gate_up": Fake((P, 2 * I, n_in), BF)})
+    for n, n_out in ((N, (1 << 30) + 8), ((1 << 30) + 1, H), (1 << 30, 1 << 22)):
+        with pytest.raises(B.MoeError) as e:
+            router.expert_ffn(**{**plain, "rows": Fake((n, H), BF), "down": Fake((P, n_out, I), BF)})
+        assert e.value.status == CAP
+    assert c.launched == []
+
+
+def _printed(tmp_path, header, expressions):
+    """The values of C++ expressions of ints."""
+    src, exe = tmp_path / "values.cu", tmp_path / "values"
+    body = "".join(f'printf("%d ", (int)({e}));' for e in expressions)
+    src.write_text(f'#include <stdio.h>\n#include "{header}"\nusing namespace moe;\nint main()\n{{\n{body}\nreturn 0;\n}}\n')
+    csrc = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2602_21140_b200", "csrc")
+    subprocess.check_call([os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc"), "-gencode", "arch=compute_100a,code=sm_100a", "-std=c++17", "-I", csrc,
+                           "-o", str(exe), str(src)])
+    return [int(v) for v in subprocess.check_output([str(exe)], text=True).split()]
+
+
+SPREAD = [(n, n_in, cols, n_out, P_) for n in (1, 4096, 1 << 30, (1 << 30) + 1) for n_in in (8, 1 << 15, 1 << 19, 1 << 24) for cols in (32, 1 << 20, 1 << 25)
+          for n_out in (8, 1 << 15, 1 << 23, 1 << 30, (1 << 30) + 8) for P_ in (1, 36, 4096)]
+
+
+def test_the_sizes_that_the_binding_lets_through_are_those_of_the_c_code(tmp_path):
+    want = _printed(tmp_path, "expert_product.h", [" && ".join(f"expert_product_fits({n}ll, {a}ll, {b}ll, {p})" for x, y in ((cols, n_in), (n_out, cols // 2))
+                                                               for a, b in ((x, y), (y, x))) for n, n_in, cols, n_out, p in SPREAD])
+    got = [B._network_status(*sizes) for sizes in SPREAD]
+    assert got == [OK if w else CAP for w in want] and 0 < sum(want) < len(want)
