@@ -565,13 +565,16 @@ def _aligned16(*tensors) -> bool:
 
 
 @functools.lru_cache(maxsize=256)
-def _network_status(n: int, n_in: int, cols: int, n_out: int, slots: int) -> int:
-    """What the C calls of a gated network on n rows say to its sizes (rows of n_in, two projections of cols / 2, n_out)."""
+def _network_status(n: int, n_in: int, cols: int, n_out: int, slots: int, grads: bool = False) -> int:
+    """What the C calls of a gated network on n rows, or of its gradients, say to its sizes (rows of n_in, two projections of
+    cols / 2, n_out)."""
     if n_in < 8 or n_in % 8 or cols < 32 or cols % 32 or n_out < 8 or n_out % 8:
         return MOE_ERR_INVALID_ARG
-    most, tiles = 1 << 30, 1 << 29                              # expert_product_fits in csrc/expert_product.h
+    most, tiles = 1 << 30, 1 << 29                              # expert_product_fits, weight_grad_fits in csrc/expert_product.h
     for a, b in ((cols, n_in), (n_out, cols // 2)):
         if max(n, a, b) > most or a * b * 2 >= 1 << 39 or (max(a, b) + 127) // 128 * (slots + n // 32) >= tiles:
+            return MOE_ERR_CAPACITY
+        if grads and ((a + 255) // 256 * ((b + 255) // 256) >= tiles // slots or a * b * 4 >= 1 << 39):
             return MOE_ERR_CAPACITY
     return MOE_OK
 
@@ -1194,6 +1197,11 @@ class MoeRouter:
                  and (d_rows is None or _is_dense(d_rows, bf16, (n, n_in), dev)) and g_type in (bf16, f32) and d_type in (bf16, f32)
                  and _is_dense(d_gate_up, g_type, (P, cols, n_in), dev) and _is_dense(d_down, d_type, (P, n_out, n_hidden), dev)
                  and add_ok and apart, "expert_ffn_backward")
+        st = _network_status(n, n_in, cols, n_out, P, True)
+        if st != MOE_OK:
+            raise MoeError(st, "expert_ffn_backward")
+        _require(_aligned16(d_gate_up, d_down) and (n == 0 or _aligned16(dy, rows, gate_up, down, d_rows, *self._kept_tensors(z))),
+                 "expert_ffn_backward")
         if d_rows is None:
             d_rows = torch.empty_like(rows)
         dz, h = dy.new_empty((n, cols)), dy.new_empty((n, n_hidden))

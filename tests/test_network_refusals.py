@@ -66,12 +66,42 @@ class C:
             st = BAD if bad else OK
         return self._done("product", st)
 
+    def gated_backward(self, ctx, dy, rows, counts, offsets, w, n_out, hidden, z, s, dz, h, stream=0):
+        st = _sizes(rows, n_out, hidden) if hidden >= 16 and hidden % 16 == 0 else BAD
+        if st == OK and rows:
+            bad = not z or not dz or not h or _askew(dy, w, z, s, dz, h) or _meet(
+                [(dz, rows * hidden * 4), (h, rows * hidden * 2)],
+                [(dy, rows * n_out * 2), (w, P * n_out * hidden * 2), *_kept(rows, 2 * hidden, z, s), (counts, P * 4), (offsets, P * 4)])
+            st = BAD if bad else OK
+        return self._done("gated_backward", st)
+
+    def weight_backward(self, ctx, dy, a, rows, counts, offsets, n_out, n_in, dw, dtype, add, stream=0):
+        if n_out < 8 or n_out % 8 or n_in < 8 or n_in % 8 or (add and dtype != B.MOE_DTYPE_F32):
+            return BAD
+        if max(rows, n_out, n_in) > 1 << 30 or (n_out + 255) // 256 * ((n_in + 255) // 256) >= (1 << 29) // P or n_out * n_in * 4 >= 1 << 39:
+            return CAP
+        size = P * n_out * n_in * (4 if dtype == B.MOE_DTYPE_F32 else 2)
+        bad = not dw or _askew(dw)
+        if rows:
+            bad = bad or _askew(dy, a) or _meet([(dw, size)], [(dy, rows * n_out * 2), (a, rows * n_in * 2), (counts, P * 4), (offsets, P * 4)])
+        return self._done("weight_backward", BAD if bad else OK)
+
+    def rows_backward(self, ctx, dy, rows, counts, offsets, w, n_out, n_in, da, stream=0):
+        st = _sizes(rows, n_out, n_in)
+        if st == OK and rows:
+            bad = not da or _askew(dy, w, da) or _meet([(da, rows * n_in * 2)],
+                                                       [(dy, rows * n_out * 2), (w, P * n_out * n_in * 2), (counts, P * 4), (offsets, P * 4)])
+            st = BAD if bad else OK
+        return self._done("rows_backward", st)
+
 
 @pytest.fixture
 def c(router, monkeypatch):  # noqa: F811
     c = C()
     monkeypatch.setattr(B, "moe_expert_gated", c.gated)
     monkeypatch.setattr(B, "moe_expert_product", c.product)
+    for name in ("gated_backward", "weight_backward", "rows_backward"):
+        monkeypatch.setattr(B, "moe_expert_" + name, getattr(c, name))
     return c
 
 
@@ -166,8 +196,48 @@ SPREAD = [(n, n_in, cols, n_out, P_) for n in (1, 4096, 1 << 30, (1 << 30) + 1) 
           for n_out in (8, 1 << 15, 1 << 23, 1 << 30, (1 << 30) + 8) for P_ in (1, 36, 4096)]
 
 
+BACKWARD = ["gated_backward", "weight_backward", "weight_backward", "rows_backward"]
+
+
+def _backward():
+    g = good()
+    return {"dy": Fake((N, H), BF), **g, "z": rows8(N, 2 * I), "d_rows": Fake((N, H), BF), "d_gate_up": Fake((P, 2 * I, H), F32),
+            "d_down": Fake((P, H, I), F32)}
+
+
+def test_a_networks_gradients_alignment_and_sizes(router, c):  # noqa: F811
+    """Nothing is added to one matrix's gradient in a call that another operator refuses."""
+    args = _backward()
+    router.expert_ffn_backward(**args, add=True)
+    assert c.launched == BACKWARD
+    c.launched.clear()
+    for name in ("dy", "rows", "gate_up", "down", "z.codes", "z.scales", "d_rows", "d_gate_up", "d_down"):
+        for off in (4, 8):
+            with pytest.raises(B.MoeError):
+                router.expert_ffn_backward(**_moved(args, name, _tensor(args, name)._at + off), add=True)
+    plain = {k: args[k] for k in ("dy", "rows", "slot_counts", "slot_offsets", "gate_up", "down", "z")}
+    for n_out in (12, 4, 0):
+        with pytest.raises(B.MoeError):
+            router.expert_ffn_backward(**{**plain, "dy": Fake((N, n_out), BF), "down": Fake((P, n_out, I), BF)})
+    for n_in in (12, 4, 0):
+        with pytest.raises(B.MoeError):
+            router.expert_ffn_backward(**{**plain, "rows": Fake((N, n_in), BF), "gate_up": Fake((P, 2 * I, n_in), BF)})
+    wide = 1 << 23                                             # its gradient's tiles are more than eight slots may have
+    for more in (dict(dy=Fake((N, (1 << 30) + 8), BF), down=Fake((P, (1 << 30) + 8, I), BF)),
+                 dict(rows=Fake((N, 1 << 20), BF), gate_up=Fake((P, wide, 1 << 20), BF), down=Fake((P, H, wide // 2), BF), z=Fake((N, wide), BF))):
+        with pytest.raises(B.MoeError) as e:
+            router.expert_ffn_backward(**{**plain, **more})
+        assert e.value.status == CAP
+    assert c.launched == []
+
+
 def test_the_sizes_that_the_binding_lets_through_are_those_of_the_c_code(tmp_path):
     want = _printed(tmp_path, "expert_product.h", [" && ".join(f"expert_product_fits({n}ll, {a}ll, {b}ll, {p})" for x, y in ((cols, n_in), (n_out, cols // 2))
                                                                for a, b in ((x, y), (y, x))) for n, n_in, cols, n_out, p in SPREAD])
     got = [B._network_status(*sizes) for sizes in SPREAD]
     assert got == [OK if w else CAP for w in want] and 0 < sum(want) < len(want)
+    grads = _printed(tmp_path, "expert_product.h", [" && ".join(f"weight_grad_fits({n}ll, {a}ll, {b}ll, {p})" for a, b in ((cols, n_in), (n_out, cols // 2)))
+                                                    for n, n_in, cols, n_out, p in SPREAD])
+    got = [B._network_status(*sizes, True) for sizes in SPREAD]
+    both = [w and g for w, g in zip(want, grads)]
+    assert got == [OK if b else CAP for b in both] and sum(both) < sum(want)
