@@ -548,12 +548,17 @@ def _is_mx(m: MxRows, index: int, lead=None) -> bool:
             and ss[-1] == _mx_pitch(2 * cs[-1]) and (lead is None or cs[:-1] == lead))
 
 
+def _span(t: torch.Tensor):
+    at = t.data_ptr()
+    return at, at + t.numel() * t.element_size()
+
+
 def _apart(outputs, inputs) -> bool:
-    """Whether contiguous output tensors (None: not given) share no byte with inputs or with one another."""
-    taken = [(t.data_ptr(), t.data_ptr() + t.numel() * t.element_size()) for t in inputs if t is not None]
+    """Whether contiguous output tensors (None: not given) share no byte with inputs or with one another.  (One without elements has none.)"""
+    taken = [_span(t) for t in inputs if t is not None and t.numel()]
     for t in outputs:
-        if t is not None:
-            at, end = t.data_ptr(), t.data_ptr() + t.numel() * t.element_size()
+        if t is not None and t.numel():
+            at, end = _span(t)
             if any(at < e and b < end for b, e in taken):
                 return False
             taken.append((at, end))

@@ -205,6 +205,16 @@ def _backward():
             "d_down": Fake((P, H, I), F32)}
 
 
+def test_buffers_without_rows_lie_anywhere(router, c):  # noqa: F811
+    """Slices of no rows of buffers that are in use."""
+    args = _backward()
+    for name in ("gate_up", "down", "d_gate_up", "d_down"):
+        inside = args[name]._at + 64
+        none = dict(dy=_at((0, H), inside), rows=_at((0, H), inside), d_rows=_at((0, H), inside), z=_at((0, 2 * I), inside))
+        router.expert_ffn_backward(**{**args, **none}, add=True)
+    assert c.launched == BACKWARD * 4
+
+
 def test_a_networks_gradients_alignment_and_sizes(router, c):  # noqa: F811
     """Nothing is added to one matrix's gradient in a call that another operator refuses."""
     args = _backward()
