@@ -909,6 +909,11 @@ class MoeRouter:
                 return False
         return True
 
+    @staticmethod
+    def _index_buffers(out: DispatchBuffers):
+        return (out.topk_ids, out.topk_weights, out.topk_slot, out.slot_counts, out.slot_offsets, out.rank_counts, out.rank_offsets, out.dst_row,
+                out.src_index)
+
     def _segments_ok(self, rows: MxRows, slot_counts, slot_offsets, weight: MxRows, dev: int) -> bool:
         P, w = self.num_slots, weight.codes.shape
         return (_is_mx(rows, dev) and len(rows.codes.shape) == 2 and _is_mx(weight, dev) and len(w) == 3 and w[0] == P
@@ -1234,7 +1239,9 @@ class MoeRouter:
                     out: DispatchBuffers | None = None, y: torch.Tensor | None = None, buf: torch.Tensor | None = None,
                     z: "torch.Tensor | Mx8Rows | None" = None) -> torch.Tensor:
         """One whole layer with experts in 16 bits: dispatch, the experts, and the combine (times slot_scale, as always).
-        For expert_step_backward keep ``out``, the experts' outputs ``buf`` [T * k, H] and their projections ``z``."""
+        For expert_step_backward keep ``out``, the experts' outputs ``buf`` [T * k, H] and their projections ``z``.  Outputs share no
+        byte with inputs, matrices, ``out`` or one another, but ``y`` may take the place of ``x``, and ``buf`` and ``y`` that of the
+        send buffer (a backward pass then needs its rows in 8 bits)."""
         T, H, k, dev = x.shape[0], self.cfg.hidden, self.cfg.top_k, self._index()
         # before the first launch: dispatch and combine take the sizes of their buffers on trust
         _require(self._networks_ok(gate_up, down) and _is_dense(x, torch.bfloat16, (T, H), dev)
@@ -1243,6 +1250,15 @@ class MoeRouter:
                  and (z is None or self._kept_ok(z, T * k, gate_up.shape[1], dev))
                  and (out is None or (self._outputs_ok(out, T, dev) and out.send_buf is not None
                                       and _is_dense(out.send_buf, torch.bfloat16, (T * k, H), dev))), "expert_step")
+        st = _network_status(T * k, H, gate_up.shape[1], H, self.num_slots)
+        if st != MOE_OK:
+            raise MoeError(st, "expert_step")
+        kept = self._kept_tensors(z)
+        send, index = (None, ()) if out is None else (out.send_buf, self._index_buffers(out))
+        read = (logits, gate_up, down, *index)
+        _require(T == 0 or (_aligned16(gate_up, down, send, y, buf, *kept)
+                            and (z is None or _apart(kept, (x, send, *read))) and (buf is None or _apart((buf,), (x, *kept, *read)))
+                            and (y is None or _apart((y,), (buf, *kept, *read)))), "expert_step")
         out = _on_device(dev, self.dispatch, logits, x, out)
         buf = self.expert_ffn(out.send_buf, out.slot_counts, out.slot_offsets, gate_up, down, buf, z=z)
         return _on_device(dev, self.combine, buf, T, y)

@@ -94,12 +94,21 @@ class C:
             st = BAD if bad else OK
         return self._done("rows_backward", st)
 
+    def dispatch(self, ctx, logits, x, tokens, out, stream=0):
+        return self._done("dispatch", BAD if tokens and _askew(logits, x, out.send_buf) else OK)
+
+    def combine(self, ctx, buf, tokens, y, stream=0):
+        return self._done("combine", BAD if tokens and _askew(buf, y) else OK)
+
 
 @pytest.fixture
 def c(router, monkeypatch):  # noqa: F811
     c = C()
     monkeypatch.setattr(B, "moe_expert_gated", c.gated)
     monkeypatch.setattr(B, "moe_expert_product", c.product)
+    for name in ("dispatch", "combine"):
+        monkeypatch.setattr(B, "moe_" + name, getattr(c, name))
+    monkeypatch.setattr(torch, "empty", lambda shape, dtype, device: Fake((shape,) if isinstance(shape, int) else shape, dtype))
     for name in ("gated_backward", "weight_backward", "rows_backward"):
         monkeypatch.setattr(B, "moe_expert_" + name, getattr(c, name))
     return c
@@ -179,6 +188,49 @@ def test_a_networks_alignment_and_sizes(router, c):  # noqa: F811
             router.expert_ffn(**{**plain, "rows": Fake((n, H), BF), "down": Fake((P, n_out, I), BF)})
         assert e.value.status == CAP
     assert c.launched == []
+
+
+STEP = ["dispatch", "gated", "product", "combine"]
+
+
+def _step(kept="8"):
+    g = good()
+    return dict(logits=Fake((T, E), F32), x=Fake((T, H), BF), gate_up=g["gate_up"], down=g["down"], out=_out(), y=Fake((T, H), BF), buf=Fake((N, H), BF),
+                z=rows8(N, 2 * I) if kept == "8" else Fake((N, 2 * I), BF))
+
+
+INDEX = ["topk_ids", "topk_weights", "topk_slot", "slot_counts", "slot_offsets", "rank_counts", "rank_offsets", "dst_row", "src_index"]
+
+
+def test_a_step_runs_with_its_buffers_apart(router, c):  # noqa: F811
+    args = _step()
+    router.expert_step(**args)
+    router.expert_step(**{**args, "out": None, "y": None, "buf": None, "z": None})
+    router.expert_step(**{**args, "y": args["x"]})
+    router.expert_step(**{**args, "buf": args["out"].send_buf})
+    router.expert_step(**{**args, "y": _at((T, H), args["out"].send_buf._at)})
+    assert c.launched == STEP * 5
+
+
+@pytest.mark.parametrize("kept", ["8", "16"])
+def test_a_steps_outputs_lie_nowhere_else(router, c, kept):  # noqa: F811
+    """Seen before the dispatch, which would become the latest one."""
+    args = _step(kept)
+    outputs = ["y", "buf"] + (["z.codes", "z.scales"] if kept == "8" else ["z"])
+    fine = {("y", "x"), ("y", "out.send_buf"), ("buf", "out.send_buf")}
+    for o in outputs:
+        for other in ["logits", "x", "gate_up", "down", "out.send_buf"] + ["out." + i for i in INDEX] + [q for q in outputs if q != o]:
+            if (o, other) not in fine:
+                with pytest.raises(B.MoeError):
+                    router.expert_step(**_moved(args, o, _tensor(args, other)._at))
+    for name in outputs + ["gate_up", "down"]:
+        with pytest.raises(B.MoeError):
+            router.expert_step(**_moved(args, name, _tensor(args, name)._at + 8))
+    askew = _out()
+    askew.send_buf = _at((N, H), askew.send_buf._at + 8)
+    with pytest.raises(B.MoeError):
+        router.expert_step(**{**args, "out": askew})
+    assert c.launched == [] and router._latest is None
 
 
 def _printed(tmp_path, header, expressions):
