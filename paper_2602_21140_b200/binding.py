@@ -1267,13 +1267,19 @@ class MoeRouter:
                              buf: torch.Tensor, z: "torch.Tensor | Mx8Rows", gate_up: torch.Tensor, down: torch.Tensor,
                              d_gate_up: torch.Tensor | None = None, d_down: torch.Tensor | None = None, add: bool = False,
                              grad_dtype: torch.dtype = torch.bfloat16):
-        """Gradients of the latest expert_step: (dx, d_logits, d_gate_up, d_down).  ``rows``: its send buffer, or its tokens' rows
-        x in 8 bits (rms_norm's ``y8``).  d_logits is None for dense-FFN routing, whose weights are constants."""
-        T, H, dev = dy.shape[0], self.cfg.hidden, self._index()
+        """Gradients of the latest expert_step: (dx, d_logits, d_gate_up, d_down).  ``rows``: its send buffer (where ``buf`` has
+        not taken its place), or its tokens' rows x in 8 bits (rms_norm's ``y8``).  d_logits is None for dense-FFN routing,
+        whose weights are constants.  Refused before a gradient is written where any of its operators would be."""
+        T, H, E, dev, score = dy.shape[0], self.cfg.hidden, self.cfg.num_experts, self._index(), self.cfg.score_func
         # the gradients of combine and dispatch take the context's latest dispatch: it has to be this one
         _require(self._latest is not None and self._latest[3] is out.dst_row
                  and self._networks_ok(gate_up, down) and _is_dense(dy, torch.bfloat16, (T, H), dev) and self._outputs_ok(out, T, dev)
-                 and self._kept_ok(z, T * self.cfg.top_k, gate_up.shape[1], dev), "expert_step_backward")
+                 and self._kept_ok(z, T * self.cfg.top_k, gate_up.shape[1], dev)
+                 and (score != MOE_SCORE_SIGMOID if logits is None else _is_dense(logits, torch.float32, (T, E), dev))
+                 and (isinstance(rows, Mx8Rows) or _apart((buf,), (rows,)))
+                 and ((d_gate_up is None and d_down is None)
+                      or _apart((d_gate_up, d_down), (logits, dy, buf, *self._kept_tensors(rows), *self._index_buffers(out)))),
+                 "expert_step_backward")
         d_buf, d_weights = self.combine_backward(buf, dy)
         if isinstance(rows, Mx8Rows):
             rows = self.redispatch(rows)

@@ -44,7 +44,7 @@ class C:
     """The C entry points of a network, as far as they refuse."""
 
     def __init__(self):
-        self.launched = []
+        self.launched, self.score = [], B.MOE_SCORE_SOFTMAX
 
     def _done(self, name, st):
         if st == OK:
@@ -97,6 +97,17 @@ class C:
     def dispatch(self, ctx, logits, x, tokens, out, stream=0):
         return self._done("dispatch", BAD if tokens and _askew(logits, x, out.send_buf) else OK)
 
+    def combine_backward(self, ctx, buf, dy, tokens, d_buf, d_weights, stream=0):
+        return self._done("combine_backward", BAD if tokens and _askew(buf, dy, d_buf) else OK)
+
+    def redispatch(self, ctx, codes, scales, tokens, send, stream=0):
+        return self._done("redispatch", BAD if tokens and _askew(codes, scales, send) else OK)
+
+    def dispatch_backward(self, ctx, logits, d_send, d_weights, tokens, dx, d_logits, stream=0):
+        bad = bool(d_weights) != bool(d_logits) or (d_logits and self.score == B.MOE_ROUTE_DENSE_TP)
+        bad = bad or (tokens and (_askew(d_send, dx, d_logits) or (d_logits and self.score == B.MOE_SCORE_SIGMOID and not logits)))
+        return self._done("dispatch_backward", BAD if bad else OK)
+
     def combine(self, ctx, buf, tokens, y, stream=0):
         return self._done("combine", BAD if tokens and _askew(buf, y) else OK)
 
@@ -106,7 +117,7 @@ def c(router, monkeypatch):  # noqa: F811
     c = C()
     monkeypatch.setattr(B, "moe_expert_gated", c.gated)
     monkeypatch.setattr(B, "moe_expert_product", c.product)
-    for name in ("dispatch", "combine"):
+    for name in ("dispatch", "combine", "combine_backward", "redispatch", "dispatch_backward"):
         monkeypatch.setattr(B, "moe_" + name, getattr(c, name))
     monkeypatch.setattr(torch, "empty", lambda shape, dtype, device: Fake((shape,) if isinstance(shape, int) else shape, dtype))
     for name in ("gated_backward", "weight_backward", "rows_backward"):
@@ -191,6 +202,7 @@ def test_a_networks_alignment_and_sizes(router, c):  # noqa: F811
 
 
 STEP = ["dispatch", "gated", "product", "combine"]
+BACKWARD = ["gated_backward", "weight_backward", "weight_backward", "rows_backward"]
 
 
 def _step(kept="8"):
@@ -233,6 +245,57 @@ def test_a_steps_outputs_lie_nowhere_else(router, c, kept):  # noqa: F811
     assert c.launched == [] and router._latest is None
 
 
+def _step_backward(args, rows):
+    return dict(logits=args["logits"], dy=Fake((T, H), BF), rows=rows, out=args["out"], buf=args["buf"], z=args["z"], gate_up=args["gate_up"],
+                down=args["down"], d_gate_up=Fake((P, 2 * I, H), F32), d_down=Fake((P, H, I), F32))
+
+
+ALL_BACK = ["combine_backward", "redispatch", *BACKWARD, "dispatch_backward"]
+
+
+def test_a_steps_gradients_are_refused_before_one_is_written(router, c):  # noqa: F811
+    """With add=True a caller that tries again must not have added anything."""
+    args = _step()
+    router.expert_step(**args)
+    c.launched.clear()
+    from8, from16 = _step_backward(args, rows8(T, H)), _step_backward(args, args["out"].send_buf)
+    router.expert_step_backward(**from8, add=True)
+    router.expert_step_backward(**from16, add=True)
+    router.expert_step_backward(**{**from8, "logits": None}, add=True)   # softmax: logits are for masked ones only
+    without = [s for s in ALL_BACK if s != "redispatch"]
+    assert c.launched == ALL_BACK + without + ALL_BACK
+    c.launched.clear()
+    for back in (from8, from16):
+        for bad in (Fake((T, E - 1), F32), Fake((T, E), BF), Fake((T - 1, E), F32), Fake((T, E), F32, device=1), Fake((T, E), F32, contiguous=False)):
+            with pytest.raises(B.MoeError):
+                router.expert_step_backward(**{**back, "logits": bad}, add=True)
+        for grad in ("d_gate_up", "d_down"):
+            others = ["logits", "dy", "buf", "gate_up", "down", "z.codes", "z.scales"] + ["out." + i for i in INDEX]
+            for other in others + (["rows.codes", "rows.scales"] if back is from8 else ["rows"]):
+                with pytest.raises(B.MoeError):
+                    router.expert_step_backward(**_moved(back, grad, _tensor(back, other)._at), add=True)
+            with pytest.raises(B.MoeError):
+                router.expert_step_backward(**_moved(back, grad, back[grad]._at + 4), add=True)
+    router.cfg.score_func = c.score = B.MOE_SCORE_SIGMOID
+    with pytest.raises(B.MoeError):
+        router.expert_step_backward(**{**from8, "logits": None}, add=True)
+    assert not set(c.launched) & {*BACKWARD, "dispatch_backward"}
+
+
+def test_outputs_in_the_place_of_the_rows_that_a_backward_pass_asks_for(router, c):  # noqa: F811
+    """buf over the send buffer leaves no rows but those in 8 bits."""
+    args = _step()
+    args["buf"] = args["out"].send_buf
+    router.expert_step(**args)
+    c.launched.clear()
+    for rows in (args["out"].send_buf, _at((N, H), args["buf"]._at), _at((N, H), args["buf"]._at + 2 * H)):
+        with pytest.raises(B.MoeError):
+            router.expert_step_backward(**_step_backward(args, rows))
+    assert c.launched == []
+    router.expert_step_backward(**_step_backward(args, rows8(T, H)))
+    assert c.launched == ALL_BACK
+
+
 def _printed(tmp_path, header, expressions):
     """The values of C++ expressions of ints."""
     src, exe = tmp_path / "values.cu", tmp_path / "values"
@@ -246,9 +309,6 @@ def _printed(tmp_path, header, expressions):
 
 SPREAD = [(n, n_in, cols, n_out, P_) for n in (1, 4096, 1 << 30, (1 << 30) + 1) for n_in in (8, 1 << 15, 1 << 19, 1 << 24) for cols in (32, 1 << 20, 1 << 25)
           for n_out in (8, 1 << 15, 1 << 23, 1 << 30, (1 << 30) + 8) for P_ in (1, 36, 4096)]
-
-
-BACKWARD = ["gated_backward", "weight_backward", "weight_backward", "rows_backward"]
 
 
 def _backward():
