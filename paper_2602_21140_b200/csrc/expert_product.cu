@@ -278,12 +278,22 @@ __device__ __forceinline__ void clear_tail(unsigned char *stage, int bytes, int 
     __syncwarp();
 }
 
-// Bounded wait.  `quit` is shared by the CTA: the first role that gives up sets it, the others follow.
+// Tells the roles of both CTAs to leave.  (The other CTA is there: neither passes the last cluster_sync alone.)
+__device__ __forceinline__ void give_up(volatile int *quit)
+{
+    *quit = 1;
+    asm volatile("{\n\t.reg .u32 a;\n\tmapa.shared::cluster.u32 a, %0, %1;\n\tst.shared::cluster.u32 [a], %2;\n\t}" ::"r"(
+                     smem_addr(const_cast<int *>(quit))),
+                 "r"(cluster_rank() ^ 1u), "r"(1)
+                 : "memory");
+}
+
+// Bounded wait.  `quit` is shared by the CTA: the first role that gives up sets it in both, the others follow.
 __device__ __forceinline__ bool wait_for(uint64_t *bar, unsigned parity, volatile int *quit, unsigned limit)
 {
     unsigned spins = 0;
     while (!mbar_try_wait(bar, parity)) {
-        if (++spins > limit || ((spins & 63u) == 0 && *quit)) { *quit = 1; return false; }
+        if (++spins > limit || ((spins & 63u) == 0 && *quit)) { give_up(quit); return false; }
     }
     return true;
 }
@@ -704,7 +714,7 @@ k_expert_product(const __grid_constant__ CUtensorMap map_a, const __grid_constan
     // would be reported and no tile touched.)
     constexpr uint32_t tmem = 0;
     const bool whole = *tmem_slot == 0;
-    if (tid == 0 && !whole) *quit = 1;
+    if (tid == 0 && !whole) give_up(quit);
     if (!kGrad) {
         tiles = ends[p.P - 1];
         // counts that no dispatch writes: nothing is touched
@@ -720,6 +730,7 @@ k_expert_product(const __grid_constant__ CUtensorMap map_a, const __grid_constan
     // with six (32 slots of 64 rows, 4096 x 2048: gradient by the rows 184 us, with nine 190).
     const int stage_bytes = !L::kAAlongK || most_rows > 128 ? L::kStage : kATile + (most_rows > 64 ? 64 : 32) * kLine;
     const int stages = min(kMaxStages, p.ring / stage_bytes);
+    int issued = 0;                                            // stages that this warp has asked for
 
     if (warp < kEpiWarps) {
         if (FINE) asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
@@ -874,7 +885,7 @@ k_expert_product(const __grid_constant__ CUtensorMap map_a, const __grid_constan
         // take is uniform over the warp, and issue from one elected lane.
         if (FINE) asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
         if (warp == kTmaWarp) {
-            int issued = 0, s = 0;
+            int s = 0;
             const uint32_t lead = lead_addr<CG>(full);             // the first CTA's barrier counts the bytes of both
             unsigned parity = 1;                                   // a fresh barrier passes the wait for parity 1
             bool ok = true;
@@ -921,12 +932,6 @@ k_expert_product(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                     ++issued;
                     if (++s == stages) { s = 0; parity ^= 1u; }
                 }
-            }
-            if (!ok) {
-                // loads in flight still land in this CTA's shared memory: a bounded wait for them (the barriers may be the
-                // other CTA's, so they may not complete, but the wait outlasts any copy)
-                unsigned long long until = 0;
-                for (int m = max(0, issued - stages); m < issued; ++m) drain_wait(&full[m % stages], (unsigned)(m / stages) & 1u, until);
             }
         } else if (warp == kMmaWarp && rank == 0) {
             int s = 0, buf = 0;
@@ -1014,7 +1019,17 @@ k_expert_product(const __grid_constant__ CUtensorMap map_a, const __grid_constan
     __syncwarp();
     tc_fence_before();
     cluster_sync();                                            // the pair leaves together: neither arrives on a CTA that is gone
-    if (tid == 0 && *quit) report_status(p.ctl, kDevTimeout);
+    if (*quit) {                                               // in both CTAs or in none
+        // Whichever role gave up, loads may be in flight to this CTA's shared memory, with the first one's barriers: a bounded
+        // wait for them before either leaves (the barriers may not complete, but the wait outlasts any copy)
+        if (warp == kTmaWarp) {
+            unsigned long long until = 0;
+            for (int m = max(0, issued - stages); m < issued; ++m) drain_wait(&full[m % stages], (unsigned)(m / stages) & 1u, until);
+        }
+        __syncwarp();
+        cluster_sync();
+        if (tid == 0) report_status(p.ctl, kDevTimeout);
+    }
     if (warp == kMmaWarp) {
         if (rank == 1) {                                       // the first CTA's last arrival is on its way here as well
             unsigned long long until = 0;

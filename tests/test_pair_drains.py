@@ -1,0 +1,40 @@
+"""CPU-only, read off the source: a pair of CTAs whose roles give up.  A copy that one role asked for may be on its way when
+another, which waits for it, gives up, in the same CTA or in the other: both CTAs stay until it has landed."""
+import re
+
+import pytest
+
+from test_drains import _code
+
+PAIRS = ["expert_product.cu"]
+
+
+def _function(code, name):
+    body = code[code.index(name):]
+    return body[:body.index("\n}\n")]
+
+
+@pytest.mark.parametrize("name", PAIRS)
+def test_whoever_gives_up_tells_both_ctas(name):
+    code = _code(name)
+    wait = _function(code, "bool wait_for(")
+    assert re.search(r"give_up\(quit\);\s*return false", wait) and "*quit = 1" not in wait
+    told = _function(code, "void give_up(")
+    assert "*quit = 1" in told and "mapa.shared::cluster" in told and "st.shared::cluster" in told and "cluster_rank() ^ 1u" in told
+    # nobody sets the flag in another way
+    assert len(re.findall(r"\*quit = 1", code)) == 1 and len(re.findall(r"\*quit = 0", code)) == 1
+
+
+@pytest.mark.parametrize("name", PAIRS)
+def test_both_ctas_stay_until_copies_have_landed(name):
+    code = _code(name)
+    end = code[code.rindex("tc_fence_before();\n    cluster_sync();"):]
+    end = end[:end.index("tmem_dealloc")]
+    # the verdict is read behind the meeting of the pair, so it is the same in both
+    m = re.search(r"cluster_sync\(\);\s*if \(\*quit\) \{(.*?)\n    \}\n", end, re.S)
+    assert m, end
+    body = m.group(1)
+    assert re.search(r"warp == kTmaWarp.*drain_wait\(&full\[", body, re.S)
+    assert body.index("drain_wait") < body.index("cluster_sync();") < body.index("report_status")
+    # and no role's own verdict decides about its copies
+    assert not re.search(r"if \(!ok\) \{[^}]*drain_wait\(&full", code)
