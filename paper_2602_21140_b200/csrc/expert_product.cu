@@ -999,14 +999,17 @@ k_expert_product(const __grid_constant__ CUtensorMap map_a, const __grid_constan
             // 128 x 511 rows 1488 us instead of 1054; such an arrival on every stage: 510 TFLOP/s.)
             int s = 0;
             unsigned tail_parity = 0;                              // a bit per stage, of its next use
+            unsigned patience = 0;                                 // a wait begins while the tiles without such an end before it are worked on
             bool ok = true;
             Tile t;
             for (TileStream<OP> stream(p, ends, tiles); ok && stream.next(t);) {
                 const int steps = (t.rows + kStageK - 1) / kStageK, left = t.rows - (steps - 1) * kStageK;
+                patience = more_patience(patience, p.spin_limit, steps);
                 if (steps > 0 && has_tail(left)) {
                     const int at = (s + steps - 1) % stages;
-                    ok = __all_sync(0xffffffffu, wait_for(&tail[at], (tail_parity >> at) & 1u, quit, p.spin_limit));
+                    ok = __all_sync(0xffffffffu, wait_for(&tail[at], (tail_parity >> at) & 1u, quit, max(p.spin_limit, patience)));
                     if (!ok) break;
+                    patience = 0;
                     tail_parity ^= 1u << at;
                     clear_tail(stage + at * stage_bytes, stage_bytes, left, lane);
                     if (lane == 0) mbar_arrive_lead<CG>(&peer[at]);

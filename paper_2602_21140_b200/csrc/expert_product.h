@@ -51,6 +51,15 @@ inline bool weight_grad_fits(long long rows, long long m, long long n, int P)
     return (m + 255) / 256 * ((n + 255) / 256) < kTooManyTiles / P && m * n * 4 < (1ll << 39);
 }
 
+// Polls allowed to a wait that lasts through several tiles: `so_far`, and for one more of `steps` stages what a role that works on it
+// is allowed for the tile and its stages (a stage takes 512 clocks, a poll 20 or more).  Bounded, and without overflow.
+constexpr unsigned kMostPatience = 1u << 30;
+__host__ __device__ inline unsigned more_patience(unsigned so_far, unsigned spin_limit, int steps)
+{
+    const unsigned tile = (spin_limit < kMostPatience ? spin_limit : kMostPatience) + 64u * (unsigned)steps, sum = so_far + tile;
+    return sum < kMostPatience ? sum : kMostPatience;
+}
+
 cudaError_t expert_product_launch(const ExpertArgs &a, cudaStream_t st);
 
 }  // namespace moe

@@ -58,3 +58,24 @@ def test_the_products_give_up_report_and_recover(counts, polls):
     for g, w in zip(got[1] + got[2], want[1] + want[2]):
         assert torch.equal(g, w)
     r.close()
+
+
+def test_a_wait_through_other_tiles_is_no_reason_to_give_up():
+    """Segments that end with a whole K = 16 and one at the end that does not, with polls for single tiles: the second CTA of every pair
+    waits through all of its tiles."""
+    P, M, N = 48, 1024, 2304
+    counts = [2048] * (P - 1) + [2041]
+    r = U.make_router(P)
+    assert B.moe_set_tuning(r._ctx, B.MOE_TUNE_SPIN_LIMIT, 4000) == B.MOE_OK
+    n_, off, n = U.layout(counts)
+    dy, a = U.bf16(n, M, seed=1), U.bf16(n, N, seed=2)
+    got = [r.expert_weight_backward(dy, a, n_, off, dtype=t) for t in (torch.float32, torch.bfloat16)]
+    torch.cuda.synchronize()
+    assert r.device_status() == 0
+    for p in (0, P - 2, P - 1):
+        s = slice(2048 * p, 2048 * p + counts[p])
+        left, right = dy[s].double(), a[s].double()
+        want, bound = left.T @ right, U.sum_bound(counts[p], left.abs().T @ right.abs())
+        for g in got:
+            U.within(g[p], want, (1 + U.HALF[g.dtype]) * bound + U.HALF[g.dtype] * want.abs())
+    r.close()
