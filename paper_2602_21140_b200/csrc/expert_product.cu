@@ -749,7 +749,7 @@ k_expert_product(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                 const int cols = kGrad ? min(NT, p.N - t.col) : t.rows, steps = ((kGrad ? t.rows : p.K) + kStageK - 1) / kStageK;
                 const int each = acc_steps<OP, FINE>(steps);
                 const auto wait_acc = [&] {
-                    // a stage takes 512 clocks, a poll 20 or more: a long sum is no reason to give up
+                    // a stage takes 512 clocks, a poll 39 or more: a long sum is no reason to give up
                     ok = __all_sync(0xffffffffu, wait_for(&acc_full[buf], acc_parity, quit, p.spin_limit + 64u * each));
                     tc_fence_after();
                     return ok;

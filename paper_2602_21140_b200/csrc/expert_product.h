@@ -52,8 +52,9 @@ inline bool weight_grad_fits(long long rows, long long m, long long n, int P)
 }
 
 // Polls allowed to a wait that lasts through several tiles: `so_far`, and for one more of `steps` stages what a role that works on it
-// is allowed for the tile and its stages (a stage takes 512 clocks, a poll 20 or more).  Bounded, and without overflow.
-constexpr unsigned kMostPatience = 1u << 30;
+// is allowed for the tile and its stages (512 clocks a stage; a poll takes 39 clocks at least, and 7800 where the hardware waits
+// for the barrier as long as it does).  Bounded, by a minute of the longer polls, and without overflow.
+constexpr unsigned kMostPatience = 1u << 24;
 __host__ __device__ inline unsigned more_patience(unsigned so_far, unsigned spin_limit, int steps)
 {
     const unsigned tile = (spin_limit < kMostPatience ? spin_limit : kMostPatience) + 64u * (unsigned)steps, sum = so_far + tile;

@@ -5,11 +5,12 @@ import re
 from test_drains import _code
 from test_network_refusals import _printed
 
-MOST = 1 << 30
+MOST = 1 << 24
 
 
 def test_polls_grow_with_what_is_waited_for_and_stay_bounded(tmp_path):
     calls = [(0, 2000, 0), (0, 2000, 17), (5000, 2000, 17), (0, 0, 1), (0, 1 << 20, 1 << 24), (MOST, (1 << 31) - 1, 1 << 24), (MOST - 1, 0, 1), (7, (1 << 31) - 1, 0)]
+    assert MOST * 4e-6 < 100                                   # seconds: a poll takes 7800 clocks at most
     got = _printed(tmp_path, "expert_product.h", [f"more_patience({a}u, {b}u, {c})" for a, b, c in calls])
     assert got == [min(MOST, a + min(b, MOST) + 64 * c) for a, b, c in calls]
 
