@@ -278,22 +278,12 @@ __device__ __forceinline__ void clear_tail(unsigned char *stage, int bytes, int 
     __syncwarp();
 }
 
-// Tells the roles of both CTAs to leave.  (The other CTA is there: neither passes the last cluster_sync alone.)
-__device__ __forceinline__ void give_up(volatile int *quit)
-{
-    *quit = 1;
-    asm volatile("{\n\t.reg .u32 a;\n\tmapa.shared::cluster.u32 a, %0, %1;\n\tst.shared::cluster.u32 [a], %2;\n\t}" ::"r"(
-                     smem_addr(const_cast<int *>(quit))),
-                 "r"(cluster_rank() ^ 1u), "r"(1)
-                 : "memory");
-}
-
 // Bounded wait.  `quit` is shared by the CTA: the first role that gives up sets it in both, the others follow.
 __device__ __forceinline__ bool wait_for(uint64_t *bar, unsigned parity, volatile int *quit, unsigned limit)
 {
     unsigned spins = 0;
     while (!mbar_try_wait(bar, parity)) {
-        if (++spins > limit || ((spins & 63u) == 0 && *quit)) { give_up(quit); return false; }
+        if (++spins > limit || ((spins & 63u) == 0 && *quit)) { give_up<CG>(quit); return false; }
     }
     return true;
 }
@@ -714,7 +704,7 @@ k_expert_product(const __grid_constant__ CUtensorMap map_a, const __grid_constan
     // would be reported and no tile touched.)
     constexpr uint32_t tmem = 0;
     const bool whole = *tmem_slot == 0;
-    if (tid == 0 && !whole) give_up(quit);
+    if (tid == 0 && !whole) give_up<CG>(quit);
     if (!kGrad) {
         tiles = ends[p.P - 1];
         // counts that no dispatch writes: nothing is touched

@@ -236,12 +236,13 @@ struct Layout {
     static size_t bytes(int P) { return 1024 + kEndsOff + (size_t)P * (P <= kFullTableP ? 16 : 4); }
 };
 
-// Bounded wait.  `quit` is shared by the CTA: the first role that gives up sets it, the others follow.
+// Bounded wait.  `quit` is shared by the CTA: the first role that gives up sets it (in both CTAs of a pair), the others follow.
+template <int CG>
 __device__ __forceinline__ bool wait_for(uint64_t *bar, unsigned parity, volatile int *quit, unsigned limit)
 {
     unsigned spins = 0;
     while (!mbar_try_wait(bar, parity)) {
-        if (++spins > limit || ((spins & 63u) == 0 && *quit)) { *quit = 1; return false; }
+        if (++spins > limit || ((spins & 63u) == 0 && *quit)) { give_up<CG>(quit); return false; }
     }
     return true;
 }
@@ -485,7 +486,7 @@ k_mx_product(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
     // would be reported and no tile touched.)
     constexpr uint32_t tmem = 0;
     const bool whole = *tmem_slot == 0;
-    if (tid == 0 && !whole) *quit = 1;
+    if (tid == 0 && !whole) give_up<CG>(quit);
     const int n_many = merge ? many[p.P - 1] : 0, n_all = tiles_sum(ends[p.P - 1], n_many);
     Order order = {many, ends, merge ? segments : nullptr, 0u};
     if (n_many == n_all) order.one = many;                     // only that kind
@@ -503,8 +504,9 @@ k_mx_product(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
     // take is uniform over the warp, and issue from one elected lane.  (Behind a plain `lane == 0` the
     // compiler cannot know that one lane is left and serialises every such instruction over the warp: 80
     // cycles each, 700-1300 per stage, which bound the whole kernel.)
+    int issued = 0;                                            // stages that this warp has asked for
     if (warp == kTmaWarp) {
-        int issued = 0, s = 0;
+        int s = 0;
         const uint32_t lead = lead_addr<CG>(full);
         unsigned parity = 1;                                   // a fresh barrier passes the wait for parity 1
         bool ok = true;
@@ -516,7 +518,7 @@ k_mx_product(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
             const int loads = big ? 1 : (half + kBox - 1) / kBox;
             const uint32_t bytes = CG * (kATile + (big ? kBig : loads * kBox) * kRowBytes);
             for (int k = 0; k < steps; ++k) {
-                ok = __all_sync(0xffffffffu, wait_for(&empty[s], parity, quit, p.spin_limit));
+                ok = __all_sync(0xffffffffu, wait_for<CG>(&empty[s], parity, quit, p.spin_limit));
                 if (!ok) break;
                 unsigned char *a = stage + s * L::kStage, *b = a + kATile;
                 if (elect_one()) {
@@ -534,12 +536,6 @@ k_mx_product(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
                 if (++s == STAGES) { s = 0; parity ^= 1u; }
             }
         }
-        if (!ok) {
-            // loads in flight still land in this CTA's shared memory: a bounded wait for them (their barriers also
-            // count the scales, or are the other CTA's, so they may not complete, but the wait outlasts any copy)
-            unsigned long long until = 0;
-            for (int m = max(0, issued - STAGES); m < issued; ++m) drain_wait(&full[m % STAGES], (unsigned)(m / STAGES) & 1u, until);
-        }
     } else if (warp == kMmaWarp && rank == 0) {
         int s = 0, buf = 0;
         unsigned parity = 0, acc_parity = 1, step_no = 0;
@@ -547,7 +543,7 @@ k_mx_product(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
         const uint64_t stage_desc = desc_codes(smem_addr(stage)), sf_desc = desc_scales(smem_addr(sf));
         Tile t;
         for (TileStream<NT, CG> stream(p, order, tiles); ok && next_uniform(stream, t);) {
-            ok = __all_sync(0xffffffffu, wait_for(&acc_empty[buf], acc_parity, quit, p.spin_limit));
+            ok = __all_sync(0xffffffffu, wait_for<CG>(&acc_empty[buf], acc_parity, quit, p.spin_limit));
             if (!ok) break;
             tc_fence_after();
             const uint32_t d = tmem + buf * NT;
@@ -556,7 +552,7 @@ k_mx_product(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
             bool ready = __all_sync(0xffffffffu, mbar_test_wait(&full[s], parity));
             for (int k = 0; k < steps; ++k, ++step_no) {
                 if (!ready) {
-                    ok = __all_sync(0xffffffffu, wait_for(&full[s], parity, quit, p.spin_limit));
+                    ok = __all_sync(0xffffffffu, wait_for<CG>(&full[s], parity, quit, p.spin_limit));
                     if (!ok) break;
                 }
                 tc_fence_after();
@@ -665,8 +661,8 @@ k_mx_product(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
                 const bool two = at * 2 + 1 < steps;
                 const int s1 = s + 1 == STAGES ? 0 : s + 1;
                 const unsigned parity1 = s1 ? parity : parity ^ 1u;
-                ok = wait_for(&empty[s], parity, quit, p.spin_limit);
-                ok = __all_sync(0xffffffffu, ok && (!two || wait_for(&empty[s1], parity1, quit, p.spin_limit)));
+                ok = wait_for<CG>(&empty[s], parity, quit, p.spin_limit);
+                ok = __all_sync(0xffffffffu, ok && (!two || wait_for<CG>(&empty[s1], parity1, quit, p.spin_limit)));
                 if (!ok) break;
                 const int off = (blk == 0 ? 0 : L::kSfA + (blk - 1) * 512) + lane * 16;
                 const int next = blk == 0 ? 512 : L::kRB * 512;
@@ -699,7 +695,7 @@ k_mx_product(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
         unsigned acc_parity = 0;
         Tile t;
         for (TileStream<NT, CG> stream(p, order, tiles); stream.next(t);) {
-            bool ok = wait_for(&acc_full[buf], acc_parity, quit, p.spin_limit);
+            bool ok = wait_for<CG>(&acc_full[buf], acc_parity, quit, p.spin_limit);
             ok = GATED ? warps_all(group + 1, 128, ok) : warps_all((warp >> 1) + 1, 64, ok);   // they meet at barriers below
             if (!ok) break;
             tc_fence_after();
@@ -731,7 +727,17 @@ k_mx_product(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ 
     tc_fence_before();
     if (CG == 2) cluster_sync();                               // the pair leaves together: neither arrives on a CTA that is gone
     else __syncthreads();
-    if (tid == 0 && *quit) report_status(p.ctl, kDevTimeout);
+    if (*quit) {                                               // in both CTAs of a pair or in none
+        // Whichever role gave up, loads may be in flight to this CTA's shared memory: a bounded wait for them (their barriers also
+        // count the scales, or are the other CTA's, so they may not complete, but the wait outlasts any copy)
+        if (warp == kTmaWarp) {
+            unsigned long long until = 0;
+            for (int m = max(0, issued - STAGES); m < issued; ++m) drain_wait(&full[m % STAGES], (unsigned)(m / STAGES) & 1u, until);
+        }
+        __syncwarp();
+        if (CG == 2) cluster_sync();
+        if (tid == 0) report_status(p.ctl, kDevTimeout);
+    }
     if (warp == kMmaWarp) {
         if (CG == 2 && rank == 1) {                            // the first CTA's last arrival is on its way here as well
             unsigned long long until = 0;

@@ -113,6 +113,19 @@ __device__ __forceinline__ void cluster_sync()
     asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
 }
 
+// Tells the roles of a CTA, or of both CTAs of a pair, to leave.  (The other CTA is there: neither passes the last cluster_sync
+// alone.)
+template <int CG>
+__device__ __forceinline__ void give_up(volatile int *quit)
+{
+    *quit = 1;
+    if (CG == 2)
+        asm volatile("{\n\t.reg .u32 a;\n\tmapa.shared::cluster.u32 a, %0, %1;\n\tst.shared::cluster.u32 [a], %2;\n\t}" ::"r"(
+                         smem_addr(const_cast<int *>(quit))),
+                     "r"(cluster_rank() ^ 1u), "r"(1)
+                     : "memory");
+}
+
 // Tile loads into this CTA's shared memory; `bar` is a lead_addr.
 template <int CG>
 __device__ __forceinline__ void tma_2d(void *dst, const CUtensorMap *map, int x, int y, uint32_t bar)

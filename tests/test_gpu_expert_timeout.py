@@ -83,3 +83,32 @@ def test_a_wait_through_other_tiles_is_no_reason_to_give_up():
         for g in got:
             U.within(g[p], want, (1 + U.HALF[g.dtype]) * bound + U.HALF[g.dtype] * want.abs())
     r.close()
+
+
+@pytest.mark.parametrize("slots,rows", [(32, 40), (4, 2000)], ids=["single CTAs", "pairs"])
+def test_the_products_on_4_bit_rows_give_up_and_recover(slots, rows):
+    """The gated product's epilogue outlasts a poll at a K of 64; whether a wait runs out is the hardware's to say."""
+    H, I = 64, 4096
+    r = U.make_router(slots)
+    n_, off, n = U.layout([rows] * slots)
+    a = B.mx_quantize(U.bf16(n, H, seed=1))
+    gate_up, down = B.mx_quantize(U.bf16(slots, 2 * I, H, seed=2, scale=H ** -0.5)), B.mx_quantize(U.bf16(slots, H, I, seed=3, scale=I ** -0.5))
+
+    def run():
+        y = torch.full((n + 128, H), -7.0, dtype=torch.bfloat16, device="cuda")
+        h = r.mx_expert_gated(a, n_, off, gate_up)
+        r.mx_expert_product(h, n_, off, down, y[64:64 + n])
+        torch.cuda.synchronize()
+        return h.codes, h.scales[:, :I // 32].clone(), y
+
+    want = run()
+    assert r.device_status() == 0
+    assert B.moe_set_tuning(r._ctx, B.MOE_TUNE_SPIN_LIMIT, 0) == B.MOE_OK
+    for _ in range(3):
+        y = run()[2]
+        assert (y[:64] == -7).all() and (y[-64:] == -7).all()
+        assert r.device_status() in (0, B.MOE_ERR_DEVICE_TIMEOUT)
+    assert B.moe_set_tuning(r._ctx, B.MOE_TUNE_SPIN_LIMIT, -1) == B.MOE_OK
+    got = run()
+    assert r.device_status() == 0 and all(torch.equal(g, w) for g, w in zip(got, want))
+    r.close()

@@ -6,7 +6,7 @@ import pytest
 
 from test_drains import _code
 
-PAIRS = ["expert_product.cu"]
+PAIRS = ["expert_product.cu", "mx_product.cu"]
 
 
 def _function(code, name):
@@ -18,20 +18,20 @@ def _function(code, name):
 def test_whoever_gives_up_tells_both_ctas(name):
     code = _code(name)
     wait = _function(code, "bool wait_for(")
-    assert re.search(r"give_up\(quit\);\s*return false", wait) and "*quit = 1" not in wait
-    told = _function(code, "void give_up(")
+    assert re.search(r"give_up<CG>\(quit\);\s*return false", wait)
+    told = _function(_code("tcgen05.cuh"), "void give_up(")
     assert "*quit = 1" in told and "mapa.shared::cluster" in told and "st.shared::cluster" in told and "cluster_rank() ^ 1u" in told
     # nobody sets the flag in another way
-    assert len(re.findall(r"\*quit = 1", code)) == 1 and len(re.findall(r"\*quit = 0", code)) == 1
+    assert "*quit = 1" not in code and len(re.findall(r"\*quit = 0", code)) == 1
 
 
 @pytest.mark.parametrize("name", PAIRS)
 def test_both_ctas_stay_until_copies_have_landed(name):
     code = _code(name)
-    end = code[code.rindex("tc_fence_before();\n    cluster_sync();"):]
+    end = code[max(code.rindex("tc_fence_before();\n    " + meet) for meet in ("cluster_sync();", "if (CG == 2) cluster_sync();") if "tc_fence_before();\n    " + meet in code):]
     end = end[:end.index("tmem_dealloc")]
     # the verdict is read behind the meeting of the pair, so it is the same in both
-    m = re.search(r"cluster_sync\(\);\s*if \(\*quit\) \{(.*?)\n    \}\n", end, re.S)
+    m = re.search(r"(?:cluster_sync|__syncthreads)\(\);\s*if \(\*quit\) \{(.*?)\n    \}\n", end, re.S)
     assert m, end
     body = m.group(1)
     assert re.search(r"warp == kTmaWarp.*drain_wait\(&full\[", body, re.S)
