@@ -268,7 +268,8 @@ __device__ __forceinline__ void load_grad(unsigned char *a, unsigned char *b, co
 }
 
 // The lines of a stage behind a segment, up to a whole K = 16, are made zero in both operands: they hold the next segment's rows
-// (and a NaN there times a zero would still be one).  A line is 128 bytes of one k in each of the stage's chunks.
+// (and a NaN there times a zero would still be one).  A line is 128 bytes of one k in each of the stage's chunks.  In the CTA whose
+// thread issues the MMAs by that thread's warp:
 __device__ __forceinline__ void clear_tail(unsigned char *stage, int bytes, int left, int lane)
 {
     unsigned char *lines = stage + (lane & 7) * 16;
@@ -276,6 +277,27 @@ __device__ __forceinline__ void clear_tail(unsigned char *stage, int bytes, int 
         for (int q = (lane >> 3) * kChunk; q < bytes; q += 4 * kChunk) *reinterpret_cast<uint4 *>(lines + q + i * kLine) = make_uint4(0u, 0u, 0u, 0u);
     fence_async_shared();
     __syncwarp();
+}
+
+// In the other one by loads of zeros, of lines beyond the rows, which count their bytes at `bar` of the first CTA.  (Stores and an
+// arrival there would need a release of cluster scope, 1500 clocks of it: the CTAs' shared memory is read by the first one's MMAs,
+// and what orders a load's bytes for them is the barrier that every stage has.  128 x 511 rows, 2048 x 4096: 931 us; with an arrival
+// that nothing orders 904, with the release 1488 for 1054 in an earlier state.)
+struct ZeroMaps {
+    CUtensorMap lines[4];                                      // boxes of 1, 2, 4 and 8 lines
+};
+constexpr int kTailChunks = (kFeat + NT / CG) / 64;            // of a stage
+__device__ __forceinline__ int tail_lines(int left) { return 16 - (left & 15); }
+__device__ __forceinline__ void load_zero_tail(unsigned char *stage, int left, const ZeroMaps &zeros, int beyond, uint32_t bar)
+{
+    int at = left;
+#pragma unroll
+    for (int b = 0; b < 4; ++b)
+        if (tail_lines(left) & (1 << b)) {
+#pragma unroll
+            for (int q = 0; q < kTailChunks; ++q) tma_2d<CG>(stage + q * kChunk + at * kLine, &zeros.lines[b], 0, beyond, bar);
+            at += 1 << b;
+        }
 }
 
 // Bounded wait.  `quit` is shared by the CTA: the first role that gives up sets it in both, the others follow.
@@ -620,9 +642,10 @@ __device__ __forceinline__ void store_box(const CUtensorMap *map, int slot, int 
 template <ExpertOp OP, bool FINE, bool F32>
 __global__ void __launch_bounds__(kThreadsOf<FINE>, 1)
 k_expert_product(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_big,
-                 const __grid_constant__ CUtensorMap map_y, const KernelParams p)
+                 const __grid_constant__ CUtensorMap map_y, const __grid_constant__ ZeroMaps zeros, const KernelParams p)
 {
-    // map_a: the M operand (weights, or the left operand of a weight gradient); map_b, map_big: the N operand
+    // map_a: the M operand (weights, or the left operand of a weight gradient); map_b, map_big: the N operand; map_y, zeros: of a
+    // weight gradient
     using L = Layout<OP, FINE>;
     constexpr bool kGrad = L::kGrad;
     constexpr int kBox = 32;                                   // rows per TMA load of few rows
@@ -952,7 +975,9 @@ k_expert_product(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                         const int left = t.rows - k * kStageK;     // of a weight gradient
                         if (kGrad && has_tail(left)) {
                             clear_tail(stage + s * stage_bytes, stage_bytes, left, lane);
-                            // so has the second CTA
+                            // and the second CTA's
+                            if (elect_one()) mbar_expect_tx(&peer[s], (unsigned)(kTailChunks * tail_lines(left) * kLine));
+                            __syncwarp();
                             ok = __all_sync(0xffffffffu, wait_for(&peer[s], (peer_parity >> s) & 1u, quit, p.spin_limit));
                             if (!ok) break;
                             peer_parity ^= 1u << s;
@@ -984,9 +1009,8 @@ k_expert_product(const __grid_constant__ CUtensorMap map_a, const __grid_constan
             unsigned long long until = 0;
             drain_wait(drained, 0, until);
         } else if (warp == kMmaWarp && kGrad) {
-            // The second CTA of a pair: its share of the stages that end a segment within a K = 16 (see clear_tail), announced to the
-            // first one, whose thread issues the MMA that reads these lines, as in mbar_arrive_lead.  (With a release of cluster scope:
-            // 128 x 511 rows 1488 us instead of 1054; such an arrival on every stage: 510 TFLOP/s.)
+            // The second CTA of a pair: its share of the stages that end a segment within a K = 16 (see load_zero_tail), once
+            // its own bytes of them are there.  (Such a step on every stage: 510 TFLOP/s.)
             int s = 0;
             unsigned tail_parity = 0;                              // a bit per stage, of its next use
             unsigned patience = 0;                                 // a wait begins while the tiles without such an end before it are worked on
@@ -1001,8 +1025,8 @@ k_expert_product(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                     if (!ok) break;
                     patience = 0;
                     tail_parity ^= 1u << at;
-                    clear_tail(stage + at * stage_bytes, stage_bytes, left, lane);
-                    if (lane == 0) mbar_arrive_lead<CG>(&peer[at]);
+                    if (elect_one()) load_zero_tail(stage + at * stage_bytes, left, zeros, (int)p.rows, lead_addr<CG>(&peer[at]));
+                    __syncwarp();
                 }
                 s = (s + steps) % stages;
             }
@@ -1053,11 +1077,13 @@ cudaError_t launch(const ExpertArgs &a, cudaStream_t st)
     const CUtensorMapDataType bf16 = CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
     const CUtensorMapSwizzle sw = CU_TENSOR_MAP_SWIZZLE_128B;
     CUtensorMap map_a, map_b, map_big = {}, map_y = {};
+    ZeroMaps zeros = {};
     bool ok;
     if (L::kGrad) {
         const cuuint64_t ad[2] = {(cuuint64_t)a.M, (cuuint64_t)a.rows}, as[1] = {2 * (cuuint64_t)a.M};
         const cuuint64_t bd[2] = {(cuuint64_t)a.N, (cuuint64_t)a.rows}, bs[1] = {2 * (cuuint64_t)a.N};
         ok = encode(&map_a, bf16, sw, a.a, 2, ad, as, 64, kStageK) && encode(&map_b, bf16, sw, a.b, 2, bd, bs, 64, kStageK);
+        for (int b = 0; b < 4; ++b) ok = ok && encode(&zeros.lines[b], bf16, CU_TENSOR_MAP_SWIZZLE_NONE, a.a, 2, ad, as, 64, 1 << b);
         if (!F32) {
             const cuuint64_t yd[3] = {(cuuint64_t)a.N, (cuuint64_t)a.M, (cuuint64_t)a.P}, ys[2] = {2 * (cuuint64_t)a.N, 2 * (cuuint64_t)a.N * a.M};
             ok = ok && encode(&map_y, bf16, sw, a.y, 3, yd, ys, 64, 32);
@@ -1092,7 +1118,7 @@ cudaError_t launch(const ExpertArgs &a, cudaStream_t st)
     at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at; cfg.numAttrs = a.pdl ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, kernel, map_a, map_b, map_big, map_y, p);
+    return cudaLaunchKernelEx(&cfg, kernel, map_a, map_b, map_big, map_y, zeros, p);
 }
 
 }  // namespace
