@@ -6,8 +6,8 @@
 // Quantising a block of 32 values x with largest magnitude a:
 //   s = the smallest of 0 .. 254 with a <= 448 * 2^(s - 127)     (a NaN or infinity gives 255 and codes 0)
 //   code = nearest code of x * 2^(127 - s), ties to even
-// so nothing saturates, and a block uses the top binade of the codes: x is off by at most 2^-4 of itself, or 2^-10 of 2^-6
-// of the scale.  (The 4-bit format lets the block's largest values saturate instead; here that would cost up to an eighth of a
+// so nothing saturates, and a block uses the top binade of the codes: x is off by at most 2^-4 of itself, or 2^-10 of the scale where
+// that is more (below 2^-6 of the scale the codes are multiples of 2^-9 of it, so what is below 2^-10 of it becomes 0).  (The 4-bit format lets the block's largest values saturate instead; here that would cost up to an eighth of a
 // gradient's largest terms.)  The product with a power of two is exact, so the only rounding is the one to 8 bits.
 #pragma once
 
