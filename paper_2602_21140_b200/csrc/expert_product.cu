@@ -547,12 +547,13 @@ __device__ __forceinline__ void store_gated_backward(const KernelParams &p, cons
 
 // Stages of each of a tile's accumulators.  Where sums are given in fp32 (FINE: the weight gradient) or rounded to 8 bits (the
 // gated product), a long sum goes on in another accumulator, and the epilogue adds them up in registers: the tensor core cuts
-// off what it adds, which shrinks a sum by some 2e-8 of itself with each K = 16, 1.0e-6 after 1024 and 1.6e-5 after 16384.  With
-// 960 at a time fp32 gradients are within 1e-6 of their magnitude.  With 1024 at a time one in 25000 of the 8-bit codes falls the
-// other way, whatever the length (one in 5000 with K = 7168 in one accumulator; one in 33000 with a chain of fp32 additions, and
-// one in 100000 with K = 1024).  Shorter pieces keep the epilogue, which has to add before it can store, from running under
-// the products: two and three for K of 1024 and 2048 take 15 % more time, 512 throughout 8-26 %.  A sum that is rounded to
-// bf16 needs no such care.
+// off what it adds, up to a unit in the last place with each K = 16 and more where products are 2^10 below the sum.  Gradients of
+// mixed signs (norm of the error by the norm; of one sign in brackets) are off by 1.0e-6 (2.2e-6) after 1024 in one accumulator and
+// by 1.9e-5 (8.2e-5) after 16384; with 960 at a time by 0.9e-6 (2.0e-6) whatever the length; a chain of fp32 additions by 2e-7 to 4e-7.
+// With 1024 at a time one in 25000 of the 8-bit codes falls the other way, whatever the length (one in 3400 with K = 7168 in one
+// accumulator; one in 28000 with fp32 additions, and one in 31000 and 115000 with K = 1024).  Shorter pieces keep the epilogue, which
+// has to add before it can store, from running under the products: two and three for K of 1024 and 2048 take 15 % more time, 512
+// throughout 8-26 %.  A sum that is rounded to bf16 needs no such care.
 constexpr int kGradSteps = 960 / kStageK;
 template <ExpertOp OP> constexpr int kMostSteps = OP == ExpertOp::kWeightGrad ? kGradSteps : 1024 / kStageK;
 template <ExpertOp OP, bool FINE>
