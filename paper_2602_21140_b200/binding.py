@@ -549,24 +549,33 @@ def _is_mx(m: MxRows, index: int, lead=None) -> bool:
 
 
 def _span(t: torch.Tensor):
-    at = t.data_ptr()
-    return at, at + t.numel() * t.element_size()
+    """Address and bytes of a contiguous tensor, none where there is no tensor."""
+    return (0, 0) if t is None else (t.data_ptr(), t.numel() * t.element_size())
 
 
 def _apart(outputs, inputs) -> bool:
-    """Whether contiguous output tensors (None: not given) share no byte with inputs or with one another.  (One without elements has none.)"""
-    taken = [_span(t) for t in inputs if t is not None and t.numel()]
-    for t in outputs:
-        if t is not None and t.numel():
-            at, end = _span(t)
-            if any(at < e and b < end for b, e in taken):
-                return False
-            taken.append((at, end))
+    """Whether outputs share no byte with inputs or with one another, each given by its address and its bytes."""
+    spans = [(at, at + size, True) for at, size in outputs if size]
+    if not spans:
+        return True
+    spans += [(at, at + size, False) for at, size in inputs if size]
+    spans.sort()
+    any_end = out_end = 0                                      # of those that begin before
+    for at, end, out in spans:
+        if at < out_end or (out and at < any_end):
+            return False
+        if end > any_end:
+            any_end = end
+        if out and end > out_end:
+            out_end = end
     return True
 
 
-def _aligned16(*tensors) -> bool:
-    return not any(t is not None and t.data_ptr() & 15 for t in tensors)
+def _aligned16(*addresses) -> bool:
+    together = 0
+    for a in addresses:
+        together |= a
+    return together & 15 == 0
 
 
 @functools.lru_cache(maxsize=256)
@@ -909,10 +918,14 @@ class MoeRouter:
                 return False
         return True
 
-    @staticmethod
-    def _index_buffers(out: DispatchBuffers):
-        return (out.topk_ids, out.topk_weights, out.topk_slot, out.slot_counts, out.slot_offsets, out.rank_counts, out.rank_offsets, out.dst_row,
-                out.src_index)
+    def _index_spans(self, out: DispatchBuffers, T: int):
+        """What a dispatch of T tokens uses of its index buffers."""
+        c = self.cfg
+        R, n = 4 * c.num_ranks, 4 * T * c.top_k
+        P = R * c.slots_per_rank
+        return [(out.topk_ids.data_ptr(), n), (out.topk_weights.data_ptr(), n), (out.topk_slot.data_ptr(), n), (out.slot_counts.data_ptr(), P),
+                (out.slot_offsets.data_ptr(), P + 4), (out.rank_counts.data_ptr(), R), (out.rank_offsets.data_ptr(), R + 4),
+                (out.dst_row.data_ptr(), n), (out.src_index.data_ptr(), n)]
 
     def _segments_ok(self, rows: MxRows, slot_counts, slot_offsets, weight: MxRows, dev: int) -> bool:
         P, w = self.num_slots, weight.codes.shape
@@ -1056,8 +1069,8 @@ class MoeRouter:
         return _is_mx8(z, dev, (n, cols)) if isinstance(z, Mx8Rows) else _is_dense(z, torch.bfloat16, (n, cols), dev)
 
     @staticmethod
-    def _kept_tensors(z):
-        return (z.codes, z.scales) if isinstance(z, Mx8Rows) else (z,)
+    def _kept_spans(z):
+        return [_span(z.codes), _span(z.scales)] if isinstance(z, Mx8Rows) else [_span(z)]
 
     @staticmethod
     def _kept_ptrs(z):
@@ -1112,15 +1125,26 @@ class MoeRouter:
         st = _network_status(n, n_in, cols, n_out, P)
         if st != MOE_OK:
             raise MoeError(st, "expert_ffn")
-        kept, read = self._kept_tensors(z), (gate_up, down, slot_counts, slot_offsets)
-        _require(n == 0 or (_aligned16(rows, gate_up, down, y, h, *kept)
-                            and ((z is None and h is None) or _apart((h, *kept), (rows, *read)))
-                            and (y is None or _apart((y,), (h, *kept, *read)))), "expert_ffn")
+        if n:
+            r_ptr, g_ptr, d_ptr = rows.data_ptr(), gate_up.data_ptr(), down.data_ptr()
+            ok = (r_ptr | g_ptr | d_ptr) & 15 == 0
+            if y is not None or h is not None or z is not None:
+                kept, h_span, y_span = self._kept_spans(z), _span(h), _span(y)
+                ok = (ok and _aligned16(h_span[0], y_span[0], *[at for at, _ in kept])
+                      and _apart((y_span, h_span, *kept), ((g_ptr, P * cols * n_in * 2), (d_ptr, P * n_out * n_hidden * 2),
+                                                           (slot_counts.data_ptr(), 4 * P), (slot_offsets.data_ptr(), 4 * P)))
+                      and _apart((h_span, *kept), ((r_ptr, n * n_in * 2),)))
+            _require(ok, "expert_ffn")
+        return self._expert_ffn(rows, slot_counts, slot_offsets, gate_up, down, y, h, z)
+
+    def _expert_ffn(self, rows, slot_counts, slot_offsets, gate_up, down, y, h, z) -> torch.Tensor:
+        """expert_ffn of arguments that have been looked at."""
+        n, (_, cols, n_in), n_out, n_hidden = rows.shape[0], gate_up.shape, down.shape[1], gate_up.shape[1] // 2
         if h is None:
             h = rows.new_empty((n, n_hidden))
         if y is None:
             y = torch.empty_like(rows) if n_out == n_in else rows.new_empty((n, n_out))
-        counts, offsets, stream = slot_counts.data_ptr(), slot_offsets.data_ptr(), _raw_stream(dev)
+        counts, offsets, stream = slot_counts.data_ptr(), slot_offsets.data_ptr(), _raw_stream(self._index())
         st = moe_expert_gated(self._ctx, rows.data_ptr(), n, counts, offsets, gate_up.data_ptr(), n_hidden, n_in, h.data_ptr(),
                               *self._kept_ptrs(z), stream)
         if st == MOE_OK:
@@ -1194,7 +1218,8 @@ class MoeRouter:
         P, cols, n_in = gate_up.shape if gate_up.dim() == 3 else (0, 0, 0)
         n_out, n_hidden = down.shape[1] if down.dim() == 3 else 0, cols // 2
         apart = ((d_rows is None and d_gate_up is None and d_down is None)
-                 or _apart((d_rows, d_gate_up, d_down), (dy, rows, gate_up, down, slot_counts, slot_offsets, *self._kept_tensors(z))))
+                 or _apart((_span(d_rows), _span(d_gate_up), _span(d_down)),
+                           (*[_span(t) for t in (dy, rows, gate_up, down, slot_counts, slot_offsets)], *self._kept_spans(z))))
         add_ok = not add or (d_gate_up is not None and d_down is not None and d_gate_up.dtype is f32 and d_down.dtype is f32)
         if d_gate_up is None:
             d_gate_up = torch.empty_like(gate_up, dtype=grad_dtype) if grad_dtype is not bf16 else torch.empty_like(gate_up)
@@ -1210,8 +1235,9 @@ class MoeRouter:
         st = _network_status(n, n_in, cols, n_out, P, True)
         if st != MOE_OK:
             raise MoeError(st, "expert_ffn_backward")
-        _require(_aligned16(d_gate_up, d_down) and (n == 0 or _aligned16(dy, rows, gate_up, down, d_rows, *self._kept_tensors(z))),
-                 "expert_ffn_backward")
+        _require(_aligned16(d_gate_up.data_ptr(), d_down.data_ptr())
+                 and (n == 0 or _aligned16(dy.data_ptr(), rows.data_ptr(), gate_up.data_ptr(), down.data_ptr(), 0 if d_rows is None else d_rows.data_ptr(),
+                                           *self._kept_ptrs(z))), "expert_ffn_backward")
         if d_rows is None:
             d_rows = torch.empty_like(rows)
         dz, h = dy.new_empty((n, cols)), dy.new_empty((n, n_hidden))
@@ -1253,14 +1279,16 @@ class MoeRouter:
         st = _network_status(T * k, H, gate_up.shape[1], H, self.num_slots)
         if st != MOE_OK:
             raise MoeError(st, "expert_step")
-        kept = self._kept_tensors(z)
-        send, index = (None, ()) if out is None else (out.send_buf, self._index_buffers(out))
-        read = (logits, gate_up, down, *index)
-        _require(T == 0 or (_aligned16(gate_up, down, send, y, buf, *kept)
-                            and (z is None or _apart(kept, (x, send, *read))) and (buf is None or _apart((buf,), (x, *kept, *read)))
-                            and (y is None or _apart((y,), (buf, *kept, *read)))), "expert_step")
+        if T:
+            P, cols, _ = gate_up.shape
+            w = [(gate_up.data_ptr(), P * cols * H * 2), (down.data_ptr(), P * cols * H)]
+            kept, outs, send = self._kept_spans(z), [_span(y), _span(buf)], _span(None if out is None else out.send_buf)
+            _require(_aligned16(send[0], *[at for at, _ in (*w, *kept, *outs)])
+                     and ((y is None and buf is None and z is None)
+                          or (_apart((*outs, *kept), (*w, (logits.data_ptr(), T * self.cfg.num_experts * 4), *([] if out is None else self._index_spans(out, T))))
+                              and _apart(kept, (send,)) and _apart((outs[1], *kept), ((x.data_ptr(), T * H * 2),)))), "expert_step")
         out = _on_device(dev, self.dispatch, logits, x, out)
-        buf = self.expert_ffn(out.send_buf, out.slot_counts, out.slot_offsets, gate_up, down, buf, z=z)
+        buf = self._expert_ffn(out.send_buf, out.slot_counts, out.slot_offsets, gate_up, down, buf, None, z)
         return _on_device(dev, self.combine, buf, T, y)
 
     def expert_step_backward(self, logits: torch.Tensor, dy: torch.Tensor, rows: "torch.Tensor | Mx8Rows", out: DispatchBuffers,
@@ -1276,9 +1304,10 @@ class MoeRouter:
                  and self._networks_ok(gate_up, down) and _is_dense(dy, torch.bfloat16, (T, H), dev) and self._outputs_ok(out, T, dev)
                  and self._kept_ok(z, T * self.cfg.top_k, gate_up.shape[1], dev)
                  and (score != MOE_SCORE_SIGMOID if logits is None else _is_dense(logits, torch.float32, (T, E), dev))
-                 and (isinstance(rows, Mx8Rows) or _apart((buf,), (rows,)))
+                 and (isinstance(rows, Mx8Rows) or _apart((_span(buf),), (_span(rows),)))
                  and ((d_gate_up is None and d_down is None)
-                      or _apart((d_gate_up, d_down), (logits, dy, buf, *self._kept_tensors(rows), *self._index_buffers(out)))),
+                      or _apart((_span(d_gate_up), _span(d_down)),
+                                (_span(logits), _span(dy), _span(buf), *self._kept_spans(rows), *self._index_spans(out, T)))),
                  "expert_step_backward")
         d_buf, d_weights = self.combine_backward(buf, dy)
         if isinstance(rows, Mx8Rows):
