@@ -1037,6 +1037,7 @@ class MoeRouter:
         return dx, d_logits
 
     # -- experts in 16 bits and their gradients --------------------------------
+    # (Outside autograd, as all of the binding: results carry no graph, and gradients are calls of their own.)
     def redispatch(self, x8: Mx8Rows, send_buf: torch.Tensor | None = None) -> torch.Tensor:
         """The send buffer [T * k, H] of the latest dispatch once more, from its tokens' rows [T, H] in 8 bits."""
         c, dev = self.cfg, self._index()
