@@ -705,9 +705,15 @@ class RmsNormOut:
     h: torch.Tensor                  # x + residual, x itself without a residual
     rstd: torch.Tensor               # fp32, one per row
     y8: Mx8Rows | None = None        # the normed rows in 8 bits (a call that does not keep them leaves these as they were)
-    # An x that stands in h is the caller's and no later call's output: which one it is, and the buffer whose place it took.
+    # An x that a call put into h is the caller's and no later call's output, unless the caller puts it there: which one it
+    # is, and the buffer whose place it took.
     lent: torch.Tensor | None = field(default=None, repr=False, compare=False)
     own_h: torch.Tensor | None = field(default=None, repr=False, compare=False)
+
+    def __setattr__(self, name, value):
+        if name == "h":
+            self.__dict__["lent"] = None
+        self.__dict__[name] = value
 
 
 def _row_stride(t: torch.Tensor, cols: int) -> int:
@@ -721,7 +727,7 @@ def rms_norm(x: torch.Tensor, weight: torch.Tensor, residual: torch.Tensor | Non
              out: RmsNormOut | None = None) -> RmsNormOut:
     """Root-mean-square norm of ``x`` + ``residual`` ([..., cols], bf16 / fp16 / fp32) times ``weight`` (any of these types), on the
     current stream of its device.  ``keep``: also in 8 bits, for a backward pass.  ``out.h`` may be ``residual``
-    itself."""
+    itself, where the caller has put it there."""
     shape, dtype, index = x.shape, x.dtype, x.get_device()
     code, w_code = _DTYPE_CODE.get(dtype), _DTYPE_CODE.get(weight.dtype)
     _require(index >= 0 and code is not None and w_code is not None and len(shape) > 0 and shape[-1] > 0, "rms_norm")
@@ -739,7 +745,7 @@ def rms_norm(x: torch.Tensor, weight: torch.Tensor, residual: torch.Tensor | Non
         out = RmsNormOut(x.new_empty(shape) if like is None else torch.empty_like(like), None,
                          torch.empty(shape[:-1], dtype=torch.float32, device=x.device), y8)
     else:
-        h = out.h if out.lent is None or out.h is not out.lent else out.own_h
+        h = out.h if out.lent is None else out.own_h
         _require(_is_dense(out.y, dtype, shape, index) and (residual is None or h is None or _is_dense(h, dtype, shape, index))
                  and _is_dense(out.rstd, torch.float32, shape[:-1], index) and (not keep or _is_mx8(out.y8, index, shape)), "rms_norm")
     r_ptr, h_ptr = 0, 0
@@ -753,7 +759,8 @@ def rms_norm(x: torch.Tensor, weight: torch.Tensor, residual: torch.Tensor | Non
     if st != MOE_OK:
         raise MoeError(st, "moe_rms_norm")
     out.own_h = h
-    out.h, out.lent = (x, x) if residual is None else (h, None)
+    out.h = x if residual is None else h
+    out.lent = x if residual is None else None
     return out
 
 

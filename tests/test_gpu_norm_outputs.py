@@ -24,3 +24,14 @@ def test_rows_of_earlier_calls_stay(dtype):
         assert torch.equal(t, before)
     for (y, h), o in zip(got, want):
         assert torch.equal(y, o.y) and torch.equal(h, o.h)
+
+
+def test_h_in_the_residuals_place():
+    """As the caller says, also where the residual was the x of the call before."""
+    stream, branch, w = U.bf16(37, 256, seed=1), U.bf16(37, 256, seed=2), torch.ones(256, device="cuda")
+    want = (stream.float() + branch.float()).bfloat16()
+    out = B.rms_norm(stream, w)
+    out.h = stream
+    B.rms_norm(branch, w, stream, out=out)
+    torch.cuda.synchronize()
+    assert out.h is stream and torch.equal(stream, want)

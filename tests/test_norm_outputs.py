@@ -52,6 +52,21 @@ def test_a_given_buffer_for_h_outlives_a_call_without_a_residual(calls):
     assert out.h is res and calls[-1]["h"] == calls[-1]["res"] == res.data_ptr()
 
 
+def test_the_caller_may_put_the_same_rows_there(calls):
+    """h in the residual's place, where the residual is the x of the call before."""
+    stream, branch = Row((T, H), BF), Row((T, H), BF)
+    out = _norm(stream)
+    _norm(branch, stream, out=out)                             # not said: somewhere else
+    assert calls[-1]["h"] not in (stream.data_ptr(), branch.data_ptr())
+    out = _norm(stream)
+    out.h = stream
+    _norm(branch, stream, out=out)
+    assert calls[-1]["h"] == calls[-1]["res"] == stream.data_ptr() and out.h is stream
+    again = B.RmsNormOut(**vars(_norm(stream)))                # a copy knows it as well
+    _norm(branch, stream, out=again)
+    assert calls[-1]["h"] != stream.data_ptr()
+
+
 def test_the_stream_of_a_stack_of_layers(calls):
     """x of one call is the h of the one before."""
     x, res = Row((T, H), BF), Row((T, H), BF)
